@@ -1,0 +1,691 @@
+// Attention of few query rows over the 4-bit cache: single tokens, drafts, and every shape that kv_prompt.cu leaves.
+//
+//   o_i = sum_j w_ij v_j / sum_j w_ij,   w_ij = 2^(c q_i . k_j - m_i),   c = softmax_scale * k_scale * log2(e)
+//
+// in one pass over the keys with a running reference m_i.  The rows that share a key/value head - its query heads times
+// the new tokens - are the N dimension (8 a tile) of mma.sync.m16n8k16, 16 keys are M, so a key's codes are converted
+// once for all rows:
+//   S^T[16 keys, 8 rows]  = K[16 keys, W] Q^T          A operand: key rows, converted e2m1 -> f16, times their scales
+//   O^T[W, 8 rows]       += V^T[W, 16 keys] P^T        A operand: value columns; two keys' codes of a dimension are put
+//                                                      into one byte, so that one conversion makes an operand register
+// A value code times its scale has at most 6 significant bits: both operands are exact in f16.  Queries are scaled by a
+// power of two per row and are exact too (bf16), or are the sum of two f16 parts (fp32); so are the weights.
+//
+// Bound by the cache's bytes (9/8 W a key and head for K and V together) as long as a key's conversion, about 1.5 lane
+// operations an element, hides behind them; with several N tiles by mma.sync's rate.
+//
+// Work split: the blocks of 16 keys of all (request, row block, key/value head) stretches stand in one line, which is
+// cut in equal pieces, one for each CTA, at places that need not be ends of stretches.  A stretch that several CTAs
+// share is joined by the last of them to arrive, which adds the pieces in the order of the keys: equal calls give equal
+// bits.  Lengths are read on the device; no host knows them.  Warps of a CTA take the blocks of a piece two at a time in
+// turn, each with its own ring of bulk copies, and join once per piece.
+#include <float.h>
+
+#include <atomic>
+
+#include "kv_internal.h"
+#include "tc_ptx.cuh"
+
+namespace lexi {
+namespace kv {
+namespace {
+
+constexpr int kWarps = 4;
+constexpr int kThreads = 32 * kWarps;
+constexpr int kPair = 2;                       // blocks a warp handles per step
+constexpr float kFloor = -FLT_MAX;             // reference of a row that has seen no key
+// Weights are 2^(x - m + kHead): the reference m follows the largest score only when one exceeds it by kSlack, and
+// f16 still holds what is 2^-28 of the largest
+constexpr float kHead = 6.f, kSlack = 8.f;
+
+__device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t v) {
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
+}
+// four bytes of two e2m1 codes each -> four f16 pairs
+__device__ __forceinline__ void codes4(uint32_t w, uint32_t (&h)[4]) {
+    asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\tmov.b32 {b0, b1, b2, b3}, %4;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %0, b0;\n\tcvt.rn.f16x2.e2m1x2 %1, b1;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %2, b2;\n\tcvt.rn.f16x2.e2m1x2 %3, b3;\n\t}"
+        : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(w));
+}
+__device__ __forceinline__ uint32_t scales2(uint32_t two_bytes) {
+    uint32_t h;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)two_bytes));
+    return h;
+}
+__device__ __forceinline__ uint32_t mul2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ float ex2(float v) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+__device__ __forceinline__ float2 unpack2(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2 *>(&v)); }
+
+__device__ __forceinline__ float load_q(const float *p) { return *p; }
+__device__ __forceinline__ float load_q(const __nv_bfloat16 *p) { return __bfloat162float(*p); }
+
+template <int W, int NT, bool SPLIT>
+struct Shape {
+    static constexpr int kRows = 8 * NT;
+    static constexpr int kStages = W == 256 ? 2 : 3;
+    static constexpr int kStageBytes = kPair * block_bytes(W);
+    static constexpr int kRing = kWarps * kStages * kStageBytes;
+    static constexpr int kSteps = W / 16;                     // k16 steps of the scores
+    static constexpr int kTiles = W / 16;                     // m16 tiles of the output
+    static constexpr int kQ = kRows * W * 2 * (SPLIT ? 2 : 1);
+    static constexpr int kJoinTiles = NT >= 8 ? 1 : (kTiles < 8 / NT ? kTiles : 8 / NT);   // m16 tiles joined at a time: 32 KB
+    static constexpr int kJoin = kWarps * kRows * kJoinTiles * 16 * 4;
+    static_assert(kJoin <= kRing, "the join's buffer is the ring's");
+    static constexpr int kSmem = kRing + kQ;                  // plus the line of requests
+};
+
+// The line of work, made by every CTA for itself
+struct Piece { int req, rb, head; int first, count, total; };
+
+template <typename T, int W, int NT, int MINB>
+__global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs a) {
+    constexpr bool SPLIT = sizeof(T) == 4;
+    using S = Shape<W, NT, SPLIT>;
+    extern __shared__ __align__(128) uint8_t smem[];
+    uint8_t *ring = smem, *q_s = smem + S::kRing;
+    int64_t *line = reinterpret_cast<int64_t *>(smem + S::kSmem);      // [n + 1] running sum of blocks
+    __shared__ __align__(8) uint64_t full[kWarps * S::kStages];
+    __shared__ int32_t row_pos[S::kRows];          // position of a row's token, -1 for a row that is none
+    __shared__ float row_scale[S::kRows];          // its factor from the product to the exponent
+    __shared__ float2 join_ml[kWarps][S::kRows];   // reference and sum of each warp, then weight of each warp
+    __shared__ float2 row_ml[S::kRows];
+    __shared__ long long sum_s[kWarps];
+    __shared__ int last_s;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r = lane >> 2, c = lane & 3;
+
+    if (tid < kWarps * S::kStages) tc::mbar_init(smem_u32(&full[tid]), 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+
+    // ---- the line: for request i, row blocks * heads * visible blocks (at least one, which writes the zeros)
+    const int page_tokens = a.page_blocks * kBlockTokens;
+    auto lengths = [&](int i, int &len, int &q0, int &nq) {
+        len = max(a.kv_len[i], 0);
+        q0 = a.cu[i];
+        nq = a.cu[i + 1] - q0;
+        if (q0 < 0 || nq < 0 || q0 > a.T - nq) { atomicOr(a.status, MOE_KV_STATUS_BAD_INDEX); nq = 0; }
+        if (len > (int64_t)a.width * page_tokens) { atomicOr(a.status, MOE_KV_STATUS_BAD_INDEX); len = a.width * page_tokens; }
+    };
+    // blocks that rows [row0, row1) of a request see: [0, sb) and [wb, nb)
+    auto visible = [&](int len, int nq, int row0, int row1, int &sb, int &wb, int &nb) {
+        const int p0 = len - nq + row0 / a.G, p1 = len - nq + (row1 - 1) / a.G;
+        nb = p1 < 0 ? 0 : p1 / kBlockTokens + 1;
+        wb = a.window > 0 ? max(p0 - a.window + 1, 0) / kBlockTokens : 0;
+        wb = min(wb, nb);
+        sb = a.window > 0 ? min((int)(((int64_t)a.sinks + kBlockTokens - 1) / kBlockTokens), wb) : 0;
+    };
+    auto rows_of = [&](int nq, int rb, int &row0, int &row1) {
+        row0 = rb * S::kRows;
+        row1 = min(row0 + S::kRows, nq * a.G);
+    };
+    auto blocks_of = [&](int len, int nq) {
+        long long sum = 0;
+        for (int row0 = 0; row0 < nq * a.G; row0 += S::kRows) {
+            int sb, wb, nb;
+            visible(len, nq, row0, min(row0 + S::kRows, nq * a.G), sb, wb, nb);
+            sum += max(sb + nb - wb, 1);
+        }
+        return sum * a.Hk;
+    };
+    {
+        long long carry = 0;
+        for (int base = 0; base < a.n; base += kThreads) {
+            const int i = base + tid;
+            long long mine = 0;
+            if (i < a.n) {
+                int len, q0, nq;
+                lengths(i, len, q0, nq);
+                mine = blocks_of(len, nq);
+            }
+            long long inc = mine;
+            for (int o = 1; o < 32; o <<= 1) {
+                const long long up = __shfl_up_sync(0xffffffffu, inc, o);
+                if (lane >= o) inc += up;
+            }
+            if (lane == 31) sum_s[warp] = inc;
+            __syncthreads();
+            long long before = carry, all = carry;
+            for (int w = 0; w < kWarps; ++w) { if (w < warp) before += sum_s[w]; all += sum_s[w]; }
+            if (i < a.n) line[i] = before + inc - mine;
+            carry = all;
+            __syncthreads();
+        }
+        if (tid == 0) line[a.n] = carry;
+        __syncthreads();
+    }
+    const long long total = line[a.n];
+    // a piece has at least 2 steps of every warp's
+    const long long least = 2 * kWarps * kPair;
+    const long long share = max((total + gridDim.x - 1) / (long long)gridDim.x, least);
+    long long at = share * blockIdx.x;
+    const long long end = min(at + share, total);
+    uint32_t phase = 0;          // one bit for each stage of this warp
+    bool dead = false;
+
+    while (at < end) {
+        // ---- which stretch `at` lies in
+        int lo = 0, hi = a.n;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (line[mid] <= at) lo = mid; else hi = mid;
+        }
+        const int req = lo;
+        int len, q0, nq;
+        lengths(req, len, q0, nq);
+        long long off = at - line[req];
+        int rb = 0, sb, wb, nb, row0, row1;
+        for (;; ++rb) {
+            rows_of(nq, rb, row0, row1);
+            visible(len, nq, row0, row1, sb, wb, nb);
+            const long long here = (long long)max(sb + nb - wb, 1) * a.Hk;
+            if (off < here) break;
+            off -= here;
+        }
+        const int units = max(sb + nb - wb, 1), present = sb + nb - wb;
+        const int head = (int)(off / units), first = (int)(off - (long long)head * units);
+        const int last = (int)min((long long)units, first + end - at);
+        const long long stretch = at - first;          // where the stretch begins in the line
+        const int b1 = min(last, present);             // blocks [first, b1) of the stretch are loaded
+
+        // ---- queries of the rows, as operand fragments: [N tile][two k16 steps][lane] 16 bytes
+        {
+            // a warp a row; lane l holds dimensions [l W/32, (l+1) W/32)
+            constexpr int kPer = W / 32;
+            for (int n = warp; n < S::kRows; n += kWarps) {
+                const int row = row0 + n;
+                float v[kPer];
+                const bool real = row < row1;
+                const int tok = row / a.G;
+                float top = 0.f;
+                const T *src = (const T *)a.q.p + (int64_t)(q0 + (real ? tok : 0)) * a.q.ts + (int64_t)(head * a.G + (real ? row - tok * a.G : 0)) * a.q.hs;
+#pragma unroll
+                for (int i = 0; i < kPer; ++i) {
+                    const int d = lane * kPer + i;
+                    v[i] = real && d < a.D ? load_q(src + d) : 0.f;
+                    top = fmaxf(top, fabsf(v[i]));
+                }
+#pragma unroll
+                for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                // 2^e <= top < 2^(e+1): times 2^(10-e) the row lies below 2^11, its f16 parts are exact down to 2^-34 of its top
+                int e = top > 0.f && top <= FLT_MAX ? ilogbf(top) : 0;
+                e = max(e, -100);
+                const float up = ldexpf(1.f, 10 - e);
+                if (lane == 0) {
+                    row_pos[n] = real ? len - nq + tok : -1;
+                    row_scale[n] = ldexpf(a.score_scale, e - 10);
+                }
+#pragma unroll
+                for (int i = 0; i < kPer; i += 2) {
+                    const int d = lane * kPer + i;
+                    // thread c of a fragment has dimensions [c W/4, (c+1) W/4) of row r, four for each k16 step
+                    const int fc = d / (W / 4), in = d % (W / 4), step = in / 4, part = (in % 4) / 2;
+                    uint32_t *dst = reinterpret_cast<uint32_t *>(q_s) + ((((n >> 3) * (S::kSteps / 2) + step / 2) * 32 + (n & 7) * 4 + fc) * 4 + (step & 1) * 2 + part);
+                    const float x = v[i] * up, y = v[i + 1] * up;
+                    const uint32_t h = pack2(x, y);
+                    *dst = h;
+                    if (SPLIT) {
+                        const float2 f = unpack2(h);
+                        dst[S::kRows * W / 2] = pack2(x - f.x, y - f.y);
+                    }
+                }
+            }
+        }
+        __syncthreads();
+
+        // ---- this warp's blocks
+        const int32_t *table = a.table + (int64_t)req * a.width;
+        const uint32_t my_ring = smem_u32(ring) + warp * S::kStages * S::kStageBytes;
+        const uint8_t *my_ring_p = ring + warp * S::kStages * S::kStageBytes;
+        const int steps = b1 > first ? (b1 - first + kPair - 1) / kPair : 0;
+        const int mine = steps > warp ? (steps - warp + kWarps - 1) / kWarps : 0;
+        auto block_at = [&](int u) { return u < sb ? u : wb + u - sb; };
+        auto page_of = [&](int k, int j) {      // page of block j of this warp's k-th step, -1: none
+            const int u = first + (warp + k * kWarps) * kPair + j;
+            if (k >= mine || u >= b1) return -1;
+            const int b = block_at(u);
+            int pg = table[b / a.page_blocks];
+            if (pg < 0 || pg >= a.n_pages) { atomicOr(a.status, MOE_KV_STATUS_BAD_INDEX); pg = -1; }
+            return pg;
+        };
+        // lane l holds the page of block l%2 of step (now - now%16 + l/2), and of 16 steps later
+        int pages = page_of(lane >> 1, lane & 1), pages_next = page_of(16 + (lane >> 1), lane & 1);
+        auto issue = [&](int k, int pg0, int pg1) {       // lanes 0 and 1 copy a block each
+            const int stage = k % S::kStages;
+            const int u = first + (warp + k * kWarps) * kPair + lane;
+            const int pg = lane == 0 ? pg0 : pg1;
+            const uint32_t bar = smem_u32(&full[warp * S::kStages + stage]);
+            const int present_blocks = (pg0 >= 0) + (pg1 >= 0);
+            if (lane == 0) tc::mbar_expect_tx(bar, present_blocks * block_bytes(W));
+            __syncwarp();
+            if (lane < kPair && pg >= 0) {
+                const int b = block_at(u);
+                const uint8_t *src = a.cache + (((int64_t)pg * a.Hk + head) * a.page_blocks + b % a.page_blocks) * (int64_t)block_bytes(W);
+                bulk_load(my_ring + stage * S::kStageBytes + lane * block_bytes(W), src, block_bytes(W), bar);
+            }
+        };
+        auto pages_at = [&](int k, int base, int &pg0, int &pg1) {      // base: the first step of `pages`
+            const int l = (k - base) * 2;
+            const int p0 = __shfl_sync(0xffffffffu, pages, l & 31), p1 = __shfl_sync(0xffffffffu, pages, (l + 1) & 31);
+            const int n0 = __shfl_sync(0xffffffffu, pages_next, l & 31), n1 = __shfl_sync(0xffffffffu, pages_next, (l + 1) & 31);
+            pg0 = l < 32 ? p0 : n0;
+            pg1 = l < 32 ? p1 : n1;
+        };
+        for (int k = 0; k < S::kStages && k < mine && !dead; ++k) {
+            int pg0, pg1;
+            pages_at(k, 0, pg0, pg1);
+            issue(k, pg0, pg1);
+        }
+
+        float m[NT][2], l[NT][2], o[S::kTiles][NT][4], f[NT][2];
+        int lo_max = 0, hi_min = INT32_MAX;       // keys in [lo_max, hi_min) are seen by every row
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                m[t][j] = kFloor; l[t][j] = 0.f;
+                f[t][j] = row_scale[t * 8 + 2 * c + j];
+            }
+        {
+            const int p_first = len - nq + row0 / a.G, p_last = len - nq + (row1 - 1) / a.G;
+            hi_min = p_first + 1;
+            lo_max = a.window > 0 ? p_last - a.window + 1 : 0;
+        }
+#pragma unroll
+        for (int t = 0; t < S::kTiles; ++t)
+#pragma unroll
+            for (int u = 0; u < NT; ++u)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) o[t][u][j] = 0.f;
+
+        int base = 0;
+        for (int k = 0; k < mine; ++k) {
+            if (dead) break;
+            if (k - base == 16) { base = k; pages = pages_next; pages_next = page_of(base + 16 + (lane >> 1), lane & 1); }
+            const int stage = k % S::kStages;
+            int pg[2];
+            pages_at(k, base, pg[0], pg[1]);
+            // a copy that never ends: nothing more is waited for, the status word tells
+            dead = !__all_sync(0xffffffffu, tc::mbar_wait(smem_u32(&full[warp * S::kStages + stage]), (phase >> stage) & 1u, a.status));
+            phase ^= 1u << stage;
+            const uint8_t *buf = my_ring_p + stage * S::kStageBytes;
+            const int u0 = first + (warp + k * kWarps) * kPair;
+            const bool two = pg[1] >= 0;
+
+            // ---- scores of 32 keys: s[block][N tile]
+            float s[kPair][NT][4];
+#pragma unroll
+            for (int b = 0; b < kPair; ++b) {
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) s[b][t][j] = 0.f;
+                if (b == 1 && !two) continue;
+                const uint8_t *blk = buf + b * block_bytes(W);
+                constexpr int kBytes = W / 8;               // code bytes of a thread's share of a key
+                constexpr int kGroups = W / 64;             // scales of it
+                uint32_t sc[2][kGroups];                    // f16 pairs (s, s) of keys r and r + 8
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const uint8_t *p = blk + k_scales_at(W) + (r + 8 * half) * (W / 16) + c * kGroups;
+                    if (W == 64) {
+                        sc[half][0] = scales2((uint32_t)*p * 0x101u);
+                    } else if (W == 128) {
+                        const uint32_t two_s = scales2(*reinterpret_cast<const uint16_t *>(p));
+                        sc[half][0] = __byte_perm(two_s, 0, 0x1010);
+                        sc[half][kGroups > 1 ? 1 : 0] = __byte_perm(two_s, 0, 0x3232);
+                    } else {
+                        const uint32_t four = *reinterpret_cast<const uint32_t *>(p);
+                        const uint32_t x = scales2(four & 0xffffu), y = scales2(four >> 16);
+                        sc[half][0] = __byte_perm(x, 0, 0x1010);
+                        sc[half][1 % kGroups] = __byte_perm(x, 0, 0x3232);
+                        sc[half][2 % kGroups] = __byte_perm(y, 0, 0x1010);
+                        sc[half][3 % kGroups] = __byte_perm(y, 0, 0x3232);
+                    }
+                }
+                // 8 bytes of codes a group: two words, 4 k16 steps
+#pragma unroll
+                for (int g = 0; g < kGroups; ++g) {
+                    const uint2 w0 = *reinterpret_cast<const uint2 *>(blk + r * (W / 2) + c * kBytes + g * 8);
+                    const uint2 w1 = *reinterpret_cast<const uint2 *>(blk + (r + 8) * (W / 2) + c * kBytes + g * 8);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        uint32_t h0[4], h1[4];
+                        codes4(i ? w0.y : w0.x, h0);
+                        codes4(i ? w1.y : w1.x, h1);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) { h0[j] = mul2(h0[j], sc[0][g]); h1[j] = mul2(h1[j], sc[1][g]); }
+#pragma unroll
+                        for (int t = 0; t < NT; ++t) {
+                            const uint4 q = *reinterpret_cast<const uint4 *>(q_s + ((t * (S::kSteps / 2) + g * 2 + i) * 32 + lane) * 16);
+                            mma(s[b][t], h0[0], h1[0], h0[1], h1[1], q.x, q.y);
+                            mma(s[b][t], h0[2], h1[2], h0[3], h1[3], q.z, q.w);
+                            if (SPLIT) {
+                                const uint4 ql = *reinterpret_cast<const uint4 *>(q_s + S::kRows * W * 2 + ((t * (S::kSteps / 2) + g * 2 + i) * 32 + lane) * 16);
+                                mma(s[b][t], h0[0], h1[0], h0[1], h1[1], ql.x, ql.y);
+                                mma(s[b][t], h0[2], h1[2], h0[3], h1[3], ql.z, ql.w);
+                            }
+                        }
+                    }
+                }
+            }
+
+            // ---- exponents, masks, the reference
+            bool over = false;
+            int valid[kPair];         // keys of the block that lie in the cache: the rest of its value scales count as 0
+#pragma unroll
+            for (int b = 0; b < kPair; ++b) {
+                const int key0 = u0 + b < b1 ? block_at(u0 + b) * kBlockTokens : 0;
+                const bool here = pg[b] >= 0;
+                const bool clear = here && key0 + kBlockTokens <= hi_min && (key0 >= lo_max || key0 + kBlockTokens <= a.sinks);
+                valid[b] = here ? len - key0 : 0;
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        float x = s[b][t][j] * f[t][j & 1];
+                        if (!clear) {
+                            const int key = key0 + r + 8 * (j >> 1), p = row_pos[t * 8 + 2 * c + (j & 1)];
+                            const bool see = here && key <= p && (a.window <= 0 || p - key < a.window || key < a.sinks);
+                            x = see ? x : -INFINITY;
+                        }
+                        s[b][t][j] = x;
+                        over = over || x > m[t][j & 1] + kSlack;
+                    }
+            }
+            if (__any_sync(0xffffffffu, over)) {
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        float top = m[t][j];
+#pragma unroll
+                        for (int b = 0; b < kPair; ++b) top = fmaxf(top, fmaxf(s[b][t][j], s[b][t][j + 2]));
+                        for (int x = 4; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+                        const float down = ex2(m[t][j] - top);      // 0 for a row that had seen no key
+                        const float scale = m[t][j] == top ? 1.f : down;
+                        m[t][j] = top;
+                        l[t][j] *= scale;
+#pragma unroll
+                        for (int i = 0; i < S::kTiles; ++i) { o[i][t][j] *= scale; o[i][t][j + 2] *= scale; }
+                    }
+            }
+
+            // ---- weights and values
+#pragma unroll
+            for (int b = 0; b < kPair; ++b) {
+                if (b == 1 && !two) continue;
+                if (pg[b] < 0) continue;
+                const uint8_t *blk = buf + b * block_bytes(W);
+                uint32_t p0[NT], p1[NT], q0l[NT], q1l[NT];
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    float w[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        w[j] = ex2(s[b][t][j] - m[t][j & 1] + kHead);
+                        l[t][j & 1] += w[j];
+                    }
+                    const uint32_t h0 = pack2(w[0], w[1]), h1 = pack2(w[2], w[3]);
+                    p0[t] = transpose8(h0);
+                    p1[t] = transpose8(h1);
+                    if (SPLIT) {
+                        const float2 f0 = unpack2(h0), f1 = unpack2(h1);
+                        q0l[t] = transpose8(pack2(w[0] - f0.x, w[1] - f0.y));
+                        q1l[t] = transpose8(pack2(w[2] - f1.x, w[3] - f1.y));
+                    }
+                }
+                const uint8_t *codes = blk + v_codes_at(W) + r * W;
+                constexpr int vb = W / 16;
+                constexpr int kWords = vb / 4;              // words of a key's share: 1, 2, 4
+                uint32_t ka[kWords], kb[kWords], kc[kWords], kd[kWords];      // keys 2c, 2c+1, 2c+8, 2c+9
+                const int turned = v_turn(W, r);
+                if (W == 64) {
+                    const uint2 x = *reinterpret_cast<const uint2 *>(codes + ((8 * c) ^ turned)), y = *reinterpret_cast<const uint2 *>(codes + ((32 + 8 * c) ^ turned));
+                    ka[0] = x.x; kb[0] = x.y; kc[0] = y.x; kd[0] = y.y;
+                } else if (W == 128) {
+                    const uint4 x = *reinterpret_cast<const uint4 *>(codes + ((16 * c) ^ turned)), y = *reinterpret_cast<const uint4 *>(codes + ((64 + 16 * c) ^ turned));
+                    ka[0] = x.x; ka[1 % kWords] = x.y; kb[0] = x.z; kb[1 % kWords] = x.w;
+                    kc[0] = y.x; kc[1 % kWords] = y.y; kd[0] = y.z; kd[1 % kWords] = y.w;
+                } else {
+                    const uint4 x = *reinterpret_cast<const uint4 *>(codes + ((32 * c) ^ turned)), y = *reinterpret_cast<const uint4 *>(codes + ((32 * c + 16) ^ turned));
+                    const uint4 z = *reinterpret_cast<const uint4 *>(codes + ((128 + 32 * c) ^ turned)), u = *reinterpret_cast<const uint4 *>(codes + ((128 + 32 * c + 16) ^ turned));
+                    ka[0] = x.x; ka[1 % kWords] = x.y; ka[2 % kWords] = x.z; ka[3 % kWords] = x.w;
+                    kb[0] = y.x; kb[1 % kWords] = y.y; kb[2 % kWords] = y.z; kb[3 % kWords] = y.w;
+                    kc[0] = z.x; kc[1 % kWords] = z.y; kc[2 % kWords] = z.z; kc[3 % kWords] = z.w;
+                    kd[0] = u.x; kd[1 % kWords] = u.y; kd[2 % kWords] = u.z; kd[3 % kWords] = u.w;
+                }
+                // scales of the key pairs (2c, 2c+1) and (2c+8, 2c+9); a key behind the cached ones has none, whatever its bytes
+                constexpr int kG = W == 256 ? 2 : 1;
+                uint32_t sa[kG], sb2[kG];
+#pragma unroll
+                for (int g = 0; g < kG; ++g) {
+                    const int grp = W == 64 ? r >> 1 : W == 128 ? r : 2 * r + g;
+                    const uint8_t *p = blk + v_scales_at(W) + grp * kBlockTokens + 2 * c;
+                    sa[g] = scales2(*reinterpret_cast<const uint16_t *>(p));
+                    sb2[g] = scales2(*reinterpret_cast<const uint16_t *>(p + 8));
+                    if (valid[b] < kBlockTokens) {
+                        const int x = valid[b] - 2 * c;
+                        sa[g] = x >= 2 ? sa[g] : x == 1 ? sa[g] & 0xffffu : 0u;
+                        sb2[g] = x >= 10 ? sb2[g] : x == 9 ? sb2[g] & 0xffffu : 0u;
+                    }
+                }
+#pragma unroll
+                for (int w = 0; w < kWords; ++w) {
+                    constexpr uint32_t L = 0x0f0f0f0fu;
+                    uint32_t a0[4], a1[4], a2[4], a3[4];
+                    codes4((ka[w] & L) | ((kb[w] & L) << 4), a0);
+                    codes4(((ka[w] >> 4) & L) | (kb[w] & ~L), a1);
+                    codes4((kc[w] & L) | ((kd[w] & L) << 4), a2);
+                    codes4(((kc[w] >> 4) & L) | (kd[w] & ~L), a3);
+                    const int g = W == 256 ? w >> 1 : 0;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        a0[i] = mul2(a0[i], sa[g % kG]); a1[i] = mul2(a1[i], sa[g % kG]);
+                        a2[i] = mul2(a2[i], sb2[g % kG]); a3[i] = mul2(a3[i], sb2[g % kG]);
+#pragma unroll
+                        for (int t = 0; t < NT; ++t) {
+                            mma(o[w * 4 + i][t], a0[i], a1[i], a2[i], a3[i], p0[t], p1[t]);
+                            if (SPLIT) mma(o[w * 4 + i][t], a0[i], a1[i], a2[i], a3[i], q0l[t], q1l[t]);
+                        }
+                    }
+                }
+            }
+            __syncwarp();
+            if (k + S::kStages < mine) {
+                int pg0, pg1;
+                pages_at(k + S::kStages, base, pg0, pg1);
+                issue(k + S::kStages, pg0, pg1);
+            }
+        }
+
+        // ---- join the warps: o[t][u] holds rows 8u + 2c + {0, 1}, dimensions (W/8) r + 2t + {0, 1}
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                for (int x = 4; x < 32; x <<= 1) l[t][j] += __shfl_xor_sync(0xffffffffu, l[t][j], x);
+                if (r == 0) join_ml[warp][t * 8 + 2 * c + j] = make_float2(m[t][j], l[t][j]);
+            }
+        __syncthreads();       // every warp is done with its ring too
+        if (tid < S::kRows) {
+            float top = kFloor, sum = 0.f;
+            for (int w = 0; w < kWarps; ++w) top = fmaxf(top, join_ml[w][tid].x);
+            for (int w = 0; w < kWarps; ++w) {
+                const float2 ml = join_ml[w][tid];
+                const float k = ml.x == top ? 1.f : ex2(ml.x - top);
+                sum += k * ml.y;
+                join_ml[w][tid].x = k;
+            }
+            row_ml[tid] = make_float2(top, sum);
+        }
+        __syncthreads();
+        float k_mine[NT][2];
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) k_mine[t][j] = join_ml[warp][t * 8 + 2 * c + j].x;
+
+        const bool whole = first == 0 && last == units;
+        // a CTA's first piece may be the end of a stretch, its last piece the beginning of one
+        const int my_slot = blockIdx.x * 2 + (first == 0 ? 1 : 0);
+        float *part = a.part + (int64_t)my_slot * S::kRows * W;
+        float2 *part_ml = a.part_ml + (int64_t)my_slot * S::kRows;
+        float2 *buf = reinterpret_cast<float2 *>(ring);
+        auto put = [&](int n, int d, float2 v) {            // row n, dimensions d and d + 1 of the output
+            const int row = row0 + n;
+            if (row >= row1 || d >= a.D) return;
+            const int tok = row / a.G;
+            T *dst = (T *)a.out + ((int64_t)(q0 + tok) * a.H + head * a.G + row - tok * a.G) * a.D + d;
+            if (SPLIT) *reinterpret_cast<float2 *>(dst) = v;
+            else *reinterpret_cast<__nv_bfloat162 *>(dst) = __floats2bfloat162_rn(v.x, v.y);
+        };
+#pragma unroll
+        for (int t0 = 0; t0 < S::kTiles; t0 += S::kJoinTiles) {
+            if (t0) __syncthreads();
+#pragma unroll
+            for (int tl = 0; tl < S::kJoinTiles; ++tl)
+#pragma unroll
+                for (int u = 0; u < NT; ++u)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+                        buf[((warp * S::kRows + 8 * u + 2 * c + j) * S::kJoinTiles + tl) * 8 + r] =
+                            make_float2(o[t0 + tl][u][j] * k_mine[u][j], o[t0 + tl][u][j + 2] * k_mine[u][j]);
+            __syncthreads();
+            for (int e = tid; e < S::kRows * S::kJoinTiles * 8; e += kThreads) {
+                const int n = e / (S::kJoinTiles * 8), tl = e / 8 % S::kJoinTiles, rr = e % 8;
+                float2 v = make_float2(0.f, 0.f);
+                for (int w = 0; w < kWarps; ++w) {
+                    const float2 x = buf[w * S::kRows * S::kJoinTiles * 8 + e];
+                    v.x += x.x; v.y += x.y;
+                }
+                const int d = rr * (W / 8) + 2 * (t0 + tl);
+                if (whole) {
+                    const float sum = row_ml[n].y, k = sum > 0.f || sum != sum ? a.v_scale / sum : 0.f;
+                    put(n, d, make_float2(v.x * k, v.y * k));
+                } else {
+                    *reinterpret_cast<float2 *>(part + (int64_t)n * W + d) = v;
+                }
+            }
+        }
+        if (!whole) {
+            if (tid < S::kRows) part_ml[tid] = row_ml[tid];
+            __threadfence();
+            __syncthreads();
+            const int cta0 = (int)(stretch / share), cta1 = (int)((stretch + units - 1) / share);
+            if (tid == 0) {
+                const int before = atomicAdd(a.arrived + cta0, 1);
+                last_s = before == cta1 - cta0;
+                if (last_s) a.arrived[cta0] = 0;             // ready for the next call
+            }
+            __syncthreads();
+            if (last_s) {
+                __threadfence();
+                // the pieces in the order of the keys
+                for (int e = tid; e < S::kRows * (W / 2); e += kThreads) {
+                    const int n = e / (W / 2), d = e % (W / 2) * 2;
+                    if (row0 + n >= row1) continue;
+                    float top = kFloor, sum = 0.f;
+                    for (int b = cta0; b <= cta1; ++b) top = fmaxf(top, __ldcg(&a.part_ml[(int64_t)(b * 2 + (b == cta0)) * S::kRows + n]).x);
+                    float2 v = make_float2(0.f, 0.f);
+                    for (int b = cta0; b <= cta1; ++b) {
+                        const int64_t slot = b * 2 + (b == cta0);
+                        const float2 ml = __ldcg(&a.part_ml[slot * S::kRows + n]);
+                        const float k = ml.x == top ? 1.f : ex2(ml.x - top);
+                        const float2 x = __ldcg(reinterpret_cast<const float2 *>(a.part + (slot * S::kRows + n) * W + d));
+                        sum += k * ml.y;
+                        v.x += k * x.x; v.y += k * x.y;
+                    }
+                    const float k = sum > 0.f || sum != sum ? a.v_scale / sum : 0.f;
+                    put(n, d, make_float2(v.x * k, v.y * k));
+                }
+            }
+        }
+        // the ring and the rows' tables are the next piece's; its copies come after this piece's plain accesses
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncthreads();
+        at += last - first;
+    }
+}
+
+template <typename T, int W, int NT, int MINB>
+cudaError_t launch(const AttendArgs &a, int sm_count, cudaStream_t s, uint64_t *launches) {
+    using S = Shape<W, NT, sizeof(T) == 4>;
+    auto k = attend_rows_kernel<T, W, NT, MINB>;
+    // CTAs an SM holds, for up to kFew requests and for the most, asked once per device
+    constexpr int kFew = 256;
+    static std::atomic<int> held[64][2];
+    int dev = 0;
+    cudaError_t err = cudaGetDevice(&dev);
+    if (err != cudaSuccess) return err;
+    const bool many = a.n > kFew;
+    const int smem = S::kSmem + 8 * ((many ? kMaxRequests : kFew) + 1);
+    int per_sm = dev < 64 ? held[dev][many].load() : 0;
+    if (per_sm == 0) {
+        err = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem + 8 * (kMaxRequests + 1));
+        if (err != cudaSuccess) return err;
+        err = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, k, kThreads, smem);
+        if (err != cudaSuccess) return err;
+        if (per_sm < 1) return cudaErrorInvalidConfiguration;
+        if (dev < 64) held[dev][many].store(per_sm);
+    }
+    // no more CTAs than pieces: what the block tables can hold bounds the line
+    const long long rows = (long long)a.T * a.G;
+    const long long row_blocks = rows / S::kRows + a.n;
+    const double most = (double)row_blocks * a.Hk * ((double)a.width * a.page_blocks + 1);
+    long long grid = (long long)sm_count * per_sm;
+    const long long pieces = most < 1e15 ? ((long long)most + 2 * kWarps * kPair - 1) / (2 * kWarps * kPair) : grid;
+    grid = pieces < grid ? pieces : grid;
+    grid = grid > a.max_ctas ? a.max_ctas : grid < 1 ? 1 : grid;
+    k<<<(int)grid, kThreads, smem, s>>>(a);
+    ++*launches;
+    return cudaGetLastError();
+}
+
+template <typename T, int W>
+cudaError_t by_rows(const AttendArgs &a, int sm_count, cudaStream_t s, uint64_t *launches) {
+    const long long rows = (long long)(a.max_new > 0 ? a.max_new : a.T) * a.G;
+    if (rows <= 8) return launch<T, W, 1, W == 256 ? 3 : 4>(a, sm_count, s, launches);
+    if (W == 256 || rows <= 16) return launch<T, W, 2, W == 256 ? 2 : 3>(a, sm_count, s, launches);
+    if constexpr (W < 256) return launch<T, W, 4, 2>(a, sm_count, s, launches);
+    return cudaErrorInvalidValue;
+}
+
+}  // namespace
+
+size_t attend_part_floats(int w) { return (size_t)2 * (w == 256 ? 16 : 32) * w; }
+
+cudaError_t launch_attend_rows(const AttendArgs &a, int sm_count, cudaStream_t s, uint64_t *launches) {
+    const int w = padded_width(a.D);
+    if (a.dtype == MOE_BF16)
+        return w == 64 ? by_rows<__nv_bfloat16, 64>(a, sm_count, s, launches) : w == 128 ? by_rows<__nv_bfloat16, 128>(a, sm_count, s, launches)
+                                                                                       : by_rows<__nv_bfloat16, 256>(a, sm_count, s, launches);
+    return w == 64 ? by_rows<float, 64>(a, sm_count, s, launches) : w == 128 ? by_rows<float, 128>(a, sm_count, s, launches)
+                                                                            : by_rows<float, 256>(a, sm_count, s, launches);
+}
+
+}  // namespace kv
+}  // namespace lexi
