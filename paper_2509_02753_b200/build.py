@@ -1,4 +1,5 @@
-"""Builds the CUDA library in-tree: csrc/*.cu -> liblexi_moe.so (sm_100a only).
+"""Builds the CUDA library in-tree: csrc/*.cu -> liblexi_moe.so (sm_100a only), and the Python module
+csrc/kv_binding.cpp -> _kv_native.so that calls it.
 
 nvcc cross-compiles without a GPU.  Objects go to ``_build/`` at the repository
 root; a source is recompiled when it or any header is newer than its object.
@@ -17,6 +18,7 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 OBJ_DIR = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "liblexi_moe.so")
+NATIVE = os.path.join(PKG, "_kv_native.so")
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -59,7 +61,25 @@ def build(force: bool = False, verbose: bool = False) -> str:
         tmp = LIB + f".tmp{os.getpid()}"
         run([_nvcc(), "-shared", "-o", tmp] + objects)
         os.replace(tmp, LIB)
+    build_native(run, headers, force)
     return LIB
+
+
+def build_native(run, headers, force: bool) -> None:
+    src = os.path.join(CSRC, "kv_binding.cpp")
+    if not force and os.path.exists(NATIVE) and os.path.getmtime(NATIVE) >= max(os.path.getmtime(p) for p in headers + [src]):
+        return
+    import sysconfig
+
+    import torch
+    t = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(_nvcc())) if os.path.isabs(_nvcc()) else "/usr/local/cuda"
+    tmp = NATIVE + f".tmp{os.getpid()}"
+    run(["g++", "-O2", "-std=c++17", "-shared", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+         "-I" + INCLUDE, f"-I{t}/include", f"-I{t}/include/torch/csrc/api/include", f"-I{cuda}/include",
+         "-I" + sysconfig.get_paths()["include"], src, "-o", tmp, f"-L{PKG}", "-l:liblexi_moe.so", "-Wl,-rpath,$ORIGIN",
+         f"-L{t}/lib", "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_cuda", "-ltorch_python", f"-Wl,-rpath,{t}/lib"])
+    os.replace(tmp, NATIVE)
 
 
 if __name__ == "__main__":

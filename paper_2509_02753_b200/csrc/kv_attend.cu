@@ -14,11 +14,12 @@
 // Bound by the cache's bytes (9/8 W a key and head for K and V together) as long as a key's conversion, about 1.5 lane
 // operations an element, hides behind them; with several N tiles by mma.sync's rate.
 //
-// Work split: the blocks of 16 keys of all (request, row block, key/value head) stretches stand in one line, which is
-// cut in equal pieces, one for each CTA, at places that need not be ends of stretches.  A stretch that several CTAs
-// share is joined by the last of them to arrive, which adds the pieces in the order of the keys: equal calls give equal
-// bits.  Lengths are read on the device; no host knows them.  Warps of a CTA take the blocks of a piece two at a time in
-// turn, each with its own ring of bulk copies, and join once per piece.
+// Work split: a stretch is what one (request, row block, key/value head) has to read, in blocks of 16 keys.  Where there
+// are few stretches each is cut in equal pieces so that every CTA gets one; many short stretches are pieces themselves;
+// otherwise the stretches stand in one line that is cut in equal shares, at places that need not be ends of stretches.
+// A stretch in several pieces is joined by the last of them to arrive, which adds them in the order of the keys: equal
+// calls give equal bits.  Lengths are read on the device; no host knows them.  Warps of a CTA take the blocks of a piece
+// two at a time in turn, each with its own ring of bulk copies, and join once per piece.
 #include <float.h>
 
 #include <atomic>
@@ -33,6 +34,8 @@ namespace {
 constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kPair = 2;                       // blocks a warp handles per step
+constexpr int kLeast = kWarps * kPair;         // blocks of a piece, at least: a step of every warp
+constexpr int kBrief = 32;                     // stretches of at most this many blocks are not cut
 constexpr float kFloor = -FLT_MAX;             // reference of a row that has seen no key
 // Weights are 2^(x - m + kHead): the reference m follows the largest score only when one exceeds it by kSlack, and
 // f16 still holds what is 2^-28 of the largest
@@ -45,7 +48,7 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_
                  ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
 __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ uint32_t transpose8(uint32_t v) {
@@ -99,9 +102,6 @@ struct Shape {
     static constexpr int kSmem = kRing + kQ;                  // plus the line of requests
 };
 
-// The line of work, made by every CTA for itself
-struct Piece { int req, rb, head; int first, count, total; };
-
 template <typename T, int W, int NT, int MINB>
 __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs a) {
     constexpr bool SPLIT = sizeof(T) == 4;
@@ -114,7 +114,8 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
     __shared__ float row_scale[S::kRows];          // its factor from the product to the exponent
     __shared__ float2 join_ml[kWarps][S::kRows];   // reference and sum of each warp, then weight of each warp
     __shared__ float2 row_ml[S::kRows];
-    __shared__ long long sum_s[kWarps];
+    __shared__ long long sum_s[kWarps][2];
+    __shared__ int longest_s[kWarps];
     __shared__ int last_s;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r = lane >> 2, c = lane & 3;
 
@@ -138,19 +139,43 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
         wb = min(wb, nb);
         sb = a.window > 0 ? min((int)(((int64_t)a.sinks + kBlockTokens - 1) / kBlockTokens), wb) : 0;
     };
-    auto rows_of = [&](int nq, int rb, int &row0, int &row1) {
-        row0 = rb * S::kRows;
-        row1 = min(row0 + S::kRows, nq * a.G);
+    auto units_of = [&](int len, int nq, int row0) {
+        int sb, wb, nb;
+        visible(len, nq, row0, min(row0 + S::kRows, nq * a.G), sb, wb, nb);
+        return max(sb + nb - wb, 1);
     };
-    auto blocks_of = [&](int len, int nq) {
-        long long sum = 0;
+
+    // ---- how much there is: blocks, stretches, the longest stretch
+    long long blocks = 0, stretches = 0;
+    int longest = 0;
+    for (int i = tid; i < a.n; i += kThreads) {
+        int len, q0, nq;
+        lengths(i, len, q0, nq);
         for (int row0 = 0; row0 < nq * a.G; row0 += S::kRows) {
-            int sb, wb, nb;
-            visible(len, nq, row0, min(row0 + S::kRows, nq * a.G), sb, wb, nb);
-            sum += max(sb + nb - wb, 1);
+            const int u = units_of(len, nq, row0);
+            blocks += (long long)u * a.Hk;
+            stretches += a.Hk;
+            longest = max(longest, u);
         }
-        return sum * a.Hk;
-    };
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+        blocks += __shfl_xor_sync(0xffffffffu, blocks, o);
+        stretches += __shfl_xor_sync(0xffffffffu, stretches, o);
+        longest = max(longest, __shfl_xor_sync(0xffffffffu, longest, o));
+    }
+    if (lane == 0) { sum_s[warp][0] = blocks; sum_s[warp][1] = stretches; longest_s[warp] = longest; }
+    __syncthreads();
+    blocks = 0; stretches = 0; longest = 0;
+    for (int w = 0; w < kWarps; ++w) { blocks += sum_s[w][0]; stretches += sum_s[w][1]; longest = max(longest, longest_s[w]); }
+    __syncthreads();
+
+    // ---- how it is cut.  even: stretch by stretch, ceil(units/chunk) pieces each; else the line, `share` blocks a CTA
+    const bool few = 2 * stretches <= gridDim.x, brief = longest <= kBrief;
+    const bool even = few || brief;
+    // sum of ceil(u/chunk) <= blocks/chunk + stretches <= gridDim.x
+    const int chunk = few ? (int)max((blocks + gridDim.x - stretches - 1) / max((long long)gridDim.x - stretches, 1ll), (long long)kLeast) : kBrief;
+    const long long share = max((blocks + gridDim.x - 1) / (long long)gridDim.x, (long long)2 * kLeast);
     {
         long long carry = 0;
         for (int base = 0; base < a.n; base += kThreads) {
@@ -159,17 +184,20 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
             if (i < a.n) {
                 int len, q0, nq;
                 lengths(i, len, q0, nq);
-                mine = blocks_of(len, nq);
+                for (int row0 = 0; row0 < nq * a.G; row0 += S::kRows) {
+                    const int u = units_of(len, nq, row0);
+                    mine += (long long)(even ? (u + chunk - 1) / chunk : u) * a.Hk;
+                }
             }
             long long inc = mine;
             for (int o = 1; o < 32; o <<= 1) {
                 const long long up = __shfl_up_sync(0xffffffffu, inc, o);
                 if (lane >= o) inc += up;
             }
-            if (lane == 31) sum_s[warp] = inc;
+            if (lane == 31) sum_s[warp][0] = inc;
             __syncthreads();
             long long before = carry, all = carry;
-            for (int w = 0; w < kWarps; ++w) { if (w < warp) before += sum_s[w]; all += sum_s[w]; }
+            for (int w = 0; w < kWarps; ++w) { if (w < warp) before += sum_s[w][0]; all += sum_s[w][0]; }
             if (i < a.n) line[i] = before + inc - mine;
             carry = all;
             __syncthreads();
@@ -178,11 +206,9 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
         __syncthreads();
     }
     const long long total = line[a.n];
-    // a piece has at least 2 steps of every warp's
-    const long long least = 2 * kWarps * kPair;
-    const long long share = max((total + gridDim.x - 1) / (long long)gridDim.x, least);
-    long long at = share * blockIdx.x;
-    const long long end = min(at + share, total);
+    // even: pieces blockIdx.x, + gridDim.x, ...; else blocks [at, end) of the line
+    long long at = even ? (long long)blockIdx.x : share * blockIdx.x;
+    const long long end = even ? total : min(at + share, total);
     uint32_t phase = 0;          // one bit for each stage of this warp
     bool dead = false;
 
@@ -197,19 +223,68 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
         int len, q0, nq;
         lengths(req, len, q0, nq);
         long long off = at - line[req];
-        int rb = 0, sb, wb, nb, row0, row1;
-        for (;; ++rb) {
-            rows_of(nq, rb, row0, row1);
+        int sb, wb, nb, row0 = 0, row1, units, weight;
+        for (;; row0 += S::kRows) {
+            row1 = min(row0 + S::kRows, nq * a.G);
             visible(len, nq, row0, row1, sb, wb, nb);
-            const long long here = (long long)max(sb + nb - wb, 1) * a.Hk;
+            units = max(sb + nb - wb, 1);
+            weight = even ? (units + chunk - 1) / chunk : units;
+            const long long here = (long long)weight * a.Hk;
             if (off < here) break;
             off -= here;
         }
-        const int units = max(sb + nb - wb, 1), present = sb + nb - wb;
-        const int head = (int)(off / units), first = (int)(off - (long long)head * units);
-        const int last = (int)min((long long)units, first + end - at);
-        const long long stretch = at - first;          // where the stretch begins in the line
+        const int present = sb + nb - wb;
+        const int head = (int)(off / weight), within = (int)(off - (long long)head * weight);
+        // blocks [first, last) of the stretch are this piece; cta0..cta1 have its pieces (even: cta0 + piece number)
+        const int first = even ? (int)((long long)units * within / weight) : within;
+        const int last = even ? (int)((long long)units * (within + 1) / weight) : (int)min((long long)units, within + end - at);
+        const int cta0 = even ? (int)blockIdx.x - within : (int)((at - within) / share);
+        const int cta1 = even ? cta0 + weight - 1 : (int)((at - within + units - 1) / share);
         const int b1 = min(last, present);             // blocks [first, b1) of the stretch are loaded
+
+        // ---- this warp's blocks: the first copies start before the queries are read
+        const int32_t *table = a.table + (int64_t)req * a.width;
+        const uint32_t my_ring = smem_u32(ring) + warp * S::kStages * S::kStageBytes;
+        const uint8_t *my_ring_p = ring + warp * S::kStages * S::kStageBytes;
+        const int steps = b1 > first ? (b1 - first + kPair - 1) / kPair : 0;
+        const int mine = steps > warp ? (steps - warp + kWarps - 1) / kWarps : 0;
+        auto block_at = [&](int u) { return u < sb ? u : wb + u - sb; };
+        auto page_of = [&](int k, int j) {      // page of block j of this warp's k-th step, -1: none
+            const int u = first + (warp + k * kWarps) * kPair + j;
+            if (k >= mine || u >= b1) return -1;
+            const int b = block_at(u);
+            int pg = table[b / a.page_blocks];
+            if (pg < 0 || pg >= a.n_pages) { atomicOr(a.status, MOE_KV_STATUS_BAD_INDEX); pg = -1; }
+            return pg;
+        };
+        // lane l holds the page of block l%2 of step (now - now%16 + l/2), and of 16 steps later
+        int pages = page_of(lane >> 1, lane & 1), pages_next = page_of(16 + (lane >> 1), lane & 1);
+        auto issue = [&](int k, int pg0, int pg1) {       // lanes 0 and 1 copy a block each
+            const int stage = k % S::kStages;
+            const int u = first + (warp + k * kWarps) * kPair + lane;
+            const int pg = lane == 0 ? pg0 : pg1;
+            const uint32_t bar = smem_u32(&full[warp * S::kStages + stage]);
+            const int present_blocks = (pg0 >= 0) + (pg1 >= 0);
+            if (lane == 0) tc::mbar_expect_tx(bar, present_blocks * block_bytes(W));
+            __syncwarp();
+            if (lane < kPair && pg >= 0) {
+                const int b = block_at(u);
+                const uint8_t *src = a.cache + (((int64_t)pg * a.Hk + head) * a.page_blocks + b % a.page_blocks) * (int64_t)block_bytes(W);
+                bulk_load(my_ring + stage * S::kStageBytes + lane * block_bytes(W), src, block_bytes(W), bar);
+            }
+        };
+        auto pages_at = [&](int k, int base, int &pg0, int &pg1) {      // base: the first step of `pages`
+            const int l = (k - base) * 2;
+            const int p0 = __shfl_sync(0xffffffffu, pages, l & 31), p1 = __shfl_sync(0xffffffffu, pages, (l + 1) & 31);
+            const int n0 = __shfl_sync(0xffffffffu, pages_next, l & 31), n1 = __shfl_sync(0xffffffffu, pages_next, (l + 1) & 31);
+            pg0 = l < 32 ? p0 : n0;
+            pg1 = l < 32 ? p1 : n1;
+        };
+        for (int k = 0; k < S::kStages && k < mine && !dead; ++k) {
+            int pg0, pg1;
+            pages_at(k, 0, pg0, pg1);
+            issue(k, pg0, pg1);
+        }
 
         // ---- queries of the rows, as operand fragments: [N tile][two k16 steps][lane] 16 bytes
         {
@@ -256,50 +331,12 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
         }
         __syncthreads();
 
-        // ---- this warp's blocks
-        const int32_t *table = a.table + (int64_t)req * a.width;
-        const uint32_t my_ring = smem_u32(ring) + warp * S::kStages * S::kStageBytes;
-        const uint8_t *my_ring_p = ring + warp * S::kStages * S::kStageBytes;
-        const int steps = b1 > first ? (b1 - first + kPair - 1) / kPair : 0;
-        const int mine = steps > warp ? (steps - warp + kWarps - 1) / kWarps : 0;
-        auto block_at = [&](int u) { return u < sb ? u : wb + u - sb; };
-        auto page_of = [&](int k, int j) {      // page of block j of this warp's k-th step, -1: none
-            const int u = first + (warp + k * kWarps) * kPair + j;
-            if (k >= mine || u >= b1) return -1;
-            const int b = block_at(u);
-            int pg = table[b / a.page_blocks];
-            if (pg < 0 || pg >= a.n_pages) { atomicOr(a.status, MOE_KV_STATUS_BAD_INDEX); pg = -1; }
-            return pg;
-        };
-        // lane l holds the page of block l%2 of step (now - now%16 + l/2), and of 16 steps later
-        int pages = page_of(lane >> 1, lane & 1), pages_next = page_of(16 + (lane >> 1), lane & 1);
-        auto issue = [&](int k, int pg0, int pg1) {       // lanes 0 and 1 copy a block each
-            const int stage = k % S::kStages;
-            const int u = first + (warp + k * kWarps) * kPair + lane;
-            const int pg = lane == 0 ? pg0 : pg1;
-            const uint32_t bar = smem_u32(&full[warp * S::kStages + stage]);
-            const int present_blocks = (pg0 >= 0) + (pg1 >= 0);
-            if (lane == 0) tc::mbar_expect_tx(bar, present_blocks * block_bytes(W));
-            __syncwarp();
-            if (lane < kPair && pg >= 0) {
-                const int b = block_at(u);
-                const uint8_t *src = a.cache + (((int64_t)pg * a.Hk + head) * a.page_blocks + b % a.page_blocks) * (int64_t)block_bytes(W);
-                bulk_load(my_ring + stage * S::kStageBytes + lane * block_bytes(W), src, block_bytes(W), bar);
-            }
-        };
-        auto pages_at = [&](int k, int base, int &pg0, int &pg1) {      // base: the first step of `pages`
-            const int l = (k - base) * 2;
-            const int p0 = __shfl_sync(0xffffffffu, pages, l & 31), p1 = __shfl_sync(0xffffffffu, pages, (l + 1) & 31);
-            const int n0 = __shfl_sync(0xffffffffu, pages_next, l & 31), n1 = __shfl_sync(0xffffffffu, pages_next, (l + 1) & 31);
-            pg0 = l < 32 ? p0 : n0;
-            pg1 = l < 32 ? p1 : n1;
-        };
-        for (int k = 0; k < S::kStages && k < mine && !dead; ++k) {
-            int pg0, pg1;
-            pages_at(k, 0, pg0, pg1);
-            issue(k, pg0, pg1);
+        constexpr bool kHoldQ = NT == 1 && !SPLIT && W <= 128;         // 8 or 16 registers
+        uint4 q_r[kHoldQ ? S::kSteps / 2 : 1];
+        if (kHoldQ) {
+#pragma unroll
+            for (int i = 0; i < S::kSteps / 2; ++i) q_r[i] = *reinterpret_cast<const uint4 *>(q_s + (i * 32 + lane) * 16);
         }
-
         float m[NT][2], l[NT][2], o[S::kTiles][NT][4], f[NT][2];
         int lo_max = 0, hi_min = INT32_MAX;       // keys in [lo_max, hi_min) are seen by every row
 #pragma unroll
@@ -339,10 +376,12 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
             float s[kPair][NT][4];
 #pragma unroll
             for (int b = 0; b < kPair; ++b) {
+                constexpr bool kTwo = NT == 1;      // two chains of sums: half the latency of dependent products (more tiles are chains of their own)
+                float s2[kTwo ? NT : 1][4];
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) s[b][t][j] = 0.f;
+                    for (int j = 0; j < 4; ++j) s[b][t][j] = s2[kTwo ? t : 0][j] = 0.f;
                 if (b == 1 && !two) continue;
                 const uint8_t *blk = buf + b * block_bytes(W);
                 constexpr int kBytes = W / 8;               // code bytes of a thread's share of a key
@@ -380,16 +419,20 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
                         for (int j = 0; j < 4; ++j) { h0[j] = mul2(h0[j], sc[0][g]); h1[j] = mul2(h1[j], sc[1][g]); }
 #pragma unroll
                         for (int t = 0; t < NT; ++t) {
-                            const uint4 q = *reinterpret_cast<const uint4 *>(q_s + ((t * (S::kSteps / 2) + g * 2 + i) * 32 + lane) * 16);
+                            const uint4 q = kHoldQ ? q_r[g * 2 + i] : *reinterpret_cast<const uint4 *>(q_s + ((t * (S::kSteps / 2) + g * 2 + i) * 32 + lane) * 16);
                             mma(s[b][t], h0[0], h1[0], h0[1], h1[1], q.x, q.y);
-                            mma(s[b][t], h0[2], h1[2], h0[3], h1[3], q.z, q.w);
+                            mma(kTwo ? s2[kTwo ? t : 0] : s[b][t], h0[2], h1[2], h0[3], h1[3], q.z, q.w);
                             if (SPLIT) {
                                 const uint4 ql = *reinterpret_cast<const uint4 *>(q_s + S::kRows * W * 2 + ((t * (S::kSteps / 2) + g * 2 + i) * 32 + lane) * 16);
                                 mma(s[b][t], h0[0], h1[0], h0[1], h1[1], ql.x, ql.y);
-                                mma(s[b][t], h0[2], h1[2], h0[3], h1[3], ql.z, ql.w);
+                                mma(kTwo ? s2[kTwo ? t : 0] : s[b][t], h0[2], h1[2], h0[3], h1[3], ql.z, ql.w);
                             }
                         }
                     }
+                }
+                if (kTwo) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) s[b][0][j] += s2[0][j];
                 }
             }
 
@@ -595,7 +638,6 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
             if (tid < S::kRows) part_ml[tid] = row_ml[tid];
             __threadfence();
             __syncthreads();
-            const int cta0 = (int)(stretch / share), cta1 = (int)((stretch + units - 1) / share);
             if (tid == 0) {
                 const int before = atomicAdd(a.arrived + cta0, 1);
                 last_s = before == cta1 - cta0;
@@ -627,7 +669,7 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
         // the ring and the rows' tables are the next piece's; its copies come after this piece's plain accesses
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncthreads();
-        at += last - first;
+        at += even ? (long long)gridDim.x : (long long)(last - first);
     }
 }
 
@@ -652,12 +694,11 @@ cudaError_t launch(const AttendArgs &a, int sm_count, cudaStream_t s, uint64_t *
         if (per_sm < 1) return cudaErrorInvalidConfiguration;
         if (dev < 64) held[dev][many].store(per_sm);
     }
-    // no more CTAs than pieces: what the block tables can hold bounds the line
-    const long long rows = (long long)a.T * a.G;
-    const long long row_blocks = rows / S::kRows + a.n;
-    const double most = (double)row_blocks * a.Hk * ((double)a.width * a.page_blocks + 1);
+    // no more CTAs than pieces: what the block tables can hold bounds the blocks
+    const long long strips = ((long long)a.T * a.G / S::kRows + a.n) * a.Hk;
+    const double most = (double)strips * ((double)a.width * a.page_blocks / kLeast + 1);
     long long grid = (long long)sm_count * per_sm;
-    const long long pieces = most < 1e15 ? ((long long)most + 2 * kWarps * kPair - 1) / (2 * kWarps * kPair) : grid;
+    const long long pieces = most < 1e9 ? (long long)most : grid;
     grid = pieces < grid ? pieces : grid;
     grid = grid > a.max_ctas ? a.max_ctas : grid < 1 ? 1 : grid;
     k<<<(int)grid, kThreads, smem, s>>>(a);

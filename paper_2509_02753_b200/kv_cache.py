@@ -1,7 +1,8 @@
 """Thin ctypes binding of the C ABI in ``include/moe_kv.h``: the operators around a paged cache of keys and values in 4 bits.
 
 Argument marshalling only, like ``binding.py`` (whose ``MoEError`` it raises): every step runs in the CUDA kernels of
-``liblexi_moe.so``, there is no fallback.  A ``KVPlan`` is made for one shape of attention; the cache itself, the block
+``liblexi_moe.so``, there is no fallback.  The calls of a step go through the native module ``_kv_native`` (3 to 6 us a
+call on the host instead of 17 to 35 through ctypes), the others through ctypes.  A ``KVPlan`` is made for one shape of attention; the cache itself, the block
 tables and the free list are the caller's tensors:
 
     plan = KVPlan(n_heads=32, n_kv_heads=8, head_dim=128, page_size=64, dtype=torch.bfloat16, max_requests=16, max_tokens=8192)
@@ -48,6 +49,7 @@ class moe_rope_config_t(ctypes.Structure):
 
 
 _lib = None
+_native = None
 
 
 def load_library() -> ctypes.CDLL:
@@ -64,8 +66,8 @@ def load_library() -> ctypes.CDLL:
     lib.moe_kv_plan_launch_count.argtypes = [vp]
     lib.moe_kv_page_bytes.argtypes = [P(moe_kv_config_t)]
     lib.moe_kv_device_status.argtypes = [vp, P(i32), vp]
-    lib.moe_kv_tables.argtypes = [vp, vp, vp, i32, vp, i32, vp, i32, i32, vp, vp, vp, vp, vp, vp]
     lib.moe_rope_table.argtypes = [P(moe_rope_config_t), i32, vp, vp]
+    lib.moe_kv_tables.argtypes = [vp, vp, vp, i32, vp, i32, vp, i32, i32, vp, vp, vp, vp, vp, vp]
     lib.moe_rope.argtypes = [vp, rows, i32, i32, vp, vp, i32, i32, i32, i32, vp, i64, i64, vp]
     lib.moe_kv_append.argtypes = [vp, rows, rows, rows, i32, vp, vp, i32, i32, i32, vp, f32, f32, vp, vp, i32, vp]
     lib.moe_kv_read.argtypes = [vp, vp, i32, vp, i32, f32, f32, vp, vp, vp]
@@ -76,10 +78,17 @@ def load_library() -> ctypes.CDLL:
     return lib
 
 
-def _rows(x: torch.Tensor) -> moe_kv_rows_t:
-    ts, hs, one = x.stride()
-    assert one == 1 or x.shape[2] == 1, "the dimensions of a head must be neighbours"
-    return moe_kv_rows_t(x.data_ptr(), ts, hs)
+def load_native():
+    """The module ``_kv_native`` (built by ``paper_2509_02753_b200.build``); raises if absent."""
+    global _native
+    if _native is None:
+        load_library()
+        try:
+            from . import _kv_native
+        except ImportError as e:
+            raise MoEError(f"native binding not built ({e}); run __graft_entry__.build()", -5)
+        _native = _kv_native
+    return _native
 
 
 def rope_table(rope_dim: int, n_positions: int, *, base: float = 10000.0, scaling: str = "plain", factor: float = 1.0, low: float = 1.0,
@@ -100,13 +109,17 @@ class KVPlan:
     def __init__(self, *, n_heads: int, n_kv_heads: int, head_dim: int, page_size: int, dtype: torch.dtype, max_requests: int, max_tokens: int):
         self.n_heads, self.n_kv_heads, self.head_dim, self.page_size, self.dtype = n_heads, n_kv_heads, head_dim, page_size, dtype
         self.cfg = moe_kv_config_t(n_heads, n_kv_heads, head_dim, page_size, max_requests, max_tokens, B._dtype_code(dtype))
-        self._lib = load_library()
-        out = ctypes.c_void_p()
+        self._lib, self._native = load_library(), load_native()
+        self.default_scale = 1.0 / math.sqrt(head_dim)
+        self._plan = None
         self.handle = None
+        out = ctypes.c_void_p()
         B._check("moe_kv_plan_create", self._lib.moe_kv_plan_create(ctypes.byref(self.cfg), ctypes.byref(out)))
-        self.handle = out.value
+        self.handle, self.device = out.value, torch.cuda.current_device()
+        self._plan = (self.handle, n_heads, n_kv_heads, head_dim, self.page_bytes, self.cfg.dtype, self.device)
 
     def close(self):
+        self._plan = None
         if getattr(self, "handle", None):
             B._check("moe_kv_plan_destroy", self._lib.moe_kv_plan_destroy(self.handle))
             self.handle = None
@@ -148,96 +161,42 @@ class KVPlan:
         blocks = self.page_size // 16
         return torch.zeros((n_pages, self.n_kv_heads, blocks, self.page_bytes // (self.n_kv_heads * blocks)), dtype=torch.uint8, device=device)
 
-    def _pages(self, cache: torch.Tensor) -> int:
-        assert cache.is_cuda and cache.is_contiguous() and cache.dtype == torch.uint8
-        n = cache.shape[0]
-        assert cache.numel() == n * self.page_bytes, "cache of another shape"
-        return n
-
-    def _heads(self, x: torch.Tensor, heads: int, what: str) -> moe_kv_rows_t:
-        assert x.is_cuda and x.dtype == self.dtype and x.dim() == 3 and x.shape[1] == heads and x.shape[2] == self.head_dim, what
-        return _rows(x)
+    def _call(self, what: str, f, *args, stream=None):
+        """One native call on the current stream, or on `stream` (what it allocates then belongs to that stream)."""
+        if stream is not None and stream != torch.cuda.current_stream(self.device):
+            with torch.cuda.stream(stream):
+                got = f(*args)
+        else:
+            got = f(*args)
+        if got[0] != 0:
+            raise MoEError(what, got[0])
+        return got
 
     def tables(self, ctx_len: torch.Tensor, new_len: torch.Tensor, free_pages: torch.Tensor, block_table: torch.Tensor, n_tokens: int, stream=None):
         """(kv_len, cu_new, positions, slots, pages_taken); block_table gets the fresh pages (``moe_kv_tables``)."""
-        n, dev, i32 = ctx_len.shape[0], ctx_len.device, torch.int32
-        assert ctx_len.is_cuda and ctx_len.dtype == new_len.dtype == free_pages.dtype == block_table.dtype == i32
-        assert new_len.shape[0] == n and block_table.shape[0] == n
-        assert ctx_len.is_contiguous() and new_len.is_contiguous() and free_pages.is_contiguous() and block_table.is_contiguous()
-        kv_len = torch.empty((n,), dtype=i32, device=dev)
-        cu = torch.empty((n + 1,), dtype=i32, device=dev)
-        position = torch.empty((n_tokens,), dtype=i32, device=dev)
-        slot = torch.empty((n_tokens,), dtype=torch.int64, device=dev)
-        taken = torch.empty((1,), dtype=i32, device=dev)
-        B._check("moe_kv_tables", self._lib.moe_kv_tables(
-            self.handle, ctx_len.data_ptr(), new_len.data_ptr(), n, free_pages.data_ptr(), free_pages.numel(), block_table.data_ptr(),
-            block_table.shape[1], n_tokens, kv_len.data_ptr(), cu.data_ptr(), position.data_ptr(), slot.data_ptr(), taken.data_ptr(), B._stream(stream)))
-        return kv_len, cu, position, slot, taken
-
-    def _turns(self, turns, positions, n):
-        if turns is None:
-            return None, None, 0, 0
-        assert turns.is_cuda and turns.dtype == torch.float32 and turns.is_contiguous() and turns.dim() == 3 and turns.shape[2] == 2
-        assert positions is not None and positions.is_cuda and positions.dtype == torch.int32 and positions.is_contiguous() and positions.shape[0] == n
-        return positions.data_ptr(), turns.data_ptr(), turns.shape[0], 2 * turns.shape[1]
+        return self._call("moe_kv_tables", self._native.tables, self._plan, ctx_len, new_len, free_pages, block_table, n_tokens, stream=stream)[1:]
 
     def rope(self, x: torch.Tensor, positions: torch.Tensor, turns: torch.Tensor, *, layout: str = "half", inverse: bool = False,
              out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """x [tokens, heads, head_dim] turned by its tokens' positions; inverse=True turns back, which is the gradient (``moe_rope``)."""
-        rows = self._heads(x, x.shape[1], "x")
-        if out is None:
-            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        assert out.shape == x.shape and out.dtype == x.dtype and (out.stride(2) == 1 or self.head_dim == 1)
-        p, t, n_pos, rot = self._turns(turns, positions, x.shape[0])
-        B._check("moe_rope", self._lib.moe_rope(self.handle, ctypes.byref(rows), x.shape[0], x.shape[1], p, t, n_pos, rot, LAYOUTS[layout], int(inverse),
-                                                out.data_ptr(), out.stride(0), out.stride(1), B._stream(stream)))
-        return out
+        return self._call("moe_rope", self._native.rope, self._plan, x, positions, turns, LAYOUTS[layout], inverse, out, stream=stream)[1]
 
     def append(self, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, cache: torch.Tensor, *,
                positions: Optional[torch.Tensor] = None, turns: Optional[torch.Tensor] = None, layout: str = "half", k_scale: float = 1.0,
                v_scale: float = 1.0, q_out: Optional[torch.Tensor] = None, stream=None) -> Optional[torch.Tensor]:
         """Stores keys (turned) and values at the slots and returns the turned queries (``moe_kv_append``)."""
-        n = k.shape[0]
-        assert v.shape[0] == n and slots.is_cuda and slots.dtype == torch.int64 and slots.is_contiguous() and slots.shape[0] == n
-        kr, vr = self._heads(k, self.n_kv_heads, "k"), self._heads(v, self.n_kv_heads, "v")
-        qr = None
-        if q is not None:
-            assert q.shape[0] == n
-            qr = ctypes.byref(self._heads(q, self.n_heads, "q"))
-            if q_out is None:
-                q_out = torch.empty((n, self.n_heads, self.head_dim), dtype=self.dtype, device=k.device)
-            assert q_out.is_contiguous() and q_out.shape == q.shape and q_out.dtype == self.dtype
-        p, t, n_pos, rot = self._turns(turns, positions, n)
-        B._check("moe_kv_append", self._lib.moe_kv_append(
-            self.handle, qr, ctypes.byref(kr), ctypes.byref(vr), n, p, t, n_pos, rot, LAYOUTS[layout], slots.data_ptr(), k_scale, v_scale,
-            None if q is None else q_out.data_ptr(), cache.data_ptr(), self._pages(cache), B._stream(stream)))
-        return q_out if q is not None else None
+        got = self._call("moe_kv_append", self._native.append, self._plan, q, k, v, slots, cache, positions, turns, LAYOUTS[layout], k_scale, v_scale,
+                         q_out, stream=stream)
+        return got[1] if q is not None else None
 
     def read(self, cache: torch.Tensor, slots: torch.Tensor, *, k_scale: float = 1.0, v_scale: float = 1.0, stream=None):
         """(keys, values) [tokens, n_kv_heads, head_dim] at the slots, as the numbers they stand for (``moe_kv_read``)."""
-        assert slots.is_cuda and slots.dtype == torch.int64 and slots.is_contiguous()
-        n = slots.shape[0]
-        k = torch.empty((n, self.n_kv_heads, self.head_dim), dtype=self.dtype, device=cache.device)
-        v = torch.empty_like(k)
-        B._check("moe_kv_read", self._lib.moe_kv_read(self.handle, cache.data_ptr(), self._pages(cache), slots.data_ptr(), n, k_scale, v_scale,
-                                                      k.data_ptr(), v.data_ptr(), B._stream(stream)))
-        return k, v
+        return self._call("moe_kv_read", self._native.read, self._plan, cache, slots, k_scale, v_scale, stream=stream)[1:]
 
     def attention(self, q: torch.Tensor, cu_new: torch.Tensor, kv_len: torch.Tensor, block_table: torch.Tensor, cache: torch.Tensor, *,
                   max_new: int = 0, window: int = 0, sinks: int = 0, softmax_scale: Optional[float] = None, k_scale: float = 1.0, v_scale: float = 1.0,
                   out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """Attention of the new tokens' queries [tokens, n_heads, head_dim] over their requests' caches (``moe_kv_attention``).
         max_new: the largest number of new tokens of a request (0 = unknown); it chooses kernels, not results."""
-        rows = self._heads(q, self.n_heads, "q")
-        n = kv_len.shape[0]
-        assert cu_new.dtype == kv_len.dtype == block_table.dtype == torch.int32 and cu_new.shape[0] == n + 1 and block_table.shape[0] == n
-        assert cu_new.is_cuda and kv_len.is_cuda and block_table.is_cuda and cu_new.is_contiguous() and kv_len.is_contiguous() and block_table.is_contiguous()
-        if out is None:
-            out = torch.empty((q.shape[0], self.n_heads, self.head_dim), dtype=self.dtype, device=q.device)
-        assert out.is_contiguous() and out.shape == q.shape and out.dtype == self.dtype
-        if softmax_scale is None:
-            softmax_scale = 1.0 / math.sqrt(self.head_dim)
-        B._check("moe_kv_attention", self._lib.moe_kv_attention(
-            self.handle, ctypes.byref(rows), q.shape[0], cu_new.data_ptr(), kv_len.data_ptr(), n, max_new, block_table.data_ptr(), block_table.shape[1],
-            cache.data_ptr(), self._pages(cache), softmax_scale, k_scale, v_scale, window, sinks, out.data_ptr(), B._stream(stream)))
-        return out
+        return self._call("moe_kv_attention", self._native.attention, self._plan, q, cu_new, kv_len, block_table, cache, max_new, window, sinks,
+                          self.default_scale if softmax_scale is None else softmax_scale, k_scale, v_scale, out, stream=stream)[1]
