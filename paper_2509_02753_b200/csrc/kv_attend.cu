@@ -37,8 +37,8 @@ constexpr int kPair = 2;                       // blocks a warp handles per step
 constexpr int kLeast = kWarps * kPair;         // blocks of a piece, at least: a step of every warp
 constexpr int kBrief = 32;                     // stretches of at most this many blocks are not cut
 constexpr float kFloor = -FLT_MAX;             // reference of a row that has seen no key
-// Weights are 2^(x - m + kHead): the reference m follows the largest score only when one exceeds it by kSlack, and
-// f16 still holds what is 2^-28 of the largest
+// Weights are 2^(x - m + kHead + kSlack): m is kSlack above a score that was once the largest, and follows only when a
+// score passes it; f16 holds weights up to 2^(kHead + kSlack) and down to 2^-24
 constexpr float kHead = 6.f, kSlack = 8.f;
 
 __device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -90,7 +90,7 @@ __device__ __forceinline__ float load_q(const __nv_bfloat16 *p) { return __bfloa
 template <int W, int NT, bool SPLIT>
 struct Shape {
     static constexpr int kRows = 8 * NT;
-    static constexpr int kStages = W == 256 ? 2 : 3;
+    static constexpr int kStages = 2;
     static constexpr int kStageBytes = kPair * block_bytes(W);
     static constexpr int kRing = kWarps * kStages * kStageBytes;
     static constexpr int kSteps = W / 16;                     // k16 steps of the scores
@@ -123,7 +123,7 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
 
     // ---- the line: for request i, row blocks * heads * visible blocks (at least one, which writes the zeros)
-    const int page_tokens = a.page_blocks * kBlockTokens;
+    const int page_tokens = kBlockTokens << a.page_shift;
     auto lengths = [&](int i, int &len, int &q0, int &nq) {
         len = max(a.kv_len[i], 0);
         q0 = a.cu[i];
@@ -244,47 +244,33 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
 
         // ---- this warp's blocks: the first copies start before the queries are read
         const int32_t *table = a.table + (int64_t)req * a.width;
-        const uint32_t my_ring = smem_u32(ring) + warp * S::kStages * S::kStageBytes;
+        const uint32_t my_ring = smem_u32(ring) + warp * S::kStages * S::kStageBytes, my_bar = smem_u32(&full[warp * S::kStages]);
         const uint8_t *my_ring_p = ring + warp * S::kStages * S::kStageBytes;
         const int steps = b1 > first ? (b1 - first + kPair - 1) / kPair : 0;
         const int mine = steps > warp ? (steps - warp + kWarps - 1) / kWarps : 0;
         auto block_at = [&](int u) { return u < sb ? u : wb + u - sb; };
-        auto page_of = [&](int k, int j) {      // page of block j of this warp's k-th step, -1: none
-            const int u = first + (warp + k * kWarps) * kPair + j;
+        // 16 steps at a time: lane l finds the cache block that is block l%2 of step (from + l/2); -1: none
+        auto find_blocks = [&](int from) {
+            const int k = from + (lane >> 1), u = first + (warp + k * kWarps) * kPair + (lane & 1);
             if (k >= mine || u >= b1) return -1;
-            const int b = block_at(u);
-            int pg = table[b / a.page_blocks];
-            if (pg < 0 || pg >= a.n_pages) { atomicOr(a.status, MOE_KV_STATUS_BAD_INDEX); pg = -1; }
-            return pg;
+            const int b = block_at(u), pg = table[b >> a.page_shift];
+            if (pg < 0 || pg >= a.n_pages) { atomicOr(a.status, MOE_KV_STATUS_BAD_INDEX); return -1; }
+            return ((pg * a.Hk + head) << a.page_shift) + (b & ((1 << a.page_shift) - 1));
         };
-        // lane l holds the page of block l%2 of step (now - now%16 + l/2), and of 16 steps later
-        int pages = page_of(lane >> 1, lane & 1), pages_next = page_of(16 + (lane >> 1), lane & 1);
-        auto issue = [&](int k, int pg0, int pg1) {       // lanes 0 and 1 copy a block each
-            const int stage = k % S::kStages;
-            const int u = first + (warp + k * kWarps) * kPair + lane;
-            const int pg = lane == 0 ? pg0 : pg1;
-            const uint32_t bar = smem_u32(&full[warp * S::kStages + stage]);
-            const int present_blocks = (pg0 >= 0) + (pg1 >= 0);
-            if (lane == 0) tc::mbar_expect_tx(bar, present_blocks * block_bytes(W));
+        int now = find_blocks(0), then = find_blocks(16);
+        uint32_t has_now = __ballot_sync(0xffffffffu, now >= 0), has_then = __ballot_sync(0xffffffffu, then >= 0);
+        // copies of step (from + d), d < 32: by the two lanes that found its blocks
+        auto issue = [&](int d, int stage) {
+            const bool later = d >= 16;
+            const uint32_t two = ((later ? has_then : has_now) >> (2 * (d & 15))) & 3u;
+            const uint32_t bar = my_bar + 8 * stage;
+            if (lane == 0) tc::mbar_expect_tx(bar, (uint32_t)__popc(two) * block_bytes(W));
             __syncwarp();
-            if (lane < kPair && pg >= 0) {
-                const int b = block_at(u);
-                const uint8_t *src = a.cache + (((int64_t)pg * a.Hk + head) * a.page_blocks + b % a.page_blocks) * (int64_t)block_bytes(W);
-                bulk_load(my_ring + stage * S::kStageBytes + lane * block_bytes(W), src, block_bytes(W), bar);
-            }
+            const int blk = later ? then : now;
+            if ((lane >> 1) == (d & 15) && blk >= 0)
+                bulk_load(my_ring + stage * S::kStageBytes + (lane & 1) * block_bytes(W), a.cache + (int64_t)blk * block_bytes(W), block_bytes(W), bar);
         };
-        auto pages_at = [&](int k, int base, int &pg0, int &pg1) {      // base: the first step of `pages`
-            const int l = (k - base) * 2;
-            const int p0 = __shfl_sync(0xffffffffu, pages, l & 31), p1 = __shfl_sync(0xffffffffu, pages, (l + 1) & 31);
-            const int n0 = __shfl_sync(0xffffffffu, pages_next, l & 31), n1 = __shfl_sync(0xffffffffu, pages_next, (l + 1) & 31);
-            pg0 = l < 32 ? p0 : n0;
-            pg1 = l < 32 ? p1 : n1;
-        };
-        for (int k = 0; k < S::kStages && k < mine && !dead; ++k) {
-            int pg0, pg1;
-            pages_at(k, 0, pg0, pg1);
-            issue(k, pg0, pg1);
-        }
+        for (int k = 0; k < S::kStages && k < mine && !dead; ++k) issue(k, k);
 
         // ---- queries of the rows, as operand fragments: [N tile][two k16 steps][lane] 16 bytes
         {
@@ -338,7 +324,6 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
             for (int i = 0; i < S::kSteps / 2; ++i) q_r[i] = *reinterpret_cast<const uint4 *>(q_s + (i * 32 + lane) * 16);
         }
         float m[NT][2], l[NT][2], o[S::kTiles][NT][4], f[NT][2];
-        int lo_max = 0, hi_min = INT32_MAX;       // keys in [lo_max, hi_min) are seen by every row
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -346,11 +331,12 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
                 m[t][j] = kFloor; l[t][j] = 0.f;
                 f[t][j] = row_scale[t * 8 + 2 * c + j];
             }
-        {
-            const int p_first = len - nq + row0 / a.G, p_last = len - nq + (row1 - 1) / a.G;
-            hi_min = p_first + 1;
-            lo_max = a.window > 0 ? p_last - a.window + 1 : 0;
-        }
+        // blocks of the stretch that every row sees whole: [0, sink_clear) and [clear0, clear1)
+        const int p_first = len - nq + row0 / a.G, p_last = len - nq + (row1 - 1) / a.G;
+        const int whole1 = max(p_first + 1, 0) / kBlockTokens;                                                    // blocks below are complete
+        const int whole0 = a.window > 0 ? (max(p_last - a.window + 1, 0) + kBlockTokens - 1) / kBlockTokens : 0;   // and from here inside the window
+        const int sink_clear = min(sb, min(a.sinks / kBlockTokens, whole1));
+        const int clear0 = max(whole0 - wb, 0) + sb, clear1 = whole1 - wb + sb;
 #pragma unroll
         for (int t = 0; t < S::kTiles; ++t)
 #pragma unroll
@@ -358,19 +344,23 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
 #pragma unroll
                 for (int j = 0; j < 4; ++j) o[t][u][j] = 0.f;
 
-        int base = 0;
+        int from = 0;
         for (int k = 0; k < mine; ++k) {
-            if (dead) break;
-            if (k - base == 16) { base = k; pages = pages_next; pages_next = page_of(base + 16 + (lane >> 1), lane & 1); }
+            if (k - from == 16) {
+                from = k;
+                now = then; has_now = has_then;
+                then = find_blocks(from + 16);
+                has_then = __ballot_sync(0xffffffffu, then >= 0);
+            }
             const int stage = k % S::kStages;
-            int pg[2];
-            pages_at(k, base, pg[0], pg[1]);
             // a copy that never ends: nothing more is waited for, the status word tells
-            dead = !__all_sync(0xffffffffu, tc::mbar_wait(smem_u32(&full[warp * S::kStages + stage]), (phase >> stage) & 1u, a.status));
+            dead = !__all_sync(0xffffffffu, tc::mbar_wait(my_bar + 8 * stage, (phase >> stage) & 1u, a.status));
+            if (dead) break;
             phase ^= 1u << stage;
             const uint8_t *buf = my_ring_p + stage * S::kStageBytes;
             const int u0 = first + (warp + k * kWarps) * kPair;
-            const bool two = pg[1] >= 0;
+            const uint32_t has = (has_now >> (2 * (k - from))) & 3u;
+            const bool two = has & 2u;
 
             // ---- scores of 32 keys: s[block][N tile]
             float s[kPair][NT][4];
@@ -437,39 +427,46 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
             }
 
             // ---- exponents, masks, the reference
-            bool over = false;
+            bool over = false, clear[kPair];
             int valid[kPair];         // keys of the block that lie in the cache: the rest of its value scales count as 0
 #pragma unroll
             for (int b = 0; b < kPair; ++b) {
-                const int key0 = u0 + b < b1 ? block_at(u0 + b) * kBlockTokens : 0;
-                const bool here = pg[b] >= 0;
-                const bool clear = here && key0 + kBlockTokens <= hi_min && (key0 >= lo_max || key0 + kBlockTokens <= a.sinks);
-                valid[b] = here ? len - key0 : 0;
+                const int u = u0 + b;
+                clear[b] = (has >> b & 1u) && (u < sink_clear || (u >= clear0 && u < clear1));
+                valid[b] = kBlockTokens;
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        float x = s[b][t][j] * f[t][j & 1];
-                        if (!clear) {
+                    for (int j = 0; j < 4; ++j) s[b][t][j] *= f[t][j & 1];
+                if (!clear[b]) {
+                    const bool here = has >> b & 1u;
+                    const int key0 = block_at(u) * kBlockTokens;
+                    valid[b] = len - key0;
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
                             const int key = key0 + r + 8 * (j >> 1), p = row_pos[t * 8 + 2 * c + (j & 1)];
                             const bool see = here && key <= p && (a.window <= 0 || p - key < a.window || key < a.sinks);
-                            x = see ? x : -INFINITY;
+                            s[b][t][j] = see ? s[b][t][j] : -INFINITY;
                         }
-                        s[b][t][j] = x;
-                        over = over || x > m[t][j & 1] + kSlack;
-                    }
+                }
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) over = over || s[b][t][j] > m[t][j & 1];
             }
             if (__any_sync(0xffffffffu, over)) {
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
-                        float top = m[t][j];
+                        float top = kFloor;
 #pragma unroll
                         for (int b = 0; b < kPair; ++b) top = fmaxf(top, fmaxf(s[b][t][j], s[b][t][j + 2]));
                         for (int x = 4; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
-                        const float down = ex2(m[t][j] - top);      // 0 for a row that had seen no key
-                        const float scale = m[t][j] == top ? 1.f : down;
+                        top = fmaxf(m[t][j], top + kSlack);
+                        const float scale = m[t][j] == top ? 1.f : ex2(m[t][j] - top);      // 0 for a row that had seen no key
                         m[t][j] = top;
                         l[t][j] *= scale;
 #pragma unroll
@@ -480,8 +477,7 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
             // ---- weights and values
 #pragma unroll
             for (int b = 0; b < kPair; ++b) {
-                if (b == 1 && !two) continue;
-                if (pg[b] < 0) continue;
+                if (!(has >> b & 1u)) continue;
                 const uint8_t *blk = buf + b * block_bytes(W);
                 uint32_t p0[NT], p1[NT], q0l[NT], q1l[NT];
 #pragma unroll
@@ -489,7 +485,7 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
                     float w[4];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        w[j] = ex2(s[b][t][j] - m[t][j & 1] + kHead);
+                        w[j] = ex2(s[b][t][j] - m[t][j & 1] + (kHead + kSlack));
                         l[t][j & 1] += w[j];
                     }
                     const uint32_t h0 = pack2(w[0], w[1]), h1 = pack2(w[2], w[3]);
@@ -530,7 +526,7 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
                     const uint8_t *p = blk + v_scales_at(W) + grp * kBlockTokens + 2 * c;
                     sa[g] = scales2(*reinterpret_cast<const uint16_t *>(p));
                     sb2[g] = scales2(*reinterpret_cast<const uint16_t *>(p + 8));
-                    if (valid[b] < kBlockTokens) {
+                    if (!clear[b] && valid[b] < kBlockTokens) {
                         const int x = valid[b] - 2 * c;
                         sa[g] = x >= 2 ? sa[g] : x == 1 ? sa[g] & 0xffffu : 0u;
                         sb2[g] = x >= 10 ? sb2[g] : x == 9 ? sb2[g] & 0xffffu : 0u;
@@ -558,11 +554,7 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
                 }
             }
             __syncwarp();
-            if (k + S::kStages < mine) {
-                int pg0, pg1;
-                pages_at(k + S::kStages, base, pg0, pg1);
-                issue(k + S::kStages, pg0, pg1);
-            }
+            if (k + S::kStages < mine) issue(k + S::kStages - from, stage);
         }
 
         // ---- join the warps: o[t][u] holds rows 8u + 2c + {0, 1}, dimensions (W/8) r + 2t + {0, 1}
@@ -696,7 +688,7 @@ cudaError_t launch(const AttendArgs &a, int sm_count, cudaStream_t s, uint64_t *
     }
     // no more CTAs than pieces: what the block tables can hold bounds the blocks
     const long long strips = ((long long)a.T * a.G / S::kRows + a.n) * a.Hk;
-    const double most = (double)strips * ((double)a.width * a.page_blocks / kLeast + 1);
+    const double most = (double)strips * ((double)((long long)a.width << a.page_shift) / kLeast + 1);
     long long grid = (long long)sm_count * per_sm;
     const long long pieces = most < 1e9 ? (long long)most : grid;
     grid = pieces < grid ? pieces : grid;

@@ -64,7 +64,7 @@ cudaError_t launch_read(const ReadArgs &a, cudaStream_t s, uint64_t *launches);
 struct AttendArgs {
     int dtype; Rows q; int T; const int32_t *cu, *kv_len; int n; int max_new;
     const int32_t *table; int width; const uint8_t *cache; int n_pages;
-    int H, Hk, G, D, page_blocks;             // page_blocks: blocks of 16 tokens in a page
+    int H, Hk, G, D, page_shift;              // a page has 1 << page_shift blocks of 16 tokens
     float score_scale;                        // softmax_scale * k_scale * log2(e)
     float v_scale; int window, sinks;
     void *out;

@@ -224,7 +224,7 @@ int moe_kv_attention(moe_kv_plan_t *p, const moe_kv_rows_t *q, int32_t T, const 
     AttendArgs a{};
     a.dtype = c.dtype; a.q = Rows{q->data, q->token_stride, q->head_stride}; a.T = T; a.cu = cu_new; a.kv_len = kv_len; a.n = n; a.max_new = max_new;
     a.table = block_table; a.width = width; a.cache = (const uint8_t *)cache; a.n_pages = n_pages;
-    a.H = c.n_heads; a.Hk = c.n_kv_heads; a.G = c.n_heads / c.n_kv_heads; a.D = c.head_dim; a.page_blocks = c.page_size / kBlockTokens;
+    a.H = c.n_heads; a.Hk = c.n_kv_heads; a.G = c.n_heads / c.n_kv_heads; a.D = c.head_dim; a.page_shift = c.page_size == 16 ? 0 : c.page_size == 32 ? 1 : c.page_size == 64 ? 2 : 3;
     a.score_scale = (float)((double)softmax_scale * k_scale * 1.4426950408889634);
     a.v_scale = v_scale; a.window = window; a.sinks = sinks; a.out = out;
     a.part = p->part; a.part_ml = p->part_ml; a.arrived = p->arrived; a.max_ctas = p->max_ctas; a.status = p->status;
