@@ -43,10 +43,12 @@ int check_rows(const moe_kv_rows_t *r, int dtype) {
     return aligned(r->data, elem_size(dtype)) ? MOE_OK : MOE_ERR_ALIGN;
 }
 
-int check_turn(const moe_kv_plan *p, const int32_t *position, const float *table, int32_t n_positions, int32_t rope_dim, int32_t layout) {
+int check_turn(const moe_kv_plan *p, int32_t tokens, const int32_t *position, const float *table, int32_t n_positions, int32_t rope_dim, int32_t layout) {
     if (rope_dim == 0) return MOE_OK;
     if (rope_dim < 0 || rope_dim % 2 || rope_dim > p->cfg.head_dim) return MOE_ERR_SHAPE;
-    if (!position || !table || n_positions < 1 || (layout != MOE_ROPE_HALF && layout != MOE_ROPE_PAIRS)) return MOE_ERR_INVALID_ARG;
+    if (layout != MOE_ROPE_HALF && layout != MOE_ROPE_PAIRS) return MOE_ERR_INVALID_ARG;
+    if (tokens == 0) return MOE_OK;
+    if (!position || !table || n_positions < 1) return MOE_ERR_INVALID_ARG;
     return aligned(table, 8) ? MOE_OK : MOE_ERR_ALIGN;
 }
 
@@ -164,7 +166,7 @@ int moe_rope(moe_kv_plan_t *p, const moe_kv_rows_t *x, int32_t T, int32_t H, con
              int32_t rope_dim, int32_t layout, int32_t inverse, void *y, int64_t yts, int64_t yhs, void *stream) {
     if (!p || T < 0 || T > p->cfg.max_tokens || H < 1 || H > 1024 || (inverse != 0 && inverse != 1)) return MOE_ERR_INVALID_ARG;
     if (rope_dim < 2) return MOE_ERR_SHAPE;
-    if (const int rc = check_turn(p, position, table, n_positions, rope_dim, layout)) return rc;
+    if (const int rc = check_turn(p, T, position, table, n_positions, rope_dim, layout)) return rc;
     if (T == 0) return MOE_OK;
     if (const int rc = check_rows(x, p->cfg.dtype)) return rc;
     if (!y) return MOE_ERR_INVALID_ARG;
@@ -178,7 +180,7 @@ int moe_kv_append(moe_kv_plan_t *p, const moe_kv_rows_t *q, const moe_kv_rows_t 
                   const float *table, int32_t n_positions, int32_t rope_dim, int32_t layout, const int64_t *slot, float k_scale, float v_scale,
                   void *q_out, void *cache, int32_t n_pages, void *stream) {
     if (!p || T < 0 || T > p->cfg.max_tokens || n_pages < 0 || !good_scale(k_scale) || !good_scale(v_scale)) return MOE_ERR_INVALID_ARG;
-    if (const int rc = check_turn(p, position, table, n_positions, rope_dim, layout)) return rc;
+    if (const int rc = check_turn(p, T, position, table, n_positions, rope_dim, layout)) return rc;
     if (T == 0) return MOE_OK;
     const moe_kv_config_t &c = p->cfg;
     if (const int rc = check_rows(k, c.dtype)) return rc;
