@@ -24,6 +24,7 @@
 
 #include <atomic>
 
+#include "kv_codes.cuh"
 #include "kv_internal.h"
 #include "tc_ptx.cuh"
 
@@ -56,34 +57,6 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t v) {
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
     return r;
 }
-// four bytes of two e2m1 codes each -> four f16 pairs
-__device__ __forceinline__ void codes4(uint32_t w, uint32_t (&h)[4]) {
-    asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\tmov.b32 {b0, b1, b2, b3}, %4;\n\t"
-        "cvt.rn.f16x2.e2m1x2 %0, b0;\n\tcvt.rn.f16x2.e2m1x2 %1, b1;\n\t"
-        "cvt.rn.f16x2.e2m1x2 %2, b2;\n\tcvt.rn.f16x2.e2m1x2 %3, b3;\n\t}"
-        : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(w));
-}
-__device__ __forceinline__ uint32_t scales2(uint32_t two_bytes) {
-    uint32_t h;
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)two_bytes));
-    return h;
-}
-__device__ __forceinline__ uint32_t mul2(uint32_t a, uint32_t b) {
-    uint32_t r;
-    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-    return r;
-}
-__device__ __forceinline__ float ex2(float v) {
-    float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
-    return r;
-}
-__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
-    const __half2 h = __floats2half2_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t *>(&h);
-}
-__device__ __forceinline__ float2 unpack2(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2 *>(&v)); }
-
 __device__ __forceinline__ float load_q(const float *p) { return *p; }
 __device__ __forceinline__ float load_q(const __nv_bfloat16 *p) { return __bfloat162float(*p); }
 
@@ -130,6 +103,7 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
         nq = a.cu[i + 1] - q0;
         if (q0 < 0 || nq < 0 || q0 > a.T - nq) { atomicOr(a.status, MOE_KV_STATUS_BAD_INDEX); nq = 0; }
         if (len > (int64_t)a.width * page_tokens) { atomicOr(a.status, MOE_KV_STATUS_BAD_INDEX); len = a.width * page_tokens; }
+        if (a.prompt_rows > 0 && (int64_t)nq * a.G > a.prompt_rows) nq = 0;       // kv_prompt.cu's
     };
     // blocks that rows [row0, row1) of a request see: [0, sb) and [wb, nb)
     auto visible = [&](int len, int nq, int row0, int row1, int &sb, int &wb, int &nb) {
@@ -700,7 +674,8 @@ cudaError_t launch(const AttendArgs &a, int sm_count, cudaStream_t s, uint64_t *
 
 template <typename T, int W>
 cudaError_t by_rows(const AttendArgs &a, int sm_count, cudaStream_t s, uint64_t *launches) {
-    const long long rows = (long long)(a.max_new > 0 ? a.max_new : a.T) * a.G;
+    long long rows = (long long)(a.max_new > 0 ? a.max_new : a.T) * a.G;
+    if (a.prompt_rows > 0 && rows > a.prompt_rows) rows = a.prompt_rows;
     if (rows <= 8) return launch<T, W, 1, W == 256 ? 3 : 4>(a, sm_count, s, launches);
     if (W == 256 || rows <= 16) return launch<T, W, 2, W == 256 ? 2 : 3>(a, sm_count, s, launches);
     if constexpr (W < 256) return launch<T, W, 4, 2>(a, sm_count, s, launches);

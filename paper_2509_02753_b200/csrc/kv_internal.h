@@ -69,11 +69,19 @@ struct AttendArgs {
     float v_scale; int window, sinks;
     void *out;
     float *part; float2 *part_ml; int32_t *arrived; int max_ctas;   // split over the keys
+    // requests of more query rows per key/value head than this are kv_prompt.cu's; 0: none are
+    int prompt_rows;
+    float *prompt_part; float2 *prompt_ml; int32_t *prompt_arrived;
     int32_t *status;
 };
 // rows of queries that share a key/value head, in the N dimension of mma.sync (kv_attend.cu)
 cudaError_t launch_attend_rows(const AttendArgs &a, int sm_count, cudaStream_t s, uint64_t *launches);
 size_t attend_part_floats(int w);          // per CTA of the grid
+// prompts, on tcgen05 (kv_prompt.cu)
+bool prompt_supported(int dtype, int head_dim);
+cudaError_t launch_attend_prompt(const AttendArgs &a, int sm_count, cudaStream_t s, uint64_t *launches);
+size_t prompt_part_floats(int w);          // per CTA, of which there is one per SM
+size_t prompt_part_rows();
 
 }  // namespace kv
 }  // namespace lexi

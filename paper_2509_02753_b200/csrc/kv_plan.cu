@@ -16,6 +16,9 @@ struct moe_kv_plan {
     int32_t *status = nullptr, *arrived = nullptr;
     float *part = nullptr;
     float2 *part_ml = nullptr;
+    float *prompt_part = nullptr;
+    float2 *prompt_ml = nullptr;
+    int32_t *prompt_arrived = nullptr;
     int32_t *status_host = nullptr;   // pinned
     int max_ctas = 0;
 };
@@ -24,6 +27,7 @@ namespace {
 
 constexpr int kMaxCtasPerSm = 8;
 constexpr int kPartRows = 32;         // rows of a piece, at most
+constexpr int kPromptRows = 32;       // what kv_attend.cu takes in one pass over the keys
 
 size_t elem_size(int dtype) { return dtype == MOE_BF16 ? 2 : 4; }
 bool aligned(const void *p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
@@ -82,7 +86,12 @@ int moe_kv_plan_create(const moe_kv_config_t *cfg, moe_kv_plan_t **out) {
     const size_t part = (size_t)p->max_ctas * attend_part_floats(padded_width(cfg->head_dim)) * sizeof(float);
     const size_t ml = (size_t)p->max_ctas * 2 * kPartRows * sizeof(float2);
     const size_t arrived = ((size_t)p->max_ctas * sizeof(int32_t) + 255) & ~size_t(255);
-    p->bytes = part + ml + arrived + 256;
+    // prompts: pieces of 256 rows, two for each SM
+    const bool prompts = prompt_supported(cfg->dtype, cfg->head_dim);
+    const size_t ppart = prompts ? (size_t)sms * prompt_part_floats(padded_width(cfg->head_dim)) * sizeof(float) : 0;
+    const size_t pml = prompts ? (size_t)sms * prompt_part_rows() * sizeof(float2) : 0;
+    const size_t parrived = ((size_t)sms * sizeof(int32_t) + 255) & ~size_t(255);
+    p->bytes = part + ml + ppart + pml + arrived + parrived + 256;
     void *mem = nullptr;
     if (cudaMalloc(&mem, p->bytes) != cudaSuccess || cudaMallocHost((void **)&p->status_host, 4) != cudaSuccess) {
         cudaGetLastError();
@@ -93,9 +102,13 @@ int moe_kv_plan_create(const moe_kv_config_t *cfg, moe_kv_plan_t **out) {
     p->base = (uint8_t *)mem;
     p->part = (float *)mem;
     p->part_ml = (float2 *)(p->base + part);
-    p->arrived = (int32_t *)(p->base + part + ml);
-    p->status = (int32_t *)(p->base + part + ml + arrived);
-    if (cudaMemset(p->arrived, 0, arrived + 256) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) {
+    p->prompt_part = (float *)(p->base + part + ml);
+    p->prompt_ml = (float2 *)(p->base + part + ml + ppart);
+    uint8_t *words = p->base + part + ml + ppart + pml;
+    p->arrived = (int32_t *)words;
+    p->prompt_arrived = (int32_t *)(words + arrived);
+    p->status = (int32_t *)(words + arrived + parrived);
+    if (cudaMemset(words, 0, arrived + parrived + 256) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) {
         cudaGetLastError();
         moe_kv_plan_destroy(p);
         return MOE_ERR_CUDA;
@@ -230,7 +243,15 @@ int moe_kv_attention(moe_kv_plan_t *p, const moe_kv_rows_t *q, int32_t T, const 
     a.score_scale = (float)((double)softmax_scale * k_scale * 1.4426950408889634);
     a.v_scale = v_scale; a.window = window; a.sinks = sinks; a.out = out;
     a.part = p->part; a.part_ml = p->part_ml; a.arrived = p->arrived; a.max_ctas = p->max_ctas; a.status = p->status;
-    return done(launch_attend_rows(a, p->sm_count, (cudaStream_t)stream, &p->launches));
+    a.prompt_part = p->prompt_part; a.prompt_ml = p->prompt_ml; a.prompt_arrived = p->prompt_arrived;
+    cudaStream_t s = (cudaStream_t)stream;
+    const long long rows = (long long)(max_new > 0 && max_new < T ? max_new : T) * a.G;
+    a.prompt_rows = prompt_supported(c.dtype, c.head_dim) && rows > kPromptRows ? kPromptRows : 0;
+    if (a.prompt_rows > 0) {
+        const cudaError_t err = launch_attend_prompt(a, p->sm_count, s, &p->launches);
+        if (err != cudaSuccess) return done(err);
+    }
+    return done(launch_attend_rows(a, p->sm_count, s, &p->launches));
 }
 
 }  // extern "C"

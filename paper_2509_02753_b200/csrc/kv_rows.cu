@@ -43,8 +43,6 @@ __global__ void rope_table_kernel(RopeTableArgs a) {
 // ------------------------------------------------------------------ elements
 __device__ __forceinline__ float to_f(float v) { return v; }
 __device__ __forceinline__ float to_f(__nv_bfloat16 v) { return __bfloat162float(v); }
-__device__ __forceinline__ void put(float *p, float v) { *p = v; }
-__device__ __forceinline__ void put(__nv_bfloat16 *p, float v) { *p = __float2bfloat16_rn(v); }
 
 // 8 neighbouring elements; VEC: 16-byte aligned
 template <bool VEC>
@@ -91,7 +89,7 @@ __device__ __forceinline__ void store8(__nv_bfloat16 *p, int n, const float (&v)
         *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) if (i < n) put(p + i, v[i]);
+        for (int i = 0; i < 8; ++i) if (i < n) p[i] = __float2bfloat16_rn(v[i]);
     }
 }
 
