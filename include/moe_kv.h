@@ -173,7 +173,7 @@ int moe_kv_read(moe_kv_plan_t *plan, const void *cache, int32_t n_pages, const i
  * Products in 16 bits with fp32 sums for bf16 (the stored numbers are exact there; queries are too, the
  * softmax weights have 11 bits); for fp32 queries and weights are split in two 16-bit parts.
  * A page number outside the cache sets BAD_INDEX and its keys count as absent.
- * Errors: INVALID_ARG, ALIGN, CUDA.
+ * Errors: INVALID_ARG, SHAPE (table_width * page_size above 2^30), ALIGN, CUDA.
  */
 int moe_kv_attention(moe_kv_plan_t *plan, const moe_kv_rows_t *q, int32_t n_tokens, const int32_t *cu_new,
                      const int32_t *kv_len, int32_t n_requests, int32_t max_new, const int32_t *block_table,

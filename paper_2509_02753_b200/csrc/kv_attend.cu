@@ -107,7 +107,7 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
     };
     // blocks that rows [row0, row1) of a request see: [0, sb) and [wb, nb)
     auto visible = [&](int len, int nq, int row0, int row1, int &sb, int &wb, int &nb) {
-        const int p0 = len - nq + row0 / a.G, p1 = len - nq + (row1 - 1) / a.G;
+        const int p0 = len - nq + div_g(a, row0), p1 = len - nq + div_g(a, row1 - 1);
         nb = p1 < 0 ? 0 : p1 / kBlockTokens + 1;
         wb = a.window > 0 ? max(p0 - a.window + 1, 0) / kBlockTokens : 0;
         wb = min(wb, nb);
@@ -254,7 +254,7 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
                 const int row = row0 + n;
                 float v[kPer];
                 const bool real = row < row1;
-                const int tok = row / a.G;
+                const int tok = div_g(a, row);
                 float top = 0.f;
                 const T *src = (const T *)a.q.p + (int64_t)(q0 + (real ? tok : 0)) * a.q.ts + (int64_t)(head * a.G + (real ? row - tok * a.G : 0)) * a.q.hs;
 #pragma unroll
@@ -306,7 +306,7 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
                 f[t][j] = row_scale[t * 8 + 2 * c + j];
             }
         // blocks of the stretch that every row sees whole: [0, sink_clear) and [clear0, clear1)
-        const int p_first = len - nq + row0 / a.G, p_last = len - nq + (row1 - 1) / a.G;
+        const int p_first = len - nq + div_g(a, row0), p_last = len - nq + div_g(a, row1 - 1);
         const int whole1 = max(p_first + 1, 0) / kBlockTokens;                                                    // blocks below are complete
         const int whole0 = a.window > 0 ? (max(p_last - a.window + 1, 0) + kBlockTokens - 1) / kBlockTokens : 0;   // and from here inside the window
         const int sink_clear = min(sb, min(a.sinks / kBlockTokens, whole1));
@@ -567,7 +567,7 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
         auto put = [&](int n, int d, float2 v) {            // row n, dimensions d and d + 1 of the output
             const int row = row0 + n;
             if (row >= row1 || d >= a.D) return;
-            const int tok = row / a.G;
+            const int tok = div_g(a, row);
             T *dst = (T *)a.out + ((int64_t)(q0 + tok) * a.H + head * a.G + row - tok * a.G) * a.D + d;
             if (SPLIT) *reinterpret_cast<float2 *>(dst) = v;
             else *reinterpret_cast<__nv_bfloat162 *>(dst) = __floats2bfloat162_rn(v.x, v.y);

@@ -26,6 +26,7 @@ struct moe_kv_plan {
 namespace {
 
 constexpr int kMaxCtasPerSm = 8;
+constexpr int64_t kMaxContext = 1 << 30;      // tokens that a row of a block table may stand for
 constexpr int kPartRows = 32;         // rows of a piece, at most
 constexpr int kPromptRows = 32;       // what kv_attend.cu takes in one pass over the keys
 
@@ -231,17 +232,20 @@ int moe_kv_attention(moe_kv_plan_t *p, const moe_kv_rows_t *q, int32_t T, const 
                      float v_scale, int32_t window, int32_t sinks, void *out, void *stream) {
     if (!p || T < 0 || T > p->cfg.max_tokens || n < 0 || n > p->cfg.max_requests || max_new < 0 || width < 0 || n_pages < 0 || window < 0 || sinks < 0 ||
         !std::isfinite(softmax_scale) || !good_scale(k_scale) || !good_scale(v_scale)) return MOE_ERR_INVALID_ARG;
-    if (T == 0 || n == 0) return MOE_OK;
     const moe_kv_config_t &c = p->cfg;
+    if ((int64_t)width * c.page_size > kMaxContext) return MOE_ERR_SHAPE;
+    if (T == 0 || n == 0) return MOE_OK;
     if (const int rc = check_rows(q, c.dtype)) return rc;
     if (!cu_new || !kv_len || !out || (width > 0 && !block_table) || (n_pages > 0 && !cache)) return MOE_ERR_INVALID_ARG;
     if (!aligned(cache, 16) || !aligned(out, 16)) return MOE_ERR_ALIGN;
     AttendArgs a{};
     a.dtype = c.dtype; a.q = Rows{q->data, q->token_stride, q->head_stride}; a.T = T; a.cu = cu_new; a.kv_len = kv_len; a.n = n; a.max_new = max_new;
     a.table = block_table; a.width = width; a.cache = (const uint8_t *)cache; a.n_pages = n_pages;
-    a.H = c.n_heads; a.Hk = c.n_kv_heads; a.G = c.n_heads / c.n_kv_heads; a.D = c.head_dim; a.page_shift = c.page_size == 16 ? 0 : c.page_size == 32 ? 1 : c.page_size == 64 ? 2 : 3;
+    a.H = c.n_heads; a.Hk = c.n_kv_heads; a.G = c.n_heads / c.n_kv_heads; a.D = c.head_dim; a.g_mul = (uint32_t)((0x100000000ull + a.G - 1) / a.G); a.page_shift = c.page_size == 16 ? 0 : c.page_size == 32 ? 1 : c.page_size == 64 ? 2 : 3;
     a.score_scale = (float)((double)softmax_scale * k_scale * 1.4426950408889634);
-    a.v_scale = v_scale; a.window = window; a.sinks = sinks; a.out = out;
+    a.v_scale = v_scale; a.out = out;
+    // no position reaches kMaxContext, and sums of these stay below 2^31
+    a.window = window < kMaxContext ? window : (int)kMaxContext; a.sinks = sinks < kMaxContext ? sinks : (int)kMaxContext;
     a.part = p->part; a.part_ml = p->part_ml; a.arrived = p->arrived; a.max_ctas = p->max_ctas; a.status = p->status;
     a.prompt_part = p->prompt_part; a.prompt_ml = p->prompt_ml; a.prompt_arrived = p->prompt_arrived;
     cudaStream_t s = (cudaStream_t)stream;

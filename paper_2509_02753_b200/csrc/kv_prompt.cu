@@ -10,9 +10,9 @@
 // per row and are exact in f16 too; the weights are rounded to f16 (11 bits).
 //
 // Roles: two warpgroups of softmax, one thread a row; one warpgroup that converts; one thread that issues products.  The
-// two tiles alternate: while one's weights are computed the other's products run.  A thread computes a row's weights
-// with the reference it has, and again only if a score passed it (kSlack above the largest one so far): tensor memory
-// is read once a tile and O is rescaled a few times per row.
+// two tiles alternate: while one's weights are computed the other's products run.  A row's scores stay in
+// registers from the search for the largest to the weights; its reference lies kSlack above a score that was once the
+// largest, so O is rescaled a few times per row, not per tile.
 //
 // Bounds: 2 x 256 x 128 x W multiply-adds of a key tile take 2048 cycles at W = 128; its 32768 exponentials take 2048
 // cycles too on the 16 lanes of the special-function units; conversion 384 issue cycles.
@@ -36,6 +36,9 @@ constexpr int kTileBlocks = kTileKeys / kBlockTokens;
 constexpr int kThreads = 512;
 constexpr float kFloor = -FLT_MAX;
 constexpr float kHead = 6.f, kSlack = 8.f;       // as in kv_attend.cu
+// What a stretch costs besides its tiles (queries, output, an empty pipeline), in tiles: counted in the line, or a CTA
+// with many short stretches would be last by far
+constexpr int kEntry = 3;
 
 template <int W>
 struct Shape {
@@ -66,6 +69,38 @@ __device__ __forceinline__ void st32(uint32_t taddr, const uint32_t *r) {
           "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
           "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]) : "memory");
 }
+__device__ __forceinline__ void st16(uint32_t taddr, const uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+          "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
+// two fp32 numbers in one operation
+__device__ __forceinline__ uint64_t pair(float x, float y) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+    return r;
+}
+__device__ __forceinline__ float2 halves(uint64_t v) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
 __device__ __forceinline__ void st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 // D[tmem] (+)= A[tmem] * B[smem]^T, f16
@@ -80,6 +115,9 @@ __host__ __device__ constexpr uint32_t idesc_f16(int n) { return (1u << 4) | ((u
 
 // byte offset of 16-byte chunk c of row r in a swizzled sub-tile of 128-byte rows
 __device__ __forceinline__ uint32_t swizzled(int r, int c) { return (uint32_t)(r * 128 + ((c ^ (r & 7)) << 4)); }
+
+// the lowest n of 32 bits
+__device__ __forceinline__ uint32_t below(int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; }
 
 __device__ __forceinline__ void sts16(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
@@ -128,7 +166,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
     };
     // tiles that rows [row0, row1) see: [0, st) and [wt, nt)
     auto visible = [&](int len, int nq, int row0, int row1, int &st, int &wt, int &nt) {
-        const int p0 = len - nq + row0 / a.G, p1 = len - nq + (row1 - 1) / a.G;
+        const int p0 = len - nq + div_g(a, row0), p1 = len - nq + div_g(a, row1 - 1);
         nt = p1 < 0 ? 0 : p1 / kTileKeys + 1;
         wt = a.window > 0 ? max(p0 - a.window + 1, 0) / kTileKeys : 0;
         wt = min(wt, nt);
@@ -145,7 +183,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
                 for (int row0 = 0; row0 < nq * a.G; row0 += kStretchRows) {
                     int st, wt, nt;
                     visible(len, nq, row0, min(row0 + kStretchRows, nq * a.G), st, wt, nt);
-                    mine += (long long)max(st + nt - wt, 1) * a.Hk;
+                    mine += (long long)(kEntry + max(st + nt - wt, 1)) * a.Hk;
                 }
             }
             long long inc = mine;
@@ -168,36 +206,60 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
     tc::tc_fence_after();
     const uint32_t tmem = tmem_slot;
     const long long total = line[a.n], share = max((total + gridDim.x - 1) / (long long)gridDim.x, 1ll);
-    long long at = min(share * blockIdx.x, total);
+    const long long at = min(share * blockIdx.x, total);
     const long long end = min(at + share, total);
 
-    struct Piece { int len, q0, nq, req, row0, row1, st, wt, units, present, head, first, last, cta0, cta1; };
-    auto piece_at = [&](long long x) {
-        Piece p;
+    // A stretch's place in the line is kEntry (what beginning it costs) and then its tiles.  Every role walks the pieces
+    // of the CTA's share by itself: found once, then counted on.
+    struct Piece { int req, len, q0, nq, row0, row1, st, wt, present, units, head, first, last, cta0, cta1; long long place; };
+    auto shape = [&](Piece &p) {
+        p.row1 = min(p.row0 + kStretchRows, p.nq * a.G);
+        int nt;
+        visible(p.len, p.nq, p.row0, p.row1, p.st, p.wt, nt);
+        p.present = p.st + nt - p.wt;
+        p.units = max(p.present, 1);
+    };
+    auto cut = [&](Piece &p) {          // which tiles of the stretch are this CTA's; false: behind the share
+        const long long tiles0 = p.place + kEntry;
+        p.first = (int)max(at - tiles0, 0ll);
+        p.last = (int)min(end - tiles0, (long long)p.units);
+        p.cta0 = (int)(tiles0 / share);
+        p.cta1 = (int)((tiles0 + p.units - 1) / share);
+        return p.place < end;
+    };
+    auto begin = [&](Piece &p) {
+        if (at >= end) return false;
         int lo = 0, hi = a.n;
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
-            if (line[mid] <= x) lo = mid; else hi = mid;
+            if (line[mid] <= at) lo = mid; else hi = mid;
         }
         p.req = lo;
         lengths(lo, p.len, p.q0, p.nq);
-        long long off = x - line[lo];
-        int nt;
+        p.place = line[lo];
         for (p.row0 = 0;; p.row0 += kStretchRows) {
-            p.row1 = min(p.row0 + kStretchRows, p.nq * a.G);
-            visible(p.len, p.nq, p.row0, p.row1, p.st, p.wt, nt);
-            p.units = max(p.st + nt - p.wt, 1);
-            const long long here = (long long)p.units * a.Hk;
-            if (off < here) break;
-            off -= here;
+            shape(p);
+            const long long here = (long long)(kEntry + p.units) * a.Hk;
+            if (at < p.place + here) break;
+            p.place += here;
         }
-        p.present = p.st + nt - p.wt;
-        p.head = (int)(off / p.units);
-        p.first = (int)(off - (long long)p.head * p.units);
-        p.last = (int)min((long long)p.units, p.first + end - x);
-        p.cta0 = (int)((x - p.first) / share);
-        p.cta1 = (int)((x - p.first + p.units - 1) / share);
-        return p;
+        p.head = (int)((at - p.place) / (kEntry + p.units));
+        p.place += (long long)p.head * (kEntry + p.units);
+        return cut(p);
+    };
+    auto next = [&](Piece &p) {
+        p.place += kEntry + p.units;
+        if (p.place >= end) return false;
+        if (++p.head == a.Hk) {
+            p.head = 0;
+            p.row0 += kStretchRows;
+            while (p.row0 >= p.nq * a.G) {          // the line goes on, so there is a request with rows
+                lengths(++p.req, p.len, p.q0, p.nq);
+                p.row0 = 0;
+            }
+            shape(p);
+        }
+        return cut(p);
     };
     bool dead = false;       // a wait ran out: nothing more is waited for or issued, the loops run out
     auto wait = [&](uint32_t b, uint32_t parity) { if (!dead) dead = !tc::mbar_wait(b, parity, a.status); };
@@ -214,8 +276,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
         uint2 ks, ksn, vs, vsn;
         uint32_t vc[kVWords], vn[kVWords];
         int it = 0;                                                           // tiles so far, over all pieces
-        while (at < end) {
-            const Piece p = piece_at(at);
+        Piece p;
+        for (bool more = begin(p); more; more = next(p)) {
+            if (p.last <= p.first) continue;
             const int32_t *table = a.table + (int64_t)p.req * a.width;
             const int blocks = (p.len + kBlockTokens - 1) / kBlockTokens;
             const int n = min(p.last, p.present) - p.first;
@@ -337,7 +400,6 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
                 for (int i = 0; i < kVWords; ++i) vc[i] = vn[i];
                 ks = ksn; vs = vsn;
             }
-            at += p.last - p.first;
         }
     } else if (group == 3) {
         // ================================================================ products
@@ -345,19 +407,21 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
         if (warp == 12 && lane == 0) {
             int it = 0;
             uint32_t p_phase = 0;                  // bit t
-            const uint32_t q_s = smem_u32(smem + S::kQAt);
+            // a k16 step is 32 bytes inside a 128-byte row (2 in a descriptor's units of 16), 64 elements are a sub-tile
+            const uint64_t q_d = tc::make_kmajor_sw128_desc(smem_u32(smem + S::kQAt)), k_d = tc::make_kmajor_sw128_desc(smem_u32(smem + S::kKAt)),
+                           v_d = tc::make_kmajor_sw128_desc(smem_u32(smem + S::kVAt));
             auto scores = [&](int t, int stage) {
                 if (dead) return;
+                uint64_t da = q_d + t * (S::kQTile / 16), db = k_d + stage * (S::kKTile / 16);
+#pragma unroll 1
+                for (int sub = 0; sub < W / 64; ++sub, da += kTileRows * 128 / 16, db += kTileKeys * 128 / 16)
 #pragma unroll
-                for (int i = 0; i < W / 16; ++i) {
-                    const uint64_t da = tc::make_kmajor_sw128_desc(q_s + t * S::kQTile + (i / 4) * (kTileRows * 128)) + 2 * (i % 4);
-                    const uint64_t db = tc::make_kmajor_sw128_desc(smem_u32(smem + S::kKAt) + stage * S::kKTile + (i / 4) * (kTileKeys * 128)) + 2 * (i % 4);
-                    tc::umma_bf16(tmem + S::kS + t * kTileKeys, da, db, idesc_f16(kTileKeys), i > 0);
-                }
+                    for (int i = 0; i < 4; ++i) tc::umma_bf16(tmem + S::kS + t * kTileKeys, da + 2 * i, db + 2 * i, idesc_f16(kTileKeys), sub + i > 0);
                 tc::umma_commit(s_full(t));
             };
-            while (at < end) {
-                const Piece p = piece_at(at);
+            Piece p;
+            for (bool more = begin(p); more; more = next(p)) {
+                if (p.last <= p.first) continue;
                 const int n = min(p.last, p.present) - p.first;
                 const int tiles = p.row1 - p.row0 > kTileRows ? 2 : 1;
                 if (n > 0) {
@@ -371,29 +435,29 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
                     if (!dead) tc::umma_commit(k_empty(it & 1));
                 }
                 for (int j = 0; j < n; ++j, ++it) {
-                    const int stage = it & 1, next = stage ^ 1;
+                    const int stage = it & 1, other = stage ^ 1;
                     wait(v_full(stage), (it >> 1) & 1);
-                    if (j + 1 < n) wait(k_full(next), ((it + 1) >> 1) & 1);
+                    if (j + 1 < n) wait(k_full(other), ((it + 1) >> 1) & 1);
                     for (int t = 0; t < tiles; ++t) {
                         wait(p_full(t), (p_phase >> t) & 1u);          // the weights are there, the scores are read
                         p_phase ^= 1u << t;
                         tc::tc_fence_after();
                         if (!dead) {
+                            uint64_t db = v_d + stage * (S::kVTile / 16);
+                            uint32_t pa = tmem + S::kS + t * kTileKeys;
+#pragma unroll 1
+                            for (int sub = 0; sub < 2; ++sub, db += W * 128 / 16, pa += 32)
 #pragma unroll
-                            for (int i = 0; i < kTileKeys / 16; ++i) {
-                                const uint64_t db = tc::make_kmajor_sw128_desc(smem_u32(smem + S::kVAt) + stage * S::kVTile + (i / 4) * (W * 128)) + 2 * (i % 4);
-                                umma_ts(tmem + S::kO + t * W, tmem + S::kS + t * kTileKeys + 8 * i, db, idesc_f16(W), j > 0 || i > 0);
-                            }
+                                for (int i = 0; i < 4; ++i) umma_ts(tmem + S::kO + t * W, pa + 8 * i, db + 2 * i, idesc_f16(W), j + sub + i > 0);
                             tc::umma_commit(o_full(t));
                         }
-                        if (j + 1 < n) scores(t, next);
+                        if (j + 1 < n) scores(t, other);
                     }
                     if (!dead) {
                         tc::umma_commit(v_empty(stage));
-                        if (j + 1 < n) tc::umma_commit(k_empty(next));
+                        if (j + 1 < n) tc::umma_commit(k_empty(other));
                     }
                 }
-                at += p.last - p.first;
             }
         }
         __syncwarp();
@@ -405,56 +469,61 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
         const uint32_t s_tmem = tmem + S::kS + t * kTileKeys + lanes, o_tmem = tmem + S::kO + t * W + lanes;
         uint32_t s_phase = 0, o_phase = 0;
         int it = 0;
-        while (at < end) {
-            const Piece p = piece_at(at);
+        Piece p;
+        for (bool more = begin(p); more; more = next(p)) {
+            if (p.last <= p.first) continue;
             const int n = min(p.last, p.present) - p.first;
             const int tiles = p.row1 - p.row0 > kTileRows ? 2 : 1;
             const int row = p.row0 + t * kTileRows + row_in;
             const bool real = row < p.row1;
-            const int tok = row / a.G, pos = real ? p.len - p.nq + tok : -1;
+            const int tok = div_g(a, row), pos = real ? p.len - p.nq + tok : -1;
             const int64_t out_row = (int64_t)(p.q0 + tok) * a.H + p.head * a.G + row - tok * a.G;
             float m = kFloor, l = 0.f, f = 0.f;
             if (t < tiles && n > 0) {
-                // ---- queries: a power of two per row makes them f16
-                const __nv_bfloat16 *src = (const __nv_bfloat16 *)a.q.p + (int64_t)(p.q0 + tok) * a.q.ts + (int64_t)(p.head * a.G + row - tok * a.G) * a.q.hs;
+                // ---- queries: a power of two per row makes them f16.  W/8 lanes take a row, 16 bytes each
+                constexpr int kLanes = W / 8, kAtOnce = 32 / kLanes;
                 const bool vec = (reinterpret_cast<uintptr_t>(a.q.p) & 15u) == 0 && ((a.q.ts | a.q.hs) & 7) == 0;
-                uint32_t q[W / 2];
-                float top = 0.f;
-#pragma unroll
-                for (int i = 0; i < W / 8; ++i) {
-                    uint4 x = make_uint4(0u, 0u, 0u, 0u);
-                    if (real && 8 * i < a.D) {
-                        if (vec) x = *reinterpret_cast<const uint4 *>(src + 8 * i);
+                const int64_t q_row = real ? (int64_t)(p.q0 + tok) * a.q.ts + (int64_t)(p.head * a.G + row - tok * a.G) * a.q.hs : INT64_MIN;
+                const int chunk = lane % kLanes;
+                const uint32_t dst = smem_u32(smem + S::kQAt) + t * S::kQTile + (chunk / 8) * (kTileRows * 128);
+#pragma unroll 4
+                for (int x = 0; x < 32 / kAtOnce; ++x) {
+                    const int r = x * kAtOnce + lane / kLanes;             // of the warp's 32 rows
+                    const int64_t at_row = __shfl_sync(0xffffffffu, q_row, r);
+                    const __nv_bfloat16 *src = (const __nv_bfloat16 *)a.q.p + at_row + 8 * chunk;
+                    uint4 q = make_uint4(0u, 0u, 0u, 0u);
+                    if (at_row != INT64_MIN && 8 * chunk < a.D) {
+                        if (vec) q = __ldg(reinterpret_cast<const uint4 *>(src));
                         else {
                             uint32_t w[4];
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) w[e] = (uint32_t)__bfloat16_as_ushort(src[8 * i + 2 * e]) | (uint32_t)__bfloat16_as_ushort(src[8 * i + 2 * e + 1]) << 16;
-                            x = make_uint4(w[0], w[1], w[2], w[3]);
+                            for (int e = 0; e < 4; ++e) w[e] = (uint32_t)__bfloat16_as_ushort(src[2 * e]) | (uint32_t)__bfloat16_as_ushort(src[2 * e + 1]) << 16;
+                            q = make_uint4(w[0], w[1], w[2], w[3]);
                         }
                     }
-                    q[4 * i] = x.x; q[4 * i + 1] = x.y; q[4 * i + 2] = x.z; q[4 * i + 3] = x.w;
-                }
+                    const uint32_t qw[4] = {q.x, q.y, q.z, q.w};
+                    float top = 0.f;
 #pragma unroll
-                for (int i = 0; i < W / 2; ++i) top = fmaxf(top, fmaxf(fabsf(__uint_as_float(q[i] << 16)), fabsf(__uint_as_float(q[i] & 0xffff0000u))));
-                int e = top > 0.f && top <= FLT_MAX ? ilogbf(top) : 0;
-                e = max(e, -100);
-                const float up = ldexpf(a.score_scale < 0.f ? -1.f : 1.f, 10 - e);
-                f = fmaxf(ldexpf(fabsf(a.score_scale), e - 10), 1e-30f);      // not 0, which times a masked -infinity is no number
-                const uint32_t dst = smem_u32(smem + S::kQAt) + t * S::kQTile;
+                    for (int e = 0; e < 4; ++e) top = fmaxf(top, fmaxf(fabsf(__uint_as_float(qw[e] << 16)), fabsf(__uint_as_float(qw[e] & 0xffff0000u))));
 #pragma unroll
-                for (int i = 0; i < W / 8; ++i) {
+                    for (int o = kLanes / 2; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                    int e2 = top > 0.f && top <= FLT_MAX ? ilogbf(top) : 0;
+                    e2 = max(e2, -100);
+                    const float up = ldexpf(a.score_scale < 0.f ? -1.f : 1.f, 10 - e2);
+                    const int mine = __shfl_sync(0xffffffffu, e2, (lane % kAtOnce) * kLanes);
+                    if (lane / kAtOnce == x) f = fmaxf(ldexpf(fabsf(a.score_scale), mine - 10), 1e-30f);      // not 0, which times a masked -infinity is no number
                     uint32_t h[4];
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) h[x] = pack2(__uint_as_float(q[4 * i + x] << 16) * up, __uint_as_float(q[4 * i + x] & 0xffff0000u) * up);
-                    sts16(dst + (i / 8) * (kTileRows * 128) + swizzled(row_in, i % 8), h[0], h[1], h[2], h[3]);
+                    for (int e = 0; e < 4; ++e) h[e] = pack2(__uint_as_float(qw[e] << 16) * up, __uint_as_float(qw[e] & 0xffff0000u) * up);
+                    sts16(dst + swizzled(wl + r, chunk % 8), h[0], h[1], h[2], h[3]);
                 }
                 fence_async();
                 tc::tc_fence_before();
                 __syncwarp();
                 if (lane == 0) tc::mbar_arrive(p_full(t));
 
-                const int p_first = p.len - p.nq + (p.row0 + t * kTileRows) / a.G;
-                const int p_last = p.len - p.nq + (min(p.row0 + (t + 1) * kTileRows, p.row1) - 1) / a.G;
+                const int p_first = p.len - p.nq + div_g(a, p.row0 + t * kTileRows);
+                const int p_last = p.len - p.nq + div_g(a, min(p.row0 + (t + 1) * kTileRows, p.row1) - 1);
                 for (int j = 0; j < n; ++j) {
                     const int u = p.first + j, key0 = (u < p.st ? u : p.wt + u - p.st) * kTileKeys;
                     wait(s_full(t), s_phase);
@@ -463,62 +532,94 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
                     const uint32_t gone = reinterpret_cast<volatile uint32_t *>(absent)[(it + j) & 3];
                     const bool clear = key0 + kTileKeys - 1 <= p_first && gone == 0u &&
                                        (a.window <= 0 || p_last - key0 < a.window || key0 + kTileKeys <= a.sinks);
-                    uint32_t w[kTileKeys / 2];
-                    float sum = 0.f, top = kFloor;
-                    auto weights = [&](float mm) {          // P with the reference mm, its sum, the largest exponent
-                        float s0 = 0.f, s1 = 0.f;
-                        const float away = (kHead + kSlack) - mm;
-                        top = -INFINITY;
-#pragma unroll
+                    // Code size counts: four roles run at once out of one instruction cache.  Masks (of the first and last
+                    // tiles only) are a pass of their own over the scores, the weights are one copy of code.
+                    if (!clear) {
+#pragma unroll 1
                         for (int c = 0; c < kTileKeys / 32; ++c) {
                             uint32_t r[32];
                             ld32(s_tmem + 32 * c, r);
                             tc::tmem_ld_wait();
-                            if (!clear) {
+                            // keys key0 + 32 c + i that the row sees, i = 0..31
+                            const int k0 = key0 + 32 * c;
+                            uint32_t see = below(pos + 1 - k0);
+                            if (a.window > 0) see &= ~below(pos - a.window + 1 - k0) | below(a.sinks - k0);
+                            const uint32_t out = (gone >> (10 * c)) & 3u;          // byte c, bits 2c and 2c + 1: blocks that are absent
+                            see &= ~((out & 1u ? 0xffffu : 0u) | (out & 2u ? 0xffff0000u : 0u));
 #pragma unroll
-                                for (int i = 0; i < 32; ++i) {
-                                    const int key = key0 + 32 * c + i;
-                                    const bool see = key <= pos && (a.window <= 0 || pos - key < a.window || key < a.sinks) &&
-                                                     !(gone >> (((2 * c + i / 16) >> 1) * 8 + ((2 * c + i / 16) >> 1) * 2 + ((2 * c + i / 16) & 1)) & 1u);
-                                    if (!see) r[i] = 0xff800000u;      // -infinity
-                                }
-                            }
-#pragma unroll
-                            for (int i = 0; i < 32; i += 2) {
-                                const float x = __uint_as_float(r[i]), y = __uint_as_float(r[i + 1]);
-                                top = fmaxf(top, fmaxf(x, y));
-                                const float e0 = ex2(fmaf(x, f, away)), e1 = ex2(fmaf(y, f, away));
-                                s0 += e0; s1 += e1;
-                                w[16 * c + i / 2] = pack2(e0, e1);
-                            }
+                            for (int i = 0; i < 32; ++i) r[i] = see >> i & 1u ? r[i] : 0xff800000u;      // -infinity
+                            st32(s_tmem + 32 * c, r);
                         }
-                        sum = s0 + s1;
+                        st_wait();
+                    }
+                    // ---- the row's largest score.  Loops stay rolled: the roles' straight code would not fit the
+                    // instruction caches (1.4 times the time when it did not)
+                    uint32_t ra[32], rb[32];
+                    float top0 = -INFINITY, top1 = -INFINITY, top2 = -INFINITY, top3 = -INFINITY;
+                    auto largest = [&](const uint32_t (&r)[32]) {
+#pragma unroll
+                        for (int i = 0; i < 32; i += 8) {
+                            top0 = max3(top0, __uint_as_float(r[i]), __uint_as_float(r[i + 1]));
+                            top1 = max3(top1, __uint_as_float(r[i + 2]), __uint_as_float(r[i + 3]));
+                            top2 = max3(top2, __uint_as_float(r[i + 4]), __uint_as_float(r[i + 5]));
+                            top3 = max3(top3, __uint_as_float(r[i + 6]), __uint_as_float(r[i + 7]));
+                        }
                     };
-                    weights(m);
-                    const float reach = top == -INFINITY ? -INFINITY : top * f;
-                    if (__any_sync(0xffffffffu, reach > m)) {
+                    ld32(s_tmem, ra);
+                    tc::tmem_ld_wait();
+#pragma unroll 1
+                    for (int c = 0; c < kTileKeys / 64; ++c) {
+                        ld32(s_tmem + 64 * c + 32, rb);
+                        largest(ra);
+                        tc::tmem_ld_wait();
+                        ld32(s_tmem + ((64 * c + 64) & (kTileKeys - 1)), ra);        // behind the last: the first again, for the weights
+                        largest(rb);
+                        tc::tmem_ld_wait();
+                    }
+                    const float top = fmaxf(fmaxf(top0, top1), fmaxf(top2, top3)), reach = top == -INFINITY ? -INFINITY : top * f;
+                    if (__any_sync(0xffffffffu, reach > m)) {       // O follows only when a score passes the reference
                         const float to = fmaxf(m, reach == -INFINITY ? kFloor : reach + kSlack);
                         const float scale = m == to ? 1.f : ex2(m - to);
                         if (j > 0) {
                             wait(o_full(t), o_phase ^ 1u);       // the products of the tile before
                             tc::tc_fence_after();
-#pragma unroll
-                            for (int c = 0; c < W / 32; ++c) {
-                                uint32_t r[32];
-                                ld32(o_tmem + 32 * c, r);
+#pragma unroll 1
+                            for (int c = 0; c < W / 16; ++c) {
+                                uint32_t x[16];
+                                tc::tmem_ld16(o_tmem + 16 * c, x);
                                 tc::tmem_ld_wait();
 #pragma unroll
-                                for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * scale);
-                                st32(o_tmem + 32 * c, r);
+                                for (int i = 0; i < 16; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * scale);
+                                st16(o_tmem + 16 * c, x);
                             }
                         }
                         l *= scale;
                         m = to;
-                        weights(m);
                     }
-                    l += sum;
-                    st32(s_tmem, w);
-                    st32(s_tmem + 32, w + 32);
+                    // ---- weights: 32 scores become 16 columns
+                    const uint64_t f2 = pair(f, f), away2 = pair((kHead + kSlack) - m, (kHead + kSlack) - m);
+                    uint64_t sum2 = 0ull;
+                    auto weights = [&](const uint32_t (&r)[32], int c) {
+                        uint32_t w[16];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const float2 x = halves(fma2(pair(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1])), f2, away2));
+                            const float e0 = ex2(x.x), e1 = ex2(x.y);
+                            sum2 = add2(sum2, pair(e0, e1));
+                            w[i] = pack2(e0, e1);
+                        }
+                        st16(s_tmem + 16 * c, w);
+                    };
+#pragma unroll 1
+                    for (int c = 0; c < kTileKeys / 64; ++c) {
+                        ld32(s_tmem + 64 * c + 32, rb);
+                        weights(ra, 2 * c);
+                        tc::tmem_ld_wait();
+                        if (c == 0) ld32(s_tmem + 64, ra);
+                        weights(rb, 2 * c + 1);
+                        tc::tmem_ld_wait();
+                    }
+                    l += halves(sum2).x + halves(sum2).y;
                     st_wait();
                     tc::tc_fence_before();
                     __syncwarp();
@@ -533,32 +634,49 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
             // ---- the rows' outputs, or this piece of them
             const bool whole = p.first == 0 && p.last == p.units;
             const int slot = blockIdx.x * 2 + (p.first == 0 ? 1 : 0);
-            const int in_stretch = t * kTileRows + row_in;
             if (t < tiles) {
+                // the rows go through the queries' place in shared memory (their products are done), so that 16 (8) lanes
+                // store a row's 256 (128) bytes: all of W dimensions as bf16, or 64 (32) of a piece as fp32
+                constexpr int kLanes = W / 8, kAtOnce = 32 / kLanes, kPass = W / 2;
                 const float k = whole ? (l > 0.f || l != l ? a.v_scale / l : 0.f) : 1.f;
-                __nv_bfloat16 *dst = (__nv_bfloat16 *)a.out + out_row * a.D;
-                float *part = a.prompt_part + ((int64_t)slot * kStretchRows + in_stretch) * W;
-#pragma unroll
-                for (int c = 0; c < W / 32; ++c) {
-                    uint32_t r[32];
+                const uint32_t place = smem_u32(smem + S::kQAt) + t * S::kQTile;
+                auto slot16 = [&](int r, int c) { return place + (c / 8) * (kTileRows * 128) + swizzled(wl + r, c % 8); };
+                const int chunk = lane % kLanes;
+                const int64_t to_row = real ? out_row * a.D : -1;
+                float *part = a.prompt_part + ((int64_t)slot * kStretchRows + t * kTileRows + wl) * W;
+#pragma unroll 1
+                for (int pass = 0; pass < (whole ? 1 : 2); ++pass) {
                     __syncwarp();
-                    if (n > 0) { ld32(o_tmem + 32 * c, r); tc::tmem_ld_wait(); }
+#pragma unroll 1
+                    for (int c = 0; c < (whole ? W : kPass) / 16; ++c) {
+                        uint32_t r[16];
+                        if (n > 0) { tc::tmem_ld16(o_tmem + pass * kPass + 16 * c, r); tc::tmem_ld_wait(); }
+                        else {
 #pragma unroll
-                    for (int i = 0; i < 32; i += 8) {
-                        float v[8];
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) v[e] = n > 0 ? __uint_as_float(r[i + e]) * k : 0.f;
-                        if (!real) continue;
-                        if (whole) {
-                            if (32 * c + i < a.D)
-                                *reinterpret_cast<uint4 *>(dst + 32 * c + i) = make_uint4(bf2(v[0], v[1]), bf2(v[2], v[3]), bf2(v[4], v[5]), bf2(v[6], v[7]));
-                        } else {
-                            *reinterpret_cast<float4 *>(part + 32 * c + i) = make_float4(v[0], v[1], v[2], v[3]);
-                            *reinterpret_cast<float4 *>(part + 32 * c + i + 4) = make_float4(v[4], v[5], v[6], v[7]);
+                            for (int i = 0; i < 16; ++i) r[i] = 0u;
                         }
+                        if (whole) {
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) r[i] = bf2(__uint_as_float(r[2 * i]) * k, __uint_as_float(r[2 * i + 1]) * k);
+                        }
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (i < 2 || !whole) sts16(slot16(lane, (whole ? 2 : 4) * c + i), r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]);
+                    }
+                    __syncwarp();
+#pragma unroll 4
+                    for (int x = 0; x < 32 / kAtOnce; ++x) {
+                        const int r = x * kAtOnce + lane / kLanes;
+                        const int64_t to = __shfl_sync(0xffffffffu, to_row, r);
+                        uint4 v;
+                        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(slot16(r, chunk)));
+                        if (to == -1) continue;
+                        if (!whole) *reinterpret_cast<uint4 *>(part + r * W + pass * kPass + 4 * chunk) = v;
+                        else if (8 * chunk < a.D) *reinterpret_cast<uint4 *>((__nv_bfloat16 *)a.out + to + 8 * chunk) = v;
                     }
                 }
-                if (!whole && real) a.prompt_ml[(int64_t)slot * kStretchRows + in_stretch] = make_float2(m, l);
+                __syncwarp();
+                if (!whole && real) a.prompt_ml[(int64_t)slot * kStretchRows + t * kTileRows + row_in] = make_float2(m, l);
             }
             tc::tc_fence_before();
             if (!whole) {
@@ -570,33 +688,61 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
                     if (last_s) a.prompt_arrived[p.cta0] = 0;          // ready for the next call
                 }
                 asm volatile("bar.sync 1, 256;" ::: "memory");
-                if (last_s && t < tiles && real) {
+                if (last_s) {
                     __threadfence();
-                    float top = kFloor, sum = 0.f;
-                    for (int b = p.cta0; b <= p.cta1; ++b)
-                        top = fmaxf(top, __ldcg(&a.prompt_ml[(int64_t)(b * 2 + (b == p.cta0)) * kStretchRows + in_stretch]).x);
-                    for (int b = p.cta0; b <= p.cta1; ++b) {
-                        const float2 ml = __ldcg(&a.prompt_ml[(int64_t)(b * 2 + (b == p.cta0)) * kStretchRows + in_stretch]);
-                        sum += (ml.x == top ? 1.f : ex2(ml.x - top)) * ml.y;
-                    }
-                    const float k = sum > 0.f || sum != sum ? a.v_scale / sum : 0.f;
-                    __nv_bfloat16 *dst = (__nv_bfloat16 *)a.out + out_row * a.D;
-                    for (int d = 0; d < a.D; d += 8) {
-                        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-                        for (int b = p.cta0; b <= p.cta1; ++b) {
-                            const int64_t at_row = (int64_t)(b * 2 + (b == p.cta0)) * kStretchRows + in_stretch;
-                            const float mb = __ldcg(&a.prompt_ml[at_row]).x, kb = (mb == top ? 1.f : ex2(mb - top)) * k;
-                            const float4 x = __ldcg(reinterpret_cast<const float4 *>(a.prompt_part + at_row * W + d));
-                            const float4 y = __ldcg(reinterpret_cast<const float4 *>(a.prompt_part + at_row * W + d + 4));
-                            v[0] += kb * x.x; v[1] += kb * x.y; v[2] += kb * x.z; v[3] += kb * x.w;
-                            v[4] += kb * y.x; v[5] += kb * y.y; v[6] += kb * y.z; v[7] += kb * y.w;
+                    // a warp takes rows warp, warp + 8, ..., a lane W/32 neighbouring dimensions: whole lines, 8 rows in flight
+                    constexpr int kPer = W / 32, kRowsAtOnce = 8;
+                    const int rows = p.row1 - p.row0;
+#pragma unroll 1
+                    for (int x0 = warp; x0 < rows; x0 += 8 * kRowsAtOnce) {
+                        float top[kRowsAtOnce], sum[kRowsAtOnce], v[kRowsAtOnce][kPer];
+#pragma unroll
+                        for (int y = 0; y < kRowsAtOnce; ++y) {
+                            top[y] = kFloor; sum[y] = 0.f;
+#pragma unroll
+                            for (int e = 0; e < kPer; ++e) v[y][e] = 0.f;
                         }
-                        *reinterpret_cast<uint4 *>(dst + d) = make_uint4(bf2(v[0], v[1]), bf2(v[2], v[3]), bf2(v[4], v[5]), bf2(v[6], v[7]));
+#pragma unroll 1
+                        for (int b = p.cta0; b <= p.cta1; ++b) {
+                            const int64_t at_piece = (int64_t)(b * 2 + (b == p.cta0)) * kStretchRows;
+                            float2 ml[kRowsAtOnce];
+                            float d[kRowsAtOnce][kPer];
+#pragma unroll
+                            for (int y = 0; y < kRowsAtOnce; ++y) {
+                                const int64_t at_row = at_piece + min(x0 + 8 * y, rows - 1);
+                                ml[y] = __ldcg(&a.prompt_ml[at_row]);
+                                const float *src = a.prompt_part + at_row * W + lane * kPer;
+                                if (kPer == 4) {
+                                    const float4 z = __ldcg(reinterpret_cast<const float4 *>(src));
+                                    d[y][0] = z.x; d[y][1] = z.y; d[y][2 % kPer] = z.z; d[y][3 % kPer] = z.w;
+                                } else {
+                                    const float2 z = __ldcg(reinterpret_cast<const float2 *>(src));
+                                    d[y][0] = z.x; d[y][1] = z.y;
+                                }
+                            }
+#pragma unroll
+                            for (int y = 0; y < kRowsAtOnce; ++y) {
+                                const float to = fmaxf(top[y], ml[y].x), old = top[y] == to ? 1.f : ex2(top[y] - to), k = ml[y].x == to ? 1.f : ex2(ml[y].x - to);
+                                sum[y] = sum[y] * old + ml[y].y * k;
+#pragma unroll
+                                for (int e = 0; e < kPer; ++e) v[y][e] = v[y][e] * old + d[y][e] * k;
+                                top[y] = to;
+                            }
+                        }
+#pragma unroll
+                        for (int y = 0; y < kRowsAtOnce; ++y) {
+                            const int x = x0 + 8 * y;
+                            if (x >= rows || lane * kPer >= a.D) continue;
+                            const float k = sum[y] > 0.f || sum[y] != sum[y] ? a.v_scale / sum[y] : 0.f;
+                            const int r_tok = div_g(a, p.row0 + x);
+                            uint32_t *dst = reinterpret_cast<uint32_t *>((__nv_bfloat16 *)a.out + ((int64_t)(p.q0 + r_tok) * a.H + p.head * a.G + p.row0 + x - r_tok * a.G) * a.D + lane * kPer);
+#pragma unroll
+                            for (int e = 0; e < kPer; e += 2) dst[e / 2] = bf2(v[y][e] * k, v[y][e + 1] * k);
+                        }
                     }
                 }
                 asm volatile("bar.sync 1, 256;" ::: "memory");       // last_s is the next piece's
             }
-            at += p.last - p.first;
         }
     }
     tc::tc_fence_before();
