@@ -265,13 +265,11 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
                 }
 #pragma unroll
                 for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-                // 2^e <= top < 2^(e+1): times 2^(10-e) the row lies below 2^11, its f16 parts are exact down to 2^-34 of its top
-                int e = top > 0.f && top <= FLT_MAX ? ilogbf(top) : 0;
-                e = max(e, -100);
-                const float up = ldexpf(1.f, 10 - e);
+                const int e = row_exponent(top);
+                const float up = power2(10 - e);
                 if (lane == 0) {
                     row_pos[n] = real ? len - nq + tok : -1;
-                    row_scale[n] = ldexpf(a.score_scale, e - 10);
+                    row_scale[n] = a.score_scale * power2(e - 10);
                 }
 #pragma unroll
                 for (int i = 0; i < kPer; i += 2) {

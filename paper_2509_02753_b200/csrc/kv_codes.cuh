@@ -40,6 +40,13 @@ __device__ __forceinline__ uint32_t bf2(float lo, float hi) {
     const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t *>(&h);
 }
+// e with 2^e <= top < 2^(e+1), not below -100; 0 for 0 and for what is not finite.  A row times 2^(10 - e) lies below
+// 2^11: its f16 numbers are exact down to 2^-35 of its top
+__device__ __forceinline__ int row_exponent(float top) {
+    const int e = (int)(__float_as_uint(top) >> 23 & 0xffu) - 127;
+    return top > 0.f && e < 128 ? max(e, -100) : 0;
+}
+__device__ __forceinline__ float power2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }      // -126 <= e <= 127
 
 }  // namespace kv
 }  // namespace lexi

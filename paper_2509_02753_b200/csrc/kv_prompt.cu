@@ -123,6 +123,10 @@ __device__ __forceinline__ void sts16(uint32_t at, uint32_t a, uint32_t b, uint3
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
 
+__device__ __forceinline__ void lds16(uint32_t at, uint32_t (&v)[4]) {
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(at) : "memory");
+}
+
 template <int W>
 __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a) {
     using S = Shape<W>;
@@ -480,42 +484,47 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
             const int64_t out_row = (int64_t)(p.q0 + tok) * a.H + p.head * a.G + row - tok * a.G;
             float m = kFloor, l = 0.f, f = 0.f;
             if (t < tiles && n > 0) {
-                // ---- queries: a power of two per row makes them f16.  W/8 lanes take a row, 16 bytes each
+                // ---- queries into their place, W/8 lanes a row; then a row a thread: a power of two makes it f16
                 constexpr int kLanes = W / 8, kAtOnce = 32 / kLanes;
                 const bool vec = (reinterpret_cast<uintptr_t>(a.q.p) & 15u) == 0 && ((a.q.ts | a.q.hs) & 7) == 0;
                 const int64_t q_row = real ? (int64_t)(p.q0 + tok) * a.q.ts + (int64_t)(p.head * a.G + row - tok * a.G) * a.q.hs : INT64_MIN;
                 const int chunk = lane % kLanes;
-                const uint32_t dst = smem_u32(smem + S::kQAt) + t * S::kQTile + (chunk / 8) * (kTileRows * 128);
+                const uint32_t place = smem_u32(smem + S::kQAt) + t * S::kQTile;
+                const uint32_t dst = place + (chunk / 8) * (kTileRows * 128);
 #pragma unroll 4
                 for (int x = 0; x < 32 / kAtOnce; ++x) {
                     const int r = x * kAtOnce + lane / kLanes;             // of the warp's 32 rows
                     const int64_t at_row = __shfl_sync(0xffffffffu, q_row, r);
+                    const uint32_t to = dst + swizzled(wl + r, chunk % 8);
                     const __nv_bfloat16 *src = (const __nv_bfloat16 *)a.q.p + at_row + 8 * chunk;
-                    uint4 q = make_uint4(0u, 0u, 0u, 0u);
-                    if (at_row != INT64_MIN && 8 * chunk < a.D) {
-                        if (vec) q = __ldg(reinterpret_cast<const uint4 *>(src));
-                        else {
-                            uint32_t w[4];
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) w[e] = (uint32_t)__bfloat16_as_ushort(src[2 * e]) | (uint32_t)__bfloat16_as_ushort(src[2 * e + 1]) << 16;
-                            q = make_uint4(w[0], w[1], w[2], w[3]);
-                        }
+                    if (at_row == INT64_MIN || 8 * chunk >= a.D) sts16(to, 0u, 0u, 0u, 0u);
+                    else if (vec) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(src) : "memory");
+                    else {
+#pragma unroll 1
+                        for (int e = 0; e < 8; ++e) asm volatile("st.shared.u16 [%0], %1;" ::"r"(to + 2 * e), "h"(__bfloat16_as_ushort(src[e])) : "memory");
                     }
-                    const uint32_t qw[4] = {q.x, q.y, q.z, q.w};
-                    float top = 0.f;
+                }
+                asm volatile("cp.async.wait_all;" ::: "memory");
+                __syncwarp();
+                float top = 0.f;
+#pragma unroll 4
+                for (int c = 0; c < W / 8; ++c) {
+                    uint32_t x[4];
+                    lds16(place + (c / 8) * (kTileRows * 128) + swizzled(row_in, c % 8), x);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) top = fmaxf(top, fmaxf(fabsf(__uint_as_float(qw[e] << 16)), fabsf(__uint_as_float(qw[e] & 0xffff0000u))));
+                    for (int e = 0; e < 4; ++e) top = max3(top, fabsf(__uint_as_float(x[e] << 16)), fabsf(__uint_as_float(x[e] & 0xffff0000u)));
+                }
+                const int e2 = row_exponent(top);
+                const float up = power2(10 - e2) * (a.score_scale < 0.f ? -1.f : 1.f);
+                f = fmaxf(fabsf(a.score_scale) * power2(e2 - 10), 1e-30f);      // not 0, which times a masked -infinity is no number
+#pragma unroll 4
+                for (int c = 0; c < W / 8; ++c) {
+                    uint32_t x[4];
+                    const uint32_t at_chunk = place + (c / 8) * (kTileRows * 128) + swizzled(row_in, c % 8);
+                    lds16(at_chunk, x);
 #pragma unroll
-                    for (int o = kLanes / 2; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-                    int e2 = top > 0.f && top <= FLT_MAX ? ilogbf(top) : 0;
-                    e2 = max(e2, -100);
-                    const float up = ldexpf(a.score_scale < 0.f ? -1.f : 1.f, 10 - e2);
-                    const int mine = __shfl_sync(0xffffffffu, e2, (lane % kAtOnce) * kLanes);
-                    if (lane / kAtOnce == x) f = fmaxf(ldexpf(fabsf(a.score_scale), mine - 10), 1e-30f);      // not 0, which times a masked -infinity is no number
-                    uint32_t h[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) h[e] = pack2(__uint_as_float(qw[e] << 16) * up, __uint_as_float(qw[e] & 0xffff0000u) * up);
-                    sts16(dst + swizzled(wl + r, chunk % 8), h[0], h[1], h[2], h[3]);
+                    for (int e = 0; e < 4; ++e) x[e] = pack2(__uint_as_float(x[e] << 16) * up, __uint_as_float(x[e] & 0xffff0000u) * up);
+                    sts16(at_chunk, x[0], x[1], x[2], x[3]);
                 }
                 fence_async();
                 tc::tc_fence_before();
@@ -648,31 +657,31 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
                 for (int pass = 0; pass < (whole ? 1 : 2); ++pass) {
                     __syncwarp();
 #pragma unroll 1
-                    for (int c = 0; c < (whole ? W : kPass) / 16; ++c) {
-                        uint32_t r[16];
-                        if (n > 0) { tc::tmem_ld16(o_tmem + pass * kPass + 16 * c, r); tc::tmem_ld_wait(); }
+                    for (int c = 0; c < (whole ? W : kPass) / 32; ++c) {
+                        uint32_t r[32];
+                        if (n > 0) { ld32(o_tmem + pass * kPass + 32 * c, r); tc::tmem_ld_wait(); }
                         else {
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) r[i] = 0u;
+                            for (int i = 0; i < 32; ++i) r[i] = 0u;
                         }
                         if (whole) {
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) r[i] = bf2(__uint_as_float(r[2 * i]) * k, __uint_as_float(r[2 * i + 1]) * k);
+                            for (int i = 0; i < 16; ++i) r[i] = bf2(__uint_as_float(r[2 * i]) * k, __uint_as_float(r[2 * i + 1]) * k);
                         }
 #pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            if (i < 2 || !whole) sts16(slot16(lane, (whole ? 2 : 4) * c + i), r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]);
+                        for (int i = 0; i < 8; ++i)
+                            if (i < 4 || !whole) sts16(slot16(lane, (whole ? 4 : 8) * c + i), r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]);
                     }
                     __syncwarp();
 #pragma unroll 4
                     for (int x = 0; x < 32 / kAtOnce; ++x) {
                         const int r = x * kAtOnce + lane / kLanes;
                         const int64_t to = __shfl_sync(0xffffffffu, to_row, r);
-                        uint4 v;
-                        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(slot16(r, chunk)));
+                        uint32_t v[4];
+                        lds16(slot16(r, chunk), v);
                         if (to == -1) continue;
-                        if (!whole) *reinterpret_cast<uint4 *>(part + r * W + pass * kPass + 4 * chunk) = v;
-                        else if (8 * chunk < a.D) *reinterpret_cast<uint4 *>((__nv_bfloat16 *)a.out + to + 8 * chunk) = v;
+                        if (!whole) *reinterpret_cast<uint4 *>(part + r * W + pass * kPass + 4 * chunk) = make_uint4(v[0], v[1], v[2], v[3]);
+                        else if (8 * chunk < a.D) *reinterpret_cast<uint4 *>((__nv_bfloat16 *)a.out + to + 8 * chunk) = make_uint4(v[0], v[1], v[2], v[3]);
                     }
                 }
                 __syncwarp();
