@@ -47,6 +47,7 @@ struct Shape {
     static constexpr int kQAt = 0, kKAt = 2 * kQTile, kVAt = kKAt + 2 * kKTile, kLineAt = kVAt + 2 * kVTile;
     static constexpr int kS = 0, kO = 2 * kTileKeys;          // columns of tensor memory
 };
+constexpr uint32_t kTmem = 0;                    // where an allocation of all 512 columns begins
 
 __device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
@@ -58,6 +59,20 @@ __device__ __forceinline__ void ld32(uint32_t taddr, uint32_t (&r)[32]) {
           "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
           "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
           "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void ld64(uint32_t taddr, uint32_t (&r)[64]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x64.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, "
+        "%32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47, %48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%64];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+          "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+          "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]),
+          "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]),
+          "=r"(r[40]), "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]),
+          "=r"(r[48]), "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]),
+          "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63])
         : "r"(taddr) : "memory");
 }
 __device__ __forceinline__ void st32(uint32_t taddr, const uint32_t *r) {
@@ -100,6 +115,11 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     float r;
     asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
+}
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(p));
+    return p != 0;
 }
 __device__ __forceinline__ void st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
@@ -208,7 +228,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
     tc::tc_fence_before();
     __syncthreads();
     tc::tc_fence_after();
-    const uint32_t tmem = tmem_slot;
+    const uint32_t tmem = kTmem;
+    bool dead = tmem_slot != kTmem;          // a wait ran out: nothing more is waited for or issued, the loops run out
+    if (dead && tid == 0) atomicOr(a.status, MOE_KV_STATUS_TIMEOUT);
     const long long total = line[a.n], share = max((total + gridDim.x - 1) / (long long)gridDim.x, 1ll);
     const long long at = min(share * blockIdx.x, total);
     const long long end = min(at + share, total);
@@ -265,20 +287,19 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
         }
         return cut(p);
     };
-    bool dead = false;       // a wait ran out: nothing more is waited for or issued, the loops run out
     auto wait = [&](uint32_t b, uint32_t parity) { if (!dead) dead = !tc::mbar_wait(b, parity, a.status); };
 
-    // registers by role: 2 x 176 + 104 + 56 = 512 = 4 x 128, what the block was launched with
+    // registers by role: 2 x 192 + 72 + 56 = 512 = 4 x 128, what the block was launched with
     if (group == 2) {
         // ================================================================ conversion
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         const int c8 = tid - 256;                                             // 0..127
         const int v_sub = c8 >> 6, v_c = lane & 7, v_r = (lane >> 3) + 4 * ((c8 >> 5) & 1);
         constexpr int kCodes = W / 32;                                        // 16-byte words of a key's codes
         constexpr int kVWords = W / 8;                                        // words of 8 keys' share of a stretch
-        uint4 kc[kCodes], kn[kCodes];
-        uint2 ks, ksn, vs, vsn;
-        uint32_t vc[kVWords], vn[kVWords];
+        uint4 kc[kCodes];
+        uint2 ks, vs;
+        uint32_t vc[kVWords];
         int it = 0;                                                           // tiles so far, over all pieces
         Piece p;
         for (bool more = begin(p); more; more = next(p)) {
@@ -296,39 +317,41 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
                 if (pg < 0 || pg >= a.n_pages) { atomicOr(a.status, MOE_KV_STATUS_BAD_INDEX); return -1; }
                 return ((pg * a.Hk + p.head) << a.page_shift) + (b & ((1 << a.page_shift) - 1));
             };
-            auto fetch = [&](int kb, int vb, uint4 (&kd)[kCodes], uint2 &sd, uint32_t (&vd)[kVWords], uint2 &vsd) {
-                sd = vsd = make_uint2(0u, 0u);
+            auto fetch_keys = [&](int kb) {
+                ks = make_uint2(0u, 0u);
 #pragma unroll
-                for (int i = 0; i < kCodes; ++i) kd[i] = make_uint4(0u, 0u, 0u, 0u);
+                for (int i = 0; i < kCodes; ++i) kc[i] = make_uint4(0u, 0u, 0u, 0u);
+                if (kb < 0) return;
+                const uint8_t *blk = a.cache + (int64_t)kb * block_bytes(W);
+                const int token = c8 & 15;
 #pragma unroll
-                for (int i = 0; i < kVWords; ++i) vd[i] = 0u;
-                if (kb >= 0) {
-                    const uint8_t *blk = a.cache + (int64_t)kb * block_bytes(W);
-                    const int token = c8 & 15;
+                for (int i = 0; i < kCodes; ++i) kc[i] = __ldg(reinterpret_cast<const uint4 *>(blk + token * (W / 2) + 16 * i));
+                if (W == 128) ks = __ldg(reinterpret_cast<const uint2 *>(blk + k_scales_at(W) + token * (W / 16)));
+                else ks.x = __ldg(reinterpret_cast<const uint32_t *>(blk + k_scales_at(W) + token * (W / 16)));
+            };
+            auto fetch_values = [&](int vb) {
+                vs = make_uint2(0u, 0u);
 #pragma unroll
-                    for (int i = 0; i < kCodes; ++i) kd[i] = __ldg(reinterpret_cast<const uint4 *>(blk + token * (W / 2) + 16 * i));
-                    if (W == 128) sd = __ldg(reinterpret_cast<const uint2 *>(blk + k_scales_at(W) + token * (W / 16)));
-                    else sd.x = __ldg(reinterpret_cast<const uint32_t *>(blk + k_scales_at(W) + token * (W / 16)));
+                for (int i = 0; i < kVWords; ++i) vc[i] = 0u;
+                if (vb < 0) return;
+                const uint8_t *blk = a.cache + (int64_t)vb * block_bytes(W);
+                const int half = v_c & 1;
+                const uint4 *src = reinterpret_cast<const uint4 *>(blk + v_codes_at(W) + v_r * W + ((half * (W / 2)) ^ v_turn(W, v_r)));
+#pragma unroll
+                for (int i = 0; i < kVWords / 4; ++i) {
+                    const uint4 x = __ldg(src + i);
+                    vc[4 * i] = x.x; vc[4 * i + 1] = x.y; vc[4 * i + 2] = x.z; vc[4 * i + 3] = x.w;
                 }
-                if (vb >= 0) {
-                    const uint8_t *blk = a.cache + (int64_t)vb * block_bytes(W);
-                    const int half = v_c & 1;
-                    const uint4 *src = reinterpret_cast<const uint4 *>(blk + v_codes_at(W) + v_r * W + ((half * (W / 2)) ^ v_turn(W, v_r)));
-#pragma unroll
-                    for (int i = 0; i < kVWords / 4; ++i) {
-                        const uint4 x = __ldg(src + i);
-                        vd[4 * i] = x.x; vd[4 * i + 1] = x.y; vd[4 * i + 2] = x.z; vd[4 * i + 3] = x.w;
-                    }
-                    vsd = __ldg(reinterpret_cast<const uint2 *>(blk + v_scales_at(W) + (W == 128 ? v_r : v_r >> 1) * kBlockTokens + half * 8));
-                }
+                vs = __ldg(reinterpret_cast<const uint2 *>(blk + v_scales_at(W) + (W == 128 ? v_r : v_r >> 1) * kBlockTokens + half * 8));
             };
             const int k_in = c8 >> 4, v_in = v_sub * 4 + (v_c >> 1);
+            // a tile's bytes are asked for as soon as the tile before has left the registers, its pages a tile earlier
             int kb = find(0, k_in), vb = find(0, v_in), kb2 = find(1, k_in), vb2 = find(1, v_in);
-            fetch(kb, vb, kc, ks, vc, vs);
+            fetch_keys(kb);
+            fetch_values(vb);
             for (int j = 0; j < n; ++j, ++it) {
                 const int stage = it & 1;
                 const uint32_t parity = ((it >> 1) & 1) ^ 1;
-                fetch(kb2, vb2, kn, ksn, vn, vsn);
                 const int kb_now = kb;
                 const int key0 = tile_of(j) * kTileKeys;
                 kb = kb2; vb = vb2;
@@ -362,6 +385,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
                 fence_async();
                 __syncwarp();
                 if (lane == 0) tc::mbar_arrive(k_full(stage));
+                fetch_keys(kb);
 
                 // ---- values: 8 keys of a stretch of dimensions, transposed
                 wait(v_empty(stage), parity);
@@ -398,36 +422,47 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
                 fence_async();
                 __syncwarp();
                 if (lane == 0) tc::mbar_arrive(v_full(stage));
-#pragma unroll
-                for (int i = 0; i < kCodes; ++i) kc[i] = kn[i];
-#pragma unroll
-                for (int i = 0; i < kVWords; ++i) vc[i] = vn[i];
-                ks = ksn; vs = vsn;
+                fetch_values(vb);
             }
         }
     } else if (group == 3) {
         // ================================================================ products
         asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-        if (warp == 12 && lane == 0) {
+        if (warp == 12) {
+            // The warp walks together and one thread issues, so that descriptors are in uniform registers (the whole walk in
+            // one thread: 764 us for 710 on four prompts of 2048 tokens)
+            const bool one = elect_one();
             int it = 0;
             uint32_t p_phase = 0;                  // bit t
             // a k16 step is 32 bytes inside a 128-byte row (2 in a descriptor's units of 16), 64 elements are a sub-tile
             const uint64_t q_d = tc::make_kmajor_sw128_desc(smem_u32(smem + S::kQAt)), k_d = tc::make_kmajor_sw128_desc(smem_u32(smem + S::kKAt)),
                            v_d = tc::make_kmajor_sw128_desc(smem_u32(smem + S::kVAt));
             auto scores = [&](int t, int stage) {
-                if (dead) return;
-                uint64_t da = q_d + t * (S::kQTile / 16), db = k_d + stage * (S::kKTile / 16);
-#pragma unroll 1
-                for (int sub = 0; sub < W / 64; ++sub, da += kTileRows * 128 / 16, db += kTileKeys * 128 / 16)
+                const uint64_t da = q_d + t * (S::kQTile / 16), db = k_d + stage * (S::kKTile / 16);
+                if (one && !dead) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) tc::umma_bf16(tmem + S::kS + t * kTileKeys, da + 2 * i, db + 2 * i, idesc_f16(kTileKeys), sub + i > 0);
-                tc::umma_commit(s_full(t));
+                    for (int i = 0; i < W / 16; ++i)
+                        tc::umma_bf16(kTmem + S::kS + t * kTileKeys, da + (i / 4) * (kTileRows * 128 / 16) + 2 * (i % 4), db + (i / 4) * (kTileKeys * 128 / 16) + 2 * (i % 4),
+                                      idesc_f16(kTileKeys), i > 0);
+                    tc::umma_commit(s_full(t));
+                }
+                __syncwarp();
+            };
+            auto outputs = [&](int t, int stage, bool more) {
+                const uint64_t db = v_d + stage * (S::kVTile / 16);
+                if (one && !dead) {
+#pragma unroll
+                    for (int i = 0; i < kTileKeys / 16; ++i)
+                        umma_ts(kTmem + S::kO + t * W, kTmem + S::kS + t * kTileKeys + 8 * i, db + (i / 4) * (W * 128 / 16) + 2 * (i % 4), idesc_f16(W), i > 0 || more);
+                    tc::umma_commit(o_full(t));
+                }
+                __syncwarp();
             };
             Piece p;
-            for (bool more = begin(p); more; more = next(p)) {
+            for (bool go = begin(p); go; go = next(p)) {
                 if (p.last <= p.first) continue;
-                const int n = min(p.last, p.present) - p.first;
-                const int tiles = p.row1 - p.row0 > kTileRows ? 2 : 1;
+                const int n = __reduce_max_sync(0xffffffffu, min(p.last, p.present) - p.first);        // into a uniform register
+                const int tiles = __reduce_max_sync(0xffffffffu, p.row1 - p.row0 > kTileRows ? 2 : 1);
                 if (n > 0) {
                     wait(k_full(it & 1), (it >> 1) & 1);
                     for (int t = 0; t < tiles; ++t) {
@@ -436,38 +471,35 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
                         tc::tc_fence_after();
                         scores(t, it & 1);
                     }
-                    if (!dead) tc::umma_commit(k_empty(it & 1));
+                    if (one && !dead) tc::umma_commit(k_empty(it & 1));
+                    __syncwarp();
                 }
+#pragma unroll 1
                 for (int j = 0; j < n; ++j, ++it) {
                     const int stage = it & 1, other = stage ^ 1;
                     wait(v_full(stage), (it >> 1) & 1);
                     if (j + 1 < n) wait(k_full(other), ((it + 1) >> 1) & 1);
-                    for (int t = 0; t < tiles; ++t) {
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        if (t >= tiles) continue;
                         wait(p_full(t), (p_phase >> t) & 1u);          // the weights are there, the scores are read
                         p_phase ^= 1u << t;
                         tc::tc_fence_after();
-                        if (!dead) {
-                            uint64_t db = v_d + stage * (S::kVTile / 16);
-                            uint32_t pa = tmem + S::kS + t * kTileKeys;
-#pragma unroll 1
-                            for (int sub = 0; sub < 2; ++sub, db += W * 128 / 16, pa += 32)
-#pragma unroll
-                                for (int i = 0; i < 4; ++i) umma_ts(tmem + S::kO + t * W, pa + 8 * i, db + 2 * i, idesc_f16(W), j + sub + i > 0);
-                            tc::umma_commit(o_full(t));
-                        }
+                        outputs(t, stage, j > 0);
                         if (j + 1 < n) scores(t, other);
                     }
-                    if (!dead) {
+                    if (one && !dead) {
                         tc::umma_commit(v_empty(stage));
                         if (j + 1 < n) tc::umma_commit(k_empty(other));
                     }
+                    __syncwarp();
                 }
             }
         }
         __syncwarp();
     } else {
         // ================================================================ softmax: thread = row of tile `group`
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
         const int t = group, row_in = tid & 127, wl = (warp & 3) * 32;
         const uint32_t lanes = (uint32_t)wl << 16;
         const uint32_t s_tmem = tmem + S::kS + t * kTileKeys + lanes, o_tmem = tmem + S::kO + t * W + lanes;
@@ -561,29 +593,19 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
                         }
                         st_wait();
                     }
-                    // ---- the row's largest score.  Loops stay rolled: the roles' straight code would not fit the
-                    // instruction caches (1.4 times the time when it did not)
-                    uint32_t ra[32], rb[32];
-                    float top0 = -INFINITY, top1 = -INFINITY, top2 = -INFINITY, top3 = -INFINITY;
-                    auto largest = [&](const uint32_t (&r)[32]) {
-#pragma unroll
-                        for (int i = 0; i < 32; i += 8) {
-                            top0 = max3(top0, __uint_as_float(r[i]), __uint_as_float(r[i + 1]));
-                            top1 = max3(top1, __uint_as_float(r[i + 2]), __uint_as_float(r[i + 3]));
-                            top2 = max3(top2, __uint_as_float(r[i + 4]), __uint_as_float(r[i + 5]));
-                            top3 = max3(top3, __uint_as_float(r[i + 6]), __uint_as_float(r[i + 7]));
-                        }
-                    };
-                    ld32(s_tmem, ra);
+                    // ---- the row's 128 scores stay in registers from the search for the largest to the weights: a chain of
+                    // loads from tensor memory (200 cycles each) would be the longest part of a tile
+                    uint32_t r0[64], r1[64];
+                    ld64(s_tmem, r0);
+                    ld64(s_tmem + 64, r1);
                     tc::tmem_ld_wait();
-#pragma unroll 1
-                    for (int c = 0; c < kTileKeys / 64; ++c) {
-                        ld32(s_tmem + 64 * c + 32, rb);
-                        largest(ra);
-                        tc::tmem_ld_wait();
-                        ld32(s_tmem + ((64 * c + 64) & (kTileKeys - 1)), ra);        // behind the last: the first again, for the weights
-                        largest(rb);
-                        tc::tmem_ld_wait();
+                    float top0 = -INFINITY, top1 = -INFINITY, top2 = -INFINITY, top3 = -INFINITY;
+#pragma unroll
+                    for (int i = 0; i < 64; i += 4) {
+                        top0 = max3(top0, __uint_as_float(r0[i]), __uint_as_float(r0[i + 1]));
+                        top1 = max3(top1, __uint_as_float(r0[i + 2]), __uint_as_float(r0[i + 3]));
+                        top2 = max3(top2, __uint_as_float(r1[i]), __uint_as_float(r1[i + 1]));
+                        top3 = max3(top3, __uint_as_float(r1[i + 2]), __uint_as_float(r1[i + 3]));
                     }
                     const float top = fmaxf(fmaxf(top0, top1), fmaxf(top2, top3)), reach = top == -INFINITY ? -INFINITY : top * f;
                     if (__any_sync(0xffffffffu, reach > m)) {       // O follows only when a score passes the reference
@@ -608,26 +630,21 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
                     // ---- weights: 32 scores become 16 columns
                     const uint64_t f2 = pair(f, f), away2 = pair((kHead + kSlack) - m, (kHead + kSlack) - m);
                     uint64_t sum2 = 0ull;
-                    auto weights = [&](const uint32_t (&r)[32], int c) {
+                    auto weights = [&](const uint32_t (&r)[64], int at_key) {        // 32 keys become 16 columns
                         uint32_t w[16];
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
-                            const float2 x = halves(fma2(pair(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1])), f2, away2));
+                            const float2 x = halves(fma2(pair(__uint_as_float(r[at_key % 64 + 2 * i]), __uint_as_float(r[at_key % 64 + 2 * i + 1])), f2, away2));
                             const float e0 = ex2(x.x), e1 = ex2(x.y);
                             sum2 = add2(sum2, pair(e0, e1));
                             w[i] = pack2(e0, e1);
                         }
-                        st16(s_tmem + 16 * c, w);
+                        st16(s_tmem + at_key / 2, w);
                     };
-#pragma unroll 1
-                    for (int c = 0; c < kTileKeys / 64; ++c) {
-                        ld32(s_tmem + 64 * c + 32, rb);
-                        weights(ra, 2 * c);
-                        tc::tmem_ld_wait();
-                        if (c == 0) ld32(s_tmem + 64, ra);
-                        weights(rb, 2 * c + 1);
-                        tc::tmem_ld_wait();
-                    }
+                    weights(r0, 0);
+                    weights(r0, 32);
+                    weights(r1, 64);
+                    weights(r1, 96);
                     l += halves(sum2).x + halves(sum2).y;
                     st_wait();
                     tc::tc_fence_before();
@@ -757,7 +774,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
     tc::tc_fence_before();
     __syncthreads();
     tc::tc_fence_after();
-    if (warp == 12) tc::tmem_dealloc(tmem, 512);
+    if (warp == 12) tc::tmem_dealloc(tmem_slot, 512);
 }
 
 template <int W>
