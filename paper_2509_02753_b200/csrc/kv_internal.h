@@ -27,6 +27,27 @@ __host__ __device__ constexpr int v_turn(int w, int r) {
 
 struct Rows { const void *p; int64_t ts, hs; };
 
+// n / d for every 32-bit n and d >= 1 by one high product (Granlund and Montgomery's division by invariants): the
+// kernels of few instructions a thread spent most of them in the compiler's divisions
+struct FastDiv {
+    uint32_t d, m, s1, s2;
+    __host__ __device__ FastDiv() : d(1), m(1), s1(0), s2(0) {}
+    __host__ explicit FastDiv(uint32_t by) : d(by) {
+        uint32_t l = 0;
+        while (l < 32 && (1ull << l) < by) ++l;
+        m = (uint32_t)(((1ull << 32) * ((1ull << l) - by)) / by + 1);
+        s1 = l < 1 ? l : 1;
+        s2 = l < 1 ? 0 : l - 1;
+    }
+#ifdef __CUDACC__
+    __device__ __forceinline__ uint32_t div(uint32_t n) const {
+        const uint32_t t = __umulhi(m, n);
+        return (t + ((n - t) >> s1)) >> s2;
+    }
+    __device__ __forceinline__ void split(uint32_t n, uint32_t &q, uint32_t &r) const { q = div(n); r = n - q * d; }
+#endif
+};
+
 struct TablesArgs {
     const int32_t *ctx, *fresh_tokens; int n;
     const int32_t *free_pages; int n_free;
@@ -49,14 +70,14 @@ struct RopeArgs {
 cudaError_t launch_rope(const RopeArgs &a, int sm_count, cudaStream_t s, uint64_t *launches);
 
 struct AppendArgs {
-    int dtype; Rows q, k, v; int T, H, Hk, D, page; Turn turn;
+    int dtype; Rows q, k, v; int T, H, Hk, D, page_shift; Turn turn;
     const int64_t *slot; float k_scale, v_scale, k_inv6, v_inv6; void *q_out;
     uint8_t *cache; int64_t n_slots; int32_t *status;
 };
 cudaError_t launch_append(const AppendArgs &a, int sm_count, cudaStream_t s, uint64_t *launches);
 
 struct ReadArgs {
-    int dtype; const uint8_t *cache; int64_t n_slots; const int64_t *slot; int T, Hk, D, page;
+    int dtype; const uint8_t *cache; int64_t n_slots; const int64_t *slot; int T, Hk, D, page_shift;
     float k_scale, v_scale; void *k, *v; int32_t *status;
 };
 cudaError_t launch_read(const ReadArgs &a, cudaStream_t s, uint64_t *launches);

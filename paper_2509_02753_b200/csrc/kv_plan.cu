@@ -57,6 +57,9 @@ int check_turn(const moe_kv_plan *p, int32_t tokens, const int32_t *position, co
     return aligned(table, 8) ? MOE_OK : MOE_ERR_ALIGN;
 }
 
+// log2 of a page's blocks
+int page_shift(const moe_kv_config_t &c) { return c.page_size == 16 ? 0 : c.page_size == 32 ? 1 : c.page_size == 64 ? 2 : 3; }
+
 bool good_scale(float s) { return s > 0.f && std::isfinite(s); }
 
 int done(cudaError_t err) {
@@ -209,7 +212,7 @@ int moe_kv_append(moe_kv_plan_t *p, const moe_kv_rows_t *q, const moe_kv_rows_t 
     if (!slot || !cache) return MOE_ERR_INVALID_ARG;
     if (!aligned(cache, 16)) return MOE_ERR_ALIGN;
     AppendArgs a{c.dtype, qr, Rows{k->data, k->token_stride, k->head_stride}, Rows{v->data, v->token_stride, v->head_stride}, T,
-                 c.n_heads, c.n_kv_heads, c.head_dim, c.page_size, Turn{position, (const float2 *)table, n_positions, rope_dim, layout, 0},
+                 c.n_heads, c.n_kv_heads, c.head_dim, page_shift(c) + 4, Turn{position, (const float2 *)table, n_positions, rope_dim, layout, 0},
                  slot, k_scale, v_scale, (float)(1.0 / (6.0 * (double)k_scale)), (float)(1.0 / (6.0 * (double)v_scale)), q_out,
                  (uint8_t *)cache, (int64_t)n_pages * c.page_size, p->status};
     return done(launch_append(a, p->sm_count, (cudaStream_t)stream, &p->launches));
@@ -222,7 +225,7 @@ int moe_kv_read(moe_kv_plan_t *p, const void *cache, int32_t n_pages, const int6
     if (!slot || !cache) return MOE_ERR_INVALID_ARG;
     if (!aligned(cache, 16) || !aligned(k, 16) || !aligned(v, 16)) return MOE_ERR_ALIGN;
     const moe_kv_config_t &c = p->cfg;
-    ReadArgs a{c.dtype, (const uint8_t *)cache, (int64_t)n_pages * c.page_size, slot, T, c.n_kv_heads, c.head_dim, c.page_size,
+    ReadArgs a{c.dtype, (const uint8_t *)cache, (int64_t)n_pages * c.page_size, slot, T, c.n_kv_heads, c.head_dim, page_shift(c) + 4,
                k_scale, v_scale, k, v, p->status};
     return done(launch_read(a, (cudaStream_t)stream, &p->launches));
 }
@@ -241,7 +244,7 @@ int moe_kv_attention(moe_kv_plan_t *p, const moe_kv_rows_t *q, int32_t T, const 
     AttendArgs a{};
     a.dtype = c.dtype; a.q = Rows{q->data, q->token_stride, q->head_stride}; a.T = T; a.cu = cu_new; a.kv_len = kv_len; a.n = n; a.max_new = max_new;
     a.table = block_table; a.width = width; a.cache = (const uint8_t *)cache; a.n_pages = n_pages;
-    a.H = c.n_heads; a.Hk = c.n_kv_heads; a.G = c.n_heads / c.n_kv_heads; a.D = c.head_dim; a.g_mul = (uint32_t)((0x100000000ull + a.G - 1) / a.G); a.page_shift = c.page_size == 16 ? 0 : c.page_size == 32 ? 1 : c.page_size == 64 ? 2 : 3;
+    a.H = c.n_heads; a.Hk = c.n_kv_heads; a.G = c.n_heads / c.n_kv_heads; a.D = c.head_dim; a.g_mul = (uint32_t)((0x100000000ull + a.G - 1) / a.G); a.page_shift = page_shift(c);
     a.score_scale = (float)((double)softmax_scale * k_scale * 1.4426950408889634);
     a.v_scale = v_scale; a.out = out;
     // no position reaches kMaxContext, and sums of these stay below 2^31

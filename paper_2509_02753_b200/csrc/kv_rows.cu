@@ -1,4 +1,5 @@
 // Rotary positions, storing rows in 4 bits, and reading them back.
+#include <float.h>
 #include <math.h>
 
 #include "kv_internal.h"
@@ -43,6 +44,9 @@ __global__ void rope_table_kernel(RopeTableArgs a) {
 // ------------------------------------------------------------------ elements
 __device__ __forceinline__ float to_f(float v) { return v; }
 __device__ __forceinline__ float to_f(__nv_bfloat16 v) { return __bfloat162float(v); }
+
+__device__ __forceinline__ void put(float *p, float v) { *p = v; }
+__device__ __forceinline__ void put(__nv_bfloat16 *p, float v) { *p = __float2bfloat16_rn(v); }
 
 // 8 neighbouring elements; VEC: 16-byte aligned
 template <bool VEC>
@@ -101,71 +105,133 @@ __device__ __forceinline__ void turn(float &u, float &w, float2 cs) {
     u = a;
 }
 
-// A unit of a row's work: 8 pairs that turn (two stretches of 8 dimensions in the half layout, 16 neighbouring ones in
-// the pairs layout), or up to 8 dimensions behind rope_dim that pass.  Both ends of a pair are one thread's, so a call
-// can work in place.  The same unit of several heads shares the angles.
-struct Units { int turning, passing; };
-__host__ __device__ inline Units units_of(int D, int rot) { return Units{(rot / 2 + 7) / 8, (D - rot + 7) / 8}; }
+// How the rows of a call are walked, by layout and alignment; a thread has one unit of a row, two stretches of 8
+// dimensions where it can (32 bytes of bf16 in flight per head, and the unit of several heads shares the angles):
+//   kHalves    half layout, rope_dim/2 a multiple of 8, rows on 16 bytes: stretch u with the one it turns with; behind
+//              rope_dim two neighbours
+//   kPairs     pairs layout, rows on 16 bytes: two neighbours
+//   kPartners  half layout, any rope_dim, rows on 16 bytes, not in place: one stretch; the other ends are read one by one
+//   kSingles   everything else: 8 pairs or 8 passing dimensions, one by one
+// Both ends of a pair are one thread's except in kPartners, so that the others can work in place.
+enum Walk { kHalves, kPairs, kPartners, kSingles };
 
-template <typename T, bool VEC>
-__device__ __forceinline__ void turn_unit(const T *x, T *y, int D, const Turn &tn, bool turns, int unit,
-                                          const Units &un, const float2 (&cs)[8]) {
-    const int half = tn.rot / 2;
-    float a[8], b[8];
-    if (unit < un.turning) {
-        const int i0 = unit * 8, n = min(8, half - i0);
-        if (tn.layout == MOE_ROPE_HALF) {
-            load8<VEC>(x + i0, n, a);
-            load8<VEC>(x + half + i0, n, b);
-            if (turns) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) turn(a[i], b[i], cs[i]);
-            }
-            store8<VEC>(y + i0, n, a);
-            store8<VEC>(y + half + i0, n, b);
-        } else {
-            load8<VEC>(x + 2 * i0, 2 * n, a);
-            load8<VEC>(x + 2 * i0 + 8, 2 * n - 8, b);
-            if (turns) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) { turn(a[2 * i], a[2 * i + 1], cs[i]); turn(b[2 * i], b[2 * i + 1], cs[i + 4]); }
-            }
-            store8<VEC>(y + 2 * i0, 2 * n, a);
-            store8<VEC>(y + 2 * i0 + 8, 2 * n - 8, b);
-        }
-    } else if (x != y) {
-        const int d = tn.rot + (unit - un.turning) * 8, n = min(8, D - d);
-        load8<VEC>(x + d, n, a);
-        store8<VEC>(y + d, n, a);
+__host__ __device__ inline int units_of(Walk walk, int D, int rot) {
+    switch (walk) {
+        case kHalves: return rot / 16 + (D - rot + 15) / 16;
+        case kPairs: return (D + 15) / 16;
+        case kPartners: return D / 8;
+        default: return (rot / 2 + 7) / 8 + (D - rot + 7) / 8;
     }
 }
 
-// cos and sin of the unit's pairs; false: the position is outside the table (the row then stays unturned)
-__device__ __forceinline__ bool unit_angles(const Turn &tn, int t, int unit, const Units &un, float2 (&cs)[8], int32_t *status) {
-    if (unit >= un.turning) return false;
-    const int p = tn.position[t], half = tn.rot / 2, i0 = unit * 8;
-    if (p < 0 || p >= tn.n_positions) { atomicOr(status, MOE_KV_STATUS_BAD_INDEX); return false; }
+// the angles of pairs i0.. of a row of the table, 1 and 0 behind rope_dim
+template <bool VEC>
+__device__ __forceinline__ void load_angles(const Turn &tn, int t, int i0, float2 (&cs)[8], bool &turns, int32_t *status) {
+    const int half = tn.rot / 2;
+    const int p = i0 < half ? tn.position[t] : 0;
+    turns = i0 < half && p >= 0 && p < tn.n_positions;
+    if (i0 < half && !turns) atomicOr(status, MOE_KV_STATUS_BAD_INDEX);
     const float2 *row = tn.table + (int64_t)p * half + i0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        cs[i] = i0 + i < half ? row[i] : make_float2(1.f, 0.f);
-        if (tn.inverse) cs[i].y = -cs[i].y;
+    for (int i = 0; i < 8; i += 2) {
+        float4 v = make_float4(1.f, 0.f, 1.f, 0.f);
+        if (turns) {
+            if (VEC && i0 + i + 2 <= half) v = *reinterpret_cast<const float4 *>(row + i);
+            else {
+                if (i0 + i < half) { v.x = row[i].x; v.y = row[i].y; }
+                if (i0 + i + 1 < half) { v.z = row[i + 1].x; v.w = row[i + 1].y; }
+            }
+        }
+        cs[i] = make_float2(v.x, tn.inverse ? -v.y : v.y);
+        cs[i + 1] = make_float2(v.z, tn.inverse ? -v.w : v.w);
     }
-    return true;
 }
 
-template <typename T, bool VEC>
-__global__ void __launch_bounds__(kThreads) rope_kernel(RopeArgs a, int groups, int per_group) {
-    const Units un = units_of(a.D, a.turn.rot);
-    const int nu = un.turning + un.passing;
-    const long long e = (long long)blockIdx.x * kThreads + threadIdx.x;
-    if (e >= (long long)a.T * groups * nu) return;
-    const int unit = (int)(e % nu), grp = (int)(e / nu % groups), t = (int)(e / nu / groups);
+template <typename T>
+__device__ __forceinline__ float turned_at(const T *row, const Turn &tn, const float2 *cs_row, int d);
+
+constexpr int kHeads = 4;          // heads a thread takes where there are enough rows
+
+// heads h0 .. h0 + n of unit `unit` of token t
+template <typename T, int WALK, bool TABLE16>
+__device__ __forceinline__ void turn_unit(const T *x, int64_t xhs, T *y, int64_t yhs, int n, int D, const Turn &tn, int t, int unit, int32_t *status) {
     float2 cs[8];
-    const bool turns = unit_angles(a.turn, t, unit, un, cs, a.status);
-    const int h1 = min(a.H, (grp + 1) * per_group);
-    for (int h = grp * per_group; h < h1; ++h)
-        turn_unit<T, VEC>((const T *)a.x.p + t * a.x.ts + h * a.x.hs, (T *)a.y + t * a.yts + h * a.yhs, a.D, a.turn, turns, unit, un, cs);
+    bool turns;
+    const int half = tn.rot / 2;
+    if (WALK == kHalves || WALK == kPairs) {
+        const int turning = WALK == kHalves ? half / 8 : (D + 15) / 16;
+        const bool turner = unit < turning;
+        const int d0 = WALK == kPairs ? 16 * unit : turner ? 8 * unit : tn.rot + 16 * (unit - turning);
+        const int d1 = WALK == kHalves && turner ? half + d0 : d0 + 8;
+        load_angles<TABLE16>(tn, t, WALK == kPairs ? d0 / 2 : turner ? d0 : half, cs, turns, status);
+        if (!turns && x == y) return;
+        // (four heads' loads at once took 1.5 times as long: the registers cost more warps than they keep loads in flight)
+        for (int h = 0; h < n; ++h) {
+            float a[8], b[8];
+            load8<true>(x + h * xhs + d0, 8, a);
+            if (d1 < D) load8<true>(x + h * xhs + d1, 8, b);
+            if (turns) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    if (WALK == kHalves) turn(a[i], b[i], cs[i]);
+                    else if (i < 4) turn(a[2 * i], a[2 * i + 1], cs[i]);
+                    else turn(b[2 * i - 8], b[2 * i - 7], cs[i]);
+                }
+            }
+            store8<true>(y + h * yhs + d0, 8, a);
+            if (d1 < D) store8<true>(y + h * yhs + d1, 8, b);
+        }
+    } else if (WALK == kPartners) {
+        const int d0 = 8 * unit;
+        const int p = d0 < tn.rot ? tn.position[t] : 0;
+        const bool in = d0 < tn.rot && p >= 0 && p < tn.n_positions;
+        if (d0 < tn.rot && !in) atomicOr(status, MOE_KV_STATUS_BAD_INDEX);
+        const float2 *row = in ? tn.table + (int64_t)p * half : nullptr;
+        for (int h = 0; h < n; ++h) {
+            float a[8];
+            load8<true>(x + h * xhs + d0, 8, a);
+            if (in) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (d0 + i < tn.rot) a[i] = turned_at(x + h * xhs, tn, row, d0 + i);
+            }
+            store8<true>(y + h * yhs + d0, 8, a);
+        }
+    } else {
+        const int turning = (half + 7) / 8;
+        if (unit < turning) {
+            const int i0 = 8 * unit, m = min(8, half - i0);
+            load_angles<false>(tn, t, i0, cs, turns, status);
+            if (!turns && x == y) return;
+            const bool two = tn.layout == MOE_ROPE_PAIRS;
+            for (int h = 0; h < n; ++h)
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (i < m) {
+                        const int d = two ? 2 * (i0 + i) : i0 + i, e = two ? d + 1 : d + half;
+                        float u = to_f(x[h * xhs + d]), w = to_f(x[h * xhs + e]);
+                        if (turns) turn(u, w, cs[i]);
+                        put(y + h * yhs + d, u);
+                        put(y + h * yhs + e, w);
+                    }
+        } else if (x != y) {
+            const int d = tn.rot + (unit - turning) * 8;
+            for (int h = 0; h < n; ++h)
+                for (int i = d; i < min(d + 8, D); ++i) y[h * yhs + i] = x[h * xhs + i];
+        }
+    }
+}
+
+template <typename T, int WALK, bool TABLE16>
+__global__ void __launch_bounds__(kThreads) rope_kernel(RopeArgs a, FastDiv units, FastDiv groups, int per_group) {
+    uint32_t e = blockIdx.x * kThreads + threadIdx.x, unit, grp, token;
+    units.split(e, e, unit);
+    groups.split(e, token, grp);
+    if (token >= (uint32_t)a.T) return;
+    const int64_t t = token;
+    const int h0 = (int)grp * per_group;
+    turn_unit<T, WALK, TABLE16>((const T *)a.x.p + t * a.x.ts + h0 * a.x.hs, a.x.hs, (T *)a.y + t * a.yts + h0 * a.yhs, a.yhs, min(per_group, a.H - h0), a.D,
+                                a.turn, (int)t, (int)unit, a.status);
 }
 
 // ------------------------------------------------------------------ 4 bits
@@ -191,26 +257,35 @@ __device__ __forceinline__ float2 from_e2m1_pair(uint32_t byte) {
     return __half22float2(*reinterpret_cast<const __half2 *>(&h));
 }
 
-// 16 numbers of a group -> 8 bytes of codes and the scale byte
-__device__ __forceinline__ uint2 quantise(float (&x)[16], float inv6, float scale, uint32_t &s8, int32_t *status) {
+__device__ __forceinline__ float max_or_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
+// Half of a group of 16: its 8 numbers -> 4 bytes of codes, and the group's scale byte; the neighbouring lane has the
+// other half
+__device__ __forceinline__ uint32_t quantise8(float (&x)[8], float inv6, float scale, uint32_t &s8, int32_t *status) {
     float top = 0.f;
-    bool odd = false;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        if (!(fabsf(x[i]) <= 3.4028234663852886e38f)) {          // NaN -> 0, infinity -> the largest number
-            x[i] = x[i] != x[i] ? 0.f : copysignf(3.4028234663852886e38f, x[i]);
-            odd = true;
+    for (int i = 0; i < 8; ++i) top = max_or_nan(top, fabsf(x[i]));
+    if (!(top <= FLT_MAX)) {          // a NaN -> 0, an infinity -> the largest number
+        atomicOr(status, MOE_KV_STATUS_NONFINITE);
+        top = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (!(fabsf(x[i]) <= FLT_MAX)) x[i] = x[i] != x[i] ? 0.f : copysignf(FLT_MAX, x[i]);
+            top = fmaxf(top, fabsf(x[i]));
         }
-        top = fmaxf(top, fabsf(x[i]));
     }
-    if (odd) atomicOr(status, MOE_KV_STATUS_NONFINITE);
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
     s8 = to_e4m3(fminf(__fmul_rn(top, inv6), 448.f));
     const float s = __fmul_rn(from_e4m3(s8), scale);
     const float inv = s > 0.f ? __frcp_rn(s) : 0.f;
-    uint32_t w[2] = {0u, 0u};
+    uint32_t w = 0u;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) w[i >> 2] |= to_e2m1_pair(__fmul_rn(x[2 * i], inv), __fmul_rn(x[2 * i + 1], inv)) << (8 * (i & 3));
-    return make_uint2(w[0], w[1]);
+    for (int i = 0; i < 4; ++i) w |= to_e2m1_pair(__fmul_rn(x[2 * i], inv), __fmul_rn(x[2 * i + 1], inv)) << (8 * i);
+    return w;
 }
 
 // One element of a row with its head turned
@@ -222,174 +297,154 @@ __device__ __forceinline__ float turned_at(const T *row, const Turn &tn, const f
     const bool second = tn.layout == MOE_ROPE_HALF ? d >= half : d & 1;
     const int i = tn.layout == MOE_ROPE_HALF ? (second ? d - half : d) : d >> 1;
     float w = to_f(row[tn.layout == MOE_ROPE_HALF ? (second ? d - half : d + half) : d ^ 1]);
-    const float2 cs = cs_row[i];
+    float2 cs = cs_row[i];
+    if (tn.inverse) cs.y = -cs.y;
     if (second) { turn(w, u, cs); return u; }
     turn(u, w, cs);
     return u;
 }
 
-// 16 dimensions d0.. of a key row, turned; VEC: every stretch of 8 is aligned and turns or passes as a whole
+// 8 dimensions d0.. of a row, turned; VEC: rows and the table on 16 bytes
 template <typename T, bool VEC>
-__device__ __forceinline__ void key_group(const T *row, int D, int d0, const Turn &tn, const float2 *cs_row, float (&x)[16]) {
-    if (VEC) {
-        const int half = tn.rot / 2;
+__device__ __forceinline__ void turned8(const T *row, int D, int d0, const Turn &tn, const float2 *cs_row, float (&a)[8]) {
+    if (d0 >= D) {
 #pragma unroll
-        for (int part = 0; part < 2; ++part) {
-            const int d = d0 + 8 * part;
-            float a[8], b[8];
-            if (d >= D) {
+        for (int i = 0; i < 8; ++i) a[i] = 0.f;
+        return;
+    }
+    load8<VEC>(row + d0, D - d0, a);
+    if (!cs_row || d0 >= tn.rot) return;
+    const int half = tn.rot / 2;
+    if (VEC && tn.layout == MOE_ROPE_HALF && half % 8 == 0) {
+        const bool second = d0 >= half;
+        const float4 *cs = reinterpret_cast<const float4 *>(cs_row + (second ? d0 - half : d0));
+        float b[8];
+        load8<true>(row + (second ? d0 - half : d0 + half), 8, b);
+        // as turn(), this thread's end only: own cos -+ other sin, whichever end it is
+        const uint32_t flip = second ? 0u : 0x80000000u;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) a[i] = 0.f;
-            } else {
-                load8<true>(row + d, 8, a);
-                if (cs_row && d < tn.rot) {
-                    if (tn.layout == MOE_ROPE_HALF) {
-                        const bool second = d >= half;
-                        const float2 *cs = cs_row + (second ? d - half : d);
-                        load8<true>(row + (second ? d - half : d + half), 8, b);
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            if (second) turn(b[i], a[i], cs[i]); else turn(a[i], b[i], cs[i]);
-                        }
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) turn(a[2 * i], a[2 * i + 1], cs_row[d / 2 + i]);
-                    }
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[8 * part + i] = a[i];
+        for (int i = 0; i < 8; i += 2) {
+            const float4 v = cs[i / 2];
+            a[i] = __fadd_rn(__fmul_rn(a[i], v.x), __fmul_rn(b[i], __uint_as_float(__float_as_uint(v.y) ^ flip)));
+            a[i + 1] = __fadd_rn(__fmul_rn(a[i + 1], v.z), __fmul_rn(b[i + 1], __uint_as_float(__float_as_uint(v.w) ^ flip)));
         }
+    } else if (tn.layout == MOE_ROPE_PAIRS) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (d0 / 2 + i < half) turn(a[2 * i], a[2 * i + 1], cs_row[d0 / 2 + i]);
     } else {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = d0 + i < D ? turned_at(row, tn, cs_row, d0 + i) : 0.f;
+        for (int i = 0; i < 8; ++i)
+            if (d0 + i < tn.rot) a[i] = turned_at(row, tn, cs_row, d0 + i);
     }
 }
 
 // Address of a slot's block; nullptr for a slot that is not stored
-__device__ __forceinline__ uint8_t *block_of(uint8_t *cache, int64_t slot, int64_t n_slots, int page, int Hk, int h, int W, int32_t *status) {
+__device__ __forceinline__ uint8_t *block_of(uint8_t *cache, int64_t slot, int64_t n_slots, int page_shift, int Hk, int h, int W, int32_t *status) {
     if (slot < 0 || slot >= n_slots) {
         if (slot != -1) atomicOr(status, MOE_KV_STATUS_BAD_INDEX);
         return nullptr;
     }
-    const int64_t pg = slot / page;
-    const int in = (int)(slot - pg * page);
-    return cache + ((pg * Hk + h) * (page / kBlockTokens) + in / kBlockTokens) * (int64_t)block_bytes(W);
+    const int64_t pg = slot >> page_shift;
+    const int in = (int)slot & ((1 << page_shift) - 1);
+    return cache + ((((pg * Hk + h) << page_shift) + in) >> 4) * (int64_t)block_bytes(W);
 }
 
-// One launch, three stretches of CTAs: queries turn (units as in rope_kernel), keys turn and are stored, values are
-// stored.  A thread stores one group of 16 dimensions: 8 bytes of codes and a scale.  Neighbouring threads take the
-// groups of one key row (its codes are neighbours in a block) but the same stretch of 16 tokens' value rows (which are
-// neighbours there), so both write whole sectors.
-template <typename T, bool VEC>
-__global__ void __launch_bounds__(kThreads) append_kernel(AppendArgs a, int q_ctas, int k_ctas, int groups, int per_group, int W) {
-    const int ng = W / 16;
-    if ((int)blockIdx.x < q_ctas) {
-        const Units un = units_of(a.D, a.turn.rot);
-        const int nu = un.turning + un.passing;
-        const long long e = (long long)blockIdx.x * kThreads + threadIdx.x;
-        if (e >= (long long)a.T * groups * nu) return;
-        const int unit = (int)(e % nu), grp = (int)(e / nu % groups), t = (int)(e / nu / groups);
-        float2 cs[8];
-        const bool turns = unit_angles(a.turn, t, unit, un, cs, a.status);
-        const int h1 = min(a.H, (grp + 1) * per_group);
-        for (int h = grp * per_group; h < h1; ++h)
-            turn_unit<T, VEC>((const T *)a.q.p + t * a.q.ts + h * a.q.hs, (T *)a.q_out + ((int64_t)t * a.H + h) * a.D, a.D, a.turn, turns, unit, un, cs);
+// One launch, two kinds of CTAs: queries turn as in rope_kernel; keys and values are stored by a thread for 8
+// dimensions, W/8 neighbouring threads having a row, two of them a group's scale.  Rows are read in whole lines and a
+// key's codes leave in one piece; a value's codes leave as W/8 pieces, next to those of its 15 neighbours, which the L2
+// puts together (through shared memory, a warp for 16 tokens, it took 1.8 times as long: fewer loads in flight).
+template <typename T, int WALK, bool VEC, int W>
+__global__ void __launch_bounds__(kThreads) append_kernel(AppendArgs a, uint32_t store_ratio, FastDiv units, FastDiv groups, int per_group, FastDiv rows_per_token) {
+    constexpr int kLanes = W / 8;
+    // the storing CTAs (bound by instructions) lie evenly among the turning ones (bound by memory): number f(i) is CTA i
+    // where f(i + 1) > f(i), f(i) = i * ratio / 2^32
+    const uint32_t store = __umulhi(blockIdx.x, store_ratio);
+    if (store_ratio != 0xffffffffu && __umulhi(blockIdx.x + 1, store_ratio) == store) {
+        uint32_t e = (blockIdx.x - store) * kThreads + threadIdx.x, unit, grp, token;
+        units.split(e, e, unit);
+        groups.split(e, token, grp);
+        if (token >= (uint32_t)a.T) return;
+        const int64_t t = token;
+        const int h0 = (int)grp * per_group;
+        turn_unit<T, WALK, VEC>((const T *)a.q.p + t * a.q.ts + h0 * a.q.hs, a.q.hs, (T *)a.q_out + (t * a.H + h0) * a.D, a.D, min(per_group, a.H - h0), a.D, a.turn,
+                                (int)t, (int)unit, a.status);
         return;
     }
-    const bool key = (int)blockIdx.x < q_ctas + k_ctas;
-    const long long e = (long long)(blockIdx.x - q_ctas - (key ? 0 : k_ctas)) * kThreads + threadIdx.x;
-    int g, h;
-    long long t;
-    if (key) {
-        g = (int)(e % ng); h = (int)(e / ng % a.Hk); t = e / ng / a.Hk;
-    } else {
-        const long long u = e / 16;
-        g = (int)(u % ng); h = (int)(u / ng % a.Hk); t = u / ng / a.Hk * 16 + e % 16;
-    }
-    if (t >= a.T) return;
-    const int64_t slot = a.slot[t];
-    uint8_t *blk = block_of(a.cache, slot, a.n_slots, a.page, a.Hk, h, W, a.status);
-    if (!blk) return;
-    const int token = (int)(slot % kBlockTokens);
-    float x[16];
-    uint32_t s8;
-    if (key) {
+    // keys' rows of a token, then its values'; a row's lanes are in one warp and go together
+    const uint32_t e = (store_ratio != 0xffffffffu ? store : blockIdx.x) * kThreads + threadIdx.x;
+    const int c = (int)(e % kLanes);
+    uint32_t token_no, row;
+    rows_per_token.split(e / kLanes, token_no, row);
+    const int h = (int)row < a.Hk ? (int)row : (int)row - a.Hk;
+    const int64_t t = token_no;
+    const bool key = (int)row < a.Hk;
+    const int64_t slot = t < a.T ? a.slot[t] : -1;
+    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    uint8_t *blk = block_of(a.cache, slot, a.n_slots, a.page_shift, a.Hk, h, W, a.status);
+    if (blk) {
         const float2 *cs_row = nullptr;
-        if (a.turn.rot) {
+        if (key && a.turn.rot) {
             const int p = a.turn.position[t];
             if (p >= 0 && p < a.turn.n_positions) cs_row = a.turn.table + (int64_t)p * (a.turn.rot / 2);
             else atomicOr(a.status, MOE_KV_STATUS_BAD_INDEX);
         }
-        key_group<T, VEC>((const T *)a.k.p + t * a.k.ts + h * a.k.hs, a.D, g * 16, a.turn, cs_row, x);
-        const uint2 c = quantise(x, a.k_inv6, a.k_scale, s8, a.status);
-        *reinterpret_cast<uint2 *>(blk + token * (W / 2) + g * 8) = c;
-        blk[k_scales_at(W) + token * ng + g] = (uint8_t)s8;
+        const Rows &rows = key ? a.k : a.v;
+        turned8<T, VEC>((const T *)rows.p + t * rows.ts + h * rows.hs, a.D, 8 * c, a.turn, cs_row, v);
+    }
+    uint32_t s8;
+    const uint32_t codes = quantise8(v, key ? a.k_inv6 : a.v_inv6, key ? a.k_scale : a.v_scale, s8, a.status);
+    if (!blk) return;
+    const int token = (int)(slot % kBlockTokens);
+    if (key) {
+        *reinterpret_cast<uint32_t *>(blk + token * (W / 2) + 4 * c) = codes;
+        if (c % 2 == 0) blk[k_scales_at(W) + token * (W / 16) + c / 2] = (uint8_t)s8;
     } else {
-        Turn still = a.turn;
-        still.rot = 0;
-        key_group<T, VEC>((const T *)a.v.p + t * a.v.ts + h * a.v.hs, a.D, g * 16, still, nullptr, x);
-        const uint2 c = quantise(x, a.v_inv6, a.v_scale, s8, a.status);
-        uint8_t *codes = blk + v_codes_at(W);
-        const int vb = W / 16;
-        if (W == 64) {
-            *reinterpret_cast<uint32_t *>(codes + 2 * g * 64 + ((token * 4) ^ v_turn(64, 2 * g))) = c.x;
-            *reinterpret_cast<uint32_t *>(codes + (2 * g + 1) * 64 + ((token * 4) ^ v_turn(64, 2 * g + 1))) = c.y;
-        } else if (W == 128) {
-            *reinterpret_cast<uint2 *>(codes + g * 128 + ((token * vb) ^ v_turn(128, g))) = c;
-        } else {
-            const int r = g >> 1;
-            *reinterpret_cast<uint2 *>(codes + r * 256 + ((token * vb) ^ v_turn(256, r)) + (g & 1) * 8) = c;
-        }
-        blk[v_scales_at(W) + g * kBlockTokens + token] = (uint8_t)s8;
+        constexpr int per = W / 64;                 // chunks of 8 dimensions in a stretch of the layout
+        const int r = c / per;
+        *reinterpret_cast<uint32_t *>(blk + v_codes_at(W) + r * W + ((token * (W / 16)) ^ v_turn(W, r)) + 4 * (c % per)) = codes;
+        if (c % 2 == 0) blk[v_scales_at(W) + c / 2 * kBlockTokens + token] = (uint8_t)s8;
     }
 }
 
-// A thread reads one group of 16 dimensions of a key or value row
-template <typename T>
-__global__ void __launch_bounds__(kThreads) read_kernel(ReadArgs a, int W) {
-    const int ng = (a.D + 15) / 16;
-    const long long e = (long long)blockIdx.x * kThreads + threadIdx.x;
-    const bool key = blockIdx.y == 0 && a.k != nullptr;
-    const int g = (int)(e % ng), h = (int)(e / ng % a.Hk);
-    const long long t = e / ng / a.Hk;
-    if (t >= a.T) return;
+// A thread reads 8 dimensions of a key row and of a value row
+template <typename T, int W>
+__global__ void __launch_bounds__(kThreads) read_kernel(ReadArgs a, FastDiv chunks, FastDiv heads) {
+    uint32_t e = blockIdx.x * kThreads + threadIdx.x, chunk, head, token_no;
+    chunks.split(e, e, chunk);
+    heads.split(e, token_no, head);
+    if (token_no >= (uint32_t)a.T) return;
+    const int c = (int)chunk, h = (int)head;
+    const int64_t t = token_no;
     const int64_t slot = a.slot[t];
-    const uint8_t *blk = block_of(const_cast<uint8_t *>(a.cache), slot, a.n_slots, a.page, a.Hk, h, W, a.status);
-    uint2 c = make_uint2(0u, 0u);
-    float s = 0.f;
+    const uint8_t *blk = block_of(const_cast<uint8_t *>(a.cache), slot, a.n_slots, a.page_shift, a.Hk, h, W, a.status);
+    uint32_t kw = 0u, vw = 0u;
+    float ks = 0.f, vs = 0.f;
     if (blk) {
-        const int token = (int)(slot % kBlockTokens), vb = W / 16;
-        if (key) {
-            c = *reinterpret_cast<const uint2 *>(blk + token * (W / 2) + g * 8);
-            s = from_e4m3(blk[k_scales_at(W) + token * (W / 16) + g]);
-        } else {
-            const uint8_t *codes = blk + v_codes_at(W);
-            if (W == 64) {
-                c.x = *reinterpret_cast<const uint32_t *>(codes + 2 * g * 64 + ((token * 4) ^ v_turn(64, 2 * g)));
-                c.y = *reinterpret_cast<const uint32_t *>(codes + (2 * g + 1) * 64 + ((token * 4) ^ v_turn(64, 2 * g + 1)));
-            } else if (W == 128) {
-                c = *reinterpret_cast<const uint2 *>(codes + g * 128 + ((token * vb) ^ v_turn(128, g)));
-            } else {
-                const int r = g >> 1;
-                c = *reinterpret_cast<const uint2 *>(codes + r * 256 + ((token * vb) ^ v_turn(256, r)) + (g & 1) * 8);
-            }
-            s = from_e4m3(blk[v_scales_at(W) + g * kBlockTokens + token]);
+        constexpr int per = W / 64;                 // stretches of 8 dimensions in one of the layout's
+        const int token = (int)(slot & 15), r = c / per;
+        if (a.k) {
+            kw = *reinterpret_cast<const uint32_t *>(blk + token * (W / 2) + 4 * c);
+            ks = from_e4m3(blk[k_scales_at(W) + token * (W / 16) + c / 2]);
+        }
+        if (a.v) {
+            vw = *reinterpret_cast<const uint32_t *>(blk + v_codes_at(W) + r * W + ((token * (W / 16)) ^ v_turn(W, r)) + 4 * (c % per));
+            vs = from_e4m3(blk[v_scales_at(W) + c / 2 * kBlockTokens + token]);
         }
     }
-    const float scale = key ? a.k_scale : a.v_scale;
-    T *out = (T *)(key ? a.k : a.v) + ((int64_t)t * a.Hk + h) * a.D + g * 16;
+    const int64_t out = (t * a.Hk + h) * a.D + 8 * c;
 #pragma unroll
-    for (int part = 0; part < 2; ++part) {
-        const uint32_t w = part ? c.y : c.x;
+    for (int which = 0; which < 2; ++which) {
+        T *dst = (T *)(which ? a.v : a.k);
+        if (!dst) continue;
         float x[8];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float2 f = from_e2m1_pair((w >> (8 * i)) & 0xffu);
-            x[2 * i] = f.x * s * scale;          // code * s has at most 6 bits: one rounding
-            x[2 * i + 1] = f.y * s * scale;
+            const float2 f = from_e2m1_pair((which ? vw : kw) >> (8 * i) & 0xffu);
+            x[2 * i] = f.x * (which ? vs : ks) * (which ? a.v_scale : a.k_scale);          // code * scale has at most 6 bits: one rounding
+            x[2 * i + 1] = f.y * (which ? vs : ks) * (which ? a.v_scale : a.k_scale);
         }
-        if (g * 16 + part * 8 < a.D) store8<true>(out + part * 8, 8, x);
+        store8<true>(dst + out, 8, x);
     }
 }
 
@@ -398,11 +453,47 @@ bool aligned(const void *p, int64_t ts, int64_t hs, int dtype) {
     return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && ts % e == 0 && hs % e == 0;
 }
 
-// Stretches of 8 dimensions (8 pairs) that turn or pass as a whole
-bool whole_units(int D, int rot) { return rot % 16 == 0 && D % 8 == 0; }
+Walk walk_of(int D, const Turn &tn, bool rows16, bool in_place) {
+    if (!rows16 || D % 8) return kSingles;
+    if (tn.rot == 0 || tn.layout == MOE_ROPE_PAIRS) return kPairs;
+    if (tn.rot % 16 == 0) return kHalves;
+    return in_place ? kSingles : kPartners;
+}
 
-// Heads that share a thread's angles: 4 once there are enough threads for the machine without it
-int heads_per_thread(long long threads, int sm_count) { return threads >= 4ll * 2048 * sm_count ? 4 : 1; }
+// Heads that share a thread's angles: kHeads once there are enough threads for the machine without it
+int heads_per_thread(long long threads, int sm_count) { return threads >= (long long)kHeads * 2048 * sm_count ? kHeads : 1; }
+
+bool table16(const Turn &tn) { return tn.rot == 0 || ((reinterpret_cast<uintptr_t>(tn.table) & 15u) == 0 && (tn.rot / 2) % 2 == 0); }
+
+template <typename T>
+auto rope_of(Walk w, bool t16) {
+    switch (w) {
+        case kHalves: return t16 ? rope_kernel<T, kHalves, true> : rope_kernel<T, kHalves, false>;
+        case kPairs: return t16 ? rope_kernel<T, kPairs, true> : rope_kernel<T, kPairs, false>;
+        case kPartners: return rope_kernel<T, kPartners, false>;
+        default: return rope_kernel<T, kSingles, false>;
+    }
+}
+// VEC: rows and table on 16 bytes
+template <typename T, int W>
+auto append_of(Walk w, bool vec) {
+    if (!vec) {
+        switch (w) {
+            case kHalves: return append_kernel<T, kHalves, false, W>;
+            case kPairs: return append_kernel<T, kPairs, false, W>;
+            case kPartners: return append_kernel<T, kPartners, false, W>;
+            default: return append_kernel<T, kSingles, false, W>;
+        }
+    }
+    switch (w) {
+        case kHalves: return append_kernel<T, kHalves, true, W>;
+        case kPairs: return append_kernel<T, kPairs, true, W>;
+        case kPartners: return append_kernel<T, kPartners, true, W>;
+        default: return append_kernel<T, kSingles, true, W>;
+    }
+}
+template <typename T>
+auto append_of(int width, Walk w, bool vec) { return width == 64 ? append_of<T, 64>(w, vec) : width == 128 ? append_of<T, 128>(w, vec) : append_of<T, 256>(w, vec); }
 
 }  // namespace
 
@@ -414,50 +505,84 @@ cudaError_t launch_rope_table(const RopeTableArgs &a, cudaStream_t s) {
     return cudaGetLastError();
 }
 
-cudaError_t launch_rope(const RopeArgs &a, int sm_count, cudaStream_t s, uint64_t *launches) {
-    const Units un = units_of(a.D, a.turn.rot);
-    const int nu = un.turning + un.passing;
-    const int per = heads_per_thread((long long)a.T * a.H * nu, sm_count), groups = (a.H + per - 1) / per;
-    const long long grid = ((long long)a.T * groups * nu + kThreads - 1) / kThreads;
-    if (grid == 0) return cudaSuccess;
-    if (grid > 0x7fffffffll) return cudaErrorInvalidValue;
-    const bool vec = whole_units(a.D, a.turn.rot) && aligned(a.x.p, a.x.ts, a.x.hs, a.dtype) && aligned(a.y, a.yts, a.yhs, a.dtype);
-    auto k = a.dtype == MOE_BF16 ? (vec ? rope_kernel<__nv_bfloat16, true> : rope_kernel<__nv_bfloat16, false>)
-                                 : (vec ? rope_kernel<float, true> : rope_kernel<float, false>);
-    k<<<(int)grid, kThreads, 0, s>>>(a, groups, per);
-    ++*launches;
-    return cudaGetLastError();
+// Tokens of one launch: thread numbers have 32 bits (a longer call is several launches)
+static int tokens_at_once(long long threads_per_token) {
+    const long long most = 0xf0000000ll / (threads_per_token < 1 ? 1 : threads_per_token);
+    return most > 0x7fffffff ? 0x7fffffff : (int)most;
+}
+static const void *moved(const void *p, int64_t elements, int dtype) { return (const uint8_t *)p + elements * (dtype == MOE_BF16 ? 2 : 4); }
+
+cudaError_t launch_rope(const RopeArgs &all, int sm_count, cudaStream_t s, uint64_t *launches) {
+    const bool rows16 = aligned(all.x.p, all.x.ts, all.x.hs, all.dtype) && aligned(all.y, all.yts, all.yhs, all.dtype);
+    const Walk walk = walk_of(all.D, all.turn, rows16, all.x.p == all.y);
+    const int units = units_of(walk, all.D, all.turn.rot);
+    const int per = heads_per_thread((long long)all.T * all.H * units, sm_count), groups = (all.H + per - 1) / per;
+    const bool t16 = table16(all.turn);
+    auto k = all.dtype == MOE_BF16 ? rope_of<__nv_bfloat16>(walk, t16) : rope_of<float>(walk, t16);
+    const int step = tokens_at_once((long long)groups * units);
+    for (int t0 = 0; t0 < all.T; t0 += step) {
+        RopeArgs a = all;
+        a.T = all.T - t0 < step ? all.T - t0 : step;
+        a.x.p = moved(all.x.p, t0 * all.x.ts, all.dtype);
+        a.y = (void *)moved(all.y, t0 * all.yts, all.dtype);
+        a.turn.position += t0;
+        k<<<(unsigned)(((long long)a.T * groups * units + kThreads - 1) / kThreads), kThreads, 0, s>>>(a, FastDiv(units), FastDiv(groups), per);
+        ++*launches;
+        if (cudaError_t err = cudaGetLastError()) return err;
+    }
+    return cudaSuccess;
 }
 
-cudaError_t launch_append(const AppendArgs &a, int sm_count, cudaStream_t s, uint64_t *launches) {
-    if (a.T == 0) return cudaSuccess;
-    const int W = padded_width(a.D), ng = W / 16;
-    const Units un = units_of(a.D, a.turn.rot);
-    const int nu = un.turning + un.passing;
-    const int per = heads_per_thread((long long)a.T * a.H * nu, sm_count), groups = (a.H + per - 1) / per;
-    auto ctas = [](long long n) { return (n + kThreads - 1) / kThreads; };
+cudaError_t launch_append(const AppendArgs &all, int sm_count, cudaStream_t s, uint64_t *launches) {
+    const bool q16 = !all.q.p || (aligned(all.q.p, all.q.ts, all.q.hs, all.dtype) && aligned(all.q_out, (int64_t)all.H * all.D, all.D, all.dtype));
+    const Walk walk = walk_of(all.D, all.turn, q16, all.q.p == all.q_out);
+    const int units = units_of(walk, all.D, all.turn.rot);
+    const int per = heads_per_thread((long long)all.T * all.H * units, sm_count), groups = (all.H + per - 1) / per;
     // nothing to do where the queries stay as they are, in place
-    const bool q_moves = a.q.p && (a.turn.rot || a.q.p != a.q_out);
-    const long long qc = q_moves ? ctas((long long)a.T * groups * nu) : 0;
-    const long long kc = ctas((long long)a.T * a.Hk * ng), vc = ctas((long long)((a.T + 15) / 16 * 16) * a.Hk * ng);
-    if (qc + kc + vc > 0x7fffffffll) return cudaErrorInvalidValue;
-    bool vec = whole_units(a.D, a.turn.rot) && aligned(a.k.p, a.k.ts, a.k.hs, a.dtype) && aligned(a.v.p, a.v.ts, a.v.hs, a.dtype);
-    if (a.q.p) vec = vec && aligned(a.q.p, a.q.ts, a.q.hs, a.dtype) && aligned(a.q_out, (int64_t)a.H * a.D, a.D, a.dtype);
-    auto k = a.dtype == MOE_BF16 ? (vec ? append_kernel<__nv_bfloat16, true> : append_kernel<__nv_bfloat16, false>)
-                                 : (vec ? append_kernel<float, true> : append_kernel<float, false>);
-    k<<<(int)(qc + kc + vc), kThreads, 0, s>>>(a, (int)qc, (int)kc, groups, per, W);
-    ++*launches;
-    return cudaGetLastError();
+    const bool q_moves = all.q.p && (all.turn.rot || all.q.p != all.q_out);
+    const bool vec = table16(all.turn) && aligned(all.k.p, all.k.ts, all.k.hs, all.dtype) && aligned(all.v.p, all.v.ts, all.v.hs, all.dtype);
+    const int w = padded_width(all.D);
+    auto k = all.dtype == MOE_BF16 ? append_of<__nv_bfloat16>(w, walk, vec) : append_of<float>(w, walk, vec);
+    const int step = tokens_at_once((long long)groups * units + 2ll * all.Hk * (w / 8));
+    for (int t0 = 0; t0 < all.T; t0 += step) {
+        AppendArgs a = all;
+        a.T = all.T - t0 < step ? all.T - t0 : step;
+        a.k.p = moved(all.k.p, t0 * all.k.ts, all.dtype);
+        a.v.p = moved(all.v.p, t0 * all.v.ts, all.dtype);
+        a.slot += t0;
+        if (a.turn.rot) a.turn.position += t0;
+        if (a.q.p) {
+            a.q.p = moved(all.q.p, t0 * all.q.ts, all.dtype);
+            a.q_out = (void *)moved(all.q_out, (int64_t)t0 * all.H * all.D, all.dtype);
+        }
+        const long long qc = q_moves ? ((long long)a.T * groups * units + kThreads - 1) / kThreads : 0;
+        const long long sc = ((long long)a.T * a.Hk * 2 * (w / 8) + kThreads - 1) / kThreads;
+        // ceil(2^32 sc / (qc + sc)): f(qc + sc) = sc exactly; all ones where nothing turns
+        const uint32_t ratio = qc == 0 ? 0xffffffffu : (uint32_t)((((unsigned long long)sc << 32) + qc + sc - 1) / (qc + sc));
+        k<<<(unsigned)(qc + sc), kThreads, 0, s>>>(a, ratio, FastDiv(units), FastDiv(groups), per, FastDiv(2 * a.Hk));
+        ++*launches;
+        if (cudaError_t err = cudaGetLastError()) return err;
+    }
+    return cudaSuccess;
 }
 
-cudaError_t launch_read(const ReadArgs &a, cudaStream_t s, uint64_t *launches) {
-    if (a.T == 0 || (!a.k && !a.v)) return cudaSuccess;
-    const long long grid = ((long long)a.T * a.Hk * ((a.D + 15) / 16) + kThreads - 1) / kThreads;
-    if (grid > 0x7fffffffll) return cudaErrorInvalidValue;
-    auto k = a.dtype == MOE_BF16 ? read_kernel<__nv_bfloat16> : read_kernel<float>;
-    k<<<dim3((unsigned)grid, a.k && a.v ? 2 : 1), kThreads, 0, s>>>(a, padded_width(a.D));
-    ++*launches;
-    return cudaGetLastError();
+cudaError_t launch_read(const ReadArgs &all, cudaStream_t s, uint64_t *launches) {
+    if (!all.k && !all.v) return cudaSuccess;
+    const int chunks = all.D / 8, w = padded_width(all.D);
+    auto k = all.dtype == MOE_BF16 ? (w == 64 ? read_kernel<__nv_bfloat16, 64> : w == 128 ? read_kernel<__nv_bfloat16, 128> : read_kernel<__nv_bfloat16, 256>)
+                                   : (w == 64 ? read_kernel<float, 64> : w == 128 ? read_kernel<float, 128> : read_kernel<float, 256>);
+    const int step = tokens_at_once((long long)all.Hk * chunks);
+    for (int t0 = 0; t0 < all.T; t0 += step) {
+        ReadArgs a = all;
+        a.T = all.T - t0 < step ? all.T - t0 : step;
+        a.slot += t0;
+        if (a.k) a.k = (void *)moved(all.k, (int64_t)t0 * all.Hk * all.D, all.dtype);
+        if (a.v) a.v = (void *)moved(all.v, (int64_t)t0 * all.Hk * all.D, all.dtype);
+        k<<<(unsigned)(((long long)a.T * a.Hk * chunks + kThreads - 1) / kThreads), kThreads, 0, s>>>(a, FastDiv(chunks), FastDiv(a.Hk));
+        ++*launches;
+        if (cudaError_t err = cudaGetLastError()) return err;
+    }
+    return cudaSuccess;
 }
 
 }  // namespace kv
