@@ -51,7 +51,7 @@ struct FastDiv {
 struct TablesArgs {
     const int32_t *ctx, *fresh_tokens; int n;
     const int32_t *free_pages; int n_free;
-    int32_t *table; int width, page;
+    int32_t *table; int width, page_shift;        // a page has 1 << page_shift tokens
     int n_tokens;
     int32_t *kv_len, *cu, *position; int64_t *slot; int32_t *taken;
     int32_t *status;

@@ -159,7 +159,7 @@ int moe_kv_tables(moe_kv_plan_t *p, const int32_t *ctx_len, const int32_t *new_l
         return MOE_ERR_INVALID_ARG;
     if (n > 0 && (!ctx_len || !new_len || !kv_len || (width > 0 && !block_table))) return MOE_ERR_INVALID_ARG;
     if ((n_free > 0 && !free_pages) || (n_tokens > 0 && (!position || !slot))) return MOE_ERR_INVALID_ARG;
-    TablesArgs a{ctx_len, new_len, n, free_pages, n_free, block_table, width, p->cfg.page_size, n_tokens,
+    TablesArgs a{ctx_len, new_len, n, free_pages, n_free, block_table, width, page_shift(p->cfg) + 4, n_tokens,
                  kv_len, cu_new, position, slot, taken, p->status};
     return done(launch_tables(a, p->sm_count, (cudaStream_t)stream, &p->launches));
 }

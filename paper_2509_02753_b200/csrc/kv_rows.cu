@@ -150,7 +150,9 @@ __device__ __forceinline__ void load_angles(const Turn &tn, int t, int i0, float
 template <typename T>
 __device__ __forceinline__ float turned_at(const T *row, const Turn &tn, const float2 *cs_row, int d);
 
-constexpr int kHeads = 4;          // heads a thread takes where there are enough rows
+// Heads a thread takes where there are enough rows: it reads the angles once for them.  8192 tokens x 32 heads of 128
+// dimensions, bf16: 35.7, 28.7, 27.6 us with 1, 2, 4
+constexpr int kHeads = 4;
 
 // heads h0 .. h0 + n of unit `unit` of token t
 template <typename T, int WALK, bool TABLE16>
@@ -163,13 +165,13 @@ __device__ __forceinline__ void turn_unit(const T *x, int64_t xhs, T *y, int64_t
         const bool turner = unit < turning;
         const int d0 = WALK == kPairs ? 16 * unit : turner ? 8 * unit : tn.rot + 16 * (unit - turning);
         const int d1 = WALK == kHalves && turner ? half + d0 : d0 + 8;
+        // rows are asked for before the angles, which wait for the position
+        float a[8], b[8];
+        load8<true>(x + d0, 8, a);
+        if (d1 < D) load8<true>(x + d1, 8, b);
         load_angles<TABLE16>(tn, t, WALK == kPairs ? d0 / 2 : turner ? d0 : half, cs, turns, status);
         if (!turns && x == y) return;
-        // (four heads' loads at once took 1.5 times as long: the registers cost more warps than they keep loads in flight)
         for (int h = 0; h < n; ++h) {
-            float a[8], b[8];
-            load8<true>(x + h * xhs + d0, 8, a);
-            if (d1 < D) load8<true>(x + h * xhs + d1, 8, b);
             if (turns) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
@@ -180,6 +182,10 @@ __device__ __forceinline__ void turn_unit(const T *x, int64_t xhs, T *y, int64_t
             }
             store8<true>(y + h * yhs + d0, 8, a);
             if (d1 < D) store8<true>(y + h * yhs + d1, 8, b);
+            if (h + 1 < n) {
+                load8<true>(x + (h + 1) * xhs + d0, 8, a);
+                if (d1 < D) load8<true>(x + (h + 1) * xhs + d1, 8, b);
+            }
         }
     } else if (WALK == kPartners) {
         const int d0 = 8 * unit;
@@ -304,23 +310,27 @@ __device__ __forceinline__ float turned_at(const T *row, const Turn &tn, const f
     return u;
 }
 
-// 8 dimensions d0.. of a row, turned; VEC: rows and the table on 16 bytes
+// 8 dimensions d0.. of a row, turned; VEC: rows and the table on 16 bytes.  In two parts, so that the row's bytes are
+// asked for before the position is known: a are the dimensions, b what they turn with where that is another stretch of 8
 template <typename T, bool VEC>
-__device__ __forceinline__ void turned8(const T *row, int D, int d0, const Turn &tn, const float2 *cs_row, float (&a)[8]) {
+__device__ __forceinline__ void load_turned8(const T *row, int D, int d0, const Turn &tn, bool turns, float (&a)[8], float (&b)[8]) {
     if (d0 >= D) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) a[i] = 0.f;
         return;
     }
     load8<VEC>(row + d0, D - d0, a);
+    const int half = tn.rot / 2;
+    if (VEC && turns && d0 < tn.rot && tn.layout == MOE_ROPE_HALF && half % 8 == 0) load8<true>(row + (d0 >= half ? d0 - half : d0 + half), 8, b);
+}
+template <typename T, bool VEC>
+__device__ __forceinline__ void turn8(const T *row, int d0, const Turn &tn, const float2 *cs_row, float (&a)[8], const float (&b)[8]) {
     if (!cs_row || d0 >= tn.rot) return;
     const int half = tn.rot / 2;
     if (VEC && tn.layout == MOE_ROPE_HALF && half % 8 == 0) {
+        // as turn(), this thread's end only: own cos -+ other sin, whichever end it is
         const bool second = d0 >= half;
         const float4 *cs = reinterpret_cast<const float4 *>(cs_row + (second ? d0 - half : d0));
-        float b[8];
-        load8<true>(row + (second ? d0 - half : d0 + half), 8, b);
-        // as turn(), this thread's end only: own cos -+ other sin, whichever end it is
         const uint32_t flip = second ? 0u : 0x80000000u;
 #pragma unroll
         for (int i = 0; i < 8; i += 2) {
@@ -351,11 +361,11 @@ __device__ __forceinline__ uint8_t *block_of(uint8_t *cache, int64_t slot, int64
 }
 
 // One launch, two kinds of CTAs: queries turn as in rope_kernel; keys and values are stored by a thread for 8
-// dimensions, W/8 neighbouring threads having a row, two of them a group's scale.  Rows are read in whole lines and a
+// dimensions of both, W/8 neighbouring threads having a row, two of them a group's scale.  Rows are read in whole lines and a
 // key's codes leave in one piece; a value's codes leave as W/8 pieces, next to those of its 15 neighbours, which the L2
 // puts together (through shared memory, a warp for 16 tokens, it took 1.8 times as long: fewer loads in flight).
 template <typename T, int WALK, bool VEC, int W>
-__global__ void __launch_bounds__(kThreads) append_kernel(AppendArgs a, uint32_t store_ratio, FastDiv units, FastDiv groups, int per_group, FastDiv rows_per_token) {
+__global__ void __launch_bounds__(kThreads, 4) append_kernel(AppendArgs a, uint32_t store_ratio, FastDiv units, FastDiv groups, int per_group, FastDiv heads) {
     constexpr int kLanes = W / 8;
     // the storing CTAs (bound by instructions) lie evenly among the turning ones (bound by memory): number f(i) is CTA i
     // where f(i + 1) > f(i), f(i) = i * ratio / 2^32
@@ -371,39 +381,44 @@ __global__ void __launch_bounds__(kThreads) append_kernel(AppendArgs a, uint32_t
                                 (int)t, (int)unit, a.status);
         return;
     }
-    // keys' rows of a token, then its values'; a row's lanes are in one warp and go together
+    // a row's lanes are in one warp and go together
     const uint32_t e = (store_ratio != 0xffffffffu ? store : blockIdx.x) * kThreads + threadIdx.x;
     const int c = (int)(e % kLanes);
-    uint32_t token_no, row;
-    rows_per_token.split(e / kLanes, token_no, row);
-    const int h = (int)row < a.Hk ? (int)row : (int)row - a.Hk;
+    uint32_t token_no, head;
+    heads.split(e / kLanes, token_no, head);
+    const int h = (int)head;
     const int64_t t = token_no;
-    const bool key = (int)row < a.Hk;
-    const int64_t slot = t < a.T ? a.slot[t] : -1;
-    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    const bool real = t < a.T, turns = a.turn.rot > 0;
+    const T *k_src = (const T *)a.k.p + t * a.k.ts + h * a.k.hs, *v_src = (const T *)a.v.p + t * a.v.ts + h * a.v.hs;
+    float k[8], other[8], v[8];
+    int64_t slot = -1;
+    int p = 0;
+    // all that is read but the angles, before anything waits
+    if (real) {
+        slot = a.slot[t];
+        if (turns) p = a.turn.position[t];
+        load_turned8<T, VEC>(k_src, a.D, 8 * c, a.turn, turns, k, other);
+        load_turned8<T, VEC>(v_src, a.D, 8 * c, a.turn, false, v, other);
+    }
     uint8_t *blk = block_of(a.cache, slot, a.n_slots, a.page_shift, a.Hk, h, W, a.status);
     if (blk) {
-        const float2 *cs_row = nullptr;
-        if (key && a.turn.rot) {
-            const int p = a.turn.position[t];
-            if (p >= 0 && p < a.turn.n_positions) cs_row = a.turn.table + (int64_t)p * (a.turn.rot / 2);
-            else atomicOr(a.status, MOE_KV_STATUS_BAD_INDEX);
-        }
-        const Rows &rows = key ? a.k : a.v;
-        turned8<T, VEC>((const T *)rows.p + t * rows.ts + h * rows.hs, a.D, 8 * c, a.turn, cs_row, v);
-    }
-    uint32_t s8;
-    const uint32_t codes = quantise8(v, key ? a.k_inv6 : a.v_inv6, key ? a.k_scale : a.v_scale, s8, a.status);
-    if (!blk) return;
-    const int token = (int)(slot % kBlockTokens);
-    if (key) {
-        *reinterpret_cast<uint32_t *>(blk + token * (W / 2) + 4 * c) = codes;
-        if (c % 2 == 0) blk[k_scales_at(W) + token * (W / 16) + c / 2] = (uint8_t)s8;
+        const bool in = p >= 0 && p < a.turn.n_positions;
+        if (turns && !in) atomicOr(a.status, MOE_KV_STATUS_BAD_INDEX);
+        if (8 * c < a.D) turn8<T, VEC>(k_src, 8 * c, a.turn, turns && in ? a.turn.table + (int64_t)p * (a.turn.rot / 2) : nullptr, k, other);
     } else {
-        constexpr int per = W / 64;                 // chunks of 8 dimensions in a stretch of the layout
-        const int r = c / per;
-        *reinterpret_cast<uint32_t *>(blk + v_codes_at(W) + r * W + ((token * (W / 16)) ^ v_turn(W, r)) + 4 * (c % per)) = codes;
-        if (c % 2 == 0) blk[v_scales_at(W) + c / 2 * kBlockTokens + token] = (uint8_t)s8;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) k[i] = v[i] = 0.f;          // what is not stored tells nothing of its numbers
+    }
+    uint32_t ks, vs;
+    const uint32_t kc = quantise8(k, a.k_inv6, a.k_scale, ks, a.status), vc = quantise8(v, a.v_inv6, a.v_scale, vs, a.status);
+    if (!blk) return;
+    constexpr int per = W / 64;                 // chunks of 8 dimensions in a stretch of the layout
+    const int token = (int)(slot % kBlockTokens), r = c / per;
+    *reinterpret_cast<uint32_t *>(blk + token * (W / 2) + 4 * c) = kc;
+    *reinterpret_cast<uint32_t *>(blk + v_codes_at(W) + r * W + ((token * (W / 16)) ^ v_turn(W, r)) + 4 * (c % per)) = vc;
+    if (c % 2 == 0) {
+        blk[k_scales_at(W) + token * (W / 16) + c / 2] = (uint8_t)ks;
+        blk[v_scales_at(W) + c / 2 * kBlockTokens + token] = (uint8_t)vs;
     }
 }
 
@@ -543,7 +558,7 @@ cudaError_t launch_append(const AppendArgs &all, int sm_count, cudaStream_t s, u
     const bool vec = table16(all.turn) && aligned(all.k.p, all.k.ts, all.k.hs, all.dtype) && aligned(all.v.p, all.v.ts, all.v.hs, all.dtype);
     const int w = padded_width(all.D);
     auto k = all.dtype == MOE_BF16 ? append_of<__nv_bfloat16>(w, walk, vec) : append_of<float>(w, walk, vec);
-    const int step = tokens_at_once((long long)groups * units + 2ll * all.Hk * (w / 8));
+    const int step = tokens_at_once((long long)groups * units + 1ll * all.Hk * (w / 8));
     for (int t0 = 0; t0 < all.T; t0 += step) {
         AppendArgs a = all;
         a.T = all.T - t0 < step ? all.T - t0 : step;
@@ -556,10 +571,10 @@ cudaError_t launch_append(const AppendArgs &all, int sm_count, cudaStream_t s, u
             a.q_out = (void *)moved(all.q_out, (int64_t)t0 * all.H * all.D, all.dtype);
         }
         const long long qc = q_moves ? ((long long)a.T * groups * units + kThreads - 1) / kThreads : 0;
-        const long long sc = ((long long)a.T * a.Hk * 2 * (w / 8) + kThreads - 1) / kThreads;
+        const long long sc = ((long long)a.T * a.Hk * (w / 8) + kThreads - 1) / kThreads;
         // ceil(2^32 sc / (qc + sc)): f(qc + sc) = sc exactly; all ones where nothing turns
         const uint32_t ratio = qc == 0 ? 0xffffffffu : (uint32_t)((((unsigned long long)sc << 32) + qc + sc - 1) / (qc + sc));
-        k<<<(unsigned)(qc + sc), kThreads, 0, s>>>(a, ratio, FastDiv(units), FastDiv(groups), per, FastDiv(2 * a.Hk));
+        k<<<(unsigned)(qc + sc), kThreads, 0, s>>>(a, ratio, FastDiv(units), FastDiv(groups), per, FastDiv(a.Hk));
         ++*launches;
         if (cudaError_t err = cudaGetLastError()) return err;
     }

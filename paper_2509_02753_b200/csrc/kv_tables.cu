@@ -15,7 +15,7 @@ namespace kv {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kTokensPerCta = 1024;
+constexpr int kTokensPerCta = kThreads;      // 16384 tokens of 512 requests: 8.1 us with four tokens a thread
 
 // last i with sum[i] <= x (sum[0] = 0 <= x); both sums are non-decreasing
 __device__ __forceinline__ int find(const int32_t *sum, int n, int x) {
@@ -34,6 +34,7 @@ __global__ void __launch_bounds__(kThreads) tables_kernel(TablesArgs a) {
     __shared__ unsigned long long carry_s;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     int bad = 0;
+    auto pages = [&](long long tokens) { return (tokens + (1 << a.page_shift) - 1) >> a.page_shift; };
 
     // running sums of (fresh pages, new tokens), packed in one 64-bit word, 256 requests at a time
     unsigned long long carry = 0;
@@ -45,7 +46,7 @@ __global__ void __launch_bounds__(kThreads) tables_kernel(TablesArgs a) {
             if (c < 0) { c = 0; bad |= MOE_KV_STATUS_BAD_INDEX; }
             if (m < 0) { m = 0; bad |= MOE_KV_STATUS_BAD_INDEX; }
             const long long total = (long long)c + m;
-            const unsigned fresh = (unsigned)((total + a.page - 1) / a.page - ((long long)c + a.page - 1) / a.page);
+            const unsigned fresh = (unsigned)(pages(total) - pages(c));
             mine = ((unsigned long long)fresh << 32) | (unsigned)m;
             if (blockIdx.x == 0) a.kv_len[i] = total > INT32_MAX ? INT32_MAX : (int32_t)total;
         }
@@ -85,7 +86,7 @@ __global__ void __launch_bounds__(kThreads) tables_kernel(TablesArgs a) {
             const int r = find(cu, a.n, t);
             const int c = max(a.ctx[r], 0);
             position = c + (t - cu[r]);
-            const int col = position / a.page, held = (int)(((long long)c + a.page - 1) / a.page);
+            const int col = position >> a.page_shift, held = (int)pages(c);
             int page = -1;
             if (col < held) {
                 if (col < a.width) page = a.table[(int64_t)r * a.width + col];
@@ -94,14 +95,14 @@ __global__ void __launch_bounds__(kThreads) tables_kernel(TablesArgs a) {
                 if (f < a.n_free && col < a.width) page = a.free_pages[f];
             }
             if (col >= a.width) bad |= MOE_KV_STATUS_NO_PAGES;
-            if (page >= 0) slot = (int64_t)page * a.page + position % a.page;
+            if (page >= 0) slot = ((int64_t)page << a.page_shift) + (position & ((1 << a.page_shift) - 1));
         }
         a.position[t] = position;
         a.slot[t] = slot;
     }
     for (int f = blockIdx.x * kThreads + tid; f < n_fresh; f += stride) {
         const int r = find(first, a.n, f);
-        const int held = (int)(((long long)max(a.ctx[r], 0) + a.page - 1) / a.page);
+        const int held = (int)pages(max(a.ctx[r], 0));
         const long long col = (long long)held + f - first[r];
         if (col < a.width) a.table[(int64_t)r * a.width + col] = f < a.n_free ? a.free_pages[f] : -1;
         else bad |= MOE_KV_STATUS_NO_PAGES;
