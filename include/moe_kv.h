@@ -50,7 +50,7 @@ typedef struct {
     int32_t head_dim;      /* multiple of 8, 8..256                                     */
     int32_t page_size;     /* tokens a page: 16, 32, 64 or 128                          */
     int32_t max_requests;  /* largest number of requests of a call, 1..4096             */
-    int32_t max_tokens;    /* largest number of new tokens of a call, >= 1              */
+    int32_t max_tokens;    /* largest number of new tokens of a call, >= 1; times n_heads at most 2^30 */
     int32_t dtype;         /* moe_dtype_t of queries, keys, values and outputs          */
 } moe_kv_config_t;
 

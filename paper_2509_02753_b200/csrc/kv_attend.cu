@@ -87,8 +87,8 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
     __shared__ float row_scale[S::kRows];          // its factor from the product to the exponent
     __shared__ float2 join_ml[kWarps][S::kRows];   // reference and sum of each warp, then weight of each warp
     __shared__ float2 row_ml[S::kRows];
-    __shared__ long long sum_s[kWarps][2];
-    __shared__ int longest_s[kWarps];
+    __shared__ long long sum_s[kWarps];
+    __shared__ int strips_s[kWarps], longest_s[kWarps];
     __shared__ int last_s;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r = lane >> 2, c = lane & 3;
 
@@ -98,12 +98,14 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
     // ---- the line: for request i, row blocks * heads * visible blocks (at least one, which writes the zeros)
     const int page_tokens = kBlockTokens << a.page_shift;
     auto lengths = [&](int i, int &len, int &q0, int &nq) {
+        const int64_t room = (int64_t)a.width * page_tokens;
         len = max(a.kv_len[i], 0);
         q0 = a.cu[i];
         nq = a.cu[i + 1] - q0;
-        if (q0 < 0 || nq < 0 || q0 > a.T - nq) { atomicOr(a.status, MOE_KV_STATUS_BAD_INDEX); nq = 0; }
-        if (len > (int64_t)a.width * page_tokens) { atomicOr(a.status, MOE_KV_STATUS_BAD_INDEX); len = a.width * page_tokens; }
-        if (a.prompt_rows > 0 && (int64_t)nq * a.G > a.prompt_rows) nq = 0;       // kv_prompt.cu's
+        const bool bad_rows = q0 < 0 || nq < 0 || q0 > a.T - nq;
+        if (bad_rows || len > room) atomicOr(a.status, MOE_KV_STATUS_BAD_INDEX);
+        if (bad_rows || (a.prompt_rows > 0 && nq * a.G > a.prompt_rows)) nq = 0;       // many rows: kv_prompt.cu's
+        len = (int)min((int64_t)len, room);
     };
     // blocks that rows [row0, row1) of a request see: [0, sb) and [wb, nb)
     auto visible = [&](int len, int nq, int row0, int row1, int &sb, int &wb, int &nb) {
@@ -119,102 +121,169 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
         return max(sb + nb - wb, 1);
     };
 
-    // ---- how much there is: blocks, stretches, the longest stretch
-    long long blocks = 0, stretches = 0;
-    int longest = 0;
-    for (int i = tid; i < a.n; i += kThreads) {
-        int len, q0, nq;
-        lengths(i, len, q0, nq);
-        for (int row0 = 0; row0 < nq * a.G; row0 += S::kRows) {
-            const int u = units_of(len, nq, row0);
-            blocks += (long long)u * a.Hk;
-            stretches += a.Hk;
-            longest = max(longest, u);
+    // ---- how much there is: blocks, stretches, the longest stretch; then how it is cut:
+    //   even   stretch by stretch, ceil(units/chunk) pieces each (one piece a CTA where there are few stretches; whole
+    //          stretches, several a CTA, where all are brief)
+    //   else   the line of all blocks, `share` of them a CTA
+    // A lane has a request; the row blocks of one with several are summed by the warp.  sum(chunk): chunk 0 counts blocks.
+    auto sum = [&](int len, int nq, int chunk, int &strips, int &longest) {
+        const int rows = nq * a.G, many = (rows + S::kRows - 1) / S::kRows;
+        long long mine = 0;
+        strips = many;
+        longest = 0;
+        if (many == 1) {
+            const int u = units_of(len, nq, 0);
+            longest = u;
+            mine = chunk ? (u + chunk - 1) / chunk : u;
         }
-    }
+        for (uint32_t todo = __ballot_sync(0xffffffffu, many > 1); todo; todo &= todo - 1) {
+            const int src = __ffs(todo) - 1;
+            const int l = __shfl_sync(0xffffffffu, len, src), q = __shfl_sync(0xffffffffu, nq, src), m = __shfl_sync(0xffffffffu, many, src);
+            long long part = 0;
+            int top = 0;
+            for (int rb = lane; rb < m; rb += 32) {
+                const int u = units_of(l, q, rb * S::kRows);
+                top = max(top, u);
+                part += chunk ? (u + chunk - 1) / chunk : u;
+            }
 #pragma unroll
-    for (int o = 16; o; o >>= 1) {
-        blocks += __shfl_xor_sync(0xffffffffu, blocks, o);
-        stretches += __shfl_xor_sync(0xffffffffu, stretches, o);
-        longest = max(longest, __shfl_xor_sync(0xffffffffu, longest, o));
-    }
-    if (lane == 0) { sum_s[warp][0] = blocks; sum_s[warp][1] = stretches; longest_s[warp] = longest; }
-    __syncthreads();
-    blocks = 0; stretches = 0; longest = 0;
-    for (int w = 0; w < kWarps; ++w) { blocks += sum_s[w][0]; stretches += sum_s[w][1]; longest = max(longest, longest_s[w]); }
-    __syncthreads();
-
-    // ---- how it is cut.  even: stretch by stretch, ceil(units/chunk) pieces each; else the line, `share` blocks a CTA
-    const bool few = 2 * stretches <= gridDim.x, brief = longest <= kBrief;
-    const bool even = few || brief;
-    // sum of ceil(u/chunk) <= blocks/chunk + stretches <= gridDim.x
-    const int chunk = few ? (int)max((blocks + gridDim.x - stretches - 1) / max((long long)gridDim.x - stretches, 1ll), (long long)kLeast) : kBrief;
-    const long long share = max((blocks + gridDim.x - 1) / (long long)gridDim.x, (long long)2 * kLeast);
-    {
-        long long carry = 0;
+            for (int o = 16; o; o >>= 1) part += __shfl_xor_sync(0xffffffffu, part, o);
+            top = __reduce_max_sync(0xffffffffu, top);
+            if (lane == src) { mine = part; longest = top; }
+        }
+        return mine * a.Hk;
+    };
+    bool few = false, even = false;
+    int chunk = 0;
+    long long share = 0, total = 0;
+    // pass 0 counts, pass 1 weighs and lines up (one copy of the code: this kernel's first run of an instruction costs more
+    // than its second)
+#pragma unroll 1
+    for (int pass = 0; pass < 2; ++pass) {
+        long long carry = 0, stretches = 0;
+        int most = 0;
+#pragma unroll 1
         for (int base = 0; base < a.n; base += kThreads) {
             const int i = base + tid;
-            long long mine = 0;
-            if (i < a.n) {
-                int len, q0, nq;
-                lengths(i, len, q0, nq);
-                for (int row0 = 0; row0 < nq * a.G; row0 += S::kRows) {
-                    const int u = units_of(len, nq, row0);
-                    mine += (long long)(even ? (u + chunk - 1) / chunk : u) * a.Hk;
-                }
-            }
+            int len = 0, q0, nq = 0, strips, longest;
+            if (i < a.n) lengths(i, len, q0, nq);
+            const long long mine = sum(len, nq, chunk, strips, longest);
+            stretches += strips;
+            most = max(most, longest);
             long long inc = mine;
+#pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
                 const long long up = __shfl_up_sync(0xffffffffu, inc, o);
                 if (lane >= o) inc += up;
             }
-            if (lane == 31) sum_s[warp][0] = inc;
+            if (lane == 31) sum_s[warp] = inc;
             __syncthreads();
-            long long before = carry, all = carry;
-            for (int w = 0; w < kWarps; ++w) { if (w < warp) before += sum_s[w][0]; all += sum_s[w][0]; }
+            long long before = carry;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                if (w == warp) before = carry;
+                carry += sum_s[w];
+            }
             if (i < a.n) line[i] = before + inc - mine;
-            carry = all;
             __syncthreads();
         }
-        if (tid == 0) line[a.n] = carry;
-        __syncthreads();
+        total = carry;
+        if (pass == 0) {
+            stretches = __reduce_add_sync(0xffffffffu, (int)stretches);
+            most = __reduce_max_sync(0xffffffffu, most);
+            if (lane == 0) { strips_s[warp] = (int)stretches; longest_s[warp] = most; }
+            __syncthreads();
+            stretches = 0;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) { stretches += strips_s[w]; most = max(most, longest_s[w]); }
+            stretches *= a.Hk;
+            const long long grid = gridDim.x;
+            few = 2 * stretches <= grid;
+            even = few || most <= kBrief;
+            // few: sum of ceil(u/chunk) <= blocks/chunk + stretches <= gridDim.x
+            chunk = few ? (int)max((total + grid - stretches - 1) / max(grid - stretches, 1ll), (long long)kLeast) : even ? kBrief : 0;
+            share = max((total + grid - 1) / grid, (long long)2 * kLeast);
+            if (!even) break;               // the line of blocks is there already
+        }
     }
-    const long long total = line[a.n];
+    __syncthreads();          // the barriers are initialised, the line is there
     // even: pieces blockIdx.x, + gridDim.x, ...; else blocks [at, end) of the line
     long long at = even ? (long long)blockIdx.x : share * blockIdx.x;
     const long long end = even ? total : min(at + share, total);
     uint32_t phase = 0;          // one bit for each stage of this warp
     bool dead = false;
 
+    int req = 0, len = 0, q0 = 0, nq = 0, sb = 0, wb = 0, nb = 0, row0 = 0, row1 = 0, units = 0, head = -1;
+    long long place = 0;         // where the stretch begins (even: its first piece)
+    auto shape = [&]() {
+        row1 = min(row0 + S::kRows, nq * a.G);
+        visible(len, nq, row0, row1, sb, wb, nb);
+        units = max(sb + nb - wb, 1);
+    };
     while (at < end) {
-        // ---- which stretch `at` lies in
-        int lo = 0, hi = a.n;
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (line[mid] <= at) lo = mid; else hi = mid;
+        // ---- which stretch `at` lies in: found, or the one behind the last piece's
+        if (even || head < 0) {
+            int lo = 0, hi = a.n;
+#pragma unroll 1
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (line[mid] <= at) lo = mid; else hi = mid;
+            }
+            long long from = line[lo];
+            req = lo;
+            lengths(req, len, q0, nq);
+            if (even && !few) {              // every stretch is one piece
+                const uint32_t x = (uint32_t)(at - from);
+                row0 = (int)(x / (uint32_t)a.Hk) * S::kRows;
+                head = (int)(x % (uint32_t)a.Hk);
+                shape();
+                place = at;
+            } else {
+#pragma unroll 1
+                for (row0 = 0;; row0 += S::kRows) {
+                    shape();
+                    const int weight = even ? (units + chunk - 1) / chunk : units;
+                    const long long here = (long long)weight * a.Hk;
+                    if (at < from + here) {
+                        head = (int)((uint32_t)(at - from) / (uint32_t)weight);
+                        place = from + (long long)head * weight;
+                        break;
+                    }
+                    from += here;
+                }
+            }
+        } else {
+            place = at;
+            if (++head == a.Hk) {
+                head = 0;
+                row0 += S::kRows;
+#pragma unroll 1
+                while (row0 >= nq * a.G) { lengths(++req, len, q0, nq); row0 = 0; }          // the line goes on, so there is a request with rows
+                shape();
+            }
         }
-        const int req = lo;
-        int len, q0, nq;
-        lengths(req, len, q0, nq);
-        long long off = at - line[req];
-        int sb, wb, nb, row0 = 0, row1, units, weight;
-        for (;; row0 += S::kRows) {
-            row1 = min(row0 + S::kRows, nq * a.G);
-            visible(len, nq, row0, row1, sb, wb, nb);
-            units = max(sb + nb - wb, 1);
-            weight = even ? (units + chunk - 1) / chunk : units;
-            const long long here = (long long)weight * a.Hk;
-            if (off < here) break;
-            off -= here;
-        }
+        // blocks [first, last) of the stretch are this piece; cta0..cta1 have its pieces
+        const int within = (int)(at - place);
+        const int weight = even ? (few ? (units + chunk - 1) / chunk : 1) : units;
+        const int each = units / weight, rest = units - each * weight;          // even pieces: `each` blocks, the first `rest` one more
+        const int first = even ? within * each + min(within, rest) : within;
+        const int last = even ? first + each + (within < rest) : (int)min((long long)units, within + end - at);
+        const int cta0 = even ? (int)blockIdx.x - within : first == 0 && last == units ? (int)blockIdx.x : (int)(place / share);
+        const int cta1 = even ? cta0 + weight - 1 : first == 0 && last == units ? (int)blockIdx.x : (int)((place + units - 1) / share);
         const int present = sb + nb - wb;
-        const int head = (int)(off / weight), within = (int)(off - (long long)head * weight);
-        // blocks [first, last) of the stretch are this piece; cta0..cta1 have its pieces (even: cta0 + piece number)
-        const int first = even ? (int)((long long)units * within / weight) : within;
-        const int last = even ? (int)((long long)units * (within + 1) / weight) : (int)min((long long)units, within + end - at);
-        const int cta0 = even ? (int)blockIdx.x - within : (int)((at - within) / share);
-        const int cta1 = even ? cta0 + weight - 1 : (int)((at - within + units - 1) / share);
         const int b1 = min(last, present);             // blocks [first, b1) of the stretch are loaded
+
+        // ---- queries: a warp a row, lane l has dimensions [l W/32, (l+1) W/32).  Asked for before the pages are waited for
+        constexpr int kPer = W / 32, kMine = S::kRows / kWarps;
+        float q_raw[kMine][kPer];
+#pragma unroll
+        for (int x = 0; x < kMine; ++x) {
+            const int row = row0 + warp + x * kWarps, tok = div_g(a, row);
+            const bool real = row < row1;
+            const T *src = (const T *)a.q.p + (int64_t)(q0 + (real ? tok : 0)) * a.q.ts + (int64_t)(head * a.G + (real ? row - tok * a.G : 0)) * a.q.hs;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) q_raw[x][i] = real && lane * kPer + i < a.D ? load_q(src + lane * kPer + i) : 0.f;
+        }
 
         // ---- this warp's blocks: the first copies start before the queries are read
         const int32_t *table = a.table + (int64_t)req * a.width;
@@ -246,44 +315,33 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
         };
         for (int k = 0; k < S::kStages && k < mine && !dead; ++k) issue(k, k);
 
-        // ---- queries of the rows, as operand fragments: [N tile][two k16 steps][lane] 16 bytes
-        {
-            // a warp a row; lane l holds dimensions [l W/32, (l+1) W/32)
-            constexpr int kPer = W / 32;
-            for (int n = warp; n < S::kRows; n += kWarps) {
-                const int row = row0 + n;
-                float v[kPer];
-                const bool real = row < row1;
-                const int tok = div_g(a, row);
-                float top = 0.f;
-                const T *src = (const T *)a.q.p + (int64_t)(q0 + (real ? tok : 0)) * a.q.ts + (int64_t)(head * a.G + (real ? row - tok * a.G : 0)) * a.q.hs;
+        // ---- queries as operand fragments: [N tile][two k16 steps][lane] 16 bytes
 #pragma unroll
-                for (int i = 0; i < kPer; ++i) {
-                    const int d = lane * kPer + i;
-                    v[i] = real && d < a.D ? load_q(src + d) : 0.f;
-                    top = fmaxf(top, fabsf(v[i]));
-                }
+        for (int x = 0; x < kMine; ++x) {
+            const int n = warp + x * kWarps, row = row0 + n;
+            float top = 0.f;
 #pragma unroll
-                for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-                const int e = row_exponent(top);
-                const float up = power2(10 - e);
-                if (lane == 0) {
-                    row_pos[n] = real ? len - nq + tok : -1;
-                    row_scale[n] = a.score_scale * power2(e - 10);
-                }
+            for (int i = 0; i < kPer; ++i) top = fmaxf(top, fabsf(q_raw[x][i]));
 #pragma unroll
-                for (int i = 0; i < kPer; i += 2) {
-                    const int d = lane * kPer + i;
-                    // thread c of a fragment has dimensions [c W/4, (c+1) W/4) of row r, four for each k16 step
-                    const int fc = d / (W / 4), in = d % (W / 4), step = in / 4, part = (in % 4) / 2;
-                    uint32_t *dst = reinterpret_cast<uint32_t *>(q_s) + ((((n >> 3) * (S::kSteps / 2) + step / 2) * 32 + (n & 7) * 4 + fc) * 4 + (step & 1) * 2 + part);
-                    const float x = v[i] * up, y = v[i + 1] * up;
-                    const uint32_t h = pack2(x, y);
-                    *dst = h;
-                    if (SPLIT) {
-                        const float2 f = unpack2(h);
-                        dst[S::kRows * W / 2] = pack2(x - f.x, y - f.y);
-                    }
+            for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+            const int e = row_exponent(top);
+            const float up = power2(10 - e);
+            if (lane == 0) {
+                row_pos[n] = row < row1 ? len - nq + div_g(a, row) : -1;
+                row_scale[n] = a.score_scale * power2(e - 10);
+            }
+#pragma unroll
+            for (int i = 0; i < kPer; i += 2) {
+                const int d = lane * kPer + i;
+                // thread c of a fragment has dimensions [c W/4, (c+1) W/4) of row r, four for each k16 step
+                const int fc = d / (W / 4), in = d % (W / 4), step = in / 4, part = (in % 4) / 2;
+                uint32_t *dst = reinterpret_cast<uint32_t *>(q_s) + ((((n >> 3) * (S::kSteps / 2) + step / 2) * 32 + (n & 7) * 4 + fc) * 4 + (step & 1) * 2 + part);
+                const float u = q_raw[x][i] * up, w = q_raw[x][i + 1] * up;
+                const uint32_t h = pack2(u, w);
+                *dst = h;
+                if (SPLIT) {
+                    const float2 f = unpack2(h);
+                    dst[S::kRows * W / 2] = pack2(u - f.x, w - f.y);
                 }
             }
         }
@@ -412,15 +470,18 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
                     for (int j = 0; j < 4; ++j) s[b][t][j] *= f[t][j & 1];
                 if (!clear[b]) {
                     const bool here = has >> b & 1u;
-                    const int key0 = block_at(u) * kBlockTokens;
-                    valid[b] = len - key0;
+                    const int key = block_at(u) * kBlockTokens + r;
+                    valid[b] = len - key + r;
 #pragma unroll
                     for (int t = 0; t < NT; ++t)
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const int key = key0 + r + 8 * (j >> 1), p = row_pos[t * 8 + 2 * c + (j & 1)];
-                            const bool see = here && key <= p && (a.window <= 0 || p - key < a.window || key < a.sinks);
-                            s[b][t][j] = see ? s[b][t][j] : -INFINITY;
+                        for (int j = 0; j < 2; ++j) {
+                            // the query's position less the key's, for keys r and r + 8
+                            const int back = row_pos[t * 8 + 2 * c + j] - key;
+                            const bool see0 = here && back >= 0 && (a.window <= 0 || back < a.window || key < a.sinks);
+                            const bool see8 = here && back >= 8 && (a.window <= 0 || back - 8 < a.window || key + 8 < a.sinks);
+                            s[b][t][j] = see0 ? s[b][t][j] : -INFINITY;
+                            s[b][t][j + 2] = see8 ? s[b][t][j + 2] : -INFINITY;
                         }
                 }
 #pragma unroll
@@ -582,6 +643,7 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
                         buf[((warp * S::kRows + 8 * u + 2 * c + j) * S::kJoinTiles + tl) * 8 + r] =
                             make_float2(o[t0 + tl][u][j] * k_mine[u][j], o[t0 + tl][u][j + 2] * k_mine[u][j]);
             __syncthreads();
+#pragma unroll 1
             for (int e = tid; e < S::kRows * S::kJoinTiles * 8; e += kThreads) {
                 const int n = e / (S::kJoinTiles * 8), tl = e / 8 % S::kJoinTiles, rr = e % 8;
                 float2 v = make_float2(0.f, 0.f);
@@ -600,33 +662,62 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
         }
         if (!whole) {
             if (tid < S::kRows) part_ml[tid] = row_ml[tid];
-            __threadfence();
             __syncthreads();
             if (tid == 0) {
+                __threadfence();                    // all of the CTA's writes above, by way of the barrier
                 const int before = atomicAdd(a.arrived + cta0, 1);
                 last_s = before == cta1 - cta0;
                 if (last_s) a.arrived[cta0] = 0;             // ready for the next call
+                __threadfence();
             }
             __syncthreads();
             if (last_s) {
-                __threadfence();
-                // the pieces in the order of the keys
-                for (int e = tid; e < S::kRows * (W / 2); e += kThreads) {
-                    const int n = e / (W / 2), d = e % (W / 2) * 2;
-                    if (row0 + n >= row1) continue;
-                    float top = kFloor, sum = 0.f;
-                    for (int b = cta0; b <= cta1; ++b) top = fmaxf(top, __ldcg(&a.part_ml[(int64_t)(b * 2 + (b == cta0)) * S::kRows + n]).x);
-                    float2 v = make_float2(0.f, 0.f);
-                    for (int b = cta0; b <= cta1; ++b) {
-                        const int64_t slot = b * 2 + (b == cta0);
-                        const float2 ml = __ldcg(&a.part_ml[slot * S::kRows + n]);
-                        const float k = ml.x == top ? 1.f : ex2(ml.x - top);
-                        const float2 x = __ldcg(reinterpret_cast<const float2 *>(a.part + (slot * S::kRows + n) * W + d));
-                        sum += k * ml.y;
-                        v.x += k * x.x; v.y += k * x.y;
+                // the pieces in the order of the keys, as many at a time as the ring holds: their latency is paid once for all
+                // of these (loaded by the threads that add them, four at a time, 16 pieces took 8 us)
+                constexpr int kBytes = S::kRows * W * 4, kAtOnce = S::kRing / (kBytes + S::kRows * 8);
+                static_assert(kAtOnce >= 1, "");
+                float2 *ml_s = reinterpret_cast<float2 *>(ring + kAtOnce * kBytes);
+                constexpr int kOwn = S::kRows * W / 4 / kThreads;              // a thread's quads of dimensions
+                float top[kOwn], sum[kOwn], v[kOwn][4];
+#pragma unroll
+                for (int x = 0; x < kOwn; ++x) { top[x] = kFloor; sum[x] = 0.f; v[x][0] = v[x][1] = v[x][2] = v[x][3] = 0.f; }
+#pragma unroll 1
+                for (int b0 = cta0; b0 <= cta1; b0 += kAtOnce) {
+                    const int m = min(kAtOnce, cta1 + 1 - b0);
+#pragma unroll 1
+                    for (int e = tid; e < m * (kBytes / 16); e += kThreads) {
+                        const int y = e / (kBytes / 16), b = b0 + y;
+                        const float *src = a.part + (int64_t)(b * 2 + (b == cta0)) * S::kRows * W + (e % (kBytes / 16)) * 4;
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(ring) + e * 16), "l"(src) : "memory");
                     }
-                    const float k = sum > 0.f || sum != sum ? a.v_scale / sum : 0.f;
-                    put(n, d, make_float2(v.x * k, v.y * k));
+#pragma unroll 1
+                    for (int e = tid; e < m * S::kRows; e += kThreads) {
+                        const int b = b0 + e / S::kRows;
+                        ml_s[e] = __ldcg(&a.part_ml[(int64_t)(b * 2 + (b == cta0)) * S::kRows + e % S::kRows]);
+                    }
+                    asm volatile("cp.async.wait_all;" ::: "memory");
+                    __syncthreads();
+#pragma unroll 1
+                    for (int y = 0; y < m; ++y)
+#pragma unroll
+                        for (int x = 0; x < kOwn; ++x) {
+                            const int e = tid + x * kThreads;
+                            const float2 ml = ml_s[y * S::kRows + e / (W / 4)];
+                            const float4 z = *reinterpret_cast<const float4 *>(ring + y * kBytes + e * 16);
+                            const float to = fmaxf(top[x], ml.x), old = top[x] == to ? 1.f : ex2(top[x] - to), k = ml.x == to ? 1.f : ex2(ml.x - to);
+                            sum[x] = sum[x] * old + ml.y * k;
+                            v[x][0] = v[x][0] * old + z.x * k; v[x][1] = v[x][1] * old + z.y * k;
+                            v[x][2] = v[x][2] * old + z.z * k; v[x][3] = v[x][3] * old + z.w * k;
+                            top[x] = to;
+                        }
+                    __syncthreads();
+                }
+#pragma unroll
+                for (int x = 0; x < kOwn; ++x) {
+                    const int e = tid + x * kThreads, n = e / (W / 4), d = e % (W / 4) * 4;
+                    const float k = sum[x] > 0.f || sum[x] != sum[x] ? a.v_scale / sum[x] : 0.f;
+                    put(n, d, make_float2(v[x][0] * k, v[x][1] * k));
+                    put(n, d + 2, make_float2(v[x][2] * k, v[x][3] * k));
                 }
             }
         }

@@ -90,18 +90,14 @@ struct AttendArgs {
     float v_scale; int window, sinks;
     void *out;
     float *part; float2 *part_ml; int32_t *arrived; int max_ctas;   // split over the keys
-    uint32_t g_mul;                           // ceil(2^32 / G), for div_g
+    FastDiv g_div;                            // by G
     // requests of more query rows per key/value head than this are kv_prompt.cu's; 0: none are
     int prompt_rows;
     float *prompt_part; float2 *prompt_ml; int32_t *prompt_arrived;
     int32_t *status;
 };
 #ifdef __CUDACC__
-// row / G.  With m = ceil(2^32/G) the high word of row * m is exact while row * (m G - 2^32) < 2^32, so for G <= 1024
-// below 2^22
-__device__ __forceinline__ int div_g(const AttendArgs &a, int row) {
-    return a.G == 1 ? row : row < (1 << 22) ? (int)__umulhi((uint32_t)row, a.g_mul) : row / a.G;
-}
+__device__ __forceinline__ int div_g(const AttendArgs &a, int row) { return (int)a.g_div.div((uint32_t)row); }      // row / G
 #endif
 // rows of queries that share a key/value head, in the N dimension of mma.sync (kv_attend.cu)
 cudaError_t launch_attend_rows(const AttendArgs &a, int sm_count, cudaStream_t s, uint64_t *launches);

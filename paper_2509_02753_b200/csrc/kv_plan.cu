@@ -26,6 +26,7 @@ struct moe_kv_plan {
 namespace {
 
 constexpr int kMaxCtasPerSm = 8;
+constexpr int64_t kMaxRows = 1 << 30;         // max_tokens * n_heads
 constexpr int64_t kMaxContext = 1 << 30;      // tokens that a row of a block table may stand for
 constexpr int kPartRows = 32;         // rows of a piece, at most
 constexpr int kPromptRows = 32;       // what kv_attend.cu takes in one pass over the keys
@@ -37,7 +38,8 @@ int check_config(const moe_kv_config_t *c) {
     if (!c) return MOE_ERR_INVALID_ARG;
     if (c->n_heads < 1 || c->n_kv_heads < 1 || c->n_heads % c->n_kv_heads || c->max_requests < 1 || c->max_tokens < 1 ||
         (c->dtype != MOE_F32 && c->dtype != MOE_BF16)) return MOE_ERR_INVALID_ARG;
-    if (c->head_dim < 8 || c->head_dim > 256 || c->head_dim % 8 || c->n_heads > 1024 || c->max_requests > kMaxRequests) return MOE_ERR_SHAPE;
+    if (c->head_dim < 8 || c->head_dim > 256 || c->head_dim % 8 || c->n_heads > 1024 || c->max_requests > kMaxRequests ||
+        (int64_t)c->max_tokens * c->n_heads > kMaxRows) return MOE_ERR_SHAPE;
     if (c->page_size != 16 && c->page_size != 32 && c->page_size != 64 && c->page_size != 128) return MOE_ERR_SHAPE;
     return MOE_OK;
 }
@@ -244,7 +246,7 @@ int moe_kv_attention(moe_kv_plan_t *p, const moe_kv_rows_t *q, int32_t T, const 
     AttendArgs a{};
     a.dtype = c.dtype; a.q = Rows{q->data, q->token_stride, q->head_stride}; a.T = T; a.cu = cu_new; a.kv_len = kv_len; a.n = n; a.max_new = max_new;
     a.table = block_table; a.width = width; a.cache = (const uint8_t *)cache; a.n_pages = n_pages;
-    a.H = c.n_heads; a.Hk = c.n_kv_heads; a.G = c.n_heads / c.n_kv_heads; a.D = c.head_dim; a.g_mul = (uint32_t)((0x100000000ull + a.G - 1) / a.G); a.page_shift = page_shift(c);
+    a.H = c.n_heads; a.Hk = c.n_kv_heads; a.G = c.n_heads / c.n_kv_heads; a.D = c.head_dim; a.g_div = FastDiv((uint32_t)a.G); a.page_shift = page_shift(c);
     a.score_scale = (float)((double)softmax_scale * k_scale * 1.4426950408889634);
     a.v_scale = v_scale; a.out = out;
     // no position reaches kMaxContext, and sums of these stay below 2^31
