@@ -36,6 +36,7 @@ constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kPair = 2;                       // blocks a warp handles per step
 constexpr int kLeast = kWarps * kPair;         // blocks of a piece, at least: a step of every warp
+constexpr int kEntry = 16;                     // what a stretch costs besides its blocks, in blocks: counted in the line
 constexpr int kBrief = 32;                     // stretches of at most this many blocks are not cut
 constexpr float kFloor = -FLT_MAX;             // reference of a row that has seen no key
 // Weights are 2^(x - m + kHead + kSlack): m is kSlack above a score that was once the largest, and follows only when a
@@ -124,7 +125,7 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
     // ---- how much there is: blocks, stretches, the longest stretch; then how it is cut:
     //   even   stretch by stretch, ceil(units/chunk) pieces each (one piece a CTA where there are few stretches; whole
     //          stretches, several a CTA, where all are brief)
-    //   else   the line of all blocks, `share` of them a CTA
+    //   else   the line of all stretches, kEntry and their blocks each, `share` of it a CTA
     // A lane has a request; the row blocks of one with several are summed by the warp.  sum(chunk): chunk 0 counts blocks.
     auto sum = [&](int len, int nq, int chunk, int &strips, int &longest) {
         const int rows = nq * a.G, many = (rows + S::kRows - 1) / S::kRows;
@@ -134,7 +135,7 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
         if (many == 1) {
             const int u = units_of(len, nq, 0);
             longest = u;
-            mine = chunk ? (u + chunk - 1) / chunk : u;
+            mine = chunk ? (u + chunk - 1) / chunk : u + kEntry;
         }
         for (uint32_t todo = __ballot_sync(0xffffffffu, many > 1); todo; todo &= todo - 1) {
             const int src = __ffs(todo) - 1;
@@ -144,7 +145,7 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
             for (int rb = lane; rb < m; rb += 32) {
                 const int u = units_of(l, q, rb * S::kRows);
                 top = max(top, u);
-                part += chunk ? (u + chunk - 1) / chunk : u;
+                part += chunk ? (u + chunk - 1) / chunk : u + kEntry;
             }
 #pragma unroll
             for (int o = 16; o; o >>= 1) part += __shfl_xor_sync(0xffffffffu, part, o);
@@ -201,7 +202,7 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
             few = 2 * stretches <= grid;
             even = few || most <= kBrief;
             // few: sum of ceil(u/chunk) <= blocks/chunk + stretches <= gridDim.x
-            chunk = few ? (int)max((total + grid - stretches - 1) / max(grid - stretches, 1ll), (long long)kLeast) : even ? kBrief : 0;
+            chunk = few ? (int)max((total - kEntry * stretches + grid - stretches - 1) / max(grid - stretches, 1ll), (long long)kLeast) : even ? kBrief : 0;
             share = max((total + grid - 1) / grid, (long long)2 * kLeast);
             if (!even) break;               // the line of blocks is there already
         }
@@ -242,7 +243,7 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
 #pragma unroll 1
                 for (row0 = 0;; row0 += S::kRows) {
                     shape();
-                    const int weight = even ? (units + chunk - 1) / chunk : units;
+                    const int weight = even ? (units + chunk - 1) / chunk : units + kEntry;
                     const long long here = (long long)weight * a.Hk;
                     if (at < from + here) {
                         head = (int)((uint32_t)(at - from) / (uint32_t)weight);
@@ -264,12 +265,25 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
         }
         // blocks [first, last) of the stretch are this piece; cta0..cta1 have its pieces
         const int within = (int)(at - place);
-        const int weight = even ? (few ? (units + chunk - 1) / chunk : 1) : units;
-        const int each = units / weight, rest = units - each * weight;          // even pieces: `each` blocks, the first `rest` one more
-        const int first = even ? within * each + min(within, rest) : within;
-        const int last = even ? first + each + (within < rest) : (int)min((long long)units, within + end - at);
-        const int cta0 = even ? (int)blockIdx.x - within : first == 0 && last == units ? (int)blockIdx.x : (int)(place / share);
-        const int cta1 = even ? cta0 + weight - 1 : first == 0 && last == units ? (int)blockIdx.x : (int)((place + units - 1) / share);
+        int first, last, cta0, cta1;
+        if (even) {
+            const int weight = few ? (units + chunk - 1) / chunk : 1;
+            const int each = units / weight, rest = units - each * weight;          // `each` blocks, the first `rest` pieces one more
+            first = within * each + min(within, rest);
+            last = first + each + (within < rest);
+            cta0 = (int)blockIdx.x - within;
+            cta1 = cta0 + weight - 1;
+            at += gridDim.x;
+        } else {
+            const long long block0 = place + kEntry;
+            first = max(within - kEntry, 0);
+            last = (int)min((long long)units, end - block0);
+            at = block0 + units;                    // the next stretch
+            if (last <= first) continue;
+            const bool all = first == 0 && last == units;
+            cta0 = all ? (int)blockIdx.x : (int)(block0 / share);
+            cta1 = all ? (int)blockIdx.x : (int)((block0 + units - 1) / share);
+        }
         const int present = sb + nb - wb;
         const int b1 = min(last, present);             // blocks [first, b1) of the stretch are loaded
 
@@ -724,7 +738,6 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
         // the ring and the rows' tables are the next piece's; its copies come after this piece's plain accesses
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncthreads();
-        at += even ? (long long)gridDim.x : (long long)(last - first);
     }
 }
 
