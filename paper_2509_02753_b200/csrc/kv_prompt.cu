@@ -1,13 +1,14 @@
-// Attention of prompts over the 4-bit cache: many query rows of a request, on the tcgen05 tensor cores (bf16 queries,
-// heads of up to 128 dimensions; kv_attend.cu has the formula and serves the rest).
+// Attention of prompts over the 4-bit cache: many query rows of a request, on the tcgen05 tensor cores (all but fp32 heads
+// of more than 128 dimensions; kv_attend.cu has the formula and serves the rest).
 //
 // A CTA works on 256 query rows of one (request, key/value head) - tokens times the query heads that share it, in two
-// tiles of 128 - against tiles of 128 keys:
+// tiles of 128 (one for fp32 with W = 128 and for W = 256) - against tiles of 128 keys (64 for W = 256):
 //   S_t[128 rows, 128 keys] = Q_t K^T       A, B from shared memory, sums in tensor memory
 //   O_t[128 rows, W]       += P_t V         A = the weights in tensor memory (they take S_t's columns), B from shared memory
 // A code times its scale is exact in f16, so the codes become f16 operands once per CTA and tile: K rows as they lie,
 // V transposed (8 keys of a dimension are 16 bytes), both in the 128-byte swizzle.  Queries are scaled by a power of two
-// per row and are exact in f16 too; the weights are rounded to f16 (11 bits).
+// per row and are exact in f16 too; the weights are rounded to f16 (11 bits).  For fp32 both are two f16 parts, high and
+// low, and each part has its products.
 //
 // Roles: two warpgroups of softmax, one thread a row; one warpgroup that converts; one thread that issues products.  The
 // two tiles alternate: while one's weights are computed the other's products run.  A row's scores stay in
@@ -31,8 +32,7 @@ namespace lexi {
 namespace kv {
 namespace {
 
-constexpr int kTileKeys = 128, kTileRows = 128, kStretchRows = 2 * kTileRows;
-constexpr int kTileBlocks = kTileKeys / kBlockTokens;
+constexpr int kTileRows = 128;
 constexpr int kThreads = 512;
 constexpr float kFloor = -FLT_MAX;
 constexpr float kHead = 6.f, kSlack = 8.f;       // as in kv_attend.cu
@@ -40,12 +40,19 @@ constexpr float kHead = 6.f, kSlack = 8.f;       // as in kv_attend.cu
 // with many short stretches would be last by far
 constexpr int kEntry = 3;
 
-template <int W>
+// T: type of queries and outputs; fp32 queries and weights are two f16 parts each, with products for both.  TILES: row tiles
+// of a CTA.  KEYS: keys of a tile
+template <typename T, int W, int TILES, int KEYS>
 struct Shape {
-    static constexpr int kQTile = kTileRows * W * 2;          // bytes
-    static constexpr int kKTile = kTileKeys * W * 2, kVTile = kTileKeys * W * 2;
-    static constexpr int kQAt = 0, kKAt = 2 * kQTile, kVAt = kKAt + 2 * kKTile, kLineAt = kVAt + 2 * kVTile;
-    static constexpr int kS = 0, kO = 2 * kTileKeys;          // columns of tensor memory
+    static constexpr int kParts = sizeof(T) == 4 ? 2 : 1;
+    static constexpr int kRows = TILES * kTileRows;
+    static constexpr int kQPart = kTileRows * W * 2, kQTile = kQPart * kParts;          // bytes
+    static constexpr int kKTile = KEYS * W * 2, kVTile = KEYS * W * 2;
+    static constexpr int kQAt = 0, kKAt = TILES * kQTile, kVAt = kKAt + 2 * kKTile, kLineAt = kVAt + 2 * kVTile;
+    static constexpr int kS = 0, kO = TILES * 128;            // columns of tensor memory
+    static_assert(kO + TILES * W <= 512 && KEYS <= 128 && kLineAt <= 196608, "");
+    // conversion: a thread's dimensions of a key; stretches of dimensions of V, one for KEYS/8 threads
+    static constexpr int kKeyDims = W * KEYS / 128, kStretches = 1024 / KEYS, kVDims = W / kStretches;
 };
 constexpr uint32_t kTmem = 0;                    // where an allocation of all 512 columns begins
 
@@ -147,9 +154,11 @@ __device__ __forceinline__ void lds16(uint32_t at, uint32_t (&v)[4]) {
     asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(at) : "memory");
 }
 
-template <int W>
+template <typename T, int W, int TILES, int KEYS>
 __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a) {
-    using S = Shape<W>;
+    using S = Shape<T, W, TILES, KEYS>;
+    constexpr bool SPLIT = sizeof(T) == 4;
+    constexpr int kTileKeys = KEYS, kTileBlocks = KEYS / kBlockTokens, kStretchRows = S::kRows;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     int64_t *line = reinterpret_cast<int64_t *>(smem + S::kLineAt);
@@ -176,6 +185,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    if (tid < 4) absent[tid] = 0u;
     if (warp == 12) tc::tmem_alloc(smem_u32(&tmem_slot), 512);
 
     // ---- the line: key tiles of every stretch of prompts
@@ -294,9 +304,11 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
         // ================================================================ conversion
         asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         const int c8 = tid - 256;                                             // 0..127
-        const int v_sub = c8 >> 6, v_c = lane & 7, v_r = (lane >> 3) + 4 * ((c8 >> 5) & 1);
-        constexpr int kCodes = W / 32;                                        // 16-byte words of a key's codes
-        constexpr int kVWords = W / 8;                                        // words of 8 keys' share of a stretch
+        const int key_in = c8 % KEYS, key_part = c8 / KEYS;                   // a thread's key, and which kKeyDims of it
+        const int v_sub = KEYS == 128 ? c8 >> 6 : 0, v_c = lane & 7, v_r = (lane >> 3) + 4 * (KEYS == 128 ? (c8 >> 5) & 1 : c8 >> 5);
+        constexpr int kCodes = S::kKeyDims / 32;                              // 16-byte words of its codes
+        constexpr int kVWords = S::kVDims;                                    // words of 8 keys' share of a stretch
+        static_assert(W <= 128 || (W == 256 && KEYS == 64), "");
         uint4 kc[kCodes];
         uint2 ks, vs;
         uint32_t vc[kVWords];
@@ -323,11 +335,12 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
                 for (int i = 0; i < kCodes; ++i) kc[i] = make_uint4(0u, 0u, 0u, 0u);
                 if (kb < 0) return;
                 const uint8_t *blk = a.cache + (int64_t)kb * block_bytes(W);
-                const int token = c8 & 15;
+                const int token = key_in & 15;
+                const uint8_t *codes = blk + token * (W / 2) + key_part * (S::kKeyDims / 2), *scales = blk + k_scales_at(W) + token * (W / 16) + key_part * (S::kKeyDims / 16);
 #pragma unroll
-                for (int i = 0; i < kCodes; ++i) kc[i] = __ldg(reinterpret_cast<const uint4 *>(blk + token * (W / 2) + 16 * i));
-                if (W == 128) ks = __ldg(reinterpret_cast<const uint2 *>(blk + k_scales_at(W) + token * (W / 16)));
-                else ks.x = __ldg(reinterpret_cast<const uint32_t *>(blk + k_scales_at(W) + token * (W / 16)));
+                for (int i = 0; i < kCodes; ++i) kc[i] = __ldg(reinterpret_cast<const uint4 *>(codes + 16 * i));
+                if (S::kKeyDims == 128) ks = __ldg(reinterpret_cast<const uint2 *>(scales));
+                else ks.x = __ldg(reinterpret_cast<const uint32_t *>(scales));
             };
             auto fetch_values = [&](int vb) {
                 vs = make_uint2(0u, 0u);
@@ -336,15 +349,24 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
                 if (vb < 0) return;
                 const uint8_t *blk = a.cache + (int64_t)vb * block_bytes(W);
                 const int half = v_c & 1;
-                const uint4 *src = reinterpret_cast<const uint4 *>(blk + v_codes_at(W) + v_r * W + ((half * (W / 2)) ^ v_turn(W, v_r)));
+                if (W == 256) {           // half of a stretch of the cache's layout
+                    const int r = v_r >> 1;
 #pragma unroll
-                for (int i = 0; i < kVWords / 4; ++i) {
-                    const uint4 x = __ldg(src + i);
-                    vc[4 * i] = x.x; vc[4 * i + 1] = x.y; vc[4 * i + 2] = x.z; vc[4 * i + 3] = x.w;
+                    for (int i = 0; i < 8; ++i) {
+                        const uint2 x = __ldg(reinterpret_cast<const uint2 *>(blk + v_codes_at(W) + r * W + (((half * 8 + i) * 16) ^ v_turn(W, r)) + (v_r & 1) * 8));
+                        vc[(2 * i) % kVWords] = x.x; vc[(2 * i + 1) % kVWords] = x.y;
+                    }
+                } else {
+                    const uint4 *src = reinterpret_cast<const uint4 *>(blk + v_codes_at(W) + v_r * W + ((half * (W / 2)) ^ v_turn(W, v_r)));
+#pragma unroll
+                    for (int i = 0; i < kVWords / 4; ++i) {
+                        const uint4 x = __ldg(src + i);
+                        vc[4 * i] = x.x; vc[4 * i + 1] = x.y; vc[4 * i + 2] = x.z; vc[4 * i + 3] = x.w;
+                    }
                 }
-                vs = __ldg(reinterpret_cast<const uint2 *>(blk + v_scales_at(W) + (W == 128 ? v_r : v_r >> 1) * kBlockTokens + half * 8));
+                vs = __ldg(reinterpret_cast<const uint2 *>(blk + v_scales_at(W) + (W == 64 ? v_r >> 1 : v_r) * kBlockTokens + half * 8));
             };
-            const int k_in = c8 >> 4, v_in = v_sub * 4 + (v_c >> 1);
+            const int k_in = key_in >> 4, v_in = v_sub * 4 + (v_c >> 1);
             // a tile's bytes are asked for as soon as the tile before has left the registers, its pages a tile earlier
             int kb = find(0, k_in), vb = find(0, v_in), kb2 = find(1, k_in), vb2 = find(1, v_in);
             fetch_keys(kb);
@@ -362,14 +384,15 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
                 {
                     const uint32_t gone = __ballot_sync(0xffffffffu, kb_now == -1);       // lanes 0 and 16: two blocks
                     if (lane == 0) {
-                        const uint32_t bits = ((gone & 1u) | ((gone >> 15) & 2u)) << (2 * (warp & 3));
-                        // every warp has its own byte of the tile's word; a word is written again four tiles later, when
-                        // both softmax groups have long read it
-                        reinterpret_cast<volatile uint8_t *>(&absent[it & 3])[warp & 3] = (uint8_t)bits;
+                        // 32 keys have a byte of the tile's word; a word is written again four tiles later, when the softmax
+                        // groups have long read it
+                        const int byte = warp % (KEYS / 32);
+                        const uint32_t bits = ((gone & 1u) | ((gone >> 15) & 2u)) << (2 * byte);
+                        reinterpret_cast<volatile uint8_t *>(&absent[it & 3])[byte] = (uint8_t)bits;
                     }
                     const uint32_t row = smem_u32(smem + S::kKAt + stage * S::kKTile);
 #pragma unroll
-                    for (int g = 0; g < W / 16; ++g) {        // 16 dimensions: 8 bytes of codes, one scale, two chunks
+                    for (int g = 0; g < S::kKeyDims / 16; ++g) {        // 16 dimensions: 8 bytes of codes, one scale, two chunks
                         const uint4 q = kc[g / 2];
                         const uint32_t w0 = g & 1 ? q.z : q.x, w1 = g & 1 ? q.w : q.y;
                         const uint32_t two = scales2(((g < 4 ? ks.x : ks.y) >> (8 * (g & 3))) & 0xffu);
@@ -377,9 +400,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
                         uint32_t h[4], u[4];
                         codes4(w0, h);
                         codes4(w1, u);
-                        const uint32_t base = row + (g / 4) * (kTileKeys * 128);
-                        sts16(base + swizzled(c8, (g & 3) * 2), mul2(h[0], sc), mul2(h[1], sc), mul2(h[2], sc), mul2(h[3], sc));
-                        sts16(base + swizzled(c8, (g & 3) * 2 + 1), mul2(u[0], sc), mul2(u[1], sc), mul2(u[2], sc), mul2(u[3], sc));
+                        const uint32_t base = row + (key_part * (S::kKeyDims / 64) + g / 4) * (KEYS * 128);
+                        sts16(base + swizzled(key_in, (g & 3) * 2), mul2(h[0], sc), mul2(h[1], sc), mul2(h[2], sc), mul2(h[3], sc));
+                        sts16(base + swizzled(key_in, (g & 3) * 2 + 1), mul2(u[0], sc), mul2(u[1], sc), mul2(u[2], sc), mul2(u[3], sc));
                     }
                 }
                 fence_async();
@@ -400,7 +423,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
 #pragma unroll
                     for (int i = 0; i < 4; ++i) sc[i] = scales2(((i < 2 ? vs.x : vs.y) >> (16 * (i & 1))) & 0xffffu);
                     const uint32_t base = smem_u32(smem + S::kVAt + stage * S::kVTile) + v_sub * (W * 128);
-                    constexpr int kPerKey = W / 64;           // words of a key's share: dimensions 8 w .. of the stretch
+                    constexpr int kPerKey = S::kVDims / 8;    // words of a key's share: dimensions 8 w .. of the stretch
                     constexpr uint32_t L = 0x0f0f0f0fu;
 #pragma unroll
                     for (int w = 0; w < kPerKey; ++w) {
@@ -416,7 +439,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
                         }
 #pragma unroll
                         for (int e = 0; e < 8; ++e)
-                            sts16(base + swizzled(v_r * (W / 8) + 8 * w + e, v_c), d[e][0], d[e][1], d[e][2], d[e][3]);
+                            sts16(base + swizzled(v_r * S::kVDims + 8 * w + e, v_c), d[e][0], d[e][1], d[e][2], d[e][3]);
                     }
                 }
                 fence_async();
@@ -441,9 +464,11 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
                 const uint64_t da = q_d + t * (S::kQTile / 16), db = k_d + stage * (S::kKTile / 16);
                 if (one && !dead) {
 #pragma unroll
-                    for (int i = 0; i < W / 16; ++i)
-                        tc::umma_bf16(kTmem + S::kS + t * kTileKeys, da + (i / 4) * (kTileRows * 128 / 16) + 2 * (i % 4), db + (i / 4) * (kTileKeys * 128 / 16) + 2 * (i % 4),
-                                      idesc_f16(kTileKeys), i > 0);
+                    for (int part = 0; part < S::kParts; ++part)
+#pragma unroll
+                        for (int i = 0; i < W / 16; ++i)
+                            tc::umma_bf16(kTmem + S::kS + t * KEYS, da + part * (S::kQPart / 16) + (i / 4) * (kTileRows * 128 / 16) + 2 * (i % 4),
+                                          db + (i / 4) * (KEYS * 128 / 16) + 2 * (i % 4), idesc_f16(KEYS), part + i > 0);
                     tc::umma_commit(s_full(t));
                 }
                 __syncwarp();
@@ -452,8 +477,11 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
                 const uint64_t db = v_d + stage * (S::kVTile / 16);
                 if (one && !dead) {
 #pragma unroll
-                    for (int i = 0; i < kTileKeys / 16; ++i)
-                        umma_ts(kTmem + S::kO + t * W, kTmem + S::kS + t * kTileKeys + 8 * i, db + (i / 4) * (W * 128 / 16) + 2 * (i % 4), idesc_f16(W), i > 0 || more);
+                    for (int part = 0; part < S::kParts; ++part)
+#pragma unroll
+                        for (int i = 0; i < KEYS / 16; ++i)
+                            umma_ts(kTmem + S::kO + t * W, kTmem + S::kS + t * KEYS + part * (KEYS / 2) + 8 * i, db + (i / 4) * (W * 128 / 16) + 2 * (i % 4), idesc_f16(W),
+                                    part + i > 0 || more);
                     tc::umma_commit(o_full(t));
                 }
                 __syncwarp();
@@ -462,7 +490,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
             for (bool go = begin(p); go; go = next(p)) {
                 if (p.last <= p.first) continue;
                 const int n = __reduce_max_sync(0xffffffffu, min(p.last, p.present) - p.first);        // into a uniform register
-                const int tiles = __reduce_max_sync(0xffffffffu, p.row1 - p.row0 > kTileRows ? 2 : 1);
+                const int tiles = TILES == 1 ? 1 : __reduce_max_sync(0xffffffffu, p.row1 - p.row0 > kTileRows ? 2 : 1);
                 if (n > 0) {
                     wait(k_full(it & 1), (it >> 1) & 1);
                     for (int t = 0; t < tiles; ++t) {
@@ -480,7 +508,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
                     wait(v_full(stage), (it >> 1) & 1);
                     if (j + 1 < n) wait(k_full(other), ((it + 1) >> 1) & 1);
 #pragma unroll
-                    for (int t = 0; t < 2; ++t) {
+                    for (int t = 0; t < TILES; ++t) {
                         if (t >= tiles) continue;
                         wait(p_full(t), (p_phase >> t) & 1u);          // the weights are there, the scores are read
                         p_phase ^= 1u << t;
@@ -497,7 +525,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
             }
         }
         __syncwarp();
-    } else {
+    } else if (group < TILES) {
         // ================================================================ softmax: thread = row of tile `group`
         asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
         const int t = group, row_in = tid & 127, wl = (warp & 3) * 32;
@@ -509,54 +537,73 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
         for (bool more = begin(p); more; more = next(p)) {
             if (p.last <= p.first) continue;
             const int n = min(p.last, p.present) - p.first;
-            const int tiles = p.row1 - p.row0 > kTileRows ? 2 : 1;
+            const int tiles = TILES == 1 || p.row1 - p.row0 <= kTileRows ? 1 : 2;
             const int row = p.row0 + t * kTileRows + row_in;
             const bool real = row < p.row1;
             const int tok = div_g(a, row), pos = real ? p.len - p.nq + tok : -1;
             const int64_t out_row = (int64_t)(p.q0 + tok) * a.H + p.head * a.G + row - tok * a.G;
             float m = kFloor, l = 0.f, f = 0.f;
             if (t < tiles && n > 0) {
-                // ---- queries into their place, W/8 lanes a row; then a row a thread: a power of two makes it f16
-                constexpr int kLanes = W / 8, kAtOnce = 32 / kLanes;
-                const bool vec = (reinterpret_cast<uintptr_t>(a.q.p) & 15u) == 0 && ((a.q.ts | a.q.hs) & 7) == 0;
+                // ---- queries into their place, 16 bytes a lane; then a row a thread: a power of two makes it f16 (two parts of
+                // fp32: 16 raw bytes each lie where a chunk of one part will)
+                constexpr int kPerChunk = 16 / (int)sizeof(T), kLanes = W / kPerChunk, kAtOnce = 32 / kLanes;
+                const bool vec = (reinterpret_cast<uintptr_t>(a.q.p) & 15u) == 0 && ((a.q.ts | a.q.hs) & (kPerChunk - 1)) == 0;
                 const int64_t q_row = real ? (int64_t)(p.q0 + tok) * a.q.ts + (int64_t)(p.head * a.G + row - tok * a.G) * a.q.hs : INT64_MIN;
                 const int chunk = lane % kLanes;
                 const uint32_t place = smem_u32(smem + S::kQAt) + t * S::kQTile;
-                const uint32_t dst = place + (chunk / 8) * (kTileRows * 128);
+                auto chunk_at = [&](int part, int r, int c) { return place + part * S::kQPart + (c / 8) * (kTileRows * 128) + swizzled(r, c % 8); };
 #pragma unroll 4
                 for (int x = 0; x < 32 / kAtOnce; ++x) {
                     const int r = x * kAtOnce + lane / kLanes;             // of the warp's 32 rows
                     const int64_t at_row = __shfl_sync(0xffffffffu, q_row, r);
-                    const uint32_t to = dst + swizzled(wl + r, chunk % 8);
-                    const __nv_bfloat16 *src = (const __nv_bfloat16 *)a.q.p + at_row + 8 * chunk;
-                    if (at_row == INT64_MIN || 8 * chunk >= a.D) sts16(to, 0u, 0u, 0u, 0u);
+                    const uint32_t to = SPLIT ? chunk_at(chunk & 1, wl + r, chunk >> 1) : chunk_at(0, wl + r, chunk);
+                    const T *src = (const T *)a.q.p + at_row + kPerChunk * chunk;
+                    if (at_row == INT64_MIN || kPerChunk * chunk >= a.D) sts16(to, 0u, 0u, 0u, 0u);
                     else if (vec) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(src) : "memory");
                     else {
 #pragma unroll 1
-                        for (int e = 0; e < 8; ++e) asm volatile("st.shared.u16 [%0], %1;" ::"r"(to + 2 * e), "h"(__bfloat16_as_ushort(src[e])) : "memory");
+                        for (int e = 0; e < kPerChunk; ++e) {
+                            if (SPLIT) asm volatile("st.shared.b32 [%0], %1;" ::"r"(to + 4 * e), "r"(reinterpret_cast<const uint32_t *>(src)[e]) : "memory");
+                            else asm volatile("st.shared.u16 [%0], %1;" ::"r"(to + 2 * e), "h"(reinterpret_cast<const uint16_t *>(src)[e]) : "memory");
+                        }
                     }
                 }
                 asm volatile("cp.async.wait_all;" ::: "memory");
                 __syncwarp();
+                auto numbers = [&](int c, float (&v)[8]) {                 // dimensions 8 c .. of this thread's row
+                    uint32_t x[4], y[4];
+                    lds16(chunk_at(0, row_in, c), x);
+                    if (SPLIT) lds16(chunk_at(1, row_in, c), y);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        if (SPLIT) { v[e] = __uint_as_float(x[e]); v[4 + e] = __uint_as_float(y[e]); }
+                        else { v[2 * e] = __uint_as_float(x[e] << 16); v[2 * e + 1] = __uint_as_float(x[e] & 0xffff0000u); }
+                    }
+                };
                 float top = 0.f;
 #pragma unroll 4
                 for (int c = 0; c < W / 8; ++c) {
-                    uint32_t x[4];
-                    lds16(place + (c / 8) * (kTileRows * 128) + swizzled(row_in, c % 8), x);
+                    float v[8];
+                    numbers(c, v);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) top = max3(top, fabsf(__uint_as_float(x[e] << 16)), fabsf(__uint_as_float(x[e] & 0xffff0000u)));
+                    for (int e = 0; e < 8; e += 2) top = max3(top, fabsf(v[e]), fabsf(v[e + 1]));
                 }
                 const int e2 = row_exponent(top);
                 const float up = power2(10 - e2) * (a.score_scale < 0.f ? -1.f : 1.f);
                 f = fmaxf(fabsf(a.score_scale) * power2(e2 - 10), 1e-30f);      // not 0, which times a masked -infinity is no number
 #pragma unroll 4
                 for (int c = 0; c < W / 8; ++c) {
-                    uint32_t x[4];
-                    const uint32_t at_chunk = place + (c / 8) * (kTileRows * 128) + swizzled(row_in, c % 8);
-                    lds16(at_chunk, x);
+                    float v[8];
+                    numbers(c, v);
+                    uint32_t h[4], lo[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) x[e] = pack2(__uint_as_float(x[e] << 16) * up, __uint_as_float(x[e] & 0xffff0000u) * up);
-                    sts16(at_chunk, x[0], x[1], x[2], x[3]);
+                    for (int e = 0; e < 4; ++e) {
+                        const float u = v[2 * e] * up, w = v[2 * e + 1] * up;
+                        h[e] = pack2(u, w);
+                        if (SPLIT) { const float2 g = unpack2(h[e]); lo[e] = pack2(u - g.x, w - g.y); }
+                    }
+                    sts16(chunk_at(0, row_in, c), h[0], h[1], h[2], h[3]);
+                    if (SPLIT) sts16(chunk_at(1, row_in, c), lo[0], lo[1], lo[2], lo[3]);
                 }
                 fence_async();
                 tc::tc_fence_before();
@@ -593,19 +640,21 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
                         }
                         st_wait();
                     }
-                    // ---- the row's 128 scores stay in registers from the search for the largest to the weights: a chain of
+                    // ---- the row's scores stay in registers from the search for the largest to the weights: a chain of
                     // loads from tensor memory (200 cycles each) would be the longest part of a tile
-                    uint32_t r0[64], r1[64];
+                    uint32_t r0[64], r1[KEYS == 128 ? 64 : 4];
                     ld64(s_tmem, r0);
-                    ld64(s_tmem + 64, r1);
+                    if constexpr (KEYS == 128) ld64(s_tmem + 64, r1);
                     tc::tmem_ld_wait();
                     float top0 = -INFINITY, top1 = -INFINITY, top2 = -INFINITY, top3 = -INFINITY;
 #pragma unroll
                     for (int i = 0; i < 64; i += 4) {
                         top0 = max3(top0, __uint_as_float(r0[i]), __uint_as_float(r0[i + 1]));
                         top1 = max3(top1, __uint_as_float(r0[i + 2]), __uint_as_float(r0[i + 3]));
-                        top2 = max3(top2, __uint_as_float(r1[i]), __uint_as_float(r1[i + 1]));
-                        top3 = max3(top3, __uint_as_float(r1[i + 2]), __uint_as_float(r1[i + 3]));
+                        if constexpr (KEYS == 128) {
+                            top2 = max3(top2, __uint_as_float(r1[i]), __uint_as_float(r1[i + 1]));
+                            top3 = max3(top3, __uint_as_float(r1[i + 2]), __uint_as_float(r1[i + 3]));
+                        }
                     }
                     const float top = fmaxf(fmaxf(top0, top1), fmaxf(top2, top3)), reach = top == -INFINITY ? -INFINITY : top * f;
                     if (__any_sync(0xffffffffu, reach > m)) {       // O follows only when a score passes the reference
@@ -631,20 +680,24 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
                     const uint64_t f2 = pair(f, f), away2 = pair((kHead + kSlack) - m, (kHead + kSlack) - m);
                     uint64_t sum2 = 0ull;
                     auto weights = [&](const uint32_t (&r)[64], int at_key) {        // 32 keys become 16 columns
-                        uint32_t w[16];
+                        uint32_t w[16], lo[SPLIT ? 16 : 1];
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
                             const float2 x = halves(fma2(pair(__uint_as_float(r[at_key % 64 + 2 * i]), __uint_as_float(r[at_key % 64 + 2 * i + 1])), f2, away2));
                             const float e0 = ex2(x.x), e1 = ex2(x.y);
                             sum2 = add2(sum2, pair(e0, e1));
                             w[i] = pack2(e0, e1);
+                            if (SPLIT) { const float2 g = unpack2(w[i]); lo[SPLIT ? i : 0] = pack2(e0 - g.x, e1 - g.y); }
                         }
                         st16(s_tmem + at_key / 2, w);
+                        if constexpr (SPLIT) st16(s_tmem + KEYS / 2 + at_key / 2, lo);
                     };
                     weights(r0, 0);
                     weights(r0, 32);
-                    weights(r1, 64);
-                    weights(r1, 96);
+                    if constexpr (KEYS == 128) {
+                        weights(r1, 64);
+                        weights(r1, 96);
+                    }
                     l += halves(sum2).x + halves(sum2).y;
                     st_wait();
                     tc::tc_fence_before();
@@ -661,33 +714,37 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
             const bool whole = p.first == 0 && p.last == p.units;
             const int slot = blockIdx.x * 2 + (p.first == 0 ? 1 : 0);
             if (t < tiles) {
-                // the rows go through the queries' place in shared memory (their products are done), so that 16 (8) lanes
-                // store a row's 256 (128) bytes: all of W dimensions as bf16, or 64 (32) of a piece as fp32
+                // the rows go through the queries' place in shared memory (their products are done), so that W/8 lanes store
+                // 2 W bytes of a row: all of its dimensions as bf16, or half of them as fp32
                 constexpr int kLanes = W / 8, kAtOnce = 32 / kLanes, kPass = W / 2;
                 const float k = whole ? (l > 0.f || l != l ? a.v_scale / l : 0.f) : 1.f;
                 const uint32_t place = smem_u32(smem + S::kQAt) + t * S::kQTile;
+                const bool wide = SPLIT || !whole;
                 auto slot16 = [&](int r, int c) { return place + (c / 8) * (kTileRows * 128) + swizzled(wl + r, c % 8); };
                 const int chunk = lane % kLanes;
                 const int64_t to_row = real ? out_row * a.D : -1;
                 float *part = a.prompt_part + ((int64_t)slot * kStretchRows + t * kTileRows + wl) * W;
 #pragma unroll 1
-                for (int pass = 0; pass < (whole ? 1 : 2); ++pass) {
+                for (int pass = 0; pass < (wide ? 2 : 1); ++pass) {
                     __syncwarp();
 #pragma unroll 1
-                    for (int c = 0; c < (whole ? W : kPass) / 32; ++c) {
+                    for (int c = 0; c < (wide ? kPass : W) / 32; ++c) {
                         uint32_t r[32];
                         if (n > 0) { ld32(o_tmem + pass * kPass + 32 * c, r); tc::tmem_ld_wait(); }
                         else {
 #pragma unroll
                             for (int i = 0; i < 32; ++i) r[i] = 0u;
                         }
-                        if (whole) {
+                        if (SPLIT) {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * k);
+                        } else if (whole) {
 #pragma unroll
                             for (int i = 0; i < 16; ++i) r[i] = bf2(__uint_as_float(r[2 * i]) * k, __uint_as_float(r[2 * i + 1]) * k);
                         }
 #pragma unroll
                         for (int i = 0; i < 8; ++i)
-                            if (i < 4 || !whole) sts16(slot16(lane, (whole ? 4 : 8) * c + i), r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]);
+                            if (i < 4 || wide) sts16(slot16(lane, (wide ? 8 : 4) * c + i), r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]);
                     }
                     __syncwarp();
 #pragma unroll 4
@@ -698,7 +755,10 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
                         lds16(slot16(r, chunk), v);
                         if (to == -1) continue;
                         if (!whole) *reinterpret_cast<uint4 *>(part + r * W + pass * kPass + 4 * chunk) = make_uint4(v[0], v[1], v[2], v[3]);
-                        else if (8 * chunk < a.D) *reinterpret_cast<uint4 *>((__nv_bfloat16 *)a.out + to + 8 * chunk) = make_uint4(v[0], v[1], v[2], v[3]);
+                        else {
+                            const int d = SPLIT ? pass * kPass + 4 * chunk : 8 * chunk;
+                            if (d < a.D) *reinterpret_cast<uint4 *>((T *)a.out + to + d) = make_uint4(v[0], v[1], v[2], v[3]);
+                        }
                     }
                 }
                 __syncwarp();
@@ -707,20 +767,20 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
             tc::tc_fence_before();
             if (!whole) {
                 __threadfence();
-                asm volatile("bar.sync 1, 256;" ::: "memory");
+                asm volatile("bar.sync 1, %0;" ::"n"(TILES * 128) : "memory");
                 if (tid == 0) {
                     const int before = atomicAdd(a.prompt_arrived + p.cta0, 1);
                     last_s = before == p.cta1 - p.cta0;
                     if (last_s) a.prompt_arrived[p.cta0] = 0;          // ready for the next call
                 }
-                asm volatile("bar.sync 1, 256;" ::: "memory");
+                asm volatile("bar.sync 1, %0;" ::"n"(TILES * 128) : "memory");
                 if (last_s) {
                     __threadfence();
-                    // a warp takes rows warp, warp + 8, ..., a lane W/32 neighbouring dimensions: whole lines, 8 rows in flight
-                    constexpr int kPer = W / 32, kRowsAtOnce = 8;
+                    // a warp takes every kWarps-th row, a lane W/32 neighbouring dimensions: whole lines, several rows in flight
+                    constexpr int kPer = W / 32, kRowsAtOnce = W == 256 ? 4 : 8, kWarps = 4 * TILES;
                     const int rows = p.row1 - p.row0;
 #pragma unroll 1
-                    for (int x0 = warp; x0 < rows; x0 += 8 * kRowsAtOnce) {
+                    for (int x0 = warp; x0 < rows; x0 += kWarps * kRowsAtOnce) {
                         float top[kRowsAtOnce], sum[kRowsAtOnce], v[kRowsAtOnce][kPer];
 #pragma unroll
                         for (int y = 0; y < kRowsAtOnce; ++y) {
@@ -735,12 +795,15 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
                             float d[kRowsAtOnce][kPer];
 #pragma unroll
                             for (int y = 0; y < kRowsAtOnce; ++y) {
-                                const int64_t at_row = at_piece + min(x0 + 8 * y, rows - 1);
+                                const int64_t at_row = at_piece + min(x0 + kWarps * y, rows - 1);
                                 ml[y] = __ldcg(&a.prompt_ml[at_row]);
                                 const float *src = a.prompt_part + at_row * W + lane * kPer;
-                                if (kPer == 4) {
-                                    const float4 z = __ldcg(reinterpret_cast<const float4 *>(src));
-                                    d[y][0] = z.x; d[y][1] = z.y; d[y][2 % kPer] = z.z; d[y][3 % kPer] = z.w;
+                                if (kPer >= 4) {
+#pragma unroll
+                                    for (int e = 0; e < kPer; e += 4) {
+                                        const float4 z = __ldcg(reinterpret_cast<const float4 *>(src + e));
+                                        d[y][e % kPer] = z.x; d[y][(e + 1) % kPer] = z.y; d[y][(e + 2) % kPer] = z.z; d[y][(e + 3) % kPer] = z.w;
+                                    }
                                 } else {
                                     const float2 z = __ldcg(reinterpret_cast<const float2 *>(src));
                                     d[y][0] = z.x; d[y][1] = z.y;
@@ -757,17 +820,20 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
                         }
 #pragma unroll
                         for (int y = 0; y < kRowsAtOnce; ++y) {
-                            const int x = x0 + 8 * y;
+                            const int x = x0 + kWarps * y;
                             if (x >= rows || lane * kPer >= a.D) continue;
                             const float k = sum[y] > 0.f || sum[y] != sum[y] ? a.v_scale / sum[y] : 0.f;
                             const int r_tok = div_g(a, p.row0 + x);
-                            uint32_t *dst = reinterpret_cast<uint32_t *>((__nv_bfloat16 *)a.out + ((int64_t)(p.q0 + r_tok) * a.H + p.head * a.G + p.row0 + x - r_tok * a.G) * a.D + lane * kPer);
+                            T *dst = (T *)a.out + ((int64_t)(p.q0 + r_tok) * a.H + p.head * a.G + p.row0 + x - r_tok * a.G) * a.D + lane * kPer;
 #pragma unroll
-                            for (int e = 0; e < kPer; e += 2) dst[e / 2] = bf2(v[y][e] * k, v[y][e + 1] * k);
+                            for (int e = 0; e < kPer; e += 2) {
+                                if (SPLIT) *reinterpret_cast<float2 *>(dst + e) = make_float2(v[y][e] * k, v[y][e + 1] * k);
+                                else *reinterpret_cast<uint32_t *>(dst + e) = bf2(v[y][e] * k, v[y][e + 1] * k);
+                            }
                         }
                     }
                 }
-                asm volatile("bar.sync 1, 256;" ::: "memory");       // last_s is the next piece's
+                asm volatile("bar.sync 1, %0;" ::"n"(TILES * 128) : "memory");       // last_s is the next piece's
             }
         }
     }
@@ -777,32 +843,38 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
     if (warp == 12) tc::tmem_dealloc(tmem_slot, 512);
 }
 
-template <int W>
+template <typename T, int W, int TILES, int KEYS>
 cudaError_t launch(const AttendArgs &a, int sm_count, cudaStream_t s, uint64_t *launches) {
-    auto k = attend_prompt_kernel<W>;
+    using S = Shape<T, W, TILES, KEYS>;
+    auto k = attend_prompt_kernel<T, W, TILES, KEYS>;
     static std::atomic<bool> ready[64];
     int dev = 0;
     cudaError_t err = cudaGetDevice(&dev);
     if (err != cudaSuccess) return err;
-    const int most = Shape<W>::kLineAt + 8 * (kMaxRequests + 1) + 1024;
+    const int most = S::kLineAt + 8 * (kMaxRequests + 1) + 1024;
     if (dev >= 64 || !ready[dev].load()) {
         err = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
         if (err != cudaSuccess) return err;
         if (dev < 64) ready[dev].store(true);
     }
-    k<<<sm_count, kThreads, Shape<W>::kLineAt + 8 * (a.n + 1) + 1024, s>>>(a);
+    k<<<sm_count, kThreads, S::kLineAt + 8 * (a.n + 1) + 1024, s>>>(a);
     ++*launches;
     return cudaGetLastError();
 }
 
 }  // namespace
 
-size_t prompt_part_floats(int w) { return (size_t)2 * kStretchRows * w; }
-size_t prompt_part_rows() { return 2 * kStretchRows; }
-bool prompt_supported(int dtype, int head_dim) { return dtype == MOE_BF16 && head_dim <= 128; }
+size_t prompt_part_floats(int w) { return (size_t)2 * (w == 256 ? 128 : 256) * w; }
+size_t prompt_part_rows() { return 2 * 256; }
+// fp32 heads of more than 128 dimensions would need 256 KB of shared memory
+bool prompt_supported(int dtype, int head_dim) { return dtype == MOE_BF16 || head_dim <= 128; }
 
 cudaError_t launch_attend_prompt(const AttendArgs &a, int sm_count, cudaStream_t s, uint64_t *launches) {
-    return padded_width(a.D) == 64 ? launch<64>(a, sm_count, s, launches) : launch<128>(a, sm_count, s, launches);
+    const int w = padded_width(a.D);
+    if (a.dtype == MOE_BF16)
+        return w == 64 ? launch<__nv_bfloat16, 64, 2, 128>(a, sm_count, s, launches) : w == 128 ? launch<__nv_bfloat16, 128, 2, 128>(a, sm_count, s, launches)
+                                                                                              : launch<__nv_bfloat16, 256, 1, 64>(a, sm_count, s, launches);
+    return w == 64 ? launch<float, 64, 2, 128>(a, sm_count, s, launches) : launch<float, 128, 1, 128>(a, sm_count, s, launches);
 }
 
 }  // namespace kv
