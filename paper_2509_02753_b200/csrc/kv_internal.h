@@ -91,7 +91,7 @@ struct AttendArgs {
     void *out;
     float *part; float2 *part_ml; int32_t *arrived; int max_ctas;   // split over the keys
     FastDiv g_div;                            // by G
-    // requests of more query rows per key/value head than this are kv_prompt.cu's; 0: none are
+    // requests of more query rows per key/value head than this are kv_prompt.cu's; 0: all are the launched kernel's
     int prompt_rows;
     float *prompt_part; float2 *prompt_ml; int32_t *prompt_arrived;
     int32_t *status;

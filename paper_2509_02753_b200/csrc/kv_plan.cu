@@ -29,7 +29,7 @@ constexpr int kMaxCtasPerSm = 8;
 constexpr int64_t kMaxRows = 1 << 30;         // max_tokens * n_heads
 constexpr int64_t kMaxContext = 1 << 30;      // tokens that a row of a block table may stand for
 constexpr int kPartRows = 32;         // rows of a piece, at most
-constexpr int kPromptRows = 32;       // what kv_attend.cu takes in one pass over the keys
+constexpr int kPassRows = 32;         // query rows of a pass over the keys in kv_attend.cu
 
 size_t elem_size(int dtype) { return dtype == MOE_BF16 ? 2 : 4; }
 bool aligned(const void *p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
@@ -254,12 +254,21 @@ int moe_kv_attention(moe_kv_plan_t *p, const moe_kv_rows_t *q, int32_t T, const 
     a.part = p->part; a.part_ml = p->part_ml; a.arrived = p->arrived; a.max_ctas = p->max_ctas; a.status = p->status;
     a.prompt_part = p->prompt_part; a.prompt_ml = p->prompt_ml; a.prompt_arrived = p->prompt_arrived;
     cudaStream_t s = (cudaStream_t)stream;
-    const long long rows = (long long)(max_new > 0 && max_new < T ? max_new : T) * a.G;
-    a.prompt_rows = prompt_supported(c.dtype, c.head_dim) && rows > kPromptRows ? kPromptRows : 0;
-    if (a.prompt_rows > 0) {
-        const cudaError_t err = launch_attend_prompt(a, p->sm_count, s, &p->launches);
-        if (err != cudaSuccess) return done(err);
-    }
+    // Which kernel.  One pass over the keys serves 32 rows in kv_attend.cu (16 of wide heads); more rows read them again
+    // there, while kv_prompt.cu has tiles of 128.  Measured at 8 key/value heads of 128 dimensions, 36 rows each: 16 requests
+    // of 2000 keys 69 us there, 58 here; 64 dimensions 46 and 41; 256 dimensions, 36 rows 95 and 102, 64 rows 117 and 106.
+    // While all of its work is about one step of every warp kv_attend.cu is faster whatever the rows (one request of 500
+    // keys, 256 rows: 22 us and 31).
+    const int most = max_new > 0 && max_new < T ? max_new : T;
+    const long long rows = (long long)most * a.G, strips = (rows + kPassRows - 1) / kPassRows * n * a.Hk;
+    const bool one_step = strips * (((long long)width * c.page_size + kBlockTokens - 1) / kBlockTokens) <= 32ll * p->sm_count;
+    const int limit = padded_width(c.head_dim) == 256 ? 2 * kPassRows : kPassRows;
+    if (!prompt_supported(c.dtype, c.head_dim) || rows <= limit || one_step) return done(launch_attend_rows(a, p->sm_count, s, &p->launches));
+    // requests of one size, whichever it is, all go to the one kernel; otherwise each to its own
+    const bool alike = (long long)n * most == T;
+    a.prompt_rows = alike ? 0 : limit;
+    const cudaError_t err = launch_attend_prompt(a, p->sm_count, s, &p->launches);
+    if (err != cudaSuccess || alike) return done(err);
     return done(launch_attend_rows(a, p->sm_count, s, &p->launches));
 }
 

@@ -299,10 +299,10 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
     };
     auto wait = [&](uint32_t b, uint32_t parity) { if (!dead) dead = !tc::mbar_wait(b, parity, a.status); };
 
-    // registers by role: 2 x 192 + 72 + 56 = 512 = 4 x 128, what the block was launched with
+    // registers by role: 2 x 184 + 88 + 56 = 512 = 4 x 128, what the block was launched with
     if (group == 2) {
         // ================================================================ conversion
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
         const int c8 = tid - 256;                                             // 0..127
         const int key_in = c8 % KEYS, key_part = c8 / KEYS;                   // a thread's key, and which kKeyDims of it
         const int v_sub = KEYS == 128 ? c8 >> 6 : 0, v_c = lane & 7, v_r = (lane >> 3) + 4 * (KEYS == 128 ? (c8 >> 5) & 1 : c8 >> 5);
@@ -527,7 +527,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
         __syncwarp();
     } else if (group < TILES) {
         // ================================================================ softmax: thread = row of tile `group`
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
         const int t = group, row_in = tid & 127, wl = (warp & 3) * 32;
         const uint32_t lanes = (uint32_t)wl << 16;
         const uint32_t s_tmem = tmem + S::kS + t * kTileKeys + lanes, o_tmem = tmem + S::kO + t * W + lanes;
