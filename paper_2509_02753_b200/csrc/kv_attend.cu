@@ -95,6 +95,8 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
 
     if (tid < kWarps * S::kStages) tc::mbar_init(smem_u32(&full[tid]), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    pdl_trigger();
+    pdl_wait();
 
     // ---- the line: for request i, row blocks * heads * visible blocks (at least one, which writes the zeros)
     const int page_tokens = kBlockTokens << a.page_shift;
@@ -769,9 +771,8 @@ cudaError_t launch(const AttendArgs &a, int sm_count, cudaStream_t s, uint64_t *
     const long long pieces = most < 1e9 ? (long long)most : grid;
     grid = pieces < grid ? pieces : grid;
     grid = grid > a.max_ctas ? a.max_ctas : grid < 1 ? 1 : grid;
-    k<<<(int)grid, kThreads, smem, s>>>(a);
     ++*launches;
-    return cudaGetLastError();
+    return launch_chained(k, dim3((unsigned)grid), dim3(kThreads), smem, s, true, a);
 }
 
 template <typename T, int W>

@@ -7,6 +7,9 @@
 
 #include <ATen/cuda/CUDAContext.h>
 #include <ATen/cuda/EmptyTensor.h>
+#include <ATen/core/TensorBase.h>
+#include <ATen/TensorUtils.h>
+#include <ATen/EmptyTensor.h>
 #include <ATen/ops/empty.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -93,6 +96,14 @@ at::Tensor fresh(at::IntArrayRef size, at::ScalarType type, int device) {
     return at::detail::empty_cuda(size, type, c10::Device(c10::kCUDA, (c10::DeviceIndex)device), std::nullopt);
 }
 
+// A part of a fresh buffer as a tensor of its own: several outputs cost one allocation
+at::Tensor part_of(const at::Tensor &base, int64_t offset, at::IntArrayRef size) {
+    at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(base.storage()), base.key_set(), base.dtype());
+    t.unsafeGetTensorImpl()->set_storage_offset(offset);
+    t.unsafeGetTensorImpl()->set_sizes_contiguous(size);
+    return t;
+}
+
 void *stream_of(const Plan &p) { return (void *)at::cuda::getCurrentCUDAStream((c10::DeviceIndex)p.device).stream(); }
 
 int32_t pages_of(const at::Tensor &cache, const Plan &p) {
@@ -152,8 +163,9 @@ PyObject *tables(PyObject *, PyObject *const *args, Py_ssize_t n) {
         const int64_t tokens = a.i64(), req = ctx.numel();
         WANT(ctx.dim() == 1 && fresh_len.numel() == req && table.dim() == 2 && table.size(0) == req, "lengths and block_table of different numbers of requests");
         WANT(tokens >= 0 && tokens <= INT32_MAX && free_pages.numel() <= INT32_MAX && table.size(1) <= INT32_MAX, "a size does not fit 32 bits");
-        at::Tensor kv_len = fresh({req}, at::kInt, p.device), cu = fresh({req + 1}, at::kInt, p.device), pos = fresh({tokens}, at::kInt, p.device);
-        at::Tensor slot = fresh({tokens}, at::kLong, p.device), taken = fresh({1}, at::kInt, p.device);
+        const at::Tensor words = fresh({tokens + 2 * req + 2}, at::kInt, p.device);
+        at::Tensor pos = part_of(words, 0, {tokens}), kv_len = part_of(words, tokens, {req}), cu = part_of(words, tokens + req, {req + 1});
+        at::Tensor taken = part_of(words, tokens + 2 * req + 1, {1}), slot = fresh({tokens}, at::kLong, p.device);
         const int rc = moe_kv_tables(p.handle, ctx.data_ptr<int32_t>(), fresh_len.data_ptr<int32_t>(), (int32_t)req, free_pages.data_ptr<int32_t>(),
                                      (int32_t)free_pages.numel(), table.data_ptr<int32_t>(), (int32_t)table.size(1), (int32_t)tokens,
                                      kv_len.data_ptr<int32_t>(), cu.data_ptr<int32_t>(), pos.data_ptr<int32_t>(), slot.data_ptr<int64_t>(),
@@ -217,7 +229,8 @@ PyObject *read(PyObject *, PyObject *const *args, Py_ssize_t n) {
         const at::Tensor &cache = a.tensor(), &slots = a.dense(at::kLong, "slots: dense int64 wanted");
         const float ks = a.f32(), vs = a.f32();
         WANT(slots.numel() <= INT32_MAX, "too many slots");
-        at::Tensor k = fresh({slots.numel(), p.kv_heads, p.dim}, p.type, p.device), v = fresh({slots.numel(), p.kv_heads, p.dim}, p.type, p.device);
+        const at::Tensor both = fresh({2, slots.numel(), p.kv_heads, p.dim}, p.type, p.device);
+        at::Tensor k = part_of(both, 0, {slots.numel(), p.kv_heads, p.dim}), v = part_of(both, both.numel() / 2, {slots.numel(), p.kv_heads, p.dim});
         const int rc = moe_kv_read(p.handle, cache.data_ptr(), pages_of(cache, p), slots.data_ptr<int64_t>(), (int32_t)slots.numel(), ks, vs,
                                    k.data_ptr(), v.data_ptr(), stream_of(p));
         return answer(rc, {k, v});

@@ -6,6 +6,7 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "moe_internal.h"
 #include "moe_kv.h"
 
 namespace lexi {

@@ -188,6 +188,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
     if (tid < 4) absent[tid] = 0u;
     if (warp == 12) tc::tmem_alloc(smem_u32(&tmem_slot), 512);
 
+    pdl_trigger();          // behind the allocation: a kernel that starts early and wants tensor memory cannot be ahead of this one
+    pdl_wait();
+
     // ---- the line: key tiles of every stretch of prompts
     auto lengths = [&](int i, int &len, int &q0, int &nq) {
         len = max(a.kv_len[i], 0);
@@ -857,9 +860,8 @@ cudaError_t launch(const AttendArgs &a, int sm_count, cudaStream_t s, uint64_t *
         if (err != cudaSuccess) return err;
         if (dev < 64) ready[dev].store(true);
     }
-    k<<<sm_count, kThreads, S::kLineAt + 8 * (a.n + 1) + 1024, s>>>(a);
     ++*launches;
-    return cudaGetLastError();
+    return launch_chained(k, dim3(sm_count), dim3(kThreads), S::kLineAt + 8 * (a.n + 1) + 1024, s, true, a);
 }
 
 }  // namespace

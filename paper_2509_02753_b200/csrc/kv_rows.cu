@@ -230,6 +230,8 @@ __device__ __forceinline__ void turn_unit(const T *x, int64_t xhs, T *y, int64_t
 
 template <typename T, int WALK, bool TABLE16>
 __global__ void __launch_bounds__(kThreads) rope_kernel(RopeArgs a, FastDiv units, FastDiv groups, int per_group) {
+    pdl_trigger();
+    pdl_wait();
     uint32_t e = blockIdx.x * kThreads + threadIdx.x, unit, grp, token;
     units.split(e, e, unit);
     groups.split(e, token, grp);
@@ -367,6 +369,8 @@ __device__ __forceinline__ uint8_t *block_of(uint8_t *cache, int64_t slot, int64
 template <typename T, int WALK, bool VEC, int W>
 __global__ void __launch_bounds__(kThreads, 4) append_kernel(AppendArgs a, uint32_t store_ratio, FastDiv units, FastDiv groups, int per_group, FastDiv heads) {
     constexpr int kLanes = W / 8;
+    pdl_trigger();
+    pdl_wait();
     // the storing CTAs (bound by instructions) lie evenly among the turning ones (bound by memory): number f(i) is CTA i
     // where f(i + 1) > f(i), f(i) = i * ratio / 2^32
     const uint32_t store = __umulhi(blockIdx.x, store_ratio);
@@ -425,6 +429,8 @@ __global__ void __launch_bounds__(kThreads, 4) append_kernel(AppendArgs a, uint3
 // A thread reads 8 dimensions of a key row and of a value row
 template <typename T, int W>
 __global__ void __launch_bounds__(kThreads) read_kernel(ReadArgs a, FastDiv chunks, FastDiv heads) {
+    pdl_trigger();
+    pdl_wait();
     uint32_t e = blockIdx.x * kThreads + threadIdx.x, chunk, head, token_no;
     chunks.split(e, e, chunk);
     heads.split(e, token_no, head);
@@ -541,9 +547,10 @@ cudaError_t launch_rope(const RopeArgs &all, int sm_count, cudaStream_t s, uint6
         a.x.p = moved(all.x.p, t0 * all.x.ts, all.dtype);
         a.y = (void *)moved(all.y, t0 * all.yts, all.dtype);
         a.turn.position += t0;
-        k<<<(unsigned)(((long long)a.T * groups * units + kThreads - 1) / kThreads), kThreads, 0, s>>>(a, FastDiv(units), FastDiv(groups), per);
+        const cudaError_t err = launch_chained(k, dim3((unsigned)(((long long)a.T * groups * units + kThreads - 1) / kThreads)), dim3(kThreads), 0, s, true, a, FastDiv(units),
+                                               FastDiv(groups), per);
+        if (err != cudaSuccess) return err;
         ++*launches;
-        if (cudaError_t err = cudaGetLastError()) return err;
     }
     return cudaSuccess;
 }
@@ -574,9 +581,9 @@ cudaError_t launch_append(const AppendArgs &all, int sm_count, cudaStream_t s, u
         const long long sc = ((long long)a.T * a.Hk * (w / 8) + kThreads - 1) / kThreads;
         // ceil(2^32 sc / (qc + sc)): f(qc + sc) = sc exactly; all ones where nothing turns
         const uint32_t ratio = qc == 0 ? 0xffffffffu : (uint32_t)((((unsigned long long)sc << 32) + qc + sc - 1) / (qc + sc));
-        k<<<(unsigned)(qc + sc), kThreads, 0, s>>>(a, ratio, FastDiv(units), FastDiv(groups), per, FastDiv(a.Hk));
+        const cudaError_t err = launch_chained(k, dim3((unsigned)(qc + sc)), dim3(kThreads), 0, s, true, a, ratio, FastDiv(units), FastDiv(groups), per, FastDiv(a.Hk));
+        if (err != cudaSuccess) return err;
         ++*launches;
-        if (cudaError_t err = cudaGetLastError()) return err;
     }
     return cudaSuccess;
 }
@@ -593,9 +600,10 @@ cudaError_t launch_read(const ReadArgs &all, cudaStream_t s, uint64_t *launches)
         a.slot += t0;
         if (a.k) a.k = (void *)moved(all.k, (int64_t)t0 * all.Hk * all.D, all.dtype);
         if (a.v) a.v = (void *)moved(all.v, (int64_t)t0 * all.Hk * all.D, all.dtype);
-        k<<<(unsigned)(((long long)a.T * a.Hk * chunks + kThreads - 1) / kThreads), kThreads, 0, s>>>(a, FastDiv(chunks), FastDiv(a.Hk));
+        const cudaError_t err = launch_chained(k, dim3((unsigned)(((long long)a.T * a.Hk * chunks + kThreads - 1) / kThreads)), dim3(kThreads), 0, s, true, a, FastDiv(chunks),
+                                               FastDiv(a.Hk));
+        if (err != cudaSuccess) return err;
         ++*launches;
-        if (cudaError_t err = cudaGetLastError()) return err;
     }
     return cudaSuccess;
 }

@@ -36,6 +36,9 @@ __global__ void __launch_bounds__(kThreads) tables_kernel(TablesArgs a) {
     int bad = 0;
     auto pages = [&](long long tokens) { return (tokens + (1 << a.page_shift) - 1) >> a.page_shift; };
 
+    pdl_trigger();
+    pdl_wait();
+
     // running sums of (fresh pages, new tokens), packed in one 64-bit word, 256 requests at a time
     unsigned long long carry = 0;
     for (int base = 0; base < a.n; base += kThreads) {
@@ -116,9 +119,8 @@ cudaError_t launch_tables(const TablesArgs &a, int sm_count, cudaStream_t s, uin
     const size_t smem = (size_t)2 * (a.n + 1) * sizeof(int32_t);      // at most 32 KB
     int grid = (a.n_tokens + kTokensPerCta - 1) / kTokensPerCta;
     grid = grid < 1 ? 1 : grid > 2 * sm_count ? 2 * sm_count : grid;
-    tables_kernel<<<grid, kThreads, smem, s>>>(a);
     ++*launches;
-    return cudaGetLastError();
+    return launch_chained(tables_kernel, dim3(grid), dim3(kThreads), smem, s, true, a);
 }
 
 }  // namespace kv
