@@ -89,7 +89,7 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
     __shared__ float2 join_ml[kWarps][S::kRows];   // reference and sum of each warp, then weight of each warp
     __shared__ float2 row_ml[S::kRows];
     __shared__ long long sum_s[kWarps];
-    __shared__ int strips_s[kWarps], longest_s[kWarps];
+    __shared__ int strips_s[kWarps], longest_s[kWarps], len_s[32], q0_s[32], nq_s[32];
     __shared__ int last_s;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r = lane >> 2, c = lane & 3;
 
@@ -159,10 +159,42 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
     bool few = false, even = false;
     int chunk = 0;
     long long share = 0, total = 0;
-    // pass 0 counts, pass 1 weighs and lines up (one copy of the code: this kernel's first run of an instruction costs more
-    // than its second)
+    const int grid = gridDim.x;
+    // ceil(x / by), x >= 0: 32-bit division where x has no more
+    auto div_up = [&](long long x, int by) { x += by - 1; return x >> 32 ? x / by : (long long)((uint32_t)x / (uint32_t)by); };
+    auto choose = [&](long long blocks, long long stretches, int longest) {       // blocks without the entries
+        few = 2 * stretches <= grid;
+        even = few || longest <= kBrief;
+        // few: sum of ceil(u/chunk) <= blocks/chunk + stretches <= grid
+        chunk = few ? (int)max(div_up(blocks, max(grid - (int)stretches, 1)), (long long)kLeast) : even ? kBrief : 0;
+        share = max(div_up(blocks + kEntry * stretches, grid), (long long)2 * kLeast);
+    };
+    // The usual step: up to 32 requests with one strip each.  Every warp does it for itself, in its lanes, without a barrier
+    bool simple = false;
+    if (a.n <= 32) {
+        int len = 0, q0 = 0, nq = 0;
+        if (lane < a.n) lengths(lane, len, q0, nq);
+        const int rows = nq * a.G, u = rows > 0 ? units_of(len, nq, 0) : 0;
+        const uint32_t sum_u = __reduce_add_sync(0xffffffffu, (uint32_t)u);             // u <= 2^26
+        simple = !__any_sync(0xffffffffu, rows > S::kRows) && ((unsigned long long)sum_u + 32 * kEntry) * a.Hk < (1ull << 30);
+        if (simple) {
+            choose((long long)sum_u * a.Hk, (long long)__popc(__ballot_sync(0xffffffffu, u > 0)) * a.Hk, (int)__reduce_max_sync(0xffffffffu, (uint32_t)u));
+            const int weight = u == 0 ? 0 : (even ? (int)((uint32_t)(u + chunk - 1) / (uint32_t)chunk) : u + kEntry) * a.Hk;
+            int inc = weight;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int up = __shfl_up_sync(0xffffffffu, inc, o);
+                if (lane >= o) inc += up;
+            }
+            total = __shfl_sync(0xffffffffu, inc, 31);
+            // all warps write the same
+            if (lane < a.n) { line[lane] = inc - weight; len_s[lane] = len; q0_s[lane] = q0; nq_s[lane] = nq; }
+            __syncwarp();
+        }
+    }
+    // Any other: pass 0 counts, pass 1 weighs and lines up (one copy of the code: an instruction's first run costs more)
 #pragma unroll 1
-    for (int pass = 0; pass < 2; ++pass) {
+    for (int pass = simple ? 2 : 0; pass < 2; ++pass) {
         long long carry = 0, stretches = 0;
         int most = 0;
 #pragma unroll 1
@@ -200,12 +232,7 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) { stretches += strips_s[w]; most = max(most, longest_s[w]); }
             stretches *= a.Hk;
-            const long long grid = gridDim.x;
-            few = 2 * stretches <= grid;
-            even = few || most <= kBrief;
-            // few: sum of ceil(u/chunk) <= blocks/chunk + stretches <= gridDim.x
-            chunk = few ? (int)max((total - kEntry * stretches + grid - stretches - 1) / max(grid - stretches, 1ll), (long long)kLeast) : even ? kBrief : 0;
-            share = max((total + grid - 1) / grid, (long long)2 * kLeast);
+            choose(total - kEntry * stretches, stretches, most);
             if (!even) break;               // the line of blocks is there already
         }
     }
@@ -218,6 +245,10 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
 
     int req = 0, len = 0, q0 = 0, nq = 0, sb = 0, wb = 0, nb = 0, row0 = 0, row1 = 0, units = 0, head = -1;
     long long place = 0;         // where the stretch begins (even: its first piece)
+    auto take = [&]() {
+        if (simple) { len = len_s[req]; q0 = q0_s[req]; nq = nq_s[req]; }
+        else lengths(req, len, q0, nq);
+    };
     auto shape = [&]() {
         row1 = min(row0 + S::kRows, nq * a.G);
         visible(len, nq, row0, row1, sb, wb, nb);
@@ -234,7 +265,7 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
             }
             long long from = line[lo];
             req = lo;
-            lengths(req, len, q0, nq);
+            take();
             if (even && !few) {              // every stretch is one piece
                 const uint32_t x = (uint32_t)(at - from);
                 row0 = (int)(x / (uint32_t)a.Hk) * S::kRows;
@@ -261,7 +292,7 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
                 head = 0;
                 row0 += S::kRows;
 #pragma unroll 1
-                while (row0 >= nq * a.G) { lengths(++req, len, q0, nq); row0 = 0; }          // the line goes on, so there is a request with rows
+                while (row0 >= nq * a.G) { ++req; take(); row0 = 0; }          // the line goes on, so there is a request with rows
                 shape();
             }
         }
