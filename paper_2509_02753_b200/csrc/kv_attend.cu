@@ -53,6 +53,10 @@ __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uin
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ void mma_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
 __device__ __forceinline__ uint32_t transpose8(uint32_t v) {
     uint32_t r;
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
@@ -445,11 +449,13 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
             for (int b = 0; b < kPair; ++b) {
                 constexpr bool kTwo = NT == 1;      // two chains of sums: half the latency of dependent products (more tiles are chains of their own)
                 float s2[kTwo ? NT : 1][4];
+                if (b == 1 && !two) {
 #pragma unroll
-                for (int t = 0; t < NT; ++t)
+                    for (int t = 0; t < NT; ++t)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) s[b][t][j] = s2[kTwo ? t : 0][j] = 0.f;
-                if (b == 1 && !two) continue;
+                        for (int j = 0; j < 4; ++j) s[b][t][j] = 0.f;
+                    continue;
+                }
                 const uint8_t *blk = buf + b * block_bytes(W);
                 constexpr int kBytes = W / 8;               // code bytes of a thread's share of a key
                 constexpr int kGroups = W / 64;             // scales of it
@@ -487,8 +493,10 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
 #pragma unroll
                         for (int t = 0; t < NT; ++t) {
                             const uint4 q = kHoldQ ? q_r[g * 2 + i] : *reinterpret_cast<const uint4 *>(q_s + ((t * (S::kSteps / 2) + g * 2 + i) * 32 + lane) * 16);
-                            mma(s[b][t], h0[0], h1[0], h0[1], h1[1], q.x, q.y);
-                            mma(kTwo ? s2[kTwo ? t : 0] : s[b][t], h0[2], h1[2], h0[3], h1[3], q.z, q.w);
+                            if (g + i == 0) mma_first(s[b][t], h0[0], h1[0], h0[1], h1[1], q.x, q.y);
+                            else mma(s[b][t], h0[0], h1[0], h0[1], h1[1], q.x, q.y);
+                            if (kTwo && g + i == 0) mma_first(s2[kTwo ? t : 0], h0[2], h1[2], h0[3], h1[3], q.z, q.w);
+                            else mma(kTwo ? s2[kTwo ? t : 0] : s[b][t], h0[2], h1[2], h0[3], h1[3], q.z, q.w);
                             if (SPLIT) {
                                 const uint4 ql = *reinterpret_cast<const uint4 *>(q_s + S::kRows * W * 2 + ((t * (S::kSteps / 2) + g * 2 + i) * 32 + lane) * 16);
                                 mma(s[b][t], h0[0], h1[0], h0[1], h1[1], ql.x, ql.y);
@@ -711,11 +719,10 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
             if (tid < S::kRows) part_ml[tid] = row_ml[tid];
             __syncthreads();
             if (tid == 0) {
-                __threadfence();                    // all of the CTA's writes above, by way of the barrier
-                const int before = atomicAdd(a.arrived + cta0, 1);
+                int before;                         // releases all of the CTA's writes above, by way of the barrier
+                asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(before) : "l"(a.arrived + cta0) : "memory");
                 last_s = before == cta1 - cta0;
                 if (last_s) a.arrived[cta0] = 0;             // ready for the next call
-                __threadfence();
             }
             __syncthreads();
             if (last_s) {
