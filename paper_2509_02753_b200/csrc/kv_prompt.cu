@@ -35,7 +35,7 @@ namespace {
 constexpr int kTileRows = 128;
 constexpr int kThreads = 512;
 constexpr float kFloor = -FLT_MAX;
-constexpr float kHead = 6.f, kSlack = 8.f;       // as in kv_attend.cu
+constexpr float kTop = 14.f;                     // the largest weight is 2^kTop, as in kv_attend.cu
 // What a stretch costs besides its tiles (queries, output, an empty pipeline), in tiles: counted in the line, or a CTA
 // with many short stretches would be last by far
 constexpr int kEntry = 3;
@@ -158,6 +158,9 @@ template <typename T, int W, int TILES, int KEYS>
 __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a) {
     using S = Shape<T, W, TILES, KEYS>;
     constexpr bool SPLIT = sizeof(T) == 4;
+    // The reference lies this far above a score that was once the largest.  fp32: near, so that exponents are small numbers
+    // (an exponent of 8 to 16 is rounded to 2^-20, which its weight feels); 2^kTop is then a factor, not part of the exponent
+    constexpr float kSlack = SPLIT ? 2.f : 8.f;
     constexpr int kTileKeys = KEYS, kTileBlocks = KEYS / kBlockTokens, kStretchRows = S::kRows;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
@@ -467,11 +470,13 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
                 const uint64_t da = q_d + t * (S::kQTile / 16), db = k_d + stage * (S::kKTile / 16);
                 if (one && !dead) {
 #pragma unroll
-                    for (int part = 0; part < S::kParts; ++part)
+                    for (int x = 0; x < S::kParts; ++x)
 #pragma unroll
-                        for (int i = 0; i < W / 16; ++i)
+                        for (int i = 0; i < W / 16; ++i) {
+                            const int part = S::kParts - 1 - x;          // the low part first: sums are cut off at their size so far
                             tc::umma_bf16(kTmem + S::kS + t * KEYS, da + part * (S::kQPart / 16) + (i / 4) * (kTileRows * 128 / 16) + 2 * (i % 4),
-                                          db + (i / 4) * (KEYS * 128 / 16) + 2 * (i % 4), idesc_f16(KEYS), part + i > 0);
+                                          db + (i / 4) * (KEYS * 128 / 16) + 2 * (i % 4), idesc_f16(KEYS), x + i > 0);
+                        }
                     tc::umma_commit(s_full(t));
                 }
                 __syncwarp();
@@ -680,15 +685,18 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
                         m = to;
                     }
                     // ---- weights: 32 scores become 16 columns
-                    const uint64_t f2 = pair(f, f), away2 = pair((kHead + kSlack) - m, (kHead + kSlack) - m);
-                    uint64_t sum2 = 0ull;
+                    const float away = SPLIT ? -m : kTop - m;
+                    const uint64_t f2 = pair(f, f), away2 = pair(away, away);
+                    uint64_t sum2 = 0ull, sum2b = 0ull;
                     auto weights = [&](const uint32_t (&r)[64], int at_key) {        // 32 keys become 16 columns
                         uint32_t w[16], lo[SPLIT ? 16 : 1];
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
                             const float2 x = halves(fma2(pair(__uint_as_float(r[at_key % 64 + 2 * i]), __uint_as_float(r[at_key % 64 + 2 * i + 1])), f2, away2));
-                            const float e0 = ex2(x.x), e1 = ex2(x.y);
-                            sum2 = add2(sum2, pair(e0, e1));
+                            float e0 = ex2(x.x), e1 = ex2(x.y);
+                            if (SPLIT) { e0 *= 16384.f; e1 *= 16384.f; }          // 2^kTop
+                            if (SPLIT && (i & 1)) sum2b = add2(sum2b, pair(e0, e1));
+                            else sum2 = add2(sum2, pair(e0, e1));
                             w[i] = pack2(e0, e1);
                             if (SPLIT) { const float2 g = unpack2(w[i]); lo[SPLIT ? i : 0] = pack2(e0 - g.x, e1 - g.y); }
                         }
@@ -701,6 +709,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
                         weights(r1, 64);
                         weights(r1, 96);
                     }
+                    if (SPLIT) sum2 = add2(sum2, sum2b);
                     l += halves(sum2).x + halves(sum2).y;
                     st_wait();
                     tc::tc_fence_before();
