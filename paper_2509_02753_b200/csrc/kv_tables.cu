@@ -29,9 +29,9 @@ __device__ __forceinline__ int find(const int32_t *sum, int n, int x) {
 
 __global__ void __launch_bounds__(kThreads) tables_kernel(TablesArgs a) {
     extern __shared__ int32_t sums[];
-    int32_t *cu = sums, *first = sums + a.n + 1;
-    __shared__ unsigned long long warp_sum[kThreads / 32];
-    __shared__ unsigned long long carry_s;
+    // running sums: new tokens, fresh pages, and the entries of the block table that these fill
+    int32_t *cu = sums, *first = sums + a.n + 1, *entry = sums + 2 * (a.n + 1);
+    __shared__ unsigned long long new_sum[kThreads / 32], fresh_sum[kThreads / 32], entry_sum[kThreads / 32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     int bad = 0;
     auto pages = [&](long long tokens) { return (tokens + (1 << a.page_shift) - 1) >> a.page_shift; };
@@ -39,36 +39,48 @@ __global__ void __launch_bounds__(kThreads) tables_kernel(TablesArgs a) {
     pdl_trigger();
     pdl_wait();
 
-    // running sums of (fresh pages, new tokens), packed in one 64-bit word, 256 requests at a time
-    unsigned long long carry = 0;
+    // 256 requests at a time, in 64 bits: whatever the lengths are, sums do not wrap, and what does not fit 32 bits stays at
+    // their largest value (a bad index in any case).  Entries lie inside the table, so there are at most n * width
+    unsigned long long new_carry = 0, fresh_carry = 0, entry_carry = 0;
+    auto low = [](unsigned long long x) { return x > INT32_MAX ? INT32_MAX : (int32_t)x; };
     for (int base = 0; base < a.n; base += kThreads) {
         const int i = base + tid;
-        unsigned long long mine = 0;
+        unsigned long long tokens = 0, fresh = 0, entries = 0;
         if (i < a.n) {
             int c = a.ctx[i], m = a.fresh_tokens[i];
             if (c < 0) { c = 0; bad |= MOE_KV_STATUS_BAD_INDEX; }
             if (m < 0) { m = 0; bad |= MOE_KV_STATUS_BAD_INDEX; }
-            const long long total = (long long)c + m;
-            const unsigned fresh = (unsigned)(pages(total) - pages(c));
-            mine = ((unsigned long long)fresh << 32) | (unsigned)m;
-            if (blockIdx.x == 0) a.kv_len[i] = total > INT32_MAX ? INT32_MAX : (int32_t)total;
+            const long long total = (long long)c + m, held = pages(c), wanted = pages(total);
+            tokens = (unsigned)m;
+            fresh = (unsigned long long)(wanted - held);
+            entries = (unsigned long long)(min(wanted, (long long)a.width) - min(held, (long long)a.width));
+            if (entries < fresh) bad |= MOE_KV_STATUS_NO_PAGES;
+            if (blockIdx.x == 0) a.kv_len[i] = low(total);
         }
-        unsigned long long inc = mine;
+        unsigned long long new_inc = tokens, fresh_inc = fresh, entry_inc = entries;
+#pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const unsigned long long up = __shfl_up_sync(0xffffffffu, inc, o);
-            if (lane >= o) inc += up;
+            const unsigned long long x = __shfl_up_sync(0xffffffffu, new_inc, o), y = __shfl_up_sync(0xffffffffu, fresh_inc, o),
+                                     z = __shfl_up_sync(0xffffffffu, entry_inc, o);
+            if (lane >= o) { new_inc += x; fresh_inc += y; entry_inc += z; }
         }
-        if (lane == 31) warp_sum[warp] = inc;
+        if (lane == 31) { new_sum[warp] = new_inc; fresh_sum[warp] = fresh_inc; entry_sum[warp] = entry_inc; }
         __syncthreads();
-        unsigned long long before = carry;
-        for (int w = 0; w < warp; ++w) before += warp_sum[w];
-        const unsigned long long at = before + inc - mine;
-        if (i < a.n) { cu[i] = (int32_t)(uint32_t)at; first[i] = (int32_t)(at >> 32); }
-        if (tid == kThreads - 1) carry_s = before + inc;
+        unsigned long long new_before = new_carry, fresh_before = fresh_carry, entry_before = entry_carry;
+        for (int w = 0; w < kThreads / 32; ++w) {
+            if (w == warp) { new_before = new_carry; fresh_before = fresh_carry; entry_before = entry_carry; }
+            new_carry += new_sum[w];
+            fresh_carry += fresh_sum[w];
+            entry_carry += entry_sum[w];
+        }
+        if (i < a.n) {
+            cu[i] = low(new_before + new_inc - tokens);
+            first[i] = low(fresh_before + fresh_inc - fresh);
+            entry[i] = low(entry_before + entry_inc - entries);
+        }
         __syncthreads();
-        carry = carry_s;
     }
-    if (tid == 0) { cu[a.n] = (int32_t)(uint32_t)carry; first[a.n] = (int32_t)(carry >> 32); }
+    if (tid == 0) { cu[a.n] = low(new_carry); first[a.n] = low(fresh_carry); entry[a.n] = low(entry_carry); }
     __syncthreads();
     const int n_new = cu[a.n], n_fresh = first[a.n];
 
@@ -88,13 +100,13 @@ __global__ void __launch_bounds__(kThreads) tables_kernel(TablesArgs a) {
         if (t < n_new) {
             const int r = find(cu, a.n, t);
             const int c = max(a.ctx[r], 0);
-            position = c + (t - cu[r]);
+            position = low((unsigned long long)c + (t - cu[r]));
             const int col = position >> a.page_shift, held = (int)pages(c);
             int page = -1;
             if (col < held) {
                 if (col < a.width) page = a.table[(int64_t)r * a.width + col];
             } else {
-                const int f = first[r] + col - held;
+                const long long f = (long long)first[r] + col - held;
                 if (f < a.n_free && col < a.width) page = a.free_pages[f];
             }
             if (col >= a.width) bad |= MOE_KV_STATUS_NO_PAGES;
@@ -103,12 +115,10 @@ __global__ void __launch_bounds__(kThreads) tables_kernel(TablesArgs a) {
         a.position[t] = position;
         a.slot[t] = slot;
     }
-    for (int f = blockIdx.x * kThreads + tid; f < n_fresh; f += stride) {
-        const int r = find(first, a.n, f);
-        const int held = (int)pages(max(a.ctx[r], 0));
-        const long long col = (long long)held + f - first[r];
+    for (long long e = blockIdx.x * kThreads + tid; e < entry[a.n]; e += stride) {
+        const int r = find(entry, a.n, (int)e);
+        const long long in = e - entry[r], col = pages(max(a.ctx[r], 0)) + in, f = (long long)first[r] + in;
         if (col < a.width) a.table[(int64_t)r * a.width + col] = f < a.n_free ? a.free_pages[f] : -1;
-        else bad |= MOE_KV_STATUS_NO_PAGES;
     }
     if (bad) atomicOr(a.status, bad);
 }
@@ -116,7 +126,11 @@ __global__ void __launch_bounds__(kThreads) tables_kernel(TablesArgs a) {
 }  // namespace
 
 cudaError_t launch_tables(const TablesArgs &a, int sm_count, cudaStream_t s, uint64_t *launches) {
-    const size_t smem = (size_t)2 * (a.n + 1) * sizeof(int32_t);      // at most 32 KB
+    const size_t smem = (size_t)3 * (a.n + 1) * sizeof(int32_t);      // 48 KB for the most requests, besides the static sums
+    if (smem > 40 * 1024) {
+        const cudaError_t err = cudaFuncSetAttribute(tables_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (err != cudaSuccess) return err;
+    }
     int grid = (a.n_tokens + kTokensPerCta - 1) / kTokensPerCta;
     grid = grid < 1 ? 1 : grid > 2 * sm_count ? 2 * sm_count : grid;
     ++*launches;

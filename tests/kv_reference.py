@@ -160,12 +160,14 @@ def attention(q, cu, kv_len, table, cache, page, window, sinks, scale, k_scale, 
         n = int(kv_len[i])
         nq = cu[i + 1] - cu[i]
         pages = [int(x) for x in table[i, : -(-n // page)]]
+        absent = {k for at, p in enumerate(pages) if not 0 <= p < len(cache) for k in range(at * page, (at + 1) * page)}
+        pages = [p if 0 <= p < len(cache) else 0 for p in pages]
         for h in range(heads):
             k = np.concatenate([k_all[p, h] for p in pages])[:n] * k_scale if n else np.zeros((0, dim))
             v = np.concatenate([v_all[p, h] for p in pages])[:n] * v_scale if n else np.zeros((0, dim))
             for j in range(nq):
                 p = n - nq + j
-                keys = [x for x in range(0, p + 1) if not window or p - x < window or x < sinks]
+                keys = [x for x in range(0, p + 1) if (not window or p - x < window or x < sinks) and x not in absent]
                 if not keys:
                     continue
                 for g in range(G):

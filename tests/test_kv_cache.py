@@ -144,6 +144,20 @@ def test_tables_that_do_not_fit():
     check_tables([0, 3], [4, 2], [5, 9], [[-1], [7]], 16, 4, K.STATUS_BAD_INDEX)                                    # more tokens than room
 
 
+@gpu
+def test_tables_of_lengths_that_pass_32_bits():
+    with plan_for(requests=300, tokens=8) as plan:
+        n = 300
+        new = np.full(n, 2 ** 31 - 1)
+        new[0] = 3
+        t = i32(np.full((n, 1), -7))
+        kv_len, cu, position, slot, taken = plan.tables(i32(np.full(n, 2 ** 31 - 1) * (np.arange(n) > 0)), i32(new), i32([4]), t, 8)
+        assert plan.device_status() == (-8, K.STATUS_BAD_INDEX | K.STATUS_NO_PAGES)
+        assert position[:3].tolist() == [0, 1, 2] and slot.tolist() == [64, 65, 66] + [-1] * 5
+        assert cu[:3].tolist() == [0, 3, 2 ** 31 - 1] and int(cu[-1]) == int(kv_len[-1]) == int(taken) == 2 ** 31 - 1
+        assert t.flatten().tolist() == [4] + [-7] * (n - 1)
+
+
 # ------------------------------------------------------------------------------------------ rope
 
 def plain_angles(rot, base=10000.0):
@@ -346,8 +360,9 @@ def test_slots_outside_the_cache():
 
 # ------------------------------------------------------------------------------------------ attention
 
-def attend_case(seed, lens, new, heads, kv, dim, page, dtype, window=0, sinks=0, pad=0, max_new=None, loud=1.0, extra_rows=0):
-    """Runs one call on a cache whose unused bytes are NaN scales and whose unused table entries are no pages."""
+def attend_case(seed, lens, new, heads, kv, dim, page, dtype, window=0, sinks=0, pad=0, max_new=None, loud=1.0, extra_rows=0, absent=()):
+    """Runs one call on a cache whose unused bytes are NaN scales and whose unused table entries are no pages; `absent`:
+    entries (request, column) that name no page although their tokens count."""
     rng = np.random.default_rng(seed)
     n = len(lens)
     held = [-(-x // page) for x in lens]
@@ -365,6 +380,8 @@ def attend_case(seed, lens, new, heads, kv, dim, page, dtype, window=0, sinks=0,
             x[0, :, :, dim // 3] *= 6 * loud
             slots = [int(table[i, j // page]) * page + j % page for j in range(lens[i])]
             ref.store(cache, x[0], x[1], slots, page, 0.05, 0.02)
+    for k, (i, col) in enumerate(absent):
+        table[i, col] = (-1, n_pages, 1 << 30)[k % 3]
     cu = np.concatenate(([0], np.cumsum(new))).astype(np.int32)
     q = strided(rng, int(cu[-1]) + extra_rows, heads, dim, dtype, pad)
     scale = 1.0 / math.sqrt(dim)
@@ -374,7 +391,7 @@ def attend_case(seed, lens, new, heads, kv, dim, page, dtype, window=0, sinks=0,
         out = torch.full(q.shape, 7.0, dtype=dtype, device="cuda")
         got = plan.attention(*args, out=out, **more)
         again = plan.attention(*args, **more)
-        assert plan.device_status() == (0, 0)
+        assert plan.device_status() == ((-8, K.STATUS_BAD_INDEX) if absent else (0, 0))
     assert bool((got[cu[-1]:] == 7).all())
     got, again = got[: cu[-1]], again[: cu[-1]]
     assert torch.equal(got, again), "equal calls give equal bits"
@@ -448,6 +465,81 @@ def test_many_requests():
 def test_prompts(dim, dtype):
     attend_case(6, [70, 40], [70, 33], 4, 2, dim, 16, dtype)
     attend_case(7, [300], [45], 6, 2, dim, 64, dtype, window=50, sinks=4, extra_rows=3)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_prompts_and_tokens_in_one_call(dtype):
+    """Requests of many and of few rows, none, and hints of the largest that are unknown or wrong: kernels differ, results do not."""
+    lens, new = [400, 30, 0, 100, 7], [300, 1, 0, 40, 2]
+    a = attend_case(11, lens, new, 4, 2, 64, 16, dtype)
+    for hint in (0, 1, 40, 1000):
+        b = attend_case(11, lens, new, 4, 2, 64, 16, dtype, max_new=hint)
+        assert (a.float() - b.float()).abs().max() <= 2 * UNIT[dtype] * a.float().abs().max() + 2.0 ** -11
+    attend_case(12, [200, 200], [60, 20], 8, 1, 128, 32, dtype, max_new=40)          # as many tokens as two of 40, but not alike
+    attend_case(13, [64, 64, 64], [20, 20, 20], 8, 2, 80, 16, dtype, pad=1)         # alike, rows on odd addresses
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_prompts_on_long_contexts_are_split(dim, dtype):
+    attend_case(14, [2600], [40], 4, 1, dim, 64, dtype)
+    attend_case(15, [1500, 129], [17, 128], 3, 1, dim, 16, dtype, window=700, sinks=5)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_prompts_longer_than_what_is_cached(dtype):
+    got = attend_case(16, [100, 0, 200], [150, 50, 20], 4, 1, 64, 16, dtype)
+    assert bool((got[:50] == 0).all()) and bool((got[150:200] == 0).all()) and bool((got[50:150] != 0).any())
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_absent_pages(dim, dtype):
+    attend_case(17, [300, 90], [1, 1], 2, 1, dim, 16, dtype, absent=[(0, 3), (1, 0), (0, 18)])
+    attend_case(18, [300, 90], [200, 80], 2, 1, dim, 16, dtype, absent=[(0, 3), (1, 2), (0, 9), (0, 10)])
+    attend_case(19, [300, 260], [100, 100], 2, 1, dim, 128, dtype, absent=[(0, 1), (1, 0)])
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_prompt_rows_that_are_not_finite_stay_alone(dtype):
+    with plan_for(2, 1, 64, 16, dtype, requests=1) as plan:
+        cache = plan.new_cache(10)
+        x = torch.randn(150, 1, 64, device="cuda").to(dtype)
+        plan.append(None, x, x, torch.arange(150, device="cuda"), cache)
+        q = torch.randn(150, 2, 64, device="cuda").to(dtype)
+        args = (i32([0, 150]), i32([150]), i32([list(range(10))]), cache)
+        fine = plan.attention(q, *args)
+        q[70, 1, 3], q[20, 0, 60], q[90, 0, 0] = float("nan"), float("inf"), float("-inf")
+        got = plan.attention(q, *args)
+        odd = torch.zeros(150, 2, dtype=torch.bool, device="cuda")
+        odd[70, 1] = odd[20, 0] = odd[90, 0] = True
+        assert bool(torch.isnan(got[odd]).all()) and torch.equal(got[~odd], fine[~odd])
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("scale", [0.0, -0.3])
+def test_softmax_scales_of_any_sign(dtype, scale):
+    """Scale 0 is the mean of the values; a negative one is the positive one of the negative queries."""
+    with plan_for(2, 1, 64, 16, dtype, requests=1) as plan:
+        cache = plan.new_cache(10)
+        x = torch.randn(150, 1, 64, device="cuda").to(dtype)
+        plan.append(None, x, x, torch.arange(150, device="cuda"), cache)
+        for n in (1, 100):
+            q = torch.randn(n, 2, 64, device="cuda").to(dtype)
+            args = (i32([0, n]), i32([150]), i32([list(range(10))]), cache)
+            got = plan.attention(q, *args, softmax_scale=scale)
+            if scale:
+                assert torch.equal(got, plan.attention(-q, *args, softmax_scale=-scale))
+            else:
+                v = plan.read(cache, torch.arange(150, device="cuda"))[1].double()[:, 0]
+                want = (v.cumsum(0) / torch.arange(1, 151, device="cuda").view(-1, 1))[150 - n:].unsqueeze(1)
+                assert ((got.double() - want).abs() <= v.abs().mean() * 2.0 ** -10 + want.abs() * UNIT[dtype] / 2).all()
 
 
 @gpu
