@@ -2,7 +2,7 @@
 // of more than 128 dimensions; kv_attend.cu has the formula and serves the rest).
 //
 // A CTA works on 256 query rows of one (request, key/value head) - tokens times the query heads that share it, in two
-// tiles of 128 (one for fp32 with W = 128 and for W = 256) - against tiles of 128 keys (64 for W = 256):
+// tiles of 128 (128 rows for fp32 with W = 128 and for W = 256) - against tiles of 128 keys (64 for W = 256):
 //   S_t[128 rows, 128 keys] = Q_t K^T       A, B from shared memory, sums in tensor memory
 //   O_t[128 rows, W]       += P_t V         A = the weights in tensor memory (they take S_t's columns), B from shared memory
 // A code times its scale is exact in f16, so the codes become f16 operands once per CTA and tile: K rows as they lie,
@@ -10,10 +10,13 @@
 // per row and are exact in f16 too; the weights are rounded to f16 (11 bits).  For fp32 both are two f16 parts, high and
 // low, and each part has its products.
 //
-// Roles: two warpgroups of softmax, one thread a row; one warpgroup that converts; one thread that issues products.  The
-// two tiles alternate: while one's weights are computed the other's products run.  A row's scores stay in
-// registers from the search for the largest to the weights; its reference lies kSlack above a score that was once the
-// largest, so O is rescaled a few times per row, not per tile.
+// Roles: two warpgroups of softmax (one for W = 256), one thread a row; one warpgroup that converts; one thread that issues
+// products.  The groups alternate: while one's weights are computed the other's products run.  Each has a tile of rows; for
+// fp32 with W = 128, whose queries leave room for one, both have that and every other tile of its keys (two prompts of
+// 1024 tokens on 4096 keys, 16/4 heads: 212 -> 166 us; the same for bf16 stretches of up to 128 rows loses, 42 -> 55 us
+// with 36 rows on 16000 keys, by the second set of results).  A row's scores stay in registers from the search for the
+// largest to the weights; its reference lies kSlack above a score that was once the largest, so O is rescaled a few times
+// per row, not per tile.
 //
 // Bounds: 2 x 256 x 128 x W multiply-adds of a key tile take 2048 cycles at W = 128; its 32768 exponentials take 2048
 // cycles too on the 16 lanes of the special-function units; conversion 384 issue cycles.
@@ -40,17 +43,18 @@ constexpr float kTop = 14.f;                     // the largest weight is 2^kTop
 // with many short stretches would be last by far
 constexpr int kEntry = 3;
 
-// T: type of queries and outputs; fp32 queries and weights are two f16 parts each, with products for both.  TILES: row tiles
-// of a CTA.  KEYS: keys of a tile
-template <typename T, int W, int TILES, int KEYS>
+// T: type of queries and outputs; fp32 queries and weights are two f16 parts each, with products for both.  GROUPS: softmax
+// warpgroups, each with its own scores and outputs.  TILES: row tiles of a stretch.  KEYS: keys of a tile
+template <typename T, int W, int GROUPS, int TILES, int KEYS>
 struct Shape {
     static constexpr int kParts = sizeof(T) == 4 ? 2 : 1;
-    static constexpr int kRows = TILES * kTileRows;
+    static constexpr int kRows = TILES * kTileRows, kPartRows = GROUPS * kTileRows;      // of a stretch; of a piece's results
     static constexpr int kQPart = kTileRows * W * 2, kQTile = kQPart * kParts;          // bytes
     static constexpr int kKTile = KEYS * W * 2, kVTile = KEYS * W * 2;
     static constexpr int kQAt = 0, kKAt = TILES * kQTile, kVAt = kKAt + 2 * kKTile, kLineAt = kVAt + 2 * kVTile;
-    static constexpr int kS = 0, kO = TILES * 128;            // columns of tensor memory
-    static_assert(kO + TILES * W <= 512 && KEYS <= 128 && kLineAt <= 196608, "");
+    static constexpr int kS = 0, kO = GROUPS * 128;           // columns of tensor memory
+    static constexpr bool kAlternate = TILES < GROUPS;        // the groups share the rows and take every other key tile
+    static_assert((TILES == GROUPS || (TILES == 1 && GROUPS == 2 && kParts == 2)) && kO + GROUPS * W <= 512 && KEYS <= 128 && kLineAt <= 196608, "");
     // conversion: a thread's dimensions of a key; stretches of dimensions of V, one for KEYS/8 threads
     static constexpr int kKeyDims = W * KEYS / 128, kStretches = 1024 / KEYS, kVDims = W / kStretches;
 };
@@ -154,9 +158,9 @@ __device__ __forceinline__ void lds16(uint32_t at, uint32_t (&v)[4]) {
     asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(at) : "memory");
 }
 
-template <typename T, int W, int TILES, int KEYS>
+template <typename T, int W, int GROUPS, int TILES, int KEYS>
 __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a) {
-    using S = Shape<T, W, TILES, KEYS>;
+    using S = Shape<T, W, GROUPS, TILES, KEYS>;
     constexpr bool SPLIT = sizeof(T) == 4;
     // The reference lies this far above a score that was once the largest.  fp32: near, so that exponents are small numbers
     // (an exponent of 8 to 16 is rounded to 2^-20, which its weight feels); 2^kTop is then a factor, not part of the exponent
@@ -169,6 +173,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
     __shared__ uint32_t tmem_slot, absent[4];
     __shared__ long long sum_s[kThreads / 32];
     __shared__ int last_s;
+    __shared__ float f_s[kTileRows];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, group = warp >> 2;
     const uint32_t bar = smem_u32(bars);
     // full and empty of two K stages, of two V stages; scores, weights, output and queries of two tiles
@@ -467,7 +472,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
             const uint64_t q_d = tc::make_kmajor_sw128_desc(smem_u32(smem + S::kQAt)), k_d = tc::make_kmajor_sw128_desc(smem_u32(smem + S::kKAt)),
                            v_d = tc::make_kmajor_sw128_desc(smem_u32(smem + S::kVAt));
             auto scores = [&](int t, int stage) {
-                const uint64_t da = q_d + t * (S::kQTile / 16), db = k_d + stage * (S::kKTile / 16);
+                const uint64_t da = q_d + (S::kAlternate ? 0 : t) * (S::kQTile / 16), db = k_d + stage * (S::kKTile / 16);
                 if (one && !dead) {
 #pragma unroll
                     for (int x = 0; x < S::kParts; ++x)
@@ -498,42 +503,73 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
             for (bool go = begin(p); go; go = next(p)) {
                 if (p.last <= p.first) continue;
                 const int n = __reduce_max_sync(0xffffffffu, min(p.last, p.present) - p.first);        // into a uniform register
-                const int tiles = TILES == 1 ? 1 : __reduce_max_sync(0xffffffffu, p.row1 - p.row0 > kTileRows ? 2 : 1);
-                if (n > 0) {
-                    wait(k_full(it & 1), (it >> 1) & 1);
-                    for (int t = 0; t < tiles; ++t) {
+                if constexpr (S::kAlternate) {
+                    for (int t = 0; t < 2 && t < n; ++t) {
+                        const int x = it + t;
+                        wait(k_full(x & 1), (x >> 1) & 1);
                         wait(p_full(t), (p_phase >> t) & 1u);          // the queries are there
                         p_phase ^= 1u << t;
                         tc::tc_fence_after();
-                        scores(t, it & 1);
+                        scores(t, x & 1);
+                        if (one && !dead) tc::umma_commit(k_empty(x & 1));
+                        __syncwarp();
                     }
-                    if (one && !dead) tc::umma_commit(k_empty(it & 1));
-                    __syncwarp();
-                }
 #pragma unroll 1
-                for (int j = 0; j < n; ++j, ++it) {
-                    const int stage = it & 1, other = stage ^ 1;
-                    wait(v_full(stage), (it >> 1) & 1);
-                    if (j + 1 < n) wait(k_full(other), ((it + 1) >> 1) & 1);
-#pragma unroll
-                    for (int t = 0; t < TILES; ++t) {
-                        if (t >= tiles) continue;
+                    for (int j = 0; j < n; ++j, ++it) {
+                        const int stage = it & 1, t = j & 1;
+                        wait(v_full(stage), (it >> 1) & 1);
                         wait(p_full(t), (p_phase >> t) & 1u);          // the weights are there, the scores are read
                         p_phase ^= 1u << t;
                         tc::tc_fence_after();
-                        outputs(t, stage, j > 0);
-                        if (j + 1 < n) scores(t, other);
+                        outputs(t, stage, j >= 2);
+                        if (one && !dead) tc::umma_commit(v_empty(stage));
+                        __syncwarp();
+                        if (j + 2 < n) {
+                            wait(k_full(stage), ((it + 2) >> 1) & 1);
+                            tc::tc_fence_after();
+                            scores(t, stage);
+                            if (one && !dead) tc::umma_commit(k_empty(stage));
+                            __syncwarp();
+                        }
                     }
-                    if (one && !dead) {
-                        tc::umma_commit(v_empty(stage));
-                        if (j + 1 < n) tc::umma_commit(k_empty(other));
+                } else {
+                    const int tiles = TILES == 1 ? 1 : __reduce_max_sync(0xffffffffu, p.row1 - p.row0 > kTileRows ? 2 : 1);
+                    if (n > 0) {
+                        wait(k_full(it & 1), (it >> 1) & 1);
+                        for (int t = 0; t < tiles; ++t) {
+                            wait(p_full(t), (p_phase >> t) & 1u);          // the queries are there
+                            p_phase ^= 1u << t;
+                            tc::tc_fence_after();
+                            scores(t, it & 1);
+                        }
+                        if (one && !dead) tc::umma_commit(k_empty(it & 1));
+                        __syncwarp();
                     }
-                    __syncwarp();
+#pragma unroll 1
+                    for (int j = 0; j < n; ++j, ++it) {
+                        const int stage = it & 1, other = stage ^ 1;
+                        wait(v_full(stage), (it >> 1) & 1);
+                        if (j + 1 < n) wait(k_full(other), ((it + 1) >> 1) & 1);
+#pragma unroll
+                        for (int t = 0; t < TILES; ++t) {
+                            if (t >= tiles) continue;
+                            wait(p_full(t), (p_phase >> t) & 1u);          // the weights are there, the scores are read
+                            p_phase ^= 1u << t;
+                            tc::tc_fence_after();
+                            outputs(t, stage, j > 0);
+                            if (j + 1 < n) scores(t, other);
+                        }
+                        if (one && !dead) {
+                            tc::umma_commit(v_empty(stage));
+                            if (j + 1 < n) tc::umma_commit(k_empty(other));
+                        }
+                        __syncwarp();
+                    }
                 }
             }
         }
         __syncwarp();
-    } else if (group < TILES) {
+    } else if (group < GROUPS) {
         // ================================================================ softmax: thread = row of tile `group`
         asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
         const int t = group, row_in = tid & 127, wl = (warp & 3) * 32;
@@ -546,12 +582,15 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
             if (p.last <= p.first) continue;
             const int n = min(p.last, p.present) - p.first;
             const int tiles = TILES == 1 || p.row1 - p.row0 <= kTileRows ? 1 : 2;
-            const int row = p.row0 + t * kTileRows + row_in;
+            // alternating groups have all rows and take key tiles t, t + 2, ...; their results are joined as pieces are
+            const int n_t = S::kAlternate ? (n - t + 1) / 2 : t < tiles ? n : 0;
+            const int tile0 = S::kAlternate ? p.row0 : p.row0 + t * kTileRows;
+            const int row = tile0 + row_in;
             const bool real = row < p.row1;
             const int tok = div_g(a, row), pos = real ? p.len - p.nq + tok : -1;
             const int64_t out_row = (int64_t)(p.q0 + tok) * a.H + p.head * a.G + row - tok * a.G;
             float m = kFloor, l = 0.f, f = 0.f;
-            if (t < tiles && n > 0) {
+            if (n_t > 0 && !(S::kAlternate && t == 1)) {
                 // ---- queries into their place, 16 bytes a lane; then a row a thread: a power of two makes it f16 (two parts of
                 // fp32: 16 raw bytes each lie where a chunk of one part will)
                 constexpr int kPerChunk = 16 / (int)sizeof(T), kLanes = W / kPerChunk, kAtOnce = 32 / kLanes;
@@ -614,13 +653,21 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
                     if (SPLIT) sts16(chunk_at(1, row_in, c), lo[0], lo[1], lo[2], lo[3]);
                 }
                 fence_async();
+            }
+            if (S::kAlternate && n > 0) {
+                if (t == 0) f_s[row_in] = f;
+                asm volatile("bar.sync 2, 256;" ::: "memory");
+                if (t == 1) f = f_s[row_in];
+            }
+            if (n_t > 0) {
                 tc::tc_fence_before();
                 __syncwarp();
                 if (lane == 0) tc::mbar_arrive(p_full(t));
 
-                const int p_first = p.len - p.nq + div_g(a, p.row0 + t * kTileRows);
-                const int p_last = p.len - p.nq + div_g(a, min(p.row0 + (t + 1) * kTileRows, p.row1) - 1);
-                for (int j = 0; j < n; ++j) {
+                const int p_first = p.len - p.nq + div_g(a, tile0);
+                const int p_last = p.len - p.nq + div_g(a, min(tile0 + kTileRows, p.row1) - 1);
+                for (int jj = 0; jj < n_t; ++jj) {
+                    const int j = S::kAlternate ? 2 * jj + t : jj;
                     const int u = p.first + j, key0 = (u < p.st ? u : p.wt + u - p.st) * kTileKeys;
                     wait(s_full(t), s_phase);
                     s_phase ^= 1u;
@@ -668,7 +715,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
                     if (__any_sync(0xffffffffu, reach > m)) {       // O follows only when a score passes the reference
                         const float to = fmaxf(m, reach == -INFINITY ? kFloor : reach + kSlack);
                         const float scale = m == to ? 1.f : ex2(m - to);
-                        if (j > 0) {
+                        if (jj > 0) {
                             wait(o_full(t), o_phase ^ 1u);       // the products of the tile before
                             tc::tc_fence_after();
 #pragma unroll 1
@@ -721,28 +768,30 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
                 tc::tc_fence_after();
             }
             it += max(n, 0);
+            // the queries are both groups': their place is free once both have all their scores
+            if (S::kAlternate && n > 0) asm volatile("bar.sync 2, 256;" ::: "memory");
 
             // ---- the rows' outputs, or this piece of them
-            const bool whole = p.first == 0 && p.last == p.units;
+            const bool whole = p.first == 0 && p.last == p.units && !S::kAlternate;
             const int slot = blockIdx.x * 2 + (p.first == 0 ? 1 : 0);
-            if (t < tiles) {
+            if (S::kAlternate || t < tiles) {
                 // the rows go through the queries' place in shared memory (their products are done), so that W/8 lanes store
                 // 2 W bytes of a row: all of its dimensions as bf16, or half of them as fp32
                 constexpr int kLanes = W / 8, kAtOnce = 32 / kLanes, kPass = W / 2;
                 const float k = whole ? (l > 0.f || l != l ? a.v_scale / l : 0.f) : 1.f;
-                const uint32_t place = smem_u32(smem + S::kQAt) + t * S::kQTile;
+                const uint32_t place = smem_u32(smem + S::kQAt) + t * (S::kAlternate ? S::kQPart : S::kQTile);
                 const bool wide = SPLIT || !whole;
                 auto slot16 = [&](int r, int c) { return place + (c / 8) * (kTileRows * 128) + swizzled(wl + r, c % 8); };
                 const int chunk = lane % kLanes;
                 const int64_t to_row = real ? out_row * a.D : -1;
-                float *part = a.prompt_part + ((int64_t)slot * kStretchRows + t * kTileRows + wl) * W;
+                float *part = a.prompt_part + ((int64_t)slot * S::kPartRows + t * kTileRows + wl) * W;
 #pragma unroll 1
                 for (int pass = 0; pass < (wide ? 2 : 1); ++pass) {
                     __syncwarp();
 #pragma unroll 1
                     for (int c = 0; c < (wide ? kPass : W) / 32; ++c) {
                         uint32_t r[32];
-                        if (n > 0) { ld32(o_tmem + pass * kPass + 32 * c, r); tc::tmem_ld_wait(); }
+                        if (n_t > 0) { ld32(o_tmem + pass * kPass + 32 * c, r); tc::tmem_ld_wait(); }
                         else {
 #pragma unroll
                             for (int i = 0; i < 32; ++i) r[i] = 0u;
@@ -774,22 +823,25 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
                     }
                 }
                 __syncwarp();
-                if (!whole && real) a.prompt_ml[(int64_t)slot * kStretchRows + t * kTileRows + row_in] = make_float2(m, l);
+                if (!whole && real) a.prompt_ml[(int64_t)slot * S::kPartRows + t * kTileRows + row_in] = make_float2(m, l);
             }
             tc::tc_fence_before();
             if (!whole) {
                 __threadfence();
-                asm volatile("bar.sync 1, %0;" ::"n"(TILES * 128) : "memory");
+                asm volatile("bar.sync 1, %0;" ::"n"(GROUPS * 128) : "memory");
                 if (tid == 0) {
-                    const int before = atomicAdd(a.prompt_arrived + p.cta0, 1);
-                    last_s = before == p.cta1 - p.cta0;
-                    if (last_s) a.prompt_arrived[p.cta0] = 0;          // ready for the next call
+                    last_s = S::kAlternate && p.cta0 == p.cta1;        // the stretch is this CTA's alone
+                    if (!last_s) {
+                        const int before = atomicAdd(a.prompt_arrived + p.cta0, 1);
+                        last_s = before == p.cta1 - p.cta0;
+                        if (last_s) a.prompt_arrived[p.cta0] = 0;      // ready for the next call
+                    }
                 }
-                asm volatile("bar.sync 1, %0;" ::"n"(TILES * 128) : "memory");
+                asm volatile("bar.sync 1, %0;" ::"n"(GROUPS * 128) : "memory");
                 if (last_s) {
                     __threadfence();
                     // a warp takes every kWarps-th row, a lane W/32 neighbouring dimensions: whole lines, several rows in flight
-                    constexpr int kPer = W / 32, kRowsAtOnce = W == 256 ? 4 : 8, kWarps = 4 * TILES;
+                    constexpr int kPer = W / 32, kRowsAtOnce = W == 256 ? 4 : 8, kWarps = 4 * GROUPS;
                     const int rows = p.row1 - p.row0;
 #pragma unroll 1
                     for (int x0 = warp; x0 < rows; x0 += kWarps * kRowsAtOnce) {
@@ -800,9 +852,11 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
 #pragma unroll
                             for (int e = 0; e < kPer; ++e) v[y][e] = 0.f;
                         }
+                        constexpr int kOf = S::kAlternate ? 2 : 1;             // results of a piece
 #pragma unroll 1
-                        for (int b = p.cta0; b <= p.cta1; ++b) {
-                            const int64_t at_piece = (int64_t)(b * 2 + (b == p.cta0)) * kStretchRows;
+                        for (int h = p.cta0 * kOf; h < (p.cta1 + 1) * kOf; ++h) {
+                            const int b = h / kOf;
+                            const int64_t at_piece = (int64_t)(b * 2 + (b == p.cta0)) * S::kPartRows + h % kOf * kTileRows;
                             float2 ml[kRowsAtOnce];
                             float d[kRowsAtOnce][kPer];
 #pragma unroll
@@ -845,7 +899,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
                         }
                     }
                 }
-                asm volatile("bar.sync 1, %0;" ::"n"(TILES * 128) : "memory");       // last_s is the next piece's
+                asm volatile("bar.sync 1, %0;" ::"n"(GROUPS * 128) : "memory");       // last_s is the next piece's
             }
         }
     }
@@ -855,10 +909,10 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
     if (warp == 12) tc::tmem_dealloc(tmem_slot, 512);
 }
 
-template <typename T, int W, int TILES, int KEYS>
+template <typename T, int W, int GROUPS, int TILES, int KEYS>
 cudaError_t launch(const AttendArgs &a, int sm_count, cudaStream_t s, uint64_t *launches) {
-    using S = Shape<T, W, TILES, KEYS>;
-    auto k = attend_prompt_kernel<T, W, TILES, KEYS>;
+    using S = Shape<T, W, GROUPS, TILES, KEYS>;
+    auto k = attend_prompt_kernel<T, W, GROUPS, TILES, KEYS>;
     static std::atomic<bool> ready[64];
     int dev = 0;
     cudaError_t err = cudaGetDevice(&dev);
@@ -883,9 +937,9 @@ bool prompt_supported(int dtype, int head_dim) { return dtype == MOE_BF16 || hea
 cudaError_t launch_attend_prompt(const AttendArgs &a, int sm_count, cudaStream_t s, uint64_t *launches) {
     const int w = padded_width(a.D);
     if (a.dtype == MOE_BF16)
-        return w == 64 ? launch<__nv_bfloat16, 64, 2, 128>(a, sm_count, s, launches) : w == 128 ? launch<__nv_bfloat16, 128, 2, 128>(a, sm_count, s, launches)
-                                                                                              : launch<__nv_bfloat16, 256, 1, 64>(a, sm_count, s, launches);
-    return w == 64 ? launch<float, 64, 2, 128>(a, sm_count, s, launches) : launch<float, 128, 1, 128>(a, sm_count, s, launches);
+        return w == 64 ? launch<__nv_bfloat16, 64, 2, 2, 128>(a, sm_count, s, launches) : w == 128 ? launch<__nv_bfloat16, 128, 2, 2, 128>(a, sm_count, s, launches)
+                                                                                              : launch<__nv_bfloat16, 256, 1, 1, 64>(a, sm_count, s, launches);
+    return w == 64 ? launch<float, 64, 2, 2, 128>(a, sm_count, s, launches) : launch<float, 128, 2, 1, 128>(a, sm_count, s, launches);
 }
 
 }  // namespace kv
