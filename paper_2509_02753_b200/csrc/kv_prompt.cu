@@ -40,8 +40,9 @@ constexpr int kThreads = 512;
 constexpr float kFloor = -FLT_MAX;
 constexpr float kTop = 14.f;                     // the largest weight is 2^kTop, as in kv_attend.cu
 // What a stretch costs besides its tiles (queries, output, an empty pipeline), in tiles: counted in the line, or a CTA
-// with many short stretches would be last by far
-constexpr int kEntry = 3;
+// with many short stretches would be last by far.  Alternating groups pass a tile in about half the time (with 5 for 3
+// there: 333 to 700 tokens of 15/5 heads 52 -> 49 us, 64 tokens on 16000 keys of 16/4 heads 83 -> 77)
+constexpr int kEntryTiles = 3, kEntryAlternate = 5;
 
 // T: type of queries and outputs; fp32 queries and weights are two f16 parts each, with products for both.  GROUPS: softmax
 // warpgroups, each with its own scores and outputs.  TILES: row tiles of a stretch.  KEYS: keys of a tile
@@ -165,6 +166,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
     // The reference lies this far above a score that was once the largest.  fp32: near, so that exponents are small numbers
     // (an exponent of 8 to 16 is rounded to 2^-20, which its weight feels); 2^kTop is then a factor, not part of the exponent
     constexpr float kSlack = SPLIT ? 2.f : 8.f;
+    constexpr int kEntry = S::kAlternate ? kEntryAlternate : kEntryTiles;
     constexpr int kTileKeys = KEYS, kTileBlocks = KEYS / kBlockTokens, kStretchRows = S::kRows;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
