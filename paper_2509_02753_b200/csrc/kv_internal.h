@@ -104,7 +104,6 @@ __device__ __forceinline__ int div_g(const AttendArgs &a, int row) { return (int
 cudaError_t launch_attend_rows(const AttendArgs &a, int sm_count, cudaStream_t s, uint64_t *launches);
 size_t attend_part_floats(int w);          // per CTA of the grid
 // prompts, on tcgen05 (kv_prompt.cu)
-bool prompt_supported(int dtype, int head_dim);
 cudaError_t launch_attend_prompt(const AttendArgs &a, int sm_count, cudaStream_t s, uint64_t *launches);
 size_t prompt_part_floats(int w);          // per CTA, of which there is one per SM
 size_t prompt_part_rows();

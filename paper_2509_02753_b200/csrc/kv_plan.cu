@@ -92,10 +92,9 @@ int moe_kv_plan_create(const moe_kv_config_t *cfg, moe_kv_plan_t **out) {
     const size_t part = (size_t)p->max_ctas * attend_part_floats(padded_width(cfg->head_dim)) * sizeof(float);
     const size_t ml = (size_t)p->max_ctas * 2 * kPartRows * sizeof(float2);
     const size_t arrived = ((size_t)p->max_ctas * sizeof(int32_t) + 255) & ~size_t(255);
-    // prompts: pieces of 256 rows, two for each SM
-    const bool prompts = prompt_supported(cfg->dtype, cfg->head_dim);
-    const size_t ppart = prompts ? (size_t)sms * prompt_part_floats(padded_width(cfg->head_dim)) * sizeof(float) : 0;
-    const size_t pml = prompts ? (size_t)sms * prompt_part_rows() * sizeof(float2) : 0;
+    // prompts: two pieces for each SM, whose grid that is
+    const size_t ppart = (size_t)sms * prompt_part_floats(padded_width(cfg->head_dim)) * sizeof(float);
+    const size_t pml = (size_t)sms * prompt_part_rows() * sizeof(float2);
     const size_t parrived = ((size_t)sms * sizeof(int32_t) + 255) & ~size_t(255);
     p->bytes = part + ml + ppart + pml + arrived + parrived + 256;
     void *mem = nullptr;
@@ -256,14 +255,15 @@ int moe_kv_attention(moe_kv_plan_t *p, const moe_kv_rows_t *q, int32_t T, const 
     cudaStream_t s = (cudaStream_t)stream;
     // Which kernel.  One pass over the keys serves 32 rows in kv_attend.cu (16 of wide heads); more rows read them again
     // there, while kv_prompt.cu has tiles of 128.  Measured at 8 key/value heads of 128 dimensions, 36 rows each: 16 requests
-    // of 2000 keys 69 us there, 55 here; 64 dimensions 46 and 41; 256 dimensions, 36 rows 95 and 102, 64 rows 117 and 106.
+    // of 2000 keys 69 us there, 55 here; 64 dimensions 46 and 41; 256 dimensions, 36 rows 95 and 102, 64 rows 117 and 106;
+    // in fp32, 68 rows, 241 and 156, and one request of 16000 keys 121 and 123.
     // While all of its work is about one step of every warp kv_attend.cu is faster whatever the rows (one request of 500
     // keys, 256 rows: 22 us and 31).
     const int most = max_new > 0 && max_new < T ? max_new : T;
     const long long rows = (long long)most * a.G, strips = (rows + kPassRows - 1) / kPassRows * n * a.Hk;
     const bool one_step = strips * (((long long)width * c.page_size + kBlockTokens - 1) / kBlockTokens) <= 32ll * p->sm_count;
     const int limit = padded_width(c.head_dim) == 256 ? 2 * kPassRows : kPassRows;
-    if (!prompt_supported(c.dtype, c.head_dim) || rows <= limit || one_step) return done(launch_attend_rows(a, p->sm_count, s, &p->launches));
+    if (rows <= limit || one_step) return done(launch_attend_rows(a, p->sm_count, s, &p->launches));
     // requests of one size, whichever it is, all go to the one kernel; otherwise each to its own
     const bool alike = (long long)n * most == T;
     a.prompt_rows = alike ? 0 : limit;

@@ -1,8 +1,10 @@
-// Attention of prompts over the 4-bit cache: many query rows of a request, on the tcgen05 tensor cores (all but fp32 heads
-// of more than 128 dimensions; kv_attend.cu has the formula and serves the rest).
+// Attention of prompts over the 4-bit cache: many query rows of a request, on the tcgen05 tensor cores (kv_attend.cu has
+// the formula and serves few rows).
 //
 // A CTA works on 256 query rows of one (request, key/value head) - tokens times the query heads that share it, in two
-// tiles of 128 (128 rows for fp32 with W = 128 and for W = 256) - against tiles of 128 keys (64 for W = 256):
+// tiles of 128 (128 rows for fp32 with W = 128 and for W = 256) - against tiles of 128 keys (64 for W = 256,
+// in one stage instead of two for fp32, whose queries take 128 KB: two prompts of 1024 tokens on 4096 keys, 16/4 heads,
+// 426 us; 1163 in kv_attend.cu):
 //   S_t[128 rows, 128 keys] = Q_t K^T       A, B from shared memory, sums in tensor memory
 //   O_t[128 rows, W]       += P_t V         A = the weights in tensor memory (they take S_t's columns), B from shared memory
 // A code times its scale is exact in f16, so the codes become f16 operands once per CTA and tile: K rows as they lie,
@@ -52,10 +54,16 @@ struct Shape {
     static constexpr int kRows = TILES * kTileRows, kPartRows = GROUPS * kTileRows;      // of a stretch; of a piece's results
     static constexpr int kQPart = kTileRows * W * 2, kQTile = kQPart * kParts;          // bytes
     static constexpr int kKTile = KEYS * W * 2, kVTile = KEYS * W * 2;
-    static constexpr int kQAt = 0, kKAt = TILES * kQTile, kVAt = kKAt + 2 * kKTile, kLineAt = kVAt + 2 * kVTile;
+    static constexpr int kQAt = 0, kKAt = TILES * kQTile;
+    static constexpr int kStages = kKAt + 2 * (kKTile + kVTile) <= 196608 ? 2 : 1;       // of keys, of values
+    static constexpr int kVAt = kKAt + kStages * kKTile, kLineAt = kVAt + kStages * kVTile;
     static constexpr int kS = 0, kO = GROUPS * 128;           // columns of tensor memory
     static constexpr bool kAlternate = TILES < GROUPS;        // the groups share the rows and take every other key tile
     static_assert((TILES == GROUPS || (TILES == 1 && GROUPS == 2 && kParts == 2)) && kO + GROUPS * W <= 512 && KEYS <= 128 && kLineAt <= 196608, "");
+    static_assert(!kAlternate || kStages == 2, "");
+    // of the x-th key tile: its stage, and the parity of the stage's use
+    static __device__ __forceinline__ int stage(int x) { return x & (kStages - 1); }
+    static __device__ __forceinline__ uint32_t turn(int x) { return (uint32_t)(x >> (kStages - 1)) & 1u; }
     // conversion: a thread's dimensions of a key; stretches of dimensions of V, one for KEYS/8 threads
     static constexpr int kKeyDims = W * KEYS / 128, kStretches = 1024 / KEYS, kVDims = W / kStretches;
 };
@@ -385,8 +393,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
             fetch_keys(kb);
             fetch_values(vb);
             for (int j = 0; j < n; ++j, ++it) {
-                const int stage = it & 1;
-                const uint32_t parity = ((it >> 1) & 1) ^ 1;
+                const int stage = S::stage(it);
+                const uint32_t parity = S::turn(it) ^ 1u;
                 const int kb_now = kb;
                 const int key0 = tile_of(j) * kTileKeys;
                 kb = kb2; vb = vb2;
@@ -508,18 +516,18 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
                 if constexpr (S::kAlternate) {
                     for (int t = 0; t < 2 && t < n; ++t) {
                         const int x = it + t;
-                        wait(k_full(x & 1), (x >> 1) & 1);
+                        wait(k_full(S::stage(x)), S::turn(x));
                         wait(p_full(t), (p_phase >> t) & 1u);          // the queries are there
                         p_phase ^= 1u << t;
                         tc::tc_fence_after();
-                        scores(t, x & 1);
-                        if (one && !dead) tc::umma_commit(k_empty(x & 1));
+                        scores(t, S::stage(x));
+                        if (one && !dead) tc::umma_commit(k_empty(S::stage(x)));
                         __syncwarp();
                     }
 #pragma unroll 1
                     for (int j = 0; j < n; ++j, ++it) {
-                        const int stage = it & 1, t = j & 1;
-                        wait(v_full(stage), (it >> 1) & 1);
+                        const int stage = S::stage(it), t = j & 1;
+                        wait(v_full(stage), S::turn(it));
                         wait(p_full(t), (p_phase >> t) & 1u);          // the weights are there, the scores are read
                         p_phase ^= 1u << t;
                         tc::tc_fence_after();
@@ -527,7 +535,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
                         if (one && !dead) tc::umma_commit(v_empty(stage));
                         __syncwarp();
                         if (j + 2 < n) {
-                            wait(k_full(stage), ((it + 2) >> 1) & 1);
+                            wait(k_full(stage), S::turn(it + 2));
                             tc::tc_fence_after();
                             scores(t, stage);
                             if (one && !dead) tc::umma_commit(k_empty(stage));
@@ -537,21 +545,21 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
                 } else {
                     const int tiles = TILES == 1 ? 1 : __reduce_max_sync(0xffffffffu, p.row1 - p.row0 > kTileRows ? 2 : 1);
                     if (n > 0) {
-                        wait(k_full(it & 1), (it >> 1) & 1);
+                        wait(k_full(S::stage(it)), S::turn(it));
                         for (int t = 0; t < tiles; ++t) {
                             wait(p_full(t), (p_phase >> t) & 1u);          // the queries are there
                             p_phase ^= 1u << t;
                             tc::tc_fence_after();
-                            scores(t, it & 1);
+                            scores(t, S::stage(it));
                         }
-                        if (one && !dead) tc::umma_commit(k_empty(it & 1));
+                        if (one && !dead) tc::umma_commit(k_empty(S::stage(it)));
                         __syncwarp();
                     }
 #pragma unroll 1
                     for (int j = 0; j < n; ++j, ++it) {
-                        const int stage = it & 1, other = stage ^ 1;
-                        wait(v_full(stage), (it >> 1) & 1);
-                        if (j + 1 < n) wait(k_full(other), ((it + 1) >> 1) & 1);
+                        const int stage = S::stage(it), other = S::stage(it + 1);
+                        wait(v_full(stage), S::turn(it));
+                        if (j + 1 < n) wait(k_full(other), S::turn(it + 1));
 #pragma unroll
                         for (int t = 0; t < TILES; ++t) {
                             if (t >= tiles) continue;
@@ -595,15 +603,16 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
             if (n_t > 0 && !(S::kAlternate && t == 1)) {
                 // ---- queries into their place, 16 bytes a lane; then a row a thread: a power of two makes it f16 (two parts of
                 // fp32: 16 raw bytes each lie where a chunk of one part will)
-                constexpr int kPerChunk = 16 / (int)sizeof(T), kLanes = W / kPerChunk, kAtOnce = 32 / kLanes;
+                constexpr int kPerChunk = 16 / (int)sizeof(T), kChunks = W / kPerChunk, kLanes = kChunks < 32 ? kChunks : 32, kAtOnce = 32 / kLanes,
+                              kTurns = kChunks / kLanes;
                 const bool vec = (reinterpret_cast<uintptr_t>(a.q.p) & 15u) == 0 && ((a.q.ts | a.q.hs) & (kPerChunk - 1)) == 0;
                 const int64_t q_row = real ? (int64_t)(p.q0 + tok) * a.q.ts + (int64_t)(p.head * a.G + row - tok * a.G) * a.q.hs : INT64_MIN;
-                const int chunk = lane % kLanes;
                 const uint32_t place = smem_u32(smem + S::kQAt) + t * S::kQTile;
                 auto chunk_at = [&](int part, int r, int c) { return place + part * S::kQPart + (c / 8) * (kTileRows * 128) + swizzled(r, c % 8); };
 #pragma unroll 4
-                for (int x = 0; x < 32 / kAtOnce; ++x) {
-                    const int r = x * kAtOnce + lane / kLanes;             // of the warp's 32 rows
+                for (int x = 0; x < 32 / kAtOnce * kTurns; ++x) {
+                    const int r = x / kTurns * kAtOnce + lane / kLanes;    // of the warp's 32 rows
+                    const int chunk = x % kTurns * kLanes + lane % kLanes;
                     const int64_t at_row = __shfl_sync(0xffffffffu, q_row, r);
                     const uint32_t to = SPLIT ? chunk_at(chunk & 1, wl + r, chunk >> 1) : chunk_at(0, wl + r, chunk);
                     const T *src = (const T *)a.q.p + at_row + kPerChunk * chunk;
@@ -933,15 +942,14 @@ cudaError_t launch(const AttendArgs &a, int sm_count, cudaStream_t s, uint64_t *
 
 size_t prompt_part_floats(int w) { return (size_t)2 * (w == 256 ? 128 : 256) * w; }
 size_t prompt_part_rows() { return 2 * 256; }
-// fp32 heads of more than 128 dimensions would need 256 KB of shared memory
-bool prompt_supported(int dtype, int head_dim) { return dtype == MOE_BF16 || head_dim <= 128; }
 
 cudaError_t launch_attend_prompt(const AttendArgs &a, int sm_count, cudaStream_t s, uint64_t *launches) {
     const int w = padded_width(a.D);
     if (a.dtype == MOE_BF16)
         return w == 64 ? launch<__nv_bfloat16, 64, 2, 2, 128>(a, sm_count, s, launches) : w == 128 ? launch<__nv_bfloat16, 128, 2, 2, 128>(a, sm_count, s, launches)
                                                                                               : launch<__nv_bfloat16, 256, 1, 1, 64>(a, sm_count, s, launches);
-    return w == 64 ? launch<float, 64, 2, 2, 128>(a, sm_count, s, launches) : launch<float, 128, 2, 1, 128>(a, sm_count, s, launches);
+    return w == 64 ? launch<float, 64, 2, 2, 128>(a, sm_count, s, launches) : w == 128 ? launch<float, 128, 2, 1, 128>(a, sm_count, s, launches)
+                                                                                       : launch<float, 256, 1, 1, 64>(a, sm_count, s, launches);
 }
 
 }  // namespace kv
