@@ -360,13 +360,13 @@ def test_slots_outside_the_cache():
 
 # ------------------------------------------------------------------------------------------ attention
 
-def attend_case(seed, lens, new, heads, kv, dim, page, dtype, window=0, sinks=0, pad=0, max_new=None, loud=1.0, extra_rows=0, absent=()):
+def attend_case(seed, lens, new, heads, kv, dim, page, dtype, window=0, sinks=0, pad=0, max_new=None, loud=1.0, extra_rows=0, absent=(), columns=0):
     """Runs one call on a cache whose unused bytes are NaN scales and whose unused table entries are no pages; `absent`:
-    entries (request, column) that name no page although their tokens count."""
+    entries (request, column) that name no page although their tokens count; `columns`: the table's, at least."""
     rng = np.random.default_rng(seed)
     n = len(lens)
     held = [-(-x // page) for x in lens]
-    n_pages, width = sum(held) + 2, max(held + [1]) + 1
+    n_pages, width = sum(held) + 2, max(max(held + [1]) + 1, columns)
     order = rng.permutation(n_pages)
     table = np.full((n, width), 1 << 30)
     at = 0
@@ -540,6 +540,68 @@ def test_softmax_scales_of_any_sign(dtype, scale):
                 v = plan.read(cache, torch.arange(150, device="cuda"))[1].double()[:, 0]
                 want = (v.cumsum(0) / torch.arange(1, 151, device="cuda").view(-1, 1))[150 - n:].unsqueeze(1)
                 assert ((got.double() - want).abs() <= v.abs().mean() * 2.0 ** -10 + want.abs() * UNIT[dtype] / 2).all()
+
+
+# A table with room for a long context takes prompts to tiles of 128 rows, however short they are.
+LONG = 5000
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("dim", [8, 64, 80, 128, 136, 256])
+def test_prompts_in_tiles(dim, dtype):
+    attend_case(31, [70, 40], [70, 33], 4, 2, dim, 16, dtype, columns=LONG)
+    attend_case(32, [300], [45], 6, 2, dim, 64, dtype, window=50, sinks=4, extra_rows=3, columns=LONG)
+    attend_case(33, [129, 0, 257], [65, 60, 130], 2, 1, dim, 16, dtype, pad=1, columns=LONG)
+    attend_case(34, [100, 200], [150, 80], 3, 1, dim, 128, dtype, window=1, columns=LONG)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_prompts_in_tiles_on_long_contexts(dim, dtype):
+    attend_case(35, [2600], [40], 4, 1, dim, 64, dtype, columns=LONG)
+    attend_case(36, [1500, 129], [37, 128], 3, 1, dim, 16, dtype, window=700, sinks=5, columns=LONG)
+    attend_case(37, [640, 33, 900], [300, 1, 70], 2, 2, dim, 32, dtype, sinks=200, window=300, columns=LONG)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_absent_pages_under_tiles(dim, dtype):
+    attend_case(38, [300, 90], [200, 80], 2, 1, dim, 16, dtype, absent=[(0, 3), (1, 2), (0, 9), (0, 10)], columns=LONG)
+    attend_case(39, [600, 260], [100, 100], 2, 1, dim, 128, dtype, absent=[(0, 1), (1, 0)], columns=LONG)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_requests_of_many_and_few_rows_in_tiles(dtype):
+    lens, new = [400, 30, 0, 100, 7], [300, 1, 0, 40, 2]
+    for hint in (300, 0, 1):
+        attend_case(40, lens, new, 4, 2, 128, 16, dtype, max_new=hint, columns=LONG)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_rows_in_tiles_that_are_not_finite_and_scales_of_any_sign(dim, dtype):
+    with plan_for(2, 1, dim, 16, dtype, requests=1) as plan:
+        cache = plan.new_cache(10)
+        x = torch.randn(150, 1, dim, device="cuda").to(dtype)
+        plan.append(None, x, x, torch.arange(150, device="cuda"), cache)
+        q = torch.randn(150, 2, dim, device="cuda").to(dtype)
+        args = (i32([0, 150]), i32([150]), i32([list(range(10)) + [0] * LONG]), cache)
+        assert torch.equal(plan.attention(q, *args, softmax_scale=-0.3), plan.attention(-q, *args, softmax_scale=0.3))
+        v = plan.read(cache, torch.arange(150, device="cuda"))[1].double()[:, 0]
+        want = (v.cumsum(0) / torch.arange(1, 151, device="cuda").view(-1, 1)).unsqueeze(1)
+        got = plan.attention(q, *args, softmax_scale=0.0).double()
+        assert ((got - want).abs() <= v.abs().mean() * 2.0 ** -10 + want.abs() * UNIT[dtype] / 2).all()
+        fine = plan.attention(q, *args)
+        q[70, 1, 3], q[20, 0, dim - 4], q[90, 0, 0] = float("nan"), float("inf"), float("-inf")
+        got = plan.attention(q, *args)
+        odd = torch.zeros(150, 2, dtype=torch.bool, device="cuda")
+        odd[70, 1] = odd[20, 0] = odd[90, 0] = True
+        assert bool(torch.isnan(got[odd]).all()) and torch.equal(got[~odd], fine[~odd])
 
 
 @gpu
