@@ -165,6 +165,7 @@ __device__ __forceinline__ void turn_unit(const T *x, int64_t xhs, T *y, int64_t
         const bool turner = unit < turning;
         const int d0 = WALK == kPairs ? 16 * unit : turner ? 8 * unit : tn.rot + 16 * (unit - turning);
         const int d1 = WALK == kHalves && turner ? half + d0 : d0 + 8;
+        const int pairs = WALK == kPairs ? half - d0 / 2 : 8;          // of the unit's 8, those in front of rope_dim
         // rows are asked for before the angles, which wait for the position
         float a[8], b[8];
         load8<true>(x + d0, 8, a);
@@ -176,8 +177,10 @@ __device__ __forceinline__ void turn_unit(const T *x, int64_t xhs, T *y, int64_t
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     if (WALK == kHalves) turn(a[i], b[i], cs[i]);
-                    else if (i < 4) turn(a[2 * i], a[2 * i + 1], cs[i]);
-                    else turn(b[2 * i - 8], b[2 * i - 7], cs[i]);
+                    else if (i < pairs) {          // by (1, 0) is not the same: an infinity times 0 is no number
+                        if (i < 4) turn(a[2 * i], a[2 * i + 1], cs[i]);
+                        else turn(b[2 * i - 8], b[2 * i - 7], cs[i]);
+                    }
                 }
             }
             store8<true>(y + h * yhs + d0, 8, a);

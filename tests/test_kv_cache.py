@@ -270,6 +270,35 @@ def test_rope_outside_the_table():
         assert plan.device_status() == (-8, K.STATUS_BAD_INDEX)
 
 
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("layout", ["half", "pairs"])
+@pytest.mark.parametrize("dim, rot, pad", [(96, 24, 0), (96, 24, 1), (80, 20, 8), (80, 20, 3), (40, 2, 0), (128, 64, 0), (128, 34, 8)])
+def test_numbers_that_are_not_finite_keep_to_their_pair(dim, rot, pad, layout, dtype):
+    """An infinity or a NaN reaches what it turns with and nothing else; what lies behind rope_dim passes, a -0 too, in every walk."""
+    rng = np.random.default_rng(dim + rot)
+    x = strided(rng, 6, 4, dim, dtype, pad)
+    x[0, :, rot], x[1, :, rot + 1], x[2, :, rot + 2], x[3, :, rot:] = float("inf"), float("-inf"), float("nan"), -0.0
+    x[4, :, 0], x[5, :, rot - 1] = float("inf"), float("nan")
+    pos = np.array([3, 0, 7, 4, 9, 8], np.int32)
+    turns = K.rope_table(rot, 10)
+    with plan_for(4, 1, dim, dtype=dtype, page=16) as plan, np.errstate(invalid="ignore"):
+        for inverse in (False, True):
+            want = torch.from_numpy(ref.rotate(host(x).astype(np.float32), pos, turns.cpu().numpy(), rot, layout, inverse)).to(dtype)
+            y = [plan.rope(x, i32(pos), turns, layout=layout, inverse=inverse), plan.rope(x, i32(pos), turns, layout=layout, inverse=inverse, out=x.clone())]
+            there = torch.zeros_like(x).copy_(x)
+            y.append(plan.rope(there, i32(pos), turns, layout=layout, inverse=inverse, out=there))
+            if not inverse:
+                k = torch.zeros(6, 1, dim, dtype=dtype, device="cuda")
+                y.append(plan.append(x, k, k, dev(np.arange(6)), plan.new_cache(1), positions=i32(pos), turns=turns, layout=layout))
+            for got in y:
+                got = got.cpu()
+                assert torch.equal(torch.isnan(got), torch.isnan(want))
+                assert torch.equal(torch.nan_to_num(got, nan=0.0, posinf=9.0, neginf=-9.0), torch.nan_to_num(want, nan=0.0, posinf=9.0, neginf=-9.0))
+                assert torch.equal(torch.signbit(got)[~torch.isnan(want)], torch.signbit(want)[~torch.isnan(want)])
+        assert plan.device_status() == (0, 0)
+
+
 # ------------------------------------------------------------------------------------------ append and read
 
 @gpu
