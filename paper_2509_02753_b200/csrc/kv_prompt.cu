@@ -338,14 +338,17 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
         for (bool more = begin(p); more; more = next(p)) {
             if (p.last <= p.first) continue;
             const int32_t *table = a.table + (int64_t)p.req * a.width;
-            const int blocks = (p.len + kBlockTokens - 1) / kBlockTokens;
+            // Of a tile's blocks those that some row of the stretch sees: a tile reaches in front of the window and behind the first
+            // tokens, and what lies there may be gone from the table
+            const int blocks = (p.len + kBlockTokens - 1) / kBlockTokens, sink_blocks = a.sinks / kBlockTokens + (a.sinks % kBlockTokens > 0);
+            const int window_block = a.window > 0 ? max(p.len - p.nq + div_g(a, p.row0) - a.window + 1, 0) / kBlockTokens : 0;
             const int n = min(p.last, p.present) - p.first;
             auto tile_of = [&](int j) { const int u = p.first + j; return u < p.st ? u : p.wt + u - p.st; };
-            // cache block of this thread's key (value) share of the j-th tile; -1: absent, -2: behind the cached tokens
+            // cache block of this thread's key (value) share of the j-th tile; -1: absent, -2: seen by no row
             auto find = [&](int j, int in) -> int {
                 if (j >= n) return -2;
                 const int b = tile_of(j) * kTileBlocks + in;
-                if (b >= blocks) return -2;
+                if (b >= blocks || (b < window_block && b >= sink_blocks)) return -2;
                 const int pg = table[b >> a.page_shift];
                 if (pg < 0 || pg >= a.n_pages) { atomicOr(a.status, MOE_KV_STATUS_BAD_INDEX); return -1; }
                 return ((pg * a.Hk + p.head) << a.page_shift) + (b & ((1 << a.page_shift) - 1));

@@ -604,6 +604,42 @@ def test_absent_pages_under_tiles(dim, dtype):
 
 @gpu
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("page, columns", [(16, 0), (16, LONG), (64, LONG), (128, LONG)])
+def test_pages_behind_the_window_may_be_gone(page, columns, dim, dtype):
+    """A serving loop gives back the pages that no row sees any more: neither the outputs nor the status word tell."""
+    rng = np.random.default_rng(page + dim)
+    lens, new = [700, 1000, 300], [40, 70, 1]
+    width = max(-(-max(lens) // page) + 1, columns)
+    for window, sinks in ((100, 0), (57, 4), (1, 0), (300, 129)):
+        pages = rng.permutation(sum(-(-n // page) for n in lens))
+        table, gone, at = np.full((3, width), -1), np.full((3, width), -1), 0
+        for i, n in enumerate(lens):
+            held = -(-n // page)
+            table[i, :held] = pages[at: at + held]
+            at += held
+            first = max(n - new[i] - window + 1, 0)          # what the first new row sees
+            for col in range(held):
+                if (col + 1) * page > first or col * page < sinks:
+                    gone[i, col] = table[i, col]
+        assert (gone != table).any()
+        with plan_for(4, 2, dim, page, dtype, requests=3) as plan:
+            cache = plan.new_cache(len(pages))
+            for i, n in enumerate(lens):
+                x = torch.from_numpy(rng.standard_normal((2, n, 2, dim)).astype(np.float32)).to(dtype).cuda()
+                plan.append(None, x[0], x[1], dev(np.array([table[i, j // page] * page + j % page for j in range(n)], np.int64)), cache, k_scale=0.05, v_scale=0.05)
+            q = torch.from_numpy(rng.standard_normal((sum(new), 4, dim)).astype(np.float32)).to(dtype).cuda()
+            args = (q, i32(np.cumsum([0] + new)), i32(lens))
+            more = dict(max_new=max(new), window=window, sinks=sinks, k_scale=0.05, v_scale=0.05)
+            want = plan.attention(*args, i32(table), cache, **more)
+            assert plan.device_status() == (0, 0)
+            got = plan.attention(*args, i32(gone), cache, **more)
+            assert plan.device_status() == (0, 0)
+            assert torch.equal(got, want) and bool(torch.isfinite(got).all())
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
 def test_requests_of_many_and_few_rows_in_tiles(dtype):
     lens, new = [400, 30, 0, 100, 7], [300, 1, 0, 40, 2]
     for hint in (300, 0, 1):
