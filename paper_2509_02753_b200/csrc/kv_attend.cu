@@ -26,6 +26,7 @@
 
 #include "kv_codes.cuh"
 #include "kv_internal.h"
+#include "kv_ring.cuh"
 #include "tc_ptx.cuh"
 
 namespace lexi {
@@ -244,8 +245,7 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
     // even: pieces blockIdx.x, + gridDim.x, ...; else blocks [at, end) of the line
     long long at = even ? (long long)blockIdx.x : share * blockIdx.x;
     const long long end = even ? total : min(at + share, total);
-    uint32_t phase = 0;          // one bit for each stage of this warp
-    bool dead = false;
+    RingWaits<S::kStages> waits;          // of this warp's ring
 
     int req = 0, len = 0, q0 = 0, nq = 0, sb = 0, wb = 0, nb = 0, row0 = 0, row1 = 0, units = 0, head = -1;
     long long place = 0;         // where the stretch begins (even: its first piece)
@@ -364,7 +364,7 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
             if ((lane >> 1) == (d & 15) && blk >= 0)
                 bulk_load(my_ring + stage * S::kStageBytes + (lane & 1) * block_bytes(W), a.cache + (int64_t)blk * block_bytes(W), block_bytes(W), bar);
         };
-        for (int k = 0; k < S::kStages && k < mine && !dead; ++k) issue(k, k);
+        for (int k = 0; k < S::kStages && k < mine && !waits.dead; ++k) issue(k, k);
 
         // ---- queries as operand fragments: [N tile][two k16 steps][lane] 16 bytes
 #pragma unroll
@@ -435,9 +435,7 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
             }
             const int stage = k % S::kStages;
             // a copy that never ends: nothing more is waited for, the status word tells
-            dead = !__all_sync(0xffffffffu, tc::mbar_wait(my_bar + 8 * stage, (phase >> stage) & 1u, a.status));
-            if (dead) break;
-            phase ^= 1u << stage;
+            if (!waits.arrived(k, mine, [&](int of, uint32_t parity) { return (bool)__all_sync(0xffffffffu, tc::mbar_wait(my_bar + 8 * of, parity, a.status)); })) break;
             const uint8_t *buf = my_ring_p + stage * S::kStageBytes;
             const int u0 = first + (warp + k * kWarps) * kPair;
             const uint32_t has = (has_now >> (2 * (k - from))) & 3u;

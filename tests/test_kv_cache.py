@@ -13,6 +13,7 @@ import ctypes
 import math
 import os
 import re
+import subprocess
 
 import numpy as np
 import pytest
@@ -96,6 +97,45 @@ def test_no_device_means_an_error():
     with pytest.raises(B.MoEError) as e:
         plan_for()
     assert e.value.status == -5
+
+
+RING = r"""
+#include <cstdio>
+#include <cstdlib>
+#include "kv_ring.cuh"
+
+// ring PIECES [steps, number of the wait that runs out or -1]...: prints every wait (stage, parity) and every step that was used
+int main(int argc, char **argv) {
+    lexi::kv::RingWaits<2> ring;
+    int waits = 0, bad = atoi(argv[1]);
+    for (int i = 2; i < argc; ++i) {
+        const int steps = atoi(argv[i]);
+        for (int k = 0; k < steps; ++k) {
+            const bool there = ring.arrived(k, steps, [&](int stage, uint32_t parity) {
+                printf("w%d%u ", stage, parity);
+                return waits++ != bad;
+            });
+            if (!there) break;
+            printf("u%d ", k);
+        }
+        printf("| ");
+    }
+    printf("%s", ring.dead ? "dead" : "alive");
+}
+"""
+
+
+@pytest.mark.parametrize("bad, pieces, want", [
+    (-1, (3, 1, 2), "w00 u0 w10 u1 w01 u2 | w00 u0 | w01 u0 w11 u1 | alive"),          # parities go on from piece to piece
+    (2, (5, 2), "w00 u0 w10 u1 w01 w01 w11 | | dead"),          # two were under way: once more each; nothing of the next piece
+    (4, (5, 2, 1), "w00 u0 w10 u1 w01 u2 w11 u3 w00 w00 | | | dead"),          # the last step: one
+    (0, (1, 1), "w00 w00 | | dead")])
+def test_a_ring_whose_wait_ran_out_is_not_used_again(bad, pieces, want, tmp_path):
+    """A copy that arrives after its wait ran out would pass for one of the next piece."""
+    (tmp_path / "ring.cpp").write_text(RING)
+    subprocess.run(["g++", "-std=c++17", "-I" + os.path.join(ROOT, "paper_2509_02753_b200", "csrc"), str(tmp_path / "ring.cpp"), "-o", str(tmp_path / "ring")], check=True)
+    got = subprocess.run([str(tmp_path / "ring"), str(bad), *map(str, pieces)], check=True, capture_output=True, text=True).stdout
+    assert got.split() == want.split()
 
 
 # ------------------------------------------------------------------------------------------ tables
