@@ -179,7 +179,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     int64_t *line = reinterpret_cast<int64_t *>(smem + S::kLineAt);
-    __shared__ __align__(8) uint64_t bars[14];
+    __shared__ __align__(8) uint64_t bars[15];
     __shared__ uint32_t tmem_slot, absent[4];
     __shared__ long long sum_s[kThreads / 32];
     __shared__ int last_s;
@@ -194,6 +194,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
     auto s_full = [&](int t) { return bar + 64 + 8 * t; };
     auto p_full = [&](int t) { return bar + 80 + 8 * t; };
     auto o_full = [&](int t) { return bar + 96 + 8 * t; };
+    const uint32_t all_done = bar + 112;          // of the last products, if a wait ran out
 
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
@@ -201,6 +202,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
             tc::mbar_init(v_full(i), 4); tc::mbar_init(v_empty(i), 1);
             tc::mbar_init(s_full(i), 1); tc::mbar_init(p_full(i), 4); tc::mbar_init(o_full(i), 1);
         }
+        tc::mbar_init(all_done, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (tid < 4) absent[tid] = 0u;
@@ -918,9 +920,19 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
         }
     }
     tc::tc_fence_before();
-    __syncthreads();
+    // The softmax groups wait for the last products; where one gave up, the thread that issued them does, before their operands
+    // and sums are another CTA's
+    const bool gave_up = __syncthreads_or(dead);
     tc::tc_fence_after();
-    if (warp == 12) tc::tmem_dealloc(tmem_slot, 512);
+    if (warp == 12) {
+        if (gave_up) {
+            if (elect_one()) tc::umma_commit(all_done);
+            __syncwarp();
+            tc::mbar_wait(all_done, 0u, a.status);
+            __syncwarp();
+        }
+        tc::tmem_dealloc(tmem_slot, 512);
+    }
 }
 
 template <typename T, int W, int GROUPS, int TILES, int KEYS>
