@@ -20,7 +20,8 @@
  *   offset 17 W  value scales  [W/16][16 tokens]
  *
  * A code is e2m1 (0, 0.5, 1, 1.5, 2, 3, 4, 6 and the sign in its top bit); the number held is
- * code * scale * k_scale (v_scale for values), k_scale and v_scale being two fp32 numbers of the layer.
+ * code * scale * k_scale (v_scale for values), k_scale and v_scale being two fp32 numbers of the layer,
+ * positive and normal.
  * For the 16 numbers x of a group: scale = e4m3(max|x| / (6 k_scale)), code = e2m1(x / (scale k_scale)),
  * both rounded to nearest even and held at their largest value.  A NaN is stored as 0, an infinity as
  * the largest value; either sets MOE_KV_STATUS_NONFINITE.

@@ -62,7 +62,7 @@ int check_turn(const moe_kv_plan *p, int32_t tokens, const int32_t *position, co
 // log2 of a page's blocks
 int page_shift(const moe_kv_config_t &c) { return c.page_size == 16 ? 0 : c.page_size == 32 ? 1 : c.page_size == 64 ? 2 : 3; }
 
-bool good_scale(float s) { return s > 0.f && std::isfinite(s); }
+bool good_scale(float s) { return s > 0.f && std::isnormal(s); }          // 1/(6 s) is finite
 
 int done(cudaError_t err) {
     if (err == cudaSuccess) return MOE_OK;

@@ -292,7 +292,12 @@ __device__ __forceinline__ uint32_t quantise8(float (&x)[8], float inv6, float s
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
     s8 = to_e4m3(fminf(__fmul_rn(top, inv6), 448.f));
     const float s = __fmul_rn(from_e4m3(s8), scale);
-    const float inv = s > 0.f ? __frcp_rn(s) : 0.f;
+    float inv = s > 0.f ? __frcp_rn(s) : 0.f;
+    if (inv > FLT_MAX) {          // s below 2^-128: x and s times 2^64, or a zero times infinity would be stored as a code
+        inv = __frcp_rn(__fmul_rn(s, 0x1p64f));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = __fmul_rn(x[i], 0x1p64f);
+    }
     uint32_t w = 0u;
 #pragma unroll
     for (int i = 0; i < 4; ++i) w |= to_e2m1_pair(__fmul_rn(x[2 * i], inv), __fmul_rn(x[2 * i + 1], inv)) << (8 * i);

@@ -415,6 +415,31 @@ def test_numbers_that_are_not_finite():
 
 
 @gpu
+def test_layers_of_the_smallest_scales():
+    """A group's scale times the layer's below 2^-128, whose reciprocal is no fp32 number: zeros stay zeros, and what is stored is as near
+    as elsewhere.  Not above that: products of numbers below 2^-126 are rounded to multiples of 2^-149 besides."""
+    x = torch.zeros(4, 1, 64, device="cuda")
+    x[0, 0, 3], x[0, 0, 20], x[1, 0, 1:16], x[2] = 1e-38, -2e-39, 3e-38, torch.randn(1, 64, device="cuda") * 2e-38
+    with plan_for(1, 1, 64) as plan:
+        for scale in (1e-37, 2.0 ** -126, 1e-36, 1e-30):
+            cache = plan.new_cache(1)
+            plan.append(None, x, x, torch.arange(4, device="cuda"), cache, k_scale=scale, v_scale=scale)
+            for got in plan.read(cache, torch.arange(4, device="cuda"), k_scale=scale, v_scale=scale):
+                assert bool((got[x == 0] == 0).all())
+                if scale <= 1e-36:
+                    top = x.double().unflatten(-1, (4, 16)).abs().amax(-1, keepdim=True)
+                    # half a step of the largest code; the scale's own rounding (relative 2^-4, or 2^-10 of the smallest); 64 steps of 2^-149
+                    limit = top / 6 * (1 + 2 ** -4) + 6 * scale * 2.0 ** -10 + 64 * 2.0 ** -149
+                    assert bool(((got.double() - x.double()).unflatten(-1, (4, 16)).abs() <= limit).all())
+        for scale in (2.0 ** -127, 1e-45):          # not normal numbers
+            k = x[:1]
+            for call in (lambda: plan.append(None, k, k, torch.arange(1, device="cuda"), cache, k_scale=scale), lambda: plan.read(cache, torch.arange(1, device="cuda"), v_scale=scale)):
+                with pytest.raises(B.MoEError) as e:
+                    call()
+                assert e.value.status == -1
+
+
+@gpu
 def test_slots_outside_the_cache():
     k = torch.randn(4, 2, 64, device="cuda")
     with plan_for() as plan:
