@@ -116,7 +116,8 @@ int moe_kv_device_status(moe_kv_plan_t *plan, int32_t *bits, void *cuda_stream);
  * fresh pages that the step needs (more than n_free: NO_PAGES, and the entries and slots without a page
  * are -1).  n_tokens is the capacity of position and slot: entries behind the last new token get slot
  * -1 and position 0; new tokens behind the capacity set BAD_INDEX.  A negative length counts as 0 and
- * sets BAD_INDEX.  A position outside the row of the table gets slot -1 (NO_PAGES).
+ * sets BAD_INDEX.  A position outside the row of the table gets slot -1 (NO_PAGES), one whose page is given
+ * as a negative number too (BAD_INDEX).
  * ctx_len and the free list are not changed: kv_len is the next step's ctx_len, and the caller's free
  * list then begins pages_taken entries later.  Errors: INVALID_ARG, CUDA.
  */

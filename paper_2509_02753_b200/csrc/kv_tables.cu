@@ -102,14 +102,14 @@ __global__ void __launch_bounds__(kThreads) tables_kernel(TablesArgs a) {
             const int c = max(a.ctx[r], 0);
             position = low((unsigned long long)c + (t - cu[r]));
             const int col = position >> a.page_shift, held = (int)pages(c);
+            const long long f = (long long)first[r] + col - held;          // of the free list, if the page is a fresh one
             int page = -1;
-            if (col < held) {
-                if (col < a.width) page = a.table[(int64_t)r * a.width + col];
-            } else {
-                const long long f = (long long)first[r] + col - held;
-                if (f < a.n_free && col < a.width) page = a.free_pages[f];
+            if (col >= a.width) {
+                bad |= MOE_KV_STATUS_NO_PAGES;
+            } else if (col < held || f < a.n_free) {
+                page = col < held ? a.table[(int64_t)r * a.width + col] : a.free_pages[f];
+                if (page < 0) bad |= MOE_KV_STATUS_BAD_INDEX;
             }
-            if (col >= a.width) bad |= MOE_KV_STATUS_NO_PAGES;
             if (page >= 0) slot = ((int64_t)page << a.page_shift) + (position & ((1 << a.page_shift) - 1));
         }
         a.position[t] = position;

@@ -185,6 +185,14 @@ def test_tables_that_do_not_fit():
 
 
 @gpu
+def test_new_tokens_whose_page_is_no_page():
+    """A negative entry that a new token needs, of the table or of the free list, loses the token and says so."""
+    check_tables([20, 3], [2, 1], [5, 9], [[4, -1], [7, -1]], 16, 3, K.STATUS_BAD_INDEX)
+    check_tables([16, 3], [2, 1], [-1, 9], [[4, -1], [7, -1]], 16, 3, K.STATUS_BAD_INDEX)
+    check_tables([20, 3], [0, 1], [5, 9], [[4, -1], [7, -1]], 16, 1, 0)          # nothing new there
+
+
+@gpu
 def test_tables_of_lengths_that_pass_32_bits():
     with plan_for(requests=300, tokens=8) as plan:
         n = 300
