@@ -93,8 +93,9 @@ def load_native():
 
 def rope_table(rope_dim: int, n_positions: int, *, base: float = 10000.0, scaling: str = "plain", factor: float = 1.0, low: float = 1.0,
                high: Optional[float] = None, original_context: float = 0.0, magnitude: float = 0.0, device="cuda", stream=None) -> torch.Tensor:
-    """cos and sin of every position and pair, [n_positions, rope_dim/2, 2] fp32 (``moe_rope_table``)."""
-    out = torch.empty((n_positions, rope_dim // 2, 2), dtype=torch.float32, device=device)
+    """cos and sin of every position and pair, [n_positions, rope_dim/2, 2] fp32 (``moe_rope_table``).  The tensor belongs to `stream`."""
+    with torch.cuda.stream(stream):          # None: the current one
+        out = torch.empty((n_positions, rope_dim // 2, 2), dtype=torch.float32, device=device)
     if high is None:
         high = 4.0 if scaling == "bands" else 32.0
     cfg = moe_rope_config_t(rope_dim, SCALINGS[scaling], base, factor, low, high, original_context, magnitude)

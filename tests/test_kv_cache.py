@@ -254,6 +254,18 @@ def test_rope_table_refusals():
     assert lib.moe_rope_table(ctypes.byref(cfg), 4, 12, None) == -3
 
 
+@gpu
+def test_angles_on_another_stream_are_that_streams_memory():
+    """What the call allocates belongs to the stream that fills it: a block of the current stream may still be in use there."""
+    side = torch.cuda.Stream()
+    turns = K.rope_table(64, 5000, stream=side)
+    at = turns.data_ptr()
+    own = [s["stream"] for s in torch.cuda.memory_snapshot() if s["address"] <= at < s["address"] + s["total_size"]]
+    assert own == [side.cuda_stream]
+    side.synchronize()
+    assert torch.equal(turns, K.rope_table(64, 5000))
+
+
 def strided(rng, tokens, heads, dim, dtype, pad):
     """Rows of a wider tensor, `pad` elements in front and behind."""
     wide = torch.from_numpy(rng.standard_normal((tokens, heads * dim + 2 * pad)).astype(np.float32)).to(dtype).cuda()
