@@ -91,17 +91,19 @@ enum { MOE_ROPE_HALF = 0,      /* dimension i turns with i + rope_dim/2         
 typedef struct moe_kv_plan moe_kv_plan_t;
 
 /* Validates the shapes and allocates the workspace (partial results of attention split over a long
- * context, counters, the status word).  Synchronises.
+ * context, counters, the status word) on the current device, the plan's.  Calls that launch are made with
+ * that device current; reading the status word and destroying are not bound to it.  Synchronises.
  * Errors: INVALID_ARG, SHAPE, CUDA (no sm_100 device), WORKSPACE. */
 int moe_kv_plan_create(const moe_kv_config_t *cfg, moe_kv_plan_t **out);
-int moe_kv_plan_destroy(moe_kv_plan_t *plan);               /* synchronises the device; NULL is accepted */
+int moe_kv_plan_destroy(moe_kv_plan_t *plan);               /* synchronises the plan's device; NULL is accepted */
 uint64_t moe_kv_plan_workspace_bytes(const moe_kv_plan_t *plan);
 uint64_t moe_kv_plan_launch_count(const moe_kv_plan_t *plan);
 
 /* Bytes of one page of the cache for this configuration (all key/value heads); 0 for a bad one. */
 uint64_t moe_kv_page_bytes(const moe_kv_config_t *cfg);
 
-/* Reads and clears the status word; synchronises the stream.  *bits (may be NULL) receives the
+/* Reads and clears the status word behind what is on the stream, one of the plan's device (NULL: its
+ * default stream); synchronises the stream.  *bits (may be NULL) receives the
  * MOE_KV_STATUS_* bits.  Returns MOE_OK, MOE_ERR_TIMEOUT or MOE_ERR_DEVICE_CHECK. */
 int moe_kv_device_status(moe_kv_plan_t *plan, int32_t *bits, void *cuda_stream);
 

@@ -9,7 +9,7 @@ using namespace lexi::kv;
 
 struct moe_kv_plan {
     moe_kv_config_t cfg{};
-    int sm_count = 0;
+    int device = 0, sm_count = 0;
     uint8_t *base = nullptr;          // one allocation
     uint64_t bytes = 0;
     uint64_t launches = 0;
@@ -64,6 +64,15 @@ int page_shift(const moe_kv_config_t &c) { return c.page_size == 16 ? 0 : c.page
 
 bool good_scale(float s) { return s > 0.f && std::isnormal(s); }          // 1/(6 s) is finite
 
+// The plan's device, for as long as it lives; whichever is current otherwise
+struct OnDevice {
+    int before = -1;
+    explicit OnDevice(int device) {
+        if (cudaGetDevice(&before) != cudaSuccess || before == device || cudaSetDevice(device) != cudaSuccess) before = -1;
+    }
+    ~OnDevice() { if (before >= 0) cudaSetDevice(before); }
+};
+
 int done(cudaError_t err) {
     if (err == cudaSuccess) return MOE_OK;
     cudaGetLastError();
@@ -87,6 +96,7 @@ int moe_kv_plan_create(const moe_kv_config_t *cfg, moe_kv_plan_t **out) {
     moe_kv_plan *p = new (std::nothrow) moe_kv_plan;
     if (!p) return MOE_ERR_WORKSPACE;
     p->cfg = *cfg;
+    p->device = dev;
     p->sm_count = sms;
     p->max_ctas = sms * kMaxCtasPerSm;
     const size_t part = (size_t)p->max_ctas * attend_part_floats(padded_width(cfg->head_dim)) * sizeof(float);
@@ -124,8 +134,11 @@ int moe_kv_plan_create(const moe_kv_config_t *cfg, moe_kv_plan_t **out) {
 
 int moe_kv_plan_destroy(moe_kv_plan_t *p) {
     if (!p) return MOE_OK;
-    cudaDeviceSynchronize();
-    cudaFree(p->base);
+    {
+        const OnDevice on(p->device);
+        cudaDeviceSynchronize();
+        cudaFree(p->base);
+    }
     cudaFreeHost(p->status_host);
     cudaGetLastError();
     delete p;
@@ -142,6 +155,7 @@ uint64_t moe_kv_page_bytes(const moe_kv_config_t *cfg) {
 
 int moe_kv_device_status(moe_kv_plan_t *p, int32_t *bits, void *stream) {
     if (!p) return MOE_ERR_INVALID_ARG;
+    const OnDevice on(p->device);          // a stream of NULL is this device's
     cudaStream_t s = (cudaStream_t)stream;
     if (cudaMemcpyAsync(p->status_host, p->status, 4, cudaMemcpyDeviceToHost, s) != cudaSuccess ||
         cudaMemsetAsync(p->status, 0, 4, s) != cudaSuccess || cudaStreamSynchronize(s) != cudaSuccess) {

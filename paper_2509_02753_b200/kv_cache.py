@@ -122,7 +122,7 @@ class KVPlan:
     def close(self):
         self._plan = None
         if getattr(self, "handle", None):
-            B._check("moe_kv_plan_destroy", self._lib.moe_kv_plan_destroy(self.handle))
+            B._check("moe_kv_plan_destroy", self._lib.moe_kv_plan_destroy(self.handle))          # on the plan's device
             self.handle = None
 
     def __del__(self):
@@ -150,17 +150,20 @@ class KVPlan:
         return int(self._lib.moe_kv_plan_launch_count(self.handle))
 
     def device_status(self, stream=None):
-        """(status, MOE_KV_STATUS bits) since the last read; synchronises."""
+        """(status, MOE_KV_STATUS bits) since the last read; synchronises.  Behind the plan's calls on `stream`, by default
+        the current one of the plan's device, whichever device is current."""
         bits = ctypes.c_int32()
-        status = int(self._lib.moe_kv_device_status(self.handle, ctypes.byref(bits), B._stream(stream)))
+        with torch.cuda.device(self.device):
+            status = int(self._lib.moe_kv_device_status(self.handle, ctypes.byref(bits), B._stream(stream)))
         if status == -5:
             raise MoEError("moe_kv_device_status", status)
         return status, int(bits.value)
 
-    def new_cache(self, n_pages: int, device="cuda") -> torch.Tensor:
-        """An empty cache of one layer: [n_pages, n_kv_heads, page_size/16, block bytes] uint8."""
+    def new_cache(self, n_pages: int, device=None) -> torch.Tensor:
+        """An empty cache of one layer, on the plan's device: [n_pages, n_kv_heads, page_size/16, block bytes] uint8."""
         blocks = self.page_size // 16
-        return torch.zeros((n_pages, self.n_kv_heads, blocks, self.page_bytes // (self.n_kv_heads * blocks)), dtype=torch.uint8, device=device)
+        return torch.zeros((n_pages, self.n_kv_heads, blocks, self.page_bytes // (self.n_kv_heads * blocks)), dtype=torch.uint8,
+                           device=torch.device("cuda", self.device) if device is None else device)
 
     def _call(self, what: str, f, *args, stream=None):
         """One native call on the current stream, or on `stream` (what it allocates then belongs to that stream)."""

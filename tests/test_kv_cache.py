@@ -92,6 +92,46 @@ def test_page_bytes(dim, page, kv):
     assert K.load_library().moe_kv_page_bytes(ctypes.byref(cfg)) == kv * (page // 16) * ref.block_bytes(dim)
 
 
+def test_status_word_and_caches_are_the_plans_device(monkeypatch):
+    """Two devices, the first current, the plan on the second: the status word is read behind the second's stream."""
+    current, seen = [0], []
+
+    class On:
+        def __init__(self, index):
+            self.index = index
+
+        def __enter__(self):
+            current.append(self.index)
+
+        def __exit__(self, *exc):
+            current.pop()
+
+    class Stream:
+        def __init__(self, cuda_stream):
+            self.cuda_stream = cuda_stream
+
+    class Lib:
+        def moe_kv_device_status(self, handle, bits, stream):
+            seen.append((current[-1], stream))
+            return 0
+
+        def moe_kv_page_bytes(self, cfg):
+            return K.load_library().moe_kv_page_bytes(cfg)
+
+        def moe_kv_plan_destroy(self, handle):
+            return 0
+
+    monkeypatch.setattr(torch.cuda, "device", On)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: Stream(1000 + (current[-1] if device is None else device)))
+    monkeypatch.setattr(torch, "zeros", lambda size, **more: seen.append(more["device"]))
+    plan = K.KVPlan.__new__(K.KVPlan)
+    plan.cfg = K.moe_kv_config_t(4, 2, 64, 16, 1, 1, B.MOE_F32)
+    plan.n_kv_heads, plan.page_size, plan.handle, plan.device, plan._lib = 2, 16, 1, 1, Lib()
+    assert plan.device_status() == (0, 0) and plan.device_status(Stream(7)) == (0, 0)
+    plan.new_cache(3)
+    assert seen == [(1, 1001), (1, 7), torch.device("cuda", 1)]
+
+
 @pytest.mark.skipif(torch.cuda.is_available(), reason="checks the no-device path")
 def test_no_device_means_an_error():
     with pytest.raises(B.MoEError) as e:
