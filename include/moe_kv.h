@@ -5,7 +5,8 @@
  * requests, rotary positions, storing keys and values in 4 bits, and attention over what is stored.
  * Status codes, dtypes and conventions are those of moe.h: every call is asynchronous on the stream it
  * is given, a plan serves one stream at a time, nothing of the caller's is kept after the call returns,
- * every function returns MOE_OK or a negative MOE_ERR_* code, nothing aborts.  What only the device can
+ * every function returns MOE_OK or a negative MOE_ERR_* code, nothing aborts.  Arrays lie on their type's
+ * alignment (ALIGN otherwise) unless a call says more.  What only the device can
  * see (a page number outside the cache, a free list that is too short) skips the access and is kept in
  * the plan's status word, which moe_kv_device_status reads.
  *
@@ -121,7 +122,7 @@ int moe_kv_device_status(moe_kv_plan_t *plan, int32_t *bits, void *cuda_stream);
  * sets BAD_INDEX.  A position outside the row of the table gets slot -1 (NO_PAGES), one whose page is given
  * as a negative number too (BAD_INDEX).
  * ctx_len and the free list are not changed: kv_len is the next step's ctx_len, and the caller's free
- * list then begins pages_taken entries later.  Errors: INVALID_ARG, CUDA.
+ * list then begins pages_taken entries later.  Errors: INVALID_ARG, ALIGN, CUDA.
  */
 int moe_kv_tables(moe_kv_plan_t *plan, const int32_t *ctx_len, const int32_t *new_len, int32_t n_requests,
                   const int32_t *free_pages, int32_t n_free, int32_t *block_table, int32_t table_width,

@@ -33,6 +33,9 @@ constexpr int kPassRows = 32;         // query rows of a pass over the keys in k
 
 size_t elem_size(int dtype) { return dtype == MOE_BF16 ? 2 : 4; }
 bool aligned(const void *p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+// arrays of 32-bit numbers; NULL is aligned
+template <typename... P>
+bool words(const P *...p) { return (aligned(p, 4) && ...); }
 
 int check_config(const moe_kv_config_t *c) {
     if (!c) return MOE_ERR_INVALID_ARG;
@@ -56,7 +59,7 @@ int check_turn(const moe_kv_plan *p, int32_t tokens, const int32_t *position, co
     if (layout != MOE_ROPE_HALF && layout != MOE_ROPE_PAIRS) return MOE_ERR_INVALID_ARG;
     if (tokens == 0) return MOE_OK;
     if (!position || !table || n_positions < 1) return MOE_ERR_INVALID_ARG;
-    return aligned(table, 8) ? MOE_OK : MOE_ERR_ALIGN;
+    return aligned(table, 8) && words(position) ? MOE_OK : MOE_ERR_ALIGN;
 }
 
 // log2 of a page's blocks
@@ -174,6 +177,7 @@ int moe_kv_tables(moe_kv_plan_t *p, const int32_t *ctx_len, const int32_t *new_l
         return MOE_ERR_INVALID_ARG;
     if (n > 0 && (!ctx_len || !new_len || !kv_len || (width > 0 && !block_table))) return MOE_ERR_INVALID_ARG;
     if ((n_free > 0 && !free_pages) || (n_tokens > 0 && (!position || !slot))) return MOE_ERR_INVALID_ARG;
+    if (!words(ctx_len, new_len, free_pages, block_table, kv_len, cu_new, position, taken) || !aligned(slot, 8)) return MOE_ERR_ALIGN;
     TablesArgs a{ctx_len, new_len, n, free_pages, n_free, block_table, width, page_shift(p->cfg) + 4, n_tokens,
                  kv_len, cu_new, position, slot, taken, p->status};
     return done(launch_tables(a, p->sm_count, (cudaStream_t)stream, &p->launches));
@@ -225,7 +229,7 @@ int moe_kv_append(moe_kv_plan_t *p, const moe_kv_rows_t *q, const moe_kv_rows_t 
         qr = Rows{q->data, q->token_stride, q->head_stride};
     }
     if (!slot || !cache) return MOE_ERR_INVALID_ARG;
-    if (!aligned(cache, 16)) return MOE_ERR_ALIGN;
+    if (!aligned(cache, 16) || !aligned(slot, 8)) return MOE_ERR_ALIGN;
     AppendArgs a{c.dtype, qr, Rows{k->data, k->token_stride, k->head_stride}, Rows{v->data, v->token_stride, v->head_stride}, T,
                  c.n_heads, c.n_kv_heads, c.head_dim, page_shift(c) + 4, Turn{position, (const float2 *)table, n_positions, rope_dim, layout, 0},
                  slot, k_scale, v_scale, (float)(1.0 / (6.0 * (double)k_scale)), (float)(1.0 / (6.0 * (double)v_scale)), q_out,
@@ -238,7 +242,7 @@ int moe_kv_read(moe_kv_plan_t *p, const void *cache, int32_t n_pages, const int6
     if (!p || T < 0 || T > p->cfg.max_tokens || n_pages < 0 || !good_scale(k_scale) || !good_scale(v_scale)) return MOE_ERR_INVALID_ARG;
     if (T == 0 || (!k && !v)) return MOE_OK;
     if (!slot || !cache) return MOE_ERR_INVALID_ARG;
-    if (!aligned(cache, 16) || !aligned(k, 16) || !aligned(v, 16)) return MOE_ERR_ALIGN;
+    if (!aligned(cache, 16) || !aligned(slot, 8) || !aligned(k, 16) || !aligned(v, 16)) return MOE_ERR_ALIGN;
     const moe_kv_config_t &c = p->cfg;
     ReadArgs a{c.dtype, (const uint8_t *)cache, (int64_t)n_pages * c.page_size, slot, T, c.n_kv_heads, c.head_dim, page_shift(c) + 4,
                k_scale, v_scale, k, v, p->status};
@@ -255,7 +259,7 @@ int moe_kv_attention(moe_kv_plan_t *p, const moe_kv_rows_t *q, int32_t T, const 
     if (T == 0 || n == 0) return MOE_OK;
     if (const int rc = check_rows(q, c.dtype)) return rc;
     if (!cu_new || !kv_len || !out || (width > 0 && !block_table) || (n_pages > 0 && !cache)) return MOE_ERR_INVALID_ARG;
-    if (!aligned(cache, 16) || !aligned(out, 16)) return MOE_ERR_ALIGN;
+    if (!aligned(cache, 16) || !aligned(out, 16) || !words(cu_new, kv_len, block_table)) return MOE_ERR_ALIGN;
     AttendArgs a{};
     a.dtype = c.dtype; a.q = Rows{q->data, q->token_stride, q->head_stride}; a.T = T; a.cu = cu_new; a.kv_len = kv_len; a.n = n; a.max_new = max_new;
     a.table = block_table; a.width = width; a.cache = (const uint8_t *)cache; a.n_pages = n_pages;

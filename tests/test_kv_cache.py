@@ -981,3 +981,22 @@ def test_alignment_refusals():
         assert lib.moe_rope(plan.handle, rows(p), 1, 4, p, p, 4, 64, 2, 0, p, 256, 64, None) == -1
         assert lib.moe_rope(plan.handle, rows(p), 1, 4, p, p, 4, 64, 0, 2, p, 256, 64, None) == -1
         assert plan.device_status() == (0, 0)
+
+
+@gpu
+def test_integer_arrays_off_their_alignment_are_refused():
+    lib = K.load_library()
+    with plan_for(4, 2, 64, 16, BF16) as plan:
+        mem = torch.zeros(1 << 16, dtype=torch.uint8, device="cuda")
+        p, before = mem.data_ptr(), plan.launch_count
+        rows = ctypes.byref(K.moe_kv_rows_t(p, 256, 64))
+        calls = {
+            "tables": (lib.moe_kv_tables, [plan.handle, p, p, 1, p, 1, p, 1, 1, p, p, p, p, p, None], {1: 2, 2: 2, 4: 2, 6: 2, 9: 2, 10: 2, 11: 2, 12: 4, 13: 2}),
+            "rope": (lib.moe_rope, [plan.handle, rows, 1, 4, p, p, 4, 64, 0, 0, p, 256, 64, None], {4: 2}),
+            "append": (lib.moe_kv_append, [plan.handle, rows, rows, rows, 1, p, p, 4, 64, 0, p, 1.0, 1.0, p, p, 1, None], {5: 2, 10: 4}),
+            "read": (lib.moe_kv_read, [plan.handle, p, 1, p, 1, 1.0, 1.0, p, p, None], {3: 4}),
+            "attention": (lib.moe_kv_attention, [plan.handle, rows, 1, p, p, 1, 1, p, 1, p, 1, 1.0, 1.0, 1.0, 0, 0, p, None], {3: 2, 4: 2, 7: 2})}
+        for name, (f, args, off) in calls.items():
+            for at, by in off.items():
+                assert f(*[a + by if i == at else a for i, a in enumerate(args)]) == -3, (name, at)
+        assert plan.launch_count == before and plan.device_status() == (0, 0)
