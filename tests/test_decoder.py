@@ -65,6 +65,17 @@ def test_refusals():
     dec.close()
 
 
+def test_a_step_in_which_every_request_pauses():
+    dec = make()
+    first = dec.step(tokens(20), [17, 3])
+    none = dec.step(tokens(1)[:0], [0, 0])
+    assert none.shape == (0, first.shape[1]) and [r.length for r in dec.requests] == [17, 3]
+    dec.check()
+    assert dec.step(tokens(2), [1, 1]).shape == (2, first.shape[1]) and dec.lengths.tolist() == [18, 4]
+    dec.check()
+    dec.close()
+
+
 def test_bf16_step_runs_and_stays_finite():
     dec = make(dtype=torch.bfloat16, requests=3, max_tokens=200, max_context=100, page_size=32)
     x = synth.make_tokens(synth.WORKLOADS["tiny"], 130, torch.bfloat16, "cuda")
