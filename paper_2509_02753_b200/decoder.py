@@ -91,6 +91,8 @@ class Decoder:
         for one that pauses).  Returns the stack's output for them, [sum(new), d]."""
         T = x.shape[0]
         assert T == sum(new) and len(new) == len(self.requests)
+        if any(n < 0 for n in new):
+            raise ValueError("a negative number of new tokens")
         if T == 0:
             return x
         need = self._fresh(new)

@@ -76,6 +76,16 @@ def test_a_step_in_which_every_request_pauses():
     dec.close()
 
 
+def test_negative_numbers_of_tokens_are_refused():
+    dec = make()
+    dec.step(tokens(20), [17, 3])
+    with pytest.raises(ValueError):
+        dec.step(tokens(2), [-1, 3])
+    assert [r.length for r in dec.requests] == [17, 3] and dec.lengths.tolist() == [17, 3]
+    dec.check()
+    dec.close()
+
+
 def test_bf16_step_runs_and_stays_finite():
     dec = make(dtype=torch.bfloat16, requests=3, max_tokens=200, max_context=100, page_size=32)
     x = synth.make_tokens(synth.WORKLOADS["tiny"], 130, torch.bfloat16, "cuda")
