@@ -144,11 +144,17 @@ def build(workload: str, attn: Attention, *, layers: int, dtype: torch.dtype, re
                    max_context=max_context)
 
 
+def attention_of(wl: synth.Workload) -> Attention:
+    """Heads of 128 dimensions as wide as the model, four (or the next larger number that divides) to a key/value head."""
+    heads = wl.d // 128
+    return Attention(n_heads=heads, n_kv_heads=max(n for n in range(1, max(1, heads // 4) + 1) if heads % n == 0), head_dim=128, rope_dim=128)
+
+
 def main(argv: Sequence[str]) -> None:
     workload = argv[0] if argv else "olmoe"
     requests, prompt, steps = (int(argv[i]) if len(argv) > i else v for i, v in ((1, 16), (2, 1024), (3, 64)))
     wl = synth.WORKLOADS[workload]
-    attn = Attention(n_heads=wl.d // 128, n_kv_heads=max(1, wl.d // 512), head_dim=128, rope_dim=128)
+    attn = attention_of(wl)
     dec = build(workload, attn, layers=min(wl.L, 8), dtype=torch.bfloat16, requests=requests, max_tokens=requests * prompt, max_context=prompt + steps)
     x = synth.make_tokens(wl, requests * prompt, torch.bfloat16, "cuda")
 

@@ -21,7 +21,9 @@ import torch
 
 import kv_reference as ref
 from paper_2509_02753_b200 import binding as B
+from paper_2509_02753_b200 import decoder
 from paper_2509_02753_b200 import kv_cache as K
+from paper_2509_02753_b200 import synth
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 gpu = pytest.mark.gpu
@@ -130,6 +132,15 @@ def test_status_word_and_caches_are_the_plans_device(monkeypatch):
     assert plan.device_status() == (0, 0) and plan.device_status(Stream(7)) == (0, 0)
     plan.new_cache(3)
     assert seen == [(1, 1001), (1, 7), torch.device("cuda", 1)]
+
+
+def test_every_workload_has_heads_that_a_plan_takes():
+    known = {"qwen15": (16, 4), "olmoe": (16, 4), "dsv2lite": (16, 4), "mixtral": (32, 8), "minicpm": (18, 3), "dsvl2tiny": (10, 2), "tiny": (2, 1)}
+    for name, wl in synth.WORKLOADS.items():
+        attn = decoder.attention_of(wl)
+        assert (attn.n_heads, attn.n_kv_heads) == known.get(name, (attn.n_heads, attn.n_kv_heads)), name
+        cfg = K.moe_kv_config_t(attn.n_heads, attn.n_kv_heads, attn.head_dim, 64, 1, 1, B.MOE_BF16)
+        assert K.load_library().moe_kv_page_bytes(ctypes.byref(cfg)) > 0, name
 
 
 @pytest.mark.skipif(torch.cuda.is_available(), reason="checks the no-device path")
