@@ -1,5 +1,6 @@
 """Builds the CUDA library in-tree: csrc/*.cu -> liblexi_moe.so (sm_100a only), and the Python module
-csrc/kv_binding.cpp -> _kv_native.so that calls it.
+csrc/kv_binding.cpp -> _kv_native.so that calls it (against the torch that is installed; the library needs none, and
+without torch only the library is built).
 
 nvcc cross-compiles without a GPU.  Objects go to ``_build/`` at the repository
 root; a source is recompiled when it or any header is newer than its object.
@@ -53,7 +54,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         if verbose or r.returncode != 0:
             sys.stderr.write(r.stdout + r.stderr)
         if r.returncode != 0:
-            raise RuntimeError("nvcc failed: " + " ".join(cmd))
+            raise RuntimeError("compiler failed: " + " ".join(cmd))
 
     with ThreadPoolExecutor(max_workers=8) as pool:
         list(pool.map(run, jobs))
@@ -66,12 +67,18 @@ def build(force: bool = False, verbose: bool = False) -> str:
 
 
 def build_native(run, headers, force: bool) -> None:
-    src = os.path.join(CSRC, "kv_binding.cpp")
-    if not force and os.path.exists(NATIVE) and os.path.getmtime(NATIVE) >= max(os.path.getmtime(p) for p in headers + [src]):
-        return
     import sysconfig
-
-    import torch
+    try:
+        import torch
+    except ImportError:
+        sys.stderr.write("no torch: _kv_native.so is not built\n")
+        return
+    src = os.path.join(CSRC, "kv_binding.cpp")
+    # a module of another torch or Python does not load, or worse: which ones it was built for is kept beside the objects
+    built_for, stamp = f"{torch.__version__} {torch.__file__} {sysconfig.get_config_var('SOABI')}", os.path.join(OBJ_DIR, "_kv_native.built_for")
+    same = os.path.exists(stamp) and open(stamp).read() == built_for
+    if not force and same and os.path.exists(NATIVE) and os.path.getmtime(NATIVE) >= max(os.path.getmtime(p) for p in headers + [src]):
+        return
     t = os.path.dirname(torch.__file__)
     cuda = os.path.dirname(os.path.dirname(_nvcc())) if os.path.isabs(_nvcc()) else "/usr/local/cuda"
     tmp = NATIVE + f".tmp{os.getpid()}"
@@ -80,6 +87,8 @@ def build_native(run, headers, force: bool) -> None:
          "-I" + sysconfig.get_paths()["include"], src, "-o", tmp, f"-L{PKG}", "-l:liblexi_moe.so", "-Wl,-rpath,$ORIGIN",
          f"-L{t}/lib", "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_cuda", "-ltorch_python", f"-Wl,-rpath,{t}/lib"])
     os.replace(tmp, NATIVE)
+    with open(stamp, "w") as f:
+        f.write(built_for)
 
 
 if __name__ == "__main__":

@@ -14,6 +14,7 @@ import math
 import os
 import re
 import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -21,6 +22,7 @@ import torch
 
 import kv_reference as ref
 from paper_2509_02753_b200 import binding as B
+from paper_2509_02753_b200 import build
 from paper_2509_02753_b200 import decoder
 from paper_2509_02753_b200 import kv_cache as K
 from paper_2509_02753_b200 import synth
@@ -141,6 +143,27 @@ def test_every_workload_has_heads_that_a_plan_takes():
         assert (attn.n_heads, attn.n_kv_heads) == known.get(name, (attn.n_heads, attn.n_kv_heads)), name
         cfg = K.moe_kv_config_t(attn.n_heads, attn.n_kv_heads, attn.head_dim, 64, 1, 1, B.MOE_BF16)
         assert K.load_library().moe_kv_page_bytes(ctypes.byref(cfg)) > 0, name
+
+
+def test_the_native_module_is_built_for_the_torch_there_is(monkeypatch, tmp_path):
+    """Built again for another torch though no source changed; without torch left out, and the library is built all the same."""
+    monkeypatch.setattr(build, "NATIVE", str(tmp_path / "native.so"))
+    monkeypatch.setattr(build, "OBJ_DIR", str(tmp_path))
+    ran = []
+
+    def run(cmd):
+        ran.append(cmd)
+        open(cmd[cmd.index("-o") + 1], "w").close()
+
+    build.build_native(run, [], False)
+    build.build_native(run, [], False)
+    assert len(ran) == 1
+    monkeypatch.setattr(torch, "__version__", "0.0")
+    build.build_native(run, [], False)
+    assert len(ran) == 2
+    monkeypatch.setitem(sys.modules, "torch", None)          # import raises
+    build.build_native(run, [], True)
+    assert len(ran) == 2
 
 
 @pytest.mark.skipif(torch.cuda.is_available(), reason="checks the no-device path")
