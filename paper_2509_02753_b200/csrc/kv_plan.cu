@@ -273,7 +273,7 @@ int moe_kv_attention(moe_kv_plan_t *p, const moe_kv_rows_t *q, int32_t T, const 
     cudaStream_t s = (cudaStream_t)stream;
     // Which kernel.  One pass over the keys serves 32 rows in kv_attend.cu (16 of wide heads); more rows read them again
     // there, while kv_prompt.cu has tiles of 128.  Measured at 8 key/value heads of 128 dimensions, 36 rows each: 16 requests
-    // of 2000 keys 69 us there, 55 here; 64 dimensions 46 and 41; 256 dimensions, 36 rows 95 and 102, 64 rows 117 and 106;
+    // of 2000 keys 69 us there, 57 here; 64 dimensions 46 and 41; 256 dimensions, 36 rows 95 and 102, 64 rows 117 and 106;
     // in fp32, 68 rows, 241 and 156, and one request of 16000 keys 121 and 123.
     // While all of its work is about one step of every warp kv_attend.cu is faster whatever the rows (one request of 500
     // keys, 256 rows: 22 us and 31).

@@ -9,13 +9,13 @@
 //   O_t[128 rows, W]       += P_t V         A = the weights in tensor memory (they take S_t's columns), B from shared memory
 // A code times its scale is exact in f16, so the codes become f16 operands once per CTA and tile: K rows as they lie,
 // V transposed (8 keys of a dimension are 16 bytes), both in the 128-byte swizzle.  Queries are scaled by a power of two
-// per row and are exact in f16 too; the weights are rounded to f16 (11 bits).  For fp32 both are two f16 parts, high and
-// low, and each part has its products.
+// per row and are exact in f16 too; the weights are rounded to f16 (11 bits, for outputs of 8; kv_attend.cu has the errors).
+// For fp32 both are two f16 parts, high and low, and each part has its products.
 //
 // Roles: two warpgroups of softmax (one for W = 256), one thread a row; one warpgroup that converts; one thread that issues
 // products.  The groups alternate: while one's weights are computed the other's products run.  Each has a tile of rows; for
 // fp32 with W = 128, whose queries leave room for one, both have that and every other tile of its keys (two prompts of
-// 1024 tokens on 4096 keys, 16/4 heads: 212 -> 166 us; the same for bf16 stretches of up to 128 rows loses, 42 -> 55 us
+// 1024 tokens on 4096 keys, 16/4 heads: 212 -> 164 us; the same for bf16 stretches of up to 128 rows loses, 42 -> 55 us
 // with 36 rows on 16000 keys, by the second set of results).  A row's scores stay in registers from the search for the
 // largest to the weights; its reference lies kSlack above a score that was once the largest, so O is rescaled a few times
 // per row, not per tile.
@@ -208,7 +208,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
     if (tid < 4) absent[tid] = 0u;
     if (warp == 12) tc::tmem_alloc(smem_u32(&tmem_slot), 512);
 
-    pdl_trigger();          // behind the allocation: a kernel that starts early and wants tensor memory cannot be ahead of this one
+    // Maybe ahead of warp 12's allocation.  A dependent that starts early cannot take the tensor memory first: it starts once
+    // every CTA of this kernel is there, and each has all 65536 registers of its SM
+    pdl_trigger();
     pdl_wait();
 
     // ---- the line: key tiles of every stretch of prompts
