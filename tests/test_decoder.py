@@ -41,6 +41,47 @@ def test_prompts_at_once_and_token_by_token_agree(attn):
         assert (outs[0] - other).abs().max() <= 1e-3 * outs[0].abs().max()
 
 
+@pytest.mark.parametrize("attn", [ATTN, D.Attention(4, 2, 64, 64, layout="pairs", window=9, sinks=2, k_scale=0.01, v_scale=0.01)])
+def test_a_step_against_the_formula(attn):
+    """Prompts, then a token each: the turns, the masks and the sums in 64 bits on the numbers that the cache holds (read back), the
+    MoE layer as it is.  Tolerance as above: fp32 sums of a few thousand terms."""
+    dec, seen = make(attn=attn), [0, 0]
+    layer_forward = dec.moe.layer_forward
+    for new in ([23, 17], [1, 1], [0, 3]):
+        x = tokens(40)[: sum(new)]
+        got = dec.step(x, new)
+        dec.check()
+        positions = torch.cat([torch.arange(s, s + n) for s, n in zip(seen, new)]).cuda()
+        seen = [s + n for s, n in zip(seen, new)]
+        held = [(dec.table[i, torch.arange(s, device="cuda") // dec.page].long() * dec.page + torch.arange(s, device="cuda") % dec.page) for i, s in enumerate(seen)]
+        half = attn.rope_dim // 2
+        angle = positions.double().view(-1, 1, 1) * 10000.0 ** (-torch.arange(half, device="cuda").double() / half)
+        want = x
+        for layer, weights, cache, k_l in zip(dec.layers, dec.weights, dec.caches, dec.k_vec):
+            q = (D.rms_norm(want).double() @ layer["qkv"].double().t()).view(len(x), -1, attn.head_dim)[:, : attn.n_heads]
+            at = slice(0, half), slice(half, 2 * half)
+            if attn.layout == "pairs":
+                at = slice(0, 2 * half, 2), slice(1, 2 * half, 2)
+            turned = q.clone()
+            turned[..., at[0]] = q[..., at[0]] * angle.cos() - q[..., at[1]] * angle.sin()
+            turned[..., at[1]] = q[..., at[1]] * angle.cos() + q[..., at[0]] * angle.sin()
+            out = []
+            for i, s in enumerate(seen):
+                keys, values = (t.double().repeat_interleave(attn.n_heads // attn.n_kv_heads, 1)
+                                for t in dec.kv.read(cache, held[i], k_scale=attn.k_scale, v_scale=attn.v_scale))
+                first = sum(new[:i])
+                back = positions[first: first + new[i]].view(-1, 1) - torch.arange(s, device="cuda")
+                see = back >= 0
+                if attn.window:
+                    see &= (back < attn.window) | (torch.arange(s, device="cuda") < attn.sinks)
+                w = torch.einsum("thd,khd->htk", turned[first: first + new[i]], keys) / attn.head_dim ** 0.5
+                out.append(torch.einsum("htk,khd->thd", torch.softmax(w.masked_fill(~see, float("-inf")), -1), values))
+            want = want + (torch.cat(out).flatten(1) @ layer["o"].double().t()).float()
+            want = want + layer_forward(D.rms_norm(want), weights, k_l, dec.renorm)
+        assert (got - want).abs().max() <= 1e-3 * want.abs().max()
+    dec.close()
+
+
 def test_a_row_serves_another_request_after_finish():
     dec = make()
     x = tokens(40)

@@ -755,6 +755,15 @@ def test_prompts_in_tiles_on_long_contexts(dim, dtype):
 
 @gpu
 @pytest.mark.parametrize("dtype", [BF16, F32])
+def test_prompts_in_tiles_of_many_requests(dtype):
+    """More requests than the threads that line them up at once, some with nothing."""
+    rng = np.random.default_rng(41)
+    lens = [int(x) for x in rng.integers(9, 13, 530) * (rng.random(530) < 0.9)]
+    attend_case(41, lens, lens, 4, 1, 64, 16, dtype, columns=LONG)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("dim", [64, 128, 256])
 def test_absent_pages_under_tiles(dim, dtype):
     attend_case(38, [300, 90], [200, 80], 2, 1, dim, 16, dtype, absent=[(0, 3), (1, 2), (0, 9), (0, 10)], columns=LONG)
