@@ -45,7 +45,8 @@ constexpr int kEntry = 16;                     // what a stretch costs besides i
 constexpr int kBrief = 32;                     // stretches of at most this many blocks are not cut
 constexpr float kFloor = -FLT_MAX;             // reference of a row that has seen no key
 // Weights are 2^(x - m + kHead + kSlack): m is kSlack above a score that was once the largest, and follows only when a
-// score passes it; f16 holds weights up to 2^(kHead + kSlack) and down to 2^-24
+// score passes it; f16 holds weights up to 2^(kHead + kSlack) and down to 2^-24: one below 2^-20 of its row's largest is
+// held in steps of 2^-30 of that
 constexpr float kHead = 6.f, kSlack = 8.f;
 
 __device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
