@@ -330,7 +330,7 @@ def prepare(case, seed):
             member.copy_(torch.where(torch.arange(table.shape[1], device=DEV) < common, table[cu[j]].clone(), member))
         state = {"groups": _ints(cu)}
         if op == "shared":
-            state |= {"shared": _ints([m * p if cu[j + 1] - cu[j] > 1 else 0 for j, m in enumerate(pages)]), "cu_group": cu, "pages": pages,
+            state |= {"shared": _ints([m * p if cu[j + 1] - cu[j] > 1 else 0 for j, m in enumerate(pages)]), "cu_group": cu, "pages": pages, "max_group": max(b - a for a, b in zip(cu, cu[1:])) * case["new"],
                       "start": torch.cat([_ints([m * p if cu[j + 1] - cu[j] > 1 else 0]).expand(cu[j + 1] - cu[j]) for j, m in enumerate(pages)])}
             # no holes: the cache has the pages that are in use
             used, table_of = torch.unique(table.clamp(min=0), return_inverse=True)
@@ -520,7 +520,7 @@ def _run_own(state, case, op):
         return {"shared": shared, "start": start}
     if op == "shared":
         return plan.attention_shared(state["q"], state["cu"], state["len"], state["table"], state["cache"], state["groups"], state["shared"], state["start"],
-                                     max_new=state["max_new"], k_scale=K_SCALE, v_scale=V_SCALE)
+                                     max_new=state["max_new"], max_group=state["max_group"], k_scale=K_SCALE, v_scale=V_SCALE)
     if op == "summarise":
         plan.summarise(state["cu"], state["len"], state["table"], state["cache"], state["summaries"], state["tokens"])
         high, low = plan.read_summaries(state["summaries"], state["pages"], k_scale=K_SCALE)
