@@ -186,6 +186,113 @@ int moe_kv_attention(moe_kv_plan_t *plan, const moe_kv_rows_t *q, int32_t n_toke
                      float k_scale, float v_scale, int32_t window, int32_t sinks, void *out,
                      void *cuda_stream);
 
+/*
+ * A PREFIX THAT MANY REQUESTS SHARE.  Groups are runs of consecutive requests: group g has requests
+ * [cu_group[g], cu_group[g+1]) (cu_group does not fall and stays in 0..n_requests; requests in no group are
+ * allowed).  moe_kv_shared_prefix finds, once a step, how much of the cache a group's members have in
+ * common; moe_kv_attention_shared reads that once for the group instead of once for each member.
+ *
+ * moe_kv_shared_prefix: shared_len[g] = page_size * the number of leading columns of the block table in
+ * which all members have the same page, none of them behind a member's last full page in front of its new
+ * tokens; 0 for a group of one or none.  start [n_requests]: shared_len of the request's group, 0 outside.
+ * A cu_group that falls or leaves 0..n_requests sets BAD_INDEX and shares nothing.  An entry below 0 ends
+ * what is common.  Errors: INVALID_ARG, SHAPE (table_width * page_size above 2^30), ALIGN, CUDA.
+ */
+int moe_kv_shared_prefix(moe_kv_plan_t *plan, const int32_t *cu_group, int32_t n_groups, const int32_t *cu_new,
+                         const int32_t *kv_len, int32_t n_requests, const int32_t *block_table,
+                         int32_t table_width, int32_t *shared_len, int32_t *start, void *cuda_stream);
+
+/* Bytes of scratch that moe_kv_attention_shared wants for n_tokens and max_new; 0 where it reads the keys
+ * request by request (see there) and for bad arguments. */
+uint64_t moe_kv_shared_scratch_bytes(const moe_kv_plan_t *plan, int32_t n_tokens, int32_t max_new);
+
+/*
+ * moe_kv_attention_shared: what moe_kv_attention computes without a window, with shared_len and start as
+ * moe_kv_shared_prefix wrote them for the same cu_group, cu_new, kv_len and block_table.  The rows of all
+ * members attend to the group's prefix together, each request's rows to what lies behind it, and both
+ * results are joined in fp32 before the only rounding.
+ * max_new, max_group: the largest number of new tokens of a request and of a group; they only choose the
+ * kernels; 0 = unknown.  Where max_new times the query heads of a key/value head passes 32 (64 for
+ * head_dim above 128), and with max_new unknown where n_tokens does, a request's own rows
+ * share its keys already and the call is moe_kv_attention's.  scratch: 16-byte aligned device memory of
+ * scratch_bytes >= moe_kv_shared_scratch_bytes, in use until the call's work is done.
+ * A start outside 0..kv_len - new tokens sets BAD_INDEX; start and shared_len that do not belong together
+ * give rows that no formula stands for.
+ * Errors: INVALID_ARG, SHAPE, ALIGN, WORKSPACE (scratch missing or too small), CUDA.
+ */
+int moe_kv_attention_shared(moe_kv_plan_t *plan, const moe_kv_rows_t *q, int32_t n_tokens, const int32_t *cu_new,
+                            const int32_t *kv_len, int32_t n_requests, int32_t max_new, const int32_t *block_table,
+                            int32_t table_width, const void *cache, int32_t n_pages, const int32_t *cu_group,
+                            int32_t n_groups, int32_t max_group, const int32_t *shared_len, const int32_t *start,
+                            float softmax_scale, float k_scale, float v_scale, void *scratch,
+                            uint64_t scratch_bytes, void *out, void *cuda_stream);
+
+/*
+ * PAGES THAT A CHEAP SCORE SELECTS.  summaries[page][kv head] of 2 W + 16 bytes, dense, 16-byte aligned,
+ * beside the cache:
+ *
+ *   offset 0     W bytes   largest key of the page in every dimension, in steps, rounded up (int8)
+ *   offset W     W bytes   smallest key, rounded down
+ *   offset 2 W   4 bytes   the step, fp32, before k_scale: the largest magnitude / 127; then 12 bytes of zeros
+ *
+ * A step of a served layer: moe_kv_append, moe_kv_summarise, moe_kv_select, moe_kv_attention_selected.
+ */
+
+/* Bytes of one page's summaries for this configuration (all key/value heads); 0 for a bad one. */
+uint64_t moe_kv_summary_bytes(const moe_kv_config_t *cfg);
+
+/*
+ * moe_kv_summarise: summaries of every page that holds one of the new tokens, from the cache, over the
+ * page's tokens in front of kv_len.  Whole pages are summarised anew, so a page that serves another request
+ * needs no clearing.  n_tokens: the new tokens (cu_new's last; more than that costs time, requests that
+ * end behind it set BAD_INDEX and are left out).  A page outside the cache sets BAD_INDEX.  Other pages'
+ * summaries are not touched.  Errors: INVALID_ARG, SHAPE (table_width * page_size above 2^30), ALIGN, CUDA.
+ */
+int moe_kv_summarise(moe_kv_plan_t *plan, const int32_t *cu_new, const int32_t *kv_len, int32_t n_requests,
+                     int32_t n_tokens, const int32_t *block_table, int32_t table_width, const void *cache,
+                     int32_t n_pages, void *summaries, void *cuda_stream);
+
+/* moe_kv_read_summaries: the bounds of n listed pages as numbers, high and low [n][n_kv_heads][head_dim]
+ * fp32 (codes * step * k_scale), 16-byte aligned.  Page -1 gives zeros, one outside the cache also sets
+ * BAD_INDEX.  Errors: INVALID_ARG, SHAPE (n * n_kv_heads * head_dim above 2^41), ALIGN, CUDA. */
+int moe_kv_read_summaries(moe_kv_plan_t *plan, const void *summaries, int32_t n_pages, const int32_t *page,
+                          int32_t n, float k_scale, float *high, float *low, void *cuda_stream);
+
+/*
+ * moe_kv_select: for every new token and key/value head up to n_select pages of the token's request, as
+ * columns of its row of the block table: selected [n_tokens][n_kv_heads][n_select], ascending, -1 behind
+ * the last.  With p the token's position its own page is column p / page_size; visible are the columns up
+ * to it.  If there are more than n_select, the first `first` and the last `last` are taken, and of the
+ * others those of the largest scores, equal ones from the lowest column on:
+ *   score = step * sum_d (u_d high_d + w_d low_d),    u = sum over the query heads of max(q, 0), w of min(q, 0),
+ * sums in fp32 in the order of the heads, then both rounded to whole numbers with the largest magnitude of
+ * the two at 127 (to nearest even); high, low and step as held; the sum over d is exact, its product with the step rounded
+ * once.  No key of the page has a larger sum of q . k over the heads, but for these roundings.  A NaN in q
+ * counts as 0; with an infinity all scores are 0.
+ * last >= 1, first + last <= n_select.  A token in front of the first key gets no page; rows of tokens
+ * that belong to no request are not written.  A page outside the cache among the scored ones sets
+ * BAD_INDEX and scores 0.  max_new: the largest number of new tokens of a request, chooses kernels only; 0 = unknown.
+ * Errors: INVALID_ARG, SHAPE (table_width above 49152, n_select or table_width * page_size above 2^30), ALIGN, CUDA.
+ */
+int moe_kv_select(moe_kv_plan_t *plan, const moe_kv_rows_t *q, int32_t n_tokens, const int32_t *cu_new,
+                  const int32_t *kv_len, int32_t n_requests, int32_t max_new, const int32_t *block_table,
+                  int32_t table_width, const void *summaries, int32_t n_pages, int32_t n_select, int32_t first,
+                  int32_t last, int32_t *selected, void *cuda_stream);
+
+/*
+ * moe_kv_attention_selected: softmax attention of every new token, head by head, over the keys of the
+ * listed pages that lie at or in front of its position (types, scales and products as moe_kv_attention).
+ * selected [n_tokens][n_kv_heads][n_select], in any order: columns of the request's row of the block table;
+ * -1 is no page; a page listed twice counts twice; a column outside -1..table_width-1 sets
+ * BAD_INDEX and counts as none.  A row without a key is 0; rows of tokens that belong to no
+ * request are not written.  Errors: INVALID_ARG, SHAPE (n_select or table_width * page_size above 2^30), ALIGN, CUDA.
+ */
+int moe_kv_attention_selected(moe_kv_plan_t *plan, const moe_kv_rows_t *q, int32_t n_tokens, const int32_t *cu_new,
+                              const int32_t *kv_len, int32_t n_requests, const int32_t *block_table,
+                              int32_t table_width, const void *cache, int32_t n_pages, const int32_t *selected,
+                              int32_t n_select, float softmax_scale, float k_scale, float v_scale, void *out,
+                              void *cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

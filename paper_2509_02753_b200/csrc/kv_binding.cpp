@@ -260,10 +260,147 @@ PyObject *attention(PyObject *, PyObject *const *args, Py_ssize_t n) {
     });
 }
 
+// cu_new, kv_len, block_table: the requests of a call
+struct Requests { const int32_t *cu, *len, *table; int32_t n, width; };
+Requests requests_of(Args &a) {
+    const at::Tensor &cu = a.dense(at::kInt, "cu_new: dense int32 wanted"), &len = a.dense(at::kInt, "kv_len: dense int32 wanted");
+    const at::Tensor &table = a.dense(at::kInt, "block_table: dense int32 wanted");
+    const int64_t n = len.numel();
+    WANT(n <= INT32_MAX && cu.numel() == n + 1 && table.dim() == 2 && table.size(0) == n && table.size(1) <= INT32_MAX,
+         "cu_new, kv_len and block_table of different numbers of requests");
+    return Requests{cu.data_ptr<int32_t>(), len.data_ptr<int32_t>(), table.data_ptr<int32_t>(), (int32_t)n, (int32_t)table.size(1)};
+}
+
+// q and the output of an attention call
+moe_kv_rows_t queries_of(const at::Tensor &q, const Plan &p) {
+    WANT(q.dim() > 0 && q.size(0) <= INT32_MAX, "q is too large");
+    return rows_of(q, p, p.heads, "q: [tokens, n_heads, head_dim] of the plan's type wanted");
+}
+at::Tensor output_of(const at::Tensor *given, const at::Tensor &q, const Plan &p) {
+    at::Tensor out = given ? *given : fresh(q.sizes(), p.type, p.device);
+    WANT(out.sizes() == q.sizes() && out.scalar_type() == p.type && out.is_contiguous(), "out: dense, as q wanted");
+    return out;
+}
+
+int32_t summaries_of(const at::Tensor &s, const Plan &p) {
+    WANT(s.scalar_type() == at::kByte && s.is_contiguous() && s.dim() > 0, "summaries: dense uint8 wanted");
+    const int64_t n = s.size(0), width = p.dim <= 64 ? 64 : p.dim <= 128 ? 128 : 256;
+    WANT(n <= INT32_MAX && (int64_t)s.numel() == n * p.kv_heads * (2 * width + 16), "summaries of another shape");
+    return (int32_t)n;
+}
+
+PyObject *shared_prefix(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    return guarded(args, n, [](Args &a) {
+        const Plan p = plan_of(a);
+        const c10::cuda::CUDAGuard guard((c10::DeviceIndex)p.device);
+        const at::Tensor &groups = a.dense(at::kInt, "cu_group: dense int32 wanted");
+        const Requests r = requests_of(a);
+        const int64_t g = groups.numel() - 1;
+        WANT(groups.dim() == 1 && g >= 0 && g <= INT32_MAX, "cu_group: the groups' first requests and the end wanted");
+        const at::Tensor words = fresh({g + r.n}, at::kInt, p.device);
+        at::Tensor shared = part_of(words, 0, {g}), start = part_of(words, g, {r.n});
+        const int rc = moe_kv_shared_prefix(p.handle, groups.data_ptr<int32_t>(), (int32_t)g, r.cu, r.len, r.n, r.table, r.width, shared.data_ptr<int32_t>(),
+                                            start.data_ptr<int32_t>(), stream_of(p));
+        return answer(rc, {shared, start});
+    });
+}
+
+PyObject *attention_shared(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    return guarded(args, n, [](Args &a) {
+        const Plan p = plan_of(a);
+        const c10::cuda::CUDAGuard guard((c10::DeviceIndex)p.device);
+        const at::Tensor &q = a.tensor();
+        const moe_kv_rows_t rows = queries_of(q, p);
+        const Requests r = requests_of(a);
+        const at::Tensor &cache = a.tensor(), &groups = a.dense(at::kInt, "cu_group: dense int32 wanted");
+        const at::Tensor &shared = a.dense(at::kInt, "shared_len: dense int32 wanted"), &start = a.dense(at::kInt, "start: dense int32 wanted");
+        const int64_t g = groups.numel() - 1;
+        WANT(g >= 0 && g <= INT32_MAX && shared.numel() == g && start.numel() == r.n, "cu_group, shared_len and start of different numbers");
+        const int32_t max_new = a.i32(), max_group = a.i32();
+        const float scale = a.f32(), ks = a.f32(), vs = a.f32();
+        const at::Tensor out = output_of(a.tensor_or_none(), q, p);
+        const int64_t bytes = g > 0 && r.n > 0 ? (int64_t)moe_kv_shared_scratch_bytes(p.handle, (int32_t)q.size(0), max_new) : 0;
+        const at::Tensor scratch = bytes > 0 ? fresh({bytes}, at::kByte, p.device) : at::Tensor();
+        const int rc = moe_kv_attention_shared(p.handle, &rows, (int32_t)q.size(0), r.cu, r.len, r.n, max_new, r.table, r.width, cache.data_ptr(), pages_of(cache, p),
+                                               groups.data_ptr<int32_t>(), (int32_t)g, max_group, shared.data_ptr<int32_t>(), start.data_ptr<int32_t>(), scale, ks, vs,
+                                               bytes > 0 ? scratch.data_ptr() : nullptr, (uint64_t)bytes, out.data_ptr(), stream_of(p));
+        return answer(rc, {out});
+    });
+}
+
+PyObject *summarise(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    return guarded(args, n, [](Args &a) {
+        const Plan p = plan_of(a);
+        const c10::cuda::CUDAGuard guard((c10::DeviceIndex)p.device);
+        const Requests r = requests_of(a);
+        const at::Tensor &cache = a.tensor(), &summaries = a.tensor();
+        const int32_t tokens = a.i32(), pages = pages_of(cache, p);
+        WANT(summaries_of(summaries, p) == pages, "summaries and cache of different numbers of pages");
+        const int rc = moe_kv_summarise(p.handle, r.cu, r.len, r.n, tokens, r.table, r.width, cache.data_ptr(), pages, summaries.data_ptr(), stream_of(p));
+        return answer(rc, {});
+    });
+}
+
+PyObject *read_summaries(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    return guarded(args, n, [](Args &a) {
+        const Plan p = plan_of(a);
+        const c10::cuda::CUDAGuard guard((c10::DeviceIndex)p.device);
+        const at::Tensor &summaries = a.tensor(), &pages = a.dense(at::kInt, "pages: dense int32 wanted");
+        const float ks = a.f32();
+        const int64_t m = pages.numel();
+        WANT(m <= INT32_MAX, "too many pages");
+        const at::Tensor both = fresh({2, m, p.kv_heads, p.dim}, at::kFloat, p.device);
+        at::Tensor high = part_of(both, 0, {m, p.kv_heads, p.dim}), low = part_of(both, both.numel() / 2, {m, p.kv_heads, p.dim});
+        const int rc = moe_kv_read_summaries(p.handle, summaries.data_ptr(), summaries_of(summaries, p), pages.data_ptr<int32_t>(), (int32_t)m, ks,
+                                             high.data_ptr<float>(), low.data_ptr<float>(), stream_of(p));
+        return answer(rc, {high, low});
+    });
+}
+
+PyObject *select(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    return guarded(args, n, [](Args &a) {
+        const Plan p = plan_of(a);
+        const c10::cuda::CUDAGuard guard((c10::DeviceIndex)p.device);
+        const at::Tensor &q = a.tensor();
+        const moe_kv_rows_t rows = queries_of(q, p);
+        const Requests r = requests_of(a);
+        const at::Tensor &summaries = a.tensor();
+        const int32_t n_select = a.i32(), first = a.i32(), last = a.i32(), max_new = a.i32();
+        const at::Tensor *given = a.tensor_or_none();
+        WANT(n_select >= 1, "n_select: at least one page wanted");
+        const at::Tensor out = given ? *given : fresh({q.size(0), p.kv_heads, n_select}, at::kInt, p.device);
+        WANT(out.scalar_type() == at::kInt && out.is_contiguous() && out.dim() == 3 && out.size(0) == q.size(0) && out.size(1) == p.kv_heads && out.size(2) == n_select,
+             "out: dense int32 [tokens, n_kv_heads, n_select] wanted");
+        const int rc = moe_kv_select(p.handle, &rows, (int32_t)q.size(0), r.cu, r.len, r.n, max_new, r.table, r.width, summaries.data_ptr(), summaries_of(summaries, p),
+                                     n_select, first, last, out.data_ptr<int32_t>(), stream_of(p));
+        return answer(rc, {out});
+    });
+}
+
+PyObject *attention_selected(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    return guarded(args, n, [](Args &a) {
+        const Plan p = plan_of(a);
+        const c10::cuda::CUDAGuard guard((c10::DeviceIndex)p.device);
+        const at::Tensor &q = a.tensor();
+        const moe_kv_rows_t rows = queries_of(q, p);
+        const Requests r = requests_of(a);
+        const at::Tensor &cache = a.tensor(), &selected = a.dense(at::kInt, "selected: dense int32 wanted");
+        WANT(selected.dim() == 3 && selected.size(0) == q.size(0) && selected.size(1) == p.kv_heads && selected.size(2) <= INT32_MAX,
+             "selected: [tokens, n_kv_heads, pages] wanted");
+        const float scale = a.f32(), ks = a.f32(), vs = a.f32();
+        const at::Tensor out = output_of(a.tensor_or_none(), q, p);
+        const int rc = moe_kv_attention_selected(p.handle, &rows, (int32_t)q.size(0), r.cu, r.len, r.n, r.table, r.width, cache.data_ptr(), pages_of(cache, p),
+                                                 selected.data_ptr<int32_t>(), (int32_t)selected.size(2), scale, ks, vs, out.data_ptr(), stream_of(p));
+        return answer(rc, {out});
+    });
+}
+
 #define ENTRY(name, doc) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, doc}
 PyMethodDef methods[] = {
     ENTRY(tables, "moe_kv_tables"), ENTRY(rope, "moe_rope"), ENTRY(append, "moe_kv_append"), ENTRY(read, "moe_kv_read"),
-    ENTRY(attention, "moe_kv_attention"), {nullptr, nullptr, 0, nullptr}};
+    ENTRY(attention, "moe_kv_attention"), ENTRY(shared_prefix, "moe_kv_shared_prefix"), ENTRY(attention_shared, "moe_kv_attention_shared"),
+    ENTRY(summarise, "moe_kv_summarise"), ENTRY(read_summaries, "moe_kv_read_summaries"), ENTRY(select, "moe_kv_select"),
+    ENTRY(attention_selected, "moe_kv_attention_selected"), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_kv_native", "Per-step calls of include/moe_kv.h", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

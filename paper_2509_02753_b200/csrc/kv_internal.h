@@ -26,6 +26,9 @@ __host__ __device__ constexpr int v_turn(int w, int r) {
     return w == 64 ? ((r >> 1) & 1) * 32 : w == 128 ? (r & 1) * 64 : (r & 1) * 16;
 }
 
+// a page's bounds of one head: largest and smallest key in 8 bits, the step and 12 bytes of zeros
+__host__ __device__ constexpr int summary_bytes(int w) { return 2 * w + 16; }
+
 struct Rows { const void *p; int64_t ts, hs; };
 
 // n / d for every 32-bit n and d >= 1 by one high product (Granlund and Montgomery's division by invariants): the
@@ -83,6 +86,31 @@ struct ReadArgs {
 };
 cudaError_t launch_read(const ReadArgs &a, cudaStream_t s, uint64_t *launches);
 
+// summaries of pages and the selection by them
+constexpr size_t kSelectSmem = 192 * 1024;       // of scores, at most: 49152 pages of one token
+struct SelectArgs {
+    int dtype; Rows q; int T; const int32_t *cu, *kv_len; int n; int max_new;
+    const int32_t *table; int width; const uint8_t *cache; int n_pages;
+    int Hk, G, D, page_shift;                 // a page has 1 << page_shift tokens
+    uint8_t *summaries;
+    int n_select, first, last; int32_t *selected;
+    int room;                                 // scores of a token
+    int32_t *status;
+};
+cudaError_t launch_summarise(const SelectArgs &a, cudaStream_t s, uint64_t *launches);
+cudaError_t launch_select(const SelectArgs &a, int sm_count, cudaStream_t s, uint64_t *launches);
+struct ReadSummariesArgs {
+    const uint8_t *summaries; int n_pages; const int32_t *page; int m, Hk, D; float k_scale; float *high, *low; int32_t *status;
+};
+cudaError_t launch_read_summaries(const ReadSummariesArgs &a, cudaStream_t s, uint64_t *launches);
+
+struct PrefixArgs {
+    const int32_t *groups; int n_groups; const int32_t *cu, *kv_len; int n;
+    const int32_t *table; int width, page_shift;        // a page has 1 << page_shift tokens
+    int32_t *shared, *start; int32_t *status;
+};
+cudaError_t launch_prefix(const PrefixArgs &a, int sm_count, cudaStream_t s, uint64_t *launches);
+
 struct AttendArgs {
     int dtype; Rows q; int T; const int32_t *cu, *kv_len; int n; int max_new;
     const int32_t *table; int width; const uint8_t *cache; int n_pages;
@@ -96,6 +124,14 @@ struct AttendArgs {
     int prompt_rows;
     float *prompt_part; float2 *prompt_ml; int32_t *prompt_arrived;
     int32_t *status;
+    // Shared prefixes.  Prefix: n groups, group i = requests [groups[i], groups[i + 1]) of n_members, kv_len its shared keys,
+    // max_new the largest number of its new tokens.  Rest: request i reads the keys from start[i] on.  o_part [T][H][W] and
+    // o_ml [T][H] are a row's sums, reference and denominator over its prefix: written by the one, read by the other
+    const int32_t *groups; int n_members;
+    const int32_t *start;
+    float *o_part; float2 *o_ml;
+    // Selected pages: [T][Hk][n_listed] columns of the request's row of the block table, -1: none
+    const int32_t *listed; int n_listed;
 };
 #ifdef __CUDACC__
 __device__ __forceinline__ int div_g(const AttendArgs &a, int row) { return (int)a.g_div.div((uint32_t)row); }      // row / G
@@ -103,8 +139,12 @@ __device__ __forceinline__ int div_g(const AttendArgs &a, int row) { return (int
 // rows of queries that share a key/value head, in the N dimension of mma.sync (kv_attend.cu)
 cudaError_t launch_attend_rows(const AttendArgs &a, int sm_count, cudaStream_t s, uint64_t *launches);
 size_t attend_part_floats(int w);          // per CTA of the grid
+cudaError_t launch_attend_prefix_rows(const AttendArgs &a, int sm_count, cudaStream_t s, uint64_t *launches);
+cudaError_t launch_attend_rest_rows(const AttendArgs &a, int sm_count, cudaStream_t s, uint64_t *launches);
+cudaError_t launch_attend_listed(const AttendArgs &a, int sm_count, cudaStream_t s, uint64_t *launches);
 // prompts, on tcgen05 (kv_prompt.cu)
 cudaError_t launch_attend_prompt(const AttendArgs &a, int sm_count, cudaStream_t s, uint64_t *launches);
+cudaError_t launch_attend_prefix_prompt(const AttendArgs &a, int sm_count, cudaStream_t s, uint64_t *launches);
 size_t prompt_part_floats(int w);          // per CTA, of which there is one per SM
 size_t prompt_part_rows();
 

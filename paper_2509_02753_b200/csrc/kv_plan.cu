@@ -1,4 +1,5 @@
 // C ABI of the operators around the 4-bit key/value cache (include/moe_kv.h): plan, checks of arguments, launches.
+#include <algorithm>
 #include <cmath>
 #include <cstring>
 #include <new>
@@ -82,6 +83,33 @@ int done(cudaError_t err) {
     return MOE_ERR_CUDA;
 }
 
+// What the attention calls have in common
+AttendArgs attend_args(const moe_kv_plan *p, const moe_kv_rows_t *q, int32_t T, const int32_t *cu_new, const int32_t *kv_len, int32_t n, int32_t max_new,
+                       const int32_t *block_table, int32_t width, const void *cache, int32_t n_pages, float softmax_scale, float k_scale, float v_scale, void *out) {
+    const moe_kv_config_t &c = p->cfg;
+    AttendArgs a{};
+    a.dtype = c.dtype; a.q = Rows{q->data, q->token_stride, q->head_stride}; a.T = T; a.cu = cu_new; a.kv_len = kv_len; a.n = n; a.max_new = max_new;
+    a.table = block_table; a.width = width; a.cache = (const uint8_t *)cache; a.n_pages = n_pages;
+    a.H = c.n_heads; a.Hk = c.n_kv_heads; a.G = c.n_heads / c.n_kv_heads; a.D = c.head_dim; a.g_div = FastDiv((uint32_t)a.G); a.page_shift = page_shift(c);
+    a.score_scale = (float)((double)softmax_scale * k_scale * 1.4426950408889634);
+    a.v_scale = v_scale; a.out = out;
+    a.part = p->part; a.part_ml = p->part_ml; a.arrived = p->arrived; a.max_ctas = p->max_ctas; a.status = p->status;
+    a.prompt_part = p->prompt_part; a.prompt_ml = p->prompt_ml; a.prompt_arrived = p->prompt_arrived;
+    return a;
+}
+
+// Query rows of a key/value head that kv_attend_body.cuh takes before kv_prompt_body.cuh does (see moe_kv_attention)
+int row_limit(const moe_kv_config_t &c) { return padded_width(c.head_dim) == 256 ? 2 * kPassRows : kPassRows; }
+
+// Whether a call's prefixes are read once for a group.  A request of more rows than one pass over the keys serves gains
+// nothing by it: its own rows share the reading already
+bool reads_prefixes_once(const moe_kv_plan *p, int32_t T, int32_t max_new) {
+    const long long most = max_new > 0 && max_new < T ? max_new : T;
+    return most * (p->cfg.n_heads / p->cfg.n_kv_heads) <= row_limit(p->cfg);
+}
+
+uint64_t shared_rows_bytes(const moe_kv_plan *p, int32_t T) { return (uint64_t)T * p->cfg.n_heads * padded_width(p->cfg.head_dim) * sizeof(float); }
+
 }  // namespace
 
 extern "C" {
@@ -105,10 +133,11 @@ int moe_kv_plan_create(const moe_kv_config_t *cfg, moe_kv_plan_t **out) {
     const size_t part = (size_t)p->max_ctas * attend_part_floats(padded_width(cfg->head_dim)) * sizeof(float);
     const size_t ml = (size_t)p->max_ctas * 2 * kPartRows * sizeof(float2);
     const size_t arrived = ((size_t)p->max_ctas * sizeof(int32_t) + 255) & ~size_t(255);
-    // prompts: two pieces for each SM, whose grid that is
-    const size_t ppart = (size_t)sms * prompt_part_floats(padded_width(cfg->head_dim)) * sizeof(float);
-    const size_t pml = (size_t)sms * prompt_part_rows() * sizeof(float2);
-    const size_t parrived = ((size_t)sms * sizeof(int32_t) + 255) & ~size_t(255);
+    // prompts: two pieces for each SM, whose grid that is.  The few rows of a shared prefix have their pieces here too, while
+    // the kernel of what lies behind it already uses the others
+    const size_t ppart = std::max((size_t)sms * prompt_part_floats(padded_width(cfg->head_dim)) * sizeof(float), part);
+    const size_t pml = std::max((size_t)sms * prompt_part_rows() * sizeof(float2), ml);
+    const size_t parrived = arrived;
     p->bytes = part + ml + ppart + pml + arrived + parrived + 256;
     void *mem = nullptr;
     if (cudaMalloc(&mem, p->bytes) != cudaSuccess || cudaMallocHost((void **)&p->status_host, 4) != cudaSuccess) {
@@ -260,16 +289,9 @@ int moe_kv_attention(moe_kv_plan_t *p, const moe_kv_rows_t *q, int32_t T, const 
     if (const int rc = check_rows(q, c.dtype)) return rc;
     if (!cu_new || !kv_len || !out || (width > 0 && !block_table) || (n_pages > 0 && !cache)) return MOE_ERR_INVALID_ARG;
     if (!aligned(cache, 16) || !aligned(out, 16) || !words(cu_new, kv_len, block_table)) return MOE_ERR_ALIGN;
-    AttendArgs a{};
-    a.dtype = c.dtype; a.q = Rows{q->data, q->token_stride, q->head_stride}; a.T = T; a.cu = cu_new; a.kv_len = kv_len; a.n = n; a.max_new = max_new;
-    a.table = block_table; a.width = width; a.cache = (const uint8_t *)cache; a.n_pages = n_pages;
-    a.H = c.n_heads; a.Hk = c.n_kv_heads; a.G = c.n_heads / c.n_kv_heads; a.D = c.head_dim; a.g_div = FastDiv((uint32_t)a.G); a.page_shift = page_shift(c);
-    a.score_scale = (float)((double)softmax_scale * k_scale * 1.4426950408889634);
-    a.v_scale = v_scale; a.out = out;
+    AttendArgs a = attend_args(p, q, T, cu_new, kv_len, n, max_new, block_table, width, cache, n_pages, softmax_scale, k_scale, v_scale, out);
     // no position reaches kMaxContext, and sums of these stay below 2^31
     a.window = window < kMaxContext ? window : (int)kMaxContext; a.sinks = sinks < kMaxContext ? sinks : (int)kMaxContext;
-    a.part = p->part; a.part_ml = p->part_ml; a.arrived = p->arrived; a.max_ctas = p->max_ctas; a.status = p->status;
-    a.prompt_part = p->prompt_part; a.prompt_ml = p->prompt_ml; a.prompt_arrived = p->prompt_arrived;
     cudaStream_t s = (cudaStream_t)stream;
     // Which kernel.  One pass over the keys serves 32 rows in kv_attend.cu (16 of wide heads); more rows read them again
     // there, while kv_prompt.cu has tiles of 128.  Measured at 8 key/value heads of 128 dimensions, 36 rows each: 16 requests
@@ -280,7 +302,7 @@ int moe_kv_attention(moe_kv_plan_t *p, const moe_kv_rows_t *q, int32_t T, const 
     const int most = max_new > 0 && max_new < T ? max_new : T;
     const long long rows = (long long)most * a.G, strips = (rows + kPassRows - 1) / kPassRows * n * a.Hk;
     const bool one_step = strips * (((long long)width * c.page_size + kBlockTokens - 1) / kBlockTokens) <= 32ll * p->sm_count;
-    const int limit = padded_width(c.head_dim) == 256 ? 2 * kPassRows : kPassRows;
+    const int limit = row_limit(c);
     if (rows <= limit || one_step) return done(launch_attend_rows(a, p->sm_count, s, &p->launches));
     // requests of one size, whichever it is, all go to the one kernel; otherwise each to its own
     const bool alike = (long long)n * most == T;
@@ -288,6 +310,128 @@ int moe_kv_attention(moe_kv_plan_t *p, const moe_kv_rows_t *q, int32_t T, const 
     const cudaError_t err = launch_attend_prompt(a, p->sm_count, s, &p->launches);
     if (err != cudaSuccess || alike) return done(err);
     return done(launch_attend_rows(a, p->sm_count, s, &p->launches));
+}
+
+int moe_kv_shared_prefix(moe_kv_plan_t *p, const int32_t *cu_group, int32_t n_groups, const int32_t *cu_new, const int32_t *kv_len, int32_t n,
+                         const int32_t *block_table, int32_t width, int32_t *shared_len, int32_t *start, void *stream) {
+    if (!p || n < 0 || n > p->cfg.max_requests || n_groups < 0 || n_groups > p->cfg.max_requests || width < 0) return MOE_ERR_INVALID_ARG;
+    if ((int64_t)width * p->cfg.page_size > kMaxContext) return MOE_ERR_SHAPE;
+    if (n == 0 && n_groups == 0) return MOE_OK;
+    if (n_groups > 0 && (!cu_group || !shared_len)) return MOE_ERR_INVALID_ARG;
+    if (n > 0 && (!cu_new || !kv_len || !start || (width > 0 && !block_table))) return MOE_ERR_INVALID_ARG;
+    if (!words(cu_group, cu_new, kv_len, block_table, shared_len, start)) return MOE_ERR_ALIGN;
+    PrefixArgs a{cu_group, n_groups, cu_new, kv_len, n, block_table, width, page_shift(p->cfg) + 4, shared_len, start, p->status};
+    return done(launch_prefix(a, p->sm_count, (cudaStream_t)stream, &p->launches));
+}
+
+uint64_t moe_kv_shared_scratch_bytes(const moe_kv_plan_t *p, int32_t n_tokens, int32_t max_new) {
+    if (!p || n_tokens < 1 || max_new < 0 || !reads_prefixes_once(p, n_tokens, max_new)) return 0;
+    return shared_rows_bytes(p, n_tokens) + (uint64_t)n_tokens * p->cfg.n_heads * sizeof(float2);
+}
+
+int moe_kv_attention_shared(moe_kv_plan_t *p, const moe_kv_rows_t *q, int32_t T, const int32_t *cu_new, const int32_t *kv_len, int32_t n, int32_t max_new,
+                            const int32_t *block_table, int32_t width, const void *cache, int32_t n_pages, const int32_t *cu_group, int32_t n_groups,
+                            int32_t max_group, const int32_t *shared_len, const int32_t *start, float softmax_scale, float k_scale, float v_scale,
+                            void *scratch, uint64_t scratch_bytes, void *out, void *stream) {
+    if (!p || T < 0 || T > p->cfg.max_tokens || n < 0 || n > p->cfg.max_requests || max_new < 0 || width < 0 || n_pages < 0 || n_groups < 0 ||
+        n_groups > p->cfg.max_requests || max_group < 0 || !std::isfinite(softmax_scale) || !good_scale(k_scale) || !good_scale(v_scale)) return MOE_ERR_INVALID_ARG;
+    const moe_kv_config_t &c = p->cfg;
+    if ((int64_t)width * c.page_size > kMaxContext) return MOE_ERR_SHAPE;
+    if (T == 0 || n == 0) return MOE_OK;
+    if (const int rc = check_rows(q, c.dtype)) return rc;
+    if (!cu_new || !kv_len || !out || (width > 0 && !block_table) || (n_pages > 0 && !cache)) return MOE_ERR_INVALID_ARG;
+    if (n_groups > 0 && (!cu_group || !shared_len || !start)) return MOE_ERR_INVALID_ARG;
+    if (!aligned(cache, 16) || !aligned(out, 16) || !aligned(scratch, 16) || !words(cu_new, kv_len, block_table, cu_group, shared_len, start)) return MOE_ERR_ALIGN;
+    if (n_groups == 0 || !reads_prefixes_once(p, T, max_new))
+        return moe_kv_attention(p, q, T, cu_new, kv_len, n, max_new, block_table, width, cache, n_pages, softmax_scale, k_scale, v_scale, 0, 0, out, stream);
+    if (!scratch || scratch_bytes < moe_kv_shared_scratch_bytes(p, T, max_new)) return MOE_ERR_WORKSPACE;
+    AttendArgs rest = attend_args(p, q, T, cu_new, kv_len, n, max_new, block_table, width, cache, n_pages, softmax_scale, k_scale, v_scale, out);
+    rest.start = start;
+    rest.o_part = (float *)scratch;
+    rest.o_ml = (float2 *)((uint8_t *)scratch + shared_rows_bytes(p, T));
+    AttendArgs prefix = rest;
+    prefix.kv_len = shared_len; prefix.n = n_groups; prefix.groups = cu_group; prefix.n_members = n;
+    prefix.max_new = max_group > 0 && max_group < T ? max_group : T;
+    cudaStream_t s = (cudaStream_t)stream;
+    // groups of few rows in kv_attend_body.cuh, those of many in kv_prompt_body.cuh, as the requests of moe_kv_attention
+    const long long most = prefix.max_new, limit = row_limit(c);
+    if (most * prefix.G > limit) {
+        const bool alike = n_groups * most == T;
+        prefix.prompt_rows = alike ? 0 : (int)limit;
+        const cudaError_t err = launch_attend_prefix_prompt(prefix, p->sm_count, s, &p->launches);
+        if (err != cudaSuccess) return done(err);
+        if (alike) return done(launch_attend_rest_rows(rest, p->sm_count, s, &p->launches));
+    }
+    prefix.part = p->prompt_part; prefix.part_ml = p->prompt_ml; prefix.arrived = p->prompt_arrived;
+    const cudaError_t err = launch_attend_prefix_rows(prefix, p->sm_count, s, &p->launches);
+    if (err != cudaSuccess) return done(err);
+    return done(launch_attend_rest_rows(rest, p->sm_count, s, &p->launches));
+}
+
+uint64_t moe_kv_summary_bytes(const moe_kv_config_t *cfg) {
+    if (check_config(cfg) != MOE_OK) return 0;
+    return (uint64_t)cfg->n_kv_heads * summary_bytes(padded_width(cfg->head_dim));
+}
+
+int moe_kv_summarise(moe_kv_plan_t *p, const int32_t *cu_new, const int32_t *kv_len, int32_t n, int32_t T, const int32_t *block_table, int32_t width,
+                     const void *cache, int32_t n_pages, void *summaries, void *stream) {
+    if (!p || T < 0 || T > p->cfg.max_tokens || n < 0 || n > p->cfg.max_requests || width < 0 || n_pages < 0) return MOE_ERR_INVALID_ARG;
+    const moe_kv_config_t &c = p->cfg;
+    if ((int64_t)width * c.page_size > kMaxContext) return MOE_ERR_SHAPE;
+    if (T == 0 || n == 0) return MOE_OK;
+    if (!cu_new || !kv_len || (width > 0 && !block_table) || (n_pages > 0 && (!cache || !summaries))) return MOE_ERR_INVALID_ARG;
+    if (!aligned(cache, 16) || !aligned(summaries, 16) || !words(cu_new, kv_len, block_table)) return MOE_ERR_ALIGN;
+    SelectArgs a{};
+    a.T = T; a.cu = cu_new; a.kv_len = kv_len; a.n = n; a.table = block_table; a.width = width; a.cache = (const uint8_t *)cache; a.n_pages = n_pages;
+    a.Hk = c.n_kv_heads; a.D = c.head_dim; a.page_shift = page_shift(c) + 4; a.summaries = (uint8_t *)summaries; a.status = p->status;
+    return done(launch_summarise(a, (cudaStream_t)stream, &p->launches));
+}
+
+int moe_kv_read_summaries(moe_kv_plan_t *p, const void *summaries, int32_t n_pages, const int32_t *page, int32_t m, float k_scale, float *high, float *low,
+                          void *stream) {
+    if (!p || m < 0 || n_pages < 0 || !good_scale(k_scale)) return MOE_ERR_INVALID_ARG;
+    const moe_kv_config_t &c = p->cfg;
+    if ((int64_t)m * c.n_kv_heads * (c.head_dim / 8) > kMaxRows * 256) return MOE_ERR_SHAPE;
+    if (m == 0) return MOE_OK;
+    if (!page || !high || !low || (n_pages > 0 && !summaries)) return MOE_ERR_INVALID_ARG;
+    if (!aligned(summaries, 16) || !aligned(high, 16) || !aligned(low, 16) || !words(page)) return MOE_ERR_ALIGN;
+    ReadSummariesArgs a{(const uint8_t *)summaries, n_pages, page, m, c.n_kv_heads, c.head_dim, k_scale, high, low, p->status};
+    return done(launch_read_summaries(a, (cudaStream_t)stream, &p->launches));
+}
+
+int moe_kv_select(moe_kv_plan_t *p, const moe_kv_rows_t *q, int32_t T, const int32_t *cu_new, const int32_t *kv_len, int32_t n, int32_t max_new,
+                  const int32_t *block_table, int32_t width, const void *summaries, int32_t n_pages, int32_t n_select, int32_t first, int32_t last,
+                  int32_t *selected, void *stream) {
+    if (!p || T < 0 || T > p->cfg.max_tokens || n < 0 || n > p->cfg.max_requests || max_new < 0 || width < 0 || n_pages < 0 || n_select < 1 || first < 0 ||
+        last < 1 || (int64_t)first + last > n_select) return MOE_ERR_INVALID_ARG;
+    const moe_kv_config_t &c = p->cfg;
+    if ((int64_t)width * c.page_size > kMaxContext || (size_t)width * sizeof(uint32_t) > kSelectSmem || (int64_t)n_select * c.page_size > kMaxContext) return MOE_ERR_SHAPE;
+    if (T == 0 || n == 0) return MOE_OK;
+    if (const int rc = check_rows(q, c.dtype)) return rc;
+    if (!cu_new || !kv_len || !selected || (width > 0 && !block_table) || (n_pages > 0 && !summaries)) return MOE_ERR_INVALID_ARG;
+    if (!aligned(summaries, 16) || !words(cu_new, kv_len, block_table, selected)) return MOE_ERR_ALIGN;
+    SelectArgs a{};
+    a.dtype = c.dtype; a.q = Rows{q->data, q->token_stride, q->head_stride}; a.T = T; a.cu = cu_new; a.kv_len = kv_len; a.n = n; a.max_new = max_new;
+    a.table = block_table; a.width = width; a.n_pages = n_pages; a.Hk = c.n_kv_heads; a.G = c.n_heads / c.n_kv_heads; a.D = c.head_dim;
+    a.page_shift = page_shift(c) + 4; a.summaries = (uint8_t *)const_cast<void *>(summaries); a.n_select = n_select; a.first = first; a.last = last;
+    a.selected = selected; a.status = p->status;
+    return done(launch_select(a, p->sm_count, (cudaStream_t)stream, &p->launches));
+}
+
+int moe_kv_attention_selected(moe_kv_plan_t *p, const moe_kv_rows_t *q, int32_t T, const int32_t *cu_new, const int32_t *kv_len, int32_t n,
+                              const int32_t *block_table, int32_t width, const void *cache, int32_t n_pages, const int32_t *selected, int32_t n_select,
+                              float softmax_scale, float k_scale, float v_scale, void *out, void *stream) {
+    if (!p || T < 0 || T > p->cfg.max_tokens || n < 0 || n > p->cfg.max_requests || width < 0 || n_pages < 0 || n_select < 1 ||
+        !std::isfinite(softmax_scale) || !good_scale(k_scale) || !good_scale(v_scale)) return MOE_ERR_INVALID_ARG;
+    const moe_kv_config_t &c = p->cfg;
+    if ((int64_t)width * c.page_size > kMaxContext || (int64_t)n_select * c.page_size > kMaxContext) return MOE_ERR_SHAPE;
+    if (T == 0 || n == 0) return MOE_OK;
+    if (const int rc = check_rows(q, c.dtype)) return rc;
+    if (!cu_new || !kv_len || !selected || !out || (width > 0 && !block_table) || (n_pages > 0 && !cache)) return MOE_ERR_INVALID_ARG;
+    if (!aligned(cache, 16) || !aligned(out, 16) || !words(cu_new, kv_len, block_table, selected)) return MOE_ERR_ALIGN;
+    AttendArgs a = attend_args(p, q, T, cu_new, kv_len, n, 1, block_table, width, cache, n_pages, softmax_scale, k_scale, v_scale, out);
+    a.listed = selected; a.n_listed = n_select;
+    return done(launch_attend_listed(a, p->sm_count, (cudaStream_t)stream, &p->launches));
 }
 
 }  // extern "C"

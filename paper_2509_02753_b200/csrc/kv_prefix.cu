@@ -1,0 +1,136 @@
+// How many leading pages the requests of a group have in common, one launch.
+//
+//   pages_g = the leading columns of the block table in which all members of group g have the same page, none behind a
+//             member's last full page in front of its new tokens;   shared_g = pages_g * P, 0 for a group of one
+//
+// Bound by latency up to thousands of table entries.  A cluster has a group, a warp a member at a time, 128 columns a step,
+// and no step goes behind what some member's end or difference has cut off.  The pages' numbers are compared, not the keys:
+// what the tables do not share is not shared, whatever a caller meant, and the attention is right for any groups.
+#include "kv_internal.h"
+
+namespace lexi {
+namespace kv {
+namespace {
+
+constexpr int kWarps = 8, kThreads = 32 * kWarps;
+constexpr int kMaxCluster = 8;
+
+__device__ __forceinline__ uint32_t cluster_rank() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
+__device__ __forceinline__ void st_cta0(const int *p, int v) {
+    uint32_t to;
+    asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(to) : "r"((uint32_t)__cvta_generic_to_shared(p)));
+    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(to), "r"(v) : "memory");
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
+__global__ void __launch_bounds__(kThreads) prefix_kernel(PrefixArgs a, int cluster) {
+    __shared__ int least_s, of_cta[kMaxCluster];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int rank = cluster > 1 ? (int)cluster_rank() : 0, g = blockIdx.x / cluster;
+    if (cluster > 1) cluster_arrive();
+    pdl_trigger();
+    pdl_wait();
+    if (tid == 0) least_s = a.width;
+
+    // groups that are not consecutive runs of requests: nothing is shared
+    int good = 1;
+    for (int x = tid; x <= a.n_groups; x += kThreads) {
+        const int at = a.groups[x];
+        good &= at >= 0 && at <= a.n && (x == 0 || a.groups[x - 1] <= at);
+    }
+    good = __syncthreads_and(good);
+    const int r0 = good && g < a.n_groups ? a.groups[g] : 0, r1 = good && g < a.n_groups ? a.groups[g + 1] : 0;
+    int pages = 0;
+    if (r1 - r0 > 1) {
+        int full = a.width;
+        for (int i = r0 + tid; i < r1; i += kThreads) {
+            const int len = a.kv_len[i], q0 = a.cu[i], nq = (int)min((long long)INT32_MAX, (long long)a.cu[i + 1] - q0);
+            const bool bad = len < 0 || nq < 0 || len > ((int64_t)a.width << a.page_shift);
+            if (bad) atomicOr(a.status, MOE_KV_STATUS_BAD_INDEX);
+            full = min(full, bad ? 0 : max(len - nq, 0) >> a.page_shift);
+        }
+        full = __reduce_min_sync(0xffffffffu, full);
+        if (lane == 0) atomicMin(&least_s, full);
+        __syncthreads();
+        const int32_t *lead = a.table + (int64_t)r0 * a.width;
+        for (int i = r0 + 1 + rank * kWarps + warp; i < r1; i += cluster * kWarps) {
+            const int32_t *row = a.table + (int64_t)i * a.width;
+            int most = *reinterpret_cast<volatile int *>(&least_s);
+#pragma unroll 1
+            for (int col = 0; col < most; col += 128) {
+                int x[4], y[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int at = col + 32 * j + lane;
+                    x[j] = at < most ? lead[at] : 0;
+                    y[j] = at < most ? row[at] : 0;
+                }
+                int differs = INT32_MAX;
+#pragma unroll
+                for (int j = 3; j >= 0; --j) {
+                    const uint32_t off = __ballot_sync(0xffffffffu, x[j] != y[j] || x[j] < 0);
+                    if (off) differs = col + 32 * j + __ffs(off) - 1;
+                }
+                if (differs != INT32_MAX) {
+                    if (lane == 0) atomicMin(&least_s, differs);
+                    break;
+                }
+                most = min(most, *reinterpret_cast<volatile int *>(&least_s));
+            }
+        }
+        __syncthreads();
+        pages = least_s;
+    }
+    if (cluster > 1) {
+        cluster_wait();                  // the first CTA is there
+        if (tid == 0) st_cta0(&of_cta[rank], pages);
+        cluster_arrive();
+        cluster_wait();
+        if (rank != 0) return;
+        for (int c = 0; c < cluster; ++c) pages = min(pages, of_cta[c]);
+    }
+    if (!good) {
+        if (g == 0) {
+            for (int x = tid; x < a.n_groups; x += kThreads) a.shared[x] = 0;
+            for (int x = tid; x < a.n; x += kThreads) a.start[x] = 0;
+            if (tid == 0) atomicOr(a.status, MOE_KV_STATUS_BAD_INDEX);
+        }
+        return;
+    }
+    if (g < a.n_groups) {
+        if (tid == 0) a.shared[g] = pages << a.page_shift;
+        for (int i = r0 + tid; i < r1; i += kThreads) a.start[i] = pages << a.page_shift;
+    }
+    // requests of no group
+    if (g == 0)
+        for (int i = tid; i < (a.n_groups > 0 ? a.groups[0] : a.n); i += kThreads) a.start[i] = 0;
+    if (g == a.n_groups - 1)
+        for (int i = r1 + tid; i < a.n; i += kThreads) a.start[i] = 0;
+}
+
+}  // namespace
+
+cudaError_t launch_prefix(const PrefixArgs &a, int sm_count, cudaStream_t s, uint64_t *launches) {
+    // a member for every warp at a time, if the groups are alike, while there are SMs
+    const int groups = a.n_groups > 0 ? a.n_groups : 1;
+    int cluster = 1;
+    while (cluster < kMaxCluster && a.n > groups * cluster * kWarps && (long long)groups * cluster * 2 <= 2 * sm_count) cluster *= 2;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(groups * cluster));
+    cfg.blockDim = dim3(kThreads);
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    ++*launches;
+    return cudaLaunchKernelEx(&cfg, prefix_kernel, a, cluster);
+}
+
+}  // namespace kv
+}  // namespace lexi

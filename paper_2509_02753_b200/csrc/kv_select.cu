@@ -1,0 +1,467 @@
+// Which pages a token attends to: bounds of each page's keys in 8 bits, scores from them, the pages of the largest.
+//
+//   summarise   hi_d = max, lo_d = min over the page's tokens of the stored key (code * scale: exact in f16);
+//               m = max_d(|hi_d|, |lo_d|), step = m / 127, codes ceil(127 hi_d / m) and floor(127 lo_d / m): what is held
+//               bounds the keys from both sides.  127 hi_d is exact in fp32 and 127 hi_d / m, where it is no whole number, lies
+//               2^-6 or more away from one (m has 6 significant bits), so one rounded division finds the right whole number
+//   select      u_d = sum_g max(q_gd, 0), w_d = sum_g min(q_gd, 0) over the query heads g of a key/value head: no key of the
+//               page has a larger sum of scores than sum_d (u_d hi_d + w_d lo_d).  Both vectors become whole numbers up to 127
+//               of one step, which does not matter: it is the same for all pages.  The sum of 2 W products of 8-bit
+//               numbers lies below 2^24, so it is exact whatever its order, also as fp32; times the page's step it is
+//               rounded once.  Scores are therefore equal whenever their inputs are, and ties go to the lowest page
+//
+// A summary has 2 W + 16 bytes for the page's 9 W tokens/16 of codes and scales: 1/17 of a page of 64 tokens at W = 128.
+#include "kv_codes.cuh"
+#include "kv_internal.h"
+
+namespace lexi {
+namespace kv {
+namespace {
+
+__device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+// First request i in [0, n) with f(i + 1) > x, n where there is none; f does not fall.  By a whole warp, 32 probes at a time
+template <typename F>
+__device__ __forceinline__ int warp_find(int n, int x, F f) {
+    const int lane = threadIdx.x & 31;
+    int lo = 0, hi = n;
+#pragma unroll 1
+    while (hi - lo > 32) {
+        const int step = (hi - lo + 31) / 32, at = lo + (lane + 1) * step - 1;
+        const int before = __popc(__ballot_sync(0xffffffffu, at < hi && f(min(at, hi - 1) + 1) <= x));
+        lo = min(lo + before * step, hi);
+        hi = min(lo + step, hi);
+    }
+    return lo + __popc(__ballot_sync(0xffffffffu, lo + lane < hi && f(min(lo + lane, n - 1) + 1) <= x));
+}
+
+// Keys and new tokens of a request: as the attention takes them
+struct Request { int len, q0, nq; };
+__device__ __forceinline__ Request request_of(const SelectArgs &a, int i) {
+    const int64_t room = (int64_t)a.width << a.page_shift;
+    Request r{max(a.kv_len[i], 0), a.cu[i], 0};
+    r.nq = a.cu[i + 1] - r.q0;
+    const bool bad_rows = r.q0 < 0 || r.nq < 0 || r.q0 > a.T - r.nq;
+    if (bad_rows || r.len > room) atomicOr(a.status, MOE_KV_STATUS_BAD_INDEX);
+    if (bad_rows) r.nq = 0;
+    r.len = (int)min((int64_t)r.len, room);
+    return r;
+}
+
+// ------------------------------------------------------------------------------------------------ summaries
+
+constexpr int kSumWarps = 4;
+
+// A warp has a page and a head: L = W/32 lanes have 32 dimensions each, 32/L tokens at a time.  A request's pages with new
+// tokens are at most floor(new/P) + 2, so that request i's begin at item cu[i]/P + 2 i and the grid needs no count of them.
+template <int W>
+__global__ void __launch_bounds__(32 * kSumWarps) summarise_kernel(SelectArgs a, long long warps) {
+    constexpr int kLanes = W / 32, kAtOnce = 32 / kLanes;
+    pdl_trigger();
+    pdl_wait();
+    const long long id = (long long)blockIdx.x * kSumWarps + (threadIdx.x >> 5);
+    if (id >= warps) return;
+    const int lane = threadIdx.x & 31, item = (int)(id / a.Hk), head = (int)(id % a.Hk);
+    auto begins = [&](int i) { return (max(a.cu[i], 0) >> a.page_shift) + 2 * i; };
+    const int i = warp_find(a.n, item, begins);
+    if (i >= a.n) return;
+    const Request r = request_of(a, i);
+    const int col = (max(r.len - r.nq, 0) >> a.page_shift) + item - begins(i);
+    if (r.nq == 0 || r.len == 0 || col > (r.len - 1) >> a.page_shift) return;
+    const int page = a.table[(int64_t)i * a.width + col];
+    if (page < 0 || page >= a.n_pages) { if (lane == 0) atomicOr(a.status, MOE_KV_STATUS_BAD_INDEX); return; }
+    const int tokens = min(1 << a.page_shift, r.len - (col << a.page_shift));
+    const int part = lane % kLanes, mine = lane / kLanes;
+    const uint8_t *blocks = a.cache + (((int64_t)page * a.Hk + head) << (a.page_shift - 4)) * block_bytes(W);
+
+    __half2 hi[16], lo[16];
+#pragma unroll
+    for (int d = 0; d < 16; ++d) { hi[d] = __half2half2(__ushort_as_half(0xfc00)); lo[d] = __half2half2(__ushort_as_half(0x7c00)); }
+#pragma unroll 4
+    for (int t = mine; t < tokens; t += kAtOnce) {
+        const uint8_t *blk = blocks + (t >> 4) * block_bytes(W);
+        const uint4 codes = __ldg(reinterpret_cast<const uint4 *>(blk + (t & 15) * (W / 2) + part * 16));
+        const uint32_t two = scales2(__ldg(reinterpret_cast<const uint16_t *>(blk + k_scales_at(W) + (t & 15) * (W / 16) + part * 2)));
+        const uint32_t words[4] = {codes.x, codes.y, codes.z, codes.w};
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const uint32_t sc = __byte_perm(two, 0, w < 2 ? 0x1010 : 0x3232);
+            uint32_t h[4];
+            codes4(words[w], h);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t x = mul2(h[j], sc);
+                const __half2 v = *reinterpret_cast<const __half2 *>(&x);
+                hi[4 * w + j] = __hmax2(hi[4 * w + j], v);
+                lo[4 * w + j] = __hmin2(lo[4 * w + j], v);
+            }
+        }
+    }
+#pragma unroll
+    for (int d = 0; d < 16; ++d)
+#pragma unroll
+        for (int o = kLanes; o < 32; o <<= 1) {
+            hi[d] = __hmax2(hi[d], __shfl_xor_sync(0xffffffffu, hi[d], o));
+            lo[d] = __hmin2(lo[d], __shfl_xor_sync(0xffffffffu, lo[d], o));
+        }
+    float m = 0.f;
+#pragma unroll
+    for (int d = 0; d < 16; ++d) {
+        const float2 x = __half22float2(hi[d]), y = __half22float2(lo[d]);
+        m = fmaxf(m, fmaxf(fmaxf(fabsf(x.x), fabsf(x.y)), fmaxf(fabsf(y.x), fabsf(y.y))));
+    }
+#pragma unroll
+    for (int o = 1; o < kLanes; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+
+    // four of the lanes that have the same dimensions write 16 codes each
+    uint8_t *out = a.summaries + ((int64_t)page * a.Hk + head) * summary_bytes(W);
+    if (mine < 4) {
+        const bool low = mine & 1, second = mine & 2;
+        uint32_t packed[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int d = 0; d < 16; ++d) hi[d] = low ? lo[d] : hi[d];
+#pragma unroll
+        for (int d = 0; d < 8; ++d) hi[d] = second ? hi[8 + d] : hi[d];
+        if (m > 0.f) {
+#pragma unroll
+            for (int d = 0; d < 8; ++d) {
+                const float2 x = __half22float2(hi[d]);
+                const float c0 = __fdiv_rn(x.x * 127.f, m), c1 = __fdiv_rn(x.y * 127.f, m);
+                const int b0 = (int)(low ? floorf(c0) : ceilf(c0)), b1 = (int)(low ? floorf(c1) : ceilf(c1));
+                packed[d / 2] |= (((uint32_t)b0 & 0xffu) | (((uint32_t)b1 & 0xffu) << 8)) << (16 * (d & 1));
+            }
+        }
+        *reinterpret_cast<uint4 *>(out + (low ? W : 0) + part * 32 + (second ? 16 : 0)) = make_uint4(packed[0], packed[1], packed[2], packed[3]);
+    }
+    if (lane == 0) *reinterpret_cast<uint4 *>(out + 2 * W) = make_uint4(__float_as_uint(__fdiv_rn(m, 127.f)), 0u, 0u, 0u);
+}
+
+// 8 dimensions of a page and head a thread
+__global__ void __launch_bounds__(256) read_summaries_kernel(ReadSummariesArgs a, long long threads) {
+    pdl_trigger();
+    pdl_wait();
+    const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
+    if (id >= threads) return;
+    const int eighths = a.D / 8, d = (int)(id % eighths) * 8, head = (int)(id / eighths % a.Hk);
+    const long long at = id / eighths / a.Hk;
+    const int w = padded_width(a.D), page = a.page[at];
+    float hi[8] = {}, lo[8] = {};
+    if (page >= 0 && page < a.n_pages) {
+        const uint8_t *in = a.summaries + ((int64_t)page * a.Hk + head) * summary_bytes(w);
+        const float step = *reinterpret_cast<const float *>(in + 2 * w);
+        const uint2 x = *reinterpret_cast<const uint2 *>(in + d), y = *reinterpret_cast<const uint2 *>(in + w + d);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            hi[i] = (float)(int8_t)((i < 4 ? x.x : x.y) >> (8 * (i & 3))) * step * a.k_scale;
+            lo[i] = (float)(int8_t)((i < 4 ? y.x : y.y) >> (8 * (i & 3))) * step * a.k_scale;
+        }
+    } else if (page != -1) {
+        atomicOr(a.status, MOE_KV_STATUS_BAD_INDEX);
+    }
+    const int64_t to = (at * a.Hk + head) * a.D + d;
+#pragma unroll
+    for (int i = 0; i < 8; i += 4) {
+        *reinterpret_cast<float4 *>(a.high + to + i) = make_float4(hi[i], hi[i + 1], hi[i + 2], hi[i + 3]);
+        *reinterpret_cast<float4 *>(a.low + to + i) = make_float4(lo[i], lo[i + 1], lo[i + 2], lo[i + 3]);
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ selection
+
+constexpr int kWarps = 8, kThreads = 32 * kWarps;
+constexpr int kMaxCluster = 8;
+
+__device__ __forceinline__ float load_q(const float *p) { return __ldg(p); }
+__device__ __forceinline__ float load_q(const __nv_bfloat16 *p) { return __bfloat162float(__ldg(p)); }
+// 32 products of 8-bit numbers for each of 16 pages and 8 tokens
+__device__ __forceinline__ void mma_s8(int (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// whole numbers in the order of the fp32 numbers, which are not -0
+__device__ __forceinline__ uint32_t ordered(float f) {
+    const uint32_t b = __float_as_uint(f);
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ uint32_t cluster_rank() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
+__device__ __forceinline__ uint32_t in_cta0(uint32_t addr) { uint32_t r; asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(addr)); return r; }
+__device__ __forceinline__ void st_cluster(uint32_t addr, uint32_t v) { asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory"); }
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
+// A cluster has TOK tokens of a request and a key/value head; its CTAs have a share of the pages each, 16 of them a warp at a
+// time, and put the scores into the first CTA's shared memory, which selects: a warp for each token, or all warps for one.
+// A request's tiles of TOK are at most floor(new/TOK) + 1: request i's begin at item cu[i]/TOK + i.
+template <typename T, int W, int TOK>
+__global__ void __launch_bounds__(kThreads) select_kernel(SelectArgs a, int cluster) {
+    constexpr int kChunks = 2 * W / 64;                // 64 bytes of a summary: 16 for each of four lanes
+    constexpr int kQRow = 2 * W + 16;
+    extern __shared__ __align__(16) uint32_t scores[];       // [TOK][a.room], in the order of the numbers
+    __shared__ __align__(16) uint8_t q_s[TOK * kQRow];
+    __shared__ int count_s[2][kWarps], ties_s[kWarps];
+    __shared__ uint32_t low_s[kWarps], high_s[kWarps];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r = lane >> 2, c = lane & 3;
+    const int rank = cluster > 1 ? (int)cluster_rank() : 0;
+    const int item = blockIdx.x / cluster, head = blockIdx.y;
+    if (cluster > 1) cluster_arrive();
+    pdl_trigger();
+    pdl_wait();
+
+    auto begins = [&](int i) { return TOK == 1 ? max(a.cu[i], 0) : max(a.cu[i], 0) / TOK + i; };
+    const int i = warp_find(a.n, item, begins);
+    Request q{0, 0, 0};
+    if (i < a.n) q = request_of(a, i);
+    const int tok0 = TOK == 1 ? item - q.q0 : (item - (i < a.n ? begins(i) : 0)) * TOK;          // of the request's new tokens
+    const int many = i < a.n && tok0 >= 0 ? max(min(TOK, q.nq - tok0), 0) : 0;
+    auto own_page = [&](int t) { const int p = q.len - q.nq + tok0 + t; return p < 0 ? -1 : p >> a.page_shift; };
+    // pages [first, top) of the tile's last token are to be scored, if there are more than are wanted
+    const int last_own = many > 0 ? own_page(many - 1) : -1;
+    const int top = last_own >= a.n_select ? last_own - a.last + 1 : 0, from = min(a.first, top);
+
+    if (top > from) {
+        // ---- queries: a warp a token, W/32 neighbouring dimensions a lane; sums in the order of the heads
+        constexpr int kPer = W / 32;
+        for (int t = warp; t < TOK; t += kWarps) {
+            float u[kPer], w[kPer], m = 0.f;
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) u[e] = w[e] = 0.f;
+            if (t < many) {
+                const T *src = (const T *)a.q.p + (int64_t)(q.q0 + tok0 + t) * a.q.ts + (int64_t)head * a.G * a.q.hs + lane * kPer;
+#pragma unroll 4
+                for (int g = 0; g < a.G; ++g)
+#pragma unroll
+                    for (int e = 0; e < kPer; ++e) {
+                        const float x = lane * kPer + e < a.D ? load_q(src + g * a.q.hs + e) : 0.f;
+                        u[e] += fmaxf(x, 0.f);
+                        w[e] += fminf(x, 0.f);
+                    }
+            }
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) m = fmaxf(m, fmaxf(u[e], -w[e]));
+#pragma unroll
+            for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+            const float inv = m > 0.f ? __fdiv_rn(127.f, m) : 0.f;
+            // 0 for infinity times 0; 127 where 127 / m is infinity
+            auto code = [&](float x) { return (uint32_t)max(-127, min(127, __float2int_rn(__fmul_rn(x, inv)))) & 0xffu; };
+            uint32_t cu = 0, cw = 0;
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) {
+                cu |= code(u[e]) << (8 * (e & 3));
+                cw |= code(w[e]) << (8 * (e & 3));
+                if (kPer == 2 && e == 1) {
+                    *reinterpret_cast<uint16_t *>(q_s + t * kQRow + lane * 2) = (uint16_t)cu;
+                    *reinterpret_cast<uint16_t *>(q_s + t * kQRow + W + lane * 2) = (uint16_t)cw;
+                } else if ((e & 3) == 3) {
+                    *reinterpret_cast<uint32_t *>(q_s + t * kQRow + lane * kPer + e - 3) = cu;
+                    *reinterpret_cast<uint32_t *>(q_s + t * kQRow + W + lane * kPer + e - 3) = cw;
+                    cu = cw = 0;
+                }
+            }
+        }
+        __syncthreads();
+        uint4 b[kChunks];
+#pragma unroll
+        for (int x = 0; x < kChunks; ++x)
+            b[x] = r < TOK ? *reinterpret_cast<const uint4 *>(q_s + r * kQRow + c * 16 + 64 * x) : make_uint4(0u, 0u, 0u, 0u);
+
+        // ---- scores of this CTA's pages [begin, end)
+        const int each = ((top - from + cluster - 1) / cluster + 15) & ~15;
+        const int begin = from + rank * each, end = min(begin + each, top);
+        const int32_t *table = a.table + (int64_t)i * a.width;
+        auto page_at = [&](int col) { return col < end ? table[col] : -1; };
+        if (cluster > 1) cluster_wait();          // the first CTA is there
+        const uint32_t to = cluster > 1 ? in_cta0(smem_u32(scores)) : smem_u32(scores);
+        int at = begin + warp * 16, p0 = page_at(at + r), p1 = page_at(at + r + 8);
+#pragma unroll 1
+        for (; at < end; at += kWarps * 16) {
+            const int next = at + kWarps * 16, n0 = page_at(next + r), n1 = page_at(next + r + 8);
+            const bool ok0 = p0 >= 0 && p0 < a.n_pages, ok1 = p1 >= 0 && p1 < a.n_pages;
+            if ((!ok0 && at + r < end) || (!ok1 && at + r + 8 < end)) atomicOr(a.status, MOE_KV_STATUS_BAD_INDEX);
+            // a page that is none scores as one of zeros
+            const uint8_t *s0 = a.summaries + ((int64_t)(ok0 ? p0 : 0) * a.Hk + head) * summary_bytes(W);
+            const uint8_t *s1 = a.summaries + ((int64_t)(ok1 ? p1 : 0) * a.Hk + head) * summary_bytes(W);
+            uint4 x0[kChunks], x1[kChunks];
+            float step0 = 0.f, step1 = 0.f;
+#pragma unroll
+            for (int x = 0; x < kChunks; ++x) {
+                x0[x] = ok0 ? __ldg(reinterpret_cast<const uint4 *>(s0 + c * 16 + 64 * x)) : make_uint4(0u, 0u, 0u, 0u);
+                x1[x] = ok1 ? __ldg(reinterpret_cast<const uint4 *>(s1 + c * 16 + 64 * x)) : make_uint4(0u, 0u, 0u, 0u);
+            }
+            if (ok0) step0 = __ldg(reinterpret_cast<const float *>(s0 + 2 * W));
+            if (ok1) step1 = __ldg(reinterpret_cast<const float *>(s1 + 2 * W));
+            int d[4] = {0, 0, 0, 0};
+#pragma unroll
+            for (int x = 0; x < kChunks; ++x) {
+                mma_s8(d, x0[x].x, x1[x].x, x0[x].y, x1[x].y, b[x].x, b[x].y);
+                mma_s8(d, x0[x].z, x1[x].z, x0[x].w, x1[x].w, b[x].z, b[x].w);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int t = 2 * c + (j & 1), col = at + r + 8 * (j >> 1);
+                if (t < TOK && col < end) {
+                    const uint32_t key = ordered(__fmul_rn((float)d[j], j < 2 ? step0 : step1));
+                    if (cluster > 1) st_cluster(to + (uint32_t)(t * a.room + col - from) * 4u, key);
+                    else scores[t * a.room + col - from] = key;
+                }
+            }
+            p0 = n0; p1 = n1;
+        }
+    } else if (cluster > 1) {
+        cluster_wait();
+    }
+    if (cluster > 1) {
+        cluster_arrive();
+        cluster_wait();
+        if (rank != 0) return;
+    } else {
+        __syncthreads();
+    }
+
+    // ---- the pages: the need-th largest score by its bits, then in the order of the pages
+    constexpr bool kAll = TOK == 1;                    // all warps have the token, and a part of its pages each
+    constexpr int kStride = kAll ? kThreads : 32;
+    const int t = kAll ? 0 : warp, first_lane = kAll ? tid : lane;
+    if (t >= many) return;
+    int32_t *out = a.selected + ((int64_t)(q.q0 + tok0 + t) * a.Hk + head) * a.n_select;
+    const int own = own_page(t);
+    if (own < a.n_select) {
+        for (int x = first_lane; x < a.n_select; x += kStride) out[x] = x <= own ? x : -1;
+        return;
+    }
+    const int need = a.n_select - a.first - a.last, n = own - a.last + 1 - a.first;          // of n pages behind the first, n > need
+    const uint32_t *key = scores + t * a.room;
+    for (int x = first_lane; x < a.first; x += kStride) out[x] = x;
+    for (int x = first_lane; x < a.last; x += kStride) out[a.n_select - a.last + x] = own - a.last + 1 + x;
+    if (need == 0) return;
+    int turn = 0;
+    auto all_of = [&](int mine) {                      // sum over the token's threads
+        const int sum = __reduce_add_sync(0xffffffffu, mine);
+        if (!kAll) return sum;
+        if (lane == 0) count_s[turn][warp] = sum;
+        __syncthreads();
+        int s = 0;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) s += count_s[turn][w];
+        turn ^= 1;
+        return s;
+    };
+    uint32_t least = 0xffffffffu, most = 0u;
+    for (int x = first_lane; x < n; x += kStride) { least = min(least, key[x]); most = max(most, key[x]); }
+    least = __reduce_min_sync(0xffffffffu, least);
+    most = __reduce_max_sync(0xffffffffu, most);
+    if (kAll) {
+        if (lane == 0) { low_s[warp] = least; high_s[warp] = most; }
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) { least = min(least, low_s[w]); most = max(most, high_s[w]); }
+    }
+    // the leading bits that all have are the answer's; below them, a bit is set if `need` scores reach that far
+    const int open = 32 - __clz(least ^ most);
+    uint32_t edge = open == 32 ? 0u : most >> open << open;
+#pragma unroll 1
+    for (int bit = open - 1; bit >= 0; --bit) {
+        const uint32_t reach = edge | 1u << bit;
+        int mine = 0;
+        for (int x = first_lane; x < n; x += kStride) mine += key[x] >= reach;
+        if (all_of(mine) >= need) edge = reach;
+    }
+    // this warp's part of the pages, and how many above and at the edge lie in front of it
+    const int part = kAll ? ((n + kWarps - 1) / kWarps + 31) & ~31 : n, begin = kAll ? min(warp * part, n) : 0, end = min(begin + part, n);
+    int above = 0, ties = 0;
+    for (int x = begin + lane; x < end; x += 32) { above += key[x] > edge; ties += key[x] == edge; }
+    above = __reduce_add_sync(0xffffffffu, above);
+    ties = __reduce_add_sync(0xffffffffu, ties);
+    int all_above = above, above_before = 0, ties_before = 0;
+    if (kAll) {
+        if (lane == 0) { count_s[turn][warp] = above; ties_s[warp] = ties; }
+        __syncthreads();
+        all_above = 0;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+            all_above += count_s[turn][w];
+            if (w < warp) { above_before += count_s[turn][w]; ties_before += ties_s[w]; }
+        }
+    }
+    const int wanted = need - all_above;               // of those at the edge, the first ones
+    int at = a.first + above_before + min(ties_before, wanted);
+#pragma unroll 1
+    for (int x0 = begin; x0 < end; x0 += 32) {
+        const int x = x0 + lane;
+        const uint32_t k = x < end ? key[x] : 0u;
+        const bool tie = x < end && k == edge;
+        const uint32_t tied = __ballot_sync(0xffffffffu, tie), before = (1u << lane) - 1u;
+        const bool take = x < end && (k > edge || (tie && ties_before + __popc(tied & before) < wanted));
+        const uint32_t taken = __ballot_sync(0xffffffffu, take);
+        if (take) out[at + __popc(taken & before)] = a.first + x;
+        at += __popc(taken);
+        ties_before += __popc(tied);
+    }
+}
+
+template <typename T, int W, int TOK>
+cudaError_t launch_tiles(const SelectArgs &given, int sm_count, cudaStream_t s, uint64_t *launches) {
+    SelectArgs a = given;
+    auto k = select_kernel<T, W, TOK>;
+    a.room = a.width;
+    const size_t smem = (size_t)TOK * a.room * sizeof(uint32_t);
+    if (smem > 32 * 1024) {
+        const cudaError_t err = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (err != cudaSuccess) return err;
+    }
+    const long long tiles = TOK == 1 ? a.T : a.T / TOK + a.n;
+    // more CTAs for a token's pages while there are SMs without one and 8 warps have more than a step each
+    int cluster = 1;
+    while (cluster < kMaxCluster && tiles * a.Hk * cluster * 2 <= 2 * sm_count && a.width > cluster * kWarps * 16) cluster *= 2;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(tiles * cluster), (unsigned)a.Hk);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    ++*launches;
+    return cudaLaunchKernelEx(&cfg, k, a, cluster);
+}
+
+template <typename T, int W>
+cudaError_t by_tokens(const SelectArgs &a, int sm_count, cudaStream_t s, uint64_t *launches) {
+    // eight tokens share the reading of the summaries; their scores have to fit
+    const bool eight = a.max_new != 1 && (size_t)8 * a.width * sizeof(uint32_t) <= kSelectSmem;
+    return eight ? launch_tiles<T, W, 8>(a, sm_count, s, launches) : launch_tiles<T, W, 1>(a, sm_count, s, launches);
+}
+
+}  // namespace
+
+cudaError_t launch_summarise(const SelectArgs &a, cudaStream_t s, uint64_t *launches) {
+    const long long warps = ((long long)(a.T >> a.page_shift) + 2 * a.n) * a.Hk;
+    const dim3 grid((unsigned)((warps + kSumWarps - 1) / kSumWarps)), block(32 * kSumWarps);
+    ++*launches;
+    const int w = padded_width(a.D);
+    if (w == 64) return launch_chained(summarise_kernel<64>, grid, block, 0, s, true, a, warps);
+    if (w == 128) return launch_chained(summarise_kernel<128>, grid, block, 0, s, true, a, warps);
+    return launch_chained(summarise_kernel<256>, grid, block, 0, s, true, a, warps);
+}
+
+cudaError_t launch_read_summaries(const ReadSummariesArgs &a, cudaStream_t s, uint64_t *launches) {
+    const long long threads = (long long)a.m * a.Hk * (a.D / 8);
+    ++*launches;
+    return launch_chained(read_summaries_kernel, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s, true, a, threads);
+}
+
+cudaError_t launch_select(const SelectArgs &a, int sm_count, cudaStream_t s, uint64_t *launches) {
+    const int w = padded_width(a.D);
+    if (a.dtype == MOE_BF16)
+        return w == 64 ? by_tokens<__nv_bfloat16, 64>(a, sm_count, s, launches) : w == 128 ? by_tokens<__nv_bfloat16, 128>(a, sm_count, s, launches)
+                                                                                 : by_tokens<__nv_bfloat16, 256>(a, sm_count, s, launches);
+    return w == 64 ? by_tokens<float, 64>(a, sm_count, s, launches) : w == 128 ? by_tokens<float, 128>(a, sm_count, s, launches)
+                                                                      : by_tokens<float, 256>(a, sm_count, s, launches);
+}
+
+}  // namespace kv
+}  // namespace lexi

@@ -12,6 +12,19 @@ tables and the free list are the caller's tensors:
     q = plan.append(q, k, v, slot, cache, positions=position, turns=turns)      # turned queries; keys and values stored
     o = plan.attention(q, cu, kv_len, block_table, cache, max_new=1)
 
+Requests behind one prefix, whose rows of the block table begin with the same pages (cu_group: the first request of each
+group, and the end):
+
+    shared_len, start = plan.shared_prefix(cu_group, cu, kv_len, block_table)   # once a step
+    o = plan.attention_shared(q, cu, kv_len, block_table, cache, cu_group, shared_len, start, max_new=1)
+
+Attention over the pages that a cheap score selects for each token and key/value head:
+
+    summaries = plan.new_summaries(n_pages)                           # one per layer
+    plan.summarise(cu, kv_len, block_table, cache, summaries, n_tokens)         # behind append
+    selected = plan.select(q, cu, kv_len, block_table, summaries, n_select=32, first=1, last=2, max_new=1)
+    o = plan.attention_selected(q, cu, kv_len, block_table, cache, selected)
+
 ``decoder.py`` runs them together with the MoE layer.
 """
 from __future__ import annotations
@@ -32,6 +45,8 @@ SCALINGS = {"plain": 0, "linear": 1, "base": 2, "parts": 3, "bands": 4}
 EXPORTS = (
     "moe_kv_plan_create", "moe_kv_plan_destroy", "moe_kv_plan_workspace_bytes", "moe_kv_plan_launch_count", "moe_kv_page_bytes",
     "moe_kv_device_status", "moe_kv_tables", "moe_rope_table", "moe_rope", "moe_kv_append", "moe_kv_read", "moe_kv_attention",
+    "moe_kv_shared_prefix", "moe_kv_shared_scratch_bytes", "moe_kv_attention_shared", "moe_kv_summary_bytes", "moe_kv_summarise",
+    "moe_kv_read_summaries", "moe_kv_select", "moe_kv_attention_selected",
 )
 
 
@@ -72,8 +87,17 @@ def load_library() -> ctypes.CDLL:
     lib.moe_kv_append.argtypes = [vp, rows, rows, rows, i32, vp, vp, i32, i32, i32, vp, f32, f32, vp, vp, i32, vp]
     lib.moe_kv_read.argtypes = [vp, vp, i32, vp, i32, f32, f32, vp, vp, vp]
     lib.moe_kv_attention.argtypes = [vp, rows, i32, vp, vp, i32, i32, vp, i32, vp, i32, f32, f32, f32, i32, i32, vp, vp]
+    lib.moe_kv_shared_prefix.argtypes = [vp, vp, i32, vp, vp, i32, vp, i32, vp, vp, vp]
+    lib.moe_kv_shared_scratch_bytes.argtypes = [vp, i32, i32]
+    lib.moe_kv_attention_shared.argtypes = [vp, rows, i32, vp, vp, i32, i32, vp, i32, vp, i32, vp, i32, i32, vp, vp, f32, f32, f32, vp, u64, vp, vp]
+    lib.moe_kv_summary_bytes.argtypes = [P(moe_kv_config_t)]
+    lib.moe_kv_summarise.argtypes = [vp, vp, vp, i32, i32, vp, i32, vp, i32, vp, vp]
+    lib.moe_kv_read_summaries.argtypes = [vp, vp, i32, vp, i32, f32, vp, vp, vp]
+    lib.moe_kv_select.argtypes = [vp, rows, i32, vp, vp, i32, i32, vp, i32, vp, i32, i32, i32, i32, vp, vp]
+    lib.moe_kv_attention_selected.argtypes = [vp, rows, i32, vp, vp, i32, vp, i32, vp, i32, vp, i32, f32, f32, f32, vp, vp]
+    sizes = ("moe_kv_plan_workspace_bytes", "moe_kv_plan_launch_count", "moe_kv_page_bytes", "moe_kv_shared_scratch_bytes", "moe_kv_summary_bytes")
     for name in EXPORTS:
-        getattr(lib, name).restype = u64 if name in ("moe_kv_plan_workspace_bytes", "moe_kv_plan_launch_count", "moe_kv_page_bytes") else ctypes.c_int
+        getattr(lib, name).restype = u64 if name in sizes else ctypes.c_int
     _lib = lib
     return lib
 
@@ -165,6 +189,16 @@ class KVPlan:
         return torch.zeros((n_pages, self.n_kv_heads, blocks, self.page_bytes // (self.n_kv_heads * blocks)), dtype=torch.uint8,
                            device=torch.device("cuda", self.device) if device is None else device)
 
+    @property
+    def summary_bytes(self) -> int:
+        """Bytes of one page's summaries."""
+        return int(self._lib.moe_kv_summary_bytes(ctypes.byref(self.cfg)))
+
+    def new_summaries(self, n_pages: int, device=None) -> torch.Tensor:
+        """Empty summaries of one layer's cache, on the plan's device: [n_pages, n_kv_heads, bytes] uint8."""
+        return torch.zeros((n_pages, self.n_kv_heads, self.summary_bytes // self.n_kv_heads), dtype=torch.uint8,
+                           device=torch.device("cuda", self.device) if device is None else device)
+
     def _call(self, what: str, f, *args, stream=None):
         """One native call on the current stream, or on `stream` (what it allocates then belongs to that stream)."""
         if stream is not None and stream != torch.cuda.current_stream(self.device):
@@ -203,4 +237,43 @@ class KVPlan:
         """Attention of the new tokens' queries [tokens, n_heads, head_dim] over their requests' caches (``moe_kv_attention``).
         max_new: the largest number of new tokens of a request (0 = unknown); it chooses kernels, not results."""
         return self._call("moe_kv_attention", self._native.attention, self._plan, q, cu_new, kv_len, block_table, cache, max_new, window, sinks,
+                          self.default_scale if softmax_scale is None else softmax_scale, k_scale, v_scale, out, stream=stream)[1]
+
+    def shared_prefix(self, cu_group: torch.Tensor, cu_new: torch.Tensor, kv_len: torch.Tensor, block_table: torch.Tensor, stream=None):
+        """(shared_len of each group, start of each request): how many leading keys the members of groups of consecutive
+        requests have in common by their rows of the block table (``moe_kv_shared_prefix``)."""
+        return self._call("moe_kv_shared_prefix", self._native.shared_prefix, self._plan, cu_group, cu_new, kv_len, block_table, stream=stream)[1:]
+
+    def attention_shared(self, q: torch.Tensor, cu_new: torch.Tensor, kv_len: torch.Tensor, block_table: torch.Tensor, cache: torch.Tensor,
+                         cu_group: torch.Tensor, shared_len: torch.Tensor, start: torch.Tensor, *, max_new: int = 0, max_group: int = 0,
+                         softmax_scale: Optional[float] = None, k_scale: float = 1.0, v_scale: float = 1.0, out: Optional[torch.Tensor] = None,
+                         stream=None) -> torch.Tensor:
+        """``attention`` without a window, a group's shared prefix read once for all its members (``moe_kv_attention_shared``).
+        shared_len, start: of ``shared_prefix`` for the same groups, lengths and table.  max_new, max_group: the largest
+        number of new tokens of a request and of a group (0 = unknown); they choose kernels, not results."""
+        return self._call("moe_kv_attention_shared", self._native.attention_shared, self._plan, q, cu_new, kv_len, block_table, cache, cu_group,
+                          shared_len, start, max_new, max_group, self.default_scale if softmax_scale is None else softmax_scale, k_scale, v_scale, out,
+                          stream=stream)[1]
+
+    def summarise(self, cu_new: torch.Tensor, kv_len: torch.Tensor, block_table: torch.Tensor, cache: torch.Tensor, summaries: torch.Tensor,
+                  n_tokens: int, stream=None) -> None:
+        """Bounds of the keys of every page that holds one of the n_tokens new tokens, into `summaries` (``moe_kv_summarise``)."""
+        self._call("moe_kv_summarise", self._native.summarise, self._plan, cu_new, kv_len, block_table, cache, summaries, n_tokens, stream=stream)
+
+    def read_summaries(self, summaries: torch.Tensor, pages: torch.Tensor, *, k_scale: float = 1.0, stream=None):
+        """(high, low) [pages, n_kv_heads, head_dim] fp32: the bounds of the listed pages' keys (``moe_kv_read_summaries``)."""
+        return self._call("moe_kv_read_summaries", self._native.read_summaries, self._plan, summaries, pages, k_scale, stream=stream)[1:]
+
+    def select(self, q: torch.Tensor, cu_new: torch.Tensor, kv_len: torch.Tensor, block_table: torch.Tensor, summaries: torch.Tensor, *, n_select: int,
+               first: int = 1, last: int = 1, max_new: int = 0, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """[tokens, n_kv_heads, n_select] int32: columns of the token's row of the block table, ascending, -1 behind the last: the
+        first and last pages and those whose bounds promise the largest scores (``moe_kv_select``)."""
+        return self._call("moe_kv_select", self._native.select, self._plan, q, cu_new, kv_len, block_table, summaries, n_select, first, last, max_new, out,
+                          stream=stream)[1]
+
+    def attention_selected(self, q: torch.Tensor, cu_new: torch.Tensor, kv_len: torch.Tensor, block_table: torch.Tensor, cache: torch.Tensor,
+                           selected: torch.Tensor, *, softmax_scale: Optional[float] = None, k_scale: float = 1.0, v_scale: float = 1.0,
+                           out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """Attention of the new tokens over the pages listed for them and each key/value head (``moe_kv_attention_selected``)."""
+        return self._call("moe_kv_attention_selected", self._native.attention_selected, self._plan, q, cu_new, kv_len, block_table, cache, selected,
                           self.default_scale if softmax_scale is None else softmax_scale, k_scale, v_scale, out, stream=stream)[1]

@@ -1,0 +1,778 @@
+"""Shared prefixes and selected pages of the 4-bit cache (include/moe_kv.h) against plain implementations
+(kv_selected_reference.py, kv_reference.py).
+
+Whole numbers (lengths, columns, stored bytes) have to be equal.  Attention keeps the bound that test_kv_cache.py derives: with
+A = sum_j w_j |v_j|, n keys and X = c max_j sum_d |q_d k_jd| of a row, |error| <= A (2 e + n 2^-22) + the output's rounding, e the
+rounding of a weight + 2^-21 + X W 2^-23.  Joining a prefix's sums with the rest's is one more rounded factor (ex2 and a product:
+2^-22 + 2^-24) and one more sum (2^-24) on each side of the division, as the joins of pieces that a long context has
+anyway: with n >= 2 keys, which a row of two parts has, n 2^-22 covers it.
+"""
+import ctypes
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import kv_reference as ref
+import kv_selected_reference as plain
+from paper_2509_02753_b200 import binding as B
+from paper_2509_02753_b200 import kv_cache as K
+
+gpu = pytest.mark.gpu
+BF16, F32 = torch.bfloat16, torch.float32
+UNIT = {t: torch.finfo(t).eps for t in (BF16, F32)}
+KS, VS = 0.05, 0.02
+
+
+def plan_for(heads=4, kv=2, dim=64, page=16, dtype=F32, requests=16, tokens=4096):
+    return K.KVPlan(n_heads=heads, n_kv_heads=kv, head_dim=dim, page_size=page, dtype=dtype, max_requests=requests, max_tokens=tokens)
+
+
+def i32(a):
+    return torch.as_tensor(np.asarray(a, np.int32)).cuda()
+
+
+def host(t):
+    return t.float().cpu().numpy() if t.dtype == BF16 else t.cpu().numpy()
+
+
+def queries(rng, tokens, heads, dim, dtype, pad=0):
+    """Rows of a wider tensor: `pad` elements behind each head."""
+    x = torch.from_numpy(rng.standard_normal((tokens, heads, dim + pad)).astype(np.float32)).to(dtype).cuda()
+    return x[..., :dim]
+
+
+class Batch:
+    """Requests whose first pages are shared by groups, a cache whose unused bytes are NaN scales, unused entries of the table that are no pages."""
+
+    def __init__(self, seed, lens, new, heads, kv, dim, page, dtype, groups=(), shared=(), pad=0, extra_rows=0, columns=0, loud=1.0):
+        rng = np.random.default_rng(seed)
+        n = len(lens)
+        held = [-(-x // page) for x in lens]
+        width = max(max(held + [1]) + 1, columns)
+        self.table = np.full((n, width), 1 << 30)
+        order, at = rng.permutation(sum(held) + 2), 0
+        for i in range(n):
+            self.table[i, : held[i]] = order[at: at + held[i]]
+            at += held[i]
+        for g, pages in enumerate(shared):
+            self.table[groups[g]: groups[g + 1], :pages] = self.table[groups[g], :pages]
+        self.cache = np.full((len(order), kv, page // 16, ref.block_bytes(dim)), 0x7F, np.uint8)
+        done = set()
+        for i in range(n):
+            todo = [j for j in range(lens[i]) if (self.table[i, j // page], j % page) not in done]
+            done |= {(self.table[i, j // page], j % page) for j in todo}
+            if todo:
+                x = rng.standard_normal((2, len(todo), kv, dim)).astype(np.float32)
+                x[0, :, :, dim // 3] *= 6 * loud
+                ref.store(self.cache, x[0], x[1], [int(self.table[i, j // page]) * page + j % page for j in todo], page, KS, VS)
+        self.lens, self.new, self.page, self.dtype, self.heads, self.kv, self.dim = lens, new, page, dtype, heads, kv, dim
+        self.cu = np.concatenate(([0], np.cumsum(new))).astype(np.int32)
+        self.q = queries(rng, int(self.cu[-1]) + extra_rows, heads, dim, dtype, pad)
+        self.args = (self.q, i32(self.cu), i32(lens), i32(self.table))
+        self.pages = torch.from_numpy(self.cache).cuda()
+
+    def plan(self):
+        return plan_for(self.heads, self.kv, self.dim, self.page, self.dtype, requests=len(self.lens), tokens=max(1, self.q.shape[0]))
+
+    def near(self, got, want, spread, exponent, count):
+        n = int(self.cu[-1])
+        e = (2.0 ** -11 if self.dtype == BF16 else 2.0 ** -21) + 2.0 ** -21 + exponent * ref.width(self.dim) * 2.0 ** -23
+        limit = (spread * (2 * e + count * 2.0 ** -22) + np.abs(want) * UNIT[self.dtype] / 2 + 1e-30)[:n]
+        err = np.abs(host(got)[:n] - want[:n])
+        assert np.isfinite(host(got)[:n]).all()
+        assert (err <= limit).all(), f"{(err / limit).max()} of the bound"
+
+    def reference(self):
+        n = int(self.cu[-1])
+        return ref.attention(host(self.q)[:n], self.cu, self.lens, self.table, self.cache, self.page, 0, 0, 1.0 / math.sqrt(self.dim), float(np.float32(KS)), float(np.float32(VS)))
+
+
+# ------------------------------------------------------------------------------------------ no device needed
+
+@pytest.mark.parametrize("dim, kv, want", [(8, 1, 144), (64, 2, 288), (80, 3, 3 * 272), (128, 8, 8 * 272), (136, 5, 5 * 528), (256, 1, 528)])
+def test_summary_bytes(dim, kv, want):
+    cfg = K.moe_kv_config_t(kv, kv, dim, 16, 1, 1, 1)
+    assert K.load_library().moe_kv_summary_bytes(ctypes.byref(cfg)) == want
+    assert K.load_library().moe_kv_summary_bytes(ctypes.byref(K.moe_kv_config_t(kv, kv, dim + 4, 16, 1, 1, 1))) == 0
+
+
+def test_null_arguments():
+    lib = K.load_library()
+    assert lib.moe_kv_summary_bytes(None) == 0 and lib.moe_kv_shared_scratch_bytes(None, 1, 1) == 0
+    assert lib.moe_kv_shared_prefix(None, None, 0, None, None, 0, None, 0, None, None, None) == -1
+    assert lib.moe_kv_attention_shared(None, None, 0, None, None, 0, 0, None, 0, None, 0, None, 0, 0, None, None, 1.0, 1.0, 1.0, None, 0, None, None) == -1
+    assert lib.moe_kv_summarise(None, None, None, 0, 0, None, 0, None, 0, None, None) == -1
+    assert lib.moe_kv_read_summaries(None, None, 0, None, 0, 1.0, None, None, None) == -1
+    assert lib.moe_kv_select(None, None, 0, None, None, 0, 0, None, 0, None, 0, 1, 0, 1, None, None) == -1
+    assert lib.moe_kv_attention_selected(None, None, 0, None, None, 0, None, 0, None, 0, None, 1, 1.0, 1.0, 1.0, None, None) == -1
+
+
+def test_a_bound_is_the_next_whole_number():
+    """The kernel divides 127 x by the largest magnitude in fp32 and rounds outwards; in whole numbers, over every pair of
+    magnitudes that a code (0 to 12 halves) times the fraction of a scale (8 to 15 eighths) can have, up to powers of two.
+    Outside of 2^-8 to 1 the quotient is a whole number below 1 (or none), for which the same holds with more room."""
+    odd = sorted({c * f for c in (1, 2, 3, 4, 6, 8, 12) for f in range(8, 16)})
+    for m in odd:
+        for x in odd:
+            for shift in range(-8, 8):
+                num, den = (x << shift, m) if shift >= 0 else (x, m << -shift)
+                if num > den:
+                    continue
+                assert int(np.ceil(np.float32(127 * num) / np.float32(den))) == -(-127 * num // den)
+
+
+# ------------------------------------------------------------------------------------------ shared prefixes
+
+def check_prefix(groups, new, lens, table, page, bits=0, want=None):
+    cu = np.concatenate(([0], np.cumsum(new))).astype(np.int32)
+    with plan_for(page=page, requests=max(1, len(lens), len(groups) - 1)) as plan:
+        shared, start = plan.shared_prefix(i32(groups), i32(cu), i32(lens), i32(np.asarray(table).reshape(len(lens), -1)))
+        status = plan.device_status()
+    got = shared.tolist(), start.tolist()
+    assert got == (plain.shared_prefix(groups, cu, lens, table, page) if want is None else want)
+    assert status == ((-8, bits) if bits else (0, 0))
+
+
+@gpu
+@pytest.mark.parametrize("page", [16, 128])
+@pytest.mark.parametrize("n, groups, width", [(1, [0, 1], 3), (2, [0, 2], 1), (5, [0, 2, 2, 5], 40), (9, [2, 4, 7], 7), (40, [0, 40], 130), (70, [0, 1, 3, 70], 513), (600, [0, 300, 600], 70),
+                                              (3, [], 4), (3, [1], 4)])
+def test_shared_prefix(n, groups, width, page):
+    rng = np.random.default_rng(n + width)
+    groups = groups or [0]
+    for extra in range(3):
+        table = rng.integers(0, 1000, (n, width))
+        lens = rng.integers(1, width * page + 1, n)
+        new = np.minimum(rng.integers(0, 4, n), lens)
+        for g in range(len(groups) - 1):
+            members = slice(groups[g], groups[g + 1])
+            common = int(rng.integers(0, width + 1)) if extra else width
+            if common:
+                table[members, :common] = rng.integers(0, 1000, common)
+            if extra == 2:
+                lens[members] = width * page
+        check_prefix(groups, new, lens, table, page)
+
+
+@gpu
+def test_what_is_not_shared():
+    table = np.tile(np.arange(6), (4, 1))
+    check_prefix([0, 4], [1, 1, 1, 1], [80, 64, 65, 96], table, 16)         # 64 keys: the last is new, 3 full pages in front
+    check_prefix([0, 4], [0, 0, 0, 0], [80, 64, 65, 96], table, 16)
+    check_prefix([0, 4], [1, 70, 1, 1], [80, 64, 65, 96], table, 16)        # more new tokens than keys
+    gone = table.copy()
+    gone[:, 2] = -1
+    check_prefix([0, 4], [1, 1, 1, 1], [96] * 4, gone, 16)
+    zeros = ([0], [0, 0, 0, 0])
+    check_prefix([0, 4], [1, 1, 1, 1], [96, -5, 96, 96], table, 16, K.STATUS_BAD_INDEX, zeros)
+    check_prefix([0, 4], [1, 1, 1, 1], [96, 97, 96, 96], table, 16, K.STATUS_BAD_INDEX, zeros)
+    check_prefix([0, 5], [1, 1, 1, 1], [96] * 4, table, 16, K.STATUS_BAD_INDEX, zeros)
+    check_prefix([-1, 4], [1, 1, 1, 1], [96] * 4, table, 16, K.STATUS_BAD_INDEX, zeros)
+    check_prefix([0, 3, 2, 4], [1, 1, 1, 1], [96] * 4, table, 16, K.STATUS_BAD_INDEX, ([0, 0, 0], [0, 0, 0, 0]))
+
+
+def shared_case(seed, lens, new, heads, kv, dim, page, dtype, groups, shared, max_new=None, max_group=None, scale=None, **more):
+    b = Batch(seed, lens, new, heads, kv, dim, page, dtype, groups, shared, **more)
+    with b.plan() as plan:
+        g = i32(groups)
+        length, start = plan.shared_prefix(g, *b.args[1:])
+        assert (length.tolist(), start.tolist()) == plain.shared_prefix(groups, b.cu, lens, b.table, page)
+        out = torch.full(b.q.shape, 7.0, dtype=dtype, device="cuda")
+        group = max([0] + [int(b.cu[groups[x + 1]] - b.cu[groups[x]]) for x in range(len(groups) - 1)])
+        hints = dict(max_new=max(new) if max_new is None else max_new, max_group=group if max_group is None else max_group, k_scale=KS, v_scale=VS)
+        before = plan.launch_count
+        got = plan.attention_shared(*b.args, b.pages, g, length, start, out=out, **hints)
+        launches = plan.launch_count - before
+        again = plan.attention_shared(*b.args, b.pages, g, length, start, **hints)
+        assert plan.device_status() == (0, 0)
+    assert got is out and bool((got[b.cu[-1]:] == 7).all())
+    assert torch.equal(got[: b.cu[-1]], again[: b.cu[-1]]), "equal calls give equal bits"
+    b.near(got, *b.reference())
+    return launches
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("dim", [64, 128, 256, 8, 80, 200])
+def test_single_tokens_behind_a_prefix(dim, dtype):
+    assert shared_case(1, [49, 33, 100], [1, 1, 1], 4, 2, dim, 16, dtype, [0, 3], [2]) == 2
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("heads, kv", [(1, 1), (3, 3), (7, 1), (8, 1), (9, 1), (16, 1), (17, 1), (15, 5)])
+def test_head_layouts_behind_a_prefix(heads, kv, dtype):
+    shared_case(2, [70, 65, 130, 65], [1, 1, 1, 1], heads, kv, 64, 32, dtype, [0, 4], [2], pad=3)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("page", [16, 32, 64, 128])
+def test_pages_groups_and_several_tokens(page, dtype):
+    """A request of no group in front, a group of one, a group that shares nothing, one whose new tokens begin a page."""
+    lens = [5, 3 * page + 1, 2 * page + 7, 2 * page + 3, page + 2, 20, 33, 2 * page, 9]
+    shared_case(3, lens, [2, 1, 3, 1, 2, 4, 0, 2, 1], 4, 2, 80, page, dtype, [1, 4, 5, 7, 9], [2, 0, 0, 0])
+    shared_case(4, lens, [2, 1, 3, 1, 2, 4, 0, 2, 1], 4, 2, 80, page, dtype, [1, 4, 5, 7, 9], [1, 0, 0, 0], extra_rows=3)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_groups_of_many_rows_are_prompts_to_the_tensor_cores(dim, dtype):
+    """36 and 72 rows a key/value head: tiles of 128 rows; then groups of many and few rows in one call."""
+    lens = [300 + 7 * i for i in range(18)]
+    assert shared_case(5, lens, [1] * 18, 8, 2, dim, 16, dtype, [0, 18], [18]) == 2
+    assert shared_case(6, lens, [2] * 18, 4, 2, dim, 16, dtype, [0, 18], [17], pad=1) == 2
+    assert shared_case(7, lens, [1] * 18, 8, 2, dim, 16, dtype, [0, 15, 18], [18, 19]) == (2 if dim == 256 else 3)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_a_group_of_more_rows_than_a_tile(dtype):
+    shared_case(8, [130 + i for i in range(70)], [1] * 70, 8, 1, 64, 64, dtype, [0, 70], [2])
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_a_long_prefix_is_split(dtype):
+    shared_case(9, [3000 + 11 * i for i in range(4)], [1] * 4, 4, 2, 64, 64, dtype, [0, 4], [46])
+    shared_case(10, [2600 + 11 * i for i in range(20)], [1] * 20, 8, 2, 64, 64, dtype, [0, 20], [40])
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_hints_choose_kernels_not_results(dtype):
+    lens, new, groups = [100, 90, 70, 81, 200, 120], [1, 2, 1, 1, 3, 1], [0, 4, 6]
+    for max_new, max_group in ((3, 0), (1, 1), (0, 0), (9, 2), (3, 100)):
+        shared_case(11, lens, new, 4, 2, 64, 16, dtype, groups, [4, 7], max_new=max_new, max_group=max_group)
+
+
+@gpu
+def test_requests_of_many_rows_read_their_keys_themselves():
+    assert shared_case(12, [100, 90], [40, 1], 4, 2, 64, 16, BF16, [0, 2], [3]) == 1          # a prompt and a token
+    assert shared_case(12, [100, 100], [40, 40], 4, 2, 64, 16, BF16, [0, 2], [3]) == 1
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_many_groups(dtype):
+    lens = [20 + i % 37 for i in range(300)]
+    shared_case(13, lens, [1] * 300, 2, 1, 64, 16, dtype, list(range(0, 301, 3)), [1] * 100)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_peaked_weights_on_either_side(dtype):
+    for loud in (0.02, 8.0):
+        shared_case(14, [200, 180, 190], [1, 1, 1], 4, 2, 64, 16, dtype, [0, 3], [6], loud=loud)
+
+
+@gpu
+def test_starts_that_are_none():
+    b = Batch(15, [40, 50], [1, 1], 4, 2, 64, 16, F32, [0, 2], [2])
+    with b.plan() as plan:
+        for start in ([32, 50], [-1, 32], [1 << 30, 32]):
+            plan.attention_shared(*b.args, b.pages, i32([0, 2]), i32([32]), i32(start), max_new=1, max_group=2, k_scale=KS, v_scale=VS)
+            assert plan.device_status() == (-8, K.STATUS_BAD_INDEX)
+        for groups in ([0, 3], [-1, 2], [2, 0]):
+            plan.attention_shared(*b.args, b.pages, i32(groups), i32([32]), i32([0, 0]), max_new=1, max_group=2, k_scale=KS, v_scale=VS)
+            assert plan.device_status() == (-8, K.STATUS_BAD_INDEX)
+
+
+# ------------------------------------------------------------------------------------------ summaries
+
+@gpu
+@pytest.mark.parametrize("dim", [8, 64, 80, 128, 136, 256])
+@pytest.mark.parametrize("page", [16, 32, 64, 128])
+def test_summaries(page, dim):
+    """Pages that only hold tokens of before keep their bytes; a page's tokens behind the last count for nothing (their scales are NaN)."""
+    lens, new = [1, page, 3 * page + 5, 2 * page + 1, 0, 40], [1, 1, 2 * page + 1, 1, 0, 0]
+    b = Batch(dim + page, lens, new, 3, 3, dim, page, BF16)
+    touched = [(i, c) for i in range(len(lens)) for c in range((lens[i] - new[i]) // page, -(-lens[i] // page)) if new[i]]
+    pages = [int(b.table[i, c]) for i, c in touched]
+    keys = ref.decode_all(b.cache, dim)[0]
+    want = np.full((len(b.cache), 3, 2 * ref.width(dim) + 16), 9, np.uint8)
+    high, low = np.zeros((len(pages), 3, dim), np.float32), np.zeros((len(pages), 3, dim), np.float32)
+    for x, ((i, c), pg) in enumerate(zip(touched, pages)):
+        for h in range(3):
+            up, down, step = plain.summary(keys[pg, h, : min(page, lens[i] - c * page)])
+            want[pg, h] = plain.entry(up, down, step, dim)
+            high[x, h], low[x, h] = up.astype(np.float32) * step * np.float32(KS), down.astype(np.float32) * step * np.float32(KS)
+    with b.plan() as plan:
+        got = plan.new_summaries(len(b.cache)).fill_(9)
+        for tokens in (int(b.cu[-1]), int(b.cu[-1]), plan.cfg.max_tokens):
+            plan.summarise(*b.args[1:], b.pages, got, tokens)
+        assert plan.device_status() == (0, 0)
+        assert np.array_equal(got.cpu().numpy(), want)
+        a, z = plan.read_summaries(got, i32(pages), k_scale=KS)
+        assert np.array_equal(a.cpu().numpy(), high) and np.array_equal(z.cpu().numpy(), low)
+        a, z = plan.read_summaries(got, i32([-1, pages[0], -1]), k_scale=KS)
+        assert plan.device_status() == (0, 0)
+        assert not a[0].any() and not z[2].any() and np.array_equal(a[1].cpu().numpy(), high[0])
+        a, z = plan.read_summaries(got, i32([len(b.cache), -2]), k_scale=KS)
+        assert plan.device_status() == (-8, K.STATUS_BAD_INDEX) and not a.any() and not z.any()
+
+
+@gpu
+def test_summaries_of_many_requests_and_pages_that_are_none():
+    lens, new = [1 + i % 50 for i in range(200)], [i % 3 for i in range(200)]
+    new = [min(a, x) for a, x in zip(new, lens)]
+    b = Batch(3, lens, new, 1, 1, 64, 16, F32)
+    keys = ref.decode_all(b.cache, 64)[0]
+    with b.plan() as plan:
+        got = plan.new_summaries(len(b.cache))
+        plan.summarise(*b.args[1:], b.pages, got, int(b.cu[-1]))
+        assert plan.device_status() == (0, 0)
+        got = got.cpu().numpy()
+        for i in range(200):
+            for c in range((lens[i] - new[i]) // 16, -(-lens[i] // 16)):
+                if new[i]:
+                    pg = b.table[i, c]
+                    assert np.array_equal(got[pg, 0], plain.entry(*plain.summary(keys[pg, 0, : min(16, lens[i] - 16 * c)]), 64))
+        table = b.table.copy()
+        table[5, 0], table[8, 0] = -1, len(b.cache)
+        again = plan.new_summaries(len(b.cache))
+        plan.summarise(b.args[1], b.args[2], i32(table), b.pages, again, int(b.cu[-1]))
+        assert plan.device_status() == (-8, K.STATUS_BAD_INDEX)
+        same = np.ones(len(b.cache), bool)
+        same[[b.table[5, 0], b.table[8, 0]]] = False
+        assert np.array_equal(again.cpu().numpy()[same], got[same])
+
+
+# ------------------------------------------------------------------------------------------ selection
+
+def select_case(seed, lens, new, heads, kv, dim, page, dtype, n_select, first, last, max_new=None, pad=0, extra_rows=0, columns=0, coarse=False, change=None, bits=0):
+    """Summaries of any bytes; `coarse`: of few values and one step, so that many scores are equal."""
+    rng = np.random.default_rng(seed)
+    n = len(lens)
+    held = [-(-x // page) for x in lens]
+    n_pages, width = sum(held) + 2, max(max(held + [1]), columns)
+    table = np.full((n, width), 1 << 30)
+    order, at = rng.permutation(n_pages), 0
+    for i in range(n):
+        table[i, : held[i]] = order[at: at + held[i]]
+        at += held[i]
+    w = ref.width(dim)
+    summaries = np.zeros((n_pages, kv, 2 * w + 16), np.uint8)
+    codes = rng.integers(-1, 2, (2, n_pages, kv, dim)) * (rng.random(dim) < 4 / dim) if coarse else rng.integers(-127, 128, (2, n_pages, kv, dim))
+    summaries[..., :dim], summaries[..., w: w + dim] = (x.astype(np.int8).view(np.uint8) for x in codes)
+    steps = np.ones((n_pages, kv, 1), np.float32) if coarse else (0.5 + rng.random((n_pages, kv, 1))).astype(np.float32)
+    summaries[..., 2 * w: 2 * w + 4] = steps.view(np.uint8)
+    cu = np.concatenate(([0], np.cumsum(new))).astype(np.int32)
+    q = queries(rng, int(cu[-1]) + extra_rows, heads, dim, dtype, pad)
+    if change:
+        change(q, table, n_pages)
+    want = plain.select(host(q), cu, lens, table, summaries, kv, page, n_select, first, last)
+    with plan_for(heads, kv, dim, page, dtype, requests=n, tokens=max(1, q.shape[0])) as plan:
+        out = torch.full((q.shape[0], kv, n_select), -2, dtype=torch.int32, device="cuda")
+        got = plan.select(q, i32(cu), i32(lens), i32(table), torch.from_numpy(summaries).cuda(), n_select=n_select, first=first, last=last,
+                          max_new=max(new) if max_new is None else max_new, out=out)
+        assert plan.device_status() == ((-8, bits) if bits else (0, 0))
+    assert got is out
+    assert np.array_equal(got.cpu().numpy(), want)
+    return want
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("dim", [8, 64, 80, 128, 136, 256])
+@pytest.mark.parametrize("new", [1, 5])
+def test_select(dim, dtype, new):
+    select_case(dim, [16 * 40, 16 * 33 + 1, 700, 90, new], [new] * 5, 6, 2, dim, 16, dtype, 12, 1, 2, pad=3)
+
+
+@gpu
+@pytest.mark.parametrize("first, last, n_select", [(0, 1, 1), (0, 1, 2), (1, 1, 2), (2, 3, 5), (0, 5, 9), (4, 1, 30), (1, 2, 64), (0, 1, 33)])
+@pytest.mark.parametrize("coarse", [False, True])
+def test_how_many_are_selected(first, last, n_select, coarse):
+    """Also of pages as many as wanted, one more, one less; coarse scores: ties at the edge."""
+    for new in (1, 11):
+        lens = [16 * n_select, 16 * n_select + 1, 16 * n_select - 1, 16 * n_select + 17, 16 * 100, 16 * 33 + 5]
+        select_case(n_select, [max(x, new) for x in lens], [new] * 6, 4, 2, 64, 16, F32, n_select, first, last, coarse=coarse)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("heads, kv", [(1, 1), (5, 5), (8, 1), (13, 1), (32, 2)])
+def test_select_head_layouts(heads, kv, dtype):
+    select_case(heads, [32 * 20, 32 * 9 + 3], [1, 1], heads, kv, 128, 32, dtype, 6, 1, 1)
+    select_case(heads, [32 * 20, 32 * 9 + 3], [9, 20], heads, kv, 128, 32, dtype, 6, 1, 1, extra_rows=2)
+
+
+@gpu
+@pytest.mark.parametrize("coarse", [False, True])
+def test_select_of_many_pages(coarse):
+    """Clusters of up to eight CTAs, and more pages than eight tokens' scores have room for."""
+    select_case(1, [16 * 1500 + 3], [1], 2, 1, 64, 16, F32, 40, 1, 2, coarse=coarse)
+    select_case(2, [16 * 1500 + 3, 16 * 200], [3, 2], 2, 1, 64, 16, F32, 40, 1, 2, coarse=coarse)
+    select_case(3, [16 * 300 + 3], [10], 2, 1, 64, 16, F32, 40, 1, 2, columns=7000, coarse=coarse)
+
+
+@gpu
+def test_select_of_many_requests():
+    lens = [1 + (37 * i) % 400 for i in range(100)]
+    select_case(4, lens, [min(1 + i % 4, x) for i, x in enumerate(lens)], 2, 1, 64, 16, F32, 5, 1, 1)
+    select_case(5, lens, [0 if i % 5 == 0 else 1 for i in range(100)], 2, 1, 64, 16, F32, 5, 1, 1)
+    select_case(5, lens, [1] * 100, 2, 1, 64, 16, F32, 5, 1, 1, max_new=0)
+
+
+@gpu
+def test_select_with_more_new_tokens_than_keys():
+    select_case(6, [20, 0, 3], [25, 2, 3], 2, 1, 64, 16, F32, 3, 1, 1)
+
+
+@gpu
+def test_select_of_queries_that_are_not_finite():
+    def change(q, table, n_pages):
+        q[0, 0, 3], q[1, 1, 5], q[2, 2, 7], q[3] = math.nan, math.inf, -math.inf, 0.0
+        q[4] *= 1e-42
+        q[5] *= 1e37
+        q[6] = math.nan
+    select_case(7, [16 * 30] * 7, [1] * 7, 4, 2, 64, 16, F32, 6, 1, 1, change=change)
+
+
+@gpu
+def test_select_of_pages_that_are_none():
+    def change(q, table, n_pages):
+        table[0, 3], table[0, 17], table[1, 40] = -1, n_pages, 1 << 30
+    select_case(8, [16 * 41, 16 * 51], [1, 1], 4, 2, 64, 16, F32, 6, 1, 1, change=change, bits=K.STATUS_BAD_INDEX)
+    select_case(8, [16 * 41, 16 * 51], [2, 9], 4, 2, 64, 16, F32, 6, 1, 1, change=change, bits=K.STATUS_BAD_INDEX)
+
+
+# ------------------------------------------------------------------------------------------ attention over what is selected
+
+def selected_case(seed, lens, new, heads, kv, dim, page, dtype, n_select, change=None, bits=0, **more):
+    b = Batch(seed, lens, new, heads, kv, dim, page, dtype, **more)
+    rng = np.random.default_rng(seed + 1)
+    selected = np.full((b.q.shape[0], kv, n_select), -1)
+    for i in range(len(lens)):
+        for t in range(b.cu[i], b.cu[i + 1]):
+            own = max(lens[i] - (b.cu[i + 1] - t), 0) // page
+            for h in range(kv):
+                pick = rng.permutation(own + 1)[: n_select]
+                selected[t, h, rng.permutation(n_select)[: len(pick)]] = pick          # in any order, holes between
+    if change:
+        change(selected, b)
+    n = int(b.cu[-1])
+    with b.plan() as plan:
+        args = (*b.args[:3], i32(b.table), b.pages, i32(selected))
+        out = torch.full(b.q.shape, 7.0, dtype=dtype, device="cuda")
+        got = plan.attention_selected(*args, out=out, k_scale=KS, v_scale=VS)
+        again = plan.attention_selected(*args, k_scale=KS, v_scale=VS)
+        assert plan.device_status() == ((-8, bits) if bits else (0, 0))
+    assert got is out and bool((got[n:] == 7).all())
+    assert torch.equal(got[:n], again[:n]), "equal calls give equal bits"
+    b.near(got, *plain.attention_selected(host(b.q)[:n], b.cu, lens, b.table, b.cache, selected[:n], page, 1.0 / math.sqrt(dim), float(np.float32(KS)), float(np.float32(VS))))
+    return got
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("dim", [8, 64, 80, 128, 200, 256])
+@pytest.mark.parametrize("n_select", [1, 3, 20])
+def test_selected_pages(dim, dtype, n_select):
+    selected_case(dim, [1, 16, 17, 500, 333], [1, 1, 1, 1, 1], 4, 2, dim, 16, dtype, n_select, pad=3)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("heads, kv", [(1, 1), (3, 3), (7, 1), (8, 1), (9, 1), (16, 1), (17, 1), (40, 1), (64, 2), (15, 5)])
+def test_selected_head_layouts(heads, kv, dtype):
+    selected_case(heads, [200, 70], [2, 1], heads, kv, 64, 32, dtype, 4)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("page", [16, 32, 64, 128])
+def test_selected_pages_of_several_tokens(page, dtype):
+    selected_case(page, [3 * page + 5, 2 * page, 7, 0, 5 * page + 1], [page + 3, 1, 7, 0, 4], 4, 2, 80, page, dtype, 3, extra_rows=3)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_many_selected_pages_are_split(dtype):
+    selected_case(1, [4000, 3500], [1, 1], 4, 2, 64, 16, dtype, 200)
+    selected_case(2, [2000], [1], 2, 1, 128, 64, dtype, 30)
+    selected_case(3, [600] * 60, [1] * 60, 8, 8, 64, 16, dtype, 37)          # stretches that are cut in the middle
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_many_requests_find_their_tokens(dtype):
+    lens = [1 + (37 * i) % 90 for i in range(100)]
+    selected_case(4, lens, [min(i % 4, x) for i, x in enumerate(lens)], 2, 1, 64, 16, dtype, 3)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_lists_of_any_kind(dtype):
+    """A page twice, a page behind the token, nothing at all, columns outside the table, pages outside the cache."""
+    def twice(selected, b):
+        selected[0, 0] = [2, 2, 0, -1]
+        selected[1, 1] = [5, 6, 7, 8]
+        selected[2] = -1
+    got = selected_case(5, [100, 60, 90], [1, 1, 1], 4, 2, 64, 16, dtype, 4, change=twice, bits=K.STATUS_BAD_INDEX)          # the table has 8 columns
+    assert not got[2].any() and not got[1, 2:].any()
+
+    def behind(selected, b):
+        selected[1, 1] = [7, 5, 4, 6]
+    got = selected_case(5, [100, 60, 90], [1, 1, 1], 4, 2, 64, 16, dtype, 4, change=behind)
+    assert not got[1, 2:].any()
+
+    def outside(selected, b):
+        selected[0, 0] = [1, -2, b.table.shape[1], 1 << 30]
+        selected[1, 0, 0] = -(1 << 31)
+    selected_case(6, [100, 60, 90], [1, 1, 1], 4, 2, 64, 16, dtype, 4, change=outside, bits=K.STATUS_BAD_INDEX)
+
+    def gone(selected, b):
+        b.table[0, 1], b.table[2, 0] = -1, len(b.cache)
+        selected[0], selected[2] = [0, 1, 2, 3], [0, 1, 2, 3]
+    selected_case(7, [100, 60, 90], [1, 1, 1], 4, 2, 64, 16, dtype, 4, change=gone, bits=K.STATUS_BAD_INDEX)
+
+
+@gpu
+def test_selected_with_more_new_tokens_than_keys():
+    got = selected_case(8, [20, 0], [23, 2], 4, 2, 64, 16, F32, 2)
+    assert not got[:3].any() and not got[23:].any()
+
+
+# ------------------------------------------------------------------------------------------ together
+
+def steps(plan, kv, heads, dim, page, rng):
+    """Three requests behind one prompt, decoded for a few steps with pages from a free list: yields each step's tensors."""
+    dtype = plan.dtype
+    turns = K.rope_table(dim, 4096)
+    n, prompt = 3, 5 * page
+    cache, summaries = plan.new_cache(40), plan.new_summaries(40)
+    free = torch.randperm(40, dtype=torch.int32).cuda()
+    table = torch.full((n, 12), -1, dtype=torch.int32, device="cuda")
+    lens = torch.zeros(n, dtype=torch.int32, device="cuda")
+    for new in ([prompt, 0, 0], [1, 1, 1], [1, 1, 1], [page, 3, 1], [1, 1, 1]):
+        kv_len, cu, pos, slot, taken = plan.tables(lens, i32(new), free, table, sum(new))
+        free = free[int(taken):]
+        q, k, v = (queries(rng, sum(new), h, dim, dtype) for h in (heads, kv, kv))
+        q = plan.append(q, k, v, slot, cache, positions=pos, turns=turns, k_scale=KS, v_scale=VS)
+        plan.summarise(cu, kv_len, table, cache, summaries, sum(new))
+        yield q, cu, kv_len, table, cache, summaries, max(new)
+        lens = kv_len
+        if new[1] == 0:        # the others begin with the first one's pages
+            table[1:, :5] = table[0, :5]
+            lens = lens[:1].expand(n).contiguous()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("page", [16, 64])
+def test_steps_of_a_served_layer(page, dtype):
+    """tables, append, summarise, then both kinds of attention: behind a shared prefix as without; over all pages as without a selection."""
+    rng = np.random.default_rng(page)
+    with plan_for(4, 2, 64, page, dtype) as plan:
+        for q, cu, lens, table, cache, summaries, max_new in steps(plan, 2, 4, 64, page, rng):
+            more = dict(k_scale=KS, v_scale=VS)
+            groups = i32([0, 3])
+            shared, start = plan.shared_prefix(groups, cu, lens, table)
+            want = plan.attention(q, cu, lens, table, cache, max_new=max_new, **more)
+            got = plan.attention_shared(q, cu, lens, table, cache, groups, shared, start, max_new=max_new, max_group=q.shape[0], **more)
+            few = plan.select(q, cu, lens, table, summaries, n_select=4, first=1, last=1, max_new=max_new)
+            some = plan.attention_selected(q, cu, lens, table, cache, few, **more)
+            every = plan.select(q, cu, lens, table, summaries, n_select=12, max_new=max_new)
+            all_ = plan.attention_selected(q, cu, lens, table, cache, every, **more)
+            assert plan.device_status() == (0, 0)
+            c, ln, tb = cu.cpu().numpy(), lens.cpu().numpy(), table.cpu().numpy()
+            scale = 1.0 / math.sqrt(64)
+            formula = ref.attention(host(q), c, ln, tb, cache.cpu().numpy(), page, 0, 0, scale, float(np.float32(KS)), float(np.float32(VS)))
+            picked = plain.select(host(q), c, ln, tb, summaries.cpu().numpy(), 2, page, 4, 1, 1)
+            assert np.array_equal(few.cpu().numpy(), picked)
+            over = plain.attention_selected(host(q), c, ln, tb, cache.cpu().numpy(), picked, page, scale, float(np.float32(KS)), float(np.float32(VS)))
+            e0 = (2.0 ** -11 if dtype == BF16 else 2.0 ** -21) + 2.0 ** -21
+            for out, (w, spread, exponent, count) in ((want, formula), (got, formula), (all_, formula), (some, over)):
+                limit = spread * (2 * (e0 + exponent * 64 * 2.0 ** -23) + count * 2.0 ** -22) + np.abs(w) * UNIT[dtype] / 2 + 1e-30
+                assert (np.abs(host(out) - w) <= limit).all()
+        assert shared.tolist() == [5 * page]
+
+
+@gpu
+def test_no_page_scores_above_its_bound():
+    """The score is an upper bound of the sum over the heads of q . k but for the roundings of q and of the bounds (half a
+    step of 127 of q, which the numbers |high| + |low| carry), so the page of the largest such sum is selected when it leads by that much."""
+    rng = np.random.default_rng(5)
+    b = Batch(5, [16 * 30], [1], 4, 2, 64, 16, F32)
+    with plan_for(4, 2, 64, 16, F32, requests=1, tokens=480) as plan:
+        summaries = plan.new_summaries(len(b.cache))
+        plan.summarise(i32([0, 480]), b.args[2], b.args[3], b.pages, summaries, 480)
+        high, low = (x.cpu().numpy() for x in plan.read_summaries(summaries, i32(b.table[0, :30]), k_scale=1.0))
+        assert plan.device_status() == (0, 0)
+    keys = ref.decode_all(b.cache, 64)[0]
+    q = rng.standard_normal((2, 2, 64))
+    for h in range(2):
+        for c in range(30):
+            k = keys[b.table[0, c], h]
+            sums = (q[h] @ k.T).sum(0)
+            bound = np.maximum(q[h] * high[c, h], q[h] * low[c, h]).sum()
+            assert sums.max() <= bound + 1e-5 * np.abs(q[h]).sum() * np.abs(k).max()
+
+
+@gpu
+def test_calls_in_a_graph_and_on_another_stream():
+    """Captured once, replayed on other lengths and tables; two graphs of one plan in turn."""
+    b, other = (Batch(s, lens, [1, 1, 1], 4, 2, 64, 16, BF16, [0, 3], [4], columns=12) for s, lens in ((1, [100, 90, 80]), (2, [70, 130, 66])))
+    groups = i32([0, 3])
+    with b.plan() as plan:
+        def calls(q, cu, lens, table, cache, summaries):
+            plan.summarise(cu, lens, table, cache, summaries, 3)
+            shared, start = plan.shared_prefix(groups, cu, lens, table)
+            x = plan.attention_shared(q, cu, lens, table, cache, groups, shared, start, max_new=1, max_group=3, k_scale=KS, v_scale=VS)
+            picked = plan.select(q, cu, lens, table, summaries, n_select=3, max_new=1)
+            return shared, x, picked, plan.attention_selected(q, cu, lens, table, cache, picked, k_scale=KS, v_scale=VS)
+
+        pages = max(len(b.cache), len(other.cache))
+        cache = plan.new_cache(pages)
+        state = [t.clone() for t in b.args] + [cache, plan.new_summaries(pages)]
+
+        def load(x):
+            for to, t in zip(state, x.args):
+                to.copy_(t)
+            cache.zero_()[: len(x.cache)].copy_(x.pages)
+            state[5].zero_()
+
+        load(b)
+        stream = torch.cuda.Stream()
+        stream.wait_stream(torch.cuda.current_stream())
+        graphs, outs = [], []
+        with torch.cuda.stream(stream):
+            calls(*state)
+            torch.cuda.synchronize()
+            for _ in range(2):
+                g = torch.cuda.CUDAGraph()
+                with torch.cuda.graph(g, stream=stream):
+                    outs.append(calls(*state))
+                graphs.append(g)
+        torch.cuda.current_stream().wait_stream(stream)
+        for x in (other, b, other):
+            load(x)
+            want = [t.clone() for t in calls(*state)]
+            torch.cuda.synchronize()
+            for g, got in zip(graphs, outs):
+                state[5].zero_()
+                g.replay()
+                torch.cuda.synchronize()
+                for a, z in zip(got, want):
+                    assert torch.equal(a, z)
+            side = torch.cuda.Stream()
+            side.wait_stream(torch.cuda.current_stream())
+            shared, start = plan.shared_prefix(groups, *state[1:4], stream=side)
+            got = plan.attention_shared(*state[:5], groups, shared, start, max_new=1, max_group=3, k_scale=KS, v_scale=VS, stream=side)
+            side.synchronize()
+            assert torch.equal(got, want[1])
+        assert plan.device_status() == (0, 0)
+
+
+@gpu
+def test_calls_of_nothing():
+    with plan_for() as plan:
+        cache, summaries = plan.new_cache(2), plan.new_summaries(2)
+        none, q = i32([]), torch.zeros((0, 4, 64), device="cuda")
+        cu, table = i32([0]), i32(np.zeros((0, 3)))
+        shared, start = plan.shared_prefix(i32([0]), cu, none, table)
+        assert shared.numel() == 0 and start.numel() == 0
+        shared, start = plan.shared_prefix(i32([0, 0, 0]), cu, none, table)
+        assert shared.tolist() == [0, 0]
+        assert plan.attention_shared(q, cu, none, table, cache, i32([0]), none, none).shape == (0, 4, 64)
+        plan.summarise(cu, none, table, cache, summaries, 0)
+        assert plan.read_summaries(summaries, none)[0].shape == (0, 2, 64)
+        assert plan.select(q, cu, none, table, summaries, n_select=2).shape == (0, 2, 2)
+        assert plan.attention_selected(q, cu, none, table, cache, i32(np.zeros((0, 2, 2)))).shape == (0, 4, 64)
+        assert plan.device_status() == (0, 0)
+
+
+@gpu
+def test_offsets_past_32_bits():
+    """Pages behind 2^31 and 2^32 bytes of the cache, and summaries of them."""
+    dim, page, kv = 256, 128, 8
+    per_page = kv * (page // 16) * ref.block_bytes(dim)
+    n_pages = (1 << 32) // per_page + 20
+    b = Batch(9, [300, 270], [1, 1], 8, kv, dim, page, BF16, [0, 2], [2])
+    far = torch.zeros((n_pages, *b.cache.shape[1:]), dtype=torch.uint8, device="cuda")
+    shift = n_pages - len(b.cache)
+    far[shift:].copy_(b.pages)
+    near, table = i32(b.table), i32(np.where(b.table < len(b.cache), b.table + shift, b.table))
+    q, cu, lens = b.args[:3]
+    with b.plan() as plan:
+        outs = []
+        for tb, cache in ((near, b.pages), (table, far)):
+            summaries = plan.new_summaries(len(cache))
+            plan.summarise(cu, lens, tb, cache, summaries, 2)
+            shared, start = plan.shared_prefix(i32([0, 2]), cu, lens, tb)
+            x = plan.attention_shared(q, cu, lens, tb, cache, i32([0, 2]), shared, start, max_new=1, max_group=2, k_scale=KS, v_scale=VS)
+            picked = plan.select(q, cu, lens, tb, summaries, n_select=2, max_new=1)
+            outs.append((x, picked, plan.attention_selected(q, cu, lens, tb, cache, picked, k_scale=KS, v_scale=VS)))
+        assert plan.device_status() == (0, 0)
+    for a, z in zip(*outs):
+        assert torch.equal(a, z)
+
+
+def _refused(call, status):
+    with pytest.raises(B.MoEError) as e:
+        call()
+    assert e.value.status == status
+
+
+@gpu
+def test_refusals():
+    b = Batch(1, [40, 50], [1, 1], 4, 2, 64, 16, F32, [0, 2], [2])
+    q, cu, lens, table = b.args
+    with b.plan() as plan, plan_for(8, 2, 64, 16, F32, requests=2, tokens=2) as wider:
+        summaries = plan.new_summaries(len(b.cache))
+        g = i32([0, 2])
+        shared, start = plan.shared_prefix(g, cu, lens, table)
+        ok = (q, cu, lens, table, b.pages, g, shared, start)
+        picked = plan.select(q, cu, lens, table, summaries, n_select=2)
+        for bad in (dict(k_scale=0.0), dict(v_scale=-1.0), dict(v_scale=math.inf), dict(softmax_scale=math.nan), dict(max_new=-1)):
+            _refused(lambda: plan.attention_shared(*ok, **bad), -1)
+            if "max_new" not in bad:
+                _refused(lambda: plan.attention_selected(*ok[:5], picked, **bad), -1)
+        _refused(lambda: plan.attention_shared(*ok, max_group=-1), -1)
+        for n_select, first, last in ((1, 1, 1), (4, -1, 1), (4, 1, 0), (4, 3, 2), (4, (1 << 31) - 1, 1)):
+            _refused(lambda: plan.select(q, cu, lens, table, summaries, n_select=n_select, first=first, last=last), -1)
+        _refused(lambda: plan.read_summaries(summaries, i32([0]), k_scale=0.0), -1)
+        _refused(lambda: plan.summarise(cu, lens, table, b.pages, summaries, -1), -1)
+        _refused(lambda: plan.summarise(cu, lens, table, b.pages, summaries, plan.cfg.max_tokens + 1), -1)
+        _refused(lambda: plan.shared_prefix(i32([0] * 9), cu, lens, table), -1)
+        wide = i32(np.zeros((2, 49153)))
+        _refused(lambda: plan.select(q, cu, lens, wide, summaries, n_select=2), -2)
+        for call in (lambda: plan.attention_shared(q.half(), *ok[1:]), lambda: plan.attention_shared(*ok[:6], i32([0, 0]), start), lambda: plan.attention_shared(*ok[:7], i32([0])),
+                     lambda: wider.attention_shared(*ok), lambda: plan.attention_shared(*ok[:3], i32(np.zeros((3, 4))), *ok[4:]), lambda: plan.attention_shared(*ok[:5], i32([]), shared, start),
+                     lambda: plan.shared_prefix(i32([]), cu, lens, table), lambda: plan.shared_prefix(g.long(), cu, lens, table), lambda: plan.shared_prefix(g.cpu(), cu, lens, table),
+                     lambda: plan.summarise(cu, lens, table, b.pages, plan.new_summaries(1), 2), lambda: plan.summarise(cu, lens, table, b.pages, summaries.int(), 2),
+                     lambda: plan.read_summaries(summaries[:, :1], i32([0])), lambda: plan.select(q, cu, lens, table, summaries, n_select=0),
+                     lambda: plan.select(q, cu, lens, table, summaries, n_select=2, out=picked[:1]), lambda: plan.attention_selected(*ok[:5], picked[:1]),
+                     lambda: plan.attention_selected(*ok[:5], picked.long()), lambda: plan.attention_selected(*ok[:5], picked[:, :1]),
+                     lambda: plan.attention_selected(*ok[:5], picked[:, :, :0])):
+            with pytest.raises((AssertionError, B.MoEError)):
+                call()
+        assert plan.device_status() == (0, 0)
+        lib, h = plan._lib, plan.handle
+        rows = K.moe_kv_rows_t(q.data_ptr(), q.stride(0), q.stride(1))
+        out, scratch = torch.empty_like(q), torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+        need = lib.moe_kv_shared_scratch_bytes(h, 2, 1)
+        assert need == 2 * 4 * (64 * 4 + 8) and lib.moe_kv_shared_scratch_bytes(h, 2, 0) == need
+        assert lib.moe_kv_shared_scratch_bytes(wider.handle, 100, 9) == 0 and lib.moe_kv_shared_scratch_bytes(h, 0, 1) == 0 and lib.moe_kv_shared_scratch_bytes(h, 1, -1) == 0
+
+        def shared_call(at=0, size=need, group=g.data_ptr(), tab=table.data_ptr(), where=scratch.data_ptr()):
+            return lib.moe_kv_attention_shared(h, ctypes.byref(rows), 2, cu.data_ptr(), lens.data_ptr(), 2, 1, tab, table.shape[1], b.pages.data_ptr(), len(b.cache), group, 1, 2,
+                                               shared.data_ptr(), start.data_ptr(), 0.125, 1.0, 1.0, where, size, out.data_ptr() + at, None)
+        assert shared_call() == 0
+        assert shared_call(size=need - 1) == -4 and shared_call(where=None) == -4 and shared_call(where=scratch.data_ptr() + 8) == -3
+        assert shared_call(at=8) == -3 and shared_call(group=g.data_ptr() + 2) == -3 and shared_call(group=None) == -1 and shared_call(tab=None) == -1
+        assert lib.moe_kv_summarise(h, cu.data_ptr(), lens.data_ptr(), 2, 2, table.data_ptr(), table.shape[1], b.pages.data_ptr(), len(b.cache), summaries.data_ptr() + 8, None) == -3
+        assert lib.moe_kv_read_summaries(h, summaries.data_ptr(), len(b.cache), cu.data_ptr(), 1, 1.0, scratch.data_ptr() + 4, scratch.data_ptr(), None) == -3
+        assert lib.moe_kv_select(h, ctypes.byref(rows), 2, cu.data_ptr(), lens.data_ptr(), 2, 1, table.data_ptr(), table.shape[1], summaries.data_ptr(), len(b.cache), 2, 1, 1,
+                                 scratch.data_ptr() + 2, None) == -3
+        assert lib.moe_kv_attention_selected(h, ctypes.byref(rows), 2, cu.data_ptr(), lens.data_ptr(), 2, table.data_ptr(), table.shape[1], b.pages.data_ptr(), len(b.cache),
+                                             picked.data_ptr() + 1, 2, 0.125, 1.0, 1.0, out.data_ptr(), None) == -3
+        assert lib.moe_kv_attention_selected(h, ctypes.byref(rows), 2, cu.data_ptr(), lens.data_ptr(), 2, table.data_ptr(), table.shape[1], b.pages.data_ptr(), len(b.cache),
+                                             picked.data_ptr(), 1 << 27, 0.125, 1.0, 1.0, out.data_ptr(), None) == -2
+        torch.cuda.synchronize()
+        assert plan.device_status() == (0, 0)
