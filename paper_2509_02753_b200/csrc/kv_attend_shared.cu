@@ -5,14 +5,18 @@
 namespace lexi {
 namespace kv {
 
+void prefix_rows_pieces(AttendArgs &a, int max_ctas) {
+    a.piece_rows = a.result_rows = tile_rows(padded_width(a.D), (long long)a.max_new * a.G);
+    a.piece_results = 1;
+    a.piece_ctas = max_ctas;
+}
+
 cudaError_t launch_attend_prefix_rows(const AttendArgs &a, int sm_count, cudaStream_t s, uint64_t *launches) {
-    long long rows = (long long)(a.max_new > 0 ? a.max_new : a.T) * a.G;
-    if (a.prompt_rows > 0 && rows > a.prompt_rows) rows = a.prompt_rows;
-    return launch_rows<Reads::Prefix>(rows, a, sm_count, s, launches);
+    return launch_rows<Reads::Prefix>((long long)a.max_new * a.G, a, sm_count, s, launches);
 }
 
 cudaError_t launch_attend_rest_rows(const AttendArgs &a, int sm_count, cudaStream_t s, uint64_t *launches) {
-    return launch_rows<Reads::Rest>((long long)(a.max_new > 0 ? a.max_new : a.T) * a.G, a, sm_count, s, launches);
+    return launch_rows<Reads::Rest>((long long)a.max_new * a.G, a, sm_count, s, launches);
 }
 
 }  // namespace kv

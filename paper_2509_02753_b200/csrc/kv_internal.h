@@ -125,11 +125,15 @@ struct AttendArgs {
     float *prompt_part; float2 *prompt_ml; int32_t *prompt_arrived;
     int32_t *status;
     // Shared prefixes.  Prefix: n groups, group i = requests [groups[i], groups[i + 1]) of n_members, kv_len its shared keys,
-    // max_new the largest number of its new tokens.  Rest: request i reads the keys from start[i] on.  o_part [T][H][W] and
-    // o_ml [T][H] are a row's sums, reference and denominator over its prefix: written by the one, read by the other
+    // max_new the largest number of its new tokens.  Rest: request i reads the keys from start[i] on.  A row's sums, reference
+    // and denominator over its prefix lie in o_part [T][H][W] and o_ml [T][H], o_pieces being (-1, ...), or in the pieces of
+    // its stretch, o_pieces being (first CTA, CTAs, row): that row of prompt_part and prompt_ml in slot 1 of the first CTA and
+    // 0 of the others.  A slot has piece_rows rows, results of result_rows each where there are piece_results of them; piece_ctas CTAs
+    // have slots
     const int32_t *groups; int n_members;
     const int32_t *start;
-    float *o_part; float2 *o_ml;
+    float *o_part; float2 *o_ml; int4 *o_pieces;
+    int piece_rows, result_rows, piece_results, piece_ctas;
     // Selected pages: [T][Hk][n_listed] columns of the request's row of the block table, -1: none
     const int32_t *listed; int n_listed;
 };
@@ -139,11 +143,13 @@ __device__ __forceinline__ int div_g(const AttendArgs &a, int row) { return (int
 // rows of queries that share a key/value head, in the N dimension of mma.sync (kv_attend.cu)
 cudaError_t launch_attend_rows(const AttendArgs &a, int sm_count, cudaStream_t s, uint64_t *launches);
 size_t attend_part_floats(int w);          // per CTA of the grid
+void prefix_rows_pieces(AttendArgs &a, int max_ctas);          // how the kernel below lays out its pieces
 cudaError_t launch_attend_prefix_rows(const AttendArgs &a, int sm_count, cudaStream_t s, uint64_t *launches);
 cudaError_t launch_attend_rest_rows(const AttendArgs &a, int sm_count, cudaStream_t s, uint64_t *launches);
 cudaError_t launch_attend_listed(const AttendArgs &a, int sm_count, cudaStream_t s, uint64_t *launches);
 // prompts, on tcgen05 (kv_prompt.cu)
 cudaError_t launch_attend_prompt(const AttendArgs &a, int sm_count, cudaStream_t s, uint64_t *launches);
+void prefix_prompt_pieces(AttendArgs &a, int sm_count);
 cudaError_t launch_attend_prefix_prompt(const AttendArgs &a, int sm_count, cudaStream_t s, uint64_t *launches);
 size_t prompt_part_floats(int w);          // per CTA, of which there is one per SM
 size_t prompt_part_rows();

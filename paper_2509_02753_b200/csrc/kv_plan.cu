@@ -137,7 +137,7 @@ int moe_kv_plan_create(const moe_kv_config_t *cfg, moe_kv_plan_t **out) {
     // the kernel of what lies behind it already uses the others
     const size_t ppart = std::max((size_t)sms * prompt_part_floats(padded_width(cfg->head_dim)) * sizeof(float), part);
     const size_t pml = std::max((size_t)sms * prompt_part_rows() * sizeof(float2), ml);
-    const size_t parrived = arrived;
+    const size_t parrived = ((size_t)sms * sizeof(int32_t) + 255) & ~size_t(255);
     p->bytes = part + ml + ppart + pml + arrived + parrived + 256;
     void *mem = nullptr;
     if (cudaMalloc(&mem, p->bytes) != cudaSuccess || cudaMallocHost((void **)&p->status_host, 4) != cudaSuccess) {
@@ -326,7 +326,7 @@ int moe_kv_shared_prefix(moe_kv_plan_t *p, const int32_t *cu_group, int32_t n_gr
 
 uint64_t moe_kv_shared_scratch_bytes(const moe_kv_plan_t *p, int32_t n_tokens, int32_t max_new) {
     if (!p || n_tokens < 1 || max_new < 0 || !reads_prefixes_once(p, n_tokens, max_new)) return 0;
-    return shared_rows_bytes(p, n_tokens) + (uint64_t)n_tokens * p->cfg.n_heads * sizeof(float2);
+    return shared_rows_bytes(p, n_tokens) + (uint64_t)n_tokens * p->cfg.n_heads * (sizeof(int4) + sizeof(float2));
 }
 
 int moe_kv_attention_shared(moe_kv_plan_t *p, const moe_kv_rows_t *q, int32_t T, const int32_t *cu_new, const int32_t *kv_len, int32_t n, int32_t max_new,
@@ -346,24 +346,27 @@ int moe_kv_attention_shared(moe_kv_plan_t *p, const moe_kv_rows_t *q, int32_t T,
         return moe_kv_attention(p, q, T, cu_new, kv_len, n, max_new, block_table, width, cache, n_pages, softmax_scale, k_scale, v_scale, 0, 0, out, stream);
     if (!scratch || scratch_bytes < moe_kv_shared_scratch_bytes(p, T, max_new)) return MOE_ERR_WORKSPACE;
     AttendArgs rest = attend_args(p, q, T, cu_new, kv_len, n, max_new, block_table, width, cache, n_pages, softmax_scale, k_scale, v_scale, out);
+    rest.max_new = max_new > 0 && max_new < T ? max_new : T;
     rest.start = start;
     rest.o_part = (float *)scratch;
-    rest.o_ml = (float2 *)((uint8_t *)scratch + shared_rows_bytes(p, T));
+    rest.o_pieces = (int4 *)((uint8_t *)scratch + shared_rows_bytes(p, T));
+    rest.o_ml = (float2 *)(rest.o_pieces + (size_t)T * c.n_heads);
     AttendArgs prefix = rest;
     prefix.kv_len = shared_len; prefix.n = n_groups; prefix.groups = cu_group; prefix.n_members = n;
     prefix.max_new = max_group > 0 && max_group < T ? max_group : T;
     cudaStream_t s = (cudaStream_t)stream;
-    // groups of few rows in kv_attend_body.cuh, those of many in kv_prompt_body.cuh, as the requests of moe_kv_attention
-    const long long most = prefix.max_new, limit = row_limit(c);
-    if (most * prefix.G > limit) {
-        const bool alike = n_groups * most == T;
-        prefix.prompt_rows = alike ? 0 : (int)limit;
-        const cudaError_t err = launch_attend_prefix_prompt(prefix, p->sm_count, s, &p->launches);
-        if (err != cudaSuccess) return done(err);
-        if (alike) return done(launch_attend_rest_rows(rest, p->sm_count, s, &p->launches));
+    // groups of few rows in kv_attend_body.cuh, of many in kv_prompt_body.cuh, as the requests of moe_kv_attention; all in one
+    // launch, for a small group's tiles cost the tensor cores what a large one's do
+    const bool few = (long long)prefix.max_new * prefix.G <= row_limit(c);
+    if (few) {
+        prefix.part = p->prompt_part; prefix.part_ml = p->prompt_ml;
+        prefix_rows_pieces(prefix, p->max_ctas);
+    } else {
+        prefix_prompt_pieces(prefix, p->sm_count);
     }
-    prefix.part = p->prompt_part; prefix.part_ml = p->prompt_ml; prefix.arrived = p->prompt_arrived;
-    const cudaError_t err = launch_attend_prefix_rows(prefix, p->sm_count, s, &p->launches);
+    rest.piece_rows = prefix.piece_rows; rest.result_rows = prefix.result_rows;
+    rest.piece_results = prefix.piece_results; rest.piece_ctas = prefix.piece_ctas;
+    const cudaError_t err = few ? launch_attend_prefix_rows(prefix, p->sm_count, s, &p->launches) : launch_attend_prefix_prompt(prefix, p->sm_count, s, &p->launches);
     if (err != cudaSuccess) return done(err);
     return done(launch_attend_rest_rows(rest, p->sm_count, s, &p->launches));
 }

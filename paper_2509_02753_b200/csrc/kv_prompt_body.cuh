@@ -27,8 +27,9 @@
 // serves few rows over a long context; a stretch in several pieces is joined by its last CTA in the order of the keys.
 //
 // PREFIX: "requests" are groups of requests and "keys" their shared prefix, which all rows of a group see whole (kv_prompt.cu
-// builds the one, kv_prompt_prefix.cu the other); what comes out is sums, references and denominators as they are, in a
-// place of the row's own, for kv_attend_body.cuh's Rest.
+// builds the one, kv_prompt_prefix.cu the other).  What comes out is sums, references and denominators as they are, for
+// kv_attend_body.cuh's Rest, which joins the pieces of a stretch: a stretch of 256 rows on 8192 keys has 19 pieces, 2.4 MB, which its
+// last CTA took most of 67 us to add while all others were done; Rest's CTAs have a few rows each.
 #pragma once
 
 #include <float.h>
@@ -858,6 +859,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
                 }
                 __syncwarp();
                 if (!whole && real) a.prompt_ml[(int64_t)slot * S::kPartRows + t * kTileRows + row_in] = make_float2(m, l);
+                if (PREFIX && real && p.first == 0 && p.cta0 != p.cta1 && !(S::kAlternate && t == 1))
+                    a.o_pieces[out_row] = make_int4(p.cta0, p.cta1 + 1 - p.cta0, S::kAlternate ? row_in : t * kTileRows + row_in, 0);
             }
             tc::tc_fence_before();
             if (!whole) {
@@ -865,7 +868,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
                 asm volatile("bar.sync 1, %0;" ::"n"(GROUPS * 128) : "memory");
                 if (tid == 0) {
                     last_s = (S::kAlternate || PREFIX) && p.cta0 == p.cta1;        // the stretch is this CTA's alone
-                    if (!last_s) {
+                    if (!last_s && !PREFIX) {
                         const int before = atomicAdd(a.prompt_arrived + p.cta0, 1);
                         last_s = before == p.cta1 - p.cta0;
                         if (last_s) a.prompt_arrived[p.cta0] = 0;      // ready for the next call
@@ -929,7 +932,10 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
 #pragma unroll
                                 for (int e = 0; e < kPer; e += 2)
                                     *reinterpret_cast<float2 *>(a.o_part + to_row * W + lane * kPer + e) = make_float2(v[y][e], v[y][e + 1]);
-                                if (lane == 0) a.o_ml[to_row] = make_float2(top[y], sum[y]);
+                                if (lane == 0) {
+                                    a.o_ml[to_row] = make_float2(top[y], sum[y]);
+                                    a.o_pieces[to_row] = make_int4(-1, 1, 0, 0);
+                                }
                                 continue;
                             }
                             T *dst = (T *)a.out + to_row * a.D + lane * kPer;
