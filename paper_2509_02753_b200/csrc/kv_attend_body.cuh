@@ -30,8 +30,9 @@
 //   Every   all keys of the request that the row's position and the window let it see
 //   Prefix  "requests" are groups of requests and "keys" their shared prefix, which all rows of a group see whole; what
 //           comes out is sums, references and denominators as they are, in fp32, of each piece of a stretch
-//   Rest    the keys behind the shared prefix; a row's sums are joined with those of its prefix's pieces before they are
-//           divided.  The kernel starts while the one of the prefix runs and waits for it where a row's results are joined
+//   Rest    the keys behind the shared prefix; what comes out, again, is sums.  The kernel starts while the one of the prefix
+//           runs and shares the SMs with it; only one CTA waits for it, in the end, so that this kernel's end is both kernels'.
+//           kv_attend_shared.cu joins the two
 //   Listed  a token is a "request" of its own; its blocks are those of the pages listed for it and the head
 #pragma once
 
@@ -95,7 +96,6 @@ struct Shape {
     static constexpr int kJoin = kWarps * kRows * kJoinTiles * 16 * 4;
     static_assert(kJoin <= kRing, "the join's buffer is the ring's");
     static constexpr int kSmem = kRing + kQ;                  // plus the line of requests
-    static constexpr int kOwn = kRows * W * 4;                // Rest: and the rows' sums
 };
 
 enum class Reads { Every, Prefix, Rest, Listed };
@@ -107,8 +107,7 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
     using S = Shape<W, NT, SPLIT>;
     extern __shared__ __align__(128) uint8_t smem[];
     uint8_t *ring = smem, *q_s = smem + S::kRing;
-    int64_t *line = reinterpret_cast<int64_t *>(smem + S::kSmem + (kRest ? S::kOwn : 0));      // [n + 1] running sum of blocks
-    float *own_s = reinterpret_cast<float *>(smem + S::kSmem);         // Rest: [kRows][W]
+    int64_t *line = reinterpret_cast<int64_t *>(smem + S::kSmem);      // [n + 1] running sum of blocks
     __shared__ __align__(8) uint64_t full[kWarps * S::kStages];
     __shared__ int32_t row_pos[S::kRows];          // position of a row's token, -1 for a row that is none
     __shared__ float row_scale[S::kRows];          // its factor from the product to the exponent
@@ -794,9 +793,9 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
                 }
                 return;
             }
-            if (kRest && begin > 0) {           // joined with the prefix's below
-                *reinterpret_cast<float2 *>(own_s + n * W + d) = v;
-                if (d == 0) row_ml[n] = make_float2(top, sum);
+            if (kRest && begin > 0) {
+                *reinterpret_cast<float2 *>(a.own_part + at_row * W + d) = v;
+                if (d == 0) a.own_ml[at_row] = make_float2(top, sum);
                 return;
             }
             const float k = sum > 0.f || sum != sum ? a.v_scale / sum : 0.f;
@@ -901,80 +900,11 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
                 }
             }
         }
-        if (kRest && begin > 0 && (whole || last_s)) {
-            // ---- the rows' own sums and those of their prefix: a warp a row, a lane W/32 neighbouring dimensions, the numbers of
-            // several pieces asked for at once
-            __syncthreads();
-            pdl_wait();                 // they are there
-            constexpr int kDims = W / 32, kAtOnce = 8;
-#pragma unroll 1
-            for (int n = warp; row0 + n < row1; n += kWarps) {
-                const int row = row0 + n, tok = div_g(a, row);
-                const int64_t at_row = (int64_t)(q0 + tok) * a.H + head * a.G + row - tok * a.G;
-                const int4 where = __ldcg(&a.o_pieces[at_row]);
-                const bool one = where.x == -1;
-                int pieces = one ? 1 : where.y * a.piece_results;
-                if (!one && (where.x < 0 || where.y < 1 || where.y > a.piece_ctas || where.x > a.piece_ctas - where.y || where.z < 0 || where.z >= a.piece_rows)) {
-                    if (lane == 0) atomicOr(a.status, MOE_KV_STATUS_BAD_INDEX);          // no prefix was attended to for this row
-                    pieces = 0;
-                }
-                float top = row_ml[n].x, sum = row_ml[n].y, v[kDims];
-#pragma unroll
-                for (int e = 0; e < kDims; ++e) v[e] = own_s[n * W + lane * kDims + e];
-#pragma unroll 1
-                for (int p0 = 0; p0 < pieces; p0 += kAtOnce) {
-                    float2 ml[kAtOnce];
-                    float x[kAtOnce][kDims];
-#pragma unroll
-                    for (int y = 0; y < kAtOnce; ++y) {
-                        const int p = min(p0 + y, pieces - 1), b = p / a.piece_results;
-                        const int64_t at_piece = (int64_t)((where.x + b) * 2 + (b == 0)) * a.piece_rows + (p - b * a.piece_results) * a.result_rows + where.z;
-                        ml[y] = __ldcg(one ? &a.o_ml[at_row] : &a.prompt_ml[at_piece]);
-                        const float *src = (one ? a.o_part + at_row * W : a.prompt_part + at_piece * W) + lane * kDims;
-                        if constexpr (kDims == 2) {
-                            const float2 z = __ldcg(reinterpret_cast<const float2 *>(src));
-                            x[y][0] = z.x; x[y][1] = z.y;
-                        } else {
-#pragma unroll
-                            for (int e = 0; e < kDims; e += 4) {
-                                const float4 z = __ldcg(reinterpret_cast<const float4 *>(src + e));
-                                x[y][e] = z.x; x[y][e + 1] = z.y; x[y][e + 2] = z.z; x[y][e + 3] = z.w;
-                            }
-                        }
-                    }
-                    float to = top;
-#pragma unroll
-                    for (int y = 0; y < kAtOnce; ++y) to = fmaxf(to, ml[y].x);
-                    const float old = top == to ? 1.f : ex2(top - to);
-                    sum *= old;
-#pragma unroll
-                    for (int e = 0; e < kDims; ++e) v[e] *= old;
-#pragma unroll
-                    for (int y = 0; y < kAtOnce; ++y) {
-                        if (p0 + y >= pieces) continue;
-                        const float k = ml[y].x == to ? 1.f : ex2(ml[y].x - to);
-                        sum += ml[y].y * k;
-#pragma unroll
-                        for (int e = 0; e < kDims; ++e) v[e] += x[y][e] * k;
-                    }
-                    top = to;
-                }
-                const float k = sum > 0.f || sum != sum ? a.v_scale / sum : 0.f;
-                T *dst = (T *)a.out + at_row * a.D + lane * kDims;
-                if (lane * kDims < a.D) {           // D is a multiple of 8, kDims at most 8
-#pragma unroll
-                    for (int e = 0; e < kDims; e += 2) {
-                        if (SPLIT) *reinterpret_cast<float2 *>(dst + e) = make_float2(v[e] * k, v[e + 1] * k);
-                        else *reinterpret_cast<__nv_bfloat162 *>(dst + e) = __floats2bfloat162_rn(v[e] * k, v[e + 1] * k);
-                    }
-                }
-            }
-        }
         // the ring and the rows' tables are the next piece's; its copies come after this piece's plain accesses
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncthreads();
     }
-    if (kRest) pdl_wait();          // by every CTA: that this kernel is complete means that the prefix's is
+    if (kRest && blockIdx.x == 0) pdl_wait();          // that this kernel is complete means that the prefix's is
 }
 
 template <typename T, int W, int NT, int MINB, Reads R>
@@ -988,11 +918,10 @@ cudaError_t launch(const AttendArgs &a, int sm_count, cudaStream_t s, uint64_t *
     cudaError_t err = cudaGetDevice(&dev);
     if (err != cudaSuccess) return err;
     const bool many = R != Reads::Listed && a.n > kFew;
-    constexpr int kFixed = S::kSmem + (R == Reads::Rest ? S::kOwn : 0);
-    const int smem = kFixed + 8 * ((many ? kMaxRequests : kFew) + 1);
+    const int smem = S::kSmem + 8 * ((many ? kMaxRequests : kFew) + 1);
     int per_sm = dev < 64 ? held[dev][many].load() : 0;
     if (per_sm == 0) {
-        err = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kFixed + 8 * (kMaxRequests + 1));
+        err = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem + 8 * (kMaxRequests + 1));
         if (err != cudaSuccess) return err;
         err = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, k, kThreads, smem);
         if (err != cudaSuccess) return err;

@@ -1,9 +1,104 @@
 // Attention of few query rows over the shared prefix of a group of requests, and over what lies behind it
-// (kv_attend_body.cuh has the kernel).
+// (kv_attend_body.cuh has the kernel), and the join of both:
+//
+//   o = v_scale * sum_p 2^(m_p - M) s_p / sum_p 2^(m_p - M) l_p,   M = max_p m_p
+//
+// over the pieces p of a row, each with its sums s_p, reference m_p and denominator l_p.  Bound by latency: a row of 128
+// dimensions has up to 20 pieces of 512 bytes, all of which lie in the L2.  A warp has a row and asks for eight pieces at a time.
 #include "kv_attend_body.cuh"
 
 namespace lexi {
 namespace kv {
+namespace {
+
+constexpr int kJoinWarps = 8, kAtOnce = 8;
+
+template <typename T, int W>
+__global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(AttendArgs a) {
+    constexpr int kDims = W / 32;
+    const int lane = threadIdx.x & 31;
+    const long long at_row = (long long)blockIdx.x * kJoinWarps + (threadIdx.x >> 5);
+    pdl_trigger();
+    // The row's request, from what was there before the kernels of its pieces: they began behind its end
+    bool mine = at_row < (long long)a.T * a.H;
+    if (mine) {
+        const int token = (int)(at_row / a.H);
+        const int i = warp_find(a.n, token, [&](int x) { return a.cu[x]; });
+        mine = i < a.n && a.cu[i] >= 0 && a.cu[i] <= token && a.cu[i + 1] <= a.T;
+        // as in Rest: of a request with no prefix the rows are done
+        if (mine) mine = min(a.start[i], max(min(max(a.kv_len[i], 0), (int)min((long long)a.width * (kBlockTokens << a.page_shift), (long long)INT32_MAX)) - (a.cu[i + 1] - a.cu[i]), 0)) > 0;
+    }
+    pdl_wait();
+    if (!mine) return;
+    const int4 where = __ldcg(&a.o_pieces[at_row]);
+    const float2 own = __ldcg(&a.own_ml[at_row]);
+    const bool one = where.x == -1;
+    int pieces = one ? 1 : where.y * a.piece_results;
+    if (!one && (where.x < 0 || where.y < 1 || where.y > a.piece_ctas || where.x > a.piece_ctas - where.y || where.z < 0 || where.z >= a.piece_rows)) {
+        if (lane == 0) atomicOr(a.status, MOE_KV_STATUS_BAD_INDEX);          // no prefix was attended to for this row
+        pieces = 0;
+    }
+    auto numbers = [&](const float *src, float (&x)[kDims]) {
+        if constexpr (kDims == 2) {
+            const float2 z = __ldcg(reinterpret_cast<const float2 *>(src + lane * 2));
+            x[0] = z.x; x[1] = z.y;
+        } else {
+#pragma unroll
+            for (int e = 0; e < kDims; e += 4) {
+                const float4 z = __ldcg(reinterpret_cast<const float4 *>(src + lane * kDims + e));
+                x[e] = z.x; x[e + 1] = z.y; x[e + 2] = z.z; x[e + 3] = z.w;
+            }
+        }
+    };
+    float top = own.x, sum = own.y, v[kDims];
+    numbers(a.own_part + at_row * W, v);
+#pragma unroll 1
+    for (int p0 = 0; p0 < pieces; p0 += kAtOnce) {
+        float2 ml[kAtOnce];
+        float x[kAtOnce][kDims];
+#pragma unroll
+        for (int y = 0; y < kAtOnce; ++y) {
+            const int p = min(p0 + y, pieces - 1), b = a.piece_results == 2 ? p >> 1 : p;
+            const int64_t at_piece = (int64_t)((where.x + b) * 2 + (b == 0)) * a.piece_rows + (p - b * a.piece_results) * a.result_rows + where.z;
+            ml[y] = __ldcg(one ? &a.o_ml[at_row] : &a.prompt_ml[at_piece]);
+            numbers(one ? a.o_part + at_row * W : a.prompt_part + at_piece * W, x[y]);
+        }
+        float to = top;
+#pragma unroll
+        for (int y = 0; y < kAtOnce; ++y) to = fmaxf(to, ml[y].x);
+        const float old = top == to ? 1.f : ex2(top - to);
+        sum *= old;
+#pragma unroll
+        for (int e = 0; e < kDims; ++e) v[e] *= old;
+#pragma unroll
+        for (int y = 0; y < kAtOnce; ++y) {
+            if (p0 + y >= pieces) continue;
+            const float k = ml[y].x == to ? 1.f : ex2(ml[y].x - to);
+            sum += ml[y].y * k;
+#pragma unroll
+            for (int e = 0; e < kDims; ++e) v[e] += x[y][e] * k;
+        }
+        top = to;
+    }
+    const float k = sum > 0.f || sum != sum ? a.v_scale / sum : 0.f;
+    if (lane * kDims >= a.D) return;                   // D is a multiple of 8, kDims at most 8
+    T *dst = (T *)a.out + at_row * a.D + lane * kDims;
+#pragma unroll
+    for (int e = 0; e < kDims; e += 2) {
+        if (sizeof(T) == 4) *reinterpret_cast<float2 *>(dst + e) = make_float2(v[e] * k, v[e + 1] * k);
+        else *reinterpret_cast<__nv_bfloat162 *>(dst + e) = __floats2bfloat162_rn(v[e] * k, v[e + 1] * k);
+    }
+}
+
+template <typename T>
+cudaError_t launch_join_rows(const AttendArgs &a, cudaStream_t s) {
+    const dim3 grid((unsigned)(((long long)a.T * a.H + kJoinWarps - 1) / kJoinWarps)), block(32 * kJoinWarps);
+    const int w = padded_width(a.D);
+    return w == 64 ? launch_chained(join_kernel<T, 64>, grid, block, 0, s, true, a) : w == 128 ? launch_chained(join_kernel<T, 128>, grid, block, 0, s, true, a)
+                                                                                  : launch_chained(join_kernel<T, 256>, grid, block, 0, s, true, a);
+}
+
+}  // namespace
 
 void prefix_rows_pieces(AttendArgs &a, int max_ctas) {
     a.piece_rows = a.result_rows = tile_rows(padded_width(a.D), (long long)a.max_new * a.G);
@@ -17,6 +112,11 @@ cudaError_t launch_attend_prefix_rows(const AttendArgs &a, int sm_count, cudaStr
 
 cudaError_t launch_attend_rest_rows(const AttendArgs &a, int sm_count, cudaStream_t s, uint64_t *launches) {
     return launch_rows<Reads::Rest>((long long)a.max_new * a.G, a, sm_count, s, launches);
+}
+
+cudaError_t launch_attend_join(const AttendArgs &a, cudaStream_t s, uint64_t *launches) {
+    ++*launches;
+    return a.dtype == MOE_BF16 ? launch_join_rows<__nv_bfloat16>(a, s) : launch_join_rows<float>(a, s);
 }
 
 }  // namespace kv

@@ -52,6 +52,23 @@ struct FastDiv {
 #endif
 };
 
+#ifdef __CUDACC__
+// First request i in [0, n) with f(i + 1) > x, n where there is none; f does not fall.  By a whole warp, 32 probes at a time
+template <typename F>
+__device__ __forceinline__ int warp_find(int n, int x, F f) {
+    const int lane = threadIdx.x & 31;
+    int lo = 0, hi = n;
+#pragma unroll 1
+    while (hi - lo > 32) {
+        const int step = (hi - lo + 31) / 32, at = lo + (lane + 1) * step - 1;
+        const int before = __popc(__ballot_sync(0xffffffffu, at < hi && f(min(at, hi - 1) + 1) <= x));
+        lo = min(lo + before * step, hi);
+        hi = min(lo + step, hi);
+    }
+    return lo + __popc(__ballot_sync(0xffffffffu, lo + lane < hi && f(min(lo + lane, n - 1) + 1) <= x));
+}
+#endif
+
 struct TablesArgs {
     const int32_t *ctx, *fresh_tokens; int n;
     const int32_t *free_pages; int n_free;
@@ -126,13 +143,14 @@ struct AttendArgs {
     int32_t *status;
     // Shared prefixes.  Prefix: n groups, group i = requests [groups[i], groups[i + 1]) of n_members, kv_len its shared keys,
     // max_new the largest number of its new tokens.  Rest: request i reads the keys from start[i] on.  A row's sums, reference
-    // and denominator over its prefix lie in o_part [T][H][W] and o_ml [T][H], o_pieces being (-1, ...), or in the pieces of
+    // and denominator over what is behind the prefix lie in own_part [T][H][W] and own_ml [T][H]; those over its prefix
+    // in o_part and o_ml likewise, o_pieces being (-1, ...), or in the pieces of
     // its stretch, o_pieces being (first CTA, CTAs, row): that row of prompt_part and prompt_ml in slot 1 of the first CTA and
     // 0 of the others.  A slot has piece_rows rows, results of result_rows each where there are piece_results of them; piece_ctas CTAs
     // have slots
     const int32_t *groups; int n_members;
     const int32_t *start;
-    float *o_part; float2 *o_ml; int4 *o_pieces;
+    float *o_part, *own_part; float2 *o_ml, *own_ml; int4 *o_pieces;
     int piece_rows, result_rows, piece_results, piece_ctas;
     // Selected pages: [T][Hk][n_listed] columns of the request's row of the block table, -1: none
     const int32_t *listed; int n_listed;
@@ -146,6 +164,7 @@ size_t attend_part_floats(int w);          // per CTA of the grid
 void prefix_rows_pieces(AttendArgs &a, int max_ctas);          // how the kernel below lays out its pieces
 cudaError_t launch_attend_prefix_rows(const AttendArgs &a, int sm_count, cudaStream_t s, uint64_t *launches);
 cudaError_t launch_attend_rest_rows(const AttendArgs &a, int sm_count, cudaStream_t s, uint64_t *launches);
+cudaError_t launch_attend_join(const AttendArgs &a, cudaStream_t s, uint64_t *launches);
 cudaError_t launch_attend_listed(const AttendArgs &a, int sm_count, cudaStream_t s, uint64_t *launches);
 // prompts, on tcgen05 (kv_prompt.cu)
 cudaError_t launch_attend_prompt(const AttendArgs &a, int sm_count, cudaStream_t s, uint64_t *launches);

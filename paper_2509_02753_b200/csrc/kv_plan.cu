@@ -326,7 +326,7 @@ int moe_kv_shared_prefix(moe_kv_plan_t *p, const int32_t *cu_group, int32_t n_gr
 
 uint64_t moe_kv_shared_scratch_bytes(const moe_kv_plan_t *p, int32_t n_tokens, int32_t max_new) {
     if (!p || n_tokens < 1 || max_new < 0 || !reads_prefixes_once(p, n_tokens, max_new)) return 0;
-    return shared_rows_bytes(p, n_tokens) + (uint64_t)n_tokens * p->cfg.n_heads * (sizeof(int4) + sizeof(float2));
+    return 2 * shared_rows_bytes(p, n_tokens) + (uint64_t)n_tokens * p->cfg.n_heads * (sizeof(int4) + 2 * sizeof(float2));
 }
 
 int moe_kv_attention_shared(moe_kv_plan_t *p, const moe_kv_rows_t *q, int32_t T, const int32_t *cu_new, const int32_t *kv_len, int32_t n, int32_t max_new,
@@ -348,9 +348,12 @@ int moe_kv_attention_shared(moe_kv_plan_t *p, const moe_kv_rows_t *q, int32_t T,
     AttendArgs rest = attend_args(p, q, T, cu_new, kv_len, n, max_new, block_table, width, cache, n_pages, softmax_scale, k_scale, v_scale, out);
     rest.max_new = max_new > 0 && max_new < T ? max_new : T;
     rest.start = start;
+    const size_t rows = (size_t)T * c.n_heads;
     rest.o_part = (float *)scratch;
-    rest.o_pieces = (int4 *)((uint8_t *)scratch + shared_rows_bytes(p, T));
-    rest.o_ml = (float2 *)(rest.o_pieces + (size_t)T * c.n_heads);
+    rest.own_part = (float *)((uint8_t *)scratch + shared_rows_bytes(p, T));
+    rest.o_pieces = (int4 *)((uint8_t *)scratch + 2 * shared_rows_bytes(p, T));
+    rest.o_ml = (float2 *)(rest.o_pieces + rows);
+    rest.own_ml = rest.o_ml + rows;
     AttendArgs prefix = rest;
     prefix.kv_len = shared_len; prefix.n = n_groups; prefix.groups = cu_group; prefix.n_members = n;
     prefix.max_new = max_group > 0 && max_group < T ? max_group : T;
@@ -366,9 +369,10 @@ int moe_kv_attention_shared(moe_kv_plan_t *p, const moe_kv_rows_t *q, int32_t T,
     }
     rest.piece_rows = prefix.piece_rows; rest.result_rows = prefix.result_rows;
     rest.piece_results = prefix.piece_results; rest.piece_ctas = prefix.piece_ctas;
-    const cudaError_t err = few ? launch_attend_prefix_rows(prefix, p->sm_count, s, &p->launches) : launch_attend_prefix_prompt(prefix, p->sm_count, s, &p->launches);
-    if (err != cudaSuccess) return done(err);
-    return done(launch_attend_rest_rows(rest, p->sm_count, s, &p->launches));
+    cudaError_t err = few ? launch_attend_prefix_rows(prefix, p->sm_count, s, &p->launches) : launch_attend_prefix_prompt(prefix, p->sm_count, s, &p->launches);
+    if (err == cudaSuccess) err = launch_attend_rest_rows(rest, p->sm_count, s, &p->launches);
+    if (err == cudaSuccess) err = launch_attend_join(rest, s, &p->launches);
+    return done(err);
 }
 
 uint64_t moe_kv_summary_bytes(const moe_kv_config_t *cfg) {

@@ -52,6 +52,7 @@ constexpr float kTop = 14.f;                     // the largest weight is 2^kTop
 // with many short stretches would be last by far.  Alternating groups pass a tile in about half the time (with 5 for 3
 // there: 333 to 700 tokens of 15/5 heads 52 -> 49 us, 64 tokens on 16000 keys of 16/4 heads 83 -> 77)
 constexpr int kEntryTiles = 3, kEntryAlternate = 5;
+constexpr int kLeaves = 8, kOfTen = 7;
 
 // T: type of queries and outputs; fp32 queries and weights are two f16 parts each, with products for both.  GROUPS: softmax
 // warpgroups, each with its own scores and outputs.  TILES: row tiles of a stretch.  KEYS: keys of a tile
@@ -283,7 +284,10 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
     const uint32_t tmem = kTmem;
     bool dead = tmem_slot != kTmem;          // a wait ran out: nothing more is waited for or issued, the loops run out
     if (dead && tid == 0) atomicOr(a.status, MOE_KV_STATUS_TIMEOUT);
-    const long long total = line[a.n], share = max((total + gridDim.x - 1) / (long long)gridDim.x, 1ll);
+    const long long total = line[a.n];
+    // A prefix of few tiles leaves SMs to the kernel of what lies behind it, which starts beside this one
+    const long long ctas = PREFIX && total <= kLeaves * (long long)gridDim.x ? max((long long)gridDim.x * kOfTen / 10, 1ll) : (long long)gridDim.x;
+    const long long share = max((total + ctas - 1) / ctas, 1ll);
     const long long at = min(share * blockIdx.x, total);
     const long long end = min(at + share, total);
 
@@ -863,7 +867,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
                     a.o_pieces[out_row] = make_int4(p.cta0, p.cta1 + 1 - p.cta0, S::kAlternate ? row_in : t * kTileRows + row_in, 0);
             }
             tc::tc_fence_before();
-            if (!whole) {
+            if (PREFIX && p.cta0 != p.cta1) {
+                if (S::kAlternate) asm volatile("bar.sync 1, %0;" ::"n"(GROUPS * 128) : "memory");       // both groups' place is the next queries'
+            } else if (!whole) {
                 __threadfence();
                 asm volatile("bar.sync 1, %0;" ::"n"(GROUPS * 128) : "memory");
                 if (tid == 0) {

@@ -20,21 +20,6 @@ namespace {
 
 __device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
-// First request i in [0, n) with f(i + 1) > x, n where there is none; f does not fall.  By a whole warp, 32 probes at a time
-template <typename F>
-__device__ __forceinline__ int warp_find(int n, int x, F f) {
-    const int lane = threadIdx.x & 31;
-    int lo = 0, hi = n;
-#pragma unroll 1
-    while (hi - lo > 32) {
-        const int step = (hi - lo + 31) / 32, at = lo + (lane + 1) * step - 1;
-        const int before = __popc(__ballot_sync(0xffffffffu, at < hi && f(min(at, hi - 1) + 1) <= x));
-        lo = min(lo + before * step, hi);
-        hi = min(lo + step, hi);
-    }
-    return lo + __popc(__ballot_sync(0xffffffffu, lo + lane < hi && f(min(lo + lane, n - 1) + 1) <= x));
-}
-
 // Keys and new tokens of a request: as the attention takes them
 struct Request { int len, q0, nq; };
 __device__ __forceinline__ Request request_of(const SelectArgs &a, int i) {
