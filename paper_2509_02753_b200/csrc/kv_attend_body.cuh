@@ -305,6 +305,7 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
 
     int req = 0, len = 0, q0 = 0, nq = 0, sb = 0, wb = 0, nb = 0, row0 = 0, row1 = 0, units = 0, head = -1, begin = 0;
     long long place = 0;         // where the stretch begins (even: its first piece)
+    const int32_t *listed = nullptr;
     auto take = [&]() {
         if (simple) { len = len_s[req]; q0 = q0_s[req]; nq = nq_s[req]; }
         else lengths(req, len, q0, nq);
@@ -345,8 +346,8 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
             q0 = (int)(stretch / per);
             row0 = in / a.Hk * S::kRows;
             head = in % a.Hk;
-            take_token();
-            shape();
+            units = (int)many;
+            listed = a.listed + ((int64_t)q0 * a.Hk + head) * a.n_listed;
         } else if (even || head < 0) {
             int lo = 0, hi = a.n;
 #pragma unroll 1
@@ -408,6 +409,18 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
             cta0 = all ? (int)blockIdx.x : (int)(block0 / share);
             cta1 = all ? (int)blockIdx.x : (int)((block0 + units - 1) / share);
         }
+        // Listed: pages of this warp's first steps, asked for before the token's request is looked up
+        auto page_of = [&](int from) {
+            const int u = first + (warp + (from + (lane >> 1)) * kWarps) * kPair + (lane & 1);
+            return u < last ? listed[u >> a.page_shift] : -1;
+        };
+        int page_now = 0, page_then = 0;
+        if constexpr (kListed) {
+            page_now = page_of(0);
+            page_then = page_of(16);
+            take_token();
+            shape();
+        }
         const int present = sb + nb - wb;
         const int b1 = min(last, present);             // blocks [first, b1) of the stretch are loaded
 
@@ -425,20 +438,18 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
 
         // ---- this warp's blocks: the first copies start before the queries are read
         const int32_t *table = a.table + (int64_t)(kPrefix ? a.groups[req] : req) * a.width;
-        const int32_t *listed = kListed ? a.listed + ((int64_t)q0 * a.Hk + head) * a.n_listed : nullptr;
         const uint32_t my_ring = smem_u32(ring) + warp * S::kStages * S::kStageBytes, my_bar = smem_u32(&full[warp * S::kStages]);
         const uint8_t *my_ring_p = ring + warp * S::kStages * S::kStageBytes;
         const int steps = b1 > first ? (b1 - first + kPair - 1) / kPair : 0;
         const int mine = steps > warp ? (steps - warp + kWarps - 1) / kWarps : 0;
         auto block_at = [&](int u) { return u < sb ? u : wb + u - sb; };
         // 16 steps at a time: lane l finds the cache block that is block l%2 of step (from + l/2); -1: none
-        auto find_blocks = [&](int from, int &b) {
+        auto find_blocks = [&](int from, int page, int &b) {
             const int k = from + (lane >> 1), u = first + (warp + k * kWarps) * kPair + (lane & 1);
             b = 0;
             if (k >= mine || u >= b1) return -1;
             b = block_at(u);
             if (kListed) {
-                const int page = listed[u >> a.page_shift];
                 if (page < 0 || page >= a.width) {
                     if (page != -1) atomicOr(a.status, MOE_KV_STATUS_BAD_INDEX);
                     return -1;
@@ -451,7 +462,7 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
             return ((pg * a.Hk + head) << a.page_shift) + (b & ((1 << a.page_shift) - 1));
         };
         int now_at, then_at;          // which blocks of the request they are
-        int now = find_blocks(0, now_at), then = find_blocks(16, then_at);
+        int now = find_blocks(0, page_now, now_at), then = find_blocks(16, page_then, then_at);
         uint32_t has_now = __ballot_sync(0xffffffffu, now >= 0), has_then = __ballot_sync(0xffffffffu, then >= 0);
         // copies of step (from + d), d < 32: by the two lanes that found its blocks
         auto issue = [&](int d, int stage) {
@@ -531,7 +542,7 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
             if (k - from == 16) {
                 from = k;
                 now = then; has_now = has_then; now_at = then_at;
-                then = find_blocks(from + 16, then_at);
+                then = find_blocks(from + 16, kListed ? page_of(from + 16) : 0, then_at);
                 has_then = __ballot_sync(0xffffffffu, then >= 0);
             }
             const int stage = k % S::kStages;

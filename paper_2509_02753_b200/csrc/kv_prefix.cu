@@ -3,8 +3,8 @@
 //   pages_g = the leading columns of the block table in which all members of group g have the same page, none behind a
 //             member's last full page in front of its new tokens;   shared_g = pages_g * P, 0 for a group of one
 //
-// Bound by latency up to thousands of table entries.  A cluster has a group, a warp a member at a time, 128 columns a step,
-// and no step goes behind what some member's end or difference has cut off.  The pages' numbers are compared, not the keys:
+// Bound by latency up to thousands of table entries.  A cluster has a group, a warp 256 columns of a member at a time, the first
+// columns of all members first, and none goes behind what some member's end or difference has cut off.  The pages' numbers are compared, not the keys:
 // what the tables do not share is not shared, whatever a caller meant, and the attention is right for any groups.
 #include "kv_internal.h"
 
@@ -14,6 +14,7 @@ namespace {
 
 constexpr int kWarps = 8, kThreads = 32 * kWarps;
 constexpr int kMaxCluster = 8;
+constexpr int kColumns = 256;          // of a member, a warp's step
 
 __device__ __forceinline__ uint32_t cluster_rank() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
 __device__ __forceinline__ void st_cta0(const int *p, int v) {
@@ -54,30 +55,26 @@ __global__ void __launch_bounds__(kThreads) prefix_kernel(PrefixArgs a, int clus
         if (lane == 0) atomicMin(&least_s, full);
         __syncthreads();
         const int32_t *lead = a.table + (int64_t)r0 * a.width;
-        for (int i = r0 + 1 + rank * kWarps + warp; i < r1; i += cluster * kWarps) {
-            const int32_t *row = a.table + (int64_t)i * a.width;
-            int most = *reinterpret_cast<volatile int *>(&least_s);
-#pragma unroll 1
-            for (int col = 0; col < most; col += 128) {
-                int x[4], y[4];
+        const int others = r1 - r0 - 1;
+        int member = rank * kWarps + warp, col = 0;
+        auto on = [&](int by) { for (member += by; member >= others; member -= others) col += kColumns; };
+        for (on(0); col < *reinterpret_cast<volatile int *>(&least_s); on(cluster * kWarps)) {
+            const int most = *reinterpret_cast<volatile int *>(&least_s);
+            const int32_t *row = a.table + (int64_t)(r0 + 1 + member) * a.width;
+            int x[kColumns / 32], y[kColumns / 32];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int at = col + 32 * j + lane;
-                    x[j] = at < most ? lead[at] : 0;
-                    y[j] = at < most ? row[at] : 0;
-                }
-                int differs = INT32_MAX;
-#pragma unroll
-                for (int j = 3; j >= 0; --j) {
-                    const uint32_t off = __ballot_sync(0xffffffffu, x[j] != y[j] || x[j] < 0);
-                    if (off) differs = col + 32 * j + __ffs(off) - 1;
-                }
-                if (differs != INT32_MAX) {
-                    if (lane == 0) atomicMin(&least_s, differs);
-                    break;
-                }
-                most = min(most, *reinterpret_cast<volatile int *>(&least_s));
+            for (int j = 0; j < kColumns / 32; ++j) {
+                const int at = col + 32 * j + lane;
+                x[j] = at < most ? lead[at] : 0;
+                y[j] = at < most ? row[at] : 0;
             }
+            int differs = INT32_MAX;
+#pragma unroll
+            for (int j = kColumns / 32 - 1; j >= 0; --j) {
+                const uint32_t off = __ballot_sync(0xffffffffu, x[j] != y[j] || x[j] < 0);
+                if (off) differs = col + 32 * j + __ffs(off) - 1;
+            }
+            if (differs != INT32_MAX && lane == 0) atomicMin(&least_s, differs);
         }
         __syncthreads();
         pages = least_s;
@@ -112,10 +109,10 @@ __global__ void __launch_bounds__(kThreads) prefix_kernel(PrefixArgs a, int clus
 }  // namespace
 
 cudaError_t launch_prefix(const PrefixArgs &a, int sm_count, cudaStream_t s, uint64_t *launches) {
-    // a member for every warp at a time, if the groups are alike, while there are SMs
+    // more CTAs for a group while there are SMs and, if the groups are alike, more steps than warps
     const int groups = a.n_groups > 0 ? a.n_groups : 1;
     int cluster = 1;
-    while (cluster < kMaxCluster && a.n > groups * cluster * kWarps && (long long)groups * cluster * 2 <= 2 * sm_count) cluster *= 2;
+    while (cluster < kMaxCluster && (long long)a.n * ((a.width + kColumns - 1) / kColumns) > (long long)groups * cluster * kWarps && (long long)groups * cluster * 2 <= 2 * sm_count) cluster *= 2;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(groups * cluster));
     cfg.blockDim = dim3(kThreads);

@@ -2,8 +2,10 @@
 //
 //   summarise   hi_d = max, lo_d = min over the page's tokens of the stored key (code * scale: exact in f16);
 //               m = max_d(|hi_d|, |lo_d|), step = m / 127, codes ceil(127 hi_d / m) and floor(127 lo_d / m): what is held
-//               bounds the keys from both sides.  127 hi_d is exact in fp32 and 127 hi_d / m, where it is no whole number, lies
-//               2^-6 or more away from one (m has 6 significant bits), so one rounded division finds the right whole number
+//               bounds the keys from both sides.  A stored key and m are odd numbers up to 45 times powers of two: 127 hi_d / m
+//               is b / (a 2^k) of whole numbers with b <= 127 * 45, so where it is no whole number the nearest one is 1/b of it
+//               away or more.  The product with 127/m in fp32, off by 2^-22, shrunk towards 0 or away from it by 2^-15 of
+//               itself, is therefore on the right side of every whole number
 //   select      u_d = sum_g max(q_gd, 0), w_d = sum_g min(q_gd, 0) over the query heads g of a key/value head: no key of the
 //               page has a larger sum of scores than sum_d (u_d hi_d + w_d lo_d).  Both vectors become whole numbers up to 127
 //               of one step, which does not matter: it is the same for all pages.  The sum of 2 W products of 8-bit
@@ -62,7 +64,7 @@ __global__ void __launch_bounds__(32 * kSumWarps) summarise_kernel(SelectArgs a,
     __half2 hi[16], lo[16];
 #pragma unroll
     for (int d = 0; d < 16; ++d) { hi[d] = __half2half2(__ushort_as_half(0xfc00)); lo[d] = __half2half2(__ushort_as_half(0x7c00)); }
-#pragma unroll 4
+#pragma unroll 8
     for (int t = mine; t < tokens; t += kAtOnce) {
         const uint8_t *blk = blocks + (t >> 4) * block_bytes(W);
         const uint4 codes = __ldg(reinterpret_cast<const uint4 *>(blk + (t & 15) * (W / 2) + part * 16));
@@ -108,12 +110,16 @@ __global__ void __launch_bounds__(32 * kSumWarps) summarise_kernel(SelectArgs a,
 #pragma unroll
         for (int d = 0; d < 8; ++d) hi[d] = second ? hi[8 + d] : hi[d];
         if (m > 0.f) {
+            // upwards: ceil of the number less 2^-15 of its magnitude; downwards: the same of its negative
+            const float inv = (low ? -127.f : 127.f) / m, sign = low ? -1.f : 1.f;
+            auto up = [&](float x) {
+                const float q = x * inv;
+                return (uint32_t)(int)(sign * ceilf(fmaf(fabsf(q), -0x1p-15f, q))) & 0xffu;
+            };
 #pragma unroll
             for (int d = 0; d < 8; ++d) {
                 const float2 x = __half22float2(hi[d]);
-                const float c0 = __fdiv_rn(x.x * 127.f, m), c1 = __fdiv_rn(x.y * 127.f, m);
-                const int b0 = (int)(low ? floorf(c0) : ceilf(c0)), b1 = (int)(low ? floorf(c1) : ceilf(c1));
-                packed[d / 2] |= (((uint32_t)b0 & 0xffu) | (((uint32_t)b1 & 0xffu) << 8)) << (16 * (d & 1));
+                packed[d / 2] |= (up(x.x) | (up(x.y) << 8)) << (16 * (d & 1));
             }
         }
         *reinterpret_cast<uint4 *>(out + (low ? W : 0) + part * 32 + (second ? 16 : 0)) = make_uint4(packed[0], packed[1], packed[2], packed[3]);
@@ -330,8 +336,17 @@ __global__ void __launch_bounds__(kThreads) select_kernel(SelectArgs a, int clus
         turn ^= 1;
         return s;
     };
-    uint32_t least = 0xffffffffu, most = 0u;
-    for (int x = first_lane; x < n; x += kStride) { least = min(least, key[x]); most = max(most, key[x]); }
+    // A thread keeps its first scores in registers; 0, which no score is, behind the last
+    constexpr int kKept = kAll ? 4 : 16;
+    uint32_t kept[kKept], least = 0xffffffffu, most = 0u;
+#pragma unroll
+    for (int j = 0; j < kKept; ++j) {
+        const int x = first_lane + j * kStride;
+        kept[j] = x < n ? key[x] : 0u;
+        least = min(least, x < n ? kept[j] : 0xffffffffu);
+        most = max(most, kept[j]);
+    }
+    for (int x = first_lane + kKept * kStride; x < n; x += kStride) { least = min(least, key[x]); most = max(most, key[x]); }
     least = __reduce_min_sync(0xffffffffu, least);
     most = __reduce_max_sync(0xffffffffu, most);
     if (kAll) {
@@ -340,15 +355,21 @@ __global__ void __launch_bounds__(kThreads) select_kernel(SelectArgs a, int clus
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) { least = min(least, low_s[w]); most = max(most, high_s[w]); }
     }
-    // the leading bits that all have are the answer's; below them, a bit is set if `need` scores reach that far
+    // The leading bits that all have are the edge's; below them, a bit is set if `need` scores reach that far.  Once just so many
+    // do, these are the answer: after about log2(n) bits, where one bit after the other to the last took 26 of them (select 64x32768,
+    // n = 509: 7 us of the call's 20)
     const int open = 32 - __clz(least ^ most);
     uint32_t edge = open == 32 ? 0u : most >> open << open;
 #pragma unroll 1
     for (int bit = open - 1; bit >= 0; --bit) {
         const uint32_t reach = edge | 1u << bit;
         int mine = 0;
-        for (int x = first_lane; x < n; x += kStride) mine += key[x] >= reach;
-        if (all_of(mine) >= need) edge = reach;
+#pragma unroll
+        for (int j = 0; j < kKept; ++j) mine += kept[j] >= reach;
+        for (int x = first_lane + kKept * kStride; x < n; x += kStride) mine += key[x] >= reach;
+        const int reached = all_of(mine);
+        if (reached >= need) edge = reach;
+        if (reached == need) break;
     }
     // this warp's part of the pages, and how many above and at the edge lie in front of it
     const int part = kAll ? ((n + kWarps - 1) / kWarps + 31) & ~31 : n, begin = kAll ? min(warp * part, n) : 0, end = min(begin + part, n);

@@ -110,17 +110,25 @@ def test_null_arguments():
 
 
 def test_a_bound_is_the_next_whole_number():
-    """The kernel divides 127 x by the largest magnitude in fp32 and rounds outwards; in whole numbers, over every pair of
-    magnitudes that a code (0 to 12 halves) times the fraction of a scale (8 to 15 eighths) can have, up to powers of two.
-    Outside of 2^-8 to 1 the quotient is a whole number below 1 (or none), for which the same holds with more room."""
-    odd = sorted({c * f for c in (1, 2, 3, 4, 6, 8, 12) for f in range(8, 16)})
+    """The kernel takes 127 x / m as a product with 127 / m in fp32, less 2^-15 of its magnitude, and rounds up; downwards the same
+    of the negative.  Against whole numbers, over every pair of magnitudes that a code (0 to 12 halves) times a scale (1 to
+    15 eighths) can have, up to powers of two, and both signs."""
+    f = np.float32
+    odd = sorted({c * x for c in (1, 2, 3, 4, 6, 8, 12) for x in range(1, 16)})
+
+    def up(q):
+        return int(np.ceil(f(float(q) - 2.0 ** -15 * abs(float(q)))))
+
     for m in odd:
         for x in odd:
-            for shift in range(-8, 8):
+            for shift in range(-22, 8):
                 num, den = (x << shift, m) if shift >= 0 else (x, m << -shift)
                 if num > den:
                     continue
-                assert int(np.ceil(np.float32(127 * num) / np.float32(den))) == -(-127 * num // den)
+                inv = f(127) / f(den)
+                for s in (1, -1):
+                    assert up(f(s * num) * inv) == -((-s * 127 * num) // den)
+                    assert -up(f(s * num) * -inv) == (s * 127 * num) // den
 
 
 # ------------------------------------------------------------------------------------------ shared prefixes
