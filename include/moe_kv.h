@@ -202,9 +202,10 @@ int moe_kv_shared_prefix(moe_kv_plan_t *plan, const int32_t *cu_group, int32_t n
                          const int32_t *kv_len, int32_t n_requests, const int32_t *block_table,
                          int32_t table_width, int32_t *shared_len, int32_t *start, void *cuda_stream);
 
-/* Bytes of scratch that moe_kv_attention_shared wants for n_tokens and max_new; 0 where it reads the keys
- * request by request (see there) and for bad arguments. */
-uint64_t moe_kv_shared_scratch_bytes(const moe_kv_plan_t *plan, int32_t n_tokens, int32_t max_new);
+/* Bytes of scratch that moe_kv_attention_shared wants for these arguments; 0 where it reads the keys request
+ * by request (see there) and for bad arguments. */
+uint64_t moe_kv_shared_scratch_bytes(const moe_kv_plan_t *plan, int32_t n_tokens, int32_t n_requests, int32_t max_new,
+                                     int32_t max_group, int32_t table_width);
 
 /*
  * moe_kv_attention_shared: what moe_kv_attention computes without a window, with shared_len and start as
@@ -212,9 +213,10 @@ uint64_t moe_kv_shared_scratch_bytes(const moe_kv_plan_t *plan, int32_t n_tokens
  * members attend to the group's prefix together, each request's rows to what lies behind it, and both
  * results are joined in fp32 before the only rounding.
  * max_new, max_group: the largest number of new tokens of a request and of a group; they only choose the
- * kernels; 0 = unknown.  Where max_new times the query heads of a key/value head passes 32 (64 for
- * head_dim above 128), and with max_new unknown where n_tokens does, a request's own rows
- * share its keys already and the call is moe_kv_attention's.  scratch: 16-byte aligned device memory of
+ * kernels; 0 = unknown, which counts as n_tokens.  The call is moe_kv_attention's where sharing gains nothing: where max_new
+ * times the query heads of a key/value head passes 32 (64 for head_dim above 128), for a request's own
+ * rows share its keys then, and where the cache that n_requests tables of this width can hold is small (less
+ * than 75 MB saved, 150 MB with at most 32 (64) rows a group).  scratch: 16-byte aligned device memory of
  * scratch_bytes >= moe_kv_shared_scratch_bytes, in use until the call's work is done.
  * A start outside 0..kv_len - new tokens sets BAD_INDEX; start and shared_len that do not belong together
  * give rows that no formula stands for.

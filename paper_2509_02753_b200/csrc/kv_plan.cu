@@ -31,6 +31,7 @@ constexpr int64_t kMaxRows = 1 << 30;         // max_tokens * n_heads
 constexpr int64_t kMaxContext = 1 << 30;      // tokens that a row of a block table may stand for
 constexpr int kPartRows = 32;         // rows of a piece, at most
 constexpr int kPassRows = 32;         // query rows of a pass over the keys in kv_attend.cu
+constexpr double kWorthMany = 75e6, kWorthFew = 150e6;          // bytes of the cache that reading prefixes once has to save
 
 size_t elem_size(int dtype) { return dtype == MOE_BF16 ? 2 : 4; }
 bool aligned(const void *p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
@@ -101,11 +102,22 @@ AttendArgs attend_args(const moe_kv_plan *p, const moe_kv_rows_t *q, int32_t T, 
 // Query rows of a key/value head that kv_attend_body.cuh takes before kv_prompt_body.cuh does (see moe_kv_attention)
 int row_limit(const moe_kv_config_t &c) { return padded_width(c.head_dim) == 256 ? 2 * kPassRows : kPassRows; }
 
-// Whether a call's prefixes are read once for a group.  A request of more rows than one pass over the keys serves gains
-// nothing by it: its own rows share the reading already
-bool reads_prefixes_once(const moe_kv_plan *p, int32_t T, int32_t max_new) {
-    const long long most = max_new > 0 && max_new < T ? max_new : T;
-    return most * (p->cfg.n_heads / p->cfg.n_kv_heads) <= row_limit(p->cfg);
+// Whether a call's prefixes are read once for a group.  Not where a request has more rows than one pass over the keys serves
+// (its own rows share the reading already), nor where too little could be saved: what the tables can hold, less one member's
+// share of it, has to be worth two more launches.  In us, bf16 (prefix + up to 500 keys of its own, without / with sharing):
+//   64 requests, 32/8 heads of 128: 512 keys (75 MB) 25.2 / 27.8, 1024 (112 MB) 33.4 / 33.0, 4096 80 / 40, 32768 514 / 72
+//   16 of these: 2048 keys (40 MB) 19.0 / 20.1, 8192 (153 MB) 45.8 / 29.9;   32 of 16/2 heads of 256: 4096 keys (77 MB) 29.0 / 28.9
+//   32 of 16/4 heads of 128 in fp32: 1024 keys (21 MB) 15.5 / 22.6, 4096 (77 MB) 31.4 / 28.7
+// and where a group's rows are few (kv_attend_body.cuh reads the prefix in passes of 32 rows, which hide less of its latency):
+//   8 of 32/8 heads of 128: 8192 keys (76 MB) 26.7 / 30.4, 32768 (303 MB) 75 / 44;   16 groups of 4: 1024 keys (83 MB) 30 / 39,
+//   4096 (309 MB) 78 / 70
+bool reads_prefixes_once(const moe_kv_plan *p, int32_t T, int32_t n, int32_t max_new, int32_t max_group, int32_t width) {
+    const moe_kv_config_t &c = p->cfg;
+    const long long request = max_new > 0 && max_new < T ? max_new : T, group = max_group > 0 && max_group < T ? max_group : T, g = c.n_heads / c.n_kv_heads;
+    if (request * g > row_limit(c)) return false;
+    const double bytes = (double)n * width * c.page_size * c.n_kv_heads * block_bytes(padded_width(c.head_dim)) / kBlockTokens;
+    const double saved = bytes * (1.0 - (double)request / (double)(group > request ? group : request));
+    return saved >= (group * g > row_limit(c) ? kWorthMany : kWorthFew);
 }
 
 uint64_t shared_rows_bytes(const moe_kv_plan *p, int32_t T) { return (uint64_t)T * p->cfg.n_heads * padded_width(p->cfg.head_dim) * sizeof(float); }
@@ -324,8 +336,8 @@ int moe_kv_shared_prefix(moe_kv_plan_t *p, const int32_t *cu_group, int32_t n_gr
     return done(launch_prefix(a, p->sm_count, (cudaStream_t)stream, &p->launches));
 }
 
-uint64_t moe_kv_shared_scratch_bytes(const moe_kv_plan_t *p, int32_t n_tokens, int32_t max_new) {
-    if (!p || n_tokens < 1 || max_new < 0 || !reads_prefixes_once(p, n_tokens, max_new)) return 0;
+uint64_t moe_kv_shared_scratch_bytes(const moe_kv_plan_t *p, int32_t n_tokens, int32_t n, int32_t max_new, int32_t max_group, int32_t width) {
+    if (!p || n_tokens < 1 || n < 1 || max_new < 0 || max_group < 0 || width < 1 || !reads_prefixes_once(p, n_tokens, n, max_new, max_group, width)) return 0;
     return 2 * shared_rows_bytes(p, n_tokens) + (uint64_t)n_tokens * p->cfg.n_heads * (sizeof(int4) + 2 * sizeof(float2));
 }
 
@@ -342,9 +354,9 @@ int moe_kv_attention_shared(moe_kv_plan_t *p, const moe_kv_rows_t *q, int32_t T,
     if (!cu_new || !kv_len || !out || (width > 0 && !block_table) || (n_pages > 0 && !cache)) return MOE_ERR_INVALID_ARG;
     if (n_groups > 0 && (!cu_group || !shared_len || !start)) return MOE_ERR_INVALID_ARG;
     if (!aligned(cache, 16) || !aligned(out, 16) || !aligned(scratch, 16) || !words(cu_new, kv_len, block_table, cu_group, shared_len, start)) return MOE_ERR_ALIGN;
-    if (n_groups == 0 || !reads_prefixes_once(p, T, max_new))
+    if (n_groups == 0 || !reads_prefixes_once(p, T, n, max_new, max_group, width))
         return moe_kv_attention(p, q, T, cu_new, kv_len, n, max_new, block_table, width, cache, n_pages, softmax_scale, k_scale, v_scale, 0, 0, out, stream);
-    if (!scratch || scratch_bytes < moe_kv_shared_scratch_bytes(p, T, max_new)) return MOE_ERR_WORKSPACE;
+    if (!scratch || scratch_bytes < moe_kv_shared_scratch_bytes(p, T, n, max_new, max_group, width)) return MOE_ERR_WORKSPACE;
     AttendArgs rest = attend_args(p, q, T, cu_new, kv_len, n, max_new, block_table, width, cache, n_pages, softmax_scale, k_scale, v_scale, out);
     rest.max_new = max_new > 0 && max_new < T ? max_new : T;
     rest.start = start;

@@ -88,7 +88,7 @@ def load_library() -> ctypes.CDLL:
     lib.moe_kv_read.argtypes = [vp, vp, i32, vp, i32, f32, f32, vp, vp, vp]
     lib.moe_kv_attention.argtypes = [vp, rows, i32, vp, vp, i32, i32, vp, i32, vp, i32, f32, f32, f32, i32, i32, vp, vp]
     lib.moe_kv_shared_prefix.argtypes = [vp, vp, i32, vp, vp, i32, vp, i32, vp, vp, vp]
-    lib.moe_kv_shared_scratch_bytes.argtypes = [vp, i32, i32]
+    lib.moe_kv_shared_scratch_bytes.argtypes = [vp, i32, i32, i32, i32, i32]
     lib.moe_kv_attention_shared.argtypes = [vp, rows, i32, vp, vp, i32, i32, vp, i32, vp, i32, vp, i32, i32, vp, vp, f32, f32, f32, vp, u64, vp, vp]
     lib.moe_kv_summary_bytes.argtypes = [P(moe_kv_config_t)]
     lib.moe_kv_summarise.argtypes = [vp, vp, vp, i32, i32, vp, i32, vp, i32, vp, vp]

@@ -7,6 +7,34 @@ import kv_reference as ref
 F = np.float32
 
 
+def decode_all(cache, dim):
+    """kv_reference.decode_all, all bytes at once."""
+    w = ref.width(dim)
+    token, d = np.arange(16)[:, None], np.arange(dim)[None, :]
+    shift = 4 * (d % 2) + 0 * token
+    parts = ((token * (w // 2) + d // 2, 16 * w + token * (w // 16) + d // 16), (ref.value_at(w, token, d)[0], 17 * w + d // 16 * 16 + token))
+    scale = ref.e4m3_value(np.arange(256))
+    code = np.concatenate((ref.GRID, -ref.GRID))
+    out = []
+    for at, sc in parts:
+        x = code[(cache[..., at] >> shift) & 15] * scale[cache[..., sc]]
+        out.append(x.reshape(*cache.shape[:2], -1, dim))
+    return out
+
+
+def store(cache, k, v, slots, page, k_scale, v_scale):
+    """kv_reference.store, all rows at once; no slot twice."""
+    dim, slots = k.shape[-1], np.asarray(slots)
+    w = ref.width(dim)
+    token, d, g = (slots % 16)[:, None, None], np.arange(0, w, 2)[None, None, :], np.arange(w // 16)[None, None, :]
+    where = (slots // page)[:, None, None], np.arange(k.shape[1])[None, :, None], (slots % page // 16)[:, None, None]
+    for x, factor, key in ((k, k_scale, True), (v, v_scale, False)):
+        codes, scales = ref.quantise(x, factor)
+        at = token * (w // 2) + d // 2 if key else ref.value_at(w, token, d)[0]
+        cache[where + (at,)] = codes[..., 0::2] | (codes[..., 1::2] << 4)
+        cache[where + (16 * w + token * (w // 16) + g if key else 17 * w + g * 16 + token,)] = scales
+
+
 def shared_prefix(groups, cu, kv_len, table, page):
     n, width = table.shape
     shared, start = [], [0] * n
@@ -88,7 +116,7 @@ def attention_selected(q, cu, kv_len, table, cache, selected, page, scale, k_sca
     T, H, dim = q.shape
     heads = cache.shape[1]
     G = H // heads
-    k_all, v_all = ref.decode_all(cache, dim)
+    k_all, v_all = decode_all(cache, dim)
     out, spread, exponent, count = np.zeros((T, H, dim)), np.zeros((T, H, dim)), np.zeros((T, H, 1)), np.ones((T, H, 1))
     for i in range(len(kv_len)):
         for t in range(cu[i], cu[i + 1]):
@@ -109,4 +137,31 @@ def attention_selected(q, cu, kv_len, table, cache, selected, page, scale, k_sca
                     out[r], spread[r] = weight @ v, weight @ np.abs(v)
                     exponent[r] = (np.abs(k) @ np.abs(row)).max() * abs(scale)
                     count[r] = len(at)
+    return out, spread, exponent, count
+
+
+def attention(q, cu, kv_len, table, cache, page, scale, k_scale, v_scale):
+    """(out, spread, exponent, count) as kv_reference.attention without a window, a request's rows at once; every page is in the cache."""
+    T, H, dim = q.shape
+    heads = cache.shape[1]
+    G = H // heads
+    out, spread, exponent, count = np.zeros((T, H, dim)), np.zeros((T, H, dim)), np.zeros((T, H, 1)), np.ones((T, H, 1))
+    for i in range(len(kv_len)):
+        n, rows = int(kv_len[i]), slice(cu[i], cu[i + 1])
+        new = cu[i + 1] - cu[i]
+        if n == 0 or new == 0:
+            continue
+        k, v = (x.transpose(1, 0, 2, 3).reshape(heads, -1, dim)[:, :n] * s for x, s in zip(decode_all(cache[table[i, : -(-n // page)]], dim), (k_scale, v_scale)))
+        row = q[rows].astype(np.float64).reshape(new, heads, G, dim)
+        see = np.arange(n) <= n - new + np.arange(new)[:, None]
+        x = np.einsum("thgd,hkd->thgk", row, k) * scale
+        x = np.where(see[:, None, None], x, -np.inf)
+        top = x.max(-1, keepdims=True)
+        w = np.exp(x - np.where(top > -np.inf, top, 0.0))
+        w /= np.maximum(w.sum(-1, keepdims=True), 1e-300)
+        out[rows] = np.einsum("thgk,hkd->thgd", w, v).reshape(new, H, dim)
+        spread[rows] = np.einsum("thgk,hkd->thgd", w, np.abs(v)).reshape(new, H, dim)
+        reach = np.where(see[:, None, None], np.einsum("thgd,hkd->thgk", np.abs(row), np.abs(k)), 0.0).max(-1)
+        exponent[rows] = reach.reshape(new, H, 1) * abs(scale)
+        count[rows] = np.maximum(see.sum(1), 1).reshape(new, 1, 1)
     return out, spread, exponent, count

@@ -66,7 +66,7 @@ class Batch:
             if todo:
                 x = rng.standard_normal((2, len(todo), kv, dim)).astype(np.float32)
                 x[0, :, :, dim // 3] *= 6 * loud
-                ref.store(self.cache, x[0], x[1], [int(self.table[i, j // page]) * page + j % page for j in todo], page, KS, VS)
+                plain.store(self.cache, x[0], x[1], [int(self.table[i, j // page]) * page + j % page for j in todo], page, KS, VS)
         self.lens, self.new, self.page, self.dtype, self.heads, self.kv, self.dim = lens, new, page, dtype, heads, kv, dim
         self.cu = np.concatenate(([0], np.cumsum(new))).astype(np.int32)
         self.q = queries(rng, int(self.cu[-1]) + extra_rows, heads, dim, dtype, pad)
@@ -86,7 +86,7 @@ class Batch:
 
     def reference(self):
         n = int(self.cu[-1])
-        return ref.attention(host(self.q)[:n], self.cu, self.lens, self.table, self.cache, self.page, 0, 0, 1.0 / math.sqrt(self.dim), float(np.float32(KS)), float(np.float32(VS)))
+        return plain.attention(host(self.q)[:n], self.cu, self.lens, self.table, self.cache, self.page, 1.0 / math.sqrt(self.dim), float(np.float32(KS)), float(np.float32(VS)))
 
 
 # ------------------------------------------------------------------------------------------ no device needed
@@ -100,7 +100,7 @@ def test_summary_bytes(dim, kv, want):
 
 def test_null_arguments():
     lib = K.load_library()
-    assert lib.moe_kv_summary_bytes(None) == 0 and lib.moe_kv_shared_scratch_bytes(None, 1, 1) == 0
+    assert lib.moe_kv_summary_bytes(None) == 0 and lib.moe_kv_shared_scratch_bytes(None, 1, 1, 1, 1, 1) == 0
     assert lib.moe_kv_shared_prefix(None, None, 0, None, None, 0, None, 0, None, None, None) == -1
     assert lib.moe_kv_attention_shared(None, None, 0, None, None, 0, 0, None, 0, None, 0, None, 0, 0, None, None, 1.0, 1.0, 1.0, None, 0, None, None) == -1
     assert lib.moe_kv_summarise(None, None, None, 0, 0, None, 0, None, 0, None, None) == -1
@@ -129,6 +129,25 @@ def test_a_bound_is_the_next_whole_number():
                 for s in (1, -1):
                     assert up(f(s * num) * inv) == -((-s * 127 * num) // den)
                     assert -up(f(s * num) * -inv) == (s * 127 * num) // den
+
+
+@pytest.mark.parametrize("dim", [8, 64, 80, 128, 200, 256])
+def test_the_references_agree(dim):
+    """What stores and decodes all at once does as the loops of kv_reference.py."""
+    rng = np.random.default_rng(dim)
+    a, b = np.zeros((2, 5, 3, 2, ref.block_bytes(dim)), np.uint8)
+    x = rng.standard_normal((2, 40, 3, dim)).astype(np.float32)
+    slots = rng.permutation(160)[:40]
+    ref.store(a, x[0], x[1], slots, 32, KS, VS)
+    plain.store(b, x[0], x[1], slots, 32, KS, VS)
+    assert np.array_equal(a, b)
+    for one, other in zip(ref.decode_all(a, dim), plain.decode_all(a, dim)):
+        assert np.array_equal(one, other)
+    q, cu, lens, table = rng.standard_normal((5, 6, dim)), np.array([0, 2, 2, 5]), [70, 0, 2], np.array([[4, 0, 2], [9, 9, 9], [1, 9, 9]])
+    want = ref.attention(q, cu, lens, table, a, 32, 0, 0, 0.3, KS, VS)
+    got = plain.attention(q, cu, lens, table, a, 32, 0.3, KS, VS)
+    for one, other in zip(want, got):
+        assert np.allclose(one, other, rtol=1e-12, atol=1e-14)
 
 
 # ------------------------------------------------------------------------------------------ shared prefixes
@@ -181,7 +200,17 @@ def test_what_is_not_shared():
     check_prefix([0, 3, 2, 4], [1, 1, 1, 1], [96] * 4, table, 16, K.STATUS_BAD_INDEX, ([0, 0, 0], [0, 0, 0, 0]))
 
 
-def shared_case(seed, lens, new, heads, kv, dim, page, dtype, groups, shared, max_new=None, max_group=None, scale=None, **more):
+def wide(n, kv, dim, page, share):
+    """Columns of a table with which sharing counts as worth it, `share` being what one member has of a group's tokens."""
+    return int(150e6 / (1 - share) / (n * kv * ref.block_bytes(dim) / 16) / page) + 1
+
+
+def shared_case(seed, lens, new, heads, kv, dim, page, dtype, groups, shared, max_new=None, max_group=None, columns=None, **more):
+    """Tables so wide that the prefixes are read once, unless `columns` says otherwise."""
+    if columns is None:
+        members = max([0] + [b - a for a, b in zip(groups, groups[1:])])
+        columns = wide(len(lens), kv, dim, page, max(new) / max(sum(new[a: b]) for a, b in zip(groups, groups[1:])) if members > 1 else 0.5)
+    more["columns"] = columns
     b = Batch(seed, lens, new, heads, kv, dim, page, dtype, groups, shared, **more)
     with b.plan() as plan:
         g = i32(groups)
@@ -253,14 +282,16 @@ def test_a_long_prefix_is_split(dtype):
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_hints_choose_kernels_not_results(dtype):
     lens, new, groups = [100, 90, 70, 81, 200, 120], [1, 2, 1, 1, 3, 1], [0, 4, 6]
-    for max_new, max_group in ((3, 0), (1, 1), (0, 0), (9, 2), (3, 100)):
+    for max_new, max_group in ((3, 0), (1, 1), (0, 0), (9, 2), (3, 100), (1, 2), (3, 5)):
         shared_case(11, lens, new, 4, 2, 64, 16, dtype, groups, [4, 7], max_new=max_new, max_group=max_group)
+        shared_case(11, lens, new, 4, 2, 64, 16, dtype, groups, [4, 7], max_new=max_new, max_group=max_group, columns=0)
 
 
 @gpu
-def test_requests_of_many_rows_read_their_keys_themselves():
-    assert shared_case(12, [100, 90], [40, 1], 4, 2, 64, 16, BF16, [0, 2], [3]) == 1          # a prompt and a token
-    assert shared_case(12, [100, 100], [40, 40], 4, 2, 64, 16, BF16, [0, 2], [3]) == 1
+def test_requests_of_many_rows_and_small_batches_read_their_keys_themselves():
+    assert shared_case(12, [100, 90, 95], [1, 1, 1], 4, 2, 64, 16, BF16, [0, 3], [3], columns=40) == 1
+    assert shared_case(12, [100, 90], [40, 1], 4, 2, 64, 16, BF16, [0, 2], [3], columns=40) == 1          # a prompt and a token
+    assert shared_case(12, [100, 100], [40, 40], 4, 2, 64, 16, BF16, [0, 2], [3], columns=40) == 1
 
 
 @gpu
@@ -279,7 +310,7 @@ def test_peaked_weights_on_either_side(dtype):
 
 @gpu
 def test_starts_that_are_none():
-    b = Batch(15, [40, 50], [1, 1], 4, 2, 64, 16, F32, [0, 2], [2])
+    b = Batch(15, [40, 50], [1, 1], 4, 2, 64, 16, F32, [0, 2], [2], columns=wide(2, 2, 64, 16, 0.5))
     with b.plan() as plan:
         for start in ([32, 50], [-1, 32], [1 << 30, 32]):
             plan.attention_shared(*b.args, b.pages, i32([0, 2]), i32([32]), i32(start), max_new=1, max_group=2, k_scale=KS, v_scale=VS)
@@ -300,7 +331,7 @@ def test_summaries(page, dim):
     b = Batch(dim + page, lens, new, 3, 3, dim, page, BF16)
     touched = [(i, c) for i in range(len(lens)) for c in range((lens[i] - new[i]) // page, -(-lens[i] // page)) if new[i]]
     pages = [int(b.table[i, c]) for i, c in touched]
-    keys = ref.decode_all(b.cache, dim)[0]
+    keys = plain.decode_all(b.cache, dim)[0]
     want = np.full((len(b.cache), 3, 2 * ref.width(dim) + 16), 9, np.uint8)
     high, low = np.zeros((len(pages), 3, dim), np.float32), np.zeros((len(pages), 3, dim), np.float32)
     for x, ((i, c), pg) in enumerate(zip(touched, pages)):
@@ -328,7 +359,7 @@ def test_summaries_of_many_requests_and_pages_that_are_none():
     lens, new = [1 + i % 50 for i in range(200)], [i % 3 for i in range(200)]
     new = [min(a, x) for a, x in zip(new, lens)]
     b = Batch(3, lens, new, 1, 1, 64, 16, F32)
-    keys = ref.decode_all(b.cache, 64)[0]
+    keys = plain.decode_all(b.cache, 64)[0]
     with b.plan() as plan:
         got = plan.new_summaries(len(b.cache))
         plan.summarise(*b.args[1:], b.pages, got, int(b.cu[-1]))
@@ -555,7 +586,7 @@ def steps(plan, kv, heads, dim, page, rng):
     n, prompt = 3, 5 * page
     cache, summaries = plan.new_cache(40), plan.new_summaries(40)
     free = torch.randperm(40, dtype=torch.int32).cuda()
-    table = torch.full((n, 12), -1, dtype=torch.int32, device="cuda")
+    table = torch.full((n, wide(n, kv, dim, page, 1 / 3)), -1, dtype=torch.int32, device="cuda")
     lens = torch.zeros(n, dtype=torch.int32, device="cuda")
     for new in ([prompt, 0, 0], [1, 1, 1], [1, 1, 1], [page, 3, 1], [1, 1, 1]):
         kv_len, cu, pos, slot, taken = plan.tables(lens, i32(new), free, table, sum(new))
@@ -590,7 +621,7 @@ def test_steps_of_a_served_layer(page, dtype):
             assert plan.device_status() == (0, 0)
             c, ln, tb = cu.cpu().numpy(), lens.cpu().numpy(), table.cpu().numpy()
             scale = 1.0 / math.sqrt(64)
-            formula = ref.attention(host(q), c, ln, tb, cache.cpu().numpy(), page, 0, 0, scale, float(np.float32(KS)), float(np.float32(VS)))
+            formula = plain.attention(host(q), c, ln, tb, cache.cpu().numpy(), page, scale, float(np.float32(KS)), float(np.float32(VS)))
             picked = plain.select(host(q), c, ln, tb, summaries.cpu().numpy(), 2, page, 4, 1, 1)
             assert np.array_equal(few.cpu().numpy(), picked)
             over = plain.attention_selected(host(q), c, ln, tb, cache.cpu().numpy(), picked, page, scale, float(np.float32(KS)), float(np.float32(VS)))
@@ -612,7 +643,7 @@ def test_no_page_scores_above_its_bound():
         plan.summarise(i32([0, 480]), b.args[2], b.args[3], b.pages, summaries, 480)
         high, low = (x.cpu().numpy() for x in plan.read_summaries(summaries, i32(b.table[0, :30]), k_scale=1.0))
         assert plan.device_status() == (0, 0)
-    keys = ref.decode_all(b.cache, 64)[0]
+    keys = plain.decode_all(b.cache, 64)[0]
     q = rng.standard_normal((2, 2, 64))
     for h in range(2):
         for c in range(30):
@@ -625,7 +656,7 @@ def test_no_page_scores_above_its_bound():
 @gpu
 def test_calls_in_a_graph_and_on_another_stream():
     """Captured once, replayed on other lengths and tables; two graphs of one plan in turn."""
-    b, other = (Batch(s, lens, [1, 1, 1], 4, 2, 64, 16, BF16, [0, 3], [4], columns=12) for s, lens in ((1, [100, 90, 80]), (2, [70, 130, 66])))
+    b, other = (Batch(s, lens, [1, 1, 1], 4, 2, 64, 16, BF16, [0, 3], [4], columns=wide(3, 2, 64, 16, 1 / 3)) for s, lens in ((1, [100, 90, 80]), (2, [70, 130, 66])))
     groups = i32([0, 3])
     with b.plan() as plan:
         def calls(q, cu, lens, table, cache, summaries):
@@ -701,7 +732,7 @@ def test_offsets_past_32_bits():
     dim, page, kv = 256, 128, 8
     per_page = kv * (page // 16) * ref.block_bytes(dim)
     n_pages = (1 << 32) // per_page + 20
-    b = Batch(9, [300, 270], [1, 1], 8, kv, dim, page, BF16, [0, 2], [2])
+    b = Batch(9, [300, 270], [1, 1], 8, kv, dim, page, BF16, [0, 2], [2], columns=wide(2, kv, dim, page, 0.5))
     far = torch.zeros((n_pages, *b.cache.shape[1:]), dtype=torch.uint8, device="cuda")
     shift = n_pages - len(b.cache)
     far[shift:].copy_(b.pages)
@@ -729,33 +760,34 @@ def _refused(call, status):
 
 @gpu
 def test_refusals():
-    b = Batch(1, [40, 50], [1, 1], 4, 2, 64, 16, F32, [0, 2], [2])
+    b = Batch(1, [40, 50], [1, 1], 4, 2, 64, 16, F32, [0, 2], [2], columns=wide(2, 2, 64, 16, 0.5))
     q, cu, lens, table = b.args
     with b.plan() as plan, plan_for(8, 2, 64, 16, F32, requests=2, tokens=2) as wider:
         summaries = plan.new_summaries(len(b.cache))
         g = i32([0, 2])
         shared, start = plan.shared_prefix(g, cu, lens, table)
         ok = (q, cu, lens, table, b.pages, g, shared, start)
-        picked = plan.select(q, cu, lens, table, summaries, n_select=2)
+        few = table[:, :4].contiguous()
+        picked = plan.select(q, cu, lens, few, summaries, n_select=2)
         for bad in (dict(k_scale=0.0), dict(v_scale=-1.0), dict(v_scale=math.inf), dict(softmax_scale=math.nan), dict(max_new=-1)):
             _refused(lambda: plan.attention_shared(*ok, **bad), -1)
             if "max_new" not in bad:
                 _refused(lambda: plan.attention_selected(*ok[:5], picked, **bad), -1)
         _refused(lambda: plan.attention_shared(*ok, max_group=-1), -1)
         for n_select, first, last in ((1, 1, 1), (4, -1, 1), (4, 1, 0), (4, 3, 2), (4, (1 << 31) - 1, 1)):
-            _refused(lambda: plan.select(q, cu, lens, table, summaries, n_select=n_select, first=first, last=last), -1)
+            _refused(lambda: plan.select(q, cu, lens, few, summaries, n_select=n_select, first=first, last=last), -1)
         _refused(lambda: plan.read_summaries(summaries, i32([0]), k_scale=0.0), -1)
         _refused(lambda: plan.summarise(cu, lens, table, b.pages, summaries, -1), -1)
         _refused(lambda: plan.summarise(cu, lens, table, b.pages, summaries, plan.cfg.max_tokens + 1), -1)
         _refused(lambda: plan.shared_prefix(i32([0] * 9), cu, lens, table), -1)
-        wide = i32(np.zeros((2, 49153)))
-        _refused(lambda: plan.select(q, cu, lens, wide, summaries, n_select=2), -2)
+        many = i32(np.zeros((2, 49153)))
+        _refused(lambda: plan.select(q, cu, lens, many, summaries, n_select=2), -2)
         for call in (lambda: plan.attention_shared(q.half(), *ok[1:]), lambda: plan.attention_shared(*ok[:6], i32([0, 0]), start), lambda: plan.attention_shared(*ok[:7], i32([0])),
                      lambda: wider.attention_shared(*ok), lambda: plan.attention_shared(*ok[:3], i32(np.zeros((3, 4))), *ok[4:]), lambda: plan.attention_shared(*ok[:5], i32([]), shared, start),
                      lambda: plan.shared_prefix(i32([]), cu, lens, table), lambda: plan.shared_prefix(g.long(), cu, lens, table), lambda: plan.shared_prefix(g.cpu(), cu, lens, table),
                      lambda: plan.summarise(cu, lens, table, b.pages, plan.new_summaries(1), 2), lambda: plan.summarise(cu, lens, table, b.pages, summaries.int(), 2),
-                     lambda: plan.read_summaries(summaries[:, :1], i32([0])), lambda: plan.select(q, cu, lens, table, summaries, n_select=0),
-                     lambda: plan.select(q, cu, lens, table, summaries, n_select=2, out=picked[:1]), lambda: plan.attention_selected(*ok[:5], picked[:1]),
+                     lambda: plan.read_summaries(summaries[:, :1], i32([0])), lambda: plan.select(q, cu, lens, few, summaries, n_select=0),
+                     lambda: plan.select(q, cu, lens, few, summaries, n_select=2, out=picked[:1]), lambda: plan.attention_selected(*ok[:5], picked[:1]),
                      lambda: plan.attention_selected(*ok[:5], picked.long()), lambda: plan.attention_selected(*ok[:5], picked[:, :1]),
                      lambda: plan.attention_selected(*ok[:5], picked[:, :, :0])):
             with pytest.raises((AssertionError, B.MoEError)):
@@ -764,9 +796,13 @@ def test_refusals():
         lib, h = plan._lib, plan.handle
         rows = K.moe_kv_rows_t(q.data_ptr(), q.stride(0), q.stride(1))
         out, scratch = torch.empty_like(q), torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
-        need = lib.moe_kv_shared_scratch_bytes(h, 2, 1)
-        assert need == 2 * 4 * (2 * 64 * 4 + 32) and lib.moe_kv_shared_scratch_bytes(h, 2, 0) == need
-        assert lib.moe_kv_shared_scratch_bytes(wider.handle, 100, 9) == 0 and lib.moe_kv_shared_scratch_bytes(h, 0, 1) == 0 and lib.moe_kv_shared_scratch_bytes(h, 1, -1) == 0
+        width = table.shape[1]
+        need = lib.moe_kv_shared_scratch_bytes(h, 2, 2, 1, 2, width)
+        assert need == 2 * 4 * (2 * 64 * 4 + 32) and lib.moe_kv_shared_scratch_bytes(h, 2, 2, 1, 0, width) == need
+        for none in ((2, 2, 1, 2, 100), (2, 2, 1, 1, width), (2, 2, 0, 0, width), (100, 2, 17, 90, width), (0, 2, 1, 2, width), (2, 0, 1, 2, width), (2, 2, -1, 2, width),
+                     (2, 2, 1, -1, width), (2, 2, 1, 2, 0)):
+            assert lib.moe_kv_shared_scratch_bytes(h, *none) == 0
+        assert lib.moe_kv_shared_scratch_bytes(wider.handle, 100, 2, 9, 18, width) == 0
 
         def shared_call(at=0, size=need, group=g.data_ptr(), tab=table.data_ptr(), where=scratch.data_ptr()):
             return lib.moe_kv_attention_shared(h, ctypes.byref(rows), 2, cu.data_ptr(), lens.data_ptr(), 2, 1, tab, table.shape[1], b.pages.data_ptr(), len(b.cache), group, 1, 2,
@@ -776,7 +812,7 @@ def test_refusals():
         assert shared_call(at=8) == -3 and shared_call(group=g.data_ptr() + 2) == -3 and shared_call(group=None) == -1 and shared_call(tab=None) == -1
         assert lib.moe_kv_summarise(h, cu.data_ptr(), lens.data_ptr(), 2, 2, table.data_ptr(), table.shape[1], b.pages.data_ptr(), len(b.cache), summaries.data_ptr() + 8, None) == -3
         assert lib.moe_kv_read_summaries(h, summaries.data_ptr(), len(b.cache), cu.data_ptr(), 1, 1.0, scratch.data_ptr() + 4, scratch.data_ptr(), None) == -3
-        assert lib.moe_kv_select(h, ctypes.byref(rows), 2, cu.data_ptr(), lens.data_ptr(), 2, 1, table.data_ptr(), table.shape[1], summaries.data_ptr(), len(b.cache), 2, 1, 1,
+        assert lib.moe_kv_select(h, ctypes.byref(rows), 2, cu.data_ptr(), lens.data_ptr(), 2, 1, few.data_ptr(), few.shape[1], summaries.data_ptr(), len(b.cache), 2, 1, 1,
                                  scratch.data_ptr() + 2, None) == -3
         assert lib.moe_kv_attention_selected(h, ctypes.byref(rows), 2, cu.data_ptr(), lens.data_ptr(), 2, table.data_ptr(), table.shape[1], b.pages.data_ptr(), len(b.cache),
                                              picked.data_ptr() + 1, 2, 0.125, 1.0, 1.0, out.data_ptr(), None) == -3
