@@ -164,6 +164,35 @@ constexpr int kMaxCluster = 8;
 
 __device__ __forceinline__ float load_q(const float *p) { return __ldg(p); }
 __device__ __forceinline__ float load_q(const __nv_bfloat16 *p) { return __bfloat162float(__ldg(p)); }
+// N neighbouring numbers, aligned to their size
+template <int N>
+__device__ __forceinline__ void load_q(const float *p, float (&x)[N]) {
+    if constexpr (N == 2) {
+        const float2 v = __ldg(reinterpret_cast<const float2 *>(p));
+        x[0] = v.x; x[1] = v.y;
+    } else {
+#pragma unroll
+        for (int e = 0; e < N; e += 4) {
+            const float4 v = __ldg(reinterpret_cast<const float4 *>(p + e));
+            x[e] = v.x; x[e + 1] = v.y; x[e + 2] = v.z; x[e + 3] = v.w;
+        }
+    }
+}
+template <int N>
+__device__ __forceinline__ void load_q(const __nv_bfloat16 *p, float (&x)[N]) {
+    uint32_t w[N / 2];
+    if constexpr (N == 2) {
+        w[0] = __ldg(reinterpret_cast<const uint32_t *>(p));
+    } else if constexpr (N == 4) {
+        const uint2 v = __ldg(reinterpret_cast<const uint2 *>(p));
+        w[0] = v.x; w[1] = v.y;
+    } else {
+        const uint4 v = __ldg(reinterpret_cast<const uint4 *>(p));
+        w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+    }
+#pragma unroll
+    for (int e = 0; e < N / 2; ++e) { x[2 * e] = __uint_as_float(w[e] << 16); x[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u); }
+}
 // 32 products of 8-bit numbers for each of 16 pages and 8 tokens
 __device__ __forceinline__ void mma_s8(int (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -184,7 +213,7 @@ __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.w
 // time, and put the scores into the first CTA's shared memory, which selects: a warp for each token, or all warps for one.
 // A request's tiles of TOK are at most floor(new/TOK) + 1: request i's begin at item cu[i]/TOK + i.
 template <typename T, int W, int TOK>
-__global__ void __launch_bounds__(kThreads) select_kernel(SelectArgs a, int cluster) {
+__global__ void __launch_bounds__(kThreads, W == 256 ? 2 : 4) select_kernel(SelectArgs a, int cluster) {
     constexpr int kChunks = 2 * W / 64;                // 64 bytes of a summary: 16 for each of four lanes
     constexpr int kQRow = 2 * W + 16;
     extern __shared__ __align__(16) uint32_t scores[];       // [TOK][a.room], in the order of the numbers
@@ -212,20 +241,35 @@ __global__ void __launch_bounds__(kThreads) select_kernel(SelectArgs a, int clus
     if (top > from) {
         // ---- queries: a warp a token, W/32 neighbouring dimensions a lane; sums in the order of the heads
         constexpr int kPer = W / 32;
+        constexpr uintptr_t kWide = (kPer * sizeof(T) < 16 ? kPer * sizeof(T) : 16) - 1;
+        const bool wide = (reinterpret_cast<uintptr_t>(a.q.p) & kWide) == 0 && (((a.q.ts | a.q.hs) * sizeof(T)) & kWide) == 0;
         for (int t = warp; t < TOK; t += kWarps) {
             float u[kPer], w[kPer], m = 0.f;
 #pragma unroll
             for (int e = 0; e < kPer; ++e) u[e] = w[e] = 0.f;
             if (t < many) {
                 const T *src = (const T *)a.q.p + (int64_t)(q.q0 + tok0 + t) * a.q.ts + (int64_t)head * a.G * a.q.hs + lane * kPer;
-#pragma unroll 4
-                for (int g = 0; g < a.G; ++g)
+                auto add = [&](const float (&x)[kPer]) {
 #pragma unroll
-                    for (int e = 0; e < kPer; ++e) {
-                        const float x = lane * kPer + e < a.D ? load_q(src + g * a.q.hs + e) : 0.f;
-                        u[e] += fmaxf(x, 0.f);
-                        w[e] += fminf(x, 0.f);
+                    for (int e = 0; e < kPer; ++e) { u[e] += fmaxf(x[e], 0.f); w[e] += fminf(x[e], 0.f); }
+                };
+                if (lane * kPer >= a.D) {          // D is a multiple of 8, kPer at most 8
+                } else if (wide) {
+#pragma unroll 4
+                    for (int g = 0; g < a.G; ++g) {
+                        float x[kPer];
+                        load_q<kPer>(src + g * a.q.hs, x);
+                        add(x);
                     }
+                } else {
+#pragma unroll 1
+                    for (int g = 0; g < a.G; ++g) {
+                        float x[kPer];
+#pragma unroll
+                        for (int e = 0; e < kPer; ++e) x[e] = load_q(src + g * a.q.hs + e);
+                        add(x);
+                    }
+                }
             }
 #pragma unroll
             for (int e = 0; e < kPer; ++e) m = fmaxf(m, fmaxf(u[e], -w[e]));
@@ -274,9 +318,10 @@ __global__ void __launch_bounds__(kThreads) select_kernel(SelectArgs a, int clus
             uint4 x0[kChunks], x1[kChunks];
             float step0 = 0.f, step1 = 0.f;
 #pragma unroll
-            for (int x = 0; x < kChunks; ++x) {
-                x0[x] = ok0 ? __ldg(reinterpret_cast<const uint4 *>(s0 + c * 16 + 64 * x)) : make_uint4(0u, 0u, 0u, 0u);
-                x1[x] = ok1 ? __ldg(reinterpret_cast<const uint4 *>(s1 + c * 16 + 64 * x)) : make_uint4(0u, 0u, 0u, 0u);
+            for (int x = 0; x < kChunks; ++x) {          // nothing but zeros lies behind head_dim
+                const bool in = (c * 16 + 64 * x) % W < a.D;
+                x0[x] = in && ok0 ? __ldg(reinterpret_cast<const uint4 *>(s0 + c * 16 + 64 * x)) : make_uint4(0u, 0u, 0u, 0u);
+                x1[x] = in && ok1 ? __ldg(reinterpret_cast<const uint4 *>(s1 + c * 16 + 64 * x)) : make_uint4(0u, 0u, 0u, 0u);
             }
             if (ok0) step0 = __ldg(reinterpret_cast<const float *>(s0 + 2 * W));
             if (ok1) step1 = __ldg(reinterpret_cast<const float *>(s1 + 2 * W));
@@ -336,17 +381,19 @@ __global__ void __launch_bounds__(kThreads) select_kernel(SelectArgs a, int clus
         turn ^= 1;
         return s;
     };
-    // A thread keeps its first scores in registers; 0, which no score is, behind the last
+    // This warp's part of the pages.  A lane keeps its first scores in registers; 0, which no score is, behind the last
     constexpr int kKept = kAll ? 4 : 16;
+    const int part = kAll ? ((n + kWarps - 1) / kWarps + 31) & ~31 : n, begin = kAll ? min(warp * part, n) : 0, end = min(begin + part, n);
     uint32_t kept[kKept], least = 0xffffffffu, most = 0u;
 #pragma unroll
     for (int j = 0; j < kKept; ++j) {
-        const int x = first_lane + j * kStride;
-        kept[j] = x < n ? key[x] : 0u;
-        least = min(least, x < n ? kept[j] : 0xffffffffu);
+        const int x = begin + 32 * j + lane;
+        kept[j] = x < end ? key[x] : 0u;
+        least = min(least, x < end ? kept[j] : 0xffffffffu);
         most = max(most, kept[j]);
     }
-    for (int x = first_lane + kKept * kStride; x < n; x += kStride) { least = min(least, key[x]); most = max(most, key[x]); }
+    const int rest = begin + 32 * kKept + lane;
+    for (int x = rest; x < end; x += 32) { least = min(least, key[x]); most = max(most, key[x]); }
     least = __reduce_min_sync(0xffffffffu, least);
     most = __reduce_max_sync(0xffffffffu, most);
     if (kAll) {
@@ -366,15 +413,19 @@ __global__ void __launch_bounds__(kThreads) select_kernel(SelectArgs a, int clus
         int mine = 0;
 #pragma unroll
         for (int j = 0; j < kKept; ++j) mine += kept[j] >= reach;
-        for (int x = first_lane + kKept * kStride; x < n; x += kStride) mine += key[x] >= reach;
+        for (int x = rest; x < end; x += 32) mine += key[x] >= reach;
         const int reached = all_of(mine);
         if (reached >= need) edge = reach;
         if (reached == need) break;
     }
-    // this warp's part of the pages, and how many above and at the edge lie in front of it
-    const int part = kAll ? ((n + kWarps - 1) / kWarps + 31) & ~31 : n, begin = kAll ? min(warp * part, n) : 0, end = min(begin + part, n);
+    // how many above and at the edge the warps in front have
     int above = 0, ties = 0;
-    for (int x = begin + lane; x < end; x += 32) { above += key[x] > edge; ties += key[x] == edge; }
+#pragma unroll
+    for (int j = 0; j < kKept; ++j) {
+        above += kept[j] > edge;
+        ties += kept[j] == edge && begin + 32 * j + lane < end;
+    }
+    for (int x = rest; x < end; x += 32) { above += key[x] > edge; ties += key[x] == edge; }
     above = __reduce_add_sync(0xffffffffu, above);
     ties = __reduce_add_sync(0xffffffffu, ties);
     int all_above = above, above_before = 0, ties_before = 0;
@@ -390,18 +441,20 @@ __global__ void __launch_bounds__(kThreads) select_kernel(SelectArgs a, int clus
     }
     const int wanted = need - all_above;               // of those at the edge, the first ones
     int at = a.first + above_before + min(ties_before, wanted);
-#pragma unroll 1
-    for (int x0 = begin; x0 < end; x0 += 32) {
+    auto write = [&](int x0, uint32_t k) {             // 32 pages from x0 on, a lane's score
         const int x = x0 + lane;
-        const uint32_t k = x < end ? key[x] : 0u;
-        const bool tie = x < end && k == edge;
-        const uint32_t tied = __ballot_sync(0xffffffffu, tie), before = (1u << lane) - 1u;
-        const bool take = x < end && (k > edge || (tie && ties_before + __popc(tied & before) < wanted));
+        const uint32_t tied = __ballot_sync(0xffffffffu, x < end && k == edge), before = (1u << lane) - 1u;
+        const bool take = x < end && (k > edge || (k == edge && ties_before + __popc(tied & before) < wanted));
         const uint32_t taken = __ballot_sync(0xffffffffu, take);
         if (take) out[at + __popc(taken & before)] = a.first + x;
         at += __popc(taken);
         ties_before += __popc(tied);
-    }
+    };
+#pragma unroll
+    for (int j = 0; j < kKept; ++j)
+        if (begin + 32 * j < end) write(begin + 32 * j, kept[j]);
+#pragma unroll 1
+    for (int x0 = begin + 32 * kKept; x0 < end; x0 += 32) write(x0, x0 + lane < end ? key[x0 + lane] : 0u);
 }
 
 template <typename T, int W, int TOK>
