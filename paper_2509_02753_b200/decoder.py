@@ -6,10 +6,14 @@
 for batches of requests of different lengths, prompts and single tokens in one step.  The projections are plain library
 products; everything else between them is this package's kernels: ``tables`` once a step, then per layer ``append``
 (rotary positions, 4-bit storage), ``attention`` and the MoE layer with that layer's own number of active experts.
+Requests that begin with another one's prompt share its pages (``Decoder.fork``): their attention reads these once for all
+(``shared_prefix``, ``attention_shared``).  With ``Attention.select`` a token attends to that many pages, chosen by bounds of their
+keys (``summarise``, ``select``, ``attention_selected``).
 
-    python -m paper_2509_02753_b200.decoder [workload] [requests] [prompt tokens] [steps]
+    python -m paper_2509_02753_b200.decoder [workload] [requests] [prompt tokens] [steps] [shared | pages to select]
 
-runs prompts and decoding steps of a model with that workload's MoE shapes and seeded weights and prints the time of each.
+runs prompts and decoding steps of a model with that workload's MoE shapes and seeded weights and prints the time of each; with
+"shared" one prompt that all requests go on from.
 """
 from __future__ import annotations
 
@@ -27,7 +31,8 @@ from . import synth
 
 @dataclass
 class Attention:
-    """Shape of a layer's attention.  window > 0: a token sees the last `window` tokens and the first `sinks`."""
+    """Shape of a layer's attention.  window > 0: a token sees the last `window` tokens and the first `sinks`.  select > 0: it
+    sees that many pages for each key/value head, the first `first` and the last `last` and those whose keys promise most."""
     n_heads: int
     n_kv_heads: int
     head_dim: int
@@ -37,13 +42,16 @@ class Attention:
     sinks: int = 0
     k_scale: float = 1.0
     v_scale: float = 1.0
+    select: int = 0
+    first: int = 1
+    last: int = 2
 
 
 class Request:
-    """Tokens in the cache, and the row of the block table."""
+    """Tokens in the cache, the row of the block table, and the row whose prompt it began with (its own unless forked)."""
 
     def __init__(self, row: int):
-        self.row, self.length = row, 0
+        self.row, self.length, self.origin = row, 0, row
 
 
 def rms_norm(x: torch.Tensor, eps: float = 1e-6) -> torch.Tensor:
@@ -57,12 +65,15 @@ class Decoder:
 
     def __init__(self, layers: Sequence[dict], k_vec: Sequence[int], plan: B.MoEPlan, attn: Attention, *, renorm: bool, n_pages: int, page_size: int,
                  max_requests: int, max_tokens: int, max_context: int, base: float = 10000.0, scaling: Optional[dict] = None):
+        if attn.select and attn.window:
+            raise ValueError("a window and selected pages")
         self.layers, self.k_vec, self.moe, self.attn, self.renorm = layers, list(k_vec), plan, attn, renorm
         dtype = plan.dtype
         self.kv = K.KVPlan(n_heads=attn.n_heads, n_kv_heads=attn.n_kv_heads, head_dim=attn.head_dim, page_size=page_size, dtype=dtype,
                            max_requests=max_requests, max_tokens=max_tokens)
         self.weights = [B.make_weights(w) for w in layers]
         self.caches = [self.kv.new_cache(n_pages) for _ in layers]
+        self.summaries = [self.kv.new_summaries(n_pages) if attn.select else None for _ in layers]
         self.turns = K.rope_table(attn.rope_dim, max_context, base=base, **(scaling or {}))
         self.page = page_size
         self.width = -(-max_context // page_size)
@@ -71,6 +82,7 @@ class Decoder:
         self.lengths = torch.zeros((max_requests,), dtype=torch.int32, device="cuda")
         self.requests = [Request(i) for i in range(max_requests)]
         self.free = list(range(n_pages))
+        self.more_users = {}          # of pages that several requests have: all but one of them
 
     def close(self):
         self.kv.close()
@@ -81,10 +93,45 @@ class Decoder:
     def finish(self, row: int) -> None:
         """Gives a request's pages back; the row serves another request from its first token on."""
         held = -(-self.requests[row].length // self.page)
-        self.free += self.table[row, :held].tolist()
+        for page in self.table[row, :held].tolist():
+            if page in self.more_users:
+                self.more_users[page] -= 1
+                if self.more_users[page] == 0:
+                    del self.more_users[page]
+            else:
+                self.free.append(page)
         self.table[row].fill_(-1)
         self.lengths[row] = 0
-        self.requests[row].length = 0
+        self.requests[row].length, self.requests[row].origin = 0, row
+
+    def fork(self, row: int, others: Sequence[int], tokens: Optional[int] = None) -> int:
+        """The requests `others`, which have no tokens yet, begin with the first `tokens` tokens of request `row` (all by default),
+        cut to whole pages, which they share.  Returns how many these are: the others' next tokens follow them.  Requests of
+        neighbouring rows read what they share once."""
+        source = self.requests[row]
+        tokens = source.length if tokens is None else tokens
+        if not 0 <= tokens <= source.length:
+            raise ValueError("a request cannot begin with tokens that are not there")
+        if row in others or len(set(others)) != len(others) or any(self.requests[i].length for i in others):
+            raise ValueError("only requests without tokens begin with another's")
+        pages = tokens // self.page
+        if pages == 0 or not others:
+            return pages * self.page
+        for page in self.table[row, :pages].tolist():
+            self.more_users[page] = self.more_users.get(page, 0) + len(others)
+        for i in others:
+            self.table[i, :pages] = self.table[row, :pages]
+            self.lengths[i] = pages * self.page
+            self.requests[i].length, self.requests[i].origin = pages * self.page, source.origin
+        return pages * self.page
+
+    def _groups(self, new: Sequence[int]) -> Optional[tuple]:
+        """(first request of each group of neighbours of one origin and the end, the largest group's new tokens); none if nothing is shared."""
+        origins = [r.origin for r in self.requests]
+        cu = [i for i in range(len(origins)) if i == 0 or origins[i] != origins[i - 1]] + [len(origins)]
+        if not self.more_users or len(cu) > len(origins):
+            return None
+        return cu, max(sum(new[a: b]) for a, b in zip(cu, cu[1:]))
 
     def step(self, x: torch.Tensor, new: Sequence[int]) -> torch.Tensor:
         """One step: x [sum(new), d] are the hidden states of the new tokens, request after request (new[i] of request i, 0
@@ -103,11 +150,23 @@ class Decoder:
         a, dev = self.attn, x.device
         fresh = torch.tensor(self.free[:need], dtype=torch.int32, device=dev)
         kv_len, cu, position, slot, _ = self.kv.tables(self.lengths, torch.tensor(list(new), dtype=torch.int32, device=dev), fresh, self.table, T)
-        for layer, weights, cache, k in zip(self.layers, self.weights, self.caches, self.k_vec):
+        scales = {"k_scale": a.k_scale, "v_scale": a.v_scale}
+        groups = None if a.window or a.select else self._groups(new)
+        if groups:
+            cu_group = torch.tensor(groups[0], dtype=torch.int32, device=dev)
+            shared = (cu_group, *self.kv.shared_prefix(cu_group, cu, kv_len, self.table))
+        for layer, weights, cache, summaries, k in zip(self.layers, self.weights, self.caches, self.summaries, self.k_vec):
             qkv = torch.matmul(rms_norm(x), layer["qkv"].t()).view(T, a.n_heads + 2 * a.n_kv_heads, a.head_dim)
             q, key, value = qkv.split((a.n_heads, a.n_kv_heads, a.n_kv_heads), 1)
             q = self.kv.append(q, key, value, slot, cache, positions=position, turns=self.turns, layout=a.layout, k_scale=a.k_scale, v_scale=a.v_scale)
-            o = self.kv.attention(q, cu, kv_len, self.table, cache, max_new=max(new), window=a.window, sinks=a.sinks, k_scale=a.k_scale, v_scale=a.v_scale)
+            if a.select:
+                self.kv.summarise(cu, kv_len, self.table, cache, summaries, T)
+                selected = self.kv.select(q, cu, kv_len, self.table, summaries, n_select=a.select, first=a.first, last=a.last, max_new=max(new))
+                o = self.kv.attention_selected(q, cu, kv_len, self.table, cache, selected, **scales)
+            elif groups:
+                o = self.kv.attention_shared(q, cu, kv_len, self.table, cache, *shared, max_new=max(new), max_group=groups[1], **scales)
+            else:
+                o = self.kv.attention(q, cu, kv_len, self.table, cache, max_new=max(new), window=a.window, sinks=a.sinks, **scales)
             x = x + torch.matmul(o.view(T, -1), layer["o"].t())
             x = x + self.moe.layer_forward(rms_norm(x), weights, k, self.renorm)
         del self.free[:need]
@@ -153,8 +212,11 @@ def attention_of(wl: synth.Workload) -> Attention:
 def main(argv: Sequence[str]) -> None:
     workload = argv[0] if argv else "olmoe"
     requests, prompt, steps = (int(argv[i]) if len(argv) > i else v for i, v in ((1, 16), (2, 1024), (3, 64)))
+    how = argv[4] if len(argv) > 4 else ""
     wl = synth.WORKLOADS[workload]
     attn = attention_of(wl)
+    if how and how != "shared":
+        attn.select = int(how)
     dec = build(workload, attn, layers=min(wl.L, 8), dtype=torch.bfloat16, requests=requests, max_tokens=requests * prompt, max_context=prompt + steps)
     x = synth.make_tokens(wl, requests * prompt, torch.bfloat16, "cuda")
 
@@ -169,13 +231,20 @@ def main(argv: Sequence[str]) -> None:
     dec.check()
     for row in range(requests):
         dec.finish(row)
-    first = timed(lambda: dec.step(x, [prompt] * requests))
+    if how == "shared":
+        first = timed(lambda: dec.step(x[:prompt].contiguous(), [prompt] + [0] * (requests - 1)))
+        behind = prompt - dec.fork(0, range(1, requests))
+        if behind and requests > 1:
+            dec.step(x[:prompt][prompt - behind:].repeat(requests - 1, 1), [0] + [behind] * (requests - 1))
+    else:
+        first = timed(lambda: dec.step(x, [prompt] * requests))
     token = x[:requests].contiguous()
     each = timed(lambda: [dec.step(token, [1] * requests) for _ in range(steps)]) / steps
     dec.check()
     cache = sum(c.numel() for c in dec.caches) / 2 ** 20
     print(f"{workload}: {len(dec.layers)} layers, k = {dec.k_vec}, {requests} requests, cache {cache:.0f} MiB in 4 bits")
-    print(f"prompts of {prompt} tokens: {first * 1e3:.2f} ms, {requests * prompt / first:.0f} tokens/s")
+    prompts = 1 if how == "shared" else requests
+    print(f"{'one prompt' if how == 'shared' else 'prompts'} of {prompt} tokens: {first * 1e3:.2f} ms, {prompts * prompt / first:.0f} tokens/s")
     print(f"a token of every request: {each * 1e3:.3f} ms, {requests / each:.0f} tokens/s")
     dec.close()
 

@@ -1,0 +1,129 @@
+"""The decoder stack with requests that share a prompt, and with selected pages (paper_2509_02753_b200/decoder.py).
+
+Tolerance as in test_decoder.py: sums of a few thousand fp32 additions in other orders, below 1e-3 of the largest output."""
+import pytest
+import torch
+
+from paper_2509_02753_b200 import binding as B
+from paper_2509_02753_b200 import decoder as D
+from paper_2509_02753_b200 import synth
+
+gpu = pytest.mark.gpu
+WL = synth.WORKLOADS["tiny"]
+
+
+def make(requests, *, n_pages=40, max_context=128, page_size=16, dtype=torch.float32, **more):
+    attn = D.Attention(n_heads=4, n_kv_heads=2, head_dim=64, rope_dim=32, k_scale=0.01, v_scale=0.01, **more)
+    plan = B.MoEPlan(WL.d, WL.E, WL.I, 256, 2, dtype, I_shared=WL.I_shared, shared_gate=WL.shared_gate)
+    layers = [{**synth.make_layer(WL, i, dtype, "cuda", 0), **D.make_attention_weights(attn, WL.d, i, dtype, 0)} for i in range(2)]
+    return D.Decoder(layers, [2, 1], plan, attn, renorm=WL.renorm, n_pages=n_pages, page_size=page_size, max_requests=requests, max_tokens=256, max_context=max_context)
+
+
+def tokens(n, seed=0):
+    return synth.make_tokens(WL, n + seed, torch.float32, "cuda")[seed:].contiguous()
+
+
+def near(a, b):
+    assert (a - b).abs().max() <= 1e-3 * b.abs().max()
+
+
+def test_a_window_and_selected_pages_are_refused():
+    with pytest.raises(ValueError):
+        D.Decoder([], [], None, D.Attention(1, 1, 64, 64, window=5, select=3), renorm=True, n_pages=1, page_size=16, max_requests=1, max_tokens=1, max_context=16)
+
+
+@gpu
+@pytest.mark.parametrize("max_context", [128, 1 << 20])
+def test_requests_that_go_on_from_one_prompt(max_context):
+    """Three requests: each computes the prompt itself, or two begin with the first one's pages (also read once, where the tables
+    are so wide that this counts as worth it)."""
+    prompt, more = tokens(53), [tokens(3, 100 + i) for i in range(4)]
+    alone, shared = make(3), make(3, max_context=max_context)
+    alone.step(prompt.repeat(3, 1), [53] * 3)
+    shared.step(prompt, [53, 0, 0])
+    assert shared.fork(0, [1, 2]) == 48
+    shared.step(prompt[48:].repeat(2, 1), [0, 5, 5])
+    before = shared.kv.launch_count
+    for x in more:
+        near(shared.step(x, [1, 1, 1]), alone.step(x, [1, 1, 1]))
+    if max_context > 128:
+        assert shared.kv.launch_count - before == len(more) * (2 + 2 * 4)          # tables, prefix; a layer: append, three of attention
+    shared.check()
+    alone.check()
+    assert [r.length for r in shared.requests] == [57] * 3
+    assert len(shared.free) == 40 - 3 - 3 and len(alone.free) == 40 - 12
+    assert shared.table[0, :3].tolist() == shared.table[2, :3].tolist() != shared.table[0, 1:4].tolist()
+    for dec in (alone, shared):
+        dec.close()
+
+
+@gpu
+def test_shared_pages_are_free_after_their_last_user():
+    dec = make(3)
+    dec.step(tokens(40), [40, 0, 0])
+    assert dec.fork(0, [1], 20) == 16 and dec.fork(0, [2]) == 32
+    assert [r.length for r in dec.requests] == [40, 16, 32]
+    dec.step(tokens(3), [1, 1, 1])
+    pages = dec.table[0, :2].tolist()
+    assert len(dec.free) == 40 - 5
+    dec.finish(0)
+    assert len(dec.free) == 40 - 4 and not set(pages) & set(dec.free)          # the third page was its own
+    dec.finish(2)
+    assert pages[1] in dec.free and pages[0] not in dec.free
+    dec.finish(1)
+    assert sorted(dec.free) == list(range(40)) and not dec.more_users
+    assert dec._groups([1, 1, 1]) is None
+    dec.check()
+    dec.close()
+
+
+@gpu
+def test_forks_that_are_refused():
+    dec = make(3)
+    dec.step(tokens(41), [40, 1, 0])
+    for args in ((0, [1]), (0, [0]), (0, [2, 2]), (0, [2], 41), (0, [2], -1)):
+        with pytest.raises(ValueError):
+            dec.fork(*args)
+    assert dec.fork(0, [2], 15) == 0 and dec.fork(0, []) == 32 and not dec.more_users
+    dec.close()
+
+
+@gpu
+def test_groups_are_neighbours_of_one_origin():
+    dec = make(5)
+    dec.step(tokens(32), [32, 0, 0, 0, 0])
+    dec.fork(0, [1, 3])
+    dec.fork(1, [4])
+    assert dec._groups([1, 1, 1, 2, 3]) == ([0, 2, 3, 5], 5)
+    x = tokens(5)
+    y = dec.step(x, [1] * 5)
+    dec.check()
+    for i in (1, 3, 4):           # the same prompt, the same place, but another token: as if alone
+        other = make(1)
+        other.step(tokens(32), [32])
+        near(y[i: i + 1], other.step(x[i: i + 1], [1]))
+        other.close()
+    dec.close()
+
+
+@gpu
+def test_all_pages_selected_is_attention_and_few_are_not():
+    x, more = tokens(90), [tokens(2, 50 + i) for i in range(3)]
+    outs = []
+    for select in (0, 8, 3):
+        dec = make(2, select=select)
+        got = [dec.step(torch.cat([x[:80], x[80:]]), [80, 10])] + [dec.step(y, [1, 1]) for y in more]
+        dec.check()
+        outs.append(torch.cat(got))
+        dec.close()
+    near(outs[1], outs[0])
+    assert (outs[2][:16] - outs[0][:16]).abs().max() <= 1e-3 * outs[0].abs().max()          # tokens of up to three pages see all of them
+    assert not torch.allclose(outs[2][60:80], outs[0][60:80], rtol=1e-3)
+
+
+@gpu
+@pytest.mark.parametrize("how", ["shared", "4", ""])
+def test_the_command_runs(how, capsys):
+    D.main(["tiny", "3", "70", "2"] + ([how] if how else []))
+    out = capsys.readouterr().out
+    assert "a token of every request" in out and ("one prompt" in out) == (how == "shared")
