@@ -216,7 +216,7 @@ uint64_t moe_kv_shared_scratch_bytes(const moe_kv_plan_t *plan, int32_t n_tokens
  * kernels; 0 = unknown, which counts as n_tokens.  The call is moe_kv_attention's where sharing gains nothing: where max_new
  * times the query heads of a key/value head passes 32 (64 for head_dim above 128), for a request's own
  * rows share its keys then, and where the cache that n_requests tables of this width can hold is small (less
- * than 75 MB saved, 150 MB with at most 32 (64) rows a group).  scratch: 16-byte aligned device memory of
+ * than 80 MB saved, 150 MB with at most 32 (64) rows a group).  scratch: 16-byte aligned device memory of
  * scratch_bytes >= moe_kv_shared_scratch_bytes, in use until the call's work is done.
  * A start outside 0..kv_len - new tokens sets BAD_INDEX; start and shared_len that do not belong together
  * give rows that no formula stands for.

@@ -148,7 +148,7 @@ struct AttendArgs {
     // its stretch, o_pieces being (first CTA, CTAs, row): that row of prompt_part and prompt_ml in slot 1 of the first CTA and
     // 0 of the others.  A slot has piece_rows rows, results of result_rows each where there are piece_results of them; piece_ctas CTAs
     // have slots
-    const int32_t *groups; int n_members;
+    const int32_t *groups, *member_len; int n_members;       // member_len: the requests' keys
     const int32_t *start;
     float *o_part, *own_part; float2 *o_ml, *own_ml; int4 *o_pieces;
     int piece_rows, result_rows, piece_results, piece_ctas;

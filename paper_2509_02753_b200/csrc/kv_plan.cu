@@ -31,7 +31,7 @@ constexpr int64_t kMaxRows = 1 << 30;         // max_tokens * n_heads
 constexpr int64_t kMaxContext = 1 << 30;      // tokens that a row of a block table may stand for
 constexpr int kPartRows = 32;         // rows of a piece, at most
 constexpr int kPassRows = 32;         // query rows of a pass over the keys in kv_attend.cu
-constexpr double kWorthMany = 75e6, kWorthFew = 150e6;          // bytes of the cache that reading prefixes once has to save
+constexpr double kWorthMany = 80e6, kWorthFew = 150e6;          // bytes of the cache that reading prefixes once has to save
 
 size_t elem_size(int dtype) { return dtype == MOE_BF16 ? 2 : 4; }
 bool aligned(const void *p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
@@ -104,13 +104,15 @@ int row_limit(const moe_kv_config_t &c) { return padded_width(c.head_dim) == 256
 
 // Whether a call's prefixes are read once for a group.  Not where a request has more rows than one pass over the keys serves
 // (its own rows share the reading already), nor where too little could be saved: what the tables can hold, less one member's
-// share of it, has to be worth two more launches.  In us, bf16 (prefix + up to 500 keys of its own, without / with sharing):
-//   64 requests, 32/8 heads of 128: 512 keys (75 MB) 25.2 / 27.8, 1024 (112 MB) 33.4 / 33.0, 4096 80 / 40, 32768 514 / 72
-//   16 of these: 2048 keys (40 MB) 19.0 / 20.1, 8192 (153 MB) 45.8 / 29.9;   32 of 16/2 heads of 256: 4096 keys (77 MB) 29.0 / 28.9
-//   32 of 16/4 heads of 128 in fp32: 1024 keys (21 MB) 15.5 / 22.6, 4096 (77 MB) 31.4 / 28.7
+// share of it, has to be worth two more launches.  In us, bf16 unless said, with up to 500 (64 requests) or 100 keys behind the
+// prefix, request by request / shared:
+//   64 requests, 32/8 heads of 128: 512 keys (75 MB) 25 / 26, 1024 (112 MB) 33 / 28, 4096 80 / 33, 8192 142 / 40, 32768 513 / 75
+//   16 of these: 2048 keys (40 MB) 19.0 / 20.1, 8192 (153 MB) 46 / 27
+//   32 of 16/2 heads of 256: 4096 keys (78 MB) 29 / 32, 16384 (305 MB) 78 / 43
+//   32 of 16/4 heads of 128 in fp32: 1024 keys (21 MB) 15.5 / 22.6, 4096 (78 MB) 31.3 / 29.8, 16384 94 / 42
 // and where a group's rows are few (kv_attend_body.cuh reads the prefix in passes of 32 rows, which hide less of its latency):
 //   8 of 32/8 heads of 128: 8192 keys (76 MB) 26.7 / 30.4, 32768 (303 MB) 75 / 44;   16 groups of 4: 1024 keys (83 MB) 30 / 39,
-//   4096 (309 MB) 78 / 70
+//   4096 (309 MB) 78 / 70, 16384 264 / 194
 bool reads_prefixes_once(const moe_kv_plan *p, int32_t T, int32_t n, int32_t max_new, int32_t max_group, int32_t width) {
     const moe_kv_config_t &c = p->cfg;
     const long long request = max_new > 0 && max_new < T ? max_new : T, group = max_group > 0 && max_group < T ? max_group : T, g = c.n_heads / c.n_kv_heads;
@@ -367,7 +369,7 @@ int moe_kv_attention_shared(moe_kv_plan_t *p, const moe_kv_rows_t *q, int32_t T,
     rest.o_ml = (float2 *)(rest.o_pieces + rows);
     rest.own_ml = rest.o_ml + rows;
     AttendArgs prefix = rest;
-    prefix.kv_len = shared_len; prefix.n = n_groups; prefix.groups = cu_group; prefix.n_members = n;
+    prefix.kv_len = shared_len; prefix.n = n_groups; prefix.groups = cu_group; prefix.n_members = n; prefix.member_len = kv_len;
     prefix.max_new = max_group > 0 && max_group < T ? max_group : T;
     cudaStream_t s = (cudaStream_t)stream;
     // groups of few rows in kv_attend_body.cuh, of many in kv_prompt_body.cuh, as the requests of moe_kv_attention; all in one

@@ -25,6 +25,8 @@
 //
 // Work split: as in kv_attend.cu, the key tiles of all stretches stand in one line cut evenly over the CTAs, which also
 // serves few rows over a long context; a stretch in several pieces is joined by its last CTA in the order of the keys.
+// PREFIX: every stretch in pieces of as many tiles, which stand in the line; there are few stretches and each piece pays its beginning
+// (45 requests in 4 groups, fp32: 41 us where cuts fell in the middle of two stretches, 46 where beginnings filled shares).
 //
 // PREFIX: "requests" are groups of requests and "keys" their shared prefix, which all rows of a group see whole (kv_prompt.cu
 // builds the one, kv_prompt_prefix.cu the other).  What comes out is sums, references and denominators as they are, for
@@ -52,7 +54,10 @@ constexpr float kTop = 14.f;                     // the largest weight is 2^kTop
 // with many short stretches would be last by far.  Alternating groups pass a tile in about half the time (with 5 for 3
 // there: 333 to 700 tokens of 15/5 heads 52 -> 49 us, 64 tokens on 16000 keys of 16/4 heads 83 -> 77)
 constexpr int kEntryTiles = 3, kEntryAlternate = 5;
-constexpr int kLeaves = 8, kOfTen = 7;
+// PREFIX: blocks of 16 keys (a stretch's beginning counts 16 more) that kv_attend_body.cuh's Rest reads in an SM's time for a
+// tile.  In us, with 14 / 22 / 30 / 47 / 70: 64 requests of up to 500 keys behind 2048 40 / 34 / 32 / 30 / 31, behind 8192
+// 50 / 42 / 41 / 42 / 41, behind 16384 58 / 55 / 54 / 51 / 56; 45 requests in 4 groups, fp32, 42 / 41 / 45 / 47 / 47
+constexpr int kRestOfTile = 36, kRestOfTileSplit = 22, kRestEntry = 16;
 
 // T: type of queries and outputs; fp32 queries and weights are two f16 parts each, with products for both.  GROUPS: softmax
 // warpgroups, each with its own scores and outputs.  TILES: row tiles of a stretch.  KEYS: keys of a tile
@@ -192,6 +197,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
     __shared__ long long sum_s[kThreads / 32];
     __shared__ int last_s;
     __shared__ float f_s[kTileRows];
+    __shared__ unsigned long long work_s[3];          // PREFIX: tiles, stretches, blocks behind the prefixes
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, group = warp >> 2;
     const uint32_t bar = smem_u32(bars);
     // full and empty of two K stages, of two V stages; scores, weights, output and queries of two tiles
@@ -214,6 +220,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (tid < 4) absent[tid] = 0u;
+    if (PREFIX && tid < 3) work_s[tid] = 0ull;
     if (warp == 12) tc::tmem_alloc(smem_u32(&tmem_slot), 512);
 
     // Maybe ahead of warp 12's allocation.  A dependent that starts early cannot take the tensor memory first: it starts once
@@ -249,6 +256,37 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
         wt = min(wt, nt);
         st = a.window > 0 ? min((int)(((int64_t)a.sinks + kTileKeys - 1) / kTileKeys), wt) : 0;
     };
+    // PREFIX: a stretch's pieces have `piece` tiles.  The kernel of what lies behind the prefix starts beside this one: it gets
+    // SMs by what either has to do
+    int piece = 1;
+    if constexpr (PREFIX) {
+        __syncthreads();
+        unsigned long long tiles = 0, stretches = 0, blocks = 0;
+        for (int i = tid; i < a.n; i += kThreads) {
+            int len, q0, nq, st, wt, nt;
+            lengths(i, len, q0, nq);
+            if (nq == 0) continue;
+            visible(len, nq, 0, 1, st, wt, nt);
+            const unsigned long long strips = (unsigned long long)(nq * a.G + kStretchRows - 1) / kStretchRows * a.Hk;
+            tiles += strips * nt;
+            stretches += strips;
+        }
+        for (int i = tid; i < a.n_members; i += kThreads) blocks += kRestEntry + max(a.member_len[i] - max(a.start[i], 0), 0) / kBlockTokens;
+#pragma unroll
+        for (int o = 16; o; o >>= 1) {
+            tiles += __shfl_xor_sync(0xffffffffu, tiles, o);
+            stretches += __shfl_xor_sync(0xffffffffu, stretches, o);
+            blocks += __shfl_xor_sync(0xffffffffu, blocks, o);
+        }
+        if (lane == 0) { atomicAdd(&work_s[0], tiles); atomicAdd(&work_s[1], stretches); atomicAdd(&work_s[2], blocks); }        // whole numbers
+        __syncthreads();
+        const float t = (float)work_s[0], grid = (float)gridDim.x, few = grid - (float)work_s[1];
+        float ctas = grid * t / (t + (float)work_s[2] * (float)a.Hk / (SPLIT ? kRestOfTileSplit : kRestOfTile) + 1.f);
+        if (few > 0.5f * grid) ctas = fminf(ctas, few);          // cutting adds a piece a stretch at most: one each CTA
+        piece = max((int)ceilf(t / fmaxf(ctas, 1.f)), 1);
+    }
+    constexpr int kFront = PREFIX ? 0 : kEntry;          // what a stretch has in the line in front of its tiles, and with them
+    auto weight = [&](int units) { return PREFIX ? (units + piece - 1) / piece * piece : kEntry + units; };
     {
         long long carry = 0;
         for (int base = 0; base < a.n; base += kThreads) {
@@ -260,7 +298,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
                 for (int row0 = 0; row0 < nq * a.G; row0 += kStretchRows) {
                     int st, wt, nt;
                     visible(len, nq, row0, min(row0 + kStretchRows, nq * a.G), st, wt, nt);
-                    mine += (long long)(kEntry + max(st + nt - wt, 1)) * a.Hk;
+                    mine += (long long)weight(max(st + nt - wt, 1)) * a.Hk;
                 }
             }
             long long inc = mine;
@@ -285,13 +323,12 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
     bool dead = tmem_slot != kTmem;          // a wait ran out: nothing more is waited for or issued, the loops run out
     if (dead && tid == 0) atomicOr(a.status, MOE_KV_STATUS_TIMEOUT);
     const long long total = line[a.n];
-    // A prefix of few tiles leaves SMs to the kernel of what lies behind it, which starts beside this one
-    const long long ctas = PREFIX && total <= kLeaves * (long long)gridDim.x ? max((long long)gridDim.x * kOfTen / 10, 1ll) : (long long)gridDim.x;
-    const long long share = max((total + ctas - 1) / ctas, 1ll);
+    long long share = max((total + gridDim.x - 1) / (long long)gridDim.x, 1ll);
+    if (PREFIX) share = (share + piece - 1) / piece * piece;
     const long long at = min(share * blockIdx.x, total);
     const long long end = min(at + share, total);
 
-    // A stretch's place in the line is kEntry (what beginning it costs) and then its tiles.  Every role walks the pieces
+    // A stretch's place in the line is kFront (what beginning it costs) and then its tiles.  Every role walks the pieces
     // of the CTA's share by itself: found once, then counted on.
     struct Piece { int req, len, q0, nq, row0, row1, st, wt, present, units, head, first, last, cta0, cta1; long long place; };
     auto shape = [&](Piece &p) {
@@ -302,7 +339,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
         p.units = max(p.present, 1);
     };
     auto cut = [&](Piece &p) {          // which tiles of the stretch are this CTA's; false: behind the share
-        const long long tiles0 = p.place + kEntry;
+        const long long tiles0 = p.place + kFront;
         p.first = (int)max(at - tiles0, 0ll);
         p.last = (int)min(end - tiles0, (long long)p.units);
         p.cta0 = (int)(tiles0 / share);
@@ -321,16 +358,16 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
         p.place = line[lo];
         for (p.row0 = 0;; p.row0 += kStretchRows) {
             shape(p);
-            const long long here = (long long)(kEntry + p.units) * a.Hk;
+            const long long here = (long long)weight(p.units) * a.Hk;
             if (at < p.place + here) break;
             p.place += here;
         }
-        p.head = (int)((at - p.place) / (kEntry + p.units));
-        p.place += (long long)p.head * (kEntry + p.units);
+        p.head = (int)((at - p.place) / weight(p.units));
+        p.place += (long long)p.head * weight(p.units);
         return cut(p);
     };
     auto next = [&](Piece &p) {
-        p.place += kEntry + p.units;
+        p.place += weight(p.units);
         if (p.place >= end) return false;
         if (++p.head == a.Hk) {
             p.head = 0;
