@@ -447,7 +447,7 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
         auto find_blocks = [&](int from, int page, int &b) {
             const int k = from + (lane >> 1), u = first + (warp + k * kWarps) * kPair + (lane & 1);
             b = 0;
-            if (k >= mine || u >= b1) return -1;
+            if (k >= mine || u >= b1 || (kListed && nq == 0)) return -1;          // the list of a token of no request says nothing
             b = block_at(u);
             if (kListed) {
                 if (page < 0 || page >= a.width) {

@@ -36,7 +36,7 @@ __global__ void __launch_bounds__(kThreads) prefix_kernel(PrefixArgs a, int clus
 
     // groups that are not consecutive runs of requests: nothing is shared
     int good = 1;
-    for (int x = tid; x <= a.n_groups; x += kThreads) {
+    for (int x = a.n_groups > 0 ? tid : 1; x <= a.n_groups; x += kThreads) {
         const int at = a.groups[x];
         good &= at >= 0 && at <= a.n && (x == 0 || a.groups[x - 1] <= at);
     }

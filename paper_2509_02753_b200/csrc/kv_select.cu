@@ -53,8 +53,8 @@ __global__ void __launch_bounds__(32 * kSumWarps) summarise_kernel(SelectArgs a,
     const int i = warp_find(a.n, item, begins);
     if (i >= a.n) return;
     const Request r = request_of(a, i);
-    const int col = (max(r.len - r.nq, 0) >> a.page_shift) + item - begins(i);
-    if (r.nq == 0 || r.len == 0 || col > (r.len - 1) >> a.page_shift) return;
+    const int in = item - begins(i), col = (max(r.len - r.nq, 0) >> a.page_shift) + in;
+    if (in < 0 || r.nq == 0 || r.len == 0 || col > (r.len - 1) >> a.page_shift) return;
     const int page = a.table[(int64_t)i * a.width + col];
     if (page < 0 || page >= a.n_pages) { if (lane == 0) atomicOr(a.status, MOE_KV_STATUS_BAD_INDEX); return; }
     const int tokens = min(1 << a.page_shift, r.len - (col << a.page_shift));

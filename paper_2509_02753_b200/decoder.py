@@ -48,10 +48,10 @@ class Attention:
 
 
 class Request:
-    """Tokens in the cache, the row of the block table, and the row whose prompt it began with (its own unless forked)."""
+    """Tokens in the cache, the row of the block table, and what it has in common with those that began with its prompt."""
 
     def __init__(self, row: int):
-        self.row, self.length, self.origin = row, 0, row
+        self.row, self.length, self.origin = row, 0, object()
 
 
 def rms_norm(x: torch.Tensor, eps: float = 1e-6) -> torch.Tensor:
@@ -102,7 +102,7 @@ class Decoder:
                 self.free.append(page)
         self.table[row].fill_(-1)
         self.lengths[row] = 0
-        self.requests[row].length, self.requests[row].origin = 0, row
+        self.requests[row].length, self.requests[row].origin = 0, object()
 
     def fork(self, row: int, others: Sequence[int], tokens: Optional[int] = None) -> int:
         """The requests `others`, which have no tokens yet, begin with the first `tokens` tokens of request `row` (all by default),
@@ -128,7 +128,7 @@ class Decoder:
     def _groups(self, new: Sequence[int]) -> Optional[tuple]:
         """(first request of each group of neighbours of one origin and the end, the largest group's new tokens); none if nothing is shared."""
         origins = [r.origin for r in self.requests]
-        cu = [i for i in range(len(origins)) if i == 0 or origins[i] != origins[i - 1]] + [len(origins)]
+        cu = [i for i in range(len(origins)) if i == 0 or origins[i] is not origins[i - 1]] + [len(origins)]
         if not self.more_users or len(cu) > len(origins):
             return None
         return cu, max(sum(new[a: b]) for a, b in zip(cu, cu[1:]))

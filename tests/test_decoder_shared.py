@@ -103,6 +103,10 @@ def test_groups_are_neighbours_of_one_origin():
         other.step(tokens(32), [32])
         near(y[i: i + 1], other.step(x[i: i + 1], [1]))
         other.close()
+    dec.finish(0)
+    dec.step(tokens(3), [3, 0, 0, 0, 0])          # another prompt in the row of the first
+    assert dec._groups([1, 1, 1, 2, 3])[0] == [0, 1, 2, 3, 5]
+    dec.check()
     dec.close()
 
 

@@ -577,6 +577,59 @@ def test_selected_with_more_new_tokens_than_keys():
     assert not got[:3].any() and not got[23:].any()
 
 
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_rows_in_front_of_the_first_request(dtype):
+    """cu_new begins above 0: rows, lists and outputs in front stay as they are."""
+    lens, new, front = [100, 40, 90], [1, 3, 20], 5
+    b = Batch(9, lens, new, 4, 2, 64, 16, dtype, [0, 3], [1], columns=wide(3, 2, 64, 16, 1 / 3))
+    cu = b.args[1] + front
+    q = torch.cat([torch.full_like(b.q[:front], math.nan), b.q])
+    more = dict(k_scale=KS, v_scale=VS)
+    with plan_for(4, 2, 64, 16, dtype, requests=3, tokens=64) as plan:
+        summaries, again = (plan.new_summaries(len(b.cache)) for _ in range(2))
+        plan.summarise(*b.args[1:], b.pages, summaries, 24)
+        plan.summarise(cu, *b.args[2:], b.pages, again, 24 + front)
+        assert torch.equal(summaries, again)
+        want = plan.select(*b.args, summaries, n_select=3), plan.attention(*b.args, b.pages, **more)
+        for max_new in (1, 20):
+            lists = torch.full((24 + front, 2, 3), -7, dtype=torch.int32, device="cuda")
+            plan.select(q, cu, *b.args[2:], summaries, n_select=3, max_new=max_new, out=lists)
+            assert torch.equal(lists[front:], want[0]) and bool((lists[:front] == -7).all())
+        one, other = (torch.full(q.shape, 7.0, dtype=dtype, device="cuda") for _ in range(2))
+        plan.attention_selected(q, cu, *b.args[2:], b.pages, lists, out=one, **more)
+        groups = i32([0, 3])
+        shared, start = plan.shared_prefix(groups, cu, *b.args[2:])
+        plan.attention_shared(q, cu, *b.args[2:], b.pages, groups, shared, start, max_new=1, max_group=3, out=other, **more)
+        assert torch.equal(one[front:], plan.attention_selected(*b.args, b.pages, want[0], **more))
+        assert plan.device_status() == (0, 0)
+    assert shared.tolist() == [16]
+    b.near(other[front:], *b.reference())
+    assert bool((one[:front] == 7).all()) and bool((other[:front] == 7).all())
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("many", [False, True])
+def test_rows_that_are_not_finite_stay_alone(many, dtype):
+    """In a group's prefix (also as tiles of 128 rows) and over listed pages."""
+    n = 20 if many else 3
+    b = Batch(10, [70 + i for i in range(n)], [1] * n, 4, 2, 64, 16, dtype, [0, n], [4], columns=wide(n, 2, 64, 16, 1 / n))
+    q = b.q.clone()
+    q[0, 1, 3], q[1, 2, 5], q[2, 0, 0] = math.nan, math.inf, -math.inf
+    fine = torch.ones(q.shape[:2], dtype=torch.bool)
+    fine[0, 1] = fine[1, 2] = fine[2, 0] = False
+    with b.plan() as plan:
+        groups = i32([0, n])
+        shared, start = plan.shared_prefix(groups, *b.args[1:])
+        lists = i32(np.tile(np.array([4, 0, 2]), (n, 2, 1)))
+        for call in (lambda x: plan.attention_shared(x, *b.args[1:], b.pages, groups, shared, start, max_new=1, max_group=n, k_scale=KS, v_scale=VS),
+                     lambda x: plan.attention_selected(x, *b.args[1:], b.pages, lists, k_scale=KS, v_scale=VS)):
+            want, got = call(b.q), call(q)
+            assert torch.equal(got[fine], want[fine]) and bool(torch.isnan(got[0, 1]).all())
+        assert plan.device_status() == (0, 0)
+
+
 # ------------------------------------------------------------------------------------------ together
 
 def steps(plan, kv, heads, dim, page, rng):
@@ -810,6 +863,11 @@ def test_refusals():
         assert shared_call() == 0
         assert shared_call(size=need - 1) == -4 and shared_call(where=None) == -4 and shared_call(where=scratch.data_ptr() + 8) == -3
         assert shared_call(at=8) == -3 and shared_call(group=g.data_ptr() + 2) == -3 and shared_call(group=None) == -1 and shared_call(tab=None) == -1
+        assert lib.moe_kv_shared_prefix(h, None, 0, cu.data_ptr(), lens.data_ptr(), 2, table.data_ptr(), width, None, start.data_ptr(), None) == 0
+        assert lib.moe_kv_shared_prefix(h, None, 1, cu.data_ptr(), lens.data_ptr(), 2, table.data_ptr(), width, shared.data_ptr(), start.data_ptr(), None) == -1
+        assert lib.moe_kv_shared_prefix(h, g.data_ptr() + 2, 1, cu.data_ptr(), lens.data_ptr(), 2, table.data_ptr(), width, shared.data_ptr(), start.data_ptr(), None) == -3
+        torch.cuda.synchronize()
+        assert start.tolist() == [0, 0]
         assert lib.moe_kv_summarise(h, cu.data_ptr(), lens.data_ptr(), 2, 2, table.data_ptr(), table.shape[1], b.pages.data_ptr(), len(b.cache), summaries.data_ptr() + 8, None) == -3
         assert lib.moe_kv_read_summaries(h, summaries.data_ptr(), len(b.cache), cu.data_ptr(), 1, 1.0, scratch.data_ptr() + 4, scratch.data_ptr(), None) == -3
         assert lib.moe_kv_select(h, ctypes.byref(rows), 2, cu.data_ptr(), lens.data_ptr(), 2, 1, few.data_ptr(), few.shape[1], summaries.data_ptr(), len(b.cache), 2, 1, 1,
