@@ -316,25 +316,13 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
         visible(begin, len, nq, row0, row1, sb, wb, nb);
         units = max(sb + nb - wb, 1);
     };
-    // Listed: which request token q0 belongs to, by 32 probes at a time; its keys up to its own are those it may see.  A token
-    // of no request has no row
+    // Listed: which request token q0 belongs to; its keys up to its own are those it may see.  A token of no request has no row
     auto take_token = [&]() {
-        int lo = 0, hi = a.n;          // the first request that ends behind the token
-#pragma unroll 1
-        while (hi - lo > 32) {
-            const int step = (hi - lo + 31) / 32, at_lane = lo + (lane + 1) * step - 1;
-            const int before = __popc(__ballot_sync(0xffffffffu, at_lane < hi && a.cu[min(at_lane, hi - 1) + 1] <= q0));
-            lo = min(lo + before * step, hi);
-            hi = min(lo + step, hi);
-        }
-        lo += __popc(__ballot_sync(0xffffffffu, lo + lane < hi && a.cu[min(lo + lane, a.n - 1) + 1] <= q0));
-        req = min(lo, a.n - 1);
-        const int token = q0;
-        lengths(req, len, q0, nq);
-        const bool here = token >= q0 && token - q0 < nq;
-        len = here ? max(len - nq + token - q0 + 1, 0) : 0;
+        const Request r = find_request(a.cu, a.kv_len, a.n, q0, a.T, (int64_t)a.width * page_tokens, a.status, [](int cu, int) { return cu; });
+        const bool here = q0 >= r.q0 && q0 - r.q0 < r.nq;
+        req = min(r.i, a.n - 1);
+        len = here ? max(r.len - r.nq + q0 - r.q0 + 1, 0) : 0;
         nq = here ? 1 : 0;
-        q0 = token;
     };
     while (at < end) {
         // ---- which stretch `at` lies in: found, or the one behind the last piece's

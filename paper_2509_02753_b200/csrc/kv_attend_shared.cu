@@ -23,10 +23,9 @@ __global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(AttendArgs a) {
     bool mine = at_row < (long long)a.T * a.H;
     if (mine) {
         const int token = (int)(at_row / a.H);
-        const int i = warp_find(a.n, token, [&](int x) { return a.cu[x]; });
-        mine = i < a.n && a.cu[i] >= 0 && a.cu[i] <= token && a.cu[i + 1] <= a.T;
+        const Request r = find_request(a.cu, a.kv_len, a.n, token, a.T, (int64_t)a.width * (kBlockTokens << a.page_shift), a.status, [](int cu, int) { return cu; });
         // as in Rest: of a request with no prefix the rows are done
-        if (mine) mine = min(a.start[i], max(min(max(a.kv_len[i], 0), (int)min((long long)a.width * (kBlockTokens << a.page_shift), (long long)INT32_MAX)) - (a.cu[i + 1] - a.cu[i]), 0)) > 0;
+        mine = token >= r.q0 && token - r.q0 < r.nq && min(a.start[min(r.i, a.n - 1)], r.len - r.nq) > 0;
     }
     pdl_wait();
     if (!mine) return;

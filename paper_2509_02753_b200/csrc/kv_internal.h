@@ -53,19 +53,34 @@ struct FastDiv {
 };
 
 #ifdef __CUDACC__
-// First request i in [0, n) with f(i + 1) > x, n where there is none; f does not fall.  By a whole warp, 32 probes at a time
+// A request of a call, as all kernels take it: keys that the tables have room for, first new token, new tokens
+struct Request { int i, len, q0, nq; };
+
+// The first request i with f(cu[i + 1], i + 1) > x, where f does not fall; i = n, without rows, if there is none.  By a whole warp, 32
+// probes at a time; the last ones bring the lengths along, so that these are not one more read that waits for another.
+// T: rows of the call; room: tokens that a row of the table stands for
 template <typename F>
-__device__ __forceinline__ int warp_find(int n, int x, F f) {
+__device__ __forceinline__ Request find_request(const int32_t *cu, const int32_t *kv_len, int n, int x, int T, int64_t room, int32_t *status, F f) {
     const int lane = threadIdx.x & 31;
     int lo = 0, hi = n;
 #pragma unroll 1
     while (hi - lo > 32) {
-        const int step = (hi - lo + 31) / 32, at = lo + (lane + 1) * step - 1;
-        const int before = __popc(__ballot_sync(0xffffffffu, at < hi && f(min(at, hi - 1) + 1) <= x));
+        const int step = (hi - lo + 31) / 32, at = lo + (lane + 1) * step, in = min(at, hi);
+        const int before = __popc(__ballot_sync(0xffffffffu, at <= hi && f(cu[in], in) <= x));
         lo = min(lo + before * step, hi);
         hi = min(lo + step, hi);
     }
-    return lo + __popc(__ballot_sync(0xffffffffu, lo + lane < hi && f(min(lo + lane, n - 1) + 1) <= x));
+    const int at = min(lo + lane, n - 1);
+    const int c0 = cu[at], c1 = cu[at + 1], l = kv_len[at];
+    const int found = __popc(__ballot_sync(0xffffffffu, lo + lane < hi && f(c1, at + 1) <= x));
+    Request r{lo + found, max(__shfl_sync(0xffffffffu, l, found & 31), 0), __shfl_sync(0xffffffffu, c0, found & 31), __shfl_sync(0xffffffffu, c1, found & 31)};
+    r.nq -= r.q0;
+    if (lo + found >= hi) return Request{n, 0, 0, 0};
+    const bool bad_rows = r.q0 < 0 || r.nq < 0 || r.q0 > T - r.nq;
+    if ((bad_rows || r.len > room) && lane == 0) atomicOr(status, MOE_KV_STATUS_BAD_INDEX);
+    if (bad_rows) r.nq = 0;
+    r.len = (int)min((int64_t)r.len, room);
+    return r;
 }
 #endif
 

@@ -22,19 +22,6 @@ namespace {
 
 __device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
-// Keys and new tokens of a request: as the attention takes them
-struct Request { int len, q0, nq; };
-__device__ __forceinline__ Request request_of(const SelectArgs &a, int i) {
-    const int64_t room = (int64_t)a.width << a.page_shift;
-    Request r{max(a.kv_len[i], 0), a.cu[i], 0};
-    r.nq = a.cu[i + 1] - r.q0;
-    const bool bad_rows = r.q0 < 0 || r.nq < 0 || r.q0 > a.T - r.nq;
-    if (bad_rows || r.len > room) atomicOr(a.status, MOE_KV_STATUS_BAD_INDEX);
-    if (bad_rows) r.nq = 0;
-    r.len = (int)min((int64_t)r.len, room);
-    return r;
-}
-
 // ------------------------------------------------------------------------------------------------ summaries
 
 constexpr int kSumWarps = 4;
@@ -49,13 +36,11 @@ __global__ void __launch_bounds__(32 * kSumWarps) summarise_kernel(SelectArgs a,
     const long long id = (long long)blockIdx.x * kSumWarps + (threadIdx.x >> 5);
     if (id >= warps) return;
     const int lane = threadIdx.x & 31, item = (int)(id / a.Hk), head = (int)(id % a.Hk);
-    auto begins = [&](int i) { return (max(a.cu[i], 0) >> a.page_shift) + 2 * i; };
-    const int i = warp_find(a.n, item, begins);
-    if (i >= a.n) return;
-    const Request r = request_of(a, i);
-    const int in = item - begins(i), col = (max(r.len - r.nq, 0) >> a.page_shift) + in;
+    auto begins = [&](int cu, int i) { return (max(cu, 0) >> a.page_shift) + 2 * i; };
+    const Request r = find_request(a.cu, a.kv_len, a.n, item, a.T, (int64_t)a.width << a.page_shift, a.status, begins);
+    const int in = item - begins(r.q0, r.i), col = (max(r.len - r.nq, 0) >> a.page_shift) + in;
     if (in < 0 || r.nq == 0 || r.len == 0 || col > (r.len - 1) >> a.page_shift) return;
-    const int page = a.table[(int64_t)i * a.width + col];
+    const int page = a.table[(int64_t)r.i * a.width + col];
     if (page < 0 || page >= a.n_pages) { if (lane == 0) atomicOr(a.status, MOE_KV_STATUS_BAD_INDEX); return; }
     const int tokens = min(1 << a.page_shift, r.len - (col << a.page_shift));
     const int part = lane % kLanes, mine = lane / kLanes;
@@ -227,18 +212,22 @@ __global__ void __launch_bounds__(kThreads, W == 256 ? 2 : 4) select_kernel(Sele
     pdl_trigger();
     pdl_wait();
 
-    auto begins = [&](int i) { return TOK == 1 ? max(a.cu[i], 0) : max(a.cu[i], 0) / TOK + i; };
-    const int i = warp_find(a.n, item, begins);
-    Request q{0, 0, 0};
-    if (i < a.n) q = request_of(a, i);
-    const int tok0 = TOK == 1 ? item - q.q0 : (item - (i < a.n ? begins(i) : 0)) * TOK;          // of the request's new tokens
-    const int many = i < a.n && tok0 >= 0 ? max(min(TOK, q.nq - tok0), 0) : 0;
+    auto begins = [&](int cu, int i) { return TOK == 1 ? max(cu, 0) : max(cu, 0) / TOK + i; };
+    const Request q = find_request(a.cu, a.kv_len, a.n, item, a.T, (int64_t)a.width << a.page_shift, a.status, begins);
+    const int tok0 = TOK == 1 ? item - q.q0 : (item - begins(q.q0, q.i)) * TOK;          // of the request's new tokens
+    const int many = tok0 >= 0 ? max(min(TOK, q.nq - tok0), 0) : 0;
     auto own_page = [&](int t) { const int p = q.len - q.nq + tok0 + t; return p < 0 ? -1 : p >> a.page_shift; };
     // pages [first, top) of the tile's last token are to be scored, if there are more than are wanted
     const int last_own = many > 0 ? own_page(many - 1) : -1;
     const int top = last_own >= a.n_select ? last_own - a.last + 1 : 0, from = min(a.first, top);
 
     if (top > from) {
+        // ---- this CTA's pages are [begin, end); its first ones' numbers are asked for ahead of the queries
+        const int each = ((top - from + cluster - 1) / cluster + 15) & ~15;
+        const int begin = from + rank * each, end = min(begin + each, top);
+        const int32_t *table = a.table + (int64_t)q.i * a.width;
+        auto page_at = [&](int col) { return col < end ? table[col] : -1; };
+        int at = begin + warp * 16, p0 = page_at(at + r), p1 = page_at(at + r + 8);
         // ---- queries: a warp a token, W/32 neighbouring dimensions a lane; sums in the order of the heads
         constexpr int kPer = W / 32;
         constexpr uintptr_t kWide = (kPer * sizeof(T) < 16 ? kPer * sizeof(T) : 16) - 1;
@@ -299,14 +288,9 @@ __global__ void __launch_bounds__(kThreads, W == 256 ? 2 : 4) select_kernel(Sele
         for (int x = 0; x < kChunks; ++x)
             b[x] = r < TOK ? *reinterpret_cast<const uint4 *>(q_s + r * kQRow + c * 16 + 64 * x) : make_uint4(0u, 0u, 0u, 0u);
 
-        // ---- scores of this CTA's pages [begin, end)
-        const int each = ((top - from + cluster - 1) / cluster + 15) & ~15;
-        const int begin = from + rank * each, end = min(begin + each, top);
-        const int32_t *table = a.table + (int64_t)i * a.width;
-        auto page_at = [&](int col) { return col < end ? table[col] : -1; };
+        // ---- scores
         if (cluster > 1) cluster_wait();          // the first CTA is there
         const uint32_t to = cluster > 1 ? in_cta0(smem_u32(scores)) : smem_u32(scores);
-        int at = begin + warp * 16, p0 = page_at(at + r), p1 = page_at(at + r + 8);
 #pragma unroll 1
         for (; at < end; at += kWarps * 16) {
             const int next = at + kWarps * 16, n0 = page_at(next + r), n1 = page_at(next + r + 8);
