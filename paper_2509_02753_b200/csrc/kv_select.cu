@@ -49,23 +49,39 @@ __global__ void __launch_bounds__(32 * kSumWarps) summarise_kernel(SelectArgs a,
     __half2 hi[16], lo[16];
 #pragma unroll
     for (int d = 0; d < 16; ++d) { hi[d] = __half2half2(__ushort_as_half(0xfc00)); lo[d] = __half2half2(__ushort_as_half(0x7c00)); }
-#pragma unroll 8
-    for (int t = mine; t < tokens; t += kAtOnce) {
-        const uint8_t *blk = blocks + (t >> 4) * block_bytes(W);
-        const uint4 codes = __ldg(reinterpret_cast<const uint4 *>(blk + (t & 15) * (W / 2) + part * 16));
-        const uint32_t two = scales2(__ldg(reinterpret_cast<const uint16_t *>(blk + k_scales_at(W) + (t & 15) * (W / 16) + part * 2)));
-        const uint32_t words[4] = {codes.x, codes.y, codes.z, codes.w};
+    // a lane's next eight tokens are asked for at once, whatever is missing of them
+    constexpr int kBatch = 8;
+#pragma unroll 1
+    for (int t0 = mine; t0 < tokens; t0 += kBatch * kAtOnce) {
+        uint4 codes[kBatch];
+        uint32_t scale[kBatch];
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const uint32_t sc = __byte_perm(two, 0, w < 2 ? 0x1010 : 0x3232);
-            uint32_t h[4];
-            codes4(words[w], h);
+        for (int x = 0; x < kBatch; ++x) {
+            const int t = t0 + x * kAtOnce;
+            const uint8_t *blk = blocks + (t >> 4) * block_bytes(W);
+            codes[x] = make_uint4(0u, 0u, 0u, 0u);
+            scale[x] = 0u;
+            if (t < tokens) {
+                codes[x] = __ldg(reinterpret_cast<const uint4 *>(blk + (t & 15) * (W / 2) + part * 16));
+                scale[x] = __ldg(reinterpret_cast<const uint16_t *>(blk + k_scales_at(W) + (t & 15) * (W / 16) + part * 2));
+            }
+        }
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const uint32_t x = mul2(h[j], sc);
-                const __half2 v = *reinterpret_cast<const __half2 *>(&x);
-                hi[4 * w + j] = __hmax2(hi[4 * w + j], v);
-                lo[4 * w + j] = __hmin2(lo[4 * w + j], v);
+        for (int x = 0; x < kBatch; ++x) {
+            if (t0 + x * kAtOnce >= tokens) continue;
+            const uint32_t two = scales2(scale[x]), words[4] = {codes[x].x, codes[x].y, codes[x].z, codes[x].w};
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const uint32_t sc = __byte_perm(two, 0, w < 2 ? 0x1010 : 0x3232);
+                uint32_t h[4];
+                codes4(words[w], h);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t y = mul2(h[j], sc);
+                    const __half2 v = *reinterpret_cast<const __half2 *>(&y);
+                    hi[4 * w + j] = __hmax2(hi[4 * w + j], v);
+                    lo[4 * w + j] = __hmin2(lo[4 * w + j], v);
+                }
             }
         }
     }
