@@ -260,11 +260,18 @@ __global__ void __launch_bounds__(kThreads, W == 256 ? 2 : 4) select_kernel(Sele
                 };
                 if (lane * kPer >= a.D) {          // D is a multiple of 8, kPer at most 8
                 } else if (wide) {
-#pragma unroll 4
-                    for (int g = 0; g < a.G; ++g) {
-                        float x[kPer];
-                        load_q<kPer>(src + g * a.q.hs, x);
-                        add(x);
+                    constexpr int kHeads = 4;          // asked for at once
+#pragma unroll 1
+                    for (int g0 = 0; g0 < a.G; g0 += kHeads) {
+                        float x[kHeads][kPer];
+#pragma unroll
+                        for (int g = 0; g < kHeads; ++g) {
+#pragma unroll
+                            for (int e = 0; e < kPer; ++e) x[g][e] = 0.f;
+                            if (g0 + g < a.G) load_q<kPer>(src + (g0 + g) * a.q.hs, x[g]);
+                        }
+#pragma unroll
+                        for (int g = 0; g < kHeads; ++g) add(x[g]);          // zeros change nothing
                     }
                 } else {
 #pragma unroll 1
