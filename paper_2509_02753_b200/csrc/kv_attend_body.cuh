@@ -25,7 +25,7 @@
 // calls give equal bits.  Lengths are read on the device; no host knows them.  Warps of a CTA take the blocks of a piece
 // two at a time in turn, each with its own ring of bulk copies, and join once per piece.
 //
-// Four builds of the kernel, by what the rows of a stretch read (Reads below; kv_attend.cu, kv_attend_shared.cu,
+// Five builds of the kernel, by what the rows of a stretch read (Reads below; kv_attend.cu, kv_attend_shared.cu,
 // kv_attend_selected.cu):
 //   Every   all keys of the request that the row's position and the window let it see
 //   Prefix  "requests" are groups of requests and "keys" their shared prefix, which all rows of a group see whole; what
@@ -34,10 +34,13 @@
 //           runs and shares the SMs with it; only one CTA waits for it, in the end, so that this kernel's end is both kernels'.
 //           kv_attend_shared.cu joins the two
 //   Listed  a token is a "request" of its own; its blocks are those of the pages listed for it and the head
+//   Pieces  the same where stretches are few: all have as many blocks, which the host knows, so the pieces of one are the CTAs
+//           of a cluster, which join through one another's shared memory
 #pragma once
 
 #include <float.h>
 
+#include <algorithm>
 #include <atomic>
 
 #include "kv_codes.cuh"
@@ -95,15 +98,17 @@ struct Shape {
     static constexpr int kJoinTiles = NT >= 8 ? 1 : (kTiles < 8 / NT ? kTiles : 8 / NT);   // m16 tiles joined at a time: 32 KB
     static constexpr int kJoin = kWarps * kRows * kJoinTiles * 16 * 4;
     static_assert(kJoin <= kRing, "the join's buffer is the ring's");
+    static constexpr int kRowsBytes = kRows * W * 4;          // a piece's sums, behind that buffer where the CTAs of a cluster join
+    static constexpr bool kClusters = kJoin + kRowsBytes <= kRing;
     static constexpr int kSmem = kRing + kQ;                  // plus the line of requests
 };
 
-enum class Reads { Every, Prefix, Rest, Listed };
+enum class Reads { Every, Prefix, Rest, Listed, Pieces };
 
 template <typename T, int W, int NT, int MINB, Reads R>
 __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs a) {
     constexpr bool SPLIT = sizeof(T) == 4;
-    constexpr bool kPrefix = R == Reads::Prefix, kRest = R == Reads::Rest, kListed = R == Reads::Listed;
+    constexpr bool kPrefix = R == Reads::Prefix, kRest = R == Reads::Rest, kListed = R == Reads::Listed || R == Reads::Pieces, kPieces = R == Reads::Pieces;
     using S = Shape<W, NT, SPLIT>;
     extern __shared__ __align__(128) uint8_t smem[];
     uint8_t *ring = smem, *q_s = smem + S::kRing;
@@ -224,7 +229,8 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
         // every stretch has the same blocks: no line
         const long long stretches = (long long)a.T * strips_of * a.Hk, units = (long long)a.n_listed << a.page_shift;
         choose(stretches * units, stretches, (int)units);
-        total = stretches * (even ? (units + chunk - 1) / chunk : units + kEntry);
+        if (kPieces) few = even = true;
+        total = stretches * (kPieces ? a.cluster : even ? (units + chunk - 1) / chunk : units + kEntry);
         simple = true;
     } else if (a.n <= 32) {
         int len = 0, q0 = 0, nq = 0, begin = 0;
@@ -327,7 +333,7 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
     while (at < end) {
         // ---- which stretch `at` lies in: found, or the one behind the last piece's
         if constexpr (kListed) {
-            const long long many = ((long long)a.n_listed << a.page_shift), weight = even ? (few ? (many + chunk - 1) / chunk : 1) : many + kEntry;
+            const long long many = ((long long)a.n_listed << a.page_shift), weight = kPieces ? a.cluster : even ? (few ? (many + chunk - 1) / chunk : 1) : many + kEntry;
             const long long stretch = (at | weight) >> 31 ? at / weight : (long long)((uint32_t)at / (uint32_t)weight);
             place = stretch * weight;
             const int per = strips_of * a.Hk, in = (int)(stretch % per);
@@ -380,7 +386,7 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
         const int within = (int)(at - place);
         int first, last, cta0, cta1;
         if (even) {
-            const int weight = few ? (units + chunk - 1) / chunk : 1;
+            const int weight = kPieces ? a.cluster : few ? (units + chunk - 1) / chunk : 1;
             const int each = units / weight, rest = units - each * weight;          // `each` blocks, the first `rest` pieces one more
             first = within * each + min(within, rest);
             last = first + each + (within < rest);
@@ -775,7 +781,7 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
         const bool whole = first == 0 && last == units;
         // a CTA's first piece may be the end of a stretch, its last piece the beginning of one
         const int my_slot = blockIdx.x * 2 + (first == 0 ? 1 : 0);
-        float *part = a.part + (int64_t)my_slot * S::kRows * W;
+        float *part = kPieces ? reinterpret_cast<float *>(ring + S::kJoin) : a.part + (int64_t)my_slot * S::kRows * W;
         float2 *part_ml = a.part_ml + (int64_t)my_slot * S::kRows;
         float2 *buf = reinterpret_cast<float2 *>(ring);
         // row n of the stretch, dimensions d and d + 1: sums v with reference `top` and denominator `sum`
@@ -840,6 +846,32 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
                     a.o_pieces[(int64_t)(q0 + tok) * a.H + head * a.G + row - tok * a.G] = make_int4(cta0, cta1 + 1 - cta0, tid, 0);
                 }
             }
+        } else if (kPieces) {
+            // a share of the rows' dimensions from every CTA's shared memory, in the order of the keys; no CTA leaves before all are done
+            asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+            const uint32_t part_at = smem_u32(part), ml_at = smem_u32(row_ml);
+#pragma unroll 1
+            for (int e = within * kThreads + tid; e < S::kRows * W / 4; e += a.cluster * kThreads) {
+                const int n = e / (W / 4), d = e % (W / 4) * 4;
+                float top = kFloor, sum = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+                for (int y = 0; y < a.cluster; ++y) {
+                    uint32_t ml_of, part_of;
+                    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(ml_of) : "r"(ml_at + 8u * n), "r"(y));
+                    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(part_of) : "r"(part_at + 16u * e), "r"(y));
+                    float m_y, l_y, z[4];
+                    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(m_y), "=f"(l_y) : "r"(ml_of) : "memory");
+                    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(z[0]), "=f"(z[1]), "=f"(z[2]), "=f"(z[3]) : "r"(part_of) : "memory");
+                    const float to = fmaxf(top, m_y), old = top == to ? 1.f : ex2(top - to), k = m_y == to ? 1.f : ex2(m_y - to);
+                    sum = sum * old + l_y * k;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[i] = v[i] * old + z[i] * k;
+                    top = to;
+                }
+                put(n, d, make_float2(v[0], v[1]), top, sum);
+                put(n, d + 2, make_float2(v[2], v[3]), top, sum);
+            }
+            asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
         } else if (!whole) {
             if (tid < S::kRows) part_ml[tid] = row_ml[tid];
             __syncthreads();
@@ -935,6 +967,41 @@ cudaError_t launch(const AttendArgs &a, int sm_count, cudaStream_t s, uint64_t *
     grid = pieces < grid ? pieces : grid;
     grid = grid > a.max_ctas ? a.max_ctas : grid < 1 ? 1 : grid;
     ++*launches;
+    if constexpr (R == Reads::Listed && S::kClusters) {
+        // Few stretches: as many pieces of one as there are CTAs for, each a step of every warp at least, up to the eight that a
+        // cluster may have; where more would leave a piece below kLong blocks they join through the L2.  In us, so / in clusters:
+        // 32/8 heads of 128, 128 blocks: 1 token 11.3 / 7.9, 8 tokens 13.7 / 11.9, 16 tokens 17.4 / 15.9; 7/1 heads, 256 blocks in 32
+        // or 8 pieces 12.8 / 9.6; 8/8 heads of 96, fp32, 2 tokens, 480 blocks in 37 or 8 pieces 19.5 / 21.9
+        constexpr long long kLong = 40;
+        const long long stretches = (long long)a.T * ((a.G + S::kRows - 1) / S::kRows) * a.Hk, units = (long long)a.n_listed << a.page_shift;
+        const long long room = std::min((long long)sm_count * per_sm, (long long)a.max_ctas) / std::max(stretches, 1ll);
+        const long long most = std::min(room, (units + kLeast - 1) / kLeast), pieces = std::min(most, 8ll);
+        if (pieces > 1 && (most == pieces || units <= pieces * kLong)) {
+            auto in_clusters = attend_rows_kernel<T, W, NT, MINB, Reads::Pieces>;
+            static std::atomic<bool> ready[64];
+            if (dev >= 64 || !ready[dev].load()) {
+                err = cudaFuncSetAttribute(in_clusters, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem + 8 * (kFew + 1));
+                if (err != cudaSuccess) return err;
+                if (dev < 64) ready[dev].store(true);
+            }
+            AttendArgs b = a;
+            b.cluster = (int)pieces;
+            cudaLaunchConfig_t cfg{};
+            cfg.gridDim = dim3((unsigned)(stretches * pieces));
+            cfg.blockDim = dim3(kThreads);
+            cfg.dynamicSmemBytes = smem;
+            cfg.stream = s;
+            cudaLaunchAttribute attr[2];
+            attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+            attr[0].val.programmaticStreamSerializationAllowed = 1;
+            attr[1].id = cudaLaunchAttributeClusterDimension;
+            attr[1].val.clusterDim.x = (unsigned)pieces;
+            attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+            cfg.attrs = attr;
+            cfg.numAttrs = 2;
+            return cudaLaunchKernelEx(&cfg, in_clusters, b);
+        }
+    }
     return launch_chained(k, dim3((unsigned)grid), dim3(kThreads), smem, s, true, a);
 }
 

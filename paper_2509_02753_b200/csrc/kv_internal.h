@@ -169,6 +169,7 @@ struct AttendArgs {
     int piece_rows, result_rows, piece_results, piece_ctas;
     // Selected pages: [T][Hk][n_listed] columns of the request's row of the block table, -1: none
     const int32_t *listed; int n_listed;
+    int cluster;                              // CTAs that have a stretch's pieces, 0: no clusters
 };
 #ifdef __CUDACC__
 __device__ __forceinline__ int div_g(const AttendArgs &a, int row) { return (int)a.g_div.div((uint32_t)row); }      // row / G
