@@ -197,7 +197,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
     __shared__ long long sum_s[kThreads / 32];
     __shared__ int last_s;
     __shared__ float f_s[kTileRows];
-    __shared__ unsigned long long work_s[3];          // PREFIX: tiles, stretches, blocks behind the prefixes
+    __shared__ int work_s[3];          // PREFIX: tiles, stretches, blocks behind the prefixes
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, group = warp >> 2;
     const uint32_t bar = smem_u32(bars);
     // full and empty of two K stages, of two V stages; scores, weights, output and queries of two tiles
@@ -220,7 +220,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (tid < 4) absent[tid] = 0u;
-    if (PREFIX && tid < 3) work_s[tid] = 0ull;
+    if (PREFIX && tid < 3) work_s[tid] = 0;
     if (warp == 12) tc::tmem_alloc(smem_u32(&tmem_slot), 512);
 
     // Maybe ahead of warp 12's allocation.  A dependent that starts early cannot take the tensor memory first: it starts once
@@ -258,27 +258,32 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
     };
     // PREFIX: a stretch's pieces have `piece` tiles.  The kernel of what lies behind the prefix starts beside this one: it gets
     // SMs by what either has to do
-    int piece = 1;
+    int piece = 1, own_len = 0, own_q0 = 0, own_nq = 0;          // own: of group tid
     if constexpr (PREFIX) {
         __syncthreads();
-        unsigned long long tiles = 0, stretches = 0, blocks = 0;
-        for (int i = tid; i < a.n; i += kThreads) {
-            int len, q0, nq, st, wt, nt;
-            lengths(i, len, q0, nq);
-            if (nq == 0) continue;
-            visible(len, nq, 0, 1, st, wt, nt);
-            const unsigned long long strips = (unsigned long long)(nq * a.G + kStretchRows - 1) / kStretchRows * a.Hk;
-            tiles += strips * nt;
+        // what the first reads bring is used behind the others
+        const int member = tid < a.n_members ? a.member_len[tid] : 0, from = tid < a.n_members ? a.start[tid] : 0;
+        if (tid < a.n) lengths(tid, own_len, own_q0, own_nq);
+        long long tiles = 0, stretches = 0, blocks = tid < a.n_members ? kRestEntry + max(member - max(from, 0), 0) / kBlockTokens : 0;
+        auto add = [&](int len, int nq) {
+            if (nq == 0) return;
+            const long long strips = (long long)((nq * a.G + kStretchRows - 1) / kStretchRows) * a.Hk;
+            tiles += strips * ((len + kTileKeys - 1) / kTileKeys);
             stretches += strips;
+        };
+        add(own_len, own_nq);
+        for (int i = tid + kThreads; i < a.n; i += kThreads) {
+            int len, q0, nq;
+            lengths(i, len, q0, nq);
+            add(len, nq);
         }
-        for (int i = tid; i < a.n_members; i += kThreads) blocks += kRestEntry + max(a.member_len[i] - max(a.start[i], 0), 0) / kBlockTokens;
-#pragma unroll
-        for (int o = 16; o; o >>= 1) {
-            tiles += __shfl_xor_sync(0xffffffffu, tiles, o);
-            stretches += __shfl_xor_sync(0xffffffffu, stretches, o);
-            blocks += __shfl_xor_sync(0xffffffffu, blocks, o);
-        }
-        if (lane == 0) { atomicAdd(&work_s[0], tiles); atomicAdd(&work_s[1], stretches); atomicAdd(&work_s[2], blocks); }        // whole numbers
+        for (int i = tid + kThreads; i < a.n_members; i += kThreads) blocks += kRestEntry + max(a.member_len[i] - max(a.start[i], 0), 0) / kBlockTokens;
+        auto sum = [&](long long x, int *to) {          // of numbers up to 2^21: more is much all the same
+            const int all = __reduce_add_sync(0xffffffffu, (int)min(x, 1ll << 21));
+            if (lane == 0) atomicAdd(to, all);
+        };
+        if (warp * 32 < a.n) { sum(tiles, &work_s[0]); sum(stretches, &work_s[1]); }
+        if (warp * 32 < a.n_members) sum(blocks, &work_s[2]);
         __syncthreads();
         const float t = (float)work_s[0], grid = (float)gridDim.x, few = grid - (float)work_s[1];
         float ctas = grid * t / (t + (float)work_s[2] * (float)a.Hk / (SPLIT ? kRestOfTileSplit : kRestOfTile) + 1.f);
@@ -293,8 +298,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(AttendArgs a
             const int i = base + tid;
             long long mine = 0;
             if (i < a.n) {
-                int len, q0, nq;
-                lengths(i, len, q0, nq);
+                int len = own_len, q0 = own_q0, nq = own_nq;
+                if (!PREFIX || base > 0) lengths(i, len, q0, nq);
                 for (int row0 = 0; row0 < nq * a.G; row0 += kStretchRows) {
                     int st, wt, nt;
                     visible(len, nq, row0, min(row0 + kStretchRows, nq * a.G), st, wt, nt);
