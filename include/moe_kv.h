@@ -202,10 +202,15 @@ int moe_kv_shared_prefix(moe_kv_plan_t *plan, const int32_t *cu_group, int32_t n
                          const int32_t *kv_len, int32_t n_requests, const int32_t *block_table,
                          int32_t table_width, int32_t *shared_len, int32_t *start, void *cuda_stream);
 
+/* Whether later calls of moe_kv_attention_shared read a group's prefix once: AUTO decides by the sizes of the
+ * call (see there), NEVER and ALWAYS (where a request's rows are few enough) are for measurements.  Errors: INVALID_ARG. */
+enum { MOE_KV_SHARING_AUTO = 0, MOE_KV_SHARING_NEVER = 1, MOE_KV_SHARING_ALWAYS = 2 };
+int moe_kv_plan_set_sharing(moe_kv_plan_t *plan, int32_t sharing);
+
 /* Bytes of scratch that moe_kv_attention_shared wants for these arguments; 0 where it reads the keys request
  * by request (see there) and for bad arguments. */
 uint64_t moe_kv_shared_scratch_bytes(const moe_kv_plan_t *plan, int32_t n_tokens, int32_t n_requests, int32_t max_new,
-                                     int32_t max_group, int32_t table_width);
+                                     int32_t n_groups, int32_t max_group, int32_t table_width);
 
 /*
  * moe_kv_attention_shared: what moe_kv_attention computes without a window, with shared_len and start as
@@ -213,10 +218,10 @@ uint64_t moe_kv_shared_scratch_bytes(const moe_kv_plan_t *plan, int32_t n_tokens
  * members attend to the group's prefix together, each request's rows to what lies behind it, and both
  * results are joined in fp32 before the only rounding.
  * max_new, max_group: the largest number of new tokens of a request and of a group; they only choose the
- * kernels; 0 = unknown, which counts as n_tokens.  The call is moe_kv_attention's where sharing gains nothing: where max_new
- * times the query heads of a key/value head passes 32 (64 for head_dim above 128), for a request's own
- * rows share its keys then, and where the cache that n_requests tables of this width can hold is small (less
- * than 80 MB saved, 150 MB with at most 32 (64) rows a group).  scratch: 16-byte aligned device memory of
+ * kernels; 0 = unknown, which counts as n_tokens.  The call is moe_kv_attention's where sharing gains nothing: where
+ * max_new times the query heads of a key/value head passes 32 (64 for head_dim above 128), for a request's own
+ * rows share its keys then, and under MOE_KV_SHARING_AUTO where what n_requests tables of this width can hold,
+ * less what n_groups prefixes of that length cost, is below 80 MB.  scratch: 16-byte aligned device memory of
  * scratch_bytes >= moe_kv_shared_scratch_bytes, in use until the call's work is done.
  * A start outside 0..kv_len - new tokens sets BAD_INDEX; start and shared_len that do not belong together
  * give rows that no formula stands for.

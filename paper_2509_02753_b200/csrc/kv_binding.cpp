@@ -319,7 +319,7 @@ PyObject *attention_shared(PyObject *, PyObject *const *args, Py_ssize_t n) {
         const int32_t max_new = a.i32(), max_group = a.i32();
         const float scale = a.f32(), ks = a.f32(), vs = a.f32();
         const at::Tensor out = output_of(a.tensor_or_none(), q, p);
-        const int64_t bytes = g > 0 && r.n > 0 ? (int64_t)moe_kv_shared_scratch_bytes(p.handle, (int32_t)q.size(0), r.n, max_new, max_group, r.width) : 0;
+        const int64_t bytes = (int64_t)moe_kv_shared_scratch_bytes(p.handle, (int32_t)q.size(0), r.n, max_new, (int32_t)g, max_group, r.width);
         const at::Tensor scratch = bytes > 0 ? fresh({bytes}, at::kByte, p.device) : at::Tensor();
         const int rc = moe_kv_attention_shared(p.handle, &rows, (int32_t)q.size(0), r.cu, r.len, r.n, max_new, r.table, r.width, cache.data_ptr(), pages_of(cache, p),
                                                groups.data_ptr<int32_t>(), (int32_t)g, max_group, shared.data_ptr<int32_t>(), start.data_ptr<int32_t>(), scale, ks, vs,

@@ -22,6 +22,7 @@ struct moe_kv_plan {
     int32_t *prompt_arrived = nullptr;
     int32_t *status_host = nullptr;   // pinned
     int max_ctas = 0;
+    int32_t sharing = MOE_KV_SHARING_AUTO;
 };
 
 namespace {
@@ -31,7 +32,7 @@ constexpr int64_t kMaxRows = 1 << 30;         // max_tokens * n_heads
 constexpr int64_t kMaxContext = 1 << 30;      // tokens that a row of a block table may stand for
 constexpr int kPartRows = 32;         // rows of a piece, at most
 constexpr int kPassRows = 32;         // query rows of a pass over the keys in kv_attend.cu
-constexpr double kWorthMany = 80e6, kWorthFew = 150e6;          // bytes of the cache that reading prefixes once has to save
+constexpr double kWorth = 80e6;       // bytes of the cache that reading prefixes once has to save
 
 size_t elem_size(int dtype) { return dtype == MOE_BF16 ? 2 : 4; }
 bool aligned(const void *p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
@@ -103,23 +104,25 @@ AttendArgs attend_args(const moe_kv_plan *p, const moe_kv_rows_t *q, int32_t T, 
 int row_limit(const moe_kv_config_t &c) { return padded_width(c.head_dim) == 256 ? 2 * kPassRows : kPassRows; }
 
 // Whether a call's prefixes are read once for a group.  Not where a request has more rows than one pass over the keys serves
-// (its own rows share the reading already), nor where too little could be saved: what the tables can hold, less one member's
-// share of it, has to be worth two more launches.  In us, bf16 unless said, with up to 500 (64 requests) or 100 keys behind the
-// prefix, request by request / shared:
-//   64 requests, 32/8 heads of 128: 512 keys (75 MB) 25 / 26, 1024 (112 MB) 33 / 28, 4096 80 / 33, 8192 142 / 40, 32768 513 / 75
-//   16 of these: 2048 keys (40 MB) 19.0 / 20.1, 8192 (153 MB) 46 / 27
-//   32 of 16/2 heads of 256: 4096 keys (78 MB) 29 / 32, 16384 (305 MB) 78 / 43
-//   32 of 16/4 heads of 128 in fp32: 1024 keys (21 MB) 15.5 / 22.6, 4096 (78 MB) 31.3 / 29.8, 16384 94 / 42
-// and where a group's rows are few (kv_attend_body.cuh reads the prefix in passes of 32 rows, which hide less of its latency):
-//   8 of 32/8 heads of 128: 8192 keys (76 MB) 26.7 / 30.4, 32768 (303 MB) 75 / 44;   16 groups of 4: 1024 keys (83 MB) 30 / 39,
-//   4096 (309 MB) 78 / 70, 16384 264 / 194
-bool reads_prefixes_once(const moe_kv_plan *p, int32_t T, int32_t n, int32_t max_new, int32_t max_group, int32_t width) {
+// (its own rows share the reading already), nor where too little is saved: of what the tables can hold, the groups' share is read
+// all the same, at the rate of the kernel that reads it (single rows read 2.0 blocks of 16 keys a ns, a group's rows up to 16 at a
+// time 1.1, up to 32 0.8, tiles of 128 and 256 rows 0.6), and two more launches have to be worth it.  In us, request by request /
+// shared, with up to 500 (64 requests) or 100 keys behind the prefix; in MB what this rule finds saved:
+//   64 requests, 32/8 heads of 128: 512 keys (71 MB) 25 / 26, 1024 (106 MB) 33 / 28, 4096 80 / 33, 8192 142 / 39, 32768 513 / 74
+//   16 of these: 2048 keys (31 MB) 19 / 20, 8192 (121 MB) 46 / 26;   8 of these: 8192 (51 MB) 27 / 30, 16384 (103 MB) 43 / 37
+//   4 of these: 8192 (21 MB) 20 / 23, 32768 (83 MB) 44 / 32, 65536 78 / 41
+//   32 of 16/2 heads of 256: 4096 keys (70 MB) 29 / 32, 16384 79 / 43;   of 16/4 of 128 in fp32: 1024 (19 MB) 16 / 23, 16384 95 / 42
+//   64 in 16 groups, 32/8 heads of 128: 1024 keys (29 MB) 30 / 39, 4096 (108 MB) 78 / 70, 16384 265 / 194;  16/2 of 64: 16384 (27 MB) 57 / 66
+bool reads_prefixes_once(const moe_kv_plan *p, int32_t T, int32_t n, int32_t max_new, int32_t n_groups, int32_t max_group, int32_t width) {
     const moe_kv_config_t &c = p->cfg;
     const long long request = max_new > 0 && max_new < T ? max_new : T, group = max_group > 0 && max_group < T ? max_group : T, g = c.n_heads / c.n_kv_heads;
-    if (request * g > row_limit(c)) return false;
-    const double bytes = (double)n * width * c.page_size * c.n_kv_heads * block_bytes(padded_width(c.head_dim)) / kBlockTokens;
-    const double saved = bytes * (1.0 - (double)request / (double)(group > request ? group : request));
-    return saved >= (group * g > row_limit(c) ? kWorthMany : kWorthFew);
+    if (n_groups < 1 || p->sharing == MOE_KV_SHARING_NEVER || request * g > row_limit(c)) return false;
+    if (p->sharing == MOE_KV_SHARING_ALWAYS) return true;
+    const int w = padded_width(c.head_dim);
+    const long long rows = group * g, tile = w == 256 || (w == 128 && c.dtype == MOE_F32) ? 128 : 256;
+    const double passes = rows > row_limit(c) ? 3.3 * (double)((rows + tile - 1) / tile) : w == 256 && rows > 8 ? 1.8 * (double)((rows + 15) / 16) : rows > 16 ? 2.6 : rows > 8 ? 1.8 : 1.0;
+    const double bytes = (double)n * width * c.page_size * c.n_kv_heads * block_bytes(w) / kBlockTokens;
+    return bytes * (1.0 - passes * n_groups / n) >= kWorth;
 }
 
 uint64_t shared_rows_bytes(const moe_kv_plan *p, int32_t T) { return (uint64_t)T * p->cfg.n_heads * padded_width(p->cfg.head_dim) * sizeof(float); }
@@ -338,8 +341,15 @@ int moe_kv_shared_prefix(moe_kv_plan_t *p, const int32_t *cu_group, int32_t n_gr
     return done(launch_prefix(a, p->sm_count, (cudaStream_t)stream, &p->launches));
 }
 
-uint64_t moe_kv_shared_scratch_bytes(const moe_kv_plan_t *p, int32_t n_tokens, int32_t n, int32_t max_new, int32_t max_group, int32_t width) {
-    if (!p || n_tokens < 1 || n < 1 || max_new < 0 || max_group < 0 || width < 1 || !reads_prefixes_once(p, n_tokens, n, max_new, max_group, width)) return 0;
+int moe_kv_plan_set_sharing(moe_kv_plan_t *p, int32_t sharing) {
+    if (!p || sharing < MOE_KV_SHARING_AUTO || sharing > MOE_KV_SHARING_ALWAYS) return MOE_ERR_INVALID_ARG;
+    p->sharing = sharing;
+    return MOE_OK;
+}
+
+uint64_t moe_kv_shared_scratch_bytes(const moe_kv_plan_t *p, int32_t n_tokens, int32_t n, int32_t max_new, int32_t n_groups, int32_t max_group, int32_t width) {
+    if (!p || n_tokens < 1 || n < 1 || max_new < 0 || n_groups < 1 || max_group < 0 || width < 1 ||
+        !reads_prefixes_once(p, n_tokens, n, max_new, n_groups, max_group, width)) return 0;
     return 2 * shared_rows_bytes(p, n_tokens) + (uint64_t)n_tokens * p->cfg.n_heads * (sizeof(int4) + 2 * sizeof(float2));
 }
 
@@ -356,9 +366,9 @@ int moe_kv_attention_shared(moe_kv_plan_t *p, const moe_kv_rows_t *q, int32_t T,
     if (!cu_new || !kv_len || !out || (width > 0 && !block_table) || (n_pages > 0 && !cache)) return MOE_ERR_INVALID_ARG;
     if (n_groups > 0 && (!cu_group || !shared_len || !start)) return MOE_ERR_INVALID_ARG;
     if (!aligned(cache, 16) || !aligned(out, 16) || !aligned(scratch, 16) || !words(cu_new, kv_len, block_table, cu_group, shared_len, start)) return MOE_ERR_ALIGN;
-    if (n_groups == 0 || !reads_prefixes_once(p, T, n, max_new, max_group, width))
+    if (width == 0 || !reads_prefixes_once(p, T, n, max_new, n_groups, max_group, width))
         return moe_kv_attention(p, q, T, cu_new, kv_len, n, max_new, block_table, width, cache, n_pages, softmax_scale, k_scale, v_scale, 0, 0, out, stream);
-    if (!scratch || scratch_bytes < moe_kv_shared_scratch_bytes(p, T, n, max_new, max_group, width)) return MOE_ERR_WORKSPACE;
+    if (!scratch || scratch_bytes < moe_kv_shared_scratch_bytes(p, T, n, max_new, n_groups, max_group, width)) return MOE_ERR_WORKSPACE;
     AttendArgs rest = attend_args(p, q, T, cu_new, kv_len, n, max_new, block_table, width, cache, n_pages, softmax_scale, k_scale, v_scale, out);
     rest.max_new = max_new > 0 && max_new < T ? max_new : T;
     rest.start = start;

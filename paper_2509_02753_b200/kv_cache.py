@@ -40,12 +40,13 @@ from .binding import MoEError  # noqa: F401  (what the calls below raise)
 
 STATUS_TIMEOUT, STATUS_BAD_INDEX, STATUS_NO_PAGES, STATUS_NONFINITE = 1, 2, 4, 8
 LAYOUTS = {"half": 0, "pairs": 1}
+SHARING = {"auto": 0, "never": 1, "always": 2}
 SCALINGS = {"plain": 0, "linear": 1, "base": 2, "parts": 3, "bands": 4}
 
 EXPORTS = (
     "moe_kv_plan_create", "moe_kv_plan_destroy", "moe_kv_plan_workspace_bytes", "moe_kv_plan_launch_count", "moe_kv_page_bytes",
     "moe_kv_device_status", "moe_kv_tables", "moe_rope_table", "moe_rope", "moe_kv_append", "moe_kv_read", "moe_kv_attention",
-    "moe_kv_shared_prefix", "moe_kv_shared_scratch_bytes", "moe_kv_attention_shared", "moe_kv_summary_bytes", "moe_kv_summarise",
+    "moe_kv_shared_prefix", "moe_kv_plan_set_sharing", "moe_kv_shared_scratch_bytes", "moe_kv_attention_shared", "moe_kv_summary_bytes", "moe_kv_summarise",
     "moe_kv_read_summaries", "moe_kv_select", "moe_kv_attention_selected",
 )
 
@@ -88,7 +89,8 @@ def load_library() -> ctypes.CDLL:
     lib.moe_kv_read.argtypes = [vp, vp, i32, vp, i32, f32, f32, vp, vp, vp]
     lib.moe_kv_attention.argtypes = [vp, rows, i32, vp, vp, i32, i32, vp, i32, vp, i32, f32, f32, f32, i32, i32, vp, vp]
     lib.moe_kv_shared_prefix.argtypes = [vp, vp, i32, vp, vp, i32, vp, i32, vp, vp, vp]
-    lib.moe_kv_shared_scratch_bytes.argtypes = [vp, i32, i32, i32, i32, i32]
+    lib.moe_kv_plan_set_sharing.argtypes = [vp, i32]
+    lib.moe_kv_shared_scratch_bytes.argtypes = [vp, i32, i32, i32, i32, i32, i32]
     lib.moe_kv_attention_shared.argtypes = [vp, rows, i32, vp, vp, i32, i32, vp, i32, vp, i32, vp, i32, i32, vp, vp, f32, f32, f32, vp, u64, vp, vp]
     lib.moe_kv_summary_bytes.argtypes = [P(moe_kv_config_t)]
     lib.moe_kv_summarise.argtypes = [vp, vp, vp, i32, i32, vp, i32, vp, i32, vp, vp]
@@ -243,6 +245,10 @@ class KVPlan:
         """(shared_len of each group, start of each request): how many leading keys the members of groups of consecutive
         requests have in common by their rows of the block table (``moe_kv_shared_prefix``)."""
         return self._call("moe_kv_shared_prefix", self._native.shared_prefix, self._plan, cu_group, cu_new, kv_len, block_table, stream=stream)[1:]
+
+    def set_sharing(self, sharing: str) -> None:
+        """Whether ``attention_shared`` reads a group's prefix once: "auto" where it gains, "never", "always" where it can (``moe_kv_plan_set_sharing``)."""
+        B._check("moe_kv_plan_set_sharing", self._lib.moe_kv_plan_set_sharing(self.handle, SHARING[sharing]))
 
     def attention_shared(self, q: torch.Tensor, cu_new: torch.Tensor, kv_len: torch.Tensor, block_table: torch.Tensor, cache: torch.Tensor,
                          cu_group: torch.Tensor, shared_len: torch.Tensor, start: torch.Tensor, *, max_new: int = 0, max_group: int = 0,

@@ -100,7 +100,7 @@ def test_summary_bytes(dim, kv, want):
 
 def test_null_arguments():
     lib = K.load_library()
-    assert lib.moe_kv_summary_bytes(None) == 0 and lib.moe_kv_shared_scratch_bytes(None, 1, 1, 1, 1, 1) == 0
+    assert lib.moe_kv_summary_bytes(None) == 0 and lib.moe_kv_shared_scratch_bytes(None, 1, 1, 1, 1, 1, 1) == 0
     assert lib.moe_kv_shared_prefix(None, None, 0, None, None, 0, None, 0, None, None, None) == -1
     assert lib.moe_kv_attention_shared(None, None, 0, None, None, 0, 0, None, 0, None, 0, None, 0, 0, None, None, 1.0, 1.0, 1.0, None, 0, None, None) == -1
     assert lib.moe_kv_summarise(None, None, None, 0, 0, None, 0, None, 0, None, None) == -1
@@ -200,19 +200,10 @@ def test_what_is_not_shared():
     check_prefix([0, 3, 2, 4], [1, 1, 1, 1], [96] * 4, table, 16, K.STATUS_BAD_INDEX, ([0, 0, 0], [0, 0, 0, 0]))
 
 
-def wide(n, kv, dim, page, share):
-    """Columns of a table with which sharing counts as worth it, `share` being what one member has of a group's tokens."""
-    return int(150e6 / (1 - share) / (n * kv * ref.block_bytes(dim) / 16) / page) + 1
-
-
-def shared_case(seed, lens, new, heads, kv, dim, page, dtype, groups, shared, max_new=None, max_group=None, columns=None, **more):
-    """Tables so wide that the prefixes are read once, unless `columns` says otherwise."""
-    if columns is None:
-        members = max([0] + [b - a for a, b in zip(groups, groups[1:])])
-        columns = wide(len(lens), kv, dim, page, max(new) / max(sum(new[a: b]) for a, b in zip(groups, groups[1:])) if members > 1 else 0.5)
-    more["columns"] = columns
+def shared_case(seed, lens, new, heads, kv, dim, page, dtype, groups, shared, max_new=None, max_group=None, sharing="always", **more):
     b = Batch(seed, lens, new, heads, kv, dim, page, dtype, groups, shared, **more)
     with b.plan() as plan:
+        plan.set_sharing(sharing)
         g = i32(groups)
         length, start = plan.shared_prefix(g, *b.args[1:])
         assert (length.tolist(), start.tolist()) == plain.shared_prefix(groups, b.cu, lens, b.table, page)
@@ -284,14 +275,16 @@ def test_hints_choose_kernels_not_results(dtype):
     lens, new, groups = [100, 90, 70, 81, 200, 120], [1, 2, 1, 1, 3, 1], [0, 4, 6]
     for max_new, max_group in ((3, 0), (1, 1), (0, 0), (9, 2), (3, 100), (1, 2), (3, 5)):
         shared_case(11, lens, new, 4, 2, 64, 16, dtype, groups, [4, 7], max_new=max_new, max_group=max_group)
-        shared_case(11, lens, new, 4, 2, 64, 16, dtype, groups, [4, 7], max_new=max_new, max_group=max_group, columns=0)
+        shared_case(11, lens, new, 4, 2, 64, 16, dtype, groups, [4, 7], max_new=max_new, max_group=max_group, sharing="auto")
 
 
 @gpu
 def test_requests_of_many_rows_and_small_batches_read_their_keys_themselves():
-    assert shared_case(12, [100, 90, 95], [1, 1, 1], 4, 2, 64, 16, BF16, [0, 3], [3], columns=40) == 1
-    assert shared_case(12, [100, 90], [40, 1], 4, 2, 64, 16, BF16, [0, 2], [3], columns=40) == 1          # a prompt and a token
-    assert shared_case(12, [100, 100], [40, 40], 4, 2, 64, 16, BF16, [0, 2], [3], columns=40) == 1
+    assert shared_case(12, [100, 90, 95], [1, 1, 1], 4, 2, 64, 16, BF16, [0, 3], [3], sharing="auto") == 1
+    assert shared_case(12, [100, 90, 95], [1, 1, 1], 4, 2, 64, 16, BF16, [0, 3], [3], sharing="never", columns=50000) == 1
+    assert shared_case(12, [100, 90, 95], [1, 1, 1], 4, 2, 64, 16, BF16, [0, 3], [3], sharing="auto", columns=50000) == 3
+    assert shared_case(12, [100, 90], [40, 1], 4, 2, 64, 16, BF16, [0, 2], [3]) == 1          # a prompt and a token
+    assert shared_case(12, [100, 100], [40, 40], 4, 2, 64, 16, BF16, [0, 2], [3]) == 1
 
 
 @gpu
@@ -310,8 +303,9 @@ def test_peaked_weights_on_either_side(dtype):
 
 @gpu
 def test_starts_that_are_none():
-    b = Batch(15, [40, 50], [1, 1], 4, 2, 64, 16, F32, [0, 2], [2], columns=wide(2, 2, 64, 16, 0.5))
+    b = Batch(15, [40, 50], [1, 1], 4, 2, 64, 16, F32, [0, 2], [2])
     with b.plan() as plan:
+        plan.set_sharing("always")
         for start in ([32, 50], [-1, 32], [1 << 30, 32]):
             plan.attention_shared(*b.args, b.pages, i32([0, 2]), i32([32]), i32(start), max_new=1, max_group=2, k_scale=KS, v_scale=VS)
             assert plan.device_status() == (-8, K.STATUS_BAD_INDEX)
@@ -582,11 +576,12 @@ def test_selected_with_more_new_tokens_than_keys():
 def test_rows_in_front_of_the_first_request(dtype):
     """cu_new begins above 0: rows, lists and outputs in front stay as they are."""
     lens, new, front = [100, 40, 90], [1, 3, 20], 5
-    b = Batch(9, lens, new, 4, 2, 64, 16, dtype, [0, 3], [1], columns=wide(3, 2, 64, 16, 1 / 3))
+    b = Batch(9, lens, new, 4, 2, 64, 16, dtype, [0, 3], [1])
     cu = b.args[1] + front
     q = torch.cat([torch.full_like(b.q[:front], math.nan), b.q])
     more = dict(k_scale=KS, v_scale=VS)
     with plan_for(4, 2, 64, 16, dtype, requests=3, tokens=64) as plan:
+        plan.set_sharing("always")
         summaries, again = (plan.new_summaries(len(b.cache)) for _ in range(2))
         plan.summarise(*b.args[1:], b.pages, summaries, 24)
         plan.summarise(cu, *b.args[2:], b.pages, again, 24 + front)
@@ -614,12 +609,13 @@ def test_rows_in_front_of_the_first_request(dtype):
 def test_rows_that_are_not_finite_stay_alone(many, dtype):
     """In a group's prefix (also as tiles of 128 rows) and over listed pages."""
     n = 20 if many else 3
-    b = Batch(10, [70 + i for i in range(n)], [1] * n, 4, 2, 64, 16, dtype, [0, n], [4], columns=wide(n, 2, 64, 16, 1 / n))
+    b = Batch(10, [70 + i for i in range(n)], [1] * n, 4, 2, 64, 16, dtype, [0, n], [4])
     q = b.q.clone()
     q[0, 1, 3], q[1, 2, 5], q[2, 0, 0] = math.nan, math.inf, -math.inf
     fine = torch.ones(q.shape[:2], dtype=torch.bool)
     fine[0, 1] = fine[1, 2] = fine[2, 0] = False
     with b.plan() as plan:
+        plan.set_sharing("always")
         groups = i32([0, n])
         shared, start = plan.shared_prefix(groups, *b.args[1:])
         lists = i32(np.tile(np.array([4, 0, 2]), (n, 2, 1)))
@@ -639,7 +635,7 @@ def steps(plan, kv, heads, dim, page, rng):
     n, prompt = 3, 5 * page
     cache, summaries = plan.new_cache(40), plan.new_summaries(40)
     free = torch.randperm(40, dtype=torch.int32).cuda()
-    table = torch.full((n, wide(n, kv, dim, page, 1 / 3)), -1, dtype=torch.int32, device="cuda")
+    table = torch.full((n, 12), -1, dtype=torch.int32, device="cuda")
     lens = torch.zeros(n, dtype=torch.int32, device="cuda")
     for new in ([prompt, 0, 0], [1, 1, 1], [1, 1, 1], [page, 3, 1], [1, 1, 1]):
         kv_len, cu, pos, slot, taken = plan.tables(lens, i32(new), free, table, sum(new))
@@ -661,6 +657,7 @@ def test_steps_of_a_served_layer(page, dtype):
     """tables, append, summarise, then both kinds of attention: behind a shared prefix as without; over all pages as without a selection."""
     rng = np.random.default_rng(page)
     with plan_for(4, 2, 64, page, dtype) as plan:
+        plan.set_sharing("always")
         for q, cu, lens, table, cache, summaries, max_new in steps(plan, 2, 4, 64, page, rng):
             more = dict(k_scale=KS, v_scale=VS)
             groups = i32([0, 3])
@@ -709,9 +706,11 @@ def test_no_page_scores_above_its_bound():
 @gpu
 def test_calls_in_a_graph_and_on_another_stream():
     """Captured once, replayed on other lengths and tables; two graphs of one plan in turn."""
-    b, other = (Batch(s, lens, [1, 1, 1], 4, 2, 64, 16, BF16, [0, 3], [4], columns=wide(3, 2, 64, 16, 1 / 3)) for s, lens in ((1, [100, 90, 80]), (2, [70, 130, 66])))
+    b, other = (Batch(s, lens, [1, 1, 1], 4, 2, 64, 16, BF16, [0, 3], [4], columns=12) for s, lens in ((1, [100, 90, 80]), (2, [70, 130, 66])))
     groups = i32([0, 3])
     with b.plan() as plan:
+        plan.set_sharing("always")
+
         def calls(q, cu, lens, table, cache, summaries):
             plan.summarise(cu, lens, table, cache, summaries, 3)
             shared, start = plan.shared_prefix(groups, cu, lens, table)
@@ -785,13 +784,14 @@ def test_offsets_past_32_bits():
     dim, page, kv = 256, 128, 8
     per_page = kv * (page // 16) * ref.block_bytes(dim)
     n_pages = (1 << 32) // per_page + 20
-    b = Batch(9, [300, 270], [1, 1], 8, kv, dim, page, BF16, [0, 2], [2], columns=wide(2, kv, dim, page, 0.5))
+    b = Batch(9, [300, 270], [1, 1], 8, kv, dim, page, BF16, [0, 2], [2])
     far = torch.zeros((n_pages, *b.cache.shape[1:]), dtype=torch.uint8, device="cuda")
     shift = n_pages - len(b.cache)
     far[shift:].copy_(b.pages)
     near, table = i32(b.table), i32(np.where(b.table < len(b.cache), b.table + shift, b.table))
     q, cu, lens = b.args[:3]
     with b.plan() as plan:
+        plan.set_sharing("always")
         outs = []
         for tb, cache in ((near, b.pages), (table, far)):
             summaries = plan.new_summaries(len(cache))
@@ -813,22 +813,22 @@ def _refused(call, status):
 
 @gpu
 def test_refusals():
-    b = Batch(1, [40, 50], [1, 1], 4, 2, 64, 16, F32, [0, 2], [2], columns=wide(2, 2, 64, 16, 0.5))
+    b = Batch(1, [40, 50], [1, 1], 4, 2, 64, 16, F32, [0, 2], [2])
     q, cu, lens, table = b.args
     with b.plan() as plan, plan_for(8, 2, 64, 16, F32, requests=2, tokens=2) as wider:
         summaries = plan.new_summaries(len(b.cache))
         g = i32([0, 2])
         shared, start = plan.shared_prefix(g, cu, lens, table)
         ok = (q, cu, lens, table, b.pages, g, shared, start)
-        few = table[:, :4].contiguous()
-        picked = plan.select(q, cu, lens, few, summaries, n_select=2)
+        plan.set_sharing("always")
+        picked = plan.select(q, cu, lens, table, summaries, n_select=2)
         for bad in (dict(k_scale=0.0), dict(v_scale=-1.0), dict(v_scale=math.inf), dict(softmax_scale=math.nan), dict(max_new=-1)):
             _refused(lambda: plan.attention_shared(*ok, **bad), -1)
             if "max_new" not in bad:
                 _refused(lambda: plan.attention_selected(*ok[:5], picked, **bad), -1)
         _refused(lambda: plan.attention_shared(*ok, max_group=-1), -1)
         for n_select, first, last in ((1, 1, 1), (4, -1, 1), (4, 1, 0), (4, 3, 2), (4, (1 << 31) - 1, 1)):
-            _refused(lambda: plan.select(q, cu, lens, few, summaries, n_select=n_select, first=first, last=last), -1)
+            _refused(lambda: plan.select(q, cu, lens, table, summaries, n_select=n_select, first=first, last=last), -1)
         _refused(lambda: plan.read_summaries(summaries, i32([0]), k_scale=0.0), -1)
         _refused(lambda: plan.summarise(cu, lens, table, b.pages, summaries, -1), -1)
         _refused(lambda: plan.summarise(cu, lens, table, b.pages, summaries, plan.cfg.max_tokens + 1), -1)
@@ -839,8 +839,8 @@ def test_refusals():
                      lambda: wider.attention_shared(*ok), lambda: plan.attention_shared(*ok[:3], i32(np.zeros((3, 4))), *ok[4:]), lambda: plan.attention_shared(*ok[:5], i32([]), shared, start),
                      lambda: plan.shared_prefix(i32([]), cu, lens, table), lambda: plan.shared_prefix(g.long(), cu, lens, table), lambda: plan.shared_prefix(g.cpu(), cu, lens, table),
                      lambda: plan.summarise(cu, lens, table, b.pages, plan.new_summaries(1), 2), lambda: plan.summarise(cu, lens, table, b.pages, summaries.int(), 2),
-                     lambda: plan.read_summaries(summaries[:, :1], i32([0])), lambda: plan.select(q, cu, lens, few, summaries, n_select=0),
-                     lambda: plan.select(q, cu, lens, few, summaries, n_select=2, out=picked[:1]), lambda: plan.attention_selected(*ok[:5], picked[:1]),
+                     lambda: plan.read_summaries(summaries[:, :1], i32([0])), lambda: plan.select(q, cu, lens, table, summaries, n_select=0),
+                     lambda: plan.select(q, cu, lens, table, summaries, n_select=2, out=picked[:1]), lambda: plan.attention_selected(*ok[:5], picked[:1]),
                      lambda: plan.attention_selected(*ok[:5], picked.long()), lambda: plan.attention_selected(*ok[:5], picked[:, :1]),
                      lambda: plan.attention_selected(*ok[:5], picked[:, :, :0])):
             with pytest.raises((AssertionError, B.MoEError)):
@@ -850,12 +850,14 @@ def test_refusals():
         rows = K.moe_kv_rows_t(q.data_ptr(), q.stride(0), q.stride(1))
         out, scratch = torch.empty_like(q), torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
         width = table.shape[1]
-        need = lib.moe_kv_shared_scratch_bytes(h, 2, 2, 1, 2, width)
-        assert need == 2 * 4 * (2 * 64 * 4 + 32) and lib.moe_kv_shared_scratch_bytes(h, 2, 2, 1, 0, width) == need
-        for none in ((2, 2, 1, 2, 100), (2, 2, 1, 1, width), (2, 2, 0, 0, width), (100, 2, 17, 90, width), (0, 2, 1, 2, width), (2, 0, 1, 2, width), (2, 2, -1, 2, width),
-                     (2, 2, 1, -1, width), (2, 2, 1, 2, 0)):
+        need = lib.moe_kv_shared_scratch_bytes(h, 2, 2, 1, 1, 2, width)
+        assert need == 2 * 4 * (2 * 64 * 4 + 32) and lib.moe_kv_shared_scratch_bytes(h, 2, 2, 1, 1, 0, width) == need
+        for none in ((100, 2, 17, 1, 90, width), (0, 2, 1, 1, 2, width), (2, 0, 1, 1, 2, width), (2, 2, -1, 1, 2, width), (2, 2, 1, 0, 2, width), (2, 2, 1, 1, -1, width), (2, 2, 1, 1, 2, 0)):
             assert lib.moe_kv_shared_scratch_bytes(h, *none) == 0
-        assert lib.moe_kv_shared_scratch_bytes(wider.handle, 100, 2, 9, 18, width) == 0
+        assert lib.moe_kv_shared_scratch_bytes(wider.handle, 100, 2, 9, 1, 18, width) == 0
+        for sharing, wide in ((1, 0), (0, 0), (2, 1)):
+            assert lib.moe_kv_plan_set_sharing(h, sharing) == 0 and (lib.moe_kv_shared_scratch_bytes(h, 2, 2, 1, 1, 2, width) > 0) == bool(wide)
+        assert lib.moe_kv_plan_set_sharing(h, 3) == -1 and lib.moe_kv_plan_set_sharing(h, -1) == -1 and lib.moe_kv_plan_set_sharing(None, 0) == -1
 
         def shared_call(at=0, size=need, group=g.data_ptr(), tab=table.data_ptr(), where=scratch.data_ptr()):
             return lib.moe_kv_attention_shared(h, ctypes.byref(rows), 2, cu.data_ptr(), lens.data_ptr(), 2, 1, tab, table.shape[1], b.pages.data_ptr(), len(b.cache), group, 1, 2,
@@ -870,7 +872,7 @@ def test_refusals():
         assert start.tolist() == [0, 0]
         assert lib.moe_kv_summarise(h, cu.data_ptr(), lens.data_ptr(), 2, 2, table.data_ptr(), table.shape[1], b.pages.data_ptr(), len(b.cache), summaries.data_ptr() + 8, None) == -3
         assert lib.moe_kv_read_summaries(h, summaries.data_ptr(), len(b.cache), cu.data_ptr(), 1, 1.0, scratch.data_ptr() + 4, scratch.data_ptr(), None) == -3
-        assert lib.moe_kv_select(h, ctypes.byref(rows), 2, cu.data_ptr(), lens.data_ptr(), 2, 1, few.data_ptr(), few.shape[1], summaries.data_ptr(), len(b.cache), 2, 1, 1,
+        assert lib.moe_kv_select(h, ctypes.byref(rows), 2, cu.data_ptr(), lens.data_ptr(), 2, 1, table.data_ptr(), width, summaries.data_ptr(), len(b.cache), 2, 1, 1,
                                  scratch.data_ptr() + 2, None) == -3
         assert lib.moe_kv_attention_selected(h, ctypes.byref(rows), 2, cu.data_ptr(), lens.data_ptr(), 2, table.data_ptr(), table.shape[1], b.pages.data_ptr(), len(b.cache),
                                              picked.data_ptr() + 1, 2, 0.125, 1.0, 1.0, out.data_ptr(), None) == -3
