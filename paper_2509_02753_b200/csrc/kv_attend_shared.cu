@@ -4,18 +4,18 @@
 //   o = v_scale * sum_p 2^(m_p - M) s_p / sum_p 2^(m_p - M) l_p,   M = max_p m_p
 //
 // over the pieces p of a row, each with its sums s_p, reference m_p and denominator l_p.  Bound by latency: a row of 128
-// dimensions has up to 20 pieces of 512 bytes, all of which lie in the L2.  A warp has a row and asks for eight pieces at a time.
+// dimensions has up to 20 pieces of 512 bytes, all of which lie in the L2.  A warp has a row and asks for 16 pieces (8 of 256 dimensions) at a time.
 #include "kv_attend_body.cuh"
 
 namespace lexi {
 namespace kv {
 namespace {
 
-constexpr int kJoinWarps = 8, kAtOnce = 8;
+constexpr int kJoinWarps = 8;
 
 template <typename T, int W>
 __global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(AttendArgs a) {
-    constexpr int kDims = W / 32;
+    constexpr int kDims = W / 32, kAtOnce = W == 256 ? 8 : 16;
     const int lane = threadIdx.x & 31;
     const long long at_row = (long long)blockIdx.x * kJoinWarps + (threadIdx.x >> 5);
     pdl_trigger();
@@ -57,7 +57,11 @@ __global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(AttendArgs a) {
         float x[kAtOnce][kDims];
 #pragma unroll
         for (int y = 0; y < kAtOnce; ++y) {
-            const int p = min(p0 + y, pieces - 1), b = a.piece_results == 2 ? p >> 1 : p;
+            ml[y] = make_float2(kFloor, 0.f);
+#pragma unroll
+            for (int e = 0; e < kDims; ++e) x[y][e] = 0.f;
+            const int p = p0 + y, b = a.piece_results == 2 ? p >> 1 : p;
+            if (p >= pieces) continue;
             const int64_t at_piece = (int64_t)((where.x + b) * 2 + (b == 0)) * a.piece_rows + (p - b * a.piece_results) * a.result_rows + where.z;
             ml[y] = __ldcg(one ? &a.o_ml[at_row] : &a.prompt_ml[at_piece]);
             numbers(one ? a.o_part + at_row * W : a.prompt_part + at_piece * W, x[y]);
@@ -71,7 +75,6 @@ __global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(AttendArgs a) {
         for (int e = 0; e < kDims; ++e) v[e] *= old;
 #pragma unroll
         for (int y = 0; y < kAtOnce; ++y) {
-            if (p0 + y >= pieces) continue;
             const float k = ml[y].x == to ? 1.f : ex2(ml[y].x - to);
             sum += ml[y].y * k;
 #pragma unroll
