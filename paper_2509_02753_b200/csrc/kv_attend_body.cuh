@@ -837,7 +837,7 @@ __global__ void __launch_bounds__(kThreads, MINB) attend_rows_kernel(AttendArgs 
             }
         }
         if (kPrefix && !whole) {
-            // Rest joins them: where the row's pieces are
+            // join_kernel adds them: where the row's pieces are
             if (tid < S::kRows) {
                 part_ml[tid] = row_ml[tid];
                 const int row = row0 + tid;

@@ -25,13 +25,13 @@
 //
 // Work split: as in kv_attend.cu, the key tiles of all stretches stand in one line cut evenly over the CTAs, which also
 // serves few rows over a long context; a stretch in several pieces is joined by its last CTA in the order of the keys.
-// PREFIX: every stretch in pieces of as many tiles, which stand in the line; there are few stretches and each piece pays its beginning
-// (45 requests in 4 groups, fp32: 41 us where cuts fell in the middle of two stretches, 46 where beginnings filled shares).
 //
 // PREFIX: "requests" are groups of requests and "keys" their shared prefix, which all rows of a group see whole (kv_prompt.cu
 // builds the one, kv_prompt_prefix.cu the other).  What comes out is sums, references and denominators as they are, for
-// kv_attend_body.cuh's Rest, which joins the pieces of a stretch: a stretch of 256 rows on 8192 keys has 19 pieces, 2.4 MB, which its
-// last CTA took most of 67 us to add while all others were done; Rest's CTAs have a few rows each.
+// kv_attend_shared.cu's join_kernel: a stretch of 256 rows on 8192 keys has up to 19 pieces, 2.4 MB, which its last CTA took most of
+// 67 us to add while all others were done; the join has a warp for each row.  Every stretch is cut in pieces of as many tiles,
+// which stand in the line one for a CTA: there are few stretches, and each piece pays its beginning (where beginnings counted in the
+// line as above, shares of their size held nothing else).
 #pragma once
 
 #include <float.h>
@@ -55,7 +55,7 @@ constexpr float kTop = 14.f;                     // the largest weight is 2^kTop
 // there: 333 to 700 tokens of 15/5 heads 52 -> 49 us, 64 tokens on 16000 keys of 16/4 heads 83 -> 77)
 constexpr int kEntryTiles = 3, kEntryAlternate = 5;
 // PREFIX: blocks of 16 keys (a stretch's beginning counts 16 more) that kv_attend_body.cuh's Rest reads in an SM's time for a
-// tile.  In us, with 14 / 22 / 30 / 47 / 70: 64 requests of up to 500 keys behind 2048 40 / 34 / 32 / 30 / 31, behind 8192
+// tile (SPLIT: fp32).  In us, with 14 / 22 / 30 / 47 / 70: 64 requests of up to 500 keys behind 2048 40 / 34 / 32 / 30 / 31, behind 8192
 // 50 / 42 / 41 / 42 / 41, behind 16384 58 / 55 / 54 / 51 / 56; 45 requests in 4 groups, fp32, 42 / 41 / 45 / 47 / 47
 constexpr int kRestOfTile = 36, kRestOfTileSplit = 22, kRestEntry = 16;
 

@@ -761,6 +761,30 @@ def test_calls_in_a_graph_and_on_another_stream():
 
 
 @gpu
+def test_clusters_in_a_graph():
+    """Lists that are cut into the CTAs of clusters (120 blocks for each of 2 heads), captured and replayed on other lists and numbers of keys."""
+    b = Batch(21, [2000], [1], 4, 2, 64, 64, BF16)
+    lens, lists = b.args[2].clone(), i32(np.tile(np.arange(30), (1, 2, 1)))
+    with b.plan() as plan:
+        def call():
+            return plan.attention_selected(b.q, b.args[1], lens, b.args[3], b.pages, lists, k_scale=KS, v_scale=VS)
+        call()
+        torch.cuda.synchronize()
+        stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+        stream.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(stream), torch.cuda.graph(graph, stream=stream):
+            got = call()
+        for n, order in ((2000, np.arange(30)[::-1]), (700, np.arange(30)), (1, np.arange(30)), (1999, np.full(30, 7))):
+            lens.fill_(n)
+            lists.copy_(i32(np.tile(order, (1, 2, 1))))
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(got, call())
+            b.near(got, *plain.attention_selected(host(b.q), b.cu, [n], b.table, b.cache, lists.cpu().numpy(), 64, 0.125, float(np.float32(KS)), float(np.float32(VS))))
+        assert plan.device_status() == (0, 0)
+
+
+@gpu
 def test_calls_of_nothing():
     with plan_for() as plan:
         cache, summaries = plan.new_cache(2), plan.new_summaries(2)
