@@ -12,7 +12,7 @@ namespace lexi {
 namespace kv {
 namespace {
 
-constexpr int kWarps = 8, kThreads = 32 * kWarps;
+constexpr int kFewWarps = 8, kManyWarps = 32;
 constexpr int kMaxCluster = 8;
 constexpr int kColumns = 256;          // of a member, a warp's step
 
@@ -25,9 +25,11 @@ __device__ __forceinline__ void st_cta0(const int *p, int v) {
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
-__global__ void __launch_bounds__(kThreads) prefix_kernel(PrefixArgs a, int cluster) {
+template <int WARPS>
+__global__ void __launch_bounds__(32 * WARPS) prefix_kernel(PrefixArgs a, int cluster) {
     __shared__ int least_s, of_cta[kMaxCluster];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    constexpr int threads = 32 * WARPS;
     const int rank = cluster > 1 ? (int)cluster_rank() : 0, g = blockIdx.x / cluster;
     if (cluster > 1) cluster_arrive();
     pdl_trigger();
@@ -36,7 +38,7 @@ __global__ void __launch_bounds__(kThreads) prefix_kernel(PrefixArgs a, int clus
 
     // groups that are not consecutive runs of requests: nothing is shared
     int good = 1;
-    for (int x = a.n_groups > 0 ? tid : 1; x <= a.n_groups; x += kThreads) {
+    for (int x = a.n_groups > 0 ? tid : 1; x <= a.n_groups; x += threads) {
         const int at = a.groups[x];
         good &= at >= 0 && at <= a.n && (x == 0 || a.groups[x - 1] <= at);
     }
@@ -45,7 +47,7 @@ __global__ void __launch_bounds__(kThreads) prefix_kernel(PrefixArgs a, int clus
     int pages = 0;
     if (r1 - r0 > 1) {
         int full = a.width;
-        for (int i = r0 + tid; i < r1; i += kThreads) {
+        for (int i = r0 + tid; i < r1; i += threads) {
             const int len = a.kv_len[i], q0 = a.cu[i], nq = (int)min((long long)INT32_MAX, (long long)a.cu[i + 1] - q0);
             const bool bad = len < 0 || nq < 0 || len > ((int64_t)a.width << a.page_shift);
             if (bad) atomicOr(a.status, MOE_KV_STATUS_BAD_INDEX);
@@ -56,9 +58,9 @@ __global__ void __launch_bounds__(kThreads) prefix_kernel(PrefixArgs a, int clus
         __syncthreads();
         const int32_t *lead = a.table + (int64_t)r0 * a.width;
         const int others = r1 - r0 - 1;
-        int member = rank * kWarps + warp, col = 0;
+        int member = rank * WARPS + warp, col = 0;
         auto on = [&](int by) { for (member += by; member >= others; member -= others) col += kColumns; };
-        for (on(0); col < *reinterpret_cast<volatile int *>(&least_s); on(cluster * kWarps)) {
+        for (on(0); col < *reinterpret_cast<volatile int *>(&least_s); on(cluster * WARPS)) {
             const int most = *reinterpret_cast<volatile int *>(&least_s);
             const int32_t *row = a.table + (int64_t)(r0 + 1 + member) * a.width;
             int x[kColumns / 32], y[kColumns / 32];
@@ -89,21 +91,21 @@ __global__ void __launch_bounds__(kThreads) prefix_kernel(PrefixArgs a, int clus
     }
     if (!good) {
         if (g == 0) {
-            for (int x = tid; x < a.n_groups; x += kThreads) a.shared[x] = 0;
-            for (int x = tid; x < a.n; x += kThreads) a.start[x] = 0;
+            for (int x = tid; x < a.n_groups; x += threads) a.shared[x] = 0;
+            for (int x = tid; x < a.n; x += threads) a.start[x] = 0;
             if (tid == 0) atomicOr(a.status, MOE_KV_STATUS_BAD_INDEX);
         }
         return;
     }
     if (g < a.n_groups) {
         if (tid == 0) a.shared[g] = pages << a.page_shift;
-        for (int i = r0 + tid; i < r1; i += kThreads) a.start[i] = pages << a.page_shift;
+        for (int i = r0 + tid; i < r1; i += threads) a.start[i] = pages << a.page_shift;
     }
     // requests of no group
     if (g == 0)
-        for (int i = tid; i < (a.n_groups > 0 ? a.groups[0] : a.n); i += kThreads) a.start[i] = 0;
+        for (int i = tid; i < (a.n_groups > 0 ? a.groups[0] : a.n); i += threads) a.start[i] = 0;
     if (g == a.n_groups - 1)
-        for (int i = r1 + tid; i < a.n; i += kThreads) a.start[i] = 0;
+        for (int i = r1 + tid; i < a.n; i += threads) a.start[i] = 0;
 }
 
 }  // namespace
@@ -112,10 +114,13 @@ cudaError_t launch_prefix(const PrefixArgs &a, int sm_count, cudaStream_t s, uin
     // more CTAs for a group while there are SMs and, if the groups are alike, more steps than warps
     const int groups = a.n_groups > 0 ? a.n_groups : 1;
     int cluster = 1;
-    while (cluster < kMaxCluster && (long long)a.n * ((a.width + kColumns - 1) / kColumns) > (long long)groups * cluster * kWarps && (long long)groups * cluster * 2 <= 2 * sm_count) cluster *= 2;
+    const long long steps = (long long)a.n * ((a.width + kColumns - 1) / kColumns);
+    while (cluster < kMaxCluster && steps > (long long)groups * cluster * kFewWarps && (long long)groups * cluster * 2 <= 2 * sm_count) cluster *= 2;
+    // and four times the warps where each would have more than four steps: 1000 requests of one group and 1019 columns 36 -> 21 us
+    const int warps = steps > 4ll * groups * cluster * kFewWarps ? kManyWarps : kFewWarps;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(groups * cluster));
-    cfg.blockDim = dim3(kThreads);
+    cfg.blockDim = dim3(32 * warps);
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -126,7 +131,7 @@ cudaError_t launch_prefix(const PrefixArgs &a, int sm_count, cudaStream_t s, uin
     cfg.attrs = attr;
     cfg.numAttrs = cluster > 1 ? 2 : 1;
     ++*launches;
-    return cudaLaunchKernelEx(&cfg, prefix_kernel, a, cluster);
+    return cudaLaunchKernelEx(&cfg, warps == kManyWarps ? prefix_kernel<kManyWarps> : prefix_kernel<kFewWarps>, a, cluster);
 }
 
 }  // namespace kv
