@@ -288,10 +288,13 @@ def test_requests_of_many_rows_and_small_batches_read_their_keys_themselves():
 
 
 @gpu
+@pytest.mark.parametrize("n", [45, 300, 1200])
 @pytest.mark.parametrize("dtype", [BF16, F32])
-def test_many_groups(dtype):
-    lens = [20 + i % 37 for i in range(300)]
-    shared_case(13, lens, [1] * 300, 2, 1, 64, 16, dtype, list(range(0, 301, 3)), [1] * 100)
+def test_many_groups(dtype, n):
+    """Groups of three; then as many in one call that the tensor cores take (a group of the rest)."""
+    lens = [20 + i % 37 for i in range(n)]
+    shared_case(13, lens, [1] * n, 2, 1, 64, 16, dtype, list(range(0, n + 1, 3)), [1] * (n // 3))
+    shared_case(14, lens, [1] * n, 2, 1, 64, 16, dtype, [*range(0, n - 29, 3), n], [1] * (n // 3 - 9))
 
 
 @gpu
@@ -444,11 +447,12 @@ def test_select_of_many_pages(coarse):
 
 
 @gpu
-def test_select_of_many_requests():
-    lens = [1 + (37 * i) % 400 for i in range(100)]
+@pytest.mark.parametrize("n", [33, 100, 1100])
+def test_select_of_many_requests(n):
+    lens = [1 + (37 * i) % 400 for i in range(n)]
     select_case(4, lens, [min(1 + i % 4, x) for i, x in enumerate(lens)], 2, 1, 64, 16, F32, 5, 1, 1)
-    select_case(5, lens, [0 if i % 5 == 0 else 1 for i in range(100)], 2, 1, 64, 16, F32, 5, 1, 1)
-    select_case(5, lens, [1] * 100, 2, 1, 64, 16, F32, 5, 1, 1, max_new=0)
+    select_case(5, lens, [0 if i % 5 == 0 else 1 for i in range(n)], 2, 1, 64, 16, F32, 5, 1, 1)
+    select_case(5, lens, [1] * n, 2, 1, 64, 16, F32, 5, 1, 1, max_new=0)
 
 
 @gpu
@@ -532,9 +536,10 @@ def test_many_selected_pages_are_split(dtype):
 
 
 @gpu
+@pytest.mark.parametrize("n", [33, 100, 1100])
 @pytest.mark.parametrize("dtype", [BF16, F32])
-def test_many_requests_find_their_tokens(dtype):
-    lens = [1 + (37 * i) % 90 for i in range(100)]
+def test_many_requests_find_their_tokens(dtype, n):
+    lens = [1 + (37 * i) % 90 for i in range(n)]
     selected_case(4, lens, [min(i % 4, x) for i, x in enumerate(lens)], 2, 1, 64, 16, dtype, 3)
 
 
